@@ -381,11 +381,11 @@ def work(case):
     if case["kind"] == "verify":
         es = 2 if case["dtype"] == "bf16" else 4
         # rows after a sequence's first refusal need not be read: the expected number of the others,
-        # by the rate at which a drafted token is accepted
+        # by the rate at which a drafted token is accepted (the noise is felt in the rows without a likely token)
         if case["draft"] == "logits" and case["temp"] > 0:
-            alpha = 1.0 - math.erf(case["noise"] / 2.0 / math.sqrt(2.0))
+            alpha = 1.0 - 0.6 * math.erf(case["noise"] / 2.0 / math.sqrt(2.0))
         else:
-            alpha = 0.4
+            alpha = 0.35
         K = _counts(case)
         tested = sum(float((1 - alpha ** k) / (1 - alpha)) for k in K)
         rows = tested + sum(alpha ** int(k) for k in K)
