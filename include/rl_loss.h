@@ -586,6 +586,55 @@ rl_status rl_prefix_tree_build_batch(int32_t n_rollouts, const int64_t* prompt_o
                                      int64_t* leaf_offsets_out, rl_tree_stats* stats_out,
                                      int64_t* rollout_offsets_out, int64_t* n_tokens_out);
 
+/*
+ * Orthogonalised update of weight matrices (no counterpart in the paper: the optimiser that takes the
+ * gradients which the policy loss produces, Sec. 2.3): momentum, Newton-Schulz products, and the step
+ * on the weights, for a batch of matrices of one shape. Per matrix G [m x n]:
+ *
+ *   buf = momentum buf + G;   U = G + momentum buf (nesterov) or buf;   U = G with momentum == 0
+ *   X = U / (|U|_F + eps)
+ *   ns_steps times:  A = X X^T,  X = a X + (b A + c A A) X   (on the transpose if m > n)
+ *   update       = bf16(update_scale X)
+ *   weights      = (1 - lr weight_decay) weights - lr update_scale X;   weights_bf16 = bf16(weights)
+ */
+typedef struct rl_muon_params {
+  float lr;
+  float momentum;      /* in [0, 1); 0: none, the momentum buffer is not touched */
+  int32_t nesterov;    /* U = G + momentum buf instead of buf */
+  float weight_decay;
+  float update_scale;  /* s; 0.2 sqrt(max(m, n)) gives updates of the size of AdamW's */
+  int32_t ns_steps;    /* 1 .. 16 */
+  float ns_coef[3];    /* a, b, c, each at most 8 in magnitude; a x + b x^3 + c x^5 is to map [0, 1.25]
+                          into itself (3.4445, -4.7750, 2.0315 does) */
+  float eps;           /* >= 0 */
+} rl_muon_params;
+
+/* Workspace bytes of rl_muon_update on `batch` matrices [m x n] (0 for sizes that it refuses). With s
+ * the shorter and l the longer side, about 8 s l + 4 s^2 bytes per matrix. */
+size_t rl_muon_workspace_size(int32_t batch, int64_t m, int64_t n);
+
+/*
+ *   batch, m, n    matrices and their sizes (any of them 0: nothing is done); the shorter side at most
+ *                  32,768, the longer one 2^24, batch x the shorter side (rounded up to 128) 2^24
+ *   grad           [batch] matrices of grad_dtype: row r of matrix b at element b stride_grad + r ld_grad
+ *                  (ld_grad >= n, stride_grad >= 0)
+ *   momentum       float [batch x m x n], updated in place; may be NULL with params->momentum == 0
+ *   weights        float, row r of matrix b at element b stride_w + r ld_w, updated in place, or NULL
+ *   weights_bf16   bf16 at the same places, written, or NULL: the copy that the next forward pass reads
+ *   update         bf16 [batch x m x n], written, or NULL; update or weights is needed
+ *   ws, ws_bytes   rl_muon_workspace_size(...) bytes, initialised by rl_workspace_init
+ *
+ * The products run on the tensor cores with fp16 operands and fp32 accumulation; X and the diagonals of
+ * A and b A + c A A are held in fp32. The result is within about 1e-3 of the exact X in 2-norm, less
+ * than its rounding to bf16 costs (1.7e-3). A zero matrix gives X = 0. A gradient or buffer with a NaN
+ * or an infinity makes its whole matrix's results NaN and sets RL_DEV_BAD_VALUE. Results do not depend
+ * on the schedule: repeated calls give the same bits.
+ */
+rl_status rl_muon_update(int32_t batch, int64_t m, int64_t n, const void* grad, rl_dtype grad_dtype,
+                         int64_t ld_grad, int64_t stride_grad, float* momentum, float* weights,
+                         uint16_t* weights_bf16, int64_t ld_w, int64_t stride_w, uint16_t* update,
+                         const rl_muon_params* params, void* ws, size_t ws_bytes, rl_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

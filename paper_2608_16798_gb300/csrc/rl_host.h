@@ -30,6 +30,8 @@ constexpr size_t kWsHeadCounterOffset = 24;
 // header's end).
 constexpr size_t kWsSummaryDoneOffset = 28;
 constexpr size_t kWsSummaryOffset = 32;
+// The orthogonalised update's finished CTAs of its norm pass.
+constexpr size_t kWsMuonDoneOffset = 8;
 
 rl_status set_error(rl_status st, const std::string& msg);
 rl_status cuda_error(cudaError_t e, const char* what);

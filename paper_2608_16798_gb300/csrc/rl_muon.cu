@@ -1,0 +1,918 @@
+// The orthogonalised update: momentum, Newton-Schulz products on the tensor cores (tcgen05), and
+// the step on the weights.
+//
+//   buf = mu buf + g,  u = g + mu buf (Nesterov) or buf (or g without momentum)
+//   X = u / (|u|_F + eps)          [s x l], the shorter side of the matrix first
+//   per step:  A = X X^T,  B = b A + c A^2,  X <- a X + B X
+//
+// which sends every singular value x of X through a x + b x^3 + c x^5, towards 1.
+//
+// Precision. The products read fp16 operands (11 significant bits; all magnitudes are known:
+// singular values stay below 1.25, so X, A and B are scaled by powers of two into fp16's range) and
+// accumulate in fp32. What a rounding of these operands would put into the result is kept out of it
+// in two ways. X itself is held in fp32 and enters a X unrounded: early steps only multiply small
+// singular values by a, and an fp16 X there would drown them in the rounding of the large ones
+// (simulated on a rank-16 signal over 1% noise: 2e-2 of the result against 3e-4). And the diagonals
+// of A and B, an order larger than the rest once the singular values are near 1, are held in fp32
+// and taken out of the products:
+//   A = D + Ao:  (A^2)_ij = (Ao Ao)_ij + (d_i + d_j) Ao_ij, i != j;  (A^2)_ii = d_i^2 + (Ao Ao)_ii
+//   B = E + Bo:  X <- (a + e_i) X_i + Bo X
+// which halves what is left: 2e-4 to 1e-3 of the result in 2-norm, below the 1.7e-3 of its rounding
+// to bf16.
+#include <cuda.h>
+#include <cuda_fp16.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <map>
+#include <mutex>
+#include <utility>
+
+#include "rl_device.cuh"
+#include "rl_host.h"
+#include "rl_tc.cuh"
+#include "rl_tmap.h"
+
+namespace rl {
+namespace muon {
+
+constexpr int kSMs = 152;
+constexpr float kXScale = 4096.f;  // X in fp16: elements below 1.25 * 2^12
+constexpr float kAScale = 4096.f;  // A off its diagonal: below 1.6 * 2^12
+constexpr float kBScale = 1024.f;  // B off its diagonal: below 31 * 2^10 for coefficients up to 8
+
+__host__ __device__ inline int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+
+// ---------------------------------------------------------------- layouts
+//
+// X (fp32) lies in blocks of 32 x 32: block (R, C) of a matrix at (R * l32 + C) * 1024, and in a
+// block element (r, c) at (c / 4) * 128 + r * 4 + c % 4, so that a warp whose lanes hold one row each
+// moves 512 contiguous bytes per instruction. The fp16 operands are row-major, as TMA reads them.
+
+struct Shape {
+  int32_t batch, m, n;   // the caller's matrices
+  int32_t s, l;          // the shorter and the longer side
+  int32_t sp, lp;        // padded with zeros: sp to 128, lp to 64
+  int32_t tall;          // m > n: X is the transpose of the caller's matrix
+};
+
+__device__ __forceinline__ float* x_block(float* x, const Shape& sh, int b, int R, int C) {
+  return x + ((static_cast<int64_t>(b) * (sh.sp >> 5) + R) * (sh.lp >> 5) + C) * 1024;
+}
+
+__device__ __forceinline__ void load_block_row(const float* blk, int lane, float (&v)[32]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const float4 t = *reinterpret_cast<const float4*>(blk + j * 128 + lane * 4);
+    v[4 * j] = t.x;
+    v[4 * j + 1] = t.y;
+    v[4 * j + 2] = t.z;
+    v[4 * j + 3] = t.w;
+  }
+}
+__device__ __forceinline__ void store_block_row(float* blk, int lane, const float (&v)[32]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    *reinterpret_cast<float4*>(blk + j * 128 + lane * 4) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+}
+
+__device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  uint32_t r;
+  memcpy(&r, &h, 4);
+  return r;
+}
+__device__ __forceinline__ float2 unpack_half2(uint32_t w) {
+  __half2 h;
+  memcpy(&h, &w, 4);
+  return __half22float2(h);
+}
+
+// 32 values of one row as fp16 (64 contiguous, 16-byte aligned bytes).
+__device__ __forceinline__ void store_half_row(uint16_t* to, const float (&v)[32]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    *reinterpret_cast<uint4*>(to + 8 * j) =
+        make_uint4(pack_half2(v[8 * j], v[8 * j + 1]), pack_half2(v[8 * j + 2], v[8 * j + 3]),
+                   pack_half2(v[8 * j + 4], v[8 * j + 5]), pack_half2(v[8 * j + 6], v[8 * j + 7]));
+}
+
+// A 32 x 32 block of a symmetric matrix [sp x sp] in fp16, lane l holding row r0 + l of it, at
+// (r0, c0) and, mirrored, at (c0, r0). Mirrored rows leave in pairs: lanes 2k and 2k + 1 exchange one
+// of every two columns, so that each stores two neighbouring rows' values of one column.
+__device__ __forceinline__ void store_symmetric(uint16_t* m, int sp, int r0, int c0, int lane, const float (&v)[32],
+                                                bool mirror) {
+  store_half_row(m + static_cast<int64_t>(r0 + lane) * sp + c0, v);
+  if (!mirror) return;
+  const int odd = lane & 1;
+#pragma unroll
+  for (int j = 0; j < 32; j += 2) {
+    const float got = __shfl_xor_sync(0xffffffffu, odd ? v[j] : v[j + 1], 1);
+    const uint32_t w = odd ? pack_half2(got, v[j + 1]) : pack_half2(v[j], got);
+    *reinterpret_cast<uint32_t*>(m + static_cast<int64_t>(c0 + j + odd) * sp + r0 + (lane & ~1)) = w;
+  }
+}
+
+__device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void pdl_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+// ---------------------------------------------------------------- momentum and norm
+
+struct PrepArgs {
+  Shape sh;
+  const void* grad;
+  int64_t ld_grad, stride_grad;
+  int32_t grad_bf16;
+  float* momentum;       // [batch x m x n] or null
+  float mu;
+  int32_t nesterov;
+  float eps;
+  float* x;              // u, then X
+  uint16_t* x16;
+  double* partial;       // [batch][parts]: sums of squares
+  int32_t parts;
+  float* inv;            // [batch]: 1 / (|u| + eps)
+  uint32_t* done;        // finished CTAs (zero at launch, set back by the last)
+  int32_t* status;
+};
+
+__device__ __forceinline__ float grad_at(const PrepArgs& p, int64_t i) {
+  return p.grad_bf16 ? bf16_to_f32(static_cast<const uint16_t*>(p.grad)[i]) : static_cast<const float*>(p.grad)[i];
+}
+
+// The sum of the squares of 32 values as a double, without fp32 overflow or underflow: the values are
+// scaled by the power of two that brings the largest to [1, 2).
+__device__ __forceinline__ double sum_squares(const float (&v)[32]) {
+  float top = 0.f;
+#pragma unroll
+  for (int j = 0; j < 32; ++j) top = max_nan(top, fabsf(v[j]));
+  const uint32_t e = __float_as_uint(top) >> 23;
+  if (top == 0.f) return 0.0;
+  if (e == 255u) return static_cast<double>(top) * static_cast<double>(top);  // infinite or NaN
+  // 2^(127 - e) and what is left of it for subnormals, in two factors that are both normal
+  const int k = 127 - static_cast<int>(e == 0 ? 1 : e);
+  const float f1 = __uint_as_float(static_cast<uint32_t>(127 + k / 2) << 23);
+  const float f2 = __uint_as_float(static_cast<uint32_t>(127 + (k - k / 2)) << 23);
+  float ss = 0.f;
+#pragma unroll
+  for (int j = 0; j < 32; ++j) {
+    const float y = v[j] * f1 * f2;
+    ss = fmaf(y, y, ss);
+  }
+  return static_cast<double>(ss) * __hiloint2double((1023 - 2 * k) << 20, 0);
+}
+
+constexpr int kPrepWarps = 8;
+
+// u and its sum of squares. A warp forms one 32 x 32 block of X; a CTA's warps take eight blocks that
+// lie side by side in the caller's rows.
+__global__ void __launch_bounds__(kPrepWarps * 32) momentum_kernel(const PrepArgs p) {
+  __shared__ float tile[kPrepWarps][32][33];
+  __shared__ double sums[kPrepWarps];
+  __shared__ bool last;
+  const Shape& sh = p.sh;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int nR = sh.sp >> 5, nC = sh.lp >> 5;
+  pdl_launch();
+  pdl_wait();
+  // which block: along the caller's rows first
+  const int along = sh.tall ? nR : nC, across = sh.tall ? nC : nR;
+  const int groups = (along + kPrepWarps - 1) / kPrepWarps;
+  const int64_t cta = blockIdx.x;
+  const int b = static_cast<int>(cta / (static_cast<int64_t>(groups) * across));
+  const int rest = static_cast<int>(cta % (static_cast<int64_t>(groups) * across));
+  const int a_blk = rest % groups * kPrepWarps + warp, x_blk = rest / groups;
+  double mine = 0.0;
+  if (a_blk < along) {
+    const int R = sh.tall ? a_blk : x_blk, C = sh.tall ? x_blk : a_blk;
+    // rows and columns of the caller's matrix: lane walks its row
+    const int c = a_blk * 32 + lane, r0 = x_blk * 32;
+    const int64_t g0 = b * p.stride_grad + c, m0 = static_cast<int64_t>(b) * sh.m * sh.n + c;
+    float v[32];
+#pragma unroll
+    for (int j = 0; j < 32; ++j) {
+      const int r = r0 + j;
+      float u = 0.f;
+      if (r < sh.m && c < sh.n) {
+        const float g = grad_at(p, g0 + r * p.ld_grad);
+        u = g;
+        if (p.momentum) {
+          float* at = p.momentum + m0 + static_cast<int64_t>(r) * sh.n;
+          const float buf = fmaf(p.mu, *at, g);
+          *at = buf;
+          u = p.nesterov ? fmaf(p.mu, buf, g) : buf;
+        }
+      }
+      if (sh.tall) v[j] = u;
+      else tile[warp][j][lane] = u;
+    }
+    if (!sh.tall) {
+      __syncwarp();
+#pragma unroll
+      for (int j = 0; j < 32; ++j) v[j] = tile[warp][lane][j];
+    }
+    store_block_row(x_block(p.x, sh, b, R, C), lane, v);
+    mine = warp_sum(sum_squares(v));
+  }
+  if (lane == 0) sums[warp] = mine;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    double s = 0.0;
+    for (int w = 0; w < kPrepWarps; ++w) s += sums[w];
+    p.partial[static_cast<int64_t>(b) * p.parts + rest] = s;
+    __threadfence();
+    last = atomicAdd(p.done, 1u) == gridDim.x - 1;
+    if (last) __threadfence();
+  }
+  __syncthreads();
+  if (!last) return;
+  // the last CTA: one warp per matrix adds its partial sums in a fixed order
+  for (int k = warp; k < sh.batch; k += kPrepWarps) {
+    double s = 0.0;
+    for (int i = lane; i < p.parts; i += 32) s += __ldcg(p.partial + static_cast<int64_t>(k) * p.parts + i);
+    s = warp_sum(s);
+    if (lane == 0) {
+      if (!(s <= 1.7e308)) flag_status(p.status, RL_DEV_BAD_VALUE);
+      p.inv[k] = static_cast<float>(1.0 / (sqrt(s) + static_cast<double>(p.eps)));
+    }
+  }
+  if (threadIdx.x == 0) *p.done = 0;
+}
+
+// X in fp16 for the first product.
+__global__ void __launch_bounds__(kPrepWarps * 32) normalise_kernel(const PrepArgs p) {
+  const Shape& sh = p.sh;
+  const int lane = threadIdx.x & 31;
+  const int nR = sh.sp >> 5, nC = sh.lp >> 5;
+  pdl_launch();
+  pdl_wait();
+  const int64_t blk = static_cast<int64_t>(blockIdx.x) * kPrepWarps + (threadIdx.x >> 5);
+  const int64_t per = static_cast<int64_t>(nR) * nC;
+  if (blk >= per * sh.batch) return;
+  const int b = static_cast<int>(blk / per);
+  const int R = static_cast<int>(blk % per) / nC, C = static_cast<int>(blk % per) % nC;
+  float v[32];
+  load_block_row(x_block(p.x, sh, b, R, C), lane, v);
+  const float f = p.inv[b];
+#pragma unroll
+  for (int j = 0; j < 32; ++j) v[j] = v[j] * f * kXScale;
+  store_half_row(p.x16 + (static_cast<int64_t>(b) * sh.sp + R * 32 + lane) * sh.lp + C * 32, v);
+}
+
+// ---------------------------------------------------------------- the products
+
+enum Mode { GRAM = 0, POLY = 1, APPLY = 2 };
+
+struct MmArgs {
+  Shape sh;
+  int32_t nt_m, nt_n;    // tiles of the product's rows and columns (GRAM, POLY: of both)
+  int32_t per;           // tiles of one matrix (GRAM, POLY: on and above the diagonal)
+  int32_t nkb;           // 64-element blocks of the contraction
+  int32_t splits;        // GRAM: parts of the contraction, each an item
+  float ca, cb, cc;      // the step's coefficients
+  uint16_t* a16;
+  uint16_t* b16;
+  float* d;              // [batch x sp] the diagonal of A
+  float* e;              // [batch x sp] a + the diagonal of B
+  float* x;
+  uint16_t* x16_out;
+  const float* inv;      // first step: X is still u, to be multiplied by this
+  float* parts;          // GRAM with splits > 1: [split][tile][TILE x TILE] sums
+  // the last step's outputs
+  int32_t final_step;
+  float scale;           // of the update
+  uint16_t* update;      // bf16 [batch x m x n] or null
+  float* weights;
+  uint16_t* weights_bf16;
+  int64_t ld_w, stride_w;
+  float decay, step;     // w <- decay w - step O
+  int32_t* status;
+};
+
+constexpr int BK = 64;
+constexpr uint32_t A_BYTES = 128 * BK * 2;
+constexpr uint32_t STAGE_BYTES = 2 * A_BYTES;
+constexpr uint32_t HALF_BYTES = 64 * BK * 2;
+constexpr int NS = 6;
+constexpr int kThreads = 192;  // warp 0 TMA, warp 1 MMA, warps 2-5 epilogue
+constexpr size_t kSmem = NS * STAGE_BYTES + 4 * 32 * 33 * 4 + 1024;
+static_assert(kSmem <= 232448 - 1024, "shared memory of the product kernels");
+
+// fp16 operands, fp32 accumulator, M x N; B MN-major for APPLY.
+constexpr uint32_t idesc_f16(int M, int N, bool b_mn) {
+  return (1u << 4) | (b_mn ? (1u << 16) : 0u) | (static_cast<uint32_t>(N >> 3) << 17) |
+         (static_cast<uint32_t>(M >> 4) << 24);
+}
+
+// Tile t of those on and above the diagonal: column by column.
+__device__ __forceinline__ void triangle(int t, int& i, int& j) {
+  j = static_cast<int>((sqrtf(8.f * t + 1.f) - 1.f) * 0.5f);
+  while (j * (j + 1) / 2 > t) --j;
+  while ((j + 1) * (j + 2) / 2 <= t) ++j;
+  i = t - j * (j + 1) / 2;
+}
+
+// What becomes of a 32 x 32 block (lane: row) of X X^T, scaled by 2^24.
+__device__ __forceinline__ void gram_out(const MmArgs& p, int b, int r0, int c0, int lane, float (&v)[32]) {
+  const int sp = p.sh.sp;
+#pragma unroll
+  for (int j = 0; j < 32; ++j) {
+    v[j] *= kAScale / (kXScale * kXScale);
+    if (c0 + j == r0 + lane) {
+      p.d[static_cast<int64_t>(b) * sp + r0 + lane] = v[j] * (1.f / kAScale);
+      v[j] = 0.f;
+    }
+  }
+  store_symmetric(p.a16 + static_cast<int64_t>(b) * sp * sp, sp, r0, c0, lane, v, r0 != c0);
+}
+
+// The same of Ao Ao, scaled by 2^24.
+__device__ __forceinline__ void poly_out(const MmArgs& p, int b, int r0, int c0, int lane, float (&v)[32]) {
+  const int sp = p.sh.sp;
+  const int64_t at = static_cast<int64_t>(b) * sp;
+  const float* d = p.d + at;
+  const float di = d[r0 + lane], dj = d[c0 + lane];
+  const uint4* a = reinterpret_cast<const uint4*>(p.a16 + (at + r0 + lane) * sp + c0);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const uint4 w = a[k];
+    const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+      const float2 ao = unpack_half2(ww[h]);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int j = 8 * k + 2 * h + i;
+        const float x = (i ? ao.y : ao.x) * (1.f / kAScale);
+        const float dc = __shfl_sync(0xffffffffu, dj, j);
+        const float sq = v[j] * (1.f / (kAScale * kAScale));
+        if (c0 + j == r0 + lane) {
+          p.e[at + r0 + lane] = p.ca + fmaf(p.cb, di, p.cc * fmaf(di, di, sq));
+          v[j] = 0.f;
+        } else {
+          v[j] = kBScale * fmaf(p.cb, x, p.cc * fmaf(di + dc, x, sq));
+        }
+      }
+    }
+  }
+  store_symmetric(p.b16 + at * sp, sp, r0, c0, lane, v, r0 != c0);
+}
+
+// The step's new X: kept, or in the last step the caller's outputs.
+__device__ __forceinline__ void apply_out(const MmArgs& p, int b, int r0, int c0, int lane, float (&v)[32],
+                                          float (*tile)[33]) {
+  const Shape& sh = p.sh;
+  float* blk = x_block(p.x, sh, b, r0 >> 5, c0 >> 5);
+  float x[32];
+  load_block_row(blk, lane, x);
+  float f = p.e[static_cast<int64_t>(b) * sh.sp + r0 + lane];
+  if (p.inv) f *= p.inv[b];
+#pragma unroll
+  for (int j = 0; j < 32; ++j) v[j] = fmaf(f, x[j], v[j] * (1.f / (kBScale * kXScale)));
+  if (!p.final_step) {
+    store_block_row(blk, lane, v);
+#pragma unroll
+    for (int j = 0; j < 32; ++j) v[j] *= kXScale;
+    store_half_row(p.x16_out + (static_cast<int64_t>(b) * sh.sp + r0 + lane) * sh.lp + c0, v);
+    return;
+  }
+  // lanes walk the caller's rows
+  if (!sh.tall) {
+    __syncwarp();
+#pragma unroll
+    for (int j = 0; j < 32; ++j) tile[lane][j] = v[j];
+    __syncwarp();
+#pragma unroll
+    for (int j = 0; j < 32; ++j) v[j] = tile[j][lane];
+  }
+  const int col = (sh.tall ? r0 : c0) + lane, row0 = sh.tall ? c0 : r0;
+  if (col >= sh.n) return;
+#pragma unroll
+  for (int j = 0; j < 32; ++j) {
+    const int row = row0 + j;
+    if (row < sh.m) {
+      if (p.update)
+        p.update[(static_cast<int64_t>(b) * sh.m + row) * sh.n + col] = f32_to_bf16(v[j] * p.scale);
+      if (p.weights) {
+        const int64_t at = b * p.stride_w + row * p.ld_w + col;
+        const float w = fmaf(-p.step, v[j], p.decay * p.weights[at]);
+        p.weights[at] = w;
+        if (p.weights_bf16) p.weights_bf16[at] = f32_to_bf16(w);
+      }
+    }
+  }
+}
+
+// One product, persistent: CTAs (CG = 1) or CTA pairs (CG = 2) take square tiles of 128 CG in turn.
+// Per stage of 64 along the contraction a CTA holds 128 rows of the left operand and 128 of the right
+// one's (of a pair's 256). Two accumulators in TMEM, so that the epilogue of one tile runs under the
+// products of the next.
+template <int MODE, int CG>
+__global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_constant__ CUtensorMap tmA,
+                                                              const __grid_constant__ CUtensorMap tmB, const MmArgs p) {
+  constexpr int TILE = 128 * CG;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ __align__(8) uint64_t full[NS], empty[NS], accf[2], acce[2];
+  __shared__ uint32_t tbase;
+  uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = CG == 2 ? cluster_ctarank() : 0;
+  const int unit = blockIdx.x / CG, units = gridDim.x / CG;
+  const int n_tiles = p.sh.batch * p.per;
+  const int n_items = n_tiles * (MODE == GRAM ? p.splits : 1);
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < NS; ++s) {
+      mbar_init(&full[s], 1);
+      mbar_init(&empty[s], 1);
+    }
+    for (int k = 0; k < 2; ++k) {
+      mbar_init(&accf[k], 1);
+      mbar_init(&acce[k], 4 * CG);
+    }
+    fence_mbar_init();
+  }
+  if (warp == 1) {
+    if (CG == 2) tc::tmem_alloc_pair(&tbase, 2 * TILE);
+    else tc::tmem_alloc(&tbase, 2 * TILE);
+  }
+  tc::fence_before_sync();
+  if (CG == 2) cluster_sync_all();
+  else __syncthreads();
+  tc::fence_after_sync();
+  const uint32_t tmem = tbase;
+  pdl_launch();
+  pdl_wait();
+
+  // item -> matrix, tile row and column, K blocks
+  auto decode = [&](int item, int& b, int& ti, int& tj, int& kb0, int& nkb) {
+    int part = 0;
+    if (MODE == GRAM && p.splits > 1) {
+      part = item / n_tiles;
+      item -= part * n_tiles;
+    }
+    b = item / p.per;
+    const int t = item - b * p.per;
+    if (MODE == APPLY) {
+      ti = t % p.nt_m;
+      tj = t / p.nt_m;
+    } else {
+      triangle(t, ti, tj);
+    }
+    kb0 = MODE == GRAM ? static_cast<int>(static_cast<int64_t>(part) * p.nkb / p.splits) : 0;
+    nkb = (MODE == GRAM ? static_cast<int>(static_cast<int64_t>(part + 1) * p.nkb / p.splits) : p.nkb) - kb0;
+  };
+
+  if (warp == 0) {
+    if (lane == 0) {
+      // the launch before wrote the operands through the generic proxy; TMA reads them
+      asm volatile("fence.proxy.async.global;" ::: "memory");
+      uint32_t g = 0;
+      bool ok = true;
+      for (int item = unit; item < n_items && ok; item += units) {
+        int b, ti, tj, kb0, nkb;
+        decode(item, b, ti, tj, kb0, nkb);
+        const int m0 = b * p.sh.sp + ti * TILE + static_cast<int>(rank) * 128;
+        const int n0 = tj * TILE + static_cast<int>(rank) * 128;
+        for (int kb = 0; kb < nkb; ++kb, ++g) {
+          const int s = g % NS;
+          const int k0 = (kb0 + kb) * BK;
+          const uint32_t use = g / NS;
+          if (use > 0 && !mbar_wait_bounded(&empty[s], (use - 1) & 1)) {
+            flag_status(p.status, RL_DEV_TIMEOUT);
+            ok = false;
+            break;
+          }
+          uint8_t* st = sm + s * STAGE_BYTES;
+          if (rank == 0) mbar_arrive_expect_tx(&full[s], CG * STAGE_BYTES);
+          if (CG == 2) {
+            const uint32_t bar = map_to_rank(smem_addr(&full[s]), 0);
+            tc::tma_load_2d_pair(st, &tmA, k0, m0, bar);
+            if (MODE == APPLY) {
+              tc::tma_load_2d_pair(st + A_BYTES, &tmB, n0, b * p.sh.sp + k0, bar);
+              tc::tma_load_2d_pair(st + A_BYTES + HALF_BYTES, &tmB, n0 + 64, b * p.sh.sp + k0, bar);
+            } else {
+              tc::tma_load_2d_pair(st + A_BYTES, &tmB, k0, b * p.sh.sp + n0, bar);
+            }
+          } else {
+            tc::tma_load_2d(st, &tmA, k0, m0, &full[s]);
+            if (MODE == APPLY) {
+              tc::tma_load_2d(st + A_BYTES, &tmB, n0, b * p.sh.sp + k0, &full[s]);
+              tc::tma_load_2d(st + A_BYTES + HALF_BYTES, &tmB, n0 + 64, b * p.sh.sp + k0, &full[s]);
+            } else {
+              tc::tma_load_2d(st + A_BYTES, &tmB, k0, b * p.sh.sp + n0, &full[s]);
+            }
+          }
+        }
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0 && rank == 0) {
+      constexpr uint32_t idesc = idesc_f16(TILE, TILE, MODE == APPLY);
+      uint32_t g = 0;
+      bool ok = true;
+      uint32_t t = 0;
+      for (int item = unit; item < n_items && ok; item += units, ++t) {
+        int b, ti, tj, kb0, nkb;
+        decode(item, b, ti, tj, kb0, nkb);
+        const uint32_t buf = t & 1;
+        if (t >= 2) {
+          const bool got = CG == 2 ? mbar_wait_cluster_bounded(&acce[buf], ((t >> 1) - 1) & 1)
+                                   : mbar_wait_bounded(&acce[buf], ((t >> 1) - 1) & 1);
+          if (!got) {
+            flag_status(p.status, RL_DEV_TIMEOUT);
+            break;
+          }
+        }
+        tc::fence_after_sync();
+        const uint32_t acc = tmem + buf * TILE;
+        for (int kb = 0; kb < nkb; ++kb, ++g) {
+          const int s = g % NS;
+          if (!mbar_wait_bounded(&full[s], (g / NS) & 1)) {
+            flag_status(p.status, RL_DEV_TIMEOUT);
+            ok = false;
+            break;
+          }
+          tc::fence_after_sync();
+          const uint32_t a = smem_addr(sm + s * STAGE_BYTES), bb = a + A_BYTES;
+#pragma unroll
+          for (int k = 0; k < BK / 16; ++k) {
+            const uint64_t ad = tc::desc_kmajor_sw128(a + k * 32);
+            const uint64_t bd = MODE == APPLY ? tc::desc_mnmajor_sw128(bb + k * 2048, HALF_BYTES, 1024)
+                                              : tc::desc_kmajor_sw128(bb + k * 32);
+            if (CG == 2) tc::mma_bf16_pair(acc, ad, bd, idesc, (kb | k) != 0 ? 1u : 0u);
+            else tc::mma_bf16(acc, ad, bd, idesc, (kb | k) != 0 ? 1u : 0u);
+          }
+          if (CG == 2) tc::mma_commit_pair(&empty[s], 0x3);
+          else tc::mma_commit(&empty[s]);
+        }
+        if (!ok) break;
+        if (CG == 2) tc::mma_commit_pair(&accf[buf], 0x3);
+        else tc::mma_commit(&accf[buf]);
+      }
+    }
+  } else {
+    const int q = warp & 3;  // TMEM lane quarter this warp may access
+    float(*tile)[33] = reinterpret_cast<float(*)[33]>(sm + NS * STAGE_BYTES) + (warp - 2) * 32;
+    uint32_t t = 0;
+    for (int item = unit; item < n_items; item += units, ++t) {
+      int b, ti, tj, kb0, nkb;
+      decode(item, b, ti, tj, kb0, nkb);
+      const uint32_t buf = t & 1;
+      if (!mbar_wait_sleep_bounded(&accf[buf], (t >> 1) & 1)) {
+        if (lane == 0) flag_status(p.status, RL_DEV_TIMEOUT);
+        break;
+      }
+      tc::fence_after_sync();
+      const int r0 = ti * TILE + static_cast<int>(rank) * 128 + 32 * q;
+      const uint32_t tq = tmem + buf * TILE + (static_cast<uint32_t>(32 * q) << 16);
+      const int cols = MODE == APPLY ? p.sh.lp : p.sh.sp;
+#pragma unroll 1
+      for (int c = 0; c < TILE / 32; ++c) {
+        float v[32];
+        tc::tmem_ld32(tq + c * 32, v);
+        if (c == TILE / 32 - 1) {
+          tc::fence_before_sync();
+          __syncwarp();
+          if (lane == 0) {
+            if (rank != 0) mbar_arrive_remote(map_to_rank(smem_addr(&acce[buf]), 0));
+            else mbar_arrive(&acce[buf]);
+          }
+        }
+        const int c0 = tj * TILE + c * 32;
+        if (r0 < p.sh.sp && c0 < cols) {  // past the matrix: another one's rows, or nothing
+          if (MODE == GRAM && p.splits > 1) {
+            float* blk = p.parts + static_cast<int64_t>(item) * TILE * TILE +
+                         (static_cast<int64_t>((rank * 4 + q) * (TILE / 32) + c)) * 1024;
+            store_block_row(blk, lane, v);
+          } else if (MODE == APPLY) {
+            apply_out(p, b, r0, c0, lane, v, tile);
+          } else if (c0 >= r0 || ti != tj) {
+            // in a tile on the diagonal the blocks below it are the mirror image of those above
+            if (MODE == GRAM) gram_out(p, b, r0, c0, lane, v);
+            else poly_out(p, b, r0, c0, lane, v);
+          }
+        }
+        __syncwarp();
+      }
+    }
+  }
+  tc::fence_before_sync();
+  if (CG == 2) cluster_sync_all();
+  else __syncthreads();
+  if (warp == 1) {
+    tc::fence_after_sync();
+    if (CG == 2) tc::tmem_dealloc_pair(tmem, 2 * TILE);
+    else tc::tmem_dealloc(tmem, 2 * TILE);
+  }
+}
+
+// A from the parts of its contraction, added in order: one warp per 32 x 32 block.
+template <int CG>
+__global__ void __launch_bounds__(256) gram_sum_kernel(const MmArgs p) {
+  constexpr int TILE = 128 * CG, NB = TILE / 32;
+  const int lane = threadIdx.x & 31;
+  pdl_launch();
+  pdl_wait();
+  const int n_tiles = p.sh.batch * p.per;
+  const int64_t w = static_cast<int64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5);
+  if (w >= static_cast<int64_t>(n_tiles) * NB * NB) return;
+  const int tile = static_cast<int>(w / (NB * NB)), in = static_cast<int>(w % (NB * NB));
+  const int b = tile / p.per;
+  int ti, tj;
+  triangle(tile - b * p.per, ti, tj);
+  const int r0 = ti * TILE + in / NB * 32, c0 = tj * TILE + in % NB * 32;
+  if (r0 >= p.sh.sp || c0 >= p.sh.sp || (ti == tj && c0 < r0)) return;
+  float v[32], t[32];
+  const float* src = p.parts + static_cast<int64_t>(tile) * TILE * TILE + static_cast<int64_t>(in) * 1024;
+  load_block_row(src, lane, v);
+  for (int k = 1; k < p.splits; ++k) {
+    load_block_row(src + static_cast<int64_t>(k) * n_tiles * TILE * TILE, lane, t);
+#pragma unroll
+    for (int j = 0; j < 32; ++j) v[j] += t[j];
+  }
+  gram_out(p, b, r0, c0, lane, v);
+}
+
+// ---------------------------------------------------------------- host
+
+// How the products are cut: the tile (128 or, by CTA pairs, 256) of each, and the parts of the first
+// one's contraction.
+struct Plan {
+  int cg_sym, cg_apply, splits;
+};
+
+inline int64_t tri(int64_t n) { return n * (n + 1) / 2; }
+
+Plan plan_of(int64_t batch, int64_t sp, int64_t lp) {
+  Plan p;
+  auto tiles_sym = [&](int cg) { return batch * tri(round_up(sp, 128 * cg) / (128 * cg)); };
+  p.cg_sym = tiles_sym(2) >= kSMs / 2 ? 2 : 1;
+  p.cg_apply = batch * (round_up(sp, 256) / 256) * (round_up(lp, 256) / 256) >= kSMs / 2 ? 2 : 1;
+  const int64_t units = kSMs / p.cg_sym, tiles = tiles_sym(p.cg_sym);
+  // parts of at least eight K blocks, while the tiles leave units idle
+  p.splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(units / std::max<int64_t>(tiles, 1), lp / BK / 8)));
+  return p;
+}
+
+struct Layout {
+  size_t x, x16a, x16b, a16, b16, d, e, inv, partial, parts, bytes;
+  int32_t n_parts;  // partial sums of squares per matrix
+};
+
+Shape shape_of(int32_t batch, int64_t m, int64_t n) {
+  Shape s;
+  s.batch = batch;
+  s.m = static_cast<int32_t>(m);
+  s.n = static_cast<int32_t>(n);
+  s.s = std::min(s.m, s.n);
+  s.l = std::max(s.m, s.n);
+  s.sp = static_cast<int32_t>(round_up(s.s, 128));
+  s.lp = static_cast<int32_t>(round_up(s.l, 64));
+  s.tall = m > n;
+  return s;
+}
+
+Layout layout_of(const Shape& s) {
+  Layout w;
+  size_t at = kWsHeader;
+  auto take = [&](size_t bytes) {
+    const size_t here = at;
+    at += (bytes + 255) & ~size_t(255);
+    return here;
+  };
+  const size_t B = s.batch, sp = s.sp, lp = s.lp;
+  const int64_t along = (s.tall ? s.sp : s.lp) / 32, across = (s.tall ? s.lp : s.sp) / 32;
+  w.n_parts = static_cast<int32_t>((along + kPrepWarps - 1) / kPrepWarps * across);
+  w.x = take(B * sp * lp * 4);
+  w.x16a = take(B * sp * lp * 2);
+  w.x16b = take(B * sp * lp * 2);
+  w.a16 = take(B * sp * sp * 2);
+  w.b16 = take(B * sp * sp * 2);
+  w.d = take(B * sp * 4);
+  w.e = take(B * sp * 4);
+  w.inv = take(B * 4);
+  w.partial = take(B * w.n_parts * 8);
+  const Plan p = plan_of(s.batch, s.sp, s.lp);
+  const size_t T = 128 * p.cg_sym;
+  w.parts = take(p.splits > 1 ? p.splits * B * tri(round_up(s.sp, T) / T) * T * T * 4 : 0);
+  w.bytes = at;
+  return w;
+}
+
+// Launch with programmatic dependence on the launch before it (its prologue may start early) and, for
+// pairs, a cluster of two.
+template <typename... KArgs, typename... Args>
+rl_status launch(const char* what, void (*kern)(KArgs...), int64_t grid, int threads, size_t smem, int cluster,
+                 cudaStream_t s, const Args&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr[2];
+  cfg.gridDim = dim3(static_cast<unsigned>(grid));
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cfg.attrs = attr;
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.numAttrs = 1;
+  if (cluster > 1) {
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.numAttrs = 2;
+  }
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, args...);
+  return e == cudaSuccess ? RL_OK : cuda_error(e, what);
+}
+
+// Shared memory beyond the default, once per device and kernel.
+template <int MODE, int CG>
+rl_status allow_smem() {
+  static std::mutex mu;
+  static std::map<int, bool> done;
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return cuda_error(e, "cudaGetDevice");
+  std::lock_guard<std::mutex> lock(mu);
+  if (!done[dev]) {
+    e = cudaFuncSetAttribute(product_kernel<MODE, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             static_cast<int>(kSmem));
+    if (e != cudaSuccess) return cuda_error(e, "cudaFuncSetAttribute(product_kernel)");
+    done[dev] = true;
+  }
+  return RL_OK;
+}
+
+template <int MODE, int CG>
+rl_status product(const CUtensorMap& a, const CUtensorMap& b, const MmArgs& p, cudaStream_t s) {
+  rl_status st = allow_smem<MODE, CG>();
+  if (st != RL_OK) return st;
+  const int64_t items = static_cast<int64_t>(p.sh.batch) * p.per * (MODE == GRAM ? p.splits : 1);
+  const int64_t units = std::min<int64_t>(items, kSMs / CG);
+  return launch("product_kernel launch", product_kernel<MODE, CG>, units * CG, kThreads, kSmem, CG, s, a, b, p);
+}
+
+}  // namespace muon
+}  // namespace rl
+
+using namespace rl;
+using namespace rl::muon;
+
+static rl_status muon_check(const char* fn, int32_t batch, int64_t m, int64_t n) {
+  const std::string f = std::string(fn) + ": ";
+  if (batch < 0 || m < 0 || n < 0) return set_error(RL_ERR_INVALID_ARG, f + "negative size");
+  if (std::min(m, n) > 32768 || std::max(m, n) > (int64_t(1) << 24) ||
+      round_up(std::min(m, n), 128) * batch > (int64_t(1) << 24))
+    return set_error(RL_ERR_UNSUPPORTED, f + "the shorter side is at most 32,768, the longer one 2^24, and batch times "
+                                             "the shorter side (rounded up to 128) 2^24");
+  return RL_OK;
+}
+
+extern "C" {
+
+size_t rl_muon_workspace_size(int32_t batch, int64_t m, int64_t n) {
+  clear_error();
+  if (muon_check("rl_muon_workspace_size", batch, m, n) != RL_OK) return 0;
+  if (batch == 0 || m == 0 || n == 0) return kWsHeader;
+  return layout_of(shape_of(batch, m, n)).bytes;
+}
+
+rl_status rl_muon_update(int32_t batch, int64_t m, int64_t n, const void* grad, rl_dtype grad_dtype, int64_t ld_grad,
+                         int64_t stride_grad, float* momentum, float* weights, uint16_t* weights_bf16, int64_t ld_w,
+                         int64_t stride_w, uint16_t* update, const rl_muon_params* params, void* ws, size_t ws_bytes,
+                         rl_stream_t stream) {
+  clear_error();
+  const std::string f = "rl_muon_update: ";
+  rl_status st = muon_check("rl_muon_update", batch, m, n);
+  if (st != RL_OK) return st;
+  if (!params) return set_error(RL_ERR_INVALID_ARG, f + "params is NULL");
+  if (grad_dtype != RL_BF16 && grad_dtype != RL_F32) return set_error(RL_ERR_INVALID_ARG, f + "bad grad_dtype");
+  const rl_muon_params& P = *params;
+  for (int k = 0; k < 3; ++k)
+    if (!(std::fabs(P.ns_coef[k]) <= 8.f))
+      return set_error(RL_ERR_INVALID_ARG, f + "ns_coef must be finite and at most 8 in magnitude");
+  if (P.ns_steps < 1 || P.ns_steps > 16) return set_error(RL_ERR_INVALID_ARG, f + "ns_steps outside [1, 16]");
+  if (!(P.eps >= 0.f) || !std::isfinite(P.eps) || !std::isfinite(P.lr) || !std::isfinite(P.weight_decay) ||
+      !std::isfinite(P.update_scale) || !(P.momentum >= 0.f && P.momentum < 1.f))
+    return set_error(RL_ERR_INVALID_ARG, f + "eps >= 0, momentum in [0, 1) and finite lr, weight_decay, update_scale "
+                                             "are needed");
+  if (batch == 0 || m == 0 || n == 0) return RL_OK;
+  if (!grad || !ws) return set_error(RL_ERR_INVALID_ARG, f + "grad or ws is NULL");
+  if (!weights && !update) return set_error(RL_ERR_INVALID_ARG, f + "neither weights nor update is given");
+  if (weights_bf16 && !weights) return set_error(RL_ERR_INVALID_ARG, f + "weights_bf16 without weights");
+  if (P.momentum > 0.f && !momentum) return set_error(RL_ERR_INVALID_ARG, f + "momentum > 0 without a momentum buffer");
+  if (ld_grad < n || stride_grad < 0) return set_error(RL_ERR_INVALID_ARG, f + "ld_grad < n or stride_grad < 0");
+  if (weights) {
+    const int64_t last = (m - 1) * ld_w + n;  // elements that one matrix spans
+    const bool apart = stride_w >= last || (stride_w >= n && ld_w >= (batch - 1) * stride_w + n);
+    if (ld_w < n || (batch > 1 && !apart))
+      return set_error(RL_ERR_INVALID_ARG, f + "ld_w < n, or the batch's weights overlap");
+  }
+  if (reinterpret_cast<uintptr_t>(ws) % 16 != 0) return set_error(RL_ERR_ALIGNMENT, f + "ws not 16-byte aligned");
+  if ((reinterpret_cast<uintptr_t>(grad) % (grad_dtype == RL_F32 ? 4 : 2)) != 0 ||
+      reinterpret_cast<uintptr_t>(momentum) % 4 != 0 || reinterpret_cast<uintptr_t>(weights) % 4 != 0 ||
+      reinterpret_cast<uintptr_t>(weights_bf16) % 2 != 0 || reinterpret_cast<uintptr_t>(update) % 2 != 0)
+    return set_error(RL_ERR_ALIGNMENT, f + "a pointer is not aligned to its element");
+  const Shape sh = shape_of(batch, m, n);
+  const Layout w = layout_of(sh);
+  if (ws_bytes < w.bytes) return set_error(RL_ERR_WORKSPACE_TOO_SMALL, f + "ws_bytes below rl_muon_workspace_size");
+
+  uint8_t* base = static_cast<uint8_t*>(ws);
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  int32_t* status = reinterpret_cast<int32_t*>(base);
+
+  PrepArgs pa = {};
+  pa.sh = sh;
+  pa.grad = grad;
+  pa.ld_grad = ld_grad;
+  pa.stride_grad = stride_grad;
+  pa.grad_bf16 = grad_dtype == RL_BF16;
+  pa.momentum = P.momentum > 0.f ? momentum : nullptr;
+  pa.mu = P.momentum;
+  pa.nesterov = P.nesterov;
+  pa.eps = P.eps;
+  pa.x = reinterpret_cast<float*>(base + w.x);
+  pa.x16 = reinterpret_cast<uint16_t*>(base + w.x16a);
+  pa.partial = reinterpret_cast<double*>(base + w.partial);
+  pa.parts = w.n_parts;
+  pa.inv = reinterpret_cast<float*>(base + w.inv);
+  pa.done = reinterpret_cast<uint32_t*>(base + kWsMuonDoneOffset);
+  pa.status = status;
+  st = launch("momentum_kernel launch", momentum_kernel, static_cast<int64_t>(batch) * w.n_parts, kPrepWarps * 32, 0, 1,
+              s, pa);
+  if (st != RL_OK) return st;
+  const int64_t blocks = static_cast<int64_t>(batch) * (sh.sp / 32) * (sh.lp / 32);
+  st = launch("normalise_kernel launch", normalise_kernel, (blocks + kPrepWarps - 1) / kPrepWarps, kPrepWarps * 32, 0, 1,
+              s, pa);
+  if (st != RL_OK) return st;
+
+  // operand maps: K-major boxes of 64 x 128 rows; X as the right operand of B X in boxes of 64 columns
+  // by 64 rows
+  uint16_t* x16[2] = {reinterpret_cast<uint16_t*>(base + w.x16a), reinterpret_cast<uint16_t*>(base + w.x16b)};
+  CUtensorMap xk[2], xn[2], ak, bk;
+  const int64_t rows = static_cast<int64_t>(batch) * sh.sp;
+  const auto F16 = CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+  const auto SW = CU_TENSOR_MAP_SWIZZLE_128B;
+  for (int k = 0; k < 2 && st == RL_OK; ++k) {
+    st = tmap_2d(&xk[k], F16, x16[k], sh.lp, rows, static_cast<int64_t>(sh.lp) * 2, BK, 128, SW);
+    if (st == RL_OK) st = tmap_2d(&xn[k], F16, x16[k], sh.lp, rows, static_cast<int64_t>(sh.lp) * 2, 64, BK, SW);
+  }
+  if (st == RL_OK) st = tmap_2d(&ak, F16, base + w.a16, sh.sp, rows, static_cast<int64_t>(sh.sp) * 2, BK, 128, SW);
+  if (st == RL_OK) st = tmap_2d(&bk, F16, base + w.b16, sh.sp, rows, static_cast<int64_t>(sh.sp) * 2, BK, 128, SW);
+  if (st != RL_OK) return st;
+
+  const Plan plan = plan_of(batch, sh.sp, sh.lp);
+  MmArgs a = {};
+  a.sh = sh;
+  a.ca = P.ns_coef[0];
+  a.cb = P.ns_coef[1];
+  a.cc = P.ns_coef[2];
+  a.a16 = reinterpret_cast<uint16_t*>(base + w.a16);
+  a.b16 = reinterpret_cast<uint16_t*>(base + w.b16);
+  a.d = reinterpret_cast<float*>(base + w.d);
+  a.e = reinterpret_cast<float*>(base + w.e);
+  a.x = pa.x;
+  a.parts = reinterpret_cast<float*>(base + w.parts);
+  a.scale = P.update_scale;
+  a.update = update;
+  a.weights = weights;
+  a.weights_bf16 = weights_bf16;
+  a.ld_w = ld_w;
+  a.stride_w = stride_w;
+  a.decay = static_cast<float>(1.0 - static_cast<double>(P.lr) * P.weight_decay);
+  a.step = static_cast<float>(static_cast<double>(P.lr) * P.update_scale);
+  a.status = status;
+  for (int k = 0; k < P.ns_steps; ++k) {
+    const int T = 128 * plan.cg_sym;
+    a.nt_m = a.nt_n = static_cast<int32_t>(round_up(sh.sp, T) / T);
+    a.per = static_cast<int32_t>(tri(a.nt_m));
+    a.splits = plan.splits;
+    a.nkb = sh.lp / BK;
+    st = plan.cg_sym == 2 ? product<GRAM, 2>(xk[k & 1], xk[k & 1], a, s) : product<GRAM, 1>(xk[k & 1], xk[k & 1], a, s);
+    if (st != RL_OK) return st;
+    if (plan.splits > 1) {
+      const int64_t warps = static_cast<int64_t>(batch) * a.per * (T / 32) * (T / 32);
+      auto kern = plan.cg_sym == 2 ? gram_sum_kernel<2> : gram_sum_kernel<1>;
+      st = launch("gram_sum_kernel launch", kern, (warps + 7) / 8, 256, 0, 1, s, a);
+      if (st != RL_OK) return st;
+    }
+    a.splits = 1;
+    a.nkb = sh.sp / BK;
+    st = plan.cg_sym == 2 ? product<POLY, 2>(ak, ak, a, s) : product<POLY, 1>(ak, ak, a, s);
+    if (st != RL_OK) return st;
+    const int TA = 128 * plan.cg_apply;
+    a.nt_m = static_cast<int32_t>(round_up(sh.sp, TA) / TA);
+    a.nt_n = static_cast<int32_t>(round_up(sh.lp, TA) / TA);
+    a.per = a.nt_m * a.nt_n;
+    a.x16_out = x16[(k + 1) & 1];
+    a.inv = k == 0 ? pa.inv : nullptr;
+    a.final_step = k == P.ns_steps - 1;
+    st = plan.cg_apply == 2 ? product<APPLY, 2>(bk, xn[k & 1], a, s) : product<APPLY, 1>(bk, xn[k & 1], a, s);
+    if (st != RL_OK) return st;
+  }
+  return RL_OK;
+}
+
+}  // extern "C"

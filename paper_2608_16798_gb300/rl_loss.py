@@ -54,6 +54,8 @@ EXPORTS = {
     "rl_fused_head_token_logprobs": (_I32, [_P, _P, _I64, _I64, _I64, _P, _P, _P, _P, _P, _SZ, _P]),
     "rl_fused_head_loss_fwd_bwd": (_I32, [_P, _P, _I64, _I64, _I64, _P, _P, _P, _I32, _P, _P, _P, _P, _P, _P, _P,
                                           _I32, _P, _P, _P, _P, _SZ, _P]),
+    "rl_muon_workspace_size": (_SZ, [_I32, _I64, _I64]),
+    "rl_muon_update": (_I32, [_I32, _I64, _I64, _P, _I32, _I64, _I64, _P, _P, _P, _I64, _I64, _P, _P, _P, _SZ, _P]),
 }
 
 
@@ -67,6 +69,16 @@ def make_params(clip_eps_low=0.2, clip_eps_high=0.28, kl_coef=0.0, kl_estimator=
                 tis_cap=0.0, adv_eps=1e-6, loss_agg=AGG_SEQ_MEAN_TOKEN_MEAN, token_level_adv=0) -> rl_loss_params:
     return rl_loss_params(clip_eps_low, clip_eps_high, kl_coef, kl_estimator, entropy_coef, tis_cap, adv_eps,
                           loss_agg, int(token_level_adv))
+
+
+class rl_muon_params(ctypes.Structure):
+    _fields_ = [("lr", _F), ("momentum", _F), ("nesterov", _I32), ("weight_decay", _F), ("update_scale", _F),
+                ("ns_steps", _I32), ("ns_coef", _F * 3), ("eps", _F)]
+
+
+def make_muon_params(lr=1e-5, momentum=0.95, nesterov=True, weight_decay=0.0, update_scale=1.0, ns_steps=5,
+                     ns_coef=(3.4445, -4.7750, 2.0315), eps=1e-7) -> rl_muon_params:
+    return rl_muon_params(lr, momentum, int(nesterov), weight_decay, update_scale, ns_steps, (_F * 3)(*ns_coef), eps)
 
 
 class rl_tree_stats(ctypes.Structure):
@@ -621,3 +633,67 @@ def rl_token_stats_summary(token_stats, mask, token_traj, coef, ws, summary_accu
                                       p_summary_accum, p_ws, ws.numel(), _stream(stream))
     _check("rl_token_stats_summary", st)
     return summary_accum
+
+
+def rl_muon_workspace_size(batch: int, m: int, n: int) -> int:
+    return int(lib().rl_muon_workspace_size(batch, m, n))
+
+
+def new_muon_workspace(batch: int, m: int, n: int, device=None, stream=None) -> torch.Tensor:
+    """Allocate (with torch) and initialise a workspace of rl_muon_update for matrices of this shape."""
+    nbytes = rl_muon_workspace_size(batch, m, n)
+    if nbytes == 0:
+        raise RLError("rl_muon_workspace_size", 2, rl_last_error_message())
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=device or "cuda")
+    rl_workspace_init(ws, stream)
+    return ws
+
+
+def _matrices(t, name, dtype, shape, ix):
+    """(pointer, leading dimension, batch stride) of a batch of matrices with unit stride along rows."""
+    if t.dtype != dtype or not t.is_cuda or t.get_device() != ix:
+        raise ValueError(f"{name} must be {dtype} on cuda:{ix}, got {t.dtype} on {t.device}")
+    if t.dim() not in (2, 3) or tuple(t.shape[-2:]) != shape[1:] or (t.dim() == 3 and t.shape[0] != shape[0]) or \
+            (t.dim() == 2 and shape[0] != 1):
+        raise ValueError(f"{name} must have the shape of grad, got {tuple(t.shape)}")
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name} must have unit stride along its rows")
+    ld = t.stride(-2) if t.shape[-2] > 1 else max(t.stride(-2), t.shape[-1])
+    return t.data_ptr(), ld, t.stride(0) if t.dim() == 3 and shape[0] > 1 else 0
+
+
+def rl_muon_update(grad, params: rl_muon_params, ws, momentum=None, weights=None, weights_bf16=None, update=None,
+                   stream=None):
+    """Orthogonalised update of one matrix [m, n] or a batch [batch, m, n] of them (bf16 or float32 gradients,
+    unit stride along the rows). ``momentum`` (float32, contiguous) and ``weights`` (float32, any row and batch
+    stride) are updated in place, ``weights_bf16`` (strided as ``weights``) receives the new weights' bf16 copy.
+    Without weights a bf16 ``update`` is created if none is given. Returns ``update`` (or None)."""
+    if grad.dim() not in (2, 3):
+        raise ValueError("grad must be a matrix or a batch of matrices")
+    ix = grad.get_device()
+    m, n = grad.shape[-2:]
+    batch = grad.shape[0] if grad.dim() == 3 else 1
+    shape = (batch, m, n)
+    p_grad, ld_grad, stride_grad = _matrices(grad, "grad", grad.dtype, shape, ix)
+    dt = _logits_dtype(grad) if grad.dtype in (torch.bfloat16, torch.float32) else _refuse_dtype("grad", grad)
+    p_momentum = _opt(momentum, "momentum", torch.float32, batch * m * n, index=ix)
+    p_weights = p_weights_bf16 = None
+    ld_w, stride_w = n, m * n
+    if weights is not None:
+        p_weights, ld_w, stride_w = _matrices(weights, "weights", torch.float32, shape, ix)
+    if weights_bf16 is not None:
+        p_weights_bf16, ld_b, stride_b = _matrices(weights_bf16, "weights_bf16", torch.bfloat16, shape, ix)
+        if weights is not None and (ld_b, stride_b) != (ld_w, stride_w):
+            raise ValueError("weights_bf16 must have the strides of weights")
+    if update is None and weights is None:
+        update = torch.empty(grad.shape, dtype=torch.bfloat16, device=grad.device)
+    p_update = _opt(update, "update", torch.bfloat16, batch * m * n, index=ix)
+    p_ws = _need(ws, "ws", torch.uint8, index=ix)
+    st = lib().rl_muon_update(batch, m, n, p_grad, dt, ld_grad, stride_grad, p_momentum, p_weights, p_weights_bf16,
+                              ld_w, stride_w, p_update, ctypes.byref(params), p_ws, ws.numel(), _stream(stream))
+    _check("rl_muon_update", st)
+    return update
+
+
+def _refuse_dtype(name, t):
+    raise ValueError(f"{name} must be bfloat16 or float32, got {t.dtype}")

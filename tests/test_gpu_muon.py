@@ -1,0 +1,202 @@
+"""rl_muon_update against its float64 reference.
+
+Tolerances, fixed before the first run: the products read fp16 operands, and an emulation of the scheme
+(fp16 roundings of the operands, fp32 X and diagonals) over random, low-rank and decaying matrices stays
+below 1.1e-3 of X in 2-norm and 1e-2 of its root mean square in any element; twice that is allowed,
+2^-9 in 2-norm and 2^-8 of an element more for the rounding to bf16. Momentum is one fp32 fused
+multiply-add (2^-24 of its two terms); weights are three fp32 roundings and lr s times the error of X.
+"""
+
+import numpy as np
+import pytest
+import torch
+
+import oracle.orthogonal_update as O
+
+pytestmark = pytest.mark.gpu
+
+NS_REL, NS_MAX = 2.2e-3, 2e-2
+
+
+@pytest.fixture(scope="module")
+def R():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    from paper_2608_16798_gb300 import build
+
+    build.build()
+    import paper_2608_16798_gb300.rl_loss as R
+
+    R.lib()
+    return R
+
+
+def matrices(law, batch, m, n, seed):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(batch, m, n, generator=g)
+    r = min(8, m, n)
+    u, v = torch.randn(batch, m, r, generator=g), torch.randn(batch, r, n, generator=g)
+    if law == "low_rank":
+        x = (u / torch.arange(1, r + 1)) @ v + 0.02 * x
+    elif law == "one_direction":
+        x = u[:, :, :1] @ v[:, :1] + 1e-3 * x
+    elif law == "zero_rows":
+        x[:, ::3] = 0
+    return x
+
+
+def check_x(got, ref, what, bf16):
+    got, ref = got.double().cpu().numpy(), np.asarray(ref)
+    assert np.isfinite(got).all(), what
+    for b in range(len(ref)):
+        norm = np.linalg.norm(ref[b])
+        d = got[b] - ref[b]
+        rms = norm / np.sqrt(ref[b].size)
+        assert np.linalg.norm(d) <= (NS_REL + (2.0 ** -9 if bf16 else 0.0)) * norm, (what, b, np.linalg.norm(d) / norm)
+        assert (np.abs(d) <= NS_MAX * rms + (2.0 ** -8 * np.abs(ref[b]) if bf16 else 0.0)).all(), (what, b)
+
+
+SHAPES = [(1, 1, 1), (1, 1, 7), (1, 7, 1), (2, 5, 3), (1, 64, 64), (1, 128, 128), (1, 127, 129), (3, 129, 127),
+          (2, 130, 300), (2, 300, 130), (5, 33, 1000), (1, 1000, 33), (1, 257, 1025), (1, 640, 384), (1, 128, 9000),
+          (1, 9001, 100), (12, 256, 256), (1, 1000, 1777), (1, 2305, 2049), (1, 1024, 5000)]
+
+
+@pytest.mark.parametrize("batch,m,n", SHAPES)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_update(R, batch, m, n, dtype):
+    law = ["low_rank", "normal"][(m + n) % 2]
+    grad = matrices(law, batch, m, n, 1).to(dtype)
+    mom = matrices(law, batch, m, n, 2) * 3
+    buf, _, upd, _ = O.muon_update(grad.double().numpy(), mom.numpy(), update_scale=0.5)
+    ws = R.new_muon_workspace(batch, m, n)
+    d_mom = mom.cuda()
+    got = R.rl_muon_update(grad.cuda(), R.make_muon_params(update_scale=0.5), ws, momentum=d_mom)
+    assert R.rl_query_status(ws)[1] == 0
+    check_x(got, upd, "update", True)
+    tol = 2.0 ** -23 * (np.abs(mom.double().numpy()) + np.abs(grad.double().numpy()))
+    assert (np.abs(d_mom.cpu().double().numpy() - buf) <= tol + 1e-30).all()
+
+
+@pytest.mark.parametrize("law", ["normal", "low_rank", "one_direction", "zero_rows"])
+@pytest.mark.parametrize("m,n", [(192, 320), (320, 192), (512, 512), (96, 4096)])
+@pytest.mark.parametrize("nesterov", [True, False])
+def test_weights(R, law, m, n, nesterov):
+    batch, lr, scale, wd = 2, 0.05, 0.7, 0.1
+    grad, mom, w = (matrices(law, batch, m, n, 3), matrices(law, batch, m, n, 4), matrices("normal", batch, m, n, 5))
+    _, X, _, w_ref = O.muon_update(grad.numpy(), mom.numpy(), w.numpy(), lr=lr, nesterov=nesterov, weight_decay=wd,
+                                   update_scale=scale)
+    ws = R.new_muon_workspace(batch, m, n)
+    P = R.make_muon_params(lr=lr, nesterov=nesterov, weight_decay=wd, update_scale=scale)
+    # weights in a wider buffer; what lies between the rows stays
+    wide = torch.full((batch, m, n + 3), 7.0, device="cuda")
+    wide16 = torch.full((batch, m, n + 3), 7.0, dtype=torch.bfloat16, device="cuda")
+    wide[:, :, :n] = w.cuda()
+    out = R.rl_muon_update(grad.cuda(), P, ws, momentum=mom.cuda(), weights=wide[:, :, :n], weights_bf16=wide16[:, :, :n])
+    assert out is None and R.rl_query_status(ws)[1] == 0
+    got = wide[:, :, :n].cpu()
+    for b in range(batch):
+        err = np.linalg.norm(got[b].double().numpy() - w_ref[b])
+        assert err <= lr * scale * NS_REL * np.linalg.norm(X[b]) + 4 * 2.0 ** -24 * np.linalg.norm(w_ref[b])
+    assert torch.equal(wide16[:, :, :n].cpu(), got.bfloat16())
+    assert (wide[:, :, n:] == 7).all() and (wide16[:, :, n:] == 7).all()
+
+
+def test_interleaved_batch(R):
+    """A batch whose rows alternate in memory ([m, batch, n]), for the gradient and for the weights."""
+    batch, m, n = 3, 70, 90
+    grad, w = matrices("normal", batch, m, n, 6), matrices("normal", batch, m, n, 7)
+    P = R.make_muon_params(lr=0.1, momentum=0.0)
+    ws = R.new_muon_workspace(batch, m, n)
+    plain = w.cuda()
+    R.rl_muon_update(grad.cuda(), P, ws, weights=plain)
+    g2, w2 = grad.cuda().transpose(0, 1).contiguous(), w.cuda().transpose(0, 1).contiguous()
+    R.rl_muon_update(g2.transpose(0, 1), P, ws, weights=w2.transpose(0, 1))
+    assert torch.equal(w2.transpose(0, 1), plain)
+
+
+@pytest.mark.parametrize("scale", [1e-38, 1e-30, 1e-20, 1e20, 1e30, 1e37])
+@pytest.mark.parametrize("m,n", [(100, 180), (180, 100)])
+def test_scale_of_the_gradient(R, scale, m, n):
+    """The norm neither overflows nor underflows fp32 (eps is 0 here)."""
+    g = (matrices("normal", 1, m, n, 8).double() * scale).float()
+    ref = O.newton_schulz(g[0].double().numpy(), eps=0.0)
+    ws = R.new_muon_workspace(1, m, n)
+    got = R.rl_muon_update(g.cuda(), R.make_muon_params(momentum=0.0, eps=0.0), ws)
+    assert R.rl_query_status(ws)[1] == 0
+    check_x(got, ref[None], "update", True)
+
+
+def test_zero_and_non_finite(R):
+    batch, m, n = 4, 150, 90
+    g = matrices("normal", batch, m, n, 9)
+    g[1] = 0
+    g[2, 17, 3] = float("nan")
+    g[3, 0, 89] = float("inf")
+    ws = R.new_muon_workspace(batch, m, n)
+    got = R.rl_muon_update(g.cuda(), R.make_muon_params(momentum=0.0), ws)
+    assert R.rl_query_status(ws)[1] == R.RL_DEV_BAD_VALUE
+    check_x(got[:1], O.newton_schulz(g[0].numpy())[None], "update", True)
+    assert not got[1].any()
+    assert got[2].isnan().all() and got[3].isnan().all()
+    # the workspace serves the next call after its status is cleared
+    R.rl_workspace_init(ws)
+    again = R.rl_muon_update(g[:1].expand(batch, m, n).cuda(), R.make_muon_params(momentum=0.0), ws)
+    assert R.rl_query_status(ws)[1] == 0
+    assert all(torch.equal(again[k], got[0]) for k in range(batch))
+
+
+@pytest.mark.parametrize("steps,coef", [(1, O.NS_COEF), (2, (1.5, -0.5, 0.0)), (10, (1.5, -0.5, 0.0)), (3, (2.0, -1.5, 0.5))])
+def test_steps_and_coefficients(R, steps, coef):
+    g = matrices("normal", 1, 200, 260, 10)
+    ref = O.newton_schulz(g[0].numpy(), steps, coef)
+    ws = R.new_muon_workspace(1, 200, 260)
+    got = R.rl_muon_update(g.cuda(), R.make_muon_params(momentum=0.0, ns_steps=steps, ns_coef=coef), ws)
+    check_x(got, ref[None], "update", True)
+
+
+@pytest.mark.parametrize("batch,m,n", [(1, 300, 500), (1, 128, 9000), (1, 1500, 1500)])
+def test_repeats_streams_and_graphs(R, batch, m, n):
+    """The same bits again, on another stream, and from a graph; no workspace contents are relied on."""
+    g = matrices("low_rank", batch, m, n, 11).cuda()
+    P = R.make_muon_params(momentum=0.5)
+    ws = R.new_muon_workspace(batch, m, n)
+    first = R.rl_muon_update(g, P, ws, momentum=torch.zeros_like(g))
+    ws2 = torch.full_like(ws, 255)
+    R.rl_workspace_init(ws2)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        second = R.rl_muon_update(g, P, ws2, momentum=torch.zeros_like(g))
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(first, second)
+    mom, upd = torch.zeros_like(g), torch.empty_like(first)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        R.rl_muon_update(g, P, ws, momentum=mom, update=upd)
+    for _ in range(2):
+        mom.zero_()
+        upd.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(first, upd)
+    assert R.rl_query_status(ws)[1] == 0 and R.rl_query_status(ws2)[1] == 0
+
+
+def test_binding_refusals(R):
+    g = torch.zeros(8, 16, device="cuda")
+    ws = R.new_muon_workspace(1, 8, 16)
+    P = R.make_muon_params(momentum=0.0)
+    for bad in (dict(weights=torch.zeros(8, 15, device="cuda")), dict(weights=torch.zeros(16, 8, device="cuda").T),
+                dict(weights=torch.zeros(8, 16, dtype=torch.bfloat16, device="cuda")),
+                dict(update=torch.zeros(8, 16, device="cuda")), dict(momentum=torch.zeros(8, 8, device="cuda")),
+                dict(weights=torch.zeros(8, 16, device="cuda"),
+                     weights_bf16=torch.zeros(8, 32, dtype=torch.bfloat16, device="cuda")[:, ::2])):
+        with pytest.raises(ValueError):
+            R.rl_muon_update(g, P, ws, **bad)
+    for bad in (g.half(), g.T, g[None, None], g.cpu()):
+        with pytest.raises((ValueError, R.RLError)):
+            R.rl_muon_update(bad, P, ws)
+    with pytest.raises(R.RLError):
+        R.rl_muon_update(g, P, ws[:512])
+    with pytest.raises(R.RLError):
+        R.new_muon_workspace(1, 40000, 40000)
