@@ -610,7 +610,7 @@ typedef struct rl_muon_params {
 } rl_muon_params;
 
 /* Workspace bytes of rl_muon_update on `batch` matrices [m x n] (0 for sizes that it refuses). With s
- * the shorter and l the longer side, about 8 s l + 4 s^2 bytes per matrix. */
+ * the shorter and l the longer side, about 8 s l + 6 s^2 bytes per matrix. */
 size_t rl_muon_workspace_size(int32_t batch, int64_t m, int64_t n);
 
 /*

@@ -48,7 +48,9 @@ __host__ __device__ inline int64_t round_up(int64_t x, int64_t to) { return (x +
 //
 // X (fp32) lies in blocks of 32 x 32: block (R, C) of a matrix at (R * l32 + C) * 1024, and in a
 // block element (r, c) at (c / 4) * 128 + r * 4 + c % 4, so that a warp whose lanes hold one row each
-// moves 512 contiguous bytes per instruction. The fp16 operands are row-major, as TMA reads them.
+// moves 512 contiguous bytes per instruction. The fp16 operands are row-major, as TMA reads them; of A's
+// blocks on and above the diagonal there is a second copy, in blocks for the epilogue of B, where element
+// (r, c) lies at (c / 8) * 256 + r * 8 + c % 8.
 
 struct Shape {
   int32_t batch, m, n;   // the caller's matrices
@@ -98,19 +100,16 @@ __device__ __forceinline__ void store_half_row(uint16_t* to, const float (&v)[32
                    pack_half2(v[8 * j + 4], v[8 * j + 5]), pack_half2(v[8 * j + 6], v[8 * j + 7]));
 }
 
-// A 32 x 32 block of a symmetric matrix [sp x sp] in fp16, lane l holding row r0 + l of it, at
-// (r0, c0) and, mirrored, at (c0, r0). Mirrored rows leave in pairs: lanes 2k and 2k + 1 exchange one
-// of every two columns, so that each stores two neighbouring rows' values of one column.
-__device__ __forceinline__ void store_symmetric(uint16_t* m, int sp, int r0, int c0, int lane, const float (&v)[32],
-                                                bool mirror) {
-  store_half_row(m + static_cast<int64_t>(r0 + lane) * sp + c0, v);
-  if (!mirror) return;
+// The mirror image of a 32 x 32 block whose rows the lanes hold, in pairs of fp16: lanes 2k and 2k + 1
+// exchange one of every two columns, so that f(j, w) gets in w column j (j even in even lanes, odd in
+// odd ones) of rows lane & ~1 and its neighbour.
+template <typename F>
+__device__ __forceinline__ void mirrored(int lane, const float (&v)[32], F f) {
   const int odd = lane & 1;
 #pragma unroll
   for (int j = 0; j < 32; j += 2) {
     const float got = __shfl_xor_sync(0xffffffffu, odd ? v[j] : v[j + 1], 1);
-    const uint32_t w = odd ? pack_half2(got, v[j + 1]) : pack_half2(v[j], got);
-    *reinterpret_cast<uint32_t*>(m + static_cast<int64_t>(c0 + j + odd) * sp + r0 + (lane & ~1)) = w;
+    f(j + odd, odd ? pack_half2(got, v[j + 1]) : pack_half2(v[j], got));
   }
 }
 
@@ -123,7 +122,6 @@ struct PrepArgs {
   Shape sh;
   const void* grad;
   int64_t ld_grad, stride_grad;
-  int32_t grad_bf16;
   float* momentum;       // [batch x m x n] or null
   float mu;
   int32_t nesterov;
@@ -137,8 +135,9 @@ struct PrepArgs {
   int32_t* status;
 };
 
+template <bool BF16>
 __device__ __forceinline__ float grad_at(const PrepArgs& p, int64_t i) {
-  return p.grad_bf16 ? bf16_to_f32(static_cast<const uint16_t*>(p.grad)[i]) : static_cast<const float*>(p.grad)[i];
+  return BF16 ? bf16_to_f32(static_cast<const uint16_t*>(p.grad)[i]) : static_cast<const float*>(p.grad)[i];
 }
 
 // The sum of the squares of 32 values as a double, without fp32 overflow or underflow: the values are
@@ -167,6 +166,7 @@ constexpr int kPrepWarps = 8;
 
 // u and its sum of squares. A warp forms one 32 x 32 block of X; a CTA's warps take eight blocks that
 // lie side by side in the caller's rows.
+template <bool BF16>
 __global__ void __launch_bounds__(kPrepWarps * 32) momentum_kernel(const PrepArgs p) {
   __shared__ float tile[kPrepWarps][32][33];
   __shared__ double sums[kPrepWarps];
@@ -189,25 +189,26 @@ __global__ void __launch_bounds__(kPrepWarps * 32) momentum_kernel(const PrepArg
     // rows and columns of the caller's matrix: lane walks its row
     const int c = a_blk * 32 + lane, r0 = x_blk * 32;
     const int64_t g0 = b * p.stride_grad + c, m0 = static_cast<int64_t>(b) * sh.m * sh.n + c;
+    // all loads of the block before its first store: up to 64 in flight per lane
+    const int rows = c < sh.n ? sh.m - r0 : 0;
     float v[32];
 #pragma unroll
-    for (int j = 0; j < 32; ++j) {
-      const int r = r0 + j;
-      float u = 0.f;
-      if (r < sh.m && c < sh.n) {
-        const float g = grad_at(p, g0 + r * p.ld_grad);
-        u = g;
-        if (p.momentum) {
-          float* at = p.momentum + m0 + static_cast<int64_t>(r) * sh.n;
-          const float buf = fmaf(p.mu, *at, g);
-          *at = buf;
-          u = p.nesterov ? fmaf(p.mu, buf, g) : buf;
-        }
+    for (int j = 0; j < 32; ++j) v[j] = j < rows ? grad_at<BF16>(p, g0 + (r0 + j) * p.ld_grad) : 0.f;
+    if (p.momentum) {
+      float* at = p.momentum + m0 + static_cast<int64_t>(r0) * sh.n;
+      float buf[32];
+#pragma unroll
+      for (int j = 0; j < 32; ++j) buf[j] = j < rows ? at[static_cast<int64_t>(j) * sh.n] : 0.f;
+#pragma unroll
+      for (int j = 0; j < 32; ++j) {
+        buf[j] = fmaf(p.mu, buf[j], v[j]);
+        if (j < rows) at[static_cast<int64_t>(j) * sh.n] = buf[j];
+        v[j] = p.nesterov ? fmaf(p.mu, buf[j], v[j]) : buf[j];
       }
-      if (sh.tall) v[j] = u;
-      else tile[warp][j][lane] = u;
     }
     if (!sh.tall) {
+#pragma unroll
+      for (int j = 0; j < 32; ++j) tile[warp][j][lane] = v[j];
       __syncwarp();
 #pragma unroll
       for (int j = 0; j < 32; ++j) v[j] = tile[warp][lane][j];
@@ -271,12 +272,11 @@ struct MmArgs {
   int32_t nkb;           // 64-element blocks of the contraction
   int32_t splits;        // GRAM: parts of the contraction, each an item
   float ca, cb, cc;      // the step's coefficients
-  uint16_t* a16;
-  uint16_t* b16;
+  uint16_t* a16;         // A off its diagonal, row-major
+  uint16_t* a_blk;       // the same in blocks
   float* d;              // [batch x sp] the diagonal of A
   float* e;              // [batch x sp] a + the diagonal of B
   float* x;
-  uint16_t* x16_out;
   const float* inv;      // first step: X is still u, to be multiplied by this
   float* parts;          // GRAM with splits > 1: [split][tile][TILE x TILE] sums
   // the last step's outputs
@@ -294,9 +294,12 @@ constexpr int BK = 64;
 constexpr uint32_t A_BYTES = 128 * BK * 2;
 constexpr uint32_t STAGE_BYTES = 2 * A_BYTES;
 constexpr uint32_t HALF_BYTES = 64 * BK * 2;
-constexpr int NS = 6;
-constexpr int kThreads = 192;  // warp 0 TMA, warp 1 MMA, warps 2-5 epilogue
-constexpr size_t kSmem = NS * STAGE_BYTES + 4 * 32 * 33 * 4 + 1024;
+constexpr int NS = 5;
+constexpr int kEpiWarps = 8;
+constexpr int kThreads = 64 + 32 * kEpiWarps;  // warp 0 TMA, warp 1 MMA, then the epilogue
+constexpr uint32_t SLAB_BYTES = 2048;          // a 32 x 32 fp16 block on its way out
+constexpr uint32_t EPI_BYTES = 4 * SLAB_BYTES; // per epilogue warp: two blocks and their mirror images
+constexpr size_t kSmem = NS * STAGE_BYTES + kEpiWarps * EPI_BYTES + 1024;
 static_assert(kSmem <= 232448 - 1024, "shared memory of the product kernels");
 
 // fp16 operands, fp32 accumulator, M x N; B MN-major for APPLY.
@@ -313,71 +316,96 @@ __device__ __forceinline__ void triangle(int t, int& i, int& j) {
   i = t - j * (j + 1) / 2;
 }
 
-// What becomes of a 32 x 32 block (lane: row) of X X^T, scaled by 2^24.
-__device__ __forceinline__ void gram_out(const MmArgs& p, int b, int r0, int c0, int lane, float (&v)[32]) {
-  const int sp = p.sh.sp;
-#pragma unroll
-  for (int j = 0; j < 32; ++j) {
-    v[j] *= kAScale / (kXScale * kXScale);
-    if (c0 + j == r0 + lane) {
-      p.d[static_cast<int64_t>(b) * sp + r0 + lane] = v[j] * (1.f / kAScale);
-      v[j] = 0.f;
-    }
-  }
-  store_symmetric(p.a16 + static_cast<int64_t>(b) * sp * sp, sp, r0, c0, lane, v, r0 != c0);
+// Two-dimensional bulk store of a slab (bulk-group completion).
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, int c0, int c1, const void* src) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];"
+               :: "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(smem_addr(src)) : "memory");
 }
 
-// The same of Ao Ao, scaled by 2^24.
-__device__ __forceinline__ void poly_out(const MmArgs& p, int b, int r0, int c0, int lane, float (&v)[32]) {
-  const int sp = p.sh.sp;
-  const int64_t at = static_cast<int64_t>(b) * sp;
-  const float* d = p.d + at;
-  const float di = d[r0 + lane], dj = d[c0 + lane];
-  const uint4* a = reinterpret_cast<const uint4*>(p.a16 + (at + r0 + lane) * sp + c0);
+// A 32 x 32 block out through shared memory: 64-byte rows with the 64-byte swizzle (16-byte chunk k of
+// row r at chunk k ^ (r / 2) % 4). `mirror`: also its mirror image, at (c0, r0) of the same matrix, whose
+// rows begin at row0 of the map. slab: two blocks of SLAB_BYTES that no store is reading.
+__device__ __forceinline__ void put_block(const CUtensorMap* map, int row0, int r0, int c0, int lane,
+                                          const float (&v)[32], bool mirror, uint8_t* slab) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    *reinterpret_cast<uint4*>(slab + lane * 64 + ((k ^ ((lane >> 1) & 3)) << 4)) =
+        make_uint4(pack_half2(v[8 * k], v[8 * k + 1]), pack_half2(v[8 * k + 2], v[8 * k + 3]),
+                   pack_half2(v[8 * k + 4], v[8 * k + 5]), pack_half2(v[8 * k + 6], v[8 * k + 7]));
+  if (mirror)
+    mirrored(lane, v, [&](int j, uint32_t w) {
+      *reinterpret_cast<uint32_t*>(slab + SLAB_BYTES + j * 64 + (((lane >> 3) ^ ((j >> 1) & 3)) << 4) +
+                                   ((lane & 6) << 1)) = w;
+    });
+  fence_proxy_async_smem();
+  __syncwarp();
+  if (lane == 0) {
+    tma_store_2d(map, c0, row0 + r0, slab);
+    if (mirror) tma_store_2d(map, r0, row0 + c0, slab + SLAB_BYTES);
+    bulk_commit();
+  }
+}
+
+__device__ __forceinline__ uint16_t* a_block(const MmArgs& p, int b, int r0, int c0) {
+  const int nb = p.sh.sp >> 5;
+  return p.a_blk + ((static_cast<int64_t>(b) * nb + (r0 >> 5)) * nb + (c0 >> 5)) * 1024;
+}
+
+// What becomes of a 32 x 32 block (lane: row) of X X^T, scaled by 2^24: A off its diagonal, scaled.
+__device__ __forceinline__ void gram_of(const MmArgs& p, int b, int r0, int c0, int lane, float (&v)[32]) {
+#pragma unroll
+  for (int j = 0; j < 32; ++j) v[j] *= kAScale / (kXScale * kXScale);
+  if (r0 == c0) {
+#pragma unroll
+    for (int j = 0; j < 32; ++j)
+      if (j == lane) {
+        p.d[static_cast<int64_t>(b) * p.sh.sp + r0 + lane] = v[j] * (1.f / kAScale);
+        v[j] = 0.f;
+      }
+  }
+  uint16_t* blk = a_block(p, b, r0, c0) + lane * 8;
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    *reinterpret_cast<uint4*>(blk + k * 256) =
+        make_uint4(pack_half2(v[8 * k], v[8 * k + 1]), pack_half2(v[8 * k + 2], v[8 * k + 3]),
+                   pack_half2(v[8 * k + 4], v[8 * k + 5]), pack_half2(v[8 * k + 6], v[8 * k + 7]));
+}
+
+// The same of Ao Ao, scaled by 2^24: B off its diagonal, scaled. a: this lane's row of the block of A;
+// di, dj: the diagonal at its row, and at the block's columns, one per lane.
+__device__ __forceinline__ void poly_of(const MmArgs& p, int b, int r0, int c0, int lane, float (&v)[32],
+                                        const uint4 (&a)[4], float di, float dj) {
+  const bool on_diagonal = r0 == c0;
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
-    const uint4 w = a[k];
-    const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+    const uint32_t w[4] = {a[k].x, a[k].y, a[k].z, a[k].w};
 #pragma unroll
     for (int h = 0; h < 4; ++h) {
-      const float2 ao = unpack_half2(ww[h]);
+      const float2 ao = unpack_half2(w[h]);
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int j = 8 * k + 2 * h + i;
         const float x = (i ? ao.y : ao.x) * (1.f / kAScale);
         const float dc = __shfl_sync(0xffffffffu, dj, j);
         const float sq = v[j] * (1.f / (kAScale * kAScale));
-        if (c0 + j == r0 + lane) {
-          p.e[at + r0 + lane] = p.ca + fmaf(p.cb, di, p.cc * fmaf(di, di, sq));
+        v[j] = kBScale * fmaf(p.cb, x, p.cc * fmaf(di + dc, x, sq));
+        if (on_diagonal && j == lane) {
+          p.e[static_cast<int64_t>(b) * p.sh.sp + r0 + lane] = p.ca + fmaf(p.cb, di, p.cc * fmaf(di, di, sq));
           v[j] = 0.f;
-        } else {
-          v[j] = kBScale * fmaf(p.cb, x, p.cc * fmaf(di + dc, x, sq));
         }
       }
     }
   }
-  store_symmetric(p.b16 + at * sp, sp, r0, c0, lane, v, r0 != c0);
 }
 
-// The step's new X: kept, or in the last step the caller's outputs.
-__device__ __forceinline__ void apply_out(const MmArgs& p, int b, int r0, int c0, int lane, float (&v)[32],
+// The last step's X (lane: row) to the caller's outputs, lanes walking the caller's rows. tile: 32 x 33
+// floats of shared memory.
+__device__ __forceinline__ void final_out(const MmArgs& p, int b, int r0, int c0, int lane, float (&v)[32],
                                           float (*tile)[33]) {
   const Shape& sh = p.sh;
-  float* blk = x_block(p.x, sh, b, r0 >> 5, c0 >> 5);
-  float x[32];
-  load_block_row(blk, lane, x);
-  float f = p.e[static_cast<int64_t>(b) * sh.sp + r0 + lane];
-  if (p.inv) f *= p.inv[b];
-#pragma unroll
-  for (int j = 0; j < 32; ++j) v[j] = fmaf(f, x[j], v[j] * (1.f / (kBScale * kXScale)));
-  if (!p.final_step) {
-    store_block_row(blk, lane, v);
-#pragma unroll
-    for (int j = 0; j < 32; ++j) v[j] *= kXScale;
-    store_half_row(p.x16_out + (static_cast<int64_t>(b) * sh.sp + r0 + lane) * sh.lp + c0, v);
-    return;
-  }
-  // lanes walk the caller's rows
+  const int col = (sh.tall ? r0 : c0) + lane, row0 = sh.tall ? c0 : r0;
+  const int rows = col < sh.n ? sh.m - row0 : 0;
+  const int64_t w0 = b * p.stride_w + row0 * p.ld_w + col;
   if (!sh.tall) {
     __syncwarp();
 #pragma unroll
@@ -386,20 +414,25 @@ __device__ __forceinline__ void apply_out(const MmArgs& p, int b, int r0, int c0
 #pragma unroll
     for (int j = 0; j < 32; ++j) v[j] = tile[j][lane];
   }
-  const int col = (sh.tall ? r0 : c0) + lane, row0 = sh.tall ? c0 : r0;
-  if (col >= sh.n) return;
+  if (p.update) {
+    uint16_t* to = p.update + (static_cast<int64_t>(b) * sh.m + row0) * sh.n + col;
 #pragma unroll
-  for (int j = 0; j < 32; ++j) {
-    const int row = row0 + j;
-    if (row < sh.m) {
-      if (p.update)
-        p.update[(static_cast<int64_t>(b) * sh.m + row) * sh.n + col] = f32_to_bf16(v[j] * p.scale);
-      if (p.weights) {
-        const int64_t at = b * p.stride_w + row * p.ld_w + col;
-        const float w = fmaf(-p.step, v[j], p.decay * p.weights[at]);
-        p.weights[at] = w;
-        if (p.weights_bf16) p.weights_bf16[at] = f32_to_bf16(w);
-      }
+    for (int j = 0; j < 32; ++j)
+      if (j < rows) to[static_cast<int64_t>(j) * sh.n] = f32_to_bf16(v[j] * p.scale);
+  }
+  if (p.weights) {
+    float w[32];
+#pragma unroll
+    for (int j = 0; j < 32; ++j) w[j] = j < rows ? p.weights[w0 + j * p.ld_w] : 0.f;
+#pragma unroll
+    for (int j = 0; j < 32; ++j) {
+      w[j] = fmaf(-p.step, v[j], p.decay * w[j]);
+      if (j < rows) p.weights[w0 + j * p.ld_w] = w[j];
+    }
+    if (p.weights_bf16) {
+#pragma unroll
+      for (int j = 0; j < 32; ++j)
+        if (j < rows) p.weights_bf16[w0 + j * p.ld_w] = f32_to_bf16(w[j]);
     }
   }
 }
@@ -410,7 +443,9 @@ __device__ __forceinline__ void apply_out(const MmArgs& p, int b, int r0, int c0
 // products of the next.
 template <int MODE, int CG>
 __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_constant__ CUtensorMap tmA,
-                                                              const __grid_constant__ CUtensorMap tmB, const MmArgs p) {
+                                                              const __grid_constant__ CUtensorMap tmB,
+                                                              const __grid_constant__ CUtensorMap tmOut,
+                                                              const MmArgs p) {
   constexpr int TILE = 128 * CG;
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) uint64_t full[NS], empty[NS], accf[2], acce[2];
@@ -429,7 +464,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
     }
     for (int k = 0; k < 2; ++k) {
       mbar_init(&accf[k], 1);
-      mbar_init(&acce[k], 4 * CG);
+      mbar_init(&acce[k], kEpiWarps * CG);
     }
     fence_mbar_init();
   }
@@ -553,26 +588,57 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
       }
     }
   } else {
-    const int q = warp & 3;  // TMEM lane quarter this warp may access
-    float(*tile)[33] = reinterpret_cast<float(*)[33]>(sm + NS * STAGE_BYTES) + (warp - 2) * 32;
+    // Two warps per TMEM lane quarter take the tile's 32-column blocks in turn. What a block needs from
+    // memory is loaded one block ahead, the first before the products are done.
+    const int q = warp & 3, half = (warp - 2) >> 2;
+    uint8_t* slabs = sm + NS * STAGE_BYTES + (warp - 2) * EPI_BYTES;
+    float(*tile)[33] = reinterpret_cast<float(*)[33]>(slabs);
+    uint32_t slab = 0;
     uint32_t t = 0;
     for (int item = unit; item < n_items; item += units, ++t) {
       int b, ti, tj, kb0, nkb;
       decode(item, b, ti, tj, kb0, nkb);
       const uint32_t buf = t & 1;
+      const int r0 = ti * TILE + static_cast<int>(rank) * 128 + 32 * q;
+      const uint32_t tq = tmem + buf * TILE + (static_cast<uint32_t>(32 * q) << 16);
+      const int cols = MODE == APPLY ? p.sh.lp : p.sh.sp;
+      const bool in_parts = MODE == GRAM && p.splits > 1;
+      // blocks past the matrix are another one's or nothing; in a tile on the diagonal of a symmetric
+      // product those below it are the mirror image of those above
+      auto wanted = [&](int c) {
+        const int c0 = tj * TILE + c * 32;
+        return c < TILE / 32 && r0 < p.sh.sp && c0 < cols && (MODE == APPLY || in_parts || ti != tj || c0 >= r0);
+      };
+      float x[32], f = 0.f;
+      uint4 a[4];
+      float di = 0.f, dj = 0.f;
+      auto prefetch = [&](int c) {
+        if (!wanted(c)) return;
+        const int c0 = tj * TILE + c * 32;
+        if (MODE == APPLY) load_block_row(x_block(p.x, p.sh, b, r0 >> 5, c0 >> 5), lane, x);
+        if (MODE == POLY) {
+          const uint16_t* blk = a_block(p, b, r0, c0) + lane * 8;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) a[k] = *reinterpret_cast<const uint4*>(blk + k * 256);
+          dj = p.d[static_cast<int64_t>(b) * p.sh.sp + c0 + lane];
+        }
+      };
+      if (r0 < p.sh.sp) {
+        const int64_t row = static_cast<int64_t>(b) * p.sh.sp + r0 + lane;
+        if (MODE == APPLY) f = p.inv ? p.e[row] * p.inv[b] : p.e[row];
+        if (MODE == POLY) di = p.d[row];
+      }
+      prefetch(half);
       if (!mbar_wait_sleep_bounded(&accf[buf], (t >> 1) & 1)) {
         if (lane == 0) flag_status(p.status, RL_DEV_TIMEOUT);
         break;
       }
       tc::fence_after_sync();
-      const int r0 = ti * TILE + static_cast<int>(rank) * 128 + 32 * q;
-      const uint32_t tq = tmem + buf * TILE + (static_cast<uint32_t>(32 * q) << 16);
-      const int cols = MODE == APPLY ? p.sh.lp : p.sh.sp;
 #pragma unroll 1
-      for (int c = 0; c < TILE / 32; ++c) {
+      for (int c = half; c < TILE / 32; c += 2) {
         float v[32];
         tc::tmem_ld32(tq + c * 32, v);
-        if (c == TILE / 32 - 1) {
+        if (c + 2 >= TILE / 32) {
           tc::fence_before_sync();
           __syncwarp();
           if (lane == 0) {
@@ -580,23 +646,40 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
             else mbar_arrive(&acce[buf]);
           }
         }
-        const int c0 = tj * TILE + c * 32;
-        if (r0 < p.sh.sp && c0 < cols) {  // past the matrix: another one's rows, or nothing
-          if (MODE == GRAM && p.splits > 1) {
-            float* blk = p.parts + static_cast<int64_t>(item) * TILE * TILE +
-                         (static_cast<int64_t>((rank * 4 + q) * (TILE / 32) + c)) * 1024;
-            store_block_row(blk, lane, v);
-          } else if (MODE == APPLY) {
-            apply_out(p, b, r0, c0, lane, v, tile);
-          } else if (c0 >= r0 || ti != tj) {
-            // in a tile on the diagonal the blocks below it are the mirror image of those above
-            if (MODE == GRAM) gram_out(p, b, r0, c0, lane, v);
-            else poly_out(p, b, r0, c0, lane, v);
-          }
+        if (!wanted(c)) {
+          prefetch(c + 2);
+          continue;
         }
+        const int c0 = tj * TILE + c * 32;
+        if (in_parts) {
+          store_block_row(p.parts + static_cast<int64_t>(item) * TILE * TILE +
+                              (static_cast<int64_t>((rank * 4 + q) * (TILE / 32) + c)) * 1024, lane, v);
+          continue;
+        }
+        if (MODE == GRAM) gram_of(p, b, r0, c0, lane, v);
+        if (MODE == POLY) poly_of(p, b, r0, c0, lane, v, a, di, dj);
+        if (MODE == APPLY) {
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] = fmaf(f, x[j], v[j] * (1.f / (kBScale * kXScale)));
+        }
+        prefetch(c + 2);
+        if (MODE == APPLY) {
+          if (p.final_step) {
+            final_out(p, b, r0, c0, lane, v, tile);
+            __syncwarp();
+            continue;
+          }
+          store_block_row(x_block(p.x, p.sh, b, r0 >> 5, c0 >> 5), lane, v);
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] *= kXScale;
+        }
+        if (lane == 0) tc::bulk_wait_read_1();  // the slab's previous store has read it
         __syncwarp();
+        put_block(&tmOut, b * p.sh.sp, r0, c0, lane, v, MODE != APPLY && r0 != c0, slabs + slab * 2 * SLAB_BYTES);
+        slab ^= 1;
       }
     }
+    if (lane == 0) tc::bulk_wait_all();
   }
   tc::fence_before_sync();
   if (CG == 2) cluster_sync_all();
@@ -632,7 +715,13 @@ __global__ void __launch_bounds__(256) gram_sum_kernel(const MmArgs p) {
 #pragma unroll
     for (int j = 0; j < 32; ++j) v[j] += t[j];
   }
-  gram_out(p, b, r0, c0, lane, v);
+  gram_of(p, b, r0, c0, lane, v);
+  uint16_t* a = p.a16 + static_cast<int64_t>(b) * p.sh.sp * p.sh.sp;
+  store_half_row(a + static_cast<int64_t>(r0 + lane) * p.sh.sp + c0, v);
+  if (r0 != c0)
+    mirrored(lane, v, [&](int j, uint32_t w) {
+      *reinterpret_cast<uint32_t*>(a + static_cast<int64_t>(c0 + j) * p.sh.sp + r0 + (lane & ~1)) = w;
+    });
 }
 
 // ---------------------------------------------------------------- host
@@ -657,7 +746,7 @@ Plan plan_of(int64_t batch, int64_t sp, int64_t lp) {
 }
 
 struct Layout {
-  size_t x, x16a, x16b, a16, b16, d, e, inv, partial, parts, bytes;
+  size_t x, x16a, x16b, a16, a_blk, b16, d, e, inv, partial, parts, bytes;
   int32_t n_parts;  // partial sums of squares per matrix
 };
 
@@ -689,6 +778,7 @@ Layout layout_of(const Shape& s) {
   w.x16a = take(B * sp * lp * 2);
   w.x16b = take(B * sp * lp * 2);
   w.a16 = take(B * sp * sp * 2);
+  w.a_blk = take(B * sp * sp * 2);
   w.b16 = take(B * sp * sp * 2);
   w.d = take(B * sp * 4);
   w.e = take(B * sp * 4);
@@ -746,12 +836,13 @@ rl_status allow_smem() {
 }
 
 template <int MODE, int CG>
-rl_status product(const CUtensorMap& a, const CUtensorMap& b, const MmArgs& p, cudaStream_t s) {
+rl_status product(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& out, const MmArgs& p, cudaStream_t s) {
   rl_status st = allow_smem<MODE, CG>();
   if (st != RL_OK) return st;
   const int64_t items = static_cast<int64_t>(p.sh.batch) * p.per * (MODE == GRAM ? p.splits : 1);
   const int64_t units = std::min<int64_t>(items, kSMs / CG);
-  return launch("product_kernel launch", product_kernel<MODE, CG>, units * CG, kThreads, kSmem, CG, s, a, b, p);
+  return launch("product_kernel launch", product_kernel<MODE, CG>, units * CG, kThreads, kSmem, CG, s, a, b, out,
+                p);
 }
 
 }  // namespace muon
@@ -828,7 +919,6 @@ rl_status rl_muon_update(int32_t batch, int64_t m, int64_t n, const void* grad, 
   pa.grad = grad;
   pa.ld_grad = ld_grad;
   pa.stride_grad = stride_grad;
-  pa.grad_bf16 = grad_dtype == RL_BF16;
   pa.momentum = P.momentum > 0.f ? momentum : nullptr;
   pa.mu = P.momentum;
   pa.nesterov = P.nesterov;
@@ -840,8 +930,9 @@ rl_status rl_muon_update(int32_t batch, int64_t m, int64_t n, const void* grad, 
   pa.inv = reinterpret_cast<float*>(base + w.inv);
   pa.done = reinterpret_cast<uint32_t*>(base + kWsMuonDoneOffset);
   pa.status = status;
-  st = launch("momentum_kernel launch", momentum_kernel, static_cast<int64_t>(batch) * w.n_parts, kPrepWarps * 32, 0, 1,
-              s, pa);
+  auto momentum_pass = grad_dtype == RL_BF16 ? momentum_kernel<true> : momentum_kernel<false>;
+  st = launch("momentum_kernel launch", momentum_pass, static_cast<int64_t>(batch) * w.n_parts, kPrepWarps * 32, 0, 1, s,
+              pa);
   if (st != RL_OK) return st;
   const int64_t blocks = static_cast<int64_t>(batch) * (sh.sp / 32) * (sh.lp / 32);
   st = launch("normalise_kernel launch", normalise_kernel, (blocks + kPrepWarps - 1) / kPrepWarps, kPrepWarps * 32, 0, 1,
@@ -849,18 +940,22 @@ rl_status rl_muon_update(int32_t batch, int64_t m, int64_t n, const void* grad, 
   if (st != RL_OK) return st;
 
   // operand maps: K-major boxes of 64 x 128 rows; X as the right operand of B X in boxes of 64 columns
-  // by 64 rows
+  // by 64 rows; outputs in boxes of 32 x 32
   uint16_t* x16[2] = {reinterpret_cast<uint16_t*>(base + w.x16a), reinterpret_cast<uint16_t*>(base + w.x16b)};
-  CUtensorMap xk[2], xn[2], ak, bk;
+  CUtensorMap xk[2], xn[2], xo[2], ak, ao, bk, bo;
   const int64_t rows = static_cast<int64_t>(batch) * sh.sp;
   const auto F16 = CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
-  const auto SW = CU_TENSOR_MAP_SWIZZLE_128B;
+  const auto SW = CU_TENSOR_MAP_SWIZZLE_128B, SW64 = CU_TENSOR_MAP_SWIZZLE_64B;
+  const int64_t xs = static_cast<int64_t>(sh.lp) * 2, ss = static_cast<int64_t>(sh.sp) * 2;  // row strides
   for (int k = 0; k < 2 && st == RL_OK; ++k) {
-    st = tmap_2d(&xk[k], F16, x16[k], sh.lp, rows, static_cast<int64_t>(sh.lp) * 2, BK, 128, SW);
-    if (st == RL_OK) st = tmap_2d(&xn[k], F16, x16[k], sh.lp, rows, static_cast<int64_t>(sh.lp) * 2, 64, BK, SW);
+    st = tmap_2d(&xk[k], F16, x16[k], sh.lp, rows, xs, BK, 128, SW);
+    if (st == RL_OK) st = tmap_2d(&xn[k], F16, x16[k], sh.lp, rows, xs, 64, BK, SW);
+    if (st == RL_OK) st = tmap_2d(&xo[k], F16, x16[k], sh.lp, rows, xs, 32, 32, SW64);
   }
-  if (st == RL_OK) st = tmap_2d(&ak, F16, base + w.a16, sh.sp, rows, static_cast<int64_t>(sh.sp) * 2, BK, 128, SW);
-  if (st == RL_OK) st = tmap_2d(&bk, F16, base + w.b16, sh.sp, rows, static_cast<int64_t>(sh.sp) * 2, BK, 128, SW);
+  if (st == RL_OK) st = tmap_2d(&ak, F16, base + w.a16, sh.sp, rows, ss, BK, 128, SW);
+  if (st == RL_OK) st = tmap_2d(&ao, F16, base + w.a16, sh.sp, rows, ss, 32, 32, SW64);
+  if (st == RL_OK) st = tmap_2d(&bk, F16, base + w.b16, sh.sp, rows, ss, BK, 128, SW);
+  if (st == RL_OK) st = tmap_2d(&bo, F16, base + w.b16, sh.sp, rows, ss, 32, 32, SW64);
   if (st != RL_OK) return st;
 
   const Plan plan = plan_of(batch, sh.sp, sh.lp);
@@ -870,7 +965,7 @@ rl_status rl_muon_update(int32_t batch, int64_t m, int64_t n, const void* grad, 
   a.cb = P.ns_coef[1];
   a.cc = P.ns_coef[2];
   a.a16 = reinterpret_cast<uint16_t*>(base + w.a16);
-  a.b16 = reinterpret_cast<uint16_t*>(base + w.b16);
+  a.a_blk = reinterpret_cast<uint16_t*>(base + w.a_blk);
   a.d = reinterpret_cast<float*>(base + w.d);
   a.e = reinterpret_cast<float*>(base + w.e);
   a.x = pa.x;
@@ -890,7 +985,8 @@ rl_status rl_muon_update(int32_t batch, int64_t m, int64_t n, const void* grad, 
     a.per = static_cast<int32_t>(tri(a.nt_m));
     a.splits = plan.splits;
     a.nkb = sh.lp / BK;
-    st = plan.cg_sym == 2 ? product<GRAM, 2>(xk[k & 1], xk[k & 1], a, s) : product<GRAM, 1>(xk[k & 1], xk[k & 1], a, s);
+    st = plan.cg_sym == 2 ? product<GRAM, 2>(xk[k & 1], xk[k & 1], ao, a, s)
+                          : product<GRAM, 1>(xk[k & 1], xk[k & 1], ao, a, s);
     if (st != RL_OK) return st;
     if (plan.splits > 1) {
       const int64_t warps = static_cast<int64_t>(batch) * a.per * (T / 32) * (T / 32);
@@ -900,16 +996,16 @@ rl_status rl_muon_update(int32_t batch, int64_t m, int64_t n, const void* grad, 
     }
     a.splits = 1;
     a.nkb = sh.sp / BK;
-    st = plan.cg_sym == 2 ? product<POLY, 2>(ak, ak, a, s) : product<POLY, 1>(ak, ak, a, s);
+    st = plan.cg_sym == 2 ? product<POLY, 2>(ak, ak, bo, a, s) : product<POLY, 1>(ak, ak, bo, a, s);
     if (st != RL_OK) return st;
     const int TA = 128 * plan.cg_apply;
     a.nt_m = static_cast<int32_t>(round_up(sh.sp, TA) / TA);
     a.nt_n = static_cast<int32_t>(round_up(sh.lp, TA) / TA);
     a.per = a.nt_m * a.nt_n;
-    a.x16_out = x16[(k + 1) & 1];
     a.inv = k == 0 ? pa.inv : nullptr;
     a.final_step = k == P.ns_steps - 1;
-    st = plan.cg_apply == 2 ? product<APPLY, 2>(bk, xn[k & 1], a, s) : product<APPLY, 1>(bk, xn[k & 1], a, s);
+    st = plan.cg_apply == 2 ? product<APPLY, 2>(bk, xn[k & 1], xo[(k + 1) & 1], a, s)
+                            : product<APPLY, 1>(bk, xn[k & 1], xo[(k + 1) & 1], a, s);
     if (st != RL_OK) return st;
   }
   return RL_OK;
