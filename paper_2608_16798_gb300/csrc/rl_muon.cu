@@ -48,9 +48,13 @@ __host__ __device__ inline int64_t round_up(int64_t x, int64_t to) { return (x +
 //
 // X (fp32) lies in blocks of 32 x 32: block (R, C) of a matrix at (R * l32 + C) * 1024, and in a
 // block element (r, c) at (c / 4) * 128 + r * 4 + c % 4, so that a warp whose lanes hold one row each
-// moves 512 contiguous bytes per instruction. The fp16 operands are row-major, as TMA reads them; of A's
-// blocks on and above the diagonal there is a second copy, in blocks for the epilogue of B, where element
-// (r, c) lies at (c / 8) * 256 + r * 8 + c % 8.
+// moves 512 contiguous bytes per instruction. It is held times 2^12, as its fp16 copy is.
+//
+// The fp16 operands are row-major, as TMA reads them. Of the symmetric matrices A and B only the 256 x
+// 256 tiles on and above the diagonal are formed and stored: where a product wants a block from below
+// it, the block's mirror image is loaded and the MMA told that the operand lies the other way round
+// (MN-major). Of A there is a second copy, in blocks for the epilogue of B, where element (r, c) lies at
+// (c / 8) * 256 + r * 8 + c % 8.
 
 struct Shape {
   int32_t batch, m, n;   // the caller's matrices
@@ -98,19 +102,6 @@ __device__ __forceinline__ void store_half_row(uint16_t* to, const float (&v)[32
     *reinterpret_cast<uint4*>(to + 8 * j) =
         make_uint4(pack_half2(v[8 * j], v[8 * j + 1]), pack_half2(v[8 * j + 2], v[8 * j + 3]),
                    pack_half2(v[8 * j + 4], v[8 * j + 5]), pack_half2(v[8 * j + 6], v[8 * j + 7]));
-}
-
-// The mirror image of a 32 x 32 block whose rows the lanes hold, in pairs of fp16: lanes 2k and 2k + 1
-// exchange one of every two columns, so that f(j, w) gets in w column j (j even in even lanes, odd in
-// odd ones) of rows lane & ~1 and its neighbour.
-template <typename F>
-__device__ __forceinline__ void mirrored(int lane, const float (&v)[32], F f) {
-  const int odd = lane & 1;
-#pragma unroll
-  for (int j = 0; j < 32; j += 2) {
-    const float got = __shfl_xor_sync(0xffffffffu, odd ? v[j] : v[j + 1], 1);
-    f(j + odd, odd ? pack_half2(got, v[j + 1]) : pack_half2(v[j], got));
-  }
 }
 
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
@@ -235,7 +226,8 @@ __global__ void __launch_bounds__(kPrepWarps * 32) momentum_kernel(const PrepArg
     s = warp_sum(s);
     if (lane == 0) {
       if (!(s <= 1.7e308)) flag_status(p.status, RL_DEV_BAD_VALUE);
-      p.inv[k] = static_cast<float>(1.0 / (sqrt(s) + static_cast<double>(p.eps)));
+      // finite also for a zero matrix without eps, whose X is 0
+      p.inv[k] = static_cast<float>(fmin(1.0 / (sqrt(s) + static_cast<double>(p.eps)), 3e38));
     }
   }
   if (threadIdx.x == 0) *p.done = 0;
@@ -267,8 +259,8 @@ enum Mode { GRAM = 0, POLY = 1, APPLY = 2 };
 
 struct MmArgs {
   Shape sh;
-  int32_t nt_m, nt_n;    // tiles of the product's rows and columns (GRAM, POLY: of both)
-  int32_t per;           // tiles of one matrix (GRAM, POLY: on and above the diagonal)
+  int32_t nt_m, nt_n;    // tiles of the product's rows and columns
+  int32_t per;           // items of one matrix (GRAM, POLY: see symmetric_tile)
   int32_t nkb;           // 64-element blocks of the contraction
   int32_t splits;        // GRAM: parts of the contraction, each an item
   float ca, cb, cc;      // the step's coefficients
@@ -281,12 +273,12 @@ struct MmArgs {
   float* parts;          // GRAM with splits > 1: [split][tile][TILE x TILE] sums
   // the last step's outputs
   int32_t final_step;
-  float scale;           // of the update
+  float scale;           // of the update, 2^-12 taken in
   uint16_t* update;      // bf16 [batch x m x n] or null
   float* weights;
   uint16_t* weights_bf16;
   int64_t ld_w, stride_w;
-  float decay, step;     // w <- decay w - step O
+  float decay, step;     // w <- decay w - step (2^12 X)
   int32_t* status;
 };
 
@@ -297,23 +289,30 @@ constexpr uint32_t HALF_BYTES = 64 * BK * 2;
 constexpr int NS = 5;
 constexpr int kEpiWarps = 8;
 constexpr int kThreads = 64 + 32 * kEpiWarps;  // warp 0 TMA, warp 1 MMA, then the epilogue
-constexpr uint32_t SLAB_BYTES = 2048;          // a 32 x 32 fp16 block on its way out
-constexpr uint32_t EPI_BYTES = 4 * SLAB_BYTES; // per epilogue warp: two blocks and their mirror images
+constexpr uint32_t SLAB_BYTES = 4096;          // 32 x 64 fp16 values on their way out
+constexpr uint32_t EPI_BYTES = 2 * SLAB_BYTES; // per epilogue warp
 constexpr size_t kSmem = NS * STAGE_BYTES + kEpiWarps * EPI_BYTES + 1024;
 static_assert(kSmem <= 232448 - 1024, "shared memory of the product kernels");
 
-// fp16 operands, fp32 accumulator, M x N; B MN-major for APPLY.
-constexpr uint32_t idesc_f16(int M, int N, bool b_mn) {
-  return (1u << 4) | (b_mn ? (1u << 16) : 0u) | (static_cast<uint32_t>(N >> 3) << 17) |
+// fp16 operands, fp32 accumulator, M x N; A and/or B MN-major.
+__host__ __device__ constexpr uint32_t idesc_f16(int M, int N, bool a_mn, bool b_mn) {
+  return (1u << 4) | (a_mn ? (1u << 15) : 0u) | (b_mn ? (1u << 16) : 0u) | (static_cast<uint32_t>(N >> 3) << 17) |
          (static_cast<uint32_t>(M >> 4) << 24);
 }
 
-// Tile t of those on and above the diagonal: column by column.
-__device__ __forceinline__ void triangle(int t, int& i, int& j) {
-  j = static_cast<int>((sqrtf(8.f * t + 1.f) - 1.f) * 0.5f);
-  while (j * (j + 1) / 2 > t) --j;
-  while ((j + 1) * (j + 2) / 2 <= t) ++j;
-  i = t - j * (j + 1) / 2;
+// Item t of a symmetric product: the 256 x 256 tiles on and above the diagonal column by column, and
+// with 128 x 128 tiles the four parts of each of them. False where the matrix has no such part.
+template <int CG>
+__device__ __forceinline__ bool symmetric_tile(int t, int nt, int& i, int& j) {
+  const int big = CG == 2 ? t : t >> 2;
+  j = static_cast<int>((sqrtf(8.f * big + 1.f) - 1.f) * 0.5f);
+  while (j * (j + 1) / 2 > big) --j;
+  while ((j + 1) * (j + 2) / 2 <= big) ++j;
+  i = big - j * (j + 1) / 2;
+  if (CG == 2) return true;
+  i = 2 * i + (t & 1);
+  j = 2 * j + (t >> 1 & 1);
+  return i < nt && j < nt;
 }
 
 // Two-dimensional bulk store of a slab (bulk-group completion).
@@ -322,28 +321,18 @@ __device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, int c0, int
                :: "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(smem_addr(src)) : "memory");
 }
 
-// A 32 x 32 block out through shared memory: 64-byte rows with the 64-byte swizzle (16-byte chunk k of
-// row r at chunk k ^ (r / 2) % 4). `mirror`: also its mirror image, at (c0, r0) of the same matrix, whose
-// rows begin at row0 of the map. slab: two blocks of SLAB_BYTES that no store is reading.
-__device__ __forceinline__ void put_block(const CUtensorMap* map, int row0, int r0, int c0, int lane,
-                                          const float (&v)[32], bool mirror, uint8_t* slab) {
+// 32 values of a lane's row as fp16 into half `h` of a slab: 32 rows of 128 bytes with the 128-byte
+// swizzle (16-byte chunk k of row r at chunk k ^ r % 8).
+__device__ __forceinline__ void fill_slab(uint8_t* slab, int h, int lane, const uint4 (&w)[4]) {
 #pragma unroll
   for (int k = 0; k < 4; ++k)
-    *reinterpret_cast<uint4*>(slab + lane * 64 + ((k ^ ((lane >> 1) & 3)) << 4)) =
-        make_uint4(pack_half2(v[8 * k], v[8 * k + 1]), pack_half2(v[8 * k + 2], v[8 * k + 3]),
-                   pack_half2(v[8 * k + 4], v[8 * k + 5]), pack_half2(v[8 * k + 6], v[8 * k + 7]));
-  if (mirror)
-    mirrored(lane, v, [&](int j, uint32_t w) {
-      *reinterpret_cast<uint32_t*>(slab + SLAB_BYTES + j * 64 + (((lane >> 3) ^ ((j >> 1) & 3)) << 4) +
-                                   ((lane & 6) << 1)) = w;
-    });
-  fence_proxy_async_smem();
-  __syncwarp();
-  if (lane == 0) {
-    tma_store_2d(map, c0, row0 + r0, slab);
-    if (mirror) tma_store_2d(map, r0, row0 + c0, slab + SLAB_BYTES);
-    bulk_commit();
-  }
+    *reinterpret_cast<uint4*>(slab + lane * 128 + (((4 * h + k) ^ (lane & 7)) << 4)) = w[k];
+}
+__device__ __forceinline__ void pack_row(const float (&v)[32], uint4 (&w)[4]) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    w[k] = make_uint4(pack_half2(v[8 * k], v[8 * k + 1]), pack_half2(v[8 * k + 2], v[8 * k + 3]),
+                      pack_half2(v[8 * k + 4], v[8 * k + 5]), pack_half2(v[8 * k + 6], v[8 * k + 7]));
 }
 
 __device__ __forceinline__ uint16_t* a_block(const MmArgs& p, int b, int r0, int c0) {
@@ -351,8 +340,10 @@ __device__ __forceinline__ uint16_t* a_block(const MmArgs& p, int b, int r0, int
   return p.a_blk + ((static_cast<int64_t>(b) * nb + (r0 >> 5)) * nb + (c0 >> 5)) * 1024;
 }
 
-// What becomes of a 32 x 32 block (lane: row) of X X^T, scaled by 2^24: A off its diagonal, scaled.
-__device__ __forceinline__ void gram_of(const MmArgs& p, int b, int r0, int c0, int lane, float (&v)[32]) {
+// What becomes of a 32 x 32 block (lane: row) of X X^T, scaled by 2^24: A off its diagonal, scaled, in w
+// and in its block.
+__device__ __forceinline__ void gram_of(const MmArgs& p, int b, int r0, int c0, int lane, float (&v)[32],
+                                        uint4 (&w)[4]) {
 #pragma unroll
   for (int j = 0; j < 32; ++j) v[j] *= kAScale / (kXScale * kXScale);
   if (r0 == c0) {
@@ -363,38 +354,45 @@ __device__ __forceinline__ void gram_of(const MmArgs& p, int b, int r0, int c0, 
         v[j] = 0.f;
       }
   }
+  pack_row(v, w);
   uint16_t* blk = a_block(p, b, r0, c0) + lane * 8;
 #pragma unroll
-  for (int k = 0; k < 4; ++k)
-    *reinterpret_cast<uint4*>(blk + k * 256) =
-        make_uint4(pack_half2(v[8 * k], v[8 * k + 1]), pack_half2(v[8 * k + 2], v[8 * k + 3]),
-                   pack_half2(v[8 * k + 4], v[8 * k + 5]), pack_half2(v[8 * k + 6], v[8 * k + 7]));
+  for (int k = 0; k < 4; ++k) *reinterpret_cast<uint4*>(blk + k * 256) = w[k];
 }
 
 // The same of Ao Ao, scaled by 2^24: B off its diagonal, scaled. a: this lane's row of the block of A;
-// di, dj: the diagonal at its row, and at the block's columns, one per lane.
+// di: the diagonal of A at its row.
 __device__ __forceinline__ void poly_of(const MmArgs& p, int b, int r0, int c0, int lane, float (&v)[32],
-                                        const uint4 (&a)[4], float di, float dj) {
-  const bool on_diagonal = r0 == c0;
+                                        const uint4 (&a)[4], float di) {
+  const int64_t row = static_cast<int64_t>(b) * p.sh.sp;
+  if (r0 == c0) {
+#pragma unroll
+    for (int j = 0; j < 32; ++j)
+      if (j == lane)
+        p.e[row + r0 + lane] = p.ca + fmaf(p.cb, di, p.cc * fmaf(di, di, v[j] * (1.f / (kAScale * kAScale))));
+  }
+  // B_ij = h_ij (k1 + k2 d_j) + k3 v_ij with h the fp16 value of A_ij and k1 for this row
+  const float k2 = p.cc * (kBScale / kAScale), k3 = p.cc * (kBScale / (kAScale * kAScale));
+  const float k1 = fmaf(k2, di, p.cb * (kBScale / kAScale));
+  const float4* d = reinterpret_cast<const float4*>(p.d + row + c0);
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
     const uint32_t w[4] = {a[k].x, a[k].y, a[k].z, a[k].w};
 #pragma unroll
-    for (int h = 0; h < 4; ++h) {
-      const float2 ao = unpack_half2(w[h]);
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int j = 8 * k + 2 * h + i;
-        const float x = (i ? ao.y : ao.x) * (1.f / kAScale);
-        const float dc = __shfl_sync(0xffffffffu, dj, j);
-        const float sq = v[j] * (1.f / (kAScale * kAScale));
-        v[j] = kBScale * fmaf(p.cb, x, p.cc * fmaf(di + dc, x, sq));
-        if (on_diagonal && j == lane) {
-          p.e[static_cast<int64_t>(b) * p.sh.sp + r0 + lane] = p.ca + fmaf(p.cb, di, p.cc * fmaf(di, di, sq));
-          v[j] = 0.f;
-        }
-      }
+    for (int h = 0; h < 2; ++h) {
+      const float4 dj = d[2 * k + h];
+      const float2 a0 = unpack_half2(w[2 * h]), a1 = unpack_half2(w[2 * h + 1]);
+      float* o = v + 8 * k + 4 * h;
+      o[0] = fmaf(a0.x, fmaf(k2, dj.x, k1), k3 * o[0]);
+      o[1] = fmaf(a0.y, fmaf(k2, dj.y, k1), k3 * o[1]);
+      o[2] = fmaf(a1.x, fmaf(k2, dj.z, k1), k3 * o[2]);
+      o[3] = fmaf(a1.y, fmaf(k2, dj.w, k1), k3 * o[3]);
     }
+  }
+  if (r0 == c0) {
+#pragma unroll
+    for (int j = 0; j < 32; ++j)
+      if (j == lane) v[j] = 0.f;
   }
 }
 
@@ -443,6 +441,7 @@ __device__ __forceinline__ void final_out(const MmArgs& p, int b, int r0, int c0
 // products of the next.
 template <int MODE, int CG>
 __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_constant__ CUtensorMap tmA,
+                                                              const __grid_constant__ CUtensorMap tmAt,
                                                               const __grid_constant__ CUtensorMap tmB,
                                                               const __grid_constant__ CUtensorMap tmOut,
                                                               const MmArgs p) {
@@ -480,8 +479,8 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
   pdl_launch();
   pdl_wait();
 
-  // item -> matrix, tile row and column, K blocks
-  auto decode = [&](int item, int& b, int& ti, int& tj, int& kb0, int& nkb) {
+  // item -> matrix, tile row and column, K blocks; false if there is no such tile
+  auto decode = [&](int item, int& b, int& ti, int& tj, int& kb0, int& nkb) -> bool {
     int part = 0;
     if (MODE == GRAM && p.splits > 1) {
       part = item / n_tiles;
@@ -489,15 +488,15 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
     }
     b = item / p.per;
     const int t = item - b * p.per;
-    if (MODE == APPLY) {
-      ti = t % p.nt_m;
-      tj = t / p.nt_m;
-    } else {
-      triangle(t, ti, tj);
-    }
     kb0 = MODE == GRAM ? static_cast<int>(static_cast<int64_t>(part) * p.nkb / p.splits) : 0;
     nkb = (MODE == GRAM ? static_cast<int>(static_cast<int64_t>(part + 1) * p.nkb / p.splits) : p.nkb) - kb0;
+    if (MODE != APPLY) return symmetric_tile<CG>(t, p.nt_m, ti, tj);
+    ti = t % p.nt_m;
+    tj = t / p.nt_m;
+    return true;
   };
+  // whether K block k0 of an operand's rows m0 .. of a symmetric matrix is stored the other way round
+  auto below = [](int m0, int k0) { return (k0 >> 8) < (m0 >> 8); };
 
   if (warp == 0) {
     if (lane == 0) {
@@ -507,9 +506,9 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
       bool ok = true;
       for (int item = unit; item < n_items && ok; item += units) {
         int b, ti, tj, kb0, nkb;
-        decode(item, b, ti, tj, kb0, nkb);
-        const int m0 = b * p.sh.sp + ti * TILE + static_cast<int>(rank) * 128;
-        const int n0 = tj * TILE + static_cast<int>(rank) * 128;
+        if (!decode(item, b, ti, tj, kb0, nkb)) continue;
+        const int y0 = b * p.sh.sp;  // the matrix's first row in the maps
+        const int m0 = ti * TILE + static_cast<int>(rank) * 128, n0 = tj * TILE + static_cast<int>(rank) * 128;
         for (int kb = 0; kb < nkb; ++kb, ++g) {
           const int s = g % NS;
           const int k0 = (kb0 + kb) * BK;
@@ -521,36 +520,38 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
           }
           uint8_t* st = sm + s * STAGE_BYTES;
           if (rank == 0) mbar_arrive_expect_tx(&full[s], CG * STAGE_BYTES);
-          if (CG == 2) {
-            const uint32_t bar = map_to_rank(smem_addr(&full[s]), 0);
-            tc::tma_load_2d_pair(st, &tmA, k0, m0, bar);
-            if (MODE == APPLY) {
-              tc::tma_load_2d_pair(st + A_BYTES, &tmB, n0, b * p.sh.sp + k0, bar);
-              tc::tma_load_2d_pair(st + A_BYTES + HALF_BYTES, &tmB, n0 + 64, b * p.sh.sp + k0, bar);
-            } else {
-              tc::tma_load_2d_pair(st + A_BYTES, &tmB, k0, b * p.sh.sp + n0, bar);
-            }
+          const uint32_t bar = CG == 2 ? map_to_rank(smem_addr(&full[s]), 0) : 0;
+          auto load = [&](uint8_t* dst, const CUtensorMap* map, int c0, int c1) {
+            if (CG == 2) tc::tma_load_2d_pair(dst, map, c0, c1, bar);
+            else tc::tma_load_2d(dst, map, c0, c1, &full[s]);
+          };
+          if (MODE != GRAM && below(m0, k0)) {
+            load(st, &tmAt, m0, y0 + k0);
+            load(st + HALF_BYTES, &tmAt, m0 + 64, y0 + k0);
           } else {
-            tc::tma_load_2d(st, &tmA, k0, m0, &full[s]);
-            if (MODE == APPLY) {
-              tc::tma_load_2d(st + A_BYTES, &tmB, n0, b * p.sh.sp + k0, &full[s]);
-              tc::tma_load_2d(st + A_BYTES + HALF_BYTES, &tmB, n0 + 64, b * p.sh.sp + k0, &full[s]);
-            } else {
-              tc::tma_load_2d(st + A_BYTES, &tmB, k0, b * p.sh.sp + n0, &full[s]);
-            }
+            load(st, &tmA, k0, y0 + m0);
+          }
+          if (MODE == APPLY || (MODE == POLY && below(n0, k0))) {
+            const CUtensorMap* map = MODE == APPLY ? &tmB : &tmAt;
+            load(st + A_BYTES, map, n0, y0 + k0);
+            load(st + A_BYTES + HALF_BYTES, map, n0 + 64, y0 + k0);
+          } else {
+            load(st + A_BYTES, &tmA, k0, y0 + n0);
           }
         }
       }
     }
   } else if (warp == 1) {
     if (lane == 0 && rank == 0) {
-      constexpr uint32_t idesc = idesc_f16(TILE, TILE, MODE == APPLY);
       uint32_t g = 0;
       bool ok = true;
       uint32_t t = 0;
       for (int item = unit; item < n_items && ok; item += units, ++t) {
         int b, ti, tj, kb0, nkb;
-        decode(item, b, ti, tj, kb0, nkb);
+        if (!decode(item, b, ti, tj, kb0, nkb)) {
+          --t;  // not a use of an accumulator
+          continue;
+        }
         const uint32_t buf = t & 1;
         if (t >= 2) {
           const bool got = CG == 2 ? mbar_wait_cluster_bounded(&acce[buf], ((t >> 1) - 1) & 1)
@@ -571,11 +572,16 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
           }
           tc::fence_after_sync();
           const uint32_t a = smem_addr(sm + s * STAGE_BYTES), bb = a + A_BYTES;
+          const int k0 = (kb0 + kb) * BK;
+          const bool a_mn = MODE != GRAM && below(ti * TILE, k0);
+          const bool b_mn = MODE == APPLY || (MODE == POLY && below(tj * TILE, k0));
+          const uint32_t idesc = idesc_f16(TILE, TILE, a_mn, b_mn);
 #pragma unroll
           for (int k = 0; k < BK / 16; ++k) {
-            const uint64_t ad = tc::desc_kmajor_sw128(a + k * 32);
-            const uint64_t bd = MODE == APPLY ? tc::desc_mnmajor_sw128(bb + k * 2048, HALF_BYTES, 1024)
-                                              : tc::desc_kmajor_sw128(bb + k * 32);
+            const uint64_t ad = a_mn ? tc::desc_mnmajor_sw128(a + k * 2048, HALF_BYTES, 1024)
+                                     : tc::desc_kmajor_sw128(a + k * 32);
+            const uint64_t bd = b_mn ? tc::desc_mnmajor_sw128(bb + k * 2048, HALF_BYTES, 1024)
+                                     : tc::desc_kmajor_sw128(bb + k * 32);
             if (CG == 2) tc::mma_bf16_pair(acc, ad, bd, idesc, (kb | k) != 0 ? 1u : 0u);
             else tc::mma_bf16(acc, ad, bd, idesc, (kb | k) != 0 ? 1u : 0u);
           }
@@ -588,57 +594,53 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
       }
     }
   } else {
-    // Two warps per TMEM lane quarter take the tile's 32-column blocks in turn. What a block needs from
-    // memory is loaded one block ahead, the first before the products are done.
-    const int q = warp & 3, half = (warp - 2) >> 2;
+    // Two warps per TMEM lane quarter, each with half of the tile's 32-column blocks. What a block needs
+    // from memory is loaded one block ahead, the first before the products are done.
+    constexpr int NBLK = TILE / 64;
+    const int q = warp & 3, first = ((warp - 2) >> 2) * NBLK;
     uint8_t* slabs = sm + NS * STAGE_BYTES + (warp - 2) * EPI_BYTES;
     float(*tile)[33] = reinterpret_cast<float(*)[33]>(slabs);
     uint32_t slab = 0;
     uint32_t t = 0;
-    for (int item = unit; item < n_items; item += units, ++t) {
+    for (int item = unit; item < n_items; item += units) {
       int b, ti, tj, kb0, nkb;
-      decode(item, b, ti, tj, kb0, nkb);
-      const uint32_t buf = t & 1;
+      if (!decode(item, b, ti, tj, kb0, nkb)) continue;
+      const uint32_t buf = t & 1, phase = (t >> 1) & 1;
+      ++t;
       const int r0 = ti * TILE + static_cast<int>(rank) * 128 + 32 * q;
-      const uint32_t tq = tmem + buf * TILE + (static_cast<uint32_t>(32 * q) << 16);
       const int cols = MODE == APPLY ? p.sh.lp : p.sh.sp;
+      // the 64-column halves past the matrix are another one's or nothing
+      const int blocks = r0 < p.sh.sp ? min(NBLK, (cols - tj * TILE) / 32 - first) : 0;
+      const int cb = tj * TILE + first * 32;  // the warp's first column
       const bool in_parts = MODE == GRAM && p.splits > 1;
-      // blocks past the matrix are another one's or nothing; in a tile on the diagonal of a symmetric
-      // product those below it are the mirror image of those above
-      auto wanted = [&](int c) {
-        const int c0 = tj * TILE + c * 32;
-        return c < TILE / 32 && r0 < p.sh.sp && c0 < cols && (MODE == APPLY || in_parts || ti != tj || c0 >= r0);
-      };
       float x[32], f = 0.f;
       uint4 a[4];
-      float di = 0.f, dj = 0.f;
-      auto prefetch = [&](int c) {
-        if (!wanted(c)) return;
-        const int c0 = tj * TILE + c * 32;
-        if (MODE == APPLY) load_block_row(x_block(p.x, p.sh, b, r0 >> 5, c0 >> 5), lane, x);
+      auto prefetch = [&](int i) {
+        if (i >= blocks) return;
+        if (MODE == APPLY) load_block_row(x_block(p.x, p.sh, b, r0 >> 5, (cb >> 5) + i), lane, x);
         if (MODE == POLY) {
-          const uint16_t* blk = a_block(p, b, r0, c0) + lane * 8;
+          const uint16_t* blk = a_block(p, b, r0, cb + 32 * i) + lane * 8;
 #pragma unroll
           for (int k = 0; k < 4; ++k) a[k] = *reinterpret_cast<const uint4*>(blk + k * 256);
-          dj = p.d[static_cast<int64_t>(b) * p.sh.sp + c0 + lane];
         }
       };
       if (r0 < p.sh.sp) {
         const int64_t row = static_cast<int64_t>(b) * p.sh.sp + r0 + lane;
-        if (MODE == APPLY) f = p.inv ? p.e[row] * p.inv[b] : p.e[row];
-        if (MODE == POLY) di = p.d[row];
+        if (MODE == APPLY) f = p.e[row];
+        if (MODE == POLY) f = p.d[row];
       }
-      prefetch(half);
-      if (!mbar_wait_sleep_bounded(&accf[buf], (t >> 1) & 1)) {
+      prefetch(0);
+      if (!mbar_wait_sleep_bounded(&accf[buf], phase)) {
         if (lane == 0) flag_status(p.status, RL_DEV_TIMEOUT);
         break;
       }
       tc::fence_after_sync();
+      const uint32_t tq = tmem + buf * TILE + (static_cast<uint32_t>(32 * q) << 16) + first * 32;
 #pragma unroll 1
-      for (int c = half; c < TILE / 32; c += 2) {
+      for (int i = 0; i < NBLK; ++i) {
         float v[32];
-        tc::tmem_ld32(tq + c * 32, v);
-        if (c + 2 >= TILE / 32) {
+        tc::tmem_ld32(tq + i * 32, v);
+        if (i == NBLK - 1) {
           tc::fence_before_sync();
           __syncwarp();
           if (lane == 0) {
@@ -646,23 +648,26 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
             else mbar_arrive(&acce[buf]);
           }
         }
-        if (!wanted(c)) {
-          prefetch(c + 2);
-          continue;
-        }
-        const int c0 = tj * TILE + c * 32;
+        if (i >= blocks) continue;
+        const int c0 = cb + 32 * i;
         if (in_parts) {
           store_block_row(p.parts + static_cast<int64_t>(item) * TILE * TILE +
-                              (static_cast<int64_t>((rank * 4 + q) * (TILE / 32) + c)) * 1024, lane, v);
+                              (static_cast<int64_t>((rank * 4 + q) * (TILE / 32) + first + i)) * 1024, lane, v);
           continue;
         }
-        if (MODE == GRAM) gram_of(p, b, r0, c0, lane, v);
-        if (MODE == POLY) poly_of(p, b, r0, c0, lane, v, a, di, dj);
+        uint4 w[4];
+        if (MODE == GRAM) gram_of(p, b, r0, c0, lane, v, w);
+        if (MODE == POLY) poly_of(p, b, r0, c0, lane, v, a, f);
         if (MODE == APPLY) {
+          if (p.inv) {
+            const float inv = p.inv[b];
 #pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] = fmaf(f, x[j], v[j] * (1.f / (kBScale * kXScale)));
+            for (int j = 0; j < 32; ++j) x[j] = x[j] * inv * kXScale;
+          }
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] = fmaf(f, x[j], v[j] * (1.f / kBScale));
         }
-        prefetch(c + 2);
+        prefetch(i + 1);
         if (MODE == APPLY) {
           if (p.final_step) {
             final_out(p, b, r0, c0, lane, v, tile);
@@ -670,13 +675,23 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
             continue;
           }
           store_block_row(x_block(p.x, p.sh, b, r0 >> 5, c0 >> 5), lane, v);
-#pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] *= kXScale;
         }
-        if (lane == 0) tc::bulk_wait_read_1();  // the slab's previous store has read it
-        __syncwarp();
-        put_block(&tmOut, b * p.sh.sp, r0, c0, lane, v, MODE != APPLY && r0 != c0, slabs + slab * 2 * SLAB_BYTES);
-        slab ^= 1;
+        if (MODE != GRAM) pack_row(v, w);
+        uint8_t* sb = slabs + slab * SLAB_BYTES;
+        if ((i & 1) == 0) {
+          if (lane == 0) tc::bulk_wait_read_1();  // the slab's previous store has read it
+          __syncwarp();
+        }
+        fill_slab(sb, i & 1, lane, w);
+        if (i & 1) {
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) {
+            tma_store_2d(&tmOut, c0 - 32, b * p.sh.sp + r0, sb);
+            bulk_commit();
+          }
+          slab ^= 1;
+        }
       }
     }
     if (lane == 0) tc::bulk_wait_all();
@@ -699,14 +714,14 @@ __global__ void __launch_bounds__(256) gram_sum_kernel(const MmArgs p) {
   pdl_launch();
   pdl_wait();
   const int n_tiles = p.sh.batch * p.per;
-  const int64_t w = static_cast<int64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5);
-  if (w >= static_cast<int64_t>(n_tiles) * NB * NB) return;
-  const int tile = static_cast<int>(w / (NB * NB)), in = static_cast<int>(w % (NB * NB));
+  const int64_t blk = static_cast<int64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5);
+  if (blk >= static_cast<int64_t>(n_tiles) * NB * NB) return;
+  const int tile = static_cast<int>(blk / (NB * NB)), in = static_cast<int>(blk % (NB * NB));
   const int b = tile / p.per;
   int ti, tj;
-  triangle(tile - b * p.per, ti, tj);
+  if (!symmetric_tile<CG>(tile - b * p.per, p.nt_m, ti, tj)) return;
   const int r0 = ti * TILE + in / NB * 32, c0 = tj * TILE + in % NB * 32;
-  if (r0 >= p.sh.sp || c0 >= p.sh.sp || (ti == tj && c0 < r0)) return;
+  if (r0 >= p.sh.sp || c0 >= p.sh.sp) return;
   float v[32], t[32];
   const float* src = p.parts + static_cast<int64_t>(tile) * TILE * TILE + static_cast<int64_t>(in) * 1024;
   load_block_row(src, lane, v);
@@ -715,13 +730,11 @@ __global__ void __launch_bounds__(256) gram_sum_kernel(const MmArgs p) {
 #pragma unroll
     for (int j = 0; j < 32; ++j) v[j] += t[j];
   }
-  gram_of(p, b, r0, c0, lane, v);
-  uint16_t* a = p.a16 + static_cast<int64_t>(b) * p.sh.sp * p.sh.sp;
-  store_half_row(a + static_cast<int64_t>(r0 + lane) * p.sh.sp + c0, v);
-  if (r0 != c0)
-    mirrored(lane, v, [&](int j, uint32_t w) {
-      *reinterpret_cast<uint32_t*>(a + static_cast<int64_t>(c0 + j) * p.sh.sp + r0 + (lane & ~1)) = w;
-    });
+  uint4 w[4];
+  gram_of(p, b, r0, c0, lane, v, w);
+  uint16_t* to = p.a16 + (static_cast<int64_t>(b) * p.sh.sp + r0 + lane) * p.sh.sp + c0;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) *reinterpret_cast<uint4*>(to + 8 * k) = w[k];
 }
 
 // ---------------------------------------------------------------- host
@@ -732,11 +745,15 @@ struct Plan {
   int cg_sym, cg_apply, splits;
 };
 
-inline int64_t tri(int64_t n) { return n * (n + 1) / 2; }
+// Items of a symmetric product of one matrix (symmetric_tile).
+inline int64_t symmetric_items(int64_t sp, int cg) {
+  const int64_t n = round_up(sp, 256) / 256;
+  return n * (n + 1) / 2 * (cg == 2 ? 1 : 4);
+}
 
 Plan plan_of(int64_t batch, int64_t sp, int64_t lp) {
   Plan p;
-  auto tiles_sym = [&](int cg) { return batch * tri(round_up(sp, 128 * cg) / (128 * cg)); };
+  auto tiles_sym = [&](int cg) { return batch * symmetric_items(sp, cg); };
   p.cg_sym = tiles_sym(2) >= kSMs / 2 ? 2 : 1;
   p.cg_apply = batch * (round_up(sp, 256) / 256) * (round_up(lp, 256) / 256) >= kSMs / 2 ? 2 : 1;
   const int64_t units = kSMs / p.cg_sym, tiles = tiles_sym(p.cg_sym);
@@ -786,7 +803,7 @@ Layout layout_of(const Shape& s) {
   w.partial = take(B * w.n_parts * 8);
   const Plan p = plan_of(s.batch, s.sp, s.lp);
   const size_t T = 128 * p.cg_sym;
-  w.parts = take(p.splits > 1 ? p.splits * B * tri(round_up(s.sp, T) / T) * T * T * 4 : 0);
+  w.parts = take(p.splits > 1 ? p.splits * B * symmetric_items(s.sp, p.cg_sym) * T * T * 4 : 0);
   w.bytes = at;
   return w;
 }
@@ -836,13 +853,14 @@ rl_status allow_smem() {
 }
 
 template <int MODE, int CG>
-rl_status product(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& out, const MmArgs& p, cudaStream_t s) {
+rl_status product(const CUtensorMap& a, const CUtensorMap& at, const CUtensorMap& b, const CUtensorMap& out,
+                  const MmArgs& p, cudaStream_t s) {
   rl_status st = allow_smem<MODE, CG>();
   if (st != RL_OK) return st;
   const int64_t items = static_cast<int64_t>(p.sh.batch) * p.per * (MODE == GRAM ? p.splits : 1);
   const int64_t units = std::min<int64_t>(items, kSMs / CG);
-  return launch("product_kernel launch", product_kernel<MODE, CG>, units * CG, kThreads, kSmem, CG, s, a, b, out,
-                p);
+  return launch("product_kernel launch", product_kernel<MODE, CG>, units * CG, kThreads, kSmem, CG, s, a, at, b,
+                out, p);
 }
 
 }  // namespace muon
@@ -939,23 +957,26 @@ rl_status rl_muon_update(int32_t batch, int64_t m, int64_t n, const void* grad, 
               s, pa);
   if (st != RL_OK) return st;
 
-  // operand maps: K-major boxes of 64 x 128 rows; X as the right operand of B X in boxes of 64 columns
-  // by 64 rows; outputs in boxes of 32 x 32
+  // boxes of 64 columns: 128 rows of a K-major operand, 64 of an MN-major one, 32 of an output
   uint16_t* x16[2] = {reinterpret_cast<uint16_t*>(base + w.x16a), reinterpret_cast<uint16_t*>(base + w.x16b)};
-  CUtensorMap xk[2], xn[2], xo[2], ak, ao, bk, bo;
+  CUtensorMap xk[2], xn[2], ak, at, bk, bt;
   const int64_t rows = static_cast<int64_t>(batch) * sh.sp;
   const auto F16 = CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
-  const auto SW = CU_TENSOR_MAP_SWIZZLE_128B, SW64 = CU_TENSOR_MAP_SWIZZLE_64B;
-  const int64_t xs = static_cast<int64_t>(sh.lp) * 2, ss = static_cast<int64_t>(sh.sp) * 2;  // row strides
-  for (int k = 0; k < 2 && st == RL_OK; ++k) {
-    st = tmap_2d(&xk[k], F16, x16[k], sh.lp, rows, xs, BK, 128, SW);
-    if (st == RL_OK) st = tmap_2d(&xn[k], F16, x16[k], sh.lp, rows, xs, 64, BK, SW);
-    if (st == RL_OK) st = tmap_2d(&xo[k], F16, x16[k], sh.lp, rows, xs, 32, 32, SW64);
+  auto map = [&](CUtensorMap* m, const void* at, int64_t cols, int box_rows) {
+    if (st == RL_OK) st = tmap_2d(m, F16, at, cols, rows, cols * 2, 64, box_rows, CU_TENSOR_MAP_SWIZZLE_128B);
+  };
+  CUtensorMap xout[2], aout, bout;
+  for (int k = 0; k < 2; ++k) {
+    map(&xk[k], x16[k], sh.lp, 128);
+    map(&xn[k], x16[k], sh.lp, 64);
+    map(&xout[k], x16[k], sh.lp, 32);
   }
-  if (st == RL_OK) st = tmap_2d(&ak, F16, base + w.a16, sh.sp, rows, ss, BK, 128, SW);
-  if (st == RL_OK) st = tmap_2d(&ao, F16, base + w.a16, sh.sp, rows, ss, 32, 32, SW64);
-  if (st == RL_OK) st = tmap_2d(&bk, F16, base + w.b16, sh.sp, rows, ss, BK, 128, SW);
-  if (st == RL_OK) st = tmap_2d(&bo, F16, base + w.b16, sh.sp, rows, ss, 32, 32, SW64);
+  map(&ak, base + w.a16, sh.sp, 128);
+  map(&at, base + w.a16, sh.sp, 64);
+  map(&aout, base + w.a16, sh.sp, 32);
+  map(&bk, base + w.b16, sh.sp, 128);
+  map(&bt, base + w.b16, sh.sp, 64);
+  map(&bout, base + w.b16, sh.sp, 32);
   if (st != RL_OK) return st;
 
   const Plan plan = plan_of(batch, sh.sp, sh.lp);
@@ -970,23 +991,23 @@ rl_status rl_muon_update(int32_t batch, int64_t m, int64_t n, const void* grad, 
   a.e = reinterpret_cast<float*>(base + w.e);
   a.x = pa.x;
   a.parts = reinterpret_cast<float*>(base + w.parts);
-  a.scale = P.update_scale;
+  a.scale = P.update_scale / kXScale;
   a.update = update;
   a.weights = weights;
   a.weights_bf16 = weights_bf16;
   a.ld_w = ld_w;
   a.stride_w = stride_w;
   a.decay = static_cast<float>(1.0 - static_cast<double>(P.lr) * P.weight_decay);
-  a.step = static_cast<float>(static_cast<double>(P.lr) * P.update_scale);
+  a.step = static_cast<float>(static_cast<double>(P.lr) * P.update_scale / kXScale);
   a.status = status;
   for (int k = 0; k < P.ns_steps; ++k) {
     const int T = 128 * plan.cg_sym;
     a.nt_m = a.nt_n = static_cast<int32_t>(round_up(sh.sp, T) / T);
-    a.per = static_cast<int32_t>(tri(a.nt_m));
+    a.per = static_cast<int32_t>(symmetric_items(sh.sp, plan.cg_sym));
     a.splits = plan.splits;
     a.nkb = sh.lp / BK;
-    st = plan.cg_sym == 2 ? product<GRAM, 2>(xk[k & 1], xk[k & 1], ao, a, s)
-                          : product<GRAM, 1>(xk[k & 1], xk[k & 1], ao, a, s);
+    st = plan.cg_sym == 2 ? product<GRAM, 2>(xk[k & 1], xk[k & 1], xk[k & 1], aout, a, s)
+                          : product<GRAM, 1>(xk[k & 1], xk[k & 1], xk[k & 1], aout, a, s);
     if (st != RL_OK) return st;
     if (plan.splits > 1) {
       const int64_t warps = static_cast<int64_t>(batch) * a.per * (T / 32) * (T / 32);
@@ -996,7 +1017,7 @@ rl_status rl_muon_update(int32_t batch, int64_t m, int64_t n, const void* grad, 
     }
     a.splits = 1;
     a.nkb = sh.sp / BK;
-    st = plan.cg_sym == 2 ? product<POLY, 2>(ak, ak, bo, a, s) : product<POLY, 1>(ak, ak, bo, a, s);
+    st = plan.cg_sym == 2 ? product<POLY, 2>(ak, at, ak, bout, a, s) : product<POLY, 1>(ak, at, ak, bout, a, s);
     if (st != RL_OK) return st;
     const int TA = 128 * plan.cg_apply;
     a.nt_m = static_cast<int32_t>(round_up(sh.sp, TA) / TA);
@@ -1004,8 +1025,8 @@ rl_status rl_muon_update(int32_t batch, int64_t m, int64_t n, const void* grad, 
     a.per = a.nt_m * a.nt_n;
     a.inv = k == 0 ? pa.inv : nullptr;
     a.final_step = k == P.ns_steps - 1;
-    st = plan.cg_apply == 2 ? product<APPLY, 2>(bk, xn[k & 1], xo[(k + 1) & 1], a, s)
-                            : product<APPLY, 1>(bk, xn[k & 1], xo[(k + 1) & 1], a, s);
+    st = plan.cg_apply == 2 ? product<APPLY, 2>(bk, bt, xn[k & 1], xout[(k + 1) & 1], a, s)
+                            : product<APPLY, 1>(bk, bt, xn[k & 1], xout[(k + 1) & 1], a, s);
     if (st != RL_OK) return st;
   }
   return RL_OK;
