@@ -255,7 +255,7 @@ __global__ void __launch_bounds__(kPrepWarps * 32) normalise_kernel(const PrepAr
 
 // ---------------------------------------------------------------- the products
 
-enum Mode { GRAM = 0, POLY = 1, APPLY = 2 };
+enum Mode { GRAM = 0, POLY = 1, APPLY = 2, FINAL = 3 };  // FINAL: the last step's APPLY
 
 struct MmArgs {
   Shape sh;
@@ -272,7 +272,6 @@ struct MmArgs {
   const float* inv;      // first step: X is still u, to be multiplied by this
   float* parts;          // GRAM with splits > 1: [split][tile][TILE x TILE] sums
   // the last step's outputs
-  int32_t final_step;
   float scale;           // of the update, 2^-12 taken in
   uint16_t* update;      // bf16 [batch x m x n] or null
   float* weights;
@@ -397,42 +396,49 @@ __device__ __forceinline__ void poly_of(const MmArgs& p, int b, int r0, int c0, 
 }
 
 // The last step's X (lane: row) to the caller's outputs, lanes walking the caller's rows. tile: 32 x 33
-// floats of shared memory.
-__device__ __forceinline__ void final_out(const MmArgs& p, int b, int r0, int c0, int lane, float (&v)[32],
+// floats of shared memory. Eight rows at a time: their loads are in flight together, and the code stays
+// short (unrolled over all 32, with the products' other code, it outgrew the instruction cache: the
+// twelve 1,024 x 1,024 matrices' last product took 72 us).
+__device__ __forceinline__ void final_out(const MmArgs& p, int b, int r0, int c0, int lane, const float (&v)[32],
                                           float (*tile)[33]) {
   const Shape& sh = p.sh;
   const int col = (sh.tall ? r0 : c0) + lane, row0 = sh.tall ? c0 : r0;
   const int rows = col < sh.n ? sh.m - row0 : 0;
+  __syncwarp();
+#pragma unroll
+  for (int j = 0; j < 32; ++j) tile[lane][j] = v[j];
+  __syncwarp();
+  // element (row0 + j, col): tile[j][lane], of the transpose tile[lane][j]
+  const float* from = sh.tall ? &tile[lane][0] : &tile[0][lane];
+  const int step = sh.tall ? 1 : 33;
+  uint16_t* up = p.update ? p.update + (static_cast<int64_t>(b) * sh.m + row0) * sh.n + col : nullptr;
   const int64_t w0 = b * p.stride_w + row0 * p.ld_w + col;
-  if (!sh.tall) {
-    __syncwarp();
+#pragma unroll 1
+  for (int j0 = 0; j0 < 32; j0 += 8) {
+    float x[8], w[8];
 #pragma unroll
-    for (int j = 0; j < 32; ++j) tile[lane][j] = v[j];
-    __syncwarp();
+    for (int j = 0; j < 8; ++j) x[j] = from[(j0 + j) * step];
+    if (p.weights) {
 #pragma unroll
-    for (int j = 0; j < 32; ++j) v[j] = tile[j][lane];
-  }
-  if (p.update) {
-    uint16_t* to = p.update + (static_cast<int64_t>(b) * sh.m + row0) * sh.n + col;
-#pragma unroll
-    for (int j = 0; j < 32; ++j)
-      if (j < rows) to[static_cast<int64_t>(j) * sh.n] = f32_to_bf16(v[j] * p.scale);
-  }
-  if (p.weights) {
-    float w[32];
-#pragma unroll
-    for (int j = 0; j < 32; ++j) w[j] = j < rows ? p.weights[w0 + j * p.ld_w] : 0.f;
-#pragma unroll
-    for (int j = 0; j < 32; ++j) {
-      w[j] = fmaf(-p.step, v[j], p.decay * w[j]);
-      if (j < rows) p.weights[w0 + j * p.ld_w] = w[j];
+      for (int j = 0; j < 8; ++j) w[j] = j0 + j < rows ? p.weights[w0 + (j0 + j) * p.ld_w] : 0.f;
     }
-    if (p.weights_bf16) {
+    if (up) {
 #pragma unroll
-      for (int j = 0; j < 32; ++j)
-        if (j < rows) p.weights_bf16[w0 + j * p.ld_w] = f32_to_bf16(w[j]);
+      for (int j = 0; j < 8; ++j)
+        if (j0 + j < rows) up[static_cast<int64_t>(j0 + j) * sh.n] = f32_to_bf16(x[j] * p.scale);
+    }
+    if (p.weights) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        w[j] = fmaf(-p.step, x[j], p.decay * w[j]);
+        if (j0 + j < rows) {
+          p.weights[w0 + (j0 + j) * p.ld_w] = w[j];
+          if (p.weights_bf16) p.weights_bf16[w0 + (j0 + j) * p.ld_w] = f32_to_bf16(w[j]);
+        }
+      }
     }
   }
+  __syncwarp();
 }
 
 // One product, persistent: CTAs (CG = 1) or CTA pairs (CG = 2) take square tiles of 128 CG in turn.
@@ -446,6 +452,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
                                                               const __grid_constant__ CUtensorMap tmOut,
                                                               const MmArgs p) {
   constexpr int TILE = 128 * CG;
+  constexpr bool APPLIES = MODE == APPLY || MODE == FINAL;
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) uint64_t full[NS], empty[NS], accf[2], acce[2];
   __shared__ uint32_t tbase;
@@ -490,7 +497,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
     const int t = item - b * p.per;
     kb0 = MODE == GRAM ? static_cast<int>(static_cast<int64_t>(part) * p.nkb / p.splits) : 0;
     nkb = (MODE == GRAM ? static_cast<int>(static_cast<int64_t>(part + 1) * p.nkb / p.splits) : p.nkb) - kb0;
-    if (MODE != APPLY) return symmetric_tile<CG>(t, p.nt_m, ti, tj);
+    if (!APPLIES) return symmetric_tile<CG>(t, p.nt_m, ti, tj);
     ti = t % p.nt_m;
     tj = t / p.nt_m;
     return true;
@@ -531,8 +538,8 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
           } else {
             load(st, &tmA, k0, y0 + m0);
           }
-          if (MODE == APPLY || (MODE == POLY && below(n0, k0))) {
-            const CUtensorMap* map = MODE == APPLY ? &tmB : &tmAt;
+          if (APPLIES || (MODE == POLY && below(n0, k0))) {
+            const CUtensorMap* map = APPLIES ? &tmB : &tmAt;
             load(st + A_BYTES, map, n0, y0 + k0);
             load(st + A_BYTES + HALF_BYTES, map, n0 + 64, y0 + k0);
           } else {
@@ -574,7 +581,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
           const uint32_t a = smem_addr(sm + s * STAGE_BYTES), bb = a + A_BYTES;
           const int k0 = (kb0 + kb) * BK;
           const bool a_mn = MODE != GRAM && below(ti * TILE, k0);
-          const bool b_mn = MODE == APPLY || (MODE == POLY && below(tj * TILE, k0));
+          const bool b_mn = APPLIES || (MODE == POLY && below(tj * TILE, k0));
           const uint32_t idesc = idesc_f16(TILE, TILE, a_mn, b_mn);
 #pragma unroll
           for (int k = 0; k < BK / 16; ++k) {
@@ -608,7 +615,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
       const uint32_t buf = t & 1, phase = (t >> 1) & 1;
       ++t;
       const int r0 = ti * TILE + static_cast<int>(rank) * 128 + 32 * q;
-      const int cols = MODE == APPLY ? p.sh.lp : p.sh.sp;
+      const int cols = APPLIES ? p.sh.lp : p.sh.sp;
       // the 64-column halves past the matrix are another one's or nothing
       const int blocks = r0 < p.sh.sp ? min(NBLK, (cols - tj * TILE) / 32 - first) : 0;
       const int cb = tj * TILE + first * 32;  // the warp's first column
@@ -617,7 +624,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
       uint4 a[4];
       auto prefetch = [&](int i) {
         if (i >= blocks) return;
-        if (MODE == APPLY) load_block_row(x_block(p.x, p.sh, b, r0 >> 5, (cb >> 5) + i), lane, x);
+        if (APPLIES) load_block_row(x_block(p.x, p.sh, b, r0 >> 5, (cb >> 5) + i), lane, x);
         if (MODE == POLY) {
           const uint16_t* blk = a_block(p, b, r0, cb + 32 * i) + lane * 8;
 #pragma unroll
@@ -626,7 +633,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
       };
       if (r0 < p.sh.sp) {
         const int64_t row = static_cast<int64_t>(b) * p.sh.sp + r0 + lane;
-        if (MODE == APPLY) f = p.e[row];
+        if (APPLIES) f = p.e[row];
         if (MODE == POLY) f = p.d[row];
       }
       prefetch(0);
@@ -636,7 +643,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
       }
       tc::fence_after_sync();
       const uint32_t tq = tmem + buf * TILE + (static_cast<uint32_t>(32 * q) << 16) + first * 32;
-#pragma unroll 1
+#pragma unroll 1  // unrolled it was slower: see final_out
       for (int i = 0; i < NBLK; ++i) {
         float v[32];
         tc::tmem_ld32(tq + i * 32, v);
@@ -658,7 +665,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
         uint4 w[4];
         if (MODE == GRAM) gram_of(p, b, r0, c0, lane, v, w);
         if (MODE == POLY) poly_of(p, b, r0, c0, lane, v, a, f);
-        if (MODE == APPLY) {
+        if (APPLIES) {
           if (p.inv) {
             const float inv = p.inv[b];
 #pragma unroll
@@ -668,14 +675,11 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
           for (int j = 0; j < 32; ++j) v[j] = fmaf(f, x[j], v[j] * (1.f / kBScale));
         }
         prefetch(i + 1);
-        if (MODE == APPLY) {
-          if (p.final_step) {
-            final_out(p, b, r0, c0, lane, v, tile);
-            __syncwarp();
-            continue;
-          }
-          store_block_row(x_block(p.x, p.sh, b, r0 >> 5, c0 >> 5), lane, v);
+        if (MODE == FINAL) {
+          final_out(p, b, r0, c0, lane, v, tile);
+          continue;
         }
+        if (MODE == APPLY) store_block_row(x_block(p.x, p.sh, b, r0 >> 5, c0 >> 5), lane, v);
         if (MODE != GRAM) pack_row(v, w);
         uint8_t* sb = slabs + slab * SLAB_BYTES;
         if ((i & 1) == 0) {
@@ -742,7 +746,7 @@ __global__ void __launch_bounds__(256) gram_sum_kernel(const MmArgs p) {
 // How the products are cut: the tile (128 or, by CTA pairs, 256) of each, and the parts of the first
 // one's contraction.
 struct Plan {
-  int cg_sym, cg_apply, splits;
+  int cg_gram, cg_poly, cg_apply, splits;
 };
 
 // Items of a symmetric product of one matrix (symmetric_tile).
@@ -753,12 +757,16 @@ inline int64_t symmetric_items(int64_t sp, int cg) {
 
 Plan plan_of(int64_t batch, int64_t sp, int64_t lp) {
   Plan p;
-  auto tiles_sym = [&](int cg) { return batch * symmetric_items(sp, cg); };
-  p.cg_sym = tiles_sym(2) >= kSMs / 2 ? 2 : 1;
+  auto items = [&](int cg) { return batch * symmetric_items(sp, cg); };
+  p.cg_poly = items(2) >= kSMs / 2 ? 2 : 1;
   p.cg_apply = batch * (round_up(sp, 256) / 256) * (round_up(lp, 256) / 256) >= kSMs / 2 ? 2 : 1;
-  const int64_t units = kSMs / p.cg_sym, tiles = tiles_sym(p.cg_sym);
-  // parts of at least eight K blocks, while the tiles leave units idle
-  p.splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(units / std::max<int64_t>(tiles, 1), lp / BK / 8)));
+  // X X^T: a K block takes a unit of either kind about as long (both are bound by what L2 delivers), so
+  // pairs wherever their items, cut into parts of at least eight K blocks, occupy half of them
+  auto parts = [&](int cg) {
+    return std::max<int64_t>(1, std::min<int64_t>(kSMs / cg / std::max<int64_t>(items(cg), 1), lp / BK / 8));
+  };
+  p.cg_gram = items(2) * parts(2) >= kSMs / 4 ? 2 : 1;
+  p.splits = static_cast<int>(parts(p.cg_gram));
   return p;
 }
 
@@ -802,8 +810,8 @@ Layout layout_of(const Shape& s) {
   w.inv = take(B * 4);
   w.partial = take(B * w.n_parts * 8);
   const Plan p = plan_of(s.batch, s.sp, s.lp);
-  const size_t T = 128 * p.cg_sym;
-  w.parts = take(p.splits > 1 ? p.splits * B * symmetric_items(s.sp, p.cg_sym) * T * T * 4 : 0);
+  const size_t T = 128 * p.cg_gram;
+  w.parts = take(p.splits > 1 ? p.splits * B * symmetric_items(s.sp, p.cg_gram) * T * T * 4 : 0);
   w.bytes = at;
   return w;
 }
@@ -1001,32 +1009,37 @@ rl_status rl_muon_update(int32_t batch, int64_t m, int64_t n, const void* grad, 
   a.step = static_cast<float>(static_cast<double>(P.lr) * P.update_scale / kXScale);
   a.status = status;
   for (int k = 0; k < P.ns_steps; ++k) {
-    const int T = 128 * plan.cg_sym;
+    const int T = 128 * plan.cg_gram;
     a.nt_m = a.nt_n = static_cast<int32_t>(round_up(sh.sp, T) / T);
-    a.per = static_cast<int32_t>(symmetric_items(sh.sp, plan.cg_sym));
+    a.per = static_cast<int32_t>(symmetric_items(sh.sp, plan.cg_gram));
     a.splits = plan.splits;
     a.nkb = sh.lp / BK;
-    st = plan.cg_sym == 2 ? product<GRAM, 2>(xk[k & 1], xk[k & 1], xk[k & 1], aout, a, s)
-                          : product<GRAM, 1>(xk[k & 1], xk[k & 1], xk[k & 1], aout, a, s);
+    const CUtensorMap& x = xk[k & 1];
+    st = plan.cg_gram == 2 ? product<GRAM, 2>(x, x, x, aout, a, s) : product<GRAM, 1>(x, x, x, aout, a, s);
     if (st != RL_OK) return st;
     if (plan.splits > 1) {
       const int64_t warps = static_cast<int64_t>(batch) * a.per * (T / 32) * (T / 32);
-      auto kern = plan.cg_sym == 2 ? gram_sum_kernel<2> : gram_sum_kernel<1>;
+      auto kern = plan.cg_gram == 2 ? gram_sum_kernel<2> : gram_sum_kernel<1>;
       st = launch("gram_sum_kernel launch", kern, (warps + 7) / 8, 256, 0, 1, s, a);
       if (st != RL_OK) return st;
     }
+    const int TP = 128 * plan.cg_poly;
+    a.nt_m = a.nt_n = static_cast<int32_t>(round_up(sh.sp, TP) / TP);
+    a.per = static_cast<int32_t>(symmetric_items(sh.sp, plan.cg_poly));
     a.splits = 1;
     a.nkb = sh.sp / BK;
-    st = plan.cg_sym == 2 ? product<POLY, 2>(ak, at, ak, bout, a, s) : product<POLY, 1>(ak, at, ak, bout, a, s);
+    st = plan.cg_poly == 2 ? product<POLY, 2>(ak, at, ak, bout, a, s) : product<POLY, 1>(ak, at, ak, bout, a, s);
     if (st != RL_OK) return st;
     const int TA = 128 * plan.cg_apply;
     a.nt_m = static_cast<int32_t>(round_up(sh.sp, TA) / TA);
     a.nt_n = static_cast<int32_t>(round_up(sh.lp, TA) / TA);
     a.per = a.nt_m * a.nt_n;
     a.inv = k == 0 ? pa.inv : nullptr;
-    a.final_step = k == P.ns_steps - 1;
-    st = plan.cg_apply == 2 ? product<APPLY, 2>(bk, bt, xn[k & 1], xout[(k + 1) & 1], a, s)
-                            : product<APPLY, 1>(bk, bt, xn[k & 1], xout[(k + 1) & 1], a, s);
+    const CUtensorMap &xr = xn[k & 1], &xo = xout[(k + 1) & 1];
+    if (k == P.ns_steps - 1)
+      st = plan.cg_apply == 2 ? product<FINAL, 2>(bk, bt, xr, xo, a, s) : product<FINAL, 1>(bk, bt, xr, xo, a, s);
+    else
+      st = plan.cg_apply == 2 ? product<APPLY, 2>(bk, bt, xr, xo, a, s) : product<APPLY, 1>(bk, bt, xr, xo, a, s);
     if (st != RL_OK) return st;
   }
   return RL_OK;
