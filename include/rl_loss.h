@@ -587,6 +587,55 @@ rl_status rl_prefix_tree_build_batch(int32_t n_rollouts, const int64_t* prompt_o
                                      int64_t* rollout_offsets_out, int64_t* n_tokens_out);
 
 /*
+ * Verification of drafted tokens against the target's probabilities, from given random numbers: the
+ * rollout engine's acceptance test of speculative decoding (Sec. 3.1's inference engine; the paper does
+ * not describe its sampling). Sequence b has K_b = draft_offsets[b + 1] - draft_offsets[b] drafted tokens
+ * x_0, x_1, .. and K_b + 1 target rows, in place order. With p_j = softmax(target row j / T) and
+ * q_j = softmax(draft row j / T) (without draft rows: 1 at x_j):
+ *
+ *   token j is accepted while  u_j q_j(x_j) < p_j(x_j);
+ *   the first refused one is replaced by the draw from max(p_j - q_j, 0) (from p_j if that is zero
+ *   everywhere); without a refusal one more token is drawn from p_K.
+ *
+ * A draw is the lowest v at which the running sum of the weights, in vocabulary order, passes s_b times
+ * their total. T = 0 is greedy: the lowest index of the row's largest entry is both test and draw, and
+ * the numbers and the draft rows are not used.
+ */
+typedef struct rl_verify_params {
+  float temperature; /* T: 0 (greedy) or at least 1e-4 */
+} rl_verify_params;
+
+/*
+ *   target_logits  [n_draft + n_seq rows x ld_target] of `dtype`: sequence b's rows begin at row
+ *                  draft_offsets[b] + b; base 16-byte aligned. Entries of -infinity are never drawn.
+ *   draft_logits   [n_draft rows x ld_draft] of `dtype`, base 16-byte aligned, or NULL
+ *   n_seq, n_draft sequences and drafted tokens (0: nothing, and only draws)
+ *   max_draft      an upper bound of K_b (rows are laid out for it: a tight one is faster)
+ *   V              entries of a row, at most 2^24; a row and its draft row have to fit in the shared
+ *                  memory of 16 CTAs (3.5 MB), else RL_ERR_UNSUPPORTED
+ *   draft_ids      int32 [n_draft] (out of range -> refused, RL_DEV_BAD_TOKEN)
+ *   draft_offsets  int32 [n_seq + 1], from 0 to n_draft (a sequence whose offsets are not in order, in range
+ *                  and at most max_draft apart: n_accepted = -1, nothing else written, RL_DEV_BAD_OFFSETS)
+ *   accept_u       float [n_draft] in [0, 1): u_j
+ *   sample_u       float [n_seq] in [0, 1): s_b
+ *   out_ids        int32 [n_draft + n_seq], laid out as the target rows: the accepted tokens, the token
+ *                  drawn, then -1
+ *   n_accepted     int32 [n_seq]
+ *   out_logp       float [n_draft + n_seq]: log p_j of the emitted tokens (T = 0: of softmax(row)), 0
+ *                  behind them: with T = 1 the rollout_logp of rl_policy_loss_fwd_bwd
+ *   ws, ws_bytes   workspace, rl_workspace_size(n_draft + n_seq, V, 0) bytes
+ *
+ * A row without a finite largest entry, or with a NaN (of the target's or of the draft's), ends its
+ * sequence with token -1 and a NaN log-probability, and sets RL_DEV_BAD_VALUE. Rows behind a sequence's
+ * first refusal are read only if they are looked at before the refusal is known.
+ */
+rl_status rl_verify_drafts(const void* target_logits, const void* draft_logits, rl_dtype dtype, int32_t n_seq,
+                           int64_t n_draft, int32_t max_draft, int64_t V, int64_t ld_target, int64_t ld_draft,
+                           const int32_t* draft_ids, const int32_t* draft_offsets, const float* accept_u,
+                           const float* sample_u, const rl_verify_params* params, int32_t* out_ids,
+                           int32_t* n_accepted, float* out_logp, void* ws, size_t ws_bytes, rl_stream_t stream);
+
+/*
  * Orthogonalised update of weight matrices (no counterpart in the paper: the optimiser that takes the
  * gradients which the policy loss produces, Sec. 2.3): momentum, Newton-Schulz products, and the step
  * on the weights, for a batch of matrices of one shape. Per matrix G [m x n]:

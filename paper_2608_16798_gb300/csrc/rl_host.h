@@ -32,6 +32,9 @@ constexpr size_t kWsSummaryDoneOffset = 28;
 constexpr size_t kWsSummaryOffset = 32;
 // The orthogonalised update's finished CTAs of its norm pass.
 constexpr size_t kWsMuonDoneOffset = 8;
+// Words of the verification of up to kWsVerifySeqs sequences, two each (zero before and after a call).
+constexpr size_t kWsVerifyOffset = 232;
+constexpr int kWsVerifySeqs = 3;
 
 rl_status set_error(rl_status st, const std::string& msg);
 rl_status cuda_error(cudaError_t e, const char* what);

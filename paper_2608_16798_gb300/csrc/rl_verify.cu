@@ -1,0 +1,638 @@
+// Verification of drafted tokens against the target's probabilities, from given random numbers.
+//
+// Sequence b has K_b drafted tokens x_0 .. and K_b + 1 target rows z_0 .., each with
+// p = softmax(z / T); the drafts' own rows give q = softmax(zd / T), or q is 1 at x (no draft rows).
+// Token j is accepted while u_j q(x_j) < p(x_j). At the first refusal the token drawn from
+// max(p - q, 0) ends the sequence; with no refusal one more is drawn from the last row's p. A draw is
+// the lowest v at which the running sum of its weights passes s_b times their total. T = 0: greedy,
+// the row's first largest entry is both the test and the draw.
+//
+// One thread-block cluster per row, rows in the order of their place j in their sequences: by the
+// time a late row starts its sequence has often been refused earlier, and it is skipped; rows that
+// start with the first wave are not held up by that question. Nothing waits for another cluster: the
+// last of a sequence's rows to finish writes the sequence's result.
+//
+// Every warp of the cluster owns one segment of the vocabulary. It brings the segment of both rows
+// into its own shared memory by bulk copies (one barrier each, so a warp starts when its own data is
+// there), folds them into (max, sum of exponentials) pairs, and writes these to a table in every CTA of
+// the cluster. After one cluster barrier each CTA merges the table by itself: both rows' normalisers,
+// the decision, and, for a draw from p alone, the segment that holds the token. A draw from
+// max(p - q, 0) takes a second pass over the segments, still in shared memory, and a second exchange.
+// The warp whose segment holds the token finds it by a scan. HBM is read once.
+#include <algorithm>
+#include <cmath>
+#include <map>
+#include <mutex>
+#include <utility>
+
+#include "rl_device.cuh"
+#include "rl_host.h"
+
+namespace rl {
+namespace verify {
+
+constexpr int kWarps = 8;
+constexpr int kMaxCluster = 16;
+constexpr int kMaxSeg = kWarps * kMaxCluster;
+constexpr int kFirst = 1 << 30;  // a refusal at place j is kept as kFirst - j: the earliest is the largest
+
+struct Args {
+  const void* target;
+  const void* draft;       // or null
+  int64_t ld_t, ld_d;
+  int32_t V, n_seq, max_draft;
+  int64_t n_draft;
+  const int32_t* draft_ids;
+  const int32_t* offsets;  // [n_seq + 1]
+  const float* accept_u;
+  const float* sample_u;
+  float c;                 // log2(e) / T (greedy: log2(e))
+  int32_t seg;             // elements of a segment
+  int32_t seg_bytes;       // its shared memory per row
+  int32_t held;            // rows held at once: 2 with draft rows
+  int32_t check_from;      // first cluster that asks whether its sequence has been refused
+  int32_t* out_ids;
+  float* out_logp;
+  int32_t* n_accepted;
+  uint32_t* finished;      // [n_seq] rows that have finished
+  int32_t* refused;        // [n_seq] kFirst - (place of the earliest refusal so far), 0: none
+  int32_t* status;
+};
+
+template <typename T>
+struct Elem;
+template <>
+struct Elem<uint16_t> {
+  static constexpr int N = 8;  // per 16 bytes
+  static __device__ __forceinline__ void unpack(uint4 w, float (&z)[8]) {
+    z[0] = bf16_lo(w.x), z[1] = bf16_hi(w.x), z[2] = bf16_lo(w.y), z[3] = bf16_hi(w.y);
+    z[4] = bf16_lo(w.z), z[5] = bf16_hi(w.z), z[6] = bf16_lo(w.w), z[7] = bf16_hi(w.w);
+  }
+  static __device__ __forceinline__ float one(uint16_t x) { return bf16_to_f32(x); }
+};
+template <>
+struct Elem<float> {
+  static constexpr int N = 4;
+  static __device__ __forceinline__ void unpack(uint4 w, float (&z)[4]) {
+    z[0] = __uint_as_float(w.x), z[1] = __uint_as_float(w.y), z[2] = __uint_as_float(w.z), z[3] = __uint_as_float(w.w);
+  }
+  static __device__ __forceinline__ float one(float x) { return x; }
+};
+
+__device__ __forceinline__ float minus_inf() { return -__int_as_float(0x7f800000); }
+
+// A warp's segment of a row in shared memory: the 16-byte blocks of memory that it covers.
+template <typename T>
+struct Segment {
+  const T* at;  // the first block
+  int lo, hi;   // its elements are [lo, hi) from there
+  __device__ __forceinline__ int blocks() const { return (hi + Elem<T>::N - 1) / Elem<T>::N; }
+  // Block k; what is not the segment's reads as minus infinity.
+  __device__ __forceinline__ void load(int k, float (&z)[Elem<T>::N]) const {
+    constexpr int N = Elem<T>::N;
+    Elem<T>::unpack(*reinterpret_cast<const uint4*>(at + k * N), z);
+    if (k == 0 || (k + 1) * N > hi) {
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (k * N + e < lo || k * N + e >= hi) z[e] = minus_inf();
+    }
+  }
+};
+
+// Starts the copy of elements [e0, e0 + n) of a row into `to` (seg_bytes) on `bar`, by a whole warp.
+// What the last block of the whole array would read past its end comes by plain loads.
+template <typename T>
+__device__ __forceinline__ Segment<T> fetch(const T* row, int e0, int n, const T* end, uint8_t* to, uint64_t* bar,
+                                            int lane) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(row + e0), b = reinterpret_cast<uintptr_t>(row + e0 + n);
+  const uintptr_t a0 = a & ~uintptr_t(15);
+  Segment<T> s;
+  s.at = reinterpret_cast<const T*>(to);
+  s.lo = static_cast<int>(a - a0) / static_cast<int>(sizeof(T));
+  s.hi = s.lo + n;
+  if (n <= 0) {
+    s.hi = s.lo = 0;
+    if (lane == 0) mbar_arrive(bar);
+    return s;
+  }
+  uintptr_t b0 = (b + 15) & ~uintptr_t(15);
+  if (b0 > reinterpret_cast<uintptr_t>(end)) {
+    b0 = b & ~uintptr_t(15);
+    const int rest = static_cast<int>(b - b0) / static_cast<int>(sizeof(T));
+    if (lane < rest && b0 + lane * sizeof(T) >= a)
+      *reinterpret_cast<T*>(to + (b0 - a0) + lane * sizeof(T)) = reinterpret_cast<const T*>(b0)[lane];
+    __syncwarp();
+  }
+  if (lane == 0) {
+    const uint32_t bytes = b0 > a0 ? static_cast<uint32_t>(b0 - a0) : 0;
+    if (bytes == 0) {
+      mbar_arrive(bar);
+    } else {
+      mbar_arrive_expect_tx(bar, bytes);
+      bulk_g2s(to, reinterpret_cast<const void*>(a0), bytes, bar);
+    }
+  }
+  return s;
+}
+
+// (max, sum of 2^((z - max) c)) of what a lane or a warp has seen; (-inf, 0): nothing. NaNs and
+// +infinity make the sum NaN.
+struct Fold {
+  float m, s;
+};
+
+template <typename T, bool GREEDY>
+__device__ __forceinline__ Fold fold(const Segment<T>& seg, float c, int lane, int& arg) {
+  constexpr int N = Elem<T>::N;
+  Fold f{minus_inf(), 0.f};
+  const int nb = seg.blocks();
+  for (int k = lane; k < nb; k += 32) {
+    float z[N];
+    seg.load(k, z);
+    float top = z[0];
+#pragma unroll
+    for (int e = 1; e < N; ++e) top = fmaxf(top, z[e]);
+    if (top > f.m) {
+      f.s *= ex2((f.m - top) * c);
+      f.m = top;
+      if (GREEDY) {
+#pragma unroll
+        for (int e = N - 1; e >= 0; --e)
+          if (z[e] == top) arg = k * N + e - seg.lo;
+      }
+    }
+    const float ref = f.m == minus_inf() ? 0.f : f.m;
+    float s = 0.f;
+#pragma unroll
+    for (int e = 0; e < N; ++e) s += ex2((z[e] - ref) * c);
+    f.s += s;
+  }
+  const float M = redux_max(f.m);
+  const float s = warp_sum(f.s == 0.f ? 0.f : f.s * ex2((f.m - M) * c));
+  if (GREEDY) {
+    const uint32_t best = __reduce_min_sync(0xffffffffu, f.m == M ? static_cast<uint32_t>(arg) : 0xffffffffu);
+    arg = static_cast<int>(best);
+  }
+  return Fold{M, s};
+}
+
+// One entry per segment, the same table in every CTA of the cluster.
+struct Table {
+  Fold t[kMaxSeg];      // target
+  Fold d[kMaxSeg];      // draft
+  float r[kMaxSeg];     // weight of the segment in a draw from max(p - q, 0)
+  int32_t arg[kMaxSeg]; // greedy: first largest entry
+};
+
+__device__ __forceinline__ void put_f2(uint32_t addr, float a, float b) {
+  asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" :: "r"(addr), "f"(a), "f"(b) : "memory");
+}
+__device__ __forceinline__ void put_f1(uint32_t addr, float a) {
+  asm volatile("st.shared::cluster.f32 [%0], %1;" :: "r"(addr), "f"(a) : "memory");
+}
+
+// The row's (max, sum) from its segments', the same bits in every lane of every CTA.
+__device__ __forceinline__ Fold merged(const Fold* f, int n, float c, int lane) {
+  float m = minus_inf();
+  for (int k = lane; k < n; k += 32) m = fmaxf(m, f[k].m);
+  const float M = redux_max(m);
+  float s = 0.f;
+  for (int k = lane; k < n; k += 32) s += f[k].s == 0.f ? 0.f : f[k].s * ex2((f[k].m - M) * c);
+  return Fold{M, warp_sum(s)};
+}
+
+// The segment in which the running sum of the weights w(k) passes u times their total, and what is left
+// to pass within it. The last segment with any weight where rounding leaves none; -1: no weight at all.
+template <typename W>
+__device__ __forceinline__ int pick(int n, double u, int lane, W w, float& left) {
+  // lane l holds segments [4 l, 4 l + 4)
+  double mine[kMaxSeg / 32], sum = 0.0;
+#pragma unroll
+  for (int i = 0; i < kMaxSeg / 32; ++i) {
+    const int k = lane * (kMaxSeg / 32) + i;
+    mine[i] = k < n ? static_cast<double>(w(k)) : 0.0;
+    sum += mine[i];
+  }
+  double run = sum;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const double up = __shfl_up_sync(0xffffffffu, run, o);
+    if (lane >= o) run += up;
+  }
+  const double total = __shfl_sync(0xffffffffu, run, 31), goal = u * total;
+  double before = run - sum;
+  int at = -1, last = -1;
+  float rest = 0.f, last_rest = 0.f;
+#pragma unroll
+  for (int i = 0; i < kMaxSeg / 32; ++i) {
+    const int k = lane * (kMaxSeg / 32) + i;
+    if (mine[i] > 0.0) {
+      last = k;
+      last_rest = static_cast<float>(goal - before);
+      if (at < 0 && before + mine[i] > goal) {
+        at = k;
+        rest = last_rest;
+      }
+    }
+    before += mine[i];
+  }
+  const uint32_t found = __ballot_sync(0xffffffffu, at >= 0), any = __ballot_sync(0xffffffffu, last >= 0);
+  if (any == 0) {
+    left = 0.f;
+    return -1;
+  }
+  const int from = found ? __ffs(found) - 1 : 31 - __clz(any);
+  left = __shfl_sync(0xffffffffu, found ? rest : last_rest, from);
+  return __shfl_sync(0xffffffffu, found ? at : last, from);
+}
+
+// The place within a segment at which the running sum of the weights of its elements passes `left`
+// (the last with any weight where rounding leaves none; -1: none has any). w(k, x): the weights of block
+// k's elements.
+template <typename T, typename W>
+__device__ __forceinline__ int locate(const Segment<T>& seg, float left, int lane, W w) {
+  constexpr int N = Elem<T>::N;
+  const int nb = seg.blocks();
+  int last = -1;
+  float before = 0.f;
+  for (int k0 = 0; k0 < nb; k0 += 32) {
+    const int k = k0 + lane;
+    float x[N], sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < N; ++e) x[e] = 0.f;
+    if (k < nb) w(k, x);
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      sum += x[e];
+      if (x[e] > 0.f) last = k * N + e - seg.lo;
+    }
+    float run = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const float up = __shfl_up_sync(0xffffffffu, run, o);
+      if (lane >= o) run += up;
+    }
+    const uint32_t over = __ballot_sync(0xffffffffu, sum > 0.f && before + run > left);
+    if (over) {
+      const int from = __ffs(over) - 1;
+      float acc = before + (run - sum);
+      int at = -1;
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        acc += x[e];
+        if (at < 0 && x[e] > 0.f && acc > left) at = k * N + e - seg.lo;
+      }
+      return __shfl_sync(0xffffffffu, at >= 0 ? at : last, from);
+    }
+    before += __shfl_sync(0xffffffffu, run, 31);
+  }
+  return static_cast<int>(__reduce_max_sync(0xffffffffu, last));
+}
+
+// A row is finished (its result written, if it has one): the last of its sequence writes what the
+// sequence comes to and leaves the sequence's words at zero. By one thread.
+__device__ __forceinline__ void finish(const Args& p, int b, int o, int K) {
+  __threadfence();
+  if (atomicAdd(p.finished + b, 1u) != static_cast<uint32_t>(K)) return;
+  __threadfence();
+  const int f = atomicExch(p.refused + b, 0);
+  p.finished[b] = 0;
+  const int n = f ? kFirst - f : K;
+  p.n_accepted[b] = n;
+  for (int j = n + 1; j <= K; ++j) {
+    p.out_ids[o + b + j] = -1;
+    p.out_logp[o + b + j] = 0.f;
+  }
+}
+
+template <typename T, bool GREEDY>
+__global__ void __launch_bounds__(kWarps * 32) verify_kernel(const Args p) {
+  extern __shared__ __align__(16) uint8_t smem[];
+  __shared__ __align__(8) uint64_t bars[kWarps][2];
+  __shared__ __align__(16) Table tab;
+  __shared__ int32_t skip;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_ctarank(), C = cluster_nctarank();
+  const int id = blockIdx.x / C, j = id / p.n_seq, b = id % p.n_seq;
+  const int n_seg = static_cast<int>(C) * kWarps, g = static_cast<int>(rank) * kWarps + warp;
+
+  const int o = p.offsets[b], o1 = p.offsets[b + 1];
+  const int K = o1 - o;
+  if (o < 0 || o1 < o || o1 > p.n_draft || K > p.max_draft) {
+    if (j == 0 && rank == 0 && threadIdx.x == 0) {
+      flag_status(p.status, RL_DEV_BAD_OFFSETS);
+      p.n_accepted[b] = -1;
+    }
+    return;  // the whole cluster
+  }
+  if (j > K) return;
+  // another CTA's shared memory may be written once that CTA has started
+  asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+  if (id >= p.check_from) {
+    // one CTA asks, so that the cluster decides as one
+    asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+    if (rank == 0 && threadIdx.x < C) {
+      const int f = *reinterpret_cast<volatile int32_t*>(p.refused + b);
+      asm volatile("st.shared::cluster.u32 [%0], %1;"
+                   :: "r"(map_to_rank(smem_addr(&skip), threadIdx.x)), "r"(f && kFirst - f < j ? 1 : 0) : "memory");
+    }
+    __syncwarp();
+    cluster_sync_all();
+    if (skip) {
+      if (rank == 0 && threadIdx.x == 0) finish(p, b, o, K);
+      return;
+    }
+  }
+  const int64_t row = static_cast<int64_t>(o) + b + j, drow = static_cast<int64_t>(o) + j;
+  const bool tested = j < K, two = tested && !GREEDY && p.draft != nullptr;
+  const T* zt = static_cast<const T*>(p.target) + row * p.ld_t;
+  const T* zd = two ? static_cast<const T*>(p.draft) + drow * p.ld_d : nullptr;
+  const int e0 = min(g * p.seg, p.V), n = min(p.seg, p.V - e0);
+  if (lane == 0) {
+    mbar_init(&bars[warp][0], 1);
+    mbar_init(&bars[warp][1], 1);
+    fence_mbar_init();
+    fence_proxy_async_smem();
+  }
+  __syncwarp();
+  uint8_t* mine = smem + static_cast<size_t>(warp) * p.held * p.seg_bytes;
+  const T* t_end = static_cast<const T*>(p.target) + (p.n_draft + p.n_seq - 1) * p.ld_t + p.V;
+  Segment<T> st = fetch(zt, e0, n, t_end, mine, &bars[warp][0], lane), sd{};
+  if (two)
+    sd = fetch(zd, e0, n, static_cast<const T*>(p.draft) + (p.n_draft - 1) * p.ld_d + p.V, mine + p.seg_bytes,
+               &bars[warp][1], lane);
+  // the drafted token's own entries, by every thread
+  int x = -1;
+  float zx = 0.f, zdx = 0.f, ua = 0.f;
+  if (tested) {
+    x = p.draft_ids[drow];
+    ua = p.accept_u[drow];
+    if (x < 0 || x >= p.V) {
+      if (rank == 0 && threadIdx.x == 0) flag_status(p.status, RL_DEV_BAD_TOKEN);
+      x = -1;
+    } else {
+      zx = Elem<T>::one(zt[x]);
+      if (two) zdx = Elem<T>::one(zd[x]);
+    }
+  }
+  const float us = p.sample_u[b];
+
+  // ---- both rows' folds, to every CTA's table
+  bool in_time = mbar_wait_bounded(&bars[warp][0], 0);
+  int arg = 0;
+  Fold ft = fold<T, GREEDY>(st, p.c, lane, arg), fd{minus_inf(), 0.f};
+  if (two) {
+    in_time = mbar_wait_bounded(&bars[warp][1], 0) && in_time;
+    int unused = 0;
+    fd = fold<T, false>(sd, p.c, lane, unused);
+  }
+  if (!in_time && lane == 0) flag_status(p.status, RL_DEV_TIMEOUT);
+  __syncwarp();
+  if (id < p.check_from) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+  if (lane < C) {
+    put_f2(map_to_rank(smem_addr(&tab.t[g]), lane), ft.m, ft.s);
+    if (two) put_f2(map_to_rank(smem_addr(&tab.d[g]), lane), fd.m, fd.s);
+    if (GREEDY) put_f1(map_to_rank(smem_addr(&tab.arg[g]), lane), __int_as_float(arg));
+  }
+  __syncwarp();
+  cluster_sync_all();
+
+  // ---- the decision, by every warp alike
+  const float c = p.c;
+  const Fold ht = merged(tab.t, n_seg, c, lane);
+  Fold hd{0.f, 1.f};
+  if (two) hd = merged(tab.d, n_seg, c, lane);
+  const bool bad = !(ht.s > 0.f && ht.s < 3e38f) || !(hd.s > 0.f && hd.s < 3e38f);
+  const float log2s = log2f(ht.s);
+  auto logp_of = [&](float z) { return fmaf(z - ht.m, c, -log2s) * kLn2; };
+  int token = -1;  // greedy
+  if (GREEDY && !bad) {
+    uint32_t best = 0xffffffffu;
+    for (int k = lane; k < n_seg; k += 32)
+      if (tab.t[k].m == ht.m) best = min(best, static_cast<uint32_t>(k * p.seg + tab.arg[k]));
+    token = static_cast<int>(__reduce_min_sync(0xffffffffu, best));
+  }
+  bool accept = false;
+  const float it = 1.f / ht.s, id_ = 1.f / hd.s;
+  if (tested && !bad && x >= 0) {
+    if (GREEDY) {
+      accept = x == token;
+    } else {
+      const float px = ex2((zx - ht.m) * c) * it;
+      const float qx = two ? ex2((zdx - hd.m) * c) * id_ : 1.f;
+      accept = ua * qx < px;
+    }
+  }
+  const bool leader = rank == 0 && threadIdx.x == 0;
+  if (accept || bad || GREEDY) {
+    if (leader) {
+      if (bad) flag_status(p.status, RL_DEV_BAD_VALUE);
+      if (!accept) atomicMax(p.refused + b, kFirst - j);
+      p.out_ids[row] = accept ? x : token;
+      p.out_logp[row] = bad ? __int_as_float(0x7fffffff)
+                            : logp_of(accept ? zx : Elem<T>::one(zt[token]));
+      finish(p, b, o, K);
+    }
+    return;
+  }
+  // ordered before the sequence's result by the cluster barrier that follows a refusal
+  if (tested && leader) atomicMax(p.refused + b, kFirst - j);
+
+  // ---- the draw: from max(p - q, 0) after a refusal, else from p
+  float left;
+  int at = -1;
+  bool plain = !tested;
+  const int shift = sd.lo - st.lo;
+  auto weights_p = [&](int k, float (&w)[Elem<T>::N]) {
+    st.load(k, w);
+#pragma unroll
+    for (int e = 0; e < Elem<T>::N; ++e) w[e] = ex2((w[e] - ht.m) * c);
+  };
+  auto weights_r = [&](int k, float (&w)[Elem<T>::N]) {
+    constexpr int N = Elem<T>::N;
+    weights_p(k, w);
+    if (two) {
+      float y[N];
+      if (shift == 0) {
+        sd.load(k, y);
+      } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+          const int i = k * N + e;
+          y[e] = i >= st.lo && i < st.hi ? Elem<T>::one(sd.at[i + shift]) : minus_inf();
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < N; ++e) w[e] = fmaxf(fmaf(-ex2((y[e] - hd.m) * c), id_, w[e] * it), 0.f);
+    } else {
+      const int i = x - e0 + st.lo - k * N;
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (e == i) w[e] = 0.f;
+    }
+  };
+  if (!plain) {
+    float r = 0.f;
+    const int nb = st.blocks();
+    for (int k = lane; k < nb; k += 32) {
+      float w[Elem<T>::N];
+      weights_r(k, w);
+#pragma unroll
+      for (int e = 0; e < Elem<T>::N; ++e) r += w[e];
+    }
+    r = warp_sum(r);
+    if (lane < C) put_f1(map_to_rank(smem_addr(&tab.r[g]), lane), r);
+    __syncwarp();
+    cluster_sync_all();
+    at = pick(n_seg, static_cast<double>(us), lane, [&](int k) { return tab.r[k]; }, left);
+    plain = at < 0;  // p and q are equal up to rounding
+  }
+  if (plain)
+    at = pick(n_seg, static_cast<double>(us), lane,
+              [&](int k) { return tab.t[k].s == 0.f ? 0.f : tab.t[k].s * ex2((tab.t[k].m - ht.m) * c); }, left);
+  if (at != g) return;
+  const int i = plain ? locate(st, left, lane, weights_p) : locate(st, left, lane, weights_r);
+  if (lane == 0) {
+    token = e0 + max(i, 0);
+    p.out_ids[row] = token;
+    p.out_logp[row] = logp_of(Elem<T>::one(zt[token]));
+    finish(p, b, o, K);
+  }
+}
+
+// ---------------------------------------------------------------- host
+
+constexpr int kSMs = 152;
+// Shared memory per CTA beyond the tables (7 KB, static).
+constexpr int64_t kMostBytes = 220 * 1024;
+constexpr int64_t kGoodBytes = 72 * 1024;  // three CTAs per SM: one's copies run under the others' arithmetic
+
+inline int64_t segment(int64_t V, int64_t C) { return ((V + C * kWarps - 1) / (C * kWarps) + 7) / 8 * 8; }
+inline int64_t segment_bytes(int64_t V, int64_t C, int es) { return segment(V, C) * es + 16; }
+
+// CTAs per row: few enough that each holds a good piece of it, and as many as fill the GPU while a
+// segment keeps at least 1 KB. 0: the row does not fit in 16 CTAs.
+int cluster_of(int64_t V, int es, int rows_held, int64_t clusters) {
+  auto bytes = [&](int C) { return segment_bytes(V, C, es) * kWarps * rows_held; };
+  int C = 1;
+  while (C < kMaxCluster && bytes(C) > kGoodBytes) C *= 2;
+  if (bytes(C) > kMostBytes) return 0;
+  while (C < kMaxCluster && clusters * C < kSMs && segment_bytes(V, 2 * C, es) >= 1024) C *= 2;
+  return C;
+}
+
+template <typename T, bool GREEDY>
+rl_status run(Args& a, cudaStream_t s) {
+  const int held = a.draft && !GREEDY ? 2 : 1, es = sizeof(T);
+  const int64_t clusters = static_cast<int64_t>(a.n_seq) * (a.max_draft + 1);
+  const int C = cluster_of(a.V, es, held, clusters);
+  if (C == 0) return set_error(RL_ERR_UNSUPPORTED, "rl_verify_drafts: V is too large for 16 CTAs of 220 KB per row");
+  a.seg = static_cast<int32_t>(segment(a.V, C));
+  a.seg_bytes = static_cast<int32_t>(segment_bytes(a.V, C, es));
+  a.held = held;
+  const size_t smem = static_cast<size_t>(kWarps) * held * a.seg_bytes;
+  auto kern = verify_kernel<T, GREEDY>;
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = C;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  cfg.blockDim = dim3(kWarps * 32);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return cuda_error(e, "cudaGetDevice");
+  // clusters resident at once, by device and shape
+  static std::mutex mu;
+  static std::map<std::pair<int, std::pair<int, size_t>>, int> resident;
+  {
+    std::lock_guard<std::mutex> lock(mu);
+    const auto key = std::make_pair(dev, std::make_pair(C, smem));
+    auto it = resident.find(key);
+    if (it == resident.end()) {
+      e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kMostBytes));
+      if (e == cudaSuccess) e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+      if (e != cudaSuccess) return cuda_error(e, "cudaFuncSetAttribute(verify_kernel)");
+      int n = 0;
+      cfg.gridDim = dim3(C);
+      e = cudaOccupancyMaxActiveClusters(&n, kern, &cfg);
+      if (e != cudaSuccess) return cuda_error(e, "cudaOccupancyMaxActiveClusters(verify_kernel)");
+      if (n <= 0) return set_error(RL_ERR_UNSUPPORTED, "verify_kernel: no cluster fits on the device");
+      it = resident.emplace(key, n).first;
+    }
+    a.check_from = it->second;
+  }
+  cfg.gridDim = dim3(static_cast<unsigned>(clusters * C));
+  e = cudaLaunchKernelEx(&cfg, kern, a);
+  return e == cudaSuccess ? RL_OK : cuda_error(e, "verify_kernel launch");
+}
+
+}  // namespace verify
+}  // namespace rl
+
+extern "C" rl_status rl_verify_drafts(const void* target_logits, const void* draft_logits, rl_dtype dtype,
+                                      int32_t n_seq, int64_t n_draft, int32_t max_draft, int64_t V, int64_t ld_target,
+                                      int64_t ld_draft, const int32_t* draft_ids, const int32_t* draft_offsets,
+                                      const float* accept_u, const float* sample_u, const rl_verify_params* params,
+                                      int32_t* out_ids, int32_t* n_accepted, float* out_logp, void* ws,
+                                      size_t ws_bytes, rl_stream_t stream) {
+  using namespace rl;
+  clear_error();
+  const std::string f = "rl_verify_drafts: ";
+  if (dtype != RL_BF16 && dtype != RL_F32) return set_error(RL_ERR_INVALID_ARG, f + "bad dtype");
+  if (n_seq < 0 || n_draft < 0 || max_draft < 0 || V < 1) return set_error(RL_ERR_INVALID_ARG, f + "bad size");
+  if (!params) return set_error(RL_ERR_INVALID_ARG, f + "params is NULL");
+  if (!(params->temperature >= 0.f) || !std::isfinite(params->temperature) ||
+      (params->temperature > 0.f && params->temperature < 1e-4f))
+    return set_error(RL_ERR_INVALID_ARG, f + "temperature must be 0 (greedy) or at least 1e-4");
+  if (ld_target < V || (draft_logits && ld_draft < V))
+    return set_error(RL_ERR_INVALID_ARG, f + "a leading dimension is below V");
+  if (n_seq == 0) return RL_OK;
+  if (!target_logits || !draft_offsets || !sample_u || !out_ids || !n_accepted || !out_logp || !ws ||
+      (n_draft > 0 && (!draft_ids || !accept_u)))
+    return set_error(RL_ERR_INVALID_ARG, f + "a required pointer is NULL");
+  if (!aligned16(target_logits) || !aligned16(draft_logits) || !aligned16(ws))
+    return set_error(RL_ERR_ALIGNMENT, f + "logits and ws must be 16-byte aligned");
+  if (V > (1 << 24) || n_draft + n_seq > (int64_t(1) << 30) || max_draft >= verify::kFirst ||
+      static_cast<int64_t>(n_seq) * (static_cast<int64_t>(max_draft) + 1) > (int64_t(1) << 26))
+    return set_error(RL_ERR_UNSUPPORTED, f + "at most 2^24 entries, 2^30 rows and 2^26 pairs of a sequence and a place");
+  if (ws_bytes < rl_workspace_size(n_draft + n_seq, V, 0))
+    return set_error(RL_ERR_WORKSPACE_TOO_SMALL, f + "ws_bytes below rl_workspace_size(n_draft + n_seq, V, 0)");
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  uint8_t* base = static_cast<uint8_t*>(ws);
+  verify::Args a = {};
+  a.target = target_logits;
+  a.draft = draft_logits;
+  a.ld_t = ld_target;
+  a.ld_d = ld_draft;
+  a.V = static_cast<int32_t>(V);
+  a.n_seq = n_seq;
+  a.max_draft = max_draft;
+  a.n_draft = n_draft;
+  a.draft_ids = draft_ids;
+  a.offsets = draft_offsets;
+  a.accept_u = accept_u;
+  a.sample_u = sample_u;
+  const bool greedy = params->temperature == 0.f;
+  a.c = greedy ? kLog2e : kLog2e / params->temperature;
+  a.out_ids = out_ids;
+  a.out_logp = out_logp;
+  a.n_accepted = n_accepted;
+  a.status = reinterpret_cast<int32_t*>(base);
+  if (n_seq <= kWsVerifySeqs) {
+    // the header's words: zero before the call and after it
+    a.finished = reinterpret_cast<uint32_t*>(base + kWsVerifyOffset);
+    a.refused = reinterpret_cast<int32_t*>(a.finished + kWsVerifySeqs);
+  } else {
+    a.finished = reinterpret_cast<uint32_t*>(base + kWsHeader);
+    a.refused = reinterpret_cast<int32_t*>(a.finished + n_seq);
+    const cudaError_t e = cudaMemsetAsync(a.finished, 0, static_cast<size_t>(n_seq) * 8, s);
+    if (e != cudaSuccess) return cuda_error(e, "rl_verify_drafts: cudaMemsetAsync");
+  }
+  if (dtype == RL_BF16) return greedy ? verify::run<uint16_t, true>(a, s) : verify::run<uint16_t, false>(a, s);
+  return greedy ? verify::run<float, true>(a, s) : verify::run<float, false>(a, s);
+}

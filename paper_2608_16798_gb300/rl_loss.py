@@ -54,6 +54,8 @@ EXPORTS = {
     "rl_fused_head_token_logprobs": (_I32, [_P, _P, _I64, _I64, _I64, _P, _P, _P, _P, _P, _SZ, _P]),
     "rl_fused_head_loss_fwd_bwd": (_I32, [_P, _P, _I64, _I64, _I64, _P, _P, _P, _I32, _P, _P, _P, _P, _P, _P, _P,
                                           _I32, _P, _P, _P, _P, _SZ, _P]),
+    "rl_verify_drafts": (_I32, [_P, _P, _I32, _I32, _I64, _I32, _I64, _I64, _I64, _P, _P, _P, _P, _P, _P, _P, _P, _P,
+                                _SZ, _P]),
     "rl_muon_workspace_size": (_SZ, [_I32, _I64, _I64]),
     "rl_muon_update": (_I32, [_I32, _I64, _I64, _P, _I32, _I64, _I64, _P, _P, _P, _I64, _I64, _P, _P, _P, _SZ, _P]),
 }
@@ -69,6 +71,14 @@ def make_params(clip_eps_low=0.2, clip_eps_high=0.28, kl_coef=0.0, kl_estimator=
                 tis_cap=0.0, adv_eps=1e-6, loss_agg=AGG_SEQ_MEAN_TOKEN_MEAN, token_level_adv=0) -> rl_loss_params:
     return rl_loss_params(clip_eps_low, clip_eps_high, kl_coef, kl_estimator, entropy_coef, tis_cap, adv_eps,
                           loss_agg, int(token_level_adv))
+
+
+class rl_verify_params(ctypes.Structure):
+    _fields_ = [("temperature", _F)]
+
+
+def make_verify_params(temperature=1.0) -> rl_verify_params:
+    return rl_verify_params(temperature)
 
 
 class rl_muon_params(ctypes.Structure):
@@ -633,6 +643,46 @@ def rl_token_stats_summary(token_stats, mask, token_traj, coef, ws, summary_accu
                                       p_summary_accum, p_ws, ws.numel(), _stream(stream))
     _check("rl_token_stats_summary", st)
     return summary_accum
+
+
+def rl_verify_drafts(target_logits, draft_ids, draft_offsets, accept_u, sample_u, max_draft, params: rl_verify_params,
+                     ws, draft_logits=None, out_ids=None, n_accepted=None, out_logp=None, stream=None):
+    """Verify drafted tokens against the target's probabilities. ``draft_offsets`` (int32 [n_seq + 1]) cuts the
+    drafted tokens into sequences of at most ``max_draft``; ``target_logits`` has one more row per sequence
+    ([n_draft + n_seq, V]), ``draft_logits`` ([n_draft, V], or None for drafts without a distribution) one per
+    drafted token. Returns (out_ids, n_accepted, out_logp): per target row the emitted token (-1 behind the
+    last) and its log-probability, and the accepted tokens of each sequence."""
+    rows, V, ld = _rows_view(target_logits)
+    dt = _logits_dtype(target_logits)
+    dev = target_logits.device
+    ix = target_logits.get_device()
+    n_draft, n_seq = draft_ids.numel(), draft_offsets.numel() - 1
+    if rows < n_draft + n_seq:
+        raise ValueError(f"target_logits has {rows} rows, needs {n_draft + n_seq}")
+    if not target_logits.is_cuda:
+        raise ValueError("target_logits must be a CUDA tensor")
+    p_draft, ld_d = None, V
+    if draft_logits is not None:
+        d_rows, d_V, ld_d = _rows_view(draft_logits)
+        if draft_logits.dtype != target_logits.dtype or draft_logits.get_device() != ix or d_V != V or d_rows < n_draft:
+            raise ValueError("draft_logits must have target_logits' dtype, device and V, and a row per drafted token")
+        p_draft = draft_logits.data_ptr()
+    p_ids = _need(draft_ids, "draft_ids", torch.int32, index=ix)
+    p_offsets = _need(draft_offsets, "draft_offsets", torch.int32, 1, index=ix)
+    p_accept = _need(accept_u, "accept_u", torch.float32, n_draft, index=ix)
+    p_sample = _need(sample_u, "sample_u", torch.float32, n_seq, index=ix)
+    out_ids = torch.empty(n_draft + n_seq, dtype=torch.int32, device=dev) if out_ids is None else out_ids
+    n_accepted = torch.empty(n_seq, dtype=torch.int32, device=dev) if n_accepted is None else n_accepted
+    out_logp = torch.empty(n_draft + n_seq, dtype=torch.float32, device=dev) if out_logp is None else out_logp
+    p_out_ids = _need(out_ids, "out_ids", torch.int32, n_draft + n_seq, index=ix)
+    p_n_accepted = _need(n_accepted, "n_accepted", torch.int32, n_seq, index=ix)
+    p_out_logp = _need(out_logp, "out_logp", torch.float32, n_draft + n_seq, index=ix)
+    p_ws = _need(ws, "ws", torch.uint8, index=ix)
+    st = lib().rl_verify_drafts(target_logits.data_ptr(), p_draft, dt, n_seq, n_draft, int(max_draft), V, ld, ld_d, p_ids,
+                                p_offsets, p_accept, p_sample, ctypes.byref(params), p_out_ids, p_n_accepted,
+                                p_out_logp, p_ws, ws.numel(), _stream(stream))
+    _check("rl_verify_drafts", st)
+    return out_ids, n_accepted, out_logp
 
 
 def rl_muon_workspace_size(batch: int, m: int, n: int) -> int:
