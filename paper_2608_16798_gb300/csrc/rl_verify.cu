@@ -15,8 +15,8 @@
 // Every warp of the cluster owns one segment of the vocabulary. It brings the segment of both rows
 // into its own shared memory by bulk copies (one barrier each, so a warp starts when its own data is
 // there), folds them into (max, sum of exponentials) pairs, and writes these to a table in every CTA of
-// the cluster. After one cluster barrier each CTA merges the table by itself: both rows' normalisers,
-// the decision, and, for a draw from p alone, the segment that holds the token. A draw from
+// the cluster. After one cluster barrier the first warp of each CTA merges the table: both rows'
+// normalisers, the decision, and, for a draw from p alone, the segment that holds the token. A draw from
 // max(p - q, 0) takes a second pass over the segments, still in shared memory, and a second exchange.
 // The warp whose segment holds the token finds it by a scan. HBM is read once.
 #include <algorithm>
@@ -69,6 +69,7 @@ struct Elem<uint16_t> {
     z[4] = bf16_lo(w.z), z[5] = bf16_hi(w.z), z[6] = bf16_lo(w.w), z[7] = bf16_hi(w.w);
   }
   static __device__ __forceinline__ float one(uint16_t x) { return bf16_to_f32(x); }
+  static __device__ __forceinline__ uint16_t none() { return 0xff80; }
 };
 template <>
 struct Elem<float> {
@@ -77,6 +78,7 @@ struct Elem<float> {
     z[0] = __uint_as_float(w.x), z[1] = __uint_as_float(w.y), z[2] = __uint_as_float(w.z), z[3] = __uint_as_float(w.w);
   }
   static __device__ __forceinline__ float one(float x) { return x; }
+  static __device__ __forceinline__ float none() { return -__int_as_float(0x7f800000); }
 };
 
 __device__ __forceinline__ float minus_inf() { return -__int_as_float(0x7f800000); }
@@ -84,18 +86,18 @@ __device__ __forceinline__ float minus_inf() { return -__int_as_float(0x7f800000
 // A warp's segment of a row in shared memory: the 16-byte blocks of memory that it covers.
 template <typename T>
 struct Segment {
-  const T* at;  // the first block
-  int lo, hi;   // its elements are [lo, hi) from there
+  T* at;       // the first block
+  int lo, hi;  // its elements are [lo, hi) from there
   __device__ __forceinline__ int blocks() const { return (hi + Elem<T>::N - 1) / Elem<T>::N; }
-  // Block k; what is not the segment's reads as minus infinity.
   __device__ __forceinline__ void load(int k, float (&z)[Elem<T>::N]) const {
-    constexpr int N = Elem<T>::N;
-    Elem<T>::unpack(*reinterpret_cast<const uint4*>(at + k * N), z);
-    if (k == 0 || (k + 1) * N > hi) {
-#pragma unroll
-      for (int e = 0; e < N; ++e)
-        if (k * N + e < lo || k * N + e >= hi) z[e] = minus_inf();
-    }
+    Elem<T>::unpack(*reinterpret_cast<const uint4*>(at + k * Elem<T>::N), z);
+  }
+  // What the first and the last block hold of the neighbours becomes minus infinity.
+  __device__ __forceinline__ void blank_edges(int lane) const {
+    const T none = Elem<T>::none();
+    if (lane < lo) at[lane] = none;
+    if (hi + lane < blocks() * Elem<T>::N) at[hi + lane] = none;
+    __syncwarp();
   }
 };
 
@@ -107,7 +109,7 @@ __device__ __forceinline__ Segment<T> fetch(const T* row, int e0, int n, const T
   const uintptr_t a = reinterpret_cast<uintptr_t>(row + e0), b = reinterpret_cast<uintptr_t>(row + e0 + n);
   const uintptr_t a0 = a & ~uintptr_t(15);
   Segment<T> s;
-  s.at = reinterpret_cast<const T*>(to);
+  s.at = reinterpret_cast<T*>(to);
   s.lo = static_cast<int>(a - a0) / static_cast<int>(sizeof(T));
   s.hi = s.lo + n;
   if (n <= 0) {
@@ -141,39 +143,85 @@ struct Fold {
   float m, s;
 };
 
+// Two fp32 operations per instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;"
+      : "=l"(reinterpret_cast<uint64_t&>(r))
+      : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)), "l"(reinterpret_cast<uint64_t&>(c)));
+  return r;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 r;
+  asm("add.rn.f32x2 %0, %1, %2;"
+      : "=l"(reinterpret_cast<uint64_t&>(r)) : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)));
+  return r;
+}
+
+// Exponents are taken relative to the rounded product ref c, in one fused operation with z c, and every
+// change of reference uses the same rounded products, so that it adds no error of its own. Where ref c
+// could overflow (rows of the type's lowest value) the difference comes first.
+__device__ __forceinline__ bool large(float ref) { return !(fabsf(ref) < 1e30f); }
+__device__ __forceinline__ float exponent(float z, float ref, float c) {
+  return large(ref) ? (z - ref) * c : fmaf(z, c, -__fmul_rn(ref, c));
+}
+// The factor from sums relative to m to sums relative to M >= m.
+__device__ __forceinline__ float power(float m, float M, float c) {
+  return ex2(large(M) ? (m - M) * c : __fsub_rn(__fmul_rn(m, c), __fmul_rn(M, c)));
+}
+// 2^exponent of a block.
+template <int N>
+__device__ __forceinline__ void exps(float (&z)[N], float ref, float c) {
+  if (!large(ref)) {
+    const float rc = -__fmul_rn(ref, c);
+    const float2 cc = make_float2(c, c), r = make_float2(rc, rc);
+#pragma unroll
+    for (int e = 0; e < N; e += 2) {
+      const float2 t = fma2(make_float2(z[e], z[e + 1]), cc, r);
+      z[e] = ex2(t.x);
+      z[e + 1] = ex2(t.y);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < N; ++e) z[e] = ex2((z[e] - ref) * c);
+  }
+}
+
 template <typename T, bool GREEDY>
 __device__ __forceinline__ Fold fold(const Segment<T>& seg, float c, int lane, int& arg) {
   constexpr int N = Elem<T>::N;
-  Fold f{minus_inf(), 0.f};
+  float m = minus_inf();
+  float2 s = make_float2(0.f, 0.f);
   const int nb = seg.blocks();
+#pragma unroll 2
   for (int k = lane; k < nb; k += 32) {
     float z[N];
     seg.load(k, z);
     float top = z[0];
 #pragma unroll
     for (int e = 1; e < N; ++e) top = fmaxf(top, z[e]);
-    if (top > f.m) {
-      f.s *= ex2((f.m - top) * c);
-      f.m = top;
+    if (top > m) {
+      const float f = power(m, top, c);
+      s.x *= f;
+      s.y *= f;
+      m = top;
       if (GREEDY) {
 #pragma unroll
         for (int e = N - 1; e >= 0; --e)
           if (z[e] == top) arg = k * N + e - seg.lo;
       }
     }
-    const float ref = f.m == minus_inf() ? 0.f : f.m;
-    float s = 0.f;
+    exps(z, m == minus_inf() ? 0.f : m, c);
 #pragma unroll
-    for (int e = 0; e < N; ++e) s += ex2((z[e] - ref) * c);
-    f.s += s;
+    for (int e = 0; e < N; e += 2) s = add2(s, make_float2(z[e], z[e + 1]));
   }
-  const float M = redux_max(f.m);
-  const float s = warp_sum(f.s == 0.f ? 0.f : f.s * ex2((f.m - M) * c));
+  const float mine = s.x + s.y, M = redux_max(m);
+  const float sum = warp_sum(mine == 0.f ? 0.f : mine * power(m, M, c));
   if (GREEDY) {
-    const uint32_t best = __reduce_min_sync(0xffffffffu, f.m == M ? static_cast<uint32_t>(arg) : 0xffffffffu);
+    const uint32_t best = __reduce_min_sync(0xffffffffu, m == M ? static_cast<uint32_t>(arg) : 0xffffffffu);
     arg = static_cast<int>(best);
   }
-  return Fold{M, s};
+  return Fold{M, sum};
 }
 
 // One entry per segment, the same table in every CTA of the cluster.
@@ -182,6 +230,14 @@ struct Table {
   Fold d[kMaxSeg];      // draft
   float r[kMaxSeg];     // weight of the segment in a draw from max(p - q, 0)
   int32_t arg[kMaxSeg]; // greedy: first largest entry
+};
+
+// What the first warp of a CTA finds for the others.
+struct Decision {
+  Fold t, d;     // both rows
+  float left;    // of the draw: what is left to pass within the segment `at`
+  int32_t at;    // -1: no segment has any weight
+  int32_t over;  // nothing left to do: accepted, greedy, or no numbers
 };
 
 __device__ __forceinline__ void put_f2(uint32_t addr, float a, float b) {
@@ -197,40 +253,43 @@ __device__ __forceinline__ Fold merged(const Fold* f, int n, float c, int lane) 
   for (int k = lane; k < n; k += 32) m = fmaxf(m, f[k].m);
   const float M = redux_max(m);
   float s = 0.f;
-  for (int k = lane; k < n; k += 32) s += f[k].s == 0.f ? 0.f : f[k].s * ex2((f[k].m - M) * c);
+  for (int k = lane; k < n; k += 32) s += f[k].s == 0.f ? 0.f : f[k].s * power(f[k].m, M, c);
   return Fold{M, warp_sum(s)};
+}
+
+__device__ __forceinline__ float logp_of(float z, const Fold& row, float c) {
+  return (exponent(z, row.m, c) - log2f(row.s)) * kLn2;
 }
 
 // The segment in which the running sum of the weights w(k) passes u times their total, and what is left
 // to pass within it. The last segment with any weight where rounding leaves none; -1: no weight at all.
+// In fp32: the running sum of at most 128 weights (the FP64 form took half of the kernel's time).
 template <typename W>
-__device__ __forceinline__ int pick(int n, double u, int lane, W w, float& left) {
-  // lane l holds segments [4 l, 4 l + 4)
-  double mine[kMaxSeg / 32], sum = 0.0;
+__device__ __forceinline__ int pick(int n, float u, int lane, W w, float& left) {
+  constexpr int M = kMaxSeg / 32;  // lane l holds segments [M l, M l + M)
+  float mine[M], sum = 0.f;
 #pragma unroll
-  for (int i = 0; i < kMaxSeg / 32; ++i) {
-    const int k = lane * (kMaxSeg / 32) + i;
-    mine[i] = k < n ? static_cast<double>(w(k)) : 0.0;
+  for (int i = 0; i < M; ++i) {
+    mine[i] = lane * M + i < n ? w(lane * M + i) : 0.f;
     sum += mine[i];
   }
-  double run = sum;
+  float run = sum;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const double up = __shfl_up_sync(0xffffffffu, run, o);
+    const float up = __shfl_up_sync(0xffffffffu, run, o);
     if (lane >= o) run += up;
   }
-  const double total = __shfl_sync(0xffffffffu, run, 31), goal = u * total;
-  double before = run - sum;
+  const float goal = u * __shfl_sync(0xffffffffu, run, 31);
+  float before = run - sum;
   int at = -1, last = -1;
   float rest = 0.f, last_rest = 0.f;
 #pragma unroll
-  for (int i = 0; i < kMaxSeg / 32; ++i) {
-    const int k = lane * (kMaxSeg / 32) + i;
-    if (mine[i] > 0.0) {
-      last = k;
-      last_rest = static_cast<float>(goal - before);
+  for (int i = 0; i < M; ++i) {
+    if (mine[i] > 0.f) {
+      last = lane * M + i;
+      last_rest = goal - before;
       if (at < 0 && before + mine[i] > goal) {
-        at = k;
+        at = last;
         rest = last_rest;
       }
     }
@@ -292,6 +351,10 @@ __device__ __forceinline__ int locate(const Segment<T>& seg, float left, int lan
 // A row is finished (its result written, if it has one): the last of its sequence writes what the
 // sequence comes to and leaves the sequence's words at zero. By one thread.
 __device__ __forceinline__ void finish(const Args& p, int b, int o, int K) {
+  if (p.max_draft == 0) {  // sequences of one row
+    p.n_accepted[b] = 0;
+    return;
+  }
   __threadfence();
   if (atomicAdd(p.finished + b, 1u) != static_cast<uint32_t>(K)) return;
   __threadfence();
@@ -311,6 +374,7 @@ __global__ void __launch_bounds__(kWarps * 32) verify_kernel(const Args p) {
   __shared__ __align__(8) uint64_t bars[kWarps][2];
   __shared__ __align__(16) Table tab;
   __shared__ int32_t skip;
+  __shared__ Decision dec;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_ctarank(), C = cluster_nctarank();
   const int id = blockIdx.x / C, j = id / p.n_seq, b = id % p.n_seq;
@@ -378,13 +442,17 @@ __global__ void __launch_bounds__(kWarps * 32) verify_kernel(const Args p) {
   const float us = p.sample_u[b];
 
   // ---- both rows' folds, to every CTA's table
+  const float c = p.c;
   bool in_time = mbar_wait_bounded(&bars[warp][0], 0);
+  st.blank_edges(lane);
   int arg = 0;
-  Fold ft = fold<T, GREEDY>(st, p.c, lane, arg), fd{minus_inf(), 0.f};
+  const Fold ft = fold<T, GREEDY>(st, c, lane, arg);
+  Fold fd{minus_inf(), 0.f};
   if (two) {
     in_time = mbar_wait_bounded(&bars[warp][1], 0) && in_time;
+    sd.blank_edges(lane);
     int unused = 0;
-    fd = fold<T, false>(sd, p.c, lane, unused);
+    fd = fold<T, false>(sd, c, lane, unused);
   }
   if (!in_time && lane == 0) flag_status(p.status, RL_DEV_TIMEOUT);
   __syncwarp();
@@ -397,56 +465,64 @@ __global__ void __launch_bounds__(kWarps * 32) verify_kernel(const Args p) {
   __syncwarp();
   cluster_sync_all();
 
-  // ---- the decision, by every warp alike
-  const float c = p.c;
-  const Fold ht = merged(tab.t, n_seg, c, lane);
-  Fold hd{0.f, 1.f};
-  if (two) hd = merged(tab.d, n_seg, c, lane);
-  const bool bad = !(ht.s > 0.f && ht.s < 3e38f) || !(hd.s > 0.f && hd.s < 3e38f);
-  const float log2s = log2f(ht.s);
-  auto logp_of = [&](float z) { return fmaf(z - ht.m, c, -log2s) * kLn2; };
-  int token = -1;  // greedy
-  if (GREEDY && !bad) {
-    uint32_t best = 0xffffffffu;
-    for (int k = lane; k < n_seg; k += 32)
-      if (tab.t[k].m == ht.m) best = min(best, static_cast<uint32_t>(k * p.seg + tab.arg[k]));
-    token = static_cast<int>(__reduce_min_sync(0xffffffffu, best));
-  }
-  bool accept = false;
-  const float it = 1.f / ht.s, id_ = 1.f / hd.s;
-  if (tested && !bad && x >= 0) {
-    if (GREEDY) {
-      accept = x == token;
-    } else {
-      const float px = ex2((zx - ht.m) * c) * it;
-      const float qx = two ? ex2((zdx - hd.m) * c) * id_ : 1.f;
-      accept = ua * qx < px;
+  // ---- the decision, by the first warp of every CTA alike
+  const Fold* seg_t = tab.t;
+  auto weight_p = [seg_t, c](const Fold& ht) {
+    return [seg_t, ht, c](int k) { return seg_t[k].s == 0.f ? 0.f : seg_t[k].s * power(seg_t[k].m, ht.m, c); };
+  };
+  if (warp == 0) {
+    const Fold ht = merged(tab.t, n_seg, c, lane);
+    Fold hd{0.f, 1.f};
+    if (two) hd = merged(tab.d, n_seg, c, lane);
+    const bool bad = !(ht.s > 0.f && ht.s < 3e38f) || !(hd.s > 0.f && hd.s < 3e38f);
+    int token = -1;  // greedy
+    if (GREEDY && !bad) {
+      uint32_t best = 0xffffffffu;
+      for (int k = lane; k < n_seg; k += 32)
+        if (tab.t[k].m == ht.m) best = min(best, static_cast<uint32_t>(k * p.seg + tab.arg[k]));
+      token = static_cast<int>(__reduce_min_sync(0xffffffffu, best));
+    }
+    bool accept = false;
+    if (tested && !bad && x >= 0) {
+      if (GREEDY) {
+        accept = x == token;
+      } else {
+        const float px = ex2(exponent(zx, ht.m, c)) / ht.s;
+        const float qx = two ? ex2(exponent(zdx, hd.m, c)) / hd.s : 1.f;
+        accept = ua * qx < px;
+      }
+    }
+    const bool over = accept || bad || GREEDY;
+    float left = 0.f;
+    int at = -1;
+    if (!over && !tested) at = pick(n_seg, us, lane, weight_p(ht), left);
+    if (lane == 0) {
+      dec = Decision{ht, hd, left, at, over};
+      if (rank == 0 && over) {
+        if (bad) flag_status(p.status, RL_DEV_BAD_VALUE);
+        if (!accept && p.max_draft > 0) atomicMax(p.refused + b, kFirst - j);
+        p.out_ids[row] = accept ? x : token;
+        p.out_logp[row] = bad ? __int_as_float(0x7fffffff)
+                              : logp_of(accept ? zx : Elem<T>::one(zt[token]), ht, c);
+        finish(p, b, o, K);
+      }
+      // ordered before the sequence's result by the cluster barrier that follows a refusal
+      if (rank == 0 && !over && tested) atomicMax(p.refused + b, kFirst - j);
     }
   }
-  const bool leader = rank == 0 && threadIdx.x == 0;
-  if (accept || bad || GREEDY) {
-    if (leader) {
-      if (bad) flag_status(p.status, RL_DEV_BAD_VALUE);
-      if (!accept) atomicMax(p.refused + b, kFirst - j);
-      p.out_ids[row] = accept ? x : token;
-      p.out_logp[row] = bad ? __int_as_float(0x7fffffff)
-                            : logp_of(accept ? zx : Elem<T>::one(zt[token]));
-      finish(p, b, o, K);
-    }
-    return;
-  }
-  // ordered before the sequence's result by the cluster barrier that follows a refusal
-  if (tested && leader) atomicMax(p.refused + b, kFirst - j);
+  __syncthreads();
+  if (dec.over) return;
 
   // ---- the draw: from max(p - q, 0) after a refusal, else from p
-  float left;
-  int at = -1;
+  const Fold ht = dec.t, hd = dec.d;
+  const float it = 1.f / ht.s, id_ = 1.f / hd.s;
+  int at = dec.at;
+  float left = dec.left;
   bool plain = !tested;
   const int shift = sd.lo - st.lo;
   auto weights_p = [&](int k, float (&w)[Elem<T>::N]) {
     st.load(k, w);
-#pragma unroll
-    for (int e = 0; e < Elem<T>::N; ++e) w[e] = ex2((w[e] - ht.m) * c);
+    exps(w, ht.m, c);
   };
   auto weights_r = [&](int k, float (&w)[Elem<T>::N]) {
     constexpr int N = Elem<T>::N;
@@ -456,14 +532,13 @@ __global__ void __launch_bounds__(kWarps * 32) verify_kernel(const Args p) {
       if (shift == 0) {
         sd.load(k, y);
       } else {
+        // beyond the segment's ends, where p is zero, this may be any number
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-          const int i = k * N + e;
-          y[e] = i >= st.lo && i < st.hi ? Elem<T>::one(sd.at[i + shift]) : minus_inf();
-        }
+        for (int e = 0; e < N; ++e) y[e] = Elem<T>::one(sd.at[k * N + e + shift]);
       }
+      exps(y, hd.m, c);
 #pragma unroll
-      for (int e = 0; e < N; ++e) w[e] = fmaxf(fmaf(-ex2((y[e] - hd.m) * c), id_, w[e] * it), 0.f);
+      for (int e = 0; e < N; ++e) w[e] = fmaxf(fmaf(-y[e], id_, w[e] * it), 0.f);
     } else {
       const int i = x - e0 + st.lo - k * N;
 #pragma unroll
@@ -472,30 +547,28 @@ __global__ void __launch_bounds__(kWarps * 32) verify_kernel(const Args p) {
     }
   };
   if (!plain) {
-    float r = 0.f;
+    float2 r = make_float2(0.f, 0.f);
     const int nb = st.blocks();
     for (int k = lane; k < nb; k += 32) {
       float w[Elem<T>::N];
       weights_r(k, w);
 #pragma unroll
-      for (int e = 0; e < Elem<T>::N; ++e) r += w[e];
+      for (int e = 0; e < Elem<T>::N; e += 2) r = add2(r, make_float2(w[e], w[e + 1]));
     }
-    r = warp_sum(r);
-    if (lane < C) put_f1(map_to_rank(smem_addr(&tab.r[g]), lane), r);
+    const float sum = warp_sum(r.x + r.y);
+    if (lane < C) put_f1(map_to_rank(smem_addr(&tab.r[g]), lane), sum);
     __syncwarp();
     cluster_sync_all();
-    at = pick(n_seg, static_cast<double>(us), lane, [&](int k) { return tab.r[k]; }, left);
+    at = pick(n_seg, us, lane, [&](int k) { return tab.r[k]; }, left);
     plain = at < 0;  // p and q are equal up to rounding
+    if (plain) at = pick(n_seg, us, lane, weight_p(ht), left);
   }
-  if (plain)
-    at = pick(n_seg, static_cast<double>(us), lane,
-              [&](int k) { return tab.t[k].s == 0.f ? 0.f : tab.t[k].s * ex2((tab.t[k].m - ht.m) * c); }, left);
   if (at != g) return;
   const int i = plain ? locate(st, left, lane, weights_p) : locate(st, left, lane, weights_r);
   if (lane == 0) {
-    token = e0 + max(i, 0);
+    const int token = e0 + max(i, 0);
     p.out_ids[row] = token;
-    p.out_logp[row] = logp_of(Elem<T>::one(zt[token]));
+    p.out_logp[row] = logp_of(Elem<T>::one(zt[token]), ht, c);
     finish(p, b, o, K);
   }
 }
@@ -530,7 +603,7 @@ rl_status run(Args& a, cudaStream_t s) {
   a.seg = static_cast<int32_t>(segment(a.V, C));
   a.seg_bytes = static_cast<int32_t>(segment_bytes(a.V, C, es));
   a.held = held;
-  const size_t smem = static_cast<size_t>(kWarps) * held * a.seg_bytes;
+  const size_t smem = static_cast<size_t>(kWarps) * held * a.seg_bytes + 16;  // a block read past the last segment
   auto kern = verify_kernel<T, GREEDY>;
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute attr[1];
@@ -564,7 +637,7 @@ rl_status run(Args& a, cudaStream_t s) {
       if (n <= 0) return set_error(RL_ERR_UNSUPPORTED, "verify_kernel: no cluster fits on the device");
       it = resident.emplace(key, n).first;
     }
-    a.check_from = it->second;
+    a.check_from = a.max_draft == 0 ? static_cast<int32_t>(clusters) : it->second;
   }
   cfg.gridDim = dim3(static_cast<unsigned>(clusters * C));
   e = cudaLaunchKernelEx(&cfg, kern, a);
@@ -630,7 +703,7 @@ extern "C" rl_status rl_verify_drafts(const void* target_logits, const void* dra
   } else {
     a.finished = reinterpret_cast<uint32_t*>(base + kWsHeader);
     a.refused = reinterpret_cast<int32_t*>(a.finished + n_seq);
-    const cudaError_t e = cudaMemsetAsync(a.finished, 0, static_cast<size_t>(n_seq) * 8, s);
+    const cudaError_t e = max_draft == 0 ? cudaSuccess : cudaMemsetAsync(a.finished, 0, static_cast<size_t>(n_seq) * 8, s);
     if (e != cudaSuccess) return cuda_error(e, "rl_verify_drafts: cudaMemsetAsync");
   }
   if (dtype == RL_BF16) return greedy ? verify::run<uint16_t, true>(a, s) : verify::run<uint16_t, false>(a, s);
