@@ -7,10 +7,10 @@
 // the lowest v at which the running sum of its weights passes s_b times their total. T = 0: greedy,
 // the row's first largest entry is both the test and the draw.
 //
-// One thread-block cluster per row, rows in the order of their place j in their sequences: by the
-// time a late row starts its sequence has often been refused earlier, and it is skipped; rows that
-// start with the first wave are not held up by that question. Nothing waits for another cluster: the
-// last of a sequence's rows to finish writes the sequence's result.
+// Rows are worked on in the order of their place j in their sequences: by the time a late row starts
+// its sequence has often been refused earlier, and it is skipped. Nothing waits for another row: the
+// last of a sequence's rows to finish writes the sequence's result. Where there are rows for all SMs, a
+// CTA takes a row (row_kernel, below); else one thread-block cluster does (verify_kernel):
 //
 // Every warp of the cluster owns one segment of the vocabulary. It brings the segment of both rows
 // into its own shared memory by bulk copies (one barrier each, so a warp starts when its own data is
@@ -70,6 +70,7 @@ struct Elem<uint16_t> {
   }
   static __device__ __forceinline__ float one(uint16_t x) { return bf16_to_f32(x); }
   static __device__ __forceinline__ uint16_t none() { return 0xff80; }
+  static __device__ __forceinline__ uint32_t bits(uint16_t x) { return x; }
 };
 template <>
 struct Elem<float> {
@@ -79,6 +80,7 @@ struct Elem<float> {
   }
   static __device__ __forceinline__ float one(float x) { return x; }
   static __device__ __forceinline__ float none() { return -__int_as_float(0x7f800000); }
+  static __device__ __forceinline__ uint32_t bits(float x) { return __float_as_uint(x); }
 };
 
 __device__ __forceinline__ float minus_inf() { return -__int_as_float(0x7f800000); }
@@ -257,22 +259,21 @@ __device__ __forceinline__ Fold merged(const Fold* f, int n, float c, int lane) 
   return Fold{M, warp_sum(s)};
 }
 
+// No numbers: a row without a finite largest entry, or with a NaN.
+__device__ __forceinline__ bool is_bad(const Fold& f) { return !(f.s > 0.f && f.s < 3e38f); }
+
 __device__ __forceinline__ float logp_of(float z, const Fold& row, float c) {
   return (exponent(z, row.m, c) - log2f(row.s)) * kLn2;
 }
 
 // The segment in which the running sum of the weights w(k) passes u times their total, and what is left
 // to pass within it. The last segment with any weight where rounding leaves none; -1: no weight at all.
-// In fp32: the running sum of at most 128 weights (the FP64 form took half of the kernel's time).
+// In fp32: the running sum of some hundred weights (the FP64 form took half of the kernel's time).
 template <typename W>
 __device__ __forceinline__ int pick(int n, float u, int lane, W w, float& left) {
-  constexpr int M = kMaxSeg / 32;  // lane l holds segments [M l, M l + M)
-  float mine[M], sum = 0.f;
-#pragma unroll
-  for (int i = 0; i < M; ++i) {
-    mine[i] = lane * M + i < n ? w(lane * M + i) : 0.f;
-    sum += mine[i];
-  }
+  const int M = (n + 31) / 32, k0 = min(lane * M, n), k1 = min(k0 + M, n);  // lane l holds M segments
+  float sum = 0.f;
+  for (int k = k0; k < k1; ++k) sum += w(k);
   float run = sum;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -283,17 +284,17 @@ __device__ __forceinline__ int pick(int n, float u, int lane, W w, float& left) 
   float before = run - sum;
   int at = -1, last = -1;
   float rest = 0.f, last_rest = 0.f;
-#pragma unroll
-  for (int i = 0; i < M; ++i) {
-    if (mine[i] > 0.f) {
-      last = lane * M + i;
+  for (int k = k0; k < k1; ++k) {
+    const float mine = w(k);
+    if (mine > 0.f) {
+      last = k;
       last_rest = goal - before;
-      if (at < 0 && before + mine[i] > goal) {
-        at = last;
+      if (at < 0 && before + mine > goal) {
+        at = k;
         rest = last_rest;
       }
     }
-    before += mine[i];
+    before += mine;
   }
   const uint32_t found = __ballot_sync(0xffffffffu, at >= 0), any = __ballot_sync(0xffffffffu, last >= 0);
   if (any == 0) {
@@ -306,12 +307,11 @@ __device__ __forceinline__ int pick(int n, float u, int lane, W w, float& left) 
 }
 
 // The place within a segment at which the running sum of the weights of its elements passes `left`
-// (the last with any weight where rounding leaves none; -1: none has any). w(k, x): the weights of block
-// k's elements.
+// (the last with any weight where rounding leaves none; -1: none has any). The segment begins at element lo
+// of its nb blocks; w(k, x): the weights of block k's elements.
 template <typename T, typename W>
-__device__ __forceinline__ int locate(const Segment<T>& seg, float left, int lane, W w) {
+__device__ __forceinline__ int locate(int lo, int nb, float left, int lane, W w) {
   constexpr int N = Elem<T>::N;
-  const int nb = seg.blocks();
   int last = -1;
   float before = 0.f;
   for (int k0 = 0; k0 < nb; k0 += 32) {
@@ -323,7 +323,7 @@ __device__ __forceinline__ int locate(const Segment<T>& seg, float left, int lan
 #pragma unroll
     for (int e = 0; e < N; ++e) {
       sum += x[e];
-      if (x[e] > 0.f) last = k * N + e - seg.lo;
+      if (x[e] > 0.f) last = k * N + e - lo;
     }
     float run = sum;
 #pragma unroll
@@ -339,7 +339,7 @@ __device__ __forceinline__ int locate(const Segment<T>& seg, float left, int lan
 #pragma unroll
       for (int e = 0; e < N; ++e) {
         acc += x[e];
-        if (at < 0 && x[e] > 0.f && acc > left) at = k * N + e - seg.lo;
+        if (at < 0 && x[e] > 0.f && acc > left) at = k * N + e - lo;
       }
       return __shfl_sync(0xffffffffu, at >= 0 ? at : last, from);
     }
@@ -474,7 +474,7 @@ __global__ void __launch_bounds__(kWarps * 32) verify_kernel(const Args p) {
     const Fold ht = merged(tab.t, n_seg, c, lane);
     Fold hd{0.f, 1.f};
     if (two) hd = merged(tab.d, n_seg, c, lane);
-    const bool bad = !(ht.s > 0.f && ht.s < 3e38f) || !(hd.s > 0.f && hd.s < 3e38f);
+    const bool bad = is_bad(ht) || is_bad(hd);
     int token = -1;  // greedy
     if (GREEDY && !bad) {
       uint32_t best = 0xffffffffu;
@@ -564,12 +564,317 @@ __global__ void __launch_bounds__(kWarps * 32) verify_kernel(const Args p) {
     if (plain) at = pick(n_seg, us, lane, weight_p(ht), left);
   }
   if (at != g) return;
-  const int i = plain ? locate(st, left, lane, weights_p) : locate(st, left, lane, weights_r);
+  const int nb = st.blocks();
+  const int i = plain ? locate<T>(st.lo, nb, left, lane, weights_p) : locate<T>(st.lo, nb, left, lane, weights_r);
   if (lane == 0) {
     const int token = e0 + max(i, 0);
     p.out_ids[row] = token;
     p.out_logp[row] = logp_of(Elem<T>::one(zt[token]), ht, c);
     finish(p, b, o, K);
+  }
+}
+
+// ---------------------------------------------------------------- many rows: a CTA takes a row
+//
+// Plain 16-byte loads, one tile of a warp ahead of the fold; several CTAs per SM hide each other's row
+// ends. Nothing of a row is kept: a draw from p reads one tile of the row again (the fold leaves every
+// tile's weight in a table), one from p without the drafted token that token's tile too, and a draw from
+// max(p - q, 0) both rows (the first pass knows neither normaliser): at most one row of a sequence is read
+// twice. What bounds it is HBM with the exponentials
+// close behind (16 per clock and SM; at 6.8 TB/s 11.8 bf16 entries arrive in that time). Measured against a
+// cluster per row with both rows in shared memory, whose exchanges leave the copies idle half of the time.
+
+constexpr int kTileBlocks = 4;      // 16-byte blocks per lane and tile
+constexpr int kMaxTiles = 1024;     // of a row
+
+// A row in 16-byte blocks of memory, the first at the block that holds its first element.
+template <typename T>
+struct Blocks {
+  const T* base;
+  int lo, hi;  // the row is elements [lo, hi) from there
+  __device__ __forceinline__ Blocks(const T* row, int V) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(row);
+    base = reinterpret_cast<const T*>(a & ~uintptr_t(15));
+    lo = static_cast<int>(row - base);
+    hi = lo + V;
+  }
+  // Block k; what is not the row's is minus infinity.
+  __device__ __forceinline__ uint4 load(int k) const {
+    constexpr int N = Elem<T>::N;
+    if (k * N >= lo && (k + 1) * N <= hi) return __ldg(reinterpret_cast<const uint4*>(base + static_cast<int64_t>(k) * N));
+    uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const int i = k * N + e;
+      const T x = i >= lo && i < hi ? base[i] : Elem<T>::none();
+      if (sizeof(T) == 2) w[e / 2] |= static_cast<uint32_t>(Elem<T>::bits(x)) << (16 * (e & 1));
+      else w[e % 4] = Elem<T>::bits(x);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+};
+
+__device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+
+// The largest entry of a lane's blocks (NaNs do not count unless there is nothing else).
+template <typename T>
+__device__ __forceinline__ float largest(const uint4 (&w)[kTileBlocks]) {
+  if (sizeof(T) == 2) {
+    uint32_t t = w[0].x;
+#pragma unroll
+    for (int i = 0; i < kTileBlocks; ++i)
+      t = max_bf16x2(t, max_bf16x2(max_bf16x2(w[i].x, w[i].y), max_bf16x2(w[i].z, w[i].w)));
+    return fmaxf(bf16_lo(t), bf16_hi(t));
+  }
+  float m = __uint_as_float(w[0].x);
+#pragma unroll
+  for (int i = 0; i < kTileBlocks; ++i)
+    m = fmaxf(m, fmaxf(fmaxf(__uint_as_float(w[i].x), __uint_as_float(w[i].y)),
+                       fmaxf(__uint_as_float(w[i].z), __uint_as_float(w[i].w))));
+  return m;
+}
+
+// A lane's sums over what it has seen.
+struct Running {
+  float m;
+  float2 s;
+  int32_t arg;  // greedy: first largest entry
+};
+
+template <typename T, bool GREEDY>
+__device__ __forceinline__ void add_tile(Running& r, const uint4 (&w)[kTileBlocks], int k0, float c) {
+  constexpr int N = Elem<T>::N;
+  const float top = largest<T>(w);
+  if (top > r.m) {
+    const float f = power(r.m, top, c);
+    r.s.x *= f;
+    r.s.y *= f;
+    r.m = top;
+    if (GREEDY) {
+#pragma unroll
+      for (int i = kTileBlocks - 1; i >= 0; --i) {
+        float z[N];
+        Elem<T>::unpack(w[i], z);
+#pragma unroll
+        for (int e = N - 1; e >= 0; --e)
+          if (z[e] == top) r.arg = (k0 + 32 * i) * N + e;
+      }
+    }
+  }
+  const float ref = r.m == minus_inf() ? 0.f : r.m;
+#pragma unroll
+  for (int i = 0; i < kTileBlocks; ++i) {
+    float z[N];
+    Elem<T>::unpack(w[i], z);
+    exps(z, ref, c);
+#pragma unroll
+    for (int e = 0; e < N; e += 2) r.s = add2(r.s, make_float2(z[e], z[e + 1]));
+  }
+}
+
+// The warp's sums of all its lanes.
+__device__ __forceinline__ Fold of_warp(const Running& r, float c) {
+  const float mine = r.s.x + r.s.y, M = redux_max(r.m);
+  return Fold{M, warp_sum(mine == 0.f ? 0.f : mine * power(r.m, M, c))};
+}
+
+template <typename T, bool GREEDY>
+__global__ void __launch_bounds__(kWarps * 32, 3) row_kernel(const Args p) {
+  constexpr int N = Elem<T>::N;
+  constexpr int kTile = kTileBlocks * 32 * N;  // elements of a tile
+  __shared__ Fold tiles[kMaxTiles];            // a draw's weights by tile: sums, or (in s) max(p - q, 0)
+  __shared__ Fold rows[2][kWarps];
+  __shared__ int32_t args[kWarps];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int j = blockIdx.x / p.n_seq, b = blockIdx.x % p.n_seq;
+  const float c = p.c;
+  const int o = p.offsets[b], o1 = p.offsets[b + 1];
+  const int K = o1 - o;
+  if (o < 0 || o1 < o || o1 > p.n_draft || K > p.max_draft) {
+    if (j == 0 && threadIdx.x == 0) {
+      flag_status(p.status, RL_DEV_BAD_OFFSETS);
+      p.n_accepted[b] = -1;
+    }
+    return;
+  }
+  if (j > K) return;
+  if (j > 0) {
+    // one thread asks, so that the CTA decides as one
+    int f = 0;
+    if (threadIdx.x == 0) f = *reinterpret_cast<volatile int32_t*>(p.refused + b);
+    if (__syncthreads_or(f && kFirst - f < j)) {
+      if (threadIdx.x == 0) finish(p, b, o, K);
+      return;
+    }
+  }
+  const int64_t row = static_cast<int64_t>(o) + b + j, drow = static_cast<int64_t>(o) + j;
+  const bool tested = j < K, two = tested && !GREEDY && p.draft != nullptr;
+  const T* zt = static_cast<const T*>(p.target) + row * p.ld_t;
+  const T* zd = two ? static_cast<const T*>(p.draft) + drow * p.ld_d : zt;
+  const Blocks<T> bt(zt, p.V), bd(zd, p.V);
+  int x = -1;
+  float zx = 0.f, zdx = 0.f, ua = 0.f;
+  if (tested) {
+    x = p.draft_ids[drow];
+    ua = p.accept_u[drow];
+    if (x < 0 || x >= p.V) {
+      if (threadIdx.x == 0) flag_status(p.status, RL_DEV_BAD_TOKEN);
+      x = -1;
+    } else {
+      zx = Elem<T>::one(zt[x]);
+      if (two) zdx = Elem<T>::one(zd[x]);
+    }
+  }
+
+  // ---- one pass; the tiles go to the warps in turn
+  const int nt = (bt.hi + kTile - 1) / kTile;
+  const bool draws = !GREEDY && !two;  // the tiles' weights are of use
+  auto pass = [&](const Blocks<T>& bl, int r) {
+    const int n = (bl.hi + kTile - 1) / kTile;
+    Running run{minus_inf(), {0.f, 0.f}, 0};
+    uint4 w[2][kTileBlocks];
+    auto load = [&](uint4 (&to)[kTileBlocks], int t) {
+      const int k0 = t * kTileBlocks * 32 + lane;
+#pragma unroll
+      for (int i = 0; i < kTileBlocks; ++i) to[i] = bl.load(k0 + 32 * i);
+    };
+    auto take = [&](const uint4 (&from)[kTileBlocks], int t) {
+      if (draws) run = Running{minus_inf(), {0.f, 0.f}, 0};
+      add_tile<T, GREEDY>(run, from, t * kTileBlocks * 32 + lane, c);
+      if (draws) {
+        const Fold f = of_warp(run, c);
+        if (lane == 0) tiles[t] = f;
+      }
+    };
+    int t = warp;
+    if (t < n) load(w[0], t);
+    while (t < n) {
+      load(w[1], t + kWarps);
+      take(w[0], t);
+      t += kWarps;
+      if (t >= n) break;
+      load(w[0], t + kWarps);
+      take(w[1], t);
+      t += kWarps;
+    }
+    if (draws) return;
+    const Fold f = of_warp(run, c);
+    if (lane == 0) rows[r][warp] = f;
+    if (GREEDY) {
+      const uint32_t best = __reduce_min_sync(0xffffffffu, run.m == f.m ? static_cast<uint32_t>(run.arg) : 0xffffffffu);
+      if (lane == 0) args[warp] = static_cast<int32_t>(best);
+    }
+  };
+  pass(bt, 0);
+  if (two) pass(bd, 1);
+  __syncthreads();
+
+  // ---- the decision, by every warp alike
+  const Fold ht = draws ? merged(tiles, nt, c, lane) : merged(rows[0], kWarps, c, lane);
+  Fold hd{0.f, 1.f};
+  if (two) hd = merged(rows[1], kWarps, c, lane);
+  const bool bad = is_bad(ht) || is_bad(hd);
+  int token = -1;
+  bool accept = false;
+  if (GREEDY && !bad) {
+    const uint32_t best = lane < kWarps && rows[0][lane].m == ht.m ? static_cast<uint32_t>(args[lane]) : 0xffffffffu;
+    token = static_cast<int>(__reduce_min_sync(0xffffffffu, best)) - bt.lo;
+  }
+  if (tested && !bad && x >= 0) {
+    if (GREEDY) {
+      accept = x == token;
+    } else {
+      const float px = ex2(exponent(zx, ht.m, c)) / ht.s;
+      const float qx = two ? ex2(exponent(zdx, hd.m, c)) / hd.s : 1.f;
+      accept = ua * qx < px;
+    }
+  }
+  auto result = [&](int id, float lp, bool refusal) {
+    if (refusal && p.max_draft > 0) atomicMax(p.refused + b, kFirst - j);
+    p.out_ids[row] = id;
+    p.out_logp[row] = lp;
+    finish(p, b, o, K);
+  };
+  if (accept || bad || GREEDY) {
+    if (threadIdx.x == 0) {
+      if (bad) flag_status(p.status, RL_DEV_BAD_VALUE);
+      result(accept ? x : token, bad ? __int_as_float(0x7fffffff) : logp_of(accept ? zx : Elem<T>::one(zt[token]), ht, c),
+             !accept);
+    }
+    return;
+  }
+
+  // ---- the draw: from max(p - q, 0) after a refusal, else from p
+  const float it = 1.f / ht.s, id_ = 1.f / hd.s, us = p.sample_u[b];
+  const int shift = bd.lo - bt.lo;
+  auto weights_p = [&](int k, float (&w)[N]) {
+    Elem<T>::unpack(bt.load(k), w);
+    exps(w, ht.m, c);
+  };
+  auto weights_r = [&](int k, float (&w)[N]) {
+    weights_p(k, w);
+    if (two) {
+      float y[N];
+      if (shift == 0) {
+        Elem<T>::unpack(bd.load(k), y);
+      } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+          const int i = k * N + e;
+          y[e] = i >= bt.lo && i < bt.hi ? Elem<T>::one(bd.base[i + shift]) : minus_inf();
+        }
+      }
+      exps(y, hd.m, c);
+#pragma unroll
+      for (int e = 0; e < N; ++e) w[e] = fmaxf(fmaf(-y[e], id_, w[e] * it), 0.f);
+    } else {
+      const int i = x + bt.lo - k * N;
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (e == i) w[e] = 0.f;
+    }
+  };
+  // the weight of tile t, by a warp
+  auto weigh = [&](int t, auto weights) {
+    float2 r = make_float2(0.f, 0.f);
+#pragma unroll 2
+    for (int i = 0; i < kTileBlocks; ++i) {
+      float w[N];
+      weights(t * kTileBlocks * 32 + 32 * i + lane, w);
+#pragma unroll
+      for (int e = 0; e < N; e += 2) r = add2(r, make_float2(w[e], w[e + 1]));
+    }
+    const float sum = warp_sum(r.x + r.y);
+    if (lane == 0) tiles[t] = Fold{ht.m, sum};
+    __syncwarp();
+  };
+  if (two) {
+    for (int t = warp; t < nt; t += kWarps) weigh(t, weights_r);
+    __syncthreads();
+  }
+  if (warp != 0) return;
+  if (tested && !two && x >= 0) weigh((x + bt.lo) / kTile, weights_r);  // p without the token
+  bool plain = !tested;
+  float left;
+  auto weight = [&](int k) { return tiles[k].s == 0.f ? 0.f : tiles[k].s * power(tiles[k].m, ht.m, c); };
+  int at = pick(nt, us, lane, weight, left);
+  if (at < 0) {
+    // p and q are equal up to rounding: a draw from p, whose tiles are weighed by this warp alone
+    plain = true;
+    for (int t = 0; t < nt; ++t) weigh(t, weights_p);
+    at = pick(nt, us, lane, weight, left);
+  }
+  const int first = at * kTileBlocks * 32;  // the tile's first block
+  const int nb = min(kTileBlocks * 32, (bt.hi + N - 1) / N - first);
+  const int i = plain ? locate<T>(0, nb, left, lane, [&](int k, float (&w)[N]) { weights_p(first + k, w); })
+                      : locate<T>(0, nb, left, lane, [&](int k, float (&w)[N]) { weights_r(first + k, w); });
+  if (lane == 0) {
+    const int drawn = min(max(first * N + i - bt.lo, 0), p.V - 1);
+    result(drawn, logp_of(Elem<T>::one(zt[drawn]), ht, c), tested);
   }
 }
 
@@ -594,8 +899,18 @@ int cluster_of(int64_t V, int es, int rows_held, int64_t clusters) {
   return C;
 }
 
+// Whether a CTA takes a row: where every SM has at least two, and a row's tiles fit in the table.
+inline bool by_rows(int64_t V, int es, int64_t rows) {
+  return rows >= 2 * kSMs && V * es <= int64_t(kMaxTiles - 2) * kTileBlocks * 32 * 16;
+}
+
 template <typename T, bool GREEDY>
 rl_status run(Args& a, cudaStream_t s) {
+  if (by_rows(a.V, sizeof(T), a.n_draft + a.n_seq)) {
+    row_kernel<T, GREEDY><<<static_cast<unsigned>(a.n_seq) * (a.max_draft + 1), kWarps * 32, 0, s>>>(a);
+    const cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? RL_OK : cuda_error(e, "row_kernel launch");
+  }
   const int held = a.draft && !GREEDY ? 2 : 1, es = sizeof(T);
   const int64_t clusters = static_cast<int64_t>(a.n_seq) * (a.max_draft + 1);
   const int C = cluster_of(a.V, es, held, clusters);

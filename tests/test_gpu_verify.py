@@ -242,3 +242,50 @@ def test_binding_refusals(R):
         R.rl_verify_drafts(t, ids, off, u, s, 2, R.make_verify_params(-1.0), ws)
     with pytest.raises(R.RLError):
         R.rl_verify_drafts(t, ids, off, u, s, 2, P, ws[:256])
+
+
+@pytest.mark.parametrize("V,dtype,pad", [(40000, "bf16", 0), (33003, "bf16", 0), (33003, "bf16", 5), (20001, "f32", 0),
+                                         (20000, "f32", 3)])
+@pytest.mark.parametrize("draft,T", [(True, 1.0), (True, 0.6), (False, 1.0), (True, 0.0)])
+def test_many_long_rows(R, V, dtype, pad, draft, T):
+    """More rows than run at once, each of several CTAs."""
+    rng = np.random.default_rng(21)
+    c = VC.make(rng.integers(0, 5, 140), V, dtype, draft, T=T, noise=1.2, masked=0.2, seed=V + pad)
+    assert len(c["ids"]) + 140 >= 304
+    out, ws = call(R, c, pad=pad, draft_pad=(pad * 2) % 7)
+    check(R, c, out, ws)
+    again, _ = call(R, c, ws=ws, pad=pad, draft_pad=(pad * 2) % 7, max_draft=6)
+    assert all(torch.equal(a, b) for a, b in zip(out, again))
+
+
+def test_many_long_rows_and_only_draws(R):
+    c = VC.make([0] * 400, 70001, "bf16", False, T=0.7, seed=22)
+    ws = R.new_workspace(400, 70001)
+    for _ in range(3):
+        check(R, c, call(R, c, ws=ws)[0], ws)
+
+
+def test_many_long_rows_without_numbers(R):
+    """As test_refused_rows_of_numbers and test_bad_tokens_and_offsets, with more rows than run at once."""
+    n, V = 160, 40000
+    c = VC.make([1] * n, V, "bf16", True, noise=0.0, likely=0.0, seed=23)
+    t_row = 2 * np.arange(n)
+    c["draft"] = c["target"][t_row].copy()
+    c["ids"][9] = -1
+    for r, value in ((2 * 3, np.nan), (2 * 5 + 1, np.inf)):
+        c["target"][r, 77] = value
+    c["target"][2 * 7] = -np.inf
+    c["draft"][11, 5] = np.nan
+    c["offsets"][150] = 2000
+    (ids, acc, lp), ws = call(R, c)
+    assert R.rl_query_status(ws)[1] == R.RL_DEV_BAD_VALUE | R.RL_DEV_BAD_TOKEN | R.RL_DEV_BAD_OFFSETS
+    ids, acc, lp = ids.cpu().numpy(), acc.cpu().numpy(), lp.cpu().numpy()
+    want = np.ones(n, np.int64)
+    want[[3, 7, 9, 11]] = 0
+    want[[149, 150]] = -1
+    assert np.array_equal(acc, want)
+    assert (ids[[6, 14, 22]] == -1).all() and np.isnan(lp[[6, 14, 22]]).all() and ids[11] == -1 and np.isnan(lp[11])
+    assert 0 <= ids[18] < V and ids[19] == -1
+    R.rl_workspace_init(ws)
+    good = VC.make([1] * n, 33000, "bf16", True, seed=24)
+    check(R, good, call(R, good, ws=ws)[0], ws)
