@@ -584,6 +584,7 @@ __global__ void __launch_bounds__(kWarps * 32) verify_kernel(const Args p) {
 // close behind (16 per clock and SM; at 6.8 TB/s 11.8 bf16 entries arrive in that time). Measured against a
 // cluster per row with both rows in shared memory, whose exchanges leave the copies idle half of the time.
 
+constexpr int kRowWarps = 16;      // of a CTA
 constexpr int kTileBlocks = 4;      // 16-byte blocks per lane and tile
 constexpr int kMaxTiles = 1024;     // of a row
 
@@ -683,12 +684,12 @@ __device__ __forceinline__ Fold of_warp(const Running& r, float c) {
 }
 
 template <typename T, bool GREEDY>
-__global__ void __launch_bounds__(kWarps * 32, 3) row_kernel(const Args p) {
+__global__ void __launch_bounds__(kRowWarps * 32, 32 / kRowWarps) row_kernel(const Args p) {
   constexpr int N = Elem<T>::N;
   constexpr int kTile = kTileBlocks * 32 * N;  // elements of a tile
   __shared__ Fold tiles[kMaxTiles];            // a draw's weights by tile: sums, or (in s) max(p - q, 0)
-  __shared__ Fold rows[2][kWarps];
-  __shared__ int32_t args[kWarps];
+  __shared__ Fold rows[2][kRowWarps];
+  __shared__ int32_t args[kRowWarps];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int j = blockIdx.x / p.n_seq, b = blockIdx.x % p.n_seq;
   const float c = p.c;
@@ -753,13 +754,13 @@ __global__ void __launch_bounds__(kWarps * 32, 3) row_kernel(const Args p) {
     int t = warp;
     if (t < n) load(w[0], t);
     while (t < n) {
-      load(w[1], t + kWarps);
+      load(w[1], t + kRowWarps);
       take(w[0], t);
-      t += kWarps;
+      t += kRowWarps;
       if (t >= n) break;
-      load(w[0], t + kWarps);
+      load(w[0], t + kRowWarps);
       take(w[1], t);
-      t += kWarps;
+      t += kRowWarps;
     }
     if (draws) return;
     const Fold f = of_warp(run, c);
@@ -774,14 +775,14 @@ __global__ void __launch_bounds__(kWarps * 32, 3) row_kernel(const Args p) {
   __syncthreads();
 
   // ---- the decision, by every warp alike
-  const Fold ht = draws ? merged(tiles, nt, c, lane) : merged(rows[0], kWarps, c, lane);
+  const Fold ht = draws ? merged(tiles, nt, c, lane) : merged(rows[0], kRowWarps, c, lane);
   Fold hd{0.f, 1.f};
-  if (two) hd = merged(rows[1], kWarps, c, lane);
+  if (two) hd = merged(rows[1], kRowWarps, c, lane);
   const bool bad = is_bad(ht) || is_bad(hd);
   int token = -1;
   bool accept = false;
   if (GREEDY && !bad) {
-    const uint32_t best = lane < kWarps && rows[0][lane].m == ht.m ? static_cast<uint32_t>(args[lane]) : 0xffffffffu;
+    const uint32_t best = lane < kRowWarps && rows[0][lane].m == ht.m ? static_cast<uint32_t>(args[lane]) : 0xffffffffu;
     token = static_cast<int>(__reduce_min_sync(0xffffffffu, best)) - bt.lo;
   }
   if (tested && !bad && x >= 0) {
@@ -815,6 +816,12 @@ __global__ void __launch_bounds__(kWarps * 32, 3) row_kernel(const Args p) {
     Elem<T>::unpack(bt.load(k), w);
     exps(w, ht.m, c);
   };
+  // max(p - q, 0) from the exponentials of p and the logits of q
+  auto residual = [&](float (&w)[N], float (&y)[N]) {
+    exps(y, hd.m, c);
+#pragma unroll
+    for (int e = 0; e < N; ++e) w[e] = fmaxf(fmaf(-y[e], id_, w[e] * it), 0.f);
+  };
   auto weights_r = [&](int k, float (&w)[N]) {
     weights_p(k, w);
     if (two) {
@@ -828,9 +835,7 @@ __global__ void __launch_bounds__(kWarps * 32, 3) row_kernel(const Args p) {
           y[e] = i >= bt.lo && i < bt.hi ? Elem<T>::one(bd.base[i + shift]) : minus_inf();
         }
       }
-      exps(y, hd.m, c);
-#pragma unroll
-      for (int e = 0; e < N; ++e) w[e] = fmaxf(fmaf(-y[e], id_, w[e] * it), 0.f);
+      residual(w, y);
     } else {
       const int i = x + bt.lo - k * N;
 #pragma unroll
@@ -852,10 +857,33 @@ __global__ void __launch_bounds__(kWarps * 32, 3) row_kernel(const Args p) {
     if (lane == 0) tiles[t] = Fold{ht.m, sum};
     __syncwarp();
   };
-  if (two) {
-    for (int t = warp; t < nt; t += kWarps) weigh(t, weights_r);
-    __syncthreads();
+  if (two && shift == 0) {
+    // as weigh, with a tile of both rows in flight
+    for (int t = warp; t < nt; t += kRowWarps) {
+      const int k0 = t * kTileBlocks * 32 + lane;
+      uint4 w4[kTileBlocks], y4[kTileBlocks];
+#pragma unroll
+      for (int i = 0; i < kTileBlocks; ++i) w4[i] = bt.load(k0 + 32 * i);
+#pragma unroll
+      for (int i = 0; i < kTileBlocks; ++i) y4[i] = bd.load(k0 + 32 * i);
+      float2 r = make_float2(0.f, 0.f);
+#pragma unroll
+      for (int i = 0; i < kTileBlocks; ++i) {
+        float w[N], y[N];
+        Elem<T>::unpack(w4[i], w);
+        Elem<T>::unpack(y4[i], y);
+        exps(w, ht.m, c);
+        residual(w, y);
+#pragma unroll
+        for (int e = 0; e < N; e += 2) r = add2(r, make_float2(w[e], w[e + 1]));
+      }
+      const float sum = warp_sum(r.x + r.y);
+      if (lane == 0) tiles[t] = Fold{ht.m, sum};
+    }
+  } else if (two) {
+    for (int t = warp; t < nt; t += kRowWarps) weigh(t, weights_r);
   }
+  if (two) __syncthreads();
   if (warp != 0) return;
   if (tested && !two && x >= 0) weigh((x + bt.lo) / kTile, weights_r);  // p without the token
   bool plain = !tested;
@@ -899,15 +927,18 @@ int cluster_of(int64_t V, int es, int rows_held, int64_t clusters) {
   return C;
 }
 
-// Whether a CTA takes a row: where every SM has at least two, and a row's tiles fit in the table.
+// Whether a CTA takes a row: where every SM has a row, rows are long, and a row's tiles fit in the table.
+// Measured, a CTA per row against a cluster per row, us: 160 rows of 304 KB with drafts' rows 36.5 / 43.7,
+// 152 without 15.4 / 22.0, 305 of 128 KB 23.0 / 27.2, 512 of 64 KB 24.0 / 27.9; 1,280 of 16 KB 30.1 / 22.0,
+// 1,500 of 8 KB 30.4 / 20.7 (the ends of short rows are most of them).
 inline bool by_rows(int64_t V, int es, int64_t rows) {
-  return rows >= 2 * kSMs && V * es <= int64_t(kMaxTiles - 2) * kTileBlocks * 32 * 16;
+  return rows >= kSMs && V * es >= 48 * 1024 && V * es <= int64_t(kMaxTiles - 2) * kTileBlocks * 32 * 16;
 }
 
 template <typename T, bool GREEDY>
 rl_status run(Args& a, cudaStream_t s) {
   if (by_rows(a.V, sizeof(T), a.n_draft + a.n_seq)) {
-    row_kernel<T, GREEDY><<<static_cast<unsigned>(a.n_seq) * (a.max_draft + 1), kWarps * 32, 0, s>>>(a);
+    row_kernel<T, GREEDY><<<static_cast<unsigned>(a.n_seq) * (a.max_draft + 1), kRowWarps * 32, 0, s>>>(a);
     const cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? RL_OK : cuda_error(e, "row_kernel launch");
   }
