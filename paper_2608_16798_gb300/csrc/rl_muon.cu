@@ -120,7 +120,7 @@ struct PrepArgs {
   float* x;              // u, then X
   uint16_t* x16;
   double* partial;       // [batch][parts]: sums of squares
-  int32_t parts;
+  int32_t parts;         // CTAs of a matrix
   float* inv;            // [batch]: 1 / (|u| + eps)
   uint32_t* done;        // finished CTAs (zero at launch, set back by the last)
   int32_t* status;
@@ -129,6 +129,16 @@ struct PrepArgs {
 template <bool BF16>
 __device__ __forceinline__ float grad_at(const PrepArgs& p, int64_t i) {
   return BF16 ? bf16_to_f32(static_cast<const uint16_t*>(p.grad)[i]) : static_cast<const float*>(p.grad)[i];
+}
+template <bool BF16>
+__device__ __forceinline__ float4 grad_at4(const PrepArgs& p, int64_t i) {
+  if (!BF16) return *reinterpret_cast<const float4*>(static_cast<const float*>(p.grad) + i);
+  const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p.grad) + i);
+  return make_float4(bf16_lo(w.x), bf16_hi(w.x), bf16_lo(w.y), bf16_hi(w.y));
+}
+__device__ __forceinline__ float momentum_of(const PrepArgs& p, float g, float& buf) {
+  buf = fmaf(p.mu, buf, g);
+  return p.nesterov ? fmaf(p.mu, buf, g) : buf;
 }
 
 // The sum of the squares of 32 values as a double, without fp32 overflow or underflow: the values are
@@ -156,10 +166,12 @@ __device__ __forceinline__ double sum_squares(const float (&v)[32]) {
 constexpr int kPrepWarps = 8;
 
 // u and its sum of squares. A warp forms one 32 x 32 block of X; a CTA's warps take eight blocks that
-// lie side by side in the caller's rows.
-template <bool BF16>
-__global__ void __launch_bounds__(kPrepWarps * 32) momentum_kernel(const PrepArgs p) {
-  __shared__ float tile[kPrepWarps][32][33];
+// lie side by side in the caller's rows, and such groups in turn, so that the CTAs' last steps (a fence and
+// an atomic) are few. VEC: rows begin at multiples of four elements, and a lane takes 4 x 4 elements
+// twice, as vectors of the caller's rows and, transposed in registers if the matrix is tall, of X.
+template <bool BF16, bool VEC>
+__global__ void __launch_bounds__(kPrepWarps * 32, VEC ? 3 : 2) momentum_kernel(const PrepArgs p) {
+  __shared__ float tile[VEC ? 1 : kPrepWarps][32][33];
   __shared__ double sums[kPrepWarps];
   __shared__ bool last;
   const Shape& sh = p.sh;
@@ -170,49 +182,102 @@ __global__ void __launch_bounds__(kPrepWarps * 32) momentum_kernel(const PrepArg
   // which block: along the caller's rows first
   const int along = sh.tall ? nR : nC, across = sh.tall ? nC : nR;
   const int groups = (along + kPrepWarps - 1) / kPrepWarps;
-  const int64_t cta = blockIdx.x;
-  const int b = static_cast<int>(cta / (static_cast<int64_t>(groups) * across));
-  const int rest = static_cast<int>(cta % (static_cast<int64_t>(groups) * across));
-  const int a_blk = rest % groups * kPrepWarps + warp, x_blk = rest / groups;
+  const int b = blockIdx.x / p.parts, part = blockIdx.x % p.parts;
   double mine = 0.0;
-  if (a_blk < along) {
-    const int R = sh.tall ? a_blk : x_blk, C = sh.tall ? x_blk : a_blk;
-    // rows and columns of the caller's matrix: lane walks its row
-    const int c = a_blk * 32 + lane, r0 = x_blk * 32;
-    const int64_t g0 = b * p.stride_grad + c, m0 = static_cast<int64_t>(b) * sh.m * sh.n + c;
-    // all loads of the block before its first store: up to 64 in flight per lane
-    const int rows = c < sh.n ? sh.m - r0 : 0;
+  for (int64_t rest = part; rest < static_cast<int64_t>(groups) * across; rest += p.parts) {
+    const int a_blk = static_cast<int>(rest % groups) * kPrepWarps + warp, x_blk = static_cast<int>(rest / groups);
+    if (a_blk >= along) continue;
+    float* blk = x_block(p.x, sh, b, sh.tall ? a_blk : x_blk, sh.tall ? x_blk : a_blk);
+    const int64_t g0 = b * p.stride_grad, m0 = static_cast<int64_t>(b) * sh.m * sh.n;
     float v[32];
+    if (VEC) {
+      // micro-tile h: rows r0 + 16 h + [0, 4), columns c + [0, 4)
+      const int q = lane & 7, c = a_blk * 32 + 4 * q, r0 = x_blk * 32 + 4 * (lane >> 3);
+      const bool in = c < sh.n;
+      float4 g[8], buf[8];
 #pragma unroll
-    for (int j = 0; j < 32; ++j) v[j] = j < rows ? grad_at<BF16>(p, g0 + (r0 + j) * p.ld_grad) : 0.f;
-    if (p.momentum) {
-      float* at = p.momentum + m0 + static_cast<int64_t>(r0) * sh.n;
-      float buf[32];
-#pragma unroll
-      for (int j = 0; j < 32; ++j) buf[j] = j < rows ? at[static_cast<int64_t>(j) * sh.n] : 0.f;
-#pragma unroll
-      for (int j = 0; j < 32; ++j) {
-        buf[j] = fmaf(p.mu, buf[j], v[j]);
-        if (j < rows) at[static_cast<int64_t>(j) * sh.n] = buf[j];
-        v[j] = p.nesterov ? fmaf(p.mu, buf[j], v[j]) : buf[j];
+      for (int k = 0; k < 8; ++k) {
+        const int r = r0 + 16 * (k >> 2) + (k & 3);
+        g[k] = in && r < sh.m ? grad_at4<BF16>(p, g0 + r * p.ld_grad + c) : make_float4(0.f, 0.f, 0.f, 0.f);
       }
-    }
-    if (!sh.tall) {
+      if (p.momentum) {
+        float* at = p.momentum + m0 + c;
 #pragma unroll
-      for (int j = 0; j < 32; ++j) tile[warp][j][lane] = v[j];
-      __syncwarp();
+        for (int k = 0; k < 8; ++k) {
+          const int r = r0 + 16 * (k >> 2) + (k & 3);
+          buf[k] = in && r < sh.m ? *reinterpret_cast<const float4*>(at + static_cast<int64_t>(r) * sh.n)
+                                  : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
 #pragma unroll
-      for (int j = 0; j < 32; ++j) v[j] = tile[warp][lane][j];
+        for (int k = 0; k < 8; ++k) {
+          const int r = r0 + 16 * (k >> 2) + (k & 3);
+          g[k].x = momentum_of(p, g[k].x, buf[k].x);
+          g[k].y = momentum_of(p, g[k].y, buf[k].y);
+          g[k].z = momentum_of(p, g[k].z, buf[k].z);
+          g[k].w = momentum_of(p, g[k].w, buf[k].w);
+          if (in && r < sh.m) *reinterpret_cast<float4*>(at + static_cast<int64_t>(r) * sh.n) = buf[k];
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        v[4 * k] = g[k].x;
+        v[4 * k + 1] = g[k].y;
+        v[4 * k + 2] = g[k].z;
+        v[4 * k + 3] = g[k].w;
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float* t = v + 16 * h;  // row-major micro-tile
+        const int rl = 16 * h + 4 * (lane >> 3);
+        if (sh.tall) {  // X rows 4 q + e, columns rl ..
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            *reinterpret_cast<float4*>(blk + (rl >> 2) * 128 + (4 * q + e) * 4) =
+                make_float4(t[e], t[4 + e], t[8 + e], t[12 + e]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            *reinterpret_cast<float4*>(blk + q * 128 + (rl + e) * 4) =
+                make_float4(t[4 * e], t[4 * e + 1], t[4 * e + 2], t[4 * e + 3]);
+        }
+      }
+    } else {
+      // lane walks its row; all loads of the block before its first store
+      const int c = a_blk * 32 + lane, r0 = x_blk * 32;
+      const int rows = c < sh.n ? sh.m - r0 : 0;
+#pragma unroll
+      for (int j = 0; j < 32; ++j) v[j] = j < rows ? grad_at<BF16>(p, g0 + (r0 + j) * p.ld_grad + c) : 0.f;
+      if (p.momentum) {
+        float* at = p.momentum + m0 + static_cast<int64_t>(r0) * sh.n + c;
+        float buf[32];
+#pragma unroll
+        for (int j = 0; j < 32; ++j) buf[j] = j < rows ? at[static_cast<int64_t>(j) * sh.n] : 0.f;
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+          v[j] = momentum_of(p, v[j], buf[j]);
+          if (j < rows) at[static_cast<int64_t>(j) * sh.n] = buf[j];
+        }
+      }
+      if (!sh.tall) {
+        float(*own)[33] = tile[VEC ? 0 : warp];
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < 32; ++j) own[j][lane] = v[j];
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < 32; ++j) v[j] = own[lane][j];
+      }
+      store_block_row(blk, lane, v);
     }
-    store_block_row(x_block(p.x, sh, b, R, C), lane, v);
-    mine = warp_sum(sum_squares(v));
+    mine += sum_squares(v);
   }
+  mine = warp_sum(mine);
   if (lane == 0) sums[warp] = mine;
   __syncthreads();
   if (threadIdx.x == 0) {
     double s = 0.0;
     for (int w = 0; w < kPrepWarps; ++w) s += sums[w];
-    p.partial[static_cast<int64_t>(b) * p.parts + rest] = s;
+    p.partial[blockIdx.x] = s;
     __threadfence();
     last = atomicAdd(p.done, 1u) == gridDim.x - 1;
     if (last) __threadfence();
@@ -277,6 +342,7 @@ struct MmArgs {
   float* weights;
   uint16_t* weights_bf16;
   int64_t ld_w, stride_w;
+  int32_t vec;           // the caller's rows begin at multiples of four elements
   float decay, step;     // w <- decay w - step (2^12 X)
   int32_t* status;
 };
@@ -395,32 +461,59 @@ __device__ __forceinline__ void poly_of(const MmArgs& p, int b, int r0, int c0, 
   }
 }
 
-// The last step's X (lane: row) to the caller's outputs, lanes walking the caller's rows. tile: 32 x 33
-// floats of shared memory. Eight rows at a time: their loads are in flight together, and the code stays
-// short (unrolled over all 32, with the products' other code, it outgrew the instruction cache: the
-// twelve 1,024 x 1,024 matrices' last product took 72 us).
+// The last step's X (lane: row) to the caller's outputs, through 32 x 33 floats of shared memory so that
+// lanes walk the caller's rows: four elements each where rows begin at multiples of four (p.vec; w holds the
+// block's weights then, loaded ahead), else one, eight rows at a time. The code stays short on purpose:
+// unrolled over all 32 rows it outgrew, with the products', the instruction cache.
 __device__ __forceinline__ void final_out(const MmArgs& p, int b, int r0, int c0, int lane, const float (&v)[32],
-                                          float (*tile)[33]) {
+                                          float (*tile)[33], float4 (&w)[8]) {
   const Shape& sh = p.sh;
-  const int col = (sh.tall ? r0 : c0) + lane, row0 = sh.tall ? c0 : r0;
-  const int rows = col < sh.n ? sh.m - row0 : 0;
+  const int col0 = sh.tall ? r0 : c0, row0 = sh.tall ? c0 : r0;
   __syncwarp();
 #pragma unroll
   for (int j = 0; j < 32; ++j) tile[lane][j] = v[j];
   __syncwarp();
-  // element (row0 + j, col): tile[j][lane], of the transpose tile[lane][j]
-  const float* from = sh.tall ? &tile[lane][0] : &tile[0][lane];
-  const int step = sh.tall ? 1 : 33;
+  // element (row0 + j, col0 + k): tile[j][k], of the transpose tile[k][j]
+  const float* from = &tile[0][0];
+  const int sr = sh.tall ? 1 : 33, sc = sh.tall ? 33 : 1;
+  if (p.vec) {
+    const int k = 4 * (lane & 7), col = col0 + k;
+    if (col < sh.n) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int j = 4 * i + (lane >> 3), row = row0 + j;
+        const float* x = from + j * sr + k * sc;
+        const float4 o = make_float4(x[0], x[sc], x[2 * sc], x[3 * sc]);
+        if (row < sh.m) {
+          if (p.update)
+            *reinterpret_cast<uint2*>(p.update + (static_cast<int64_t>(b) * sh.m + row) * sh.n + col) =
+                make_uint2(pack_bf16x2(o.x * p.scale, o.y * p.scale), pack_bf16x2(o.z * p.scale, o.w * p.scale));
+          if (p.weights) {
+            const int64_t at = b * p.stride_w + row * p.ld_w + col;
+            const float4 y = make_float4(fmaf(-p.step, o.x, p.decay * w[i].x), fmaf(-p.step, o.y, p.decay * w[i].y),
+                                         fmaf(-p.step, o.z, p.decay * w[i].z), fmaf(-p.step, o.w, p.decay * w[i].w));
+            *reinterpret_cast<float4*>(p.weights + at) = y;
+            if (p.weights_bf16)
+              *reinterpret_cast<uint2*>(p.weights_bf16 + at) = make_uint2(pack_bf16x2(y.x, y.y), pack_bf16x2(y.z, y.w));
+          }
+        }
+      }
+    }
+    __syncwarp();
+    return;
+  }
+  const int col = col0 + lane, rows = col < sh.n ? sh.m - row0 : 0;
   uint16_t* up = p.update ? p.update + (static_cast<int64_t>(b) * sh.m + row0) * sh.n + col : nullptr;
   const int64_t w0 = b * p.stride_w + row0 * p.ld_w + col;
+  from += lane * sc;
 #pragma unroll 1
   for (int j0 = 0; j0 < 32; j0 += 8) {
-    float x[8], w[8];
+    float x[8], y[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = from[(j0 + j) * step];
+    for (int j = 0; j < 8; ++j) x[j] = from[(j0 + j) * sr];
     if (p.weights) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) w[j] = j0 + j < rows ? p.weights[w0 + (j0 + j) * p.ld_w] : 0.f;
+      for (int j = 0; j < 8; ++j) y[j] = j0 + j < rows ? p.weights[w0 + (j0 + j) * p.ld_w] : 0.f;
     }
     if (up) {
 #pragma unroll
@@ -430,15 +523,25 @@ __device__ __forceinline__ void final_out(const MmArgs& p, int b, int r0, int c0
     if (p.weights) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        w[j] = fmaf(-p.step, x[j], p.decay * w[j]);
+        y[j] = fmaf(-p.step, x[j], p.decay * y[j]);
         if (j0 + j < rows) {
-          p.weights[w0 + (j0 + j) * p.ld_w] = w[j];
-          if (p.weights_bf16) p.weights_bf16[w0 + (j0 + j) * p.ld_w] = f32_to_bf16(w[j]);
+          p.weights[w0 + (j0 + j) * p.ld_w] = y[j];
+          if (p.weights_bf16) p.weights_bf16[w0 + (j0 + j) * p.ld_w] = f32_to_bf16(y[j]);
         }
       }
     }
   }
   __syncwarp();
+}
+
+// The weights of a block, ahead of final_out.
+__device__ __forceinline__ void load_weights(const MmArgs& p, int b, int r0, int c0, int lane, float4 (&w)[8]) {
+  const Shape& sh = p.sh;
+  const int col = (sh.tall ? r0 : c0) + 4 * (lane & 7), row0 = (sh.tall ? c0 : r0) + (lane >> 3);
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (col < sh.n && row0 + 4 * i < sh.m)
+      w[i] = *reinterpret_cast<const float4*>(p.weights + b * p.stride_w + (row0 + 4 * i) * p.ld_w + col);
 }
 
 // One product, persistent: CTAs (CG = 1) or CTA pairs (CG = 2) take square tiles of 128 CG in turn.
@@ -657,6 +760,8 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
         }
         if (i >= blocks) continue;
         const int c0 = cb + 32 * i;
+        float4 wts[8];
+        if (MODE == FINAL && p.vec && p.weights) load_weights(p, b, r0, c0, lane, wts);
         if (in_parts) {
           store_block_row(p.parts + static_cast<int64_t>(item) * TILE * TILE +
                               (static_cast<int64_t>((rank * 4 + q) * (TILE / 32) + first + i)) * 1024, lane, v);
@@ -676,7 +781,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
         }
         prefetch(i + 1);
         if (MODE == FINAL) {
-          final_out(p, b, r0, c0, lane, v, tile);
+          final_out(p, b, r0, c0, lane, v, tile, wts);
           continue;
         }
         if (MODE == APPLY) store_block_row(x_block(p.x, p.sh, b, r0 >> 5, c0 >> 5), lane, v);
@@ -755,24 +860,34 @@ inline int64_t symmetric_items(int64_t sp, int cg) {
   return n * (n + 1) / 2 * (cg == 2 ? 1 : 4);
 }
 
+// The cheapest by what the kernels take, measured from 256 x 256 to 4,096 x 4,096, us: per wave of tiles
+// 3 + 0.3 per K block with single CTAs and 4.6 + 0.45 with pairs (both are bound by what L2 delivers, a
+// pair's block does four times the work), and 5.5 for a sum of parts. E.g. X X^T of 2,048 x 2,048: singles
+// 16.5, pairs in two parts 13.7 + 5.8; B X of 1,000 x 2,777: singles 18.6 (176 tiles, two waves), pairs 16.0.
 Plan plan_of(int64_t batch, int64_t sp, int64_t lp) {
-  Plan p;
-  auto items = [&](int cg) { return batch * symmetric_items(sp, cg); };
-  p.cg_poly = items(2) >= kSMs / 2 ? 2 : 1;
-  p.cg_apply = batch * (round_up(sp, 256) / 256) * (round_up(lp, 256) / 256) >= kSMs / 2 ? 2 : 1;
-  // X X^T: a K block takes a unit of either kind about as long (both are bound by what L2 delivers), so
-  // pairs wherever their items, cut into parts of at least eight K blocks, occupy half of them
-  auto parts = [&](int cg) {
-    return std::max<int64_t>(1, std::min<int64_t>(kSMs / cg / std::max<int64_t>(items(cg), 1), lp / BK / 8));
+  Plan p = {};
+  auto cost = [](int cg, int64_t items, double nkb) {
+    const int64_t units = kSMs / cg, waves = (items + units - 1) / units;
+    return static_cast<double>(waves) * (cg == 2 ? 4.6 + 0.45 * nkb : 3.0 + 0.3 * nkb);
   };
-  p.cg_gram = items(2) * parts(2) >= kSMs / 4 ? 2 : 1;
-  p.splits = static_cast<int>(parts(p.cg_gram));
+  double poly = 1e300, apply = 1e300, gram = 1e300;
+  for (int cg = 1; cg <= 2; ++cg) {
+    const int64_t T = 128 * cg, sym = batch * symmetric_items(sp, cg);
+    const int64_t all = batch * ((sp + T - 1) / T) * ((lp + T - 1) / T);
+    if (cost(cg, sym, sp / BK) < poly) poly = cost(cg, sym, sp / BK), p.cg_poly = cg;
+    if (cost(cg, all, sp / BK) < apply) apply = cost(cg, all, sp / BK), p.cg_apply = cg;
+    // parts of at least four K blocks that all run at once
+    for (int64_t k = 1; k == 1 || (k * sym <= kSMs / cg && lp / BK >= 4 * k); ++k) {
+      const double t = cost(cg, k * sym, static_cast<double>(lp / BK) / k) + (k > 1 ? 5.5 : 0.0);
+      if (t < gram) gram = t, p.cg_gram = cg, p.splits = static_cast<int>(k);
+    }
+  }
   return p;
 }
 
 struct Layout {
   size_t x, x16a, x16b, a16, a_blk, b16, d, e, inv, partial, parts, bytes;
-  int32_t n_parts;  // partial sums of squares per matrix
+  int32_t n_parts;  // partial sums of squares per matrix: CTAs of its momentum pass
 };
 
 Shape shape_of(int32_t batch, int64_t m, int64_t n) {
@@ -798,7 +913,8 @@ Layout layout_of(const Shape& s) {
   };
   const size_t B = s.batch, sp = s.sp, lp = s.lp;
   const int64_t along = (s.tall ? s.sp : s.lp) / 32, across = (s.tall ? s.lp : s.sp) / 32;
-  w.n_parts = static_cast<int32_t>((along + kPrepWarps - 1) / kPrepWarps * across);
+  w.n_parts = static_cast<int32_t>(std::min<int64_t>((along + kPrepWarps - 1) / kPrepWarps * across,
+                                                     std::max<int64_t>(1, 6 * kSMs / s.batch)));
   w.x = take(B * sp * lp * 4);
   w.x16a = take(B * sp * lp * 2);
   w.x16b = take(B * sp * lp * 2);
@@ -956,7 +1072,12 @@ rl_status rl_muon_update(int32_t batch, int64_t m, int64_t n, const void* grad, 
   pa.inv = reinterpret_cast<float*>(base + w.inv);
   pa.done = reinterpret_cast<uint32_t*>(base + kWsMuonDoneOffset);
   pa.status = status;
-  auto momentum_pass = grad_dtype == RL_BF16 ? momentum_kernel<true> : momentum_kernel<false>;
+  // rows of the gradient and of the momentum that begin at multiples of four elements
+  const size_t ge = grad_dtype == RL_F32 ? 16 : 8;
+  const bool vec = n % 4 == 0 && ld_grad % 4 == 0 && stride_grad % 4 == 0 && reinterpret_cast<uintptr_t>(grad) % ge == 0 &&
+                   aligned16(pa.momentum);
+  auto momentum_pass = grad_dtype == RL_BF16 ? (vec ? momentum_kernel<true, true> : momentum_kernel<true, false>)
+                                             : (vec ? momentum_kernel<false, true> : momentum_kernel<false, false>);
   st = launch("momentum_kernel launch", momentum_pass, static_cast<int64_t>(batch) * w.n_parts, kPrepWarps * 32, 0, 1, s,
               pa);
   if (st != RL_OK) return st;
@@ -1005,6 +1126,9 @@ rl_status rl_muon_update(int32_t batch, int64_t m, int64_t n, const void* grad, 
   a.weights_bf16 = weights_bf16;
   a.ld_w = ld_w;
   a.stride_w = stride_w;
+  a.vec = n % 4 == 0 && reinterpret_cast<uintptr_t>(update) % 8 == 0 &&
+          (!weights || (ld_w % 4 == 0 && stride_w % 4 == 0 && aligned16(weights) &&
+                        reinterpret_cast<uintptr_t>(weights_bf16) % 8 == 0));
   a.decay = static_cast<float>(1.0 - static_cast<double>(P.lr) * P.weight_decay);
   a.step = static_cast<float>(static_cast<double>(P.lr) * P.update_scale / kXScale);
   a.status = status;

@@ -200,3 +200,39 @@ def test_binding_refusals(R):
         R.rl_muon_update(g, P, ws[:512])
     with pytest.raises(R.RLError):
         R.new_muon_workspace(1, 40000, 40000)
+
+
+@pytest.mark.parametrize("batch,m,n,pad", [(3, 96, 132, 0), (2, 132, 96, 4), (2, 260, 100, 8), (1, 301, 404, 12),
+                                           (2, 404, 301, 3), (1, 66, 130, 2)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_rows_at_and_off_multiples_of_four(R, batch, m, n, pad, dtype):
+    """Vectors of four elements and single ones: gradient, momentum, weights and update by both ways."""
+    grad = matrices("low_rank", batch, m, n, 12).to(dtype)
+    mom, w = matrices("low_rank", batch, m, n, 13), matrices("normal", batch, m, n, 14)
+    P = R.make_muon_params(lr=0.1, momentum=0.9, update_scale=0.3, weight_decay=0.5)
+    ws = R.new_muon_workspace(batch, m, n)
+    buf, X, upd, w_ref = O.muon_update(grad.double().numpy(), mom.numpy(), w.numpy(), lr=0.1, mu=0.9, update_scale=0.3,
+                                       weight_decay=0.5)
+    results = []
+    for shift in (0, 1):  # elements by which everything starts off its alignment
+        def place(x, width, dt):
+            t = torch.full((batch * m * width + shift,), 5.0, dtype=dt, device="cuda")[shift:].view(batch, m, width)
+            t[:, :, :n] = x.cuda()
+            return t
+        g, d_w = place(grad, n + pad, dtype)[:, :, :n], place(w, n + pad, torch.float32)
+        d_m, d_u = place(mom, n, torch.float32), place(torch.zeros(batch, m, n), n, torch.bfloat16)
+        d_b = place(torch.zeros(batch, m, n), n + pad, torch.bfloat16)
+        R.rl_muon_update(g, P, ws, momentum=d_m, weights=d_w[:, :, :n], weights_bf16=d_b[:, :, :n], update=d_u)
+        assert R.rl_query_status(ws)[1] == 0
+        check_x(d_u, upd, "update", True)
+        tol = 2.0 ** -23 * (np.abs(mom.double().numpy()) + np.abs(grad.double().numpy()))
+        assert (np.abs(d_m.cpu().double().numpy() - buf) <= tol + 1e-30).all()
+        for b in range(batch):
+            err = np.linalg.norm(d_w[b, :, :n].cpu().double().numpy() - w_ref[b])
+            assert err <= 0.1 * 0.3 * NS_REL * np.linalg.norm(X[b]) + 4 * 2.0 ** -24 * np.linalg.norm(w_ref[b])
+        assert torch.equal(d_b[:, :, :n], d_w[:, :, :n].bfloat16())
+        assert (d_w[:, :, n:] == 5).all() and (d_b[:, :, n:] == 5).all()
+        results.append([x.clone() for x in (d_m, d_w, d_b, d_u)])
+    # both ways round alike, but for the order in which the norm's squares are added
+    for a, b in zip(*results):
+        assert (a.float() - b.float()).norm() <= 1e-3 * a.float().norm()
