@@ -586,6 +586,11 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
   else __syncthreads();
   tc::fence_after_sync();
   const uint32_t tmem = tbase;
+  if (warp == 0 && lane == 0) {
+    const CUtensorMap* used[4] = {&tmA, &tmAt, &tmB, &tmOut};
+    for (const CUtensorMap* m : used)
+      asm volatile("prefetch.tensormap [%0];" :: "l"(reinterpret_cast<uint64_t>(m)) : "memory");
+  }
   pdl_launch();
   pdl_wait();
 
@@ -653,6 +658,8 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
     }
   } else if (warp == 1) {
     if (lane == 0 && rank == 0) {
+      const uint64_t k_major = tc::desc_kmajor_sw128(0), mn_major = tc::desc_mnmajor_sw128(0, HALF_BYTES, 1024);
+      const uint32_t stage0 = smem_addr(sm) >> 4;
       uint32_t g = 0;
       bool ok = true;
       uint32_t t = 0;
@@ -681,19 +688,18 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
             break;
           }
           tc::fence_after_sync();
-          const uint32_t a = smem_addr(sm + s * STAGE_BYTES), bb = a + A_BYTES;
           const int k0 = (kb0 + kb) * BK;
           const bool a_mn = MODE != GRAM && below(ti * TILE, k0);
           const bool b_mn = APPLIES || (MODE == POLY && below(tj * TILE, k0));
           const uint32_t idesc = idesc_f16(TILE, TILE, a_mn, b_mn);
+          // descriptors differ in their start address only, in units of 16 bytes
+          const uint64_t at = stage0 + s * (STAGE_BYTES >> 4);
+          const uint64_t ad = (a_mn ? mn_major : k_major) + at, bd = (b_mn ? mn_major : k_major) + at + (A_BYTES >> 4);
+          const uint32_t da = a_mn ? 128 : 2, db = b_mn ? 128 : 2;
 #pragma unroll
           for (int k = 0; k < BK / 16; ++k) {
-            const uint64_t ad = a_mn ? tc::desc_mnmajor_sw128(a + k * 2048, HALF_BYTES, 1024)
-                                     : tc::desc_kmajor_sw128(a + k * 32);
-            const uint64_t bd = b_mn ? tc::desc_mnmajor_sw128(bb + k * 2048, HALF_BYTES, 1024)
-                                     : tc::desc_kmajor_sw128(bb + k * 32);
-            if (CG == 2) tc::mma_bf16_pair(acc, ad, bd, idesc, (kb | k) != 0 ? 1u : 0u);
-            else tc::mma_bf16(acc, ad, bd, idesc, (kb | k) != 0 ? 1u : 0u);
+            if (CG == 2) tc::mma_bf16_pair(acc, ad + k * da, bd + k * db, idesc, (kb | k) != 0 ? 1u : 0u);
+            else tc::mma_bf16(acc, ad + k * da, bd + k * db, idesc, (kb | k) != 0 ? 1u : 0u);
           }
           if (CG == 2) tc::mma_commit_pair(&empty[s], 0x3);
           else tc::mma_commit(&empty[s]);
