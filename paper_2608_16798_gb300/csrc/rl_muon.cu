@@ -852,6 +852,238 @@ __global__ void __launch_bounds__(256) gram_sum_kernel(const MmArgs p) {
   for (int k = 0; k < 4; ++k) *reinterpret_cast<uint4*>(to + 8 * k) = w[k];
 }
 
+// ---------------------------------------------------------------- matrices of at most 256 x 256
+//
+// All steps of one matrix in one CTA pair, the operands in shared memory and X (fp32) in TMEM: fifteen
+// launches that wait for each other (6 us each) become fifteen rounds of products, an epilogue in registers
+// and a cluster barrier. CTA r owns rows [128 r, 128 r + 128). It holds, in the layout of the 128-byte
+// swizzle (64 columns a block),
+//   xk  its rows of X: left and right operand of X X^T (K-major), half of the right one's rows each
+//   xn  all rows of X, its half of the columns: right operand of Bo X (MN-major)
+//   sy  its rows of Ao, then, in their place, of Bo: operands of Ao Ao (K-major) and Bo X
+// so that the pair's MMAs find their halves without an exchange; only the new X goes to both CTAs' xn.
+
+constexpr int kSmallSide = 256;
+constexpr int kSmallThreads = 256;
+constexpr uint32_t kBlk = 128 * 128;  // bytes of 128 rows of a 64-column block
+
+struct SmallSmem {
+  uint32_t xk, xn, sy, bytes;
+};
+__host__ __device__ constexpr SmallSmem small_smem(int lp) {
+  return SmallSmem{0, static_cast<uint32_t>(lp) / 64 * kBlk, static_cast<uint32_t>(lp) / 64 * kBlk * 2,
+                   static_cast<uint32_t>(lp) / 64 * kBlk * 2 + 4 * kBlk};
+}
+
+// 32 fp32 columns of this warp's 32 TMEM lanes.
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const float (&v)[32]) {
+  uint32_t r[32];
+#pragma unroll
+  for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(v[j]);
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+      "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};"
+      :: "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+         "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
+         "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
+         "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(taddr)
+      : "memory");
+  asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+
+__device__ __forceinline__ void st_cluster_u4(uint32_t addr, uint4 v) {
+  asm volatile("st.shared::cluster.v4.u32 [%0], {%1, %2, %3, %4};"
+               :: "r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+
+__global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(const __grid_constant__ CUtensorMap tmK,
+                                                                 const __grid_constant__ CUtensorMap tmN, const MmArgs p,
+                                                                 int steps) {
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ __align__(8) uint64_t loaded, accf;
+  __shared__ uint32_t tbase;
+  __shared__ float d[kSmallSide], e[128];
+  uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_ctarank();
+  const int b = blockIdx.x / 2, lp = p.sh.lp, q = warp & 3, half = warp >> 2;
+  const SmallSmem at = small_smem(lp);
+  const int row = 32 * q + lane, grow = static_cast<int>(rank) * 128 + row;  // this lane's row: here, of the matrix
+  if (threadIdx.x == 0) {
+    mbar_init(&loaded, 1);
+    mbar_init(&accf, 1);
+    fence_mbar_init();
+  }
+  if (warp == 0) tc::tmem_alloc_pair(&tbase, 512);
+  tc::fence_before_sync();
+  cluster_sync_all();
+  tc::fence_after_sync();
+  const uint32_t acc = tbase + (static_cast<uint32_t>(32 * q) << 16), xt = acc + 256;
+  pdl_launch();
+  pdl_wait();
+  if (threadIdx.x == 0) {
+    asm volatile("fence.proxy.async.global;" ::: "memory");
+    mbar_arrive_expect_tx(&loaded, at.sy);  // xk and xn
+    const int y0 = b * kSmallSide;
+    for (int c = 0; c < lp / 64; ++c)
+      tc::tma_load_2d(sm + at.xk + c * kBlk, &tmK, c * 64, y0 + static_cast<int>(rank) * 128, &loaded);
+    for (int c = 0; c < lp / 128; ++c)
+      for (int r = 0; r < 4; ++r)
+        tc::tma_load_2d(sm + at.xn + c * 2 * kBlk + r * (kBlk / 2), &tmN, static_cast<int>(rank) * (lp / 2) + c * 64,
+                        y0 + r * 64, &loaded);
+  }
+  bool dead = false;  // a wait ran out: the rest runs through without waiting
+  auto wait = [&](uint64_t* bar, uint32_t parity) {
+    if (!mbar_wait_bounded(bar, parity, dead ? 1000 : kWaitLimitNs)) {
+      if (!dead && lane == 0) flag_status(p.status, RL_DEV_TIMEOUT);
+      dead = true;
+    }
+  };
+  // X, normalised and scaled, into TMEM
+  const float inv = p.inv[b];
+  const int nblk = lp / 64, first = half * nblk;  // this warp's 32-column blocks of X
+  for (int i = 0; i < nblk; ++i) {
+    float v[32];
+    load_block_row(x_block(p.x, p.sh, b, grow >> 5, first + i), lane, v);
+#pragma unroll
+    for (int j = 0; j < 32; ++j) v[j] = v[j] * inv * kXScale;
+    tmem_st32(xt + (first + i) * 32, v);
+  }
+  wait(&loaded, 0);
+  __syncthreads();
+
+  const uint64_t k_major = tc::desc_kmajor_sw128(0), mn_major = tc::desc_mnmajor_sw128(0, 2 * kBlk, 1024);
+  const uint32_t base = smem_addr(sm) >> 4;
+  // The products whose operands both CTAs have written by now; everyone returns when they are done.
+  uint32_t rounds = 0;
+  auto multiply = [&](uint32_t left, uint32_t right, int n, int k_blocks, bool right_mn) {
+    asm volatile("fence.proxy.async;" ::: "memory");  // what was written for the MMAs, here and in the peer
+    __syncwarp();
+    tc::fence_before_sync();
+    cluster_sync_all();
+    tc::fence_after_sync();
+    if (rank == 0 && threadIdx.x == 0) {
+      const uint32_t idesc = idesc_f16(2 * 128, n, false, right_mn);
+      for (int c = 0; c < k_blocks; ++c) {
+        // 64 along the contraction: a block of a K-major operand, 64 rows of an MN-major one
+        const uint64_t l = k_major + base + ((left + c * kBlk) >> 4);
+        const uint64_t r = right_mn ? mn_major + base + ((right + c * (kBlk / 2)) >> 4)
+                                    : k_major + base + ((right + c * kBlk) >> 4);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          tc::mma_bf16_pair(tbase, l + k * 2, r + k * (right_mn ? 128 : 2), idesc, (c | k) != 0 ? 1u : 0u);
+      }
+      tc::mma_commit_pair(&accf, 0x3);
+    }
+    wait(&accf, rounds++ & 1);
+    tc::fence_after_sync();
+  };
+  // this lane's row of the 64-column block of 128 rows at `blk`, 16-byte chunk k
+  auto chunk = [&](uint32_t blk, int k) -> uint32_t { return blk + row * 128 + ((k ^ (row & 7)) << 4); };
+
+#pragma unroll 1
+  for (int step = 0; step < steps; ++step) {
+    // ---- A = X X^T: its diagonal to both CTAs' d, the rest to sy
+    multiply(at.xk, at.xk, kSmallSide, lp / 64, false);
+#pragma unroll 1
+    for (int i = 0; i < 4; ++i) {
+      const int cb = 4 * half + i, c0 = 32 * cb;  // the block and its first column
+      float v[32];
+      tc::tmem_ld32(acc + c0, v);
+#pragma unroll
+      for (int j = 0; j < 32; ++j) v[j] *= kAScale / (kXScale * kXScale);
+      if (c0 == (grow & ~31)) {
+        float own = 0.f;
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+          if (j == lane) {
+            own = v[j] * (1.f / kAScale);
+            v[j] = 0.f;
+          }
+        d[grow] = own;
+        asm volatile("st.shared::cluster.f32 [%0], %1;" :: "r"(map_to_rank(smem_addr(&d[grow]), rank ^ 1)), "f"(own) : "memory");
+      }
+      uint4 w[4];
+      pack_row(v, w);
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        *reinterpret_cast<uint4*>(sm + chunk(at.sy + (cb >> 1) * kBlk, 4 * (cb & 1) + k)) = w[k];
+    }
+    // ---- B = b A + c A^2: a + its diagonal to e, the rest in Ao's place
+    multiply(at.sy, at.sy, kSmallSide, kSmallSide / 64, false);
+    const float di = d[grow];
+    const float k2 = p.cc * (kBScale / kAScale), k3 = p.cc * (kBScale / (kAScale * kAScale));
+    const float k1 = fmaf(k2, di, p.cb * (kBScale / kAScale));
+#pragma unroll 1
+    for (int i = 0; i < 4; ++i) {
+      const int cb = 4 * half + i, c0 = 32 * cb;
+      float v[32];
+      tc::tmem_ld32(acc + c0, v);
+      const bool on_diagonal = c0 == (grow & ~31);
+      if (on_diagonal) {
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+          if (j == lane) e[row] = p.ca + fmaf(p.cb, di, p.cc * fmaf(di, di, v[j] * (1.f / (kAScale * kAScale))));
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        uint4* w = reinterpret_cast<uint4*>(sm + chunk(at.sy + (cb >> 1) * kBlk, 4 * (cb & 1) + k));
+        const uint4 h = *w;
+        const uint32_t hh[4] = {h.x, h.y, h.z, h.w};
+        uint32_t o[4];
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+          const int j = 8 * k + 2 * m;
+          const float2 a = unpack_half2(hh[m]);
+          float x = fmaf(a.x, fmaf(k2, d[c0 + j], k1), k3 * v[j]);
+          float y = fmaf(a.y, fmaf(k2, d[c0 + j + 1], k1), k3 * v[j + 1]);
+          if (on_diagonal && j == lane) x = 0.f;
+          if (on_diagonal && j + 1 == lane) y = 0.f;
+          o[m] = pack_half2(x, y);
+        }
+        *w = make_uint4(o[0], o[1], o[2], o[3]);
+      }
+    }
+    // ---- X <- e X + Bo X, kept in TMEM and as operands of the next step
+    multiply(at.sy, at.xn, lp, kSmallSide / 64, true);
+    const float f = e[row];
+    const bool last = step == steps - 1;
+#pragma unroll 1
+    for (int i = 0; i < nblk; ++i) {
+      const int cb = first + i, c0 = 32 * cb;
+      float v[32], x[32];
+      tc::tmem_ld32(acc + c0, v);
+      tc::tmem_ld32(xt + c0, x);
+#pragma unroll
+      for (int j = 0; j < 32; ++j) v[j] = fmaf(f, x[j], v[j] * (1.f / kBScale));
+      if (last) {
+        float4 wts[8];
+        const int r0 = grow & ~31;
+        if (p.vec && p.weights) load_weights(p, b, r0, c0, lane, wts);
+        final_out(p, b, r0, c0, lane, v, reinterpret_cast<float(*)[33]>(sm + at.sy + warp * 4352), wts);
+        continue;
+      }
+      tmem_st32(xt + c0, v);
+      uint4 w[4];
+      pack_row(v, w);
+      // columns [c0, c0 + 32) in xk, and in xn of the CTA that has them
+      const int owner = c0 / (lp / 2), cn = c0 - owner * (lp / 2);
+      const uint32_t to = map_to_rank(smem_addr(sm), owner) + at.xn + (cn / 64) * 2 * kBlk + rank * kBlk;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        *reinterpret_cast<uint4*>(sm + chunk(at.xk + (cb >> 1) * kBlk, 4 * (cb & 1) + k)) = w[k];
+        st_cluster_u4(chunk(to, 4 * (cb & 1) + k), w[k]);
+      }
+    }
+  }
+  tc::fence_before_sync();
+  cluster_sync_all();
+  if (warp == 0) {
+    tc::fence_after_sync();
+    tc::tmem_dealloc_pair(tbase, 512);
+  }
+}
+
 // ---------------------------------------------------------------- host
 
 // How the products are cut: the tile (128 or, by CTA pairs, 256) of each, and the parts of the first
@@ -859,6 +1091,9 @@ __global__ void __launch_bounds__(256) gram_sum_kernel(const MmArgs p) {
 struct Plan {
   int cg_gram, cg_poly, cg_apply, splits;
 };
+
+// Matrices of at most 256 x 256 go to small_kernel, padded to 256 x 128 or 256 x 256.
+inline bool is_small(const Shape& s) { return s.l <= kSmallSide; }
 
 // Items of a symmetric product of one matrix (symmetric_tile).
 inline int64_t symmetric_items(int64_t sp, int cg) {
@@ -906,6 +1141,10 @@ Shape shape_of(int32_t batch, int64_t m, int64_t n) {
   s.sp = static_cast<int32_t>(round_up(s.s, 128));
   s.lp = static_cast<int32_t>(round_up(s.l, 64));
   s.tall = m > n;
+  if (is_small(s)) {
+    s.sp = kSmallSide;
+    s.lp = static_cast<int32_t>(round_up(s.l, 128));
+  }
   return s;
 }
 
@@ -991,6 +1230,26 @@ rl_status product(const CUtensorMap& a, const CUtensorMap& at, const CUtensorMap
   const int64_t units = std::min<int64_t>(items, kSMs / CG);
   return launch("product_kernel launch", product_kernel<MODE, CG>, units * CG, kThreads, kSmem, CG, s, a, at, b,
                 out, p);
+}
+
+rl_status small(const CUtensorMap& k, const CUtensorMap& n, const MmArgs& p, int steps, cudaStream_t s) {
+  const size_t smem = small_smem(p.sh.lp).bytes + 1024;
+  static std::mutex mu;
+  static std::map<int, bool> done;
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return cuda_error(e, "cudaGetDevice");
+  {
+    std::lock_guard<std::mutex> lock(mu);
+    if (!done[dev]) {
+      e = cudaFuncSetAttribute(small_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                               static_cast<int>(small_smem(kSmallSide).bytes + 1024));
+      if (e != cudaSuccess) return cuda_error(e, "cudaFuncSetAttribute(small_kernel)");
+      done[dev] = true;
+    }
+  }
+  return launch("small_kernel launch", small_kernel, 2 * static_cast<int64_t>(p.sh.batch), kSmallThreads, smem, 2, s, k, n,
+                p, steps);
 }
 
 }  // namespace muon
@@ -1092,29 +1351,6 @@ rl_status rl_muon_update(int32_t batch, int64_t m, int64_t n, const void* grad, 
               s, pa);
   if (st != RL_OK) return st;
 
-  // boxes of 64 columns: 128 rows of a K-major operand, 64 of an MN-major one, 32 of an output
-  uint16_t* x16[2] = {reinterpret_cast<uint16_t*>(base + w.x16a), reinterpret_cast<uint16_t*>(base + w.x16b)};
-  CUtensorMap xk[2], xn[2], ak, at, bk, bt;
-  const int64_t rows = static_cast<int64_t>(batch) * sh.sp;
-  const auto F16 = CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
-  auto map = [&](CUtensorMap* m, const void* at, int64_t cols, int box_rows) {
-    if (st == RL_OK) st = tmap_2d(m, F16, at, cols, rows, cols * 2, 64, box_rows, CU_TENSOR_MAP_SWIZZLE_128B);
-  };
-  CUtensorMap xout[2], aout, bout;
-  for (int k = 0; k < 2; ++k) {
-    map(&xk[k], x16[k], sh.lp, 128);
-    map(&xn[k], x16[k], sh.lp, 64);
-    map(&xout[k], x16[k], sh.lp, 32);
-  }
-  map(&ak, base + w.a16, sh.sp, 128);
-  map(&at, base + w.a16, sh.sp, 64);
-  map(&aout, base + w.a16, sh.sp, 32);
-  map(&bk, base + w.b16, sh.sp, 128);
-  map(&bt, base + w.b16, sh.sp, 64);
-  map(&bout, base + w.b16, sh.sp, 32);
-  if (st != RL_OK) return st;
-
-  const Plan plan = plan_of(batch, sh.sp, sh.lp);
   MmArgs a = {};
   a.sh = sh;
   a.ca = P.ns_coef[0];
@@ -1138,6 +1374,39 @@ rl_status rl_muon_update(int32_t batch, int64_t m, int64_t n, const void* grad, 
   a.decay = static_cast<float>(1.0 - static_cast<double>(P.lr) * P.weight_decay);
   a.step = static_cast<float>(static_cast<double>(P.lr) * P.update_scale / kXScale);
   a.status = status;
+  a.inv = pa.inv;
+  if (is_small(sh)) {
+    CUtensorMap k, nmap;
+    const int64_t rows = static_cast<int64_t>(batch) * sh.sp, stride = static_cast<int64_t>(sh.lp) * 2;
+    const auto F16 = CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+    st = tmap_2d(&k, F16, pa.x16, sh.lp, rows, stride, 64, 128, CU_TENSOR_MAP_SWIZZLE_128B);
+    if (st == RL_OK) st = tmap_2d(&nmap, F16, pa.x16, sh.lp, rows, stride, 64, 64, CU_TENSOR_MAP_SWIZZLE_128B);
+    return st == RL_OK ? small(k, nmap, a, P.ns_steps, s) : st;
+  }
+
+  // boxes of 64 columns: 128 rows of a K-major operand, 64 of an MN-major one, 32 of an output
+  uint16_t* x16[2] = {reinterpret_cast<uint16_t*>(base + w.x16a), reinterpret_cast<uint16_t*>(base + w.x16b)};
+  CUtensorMap xk[2], xn[2], ak, at, bk, bt;
+  const int64_t rows = static_cast<int64_t>(batch) * sh.sp;
+  const auto F16 = CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+  auto map = [&](CUtensorMap* m, const void* at, int64_t cols, int box_rows) {
+    if (st == RL_OK) st = tmap_2d(m, F16, at, cols, rows, cols * 2, 64, box_rows, CU_TENSOR_MAP_SWIZZLE_128B);
+  };
+  CUtensorMap xout[2], aout, bout;
+  for (int k = 0; k < 2; ++k) {
+    map(&xk[k], x16[k], sh.lp, 128);
+    map(&xn[k], x16[k], sh.lp, 64);
+    map(&xout[k], x16[k], sh.lp, 32);
+  }
+  map(&ak, base + w.a16, sh.sp, 128);
+  map(&at, base + w.a16, sh.sp, 64);
+  map(&aout, base + w.a16, sh.sp, 32);
+  map(&bk, base + w.b16, sh.sp, 128);
+  map(&bt, base + w.b16, sh.sp, 64);
+  map(&bout, base + w.b16, sh.sp, 32);
+  if (st != RL_OK) return st;
+
+  const Plan plan = plan_of(batch, sh.sp, sh.lp);
   for (int k = 0; k < P.ns_steps; ++k) {
     const int T = 128 * plan.cg_gram;
     a.nt_m = a.nt_n = static_cast<int32_t>(round_up(sh.sp, T) / T);
