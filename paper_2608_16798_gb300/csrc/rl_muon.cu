@@ -104,6 +104,25 @@ __device__ __forceinline__ void store_half_row(uint16_t* to, const float (&v)[32
                    pack_half2(v[8 * j + 4], v[8 * j + 5]), pack_half2(v[8 * j + 6], v[8 * j + 7]));
 }
 
+// Shared memory by its 32-bit address (a pointer made of an aligned integer is a generic one to the compiler,
+// and generic loads are several times slower).
+__device__ __forceinline__ uint4 lds_u4(uint32_t a) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ void sts_u4(uint32_t a, uint4 v) {
+  asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" :: "r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ float lds_f32(uint32_t a) {
+  float v;
+  asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ void sts_f32(uint32_t a, float v) {
+  asm volatile("st.shared.f32 [%0], %1;" :: "r"(a), "f"(v) : "memory");
+}
+
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void pdl_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
@@ -388,10 +407,9 @@ __device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, int c0, int
 
 // 32 values of a lane's row as fp16 into half `h` of a slab: 32 rows of 128 bytes with the 128-byte
 // swizzle (16-byte chunk k of row r at chunk k ^ r % 8).
-__device__ __forceinline__ void fill_slab(uint8_t* slab, int h, int lane, const uint4 (&w)[4]) {
+__device__ __forceinline__ void fill_slab(uint32_t slab, int h, int lane, const uint4 (&w)[4]) {
 #pragma unroll
-  for (int k = 0; k < 4; ++k)
-    *reinterpret_cast<uint4*>(slab + lane * 128 + (((4 * h + k) ^ (lane & 7)) << 4)) = w[k];
+  for (int k = 0; k < 4; ++k) sts_u4(slab + lane * 128 + (((4 * h + k) ^ (lane & 7)) << 4), w[k]);
 }
 __device__ __forceinline__ void pack_row(const float (&v)[32], uint4 (&w)[4]) {
 #pragma unroll
@@ -405,20 +423,26 @@ __device__ __forceinline__ uint16_t* a_block(const MmArgs& p, int b, int r0, int
   return p.a_blk + ((static_cast<int64_t>(b) * nb + (r0 >> 5)) * nb + (c0 >> 5)) * 1024;
 }
 
+// The value on the diagonal of a 32 x 32 block on the diagonal (lane: row), which becomes `to`. By selects:
+// as branches the 32 cases took 3,000 cycles.
+__device__ __forceinline__ float take_diagonal(float (&v)[32], int lane, float to) {
+  float own = 0.f;
+#pragma unroll
+  for (int j = 0; j < 32; ++j) {
+    own = j == lane ? v[j] : own;
+    v[j] = j == lane ? to : v[j];
+  }
+  return own;
+}
+
 // What becomes of a 32 x 32 block (lane: row) of X X^T, scaled by 2^24: A off its diagonal, scaled, in w
 // and in its block.
 __device__ __forceinline__ void gram_of(const MmArgs& p, int b, int r0, int c0, int lane, float (&v)[32],
                                         uint4 (&w)[4]) {
 #pragma unroll
   for (int j = 0; j < 32; ++j) v[j] *= kAScale / (kXScale * kXScale);
-  if (r0 == c0) {
-#pragma unroll
-    for (int j = 0; j < 32; ++j)
-      if (j == lane) {
-        p.d[static_cast<int64_t>(b) * p.sh.sp + r0 + lane] = v[j] * (1.f / kAScale);
-        v[j] = 0.f;
-      }
-  }
+  if (r0 == c0)
+    p.d[static_cast<int64_t>(b) * p.sh.sp + r0 + lane] = take_diagonal(v, lane, 0.f) * (1.f / kAScale);
   pack_row(v, w);
   uint16_t* blk = a_block(p, b, r0, c0) + lane * 8;
 #pragma unroll
@@ -430,12 +454,10 @@ __device__ __forceinline__ void gram_of(const MmArgs& p, int b, int r0, int c0, 
 __device__ __forceinline__ void poly_of(const MmArgs& p, int b, int r0, int c0, int lane, float (&v)[32],
                                         const uint4 (&a)[4], float di) {
   const int64_t row = static_cast<int64_t>(b) * p.sh.sp;
-  if (r0 == c0) {
-#pragma unroll
-    for (int j = 0; j < 32; ++j)
-      if (j == lane)
-        p.e[row + r0 + lane] = p.ca + fmaf(p.cb, di, p.cc * fmaf(di, di, v[j] * (1.f / (kAScale * kAScale))));
-  }
+  // (Ao Ao)_ii goes into e; what it leaves in its place comes to k3 0 + 0 (..) = 0, as Ao_ii is 0
+  if (r0 == c0)
+    p.e[row + r0 + lane] =
+        p.ca + fmaf(p.cb, di, p.cc * fmaf(di, di, take_diagonal(v, lane, 0.f) * (1.f / (kAScale * kAScale))));
   // B_ij = h_ij (k1 + k2 d_j) + k3 v_ij with h the fp16 value of A_ij and k1 for this row
   const float k2 = p.cc * (kBScale / kAScale), k3 = p.cc * (kBScale / (kAScale * kAScale));
   const float k1 = fmaf(k2, di, p.cb * (kBScale / kAScale));
@@ -454,11 +476,6 @@ __device__ __forceinline__ void poly_of(const MmArgs& p, int b, int r0, int c0, 
       o[3] = fmaf(a1.y, fmaf(k2, dj.w, k1), k3 * o[3]);
     }
   }
-  if (r0 == c0) {
-#pragma unroll
-    for (int j = 0; j < 32; ++j)
-      if (j == lane) v[j] = 0.f;
-  }
 }
 
 // The last step's X (lane: row) to the caller's outputs, through 32 x 33 floats of shared memory so that
@@ -466,24 +483,23 @@ __device__ __forceinline__ void poly_of(const MmArgs& p, int b, int r0, int c0, 
 // block's weights then, loaded ahead), else one, eight rows at a time. The code stays short on purpose:
 // unrolled over all 32 rows it outgrew, with the products', the instruction cache.
 __device__ __forceinline__ void final_out(const MmArgs& p, int b, int r0, int c0, int lane, const float (&v)[32],
-                                          float (*tile)[33], float4 (&w)[8]) {
+                                          uint32_t tile, float4 (&w)[8]) {
   const Shape& sh = p.sh;
   const int col0 = sh.tall ? r0 : c0, row0 = sh.tall ? c0 : r0;
   __syncwarp();
 #pragma unroll
-  for (int j = 0; j < 32; ++j) tile[lane][j] = v[j];
+  for (int j = 0; j < 32; ++j) sts_f32(tile + (lane * 33 + j) * 4, v[j]);
   __syncwarp();
-  // element (row0 + j, col0 + k): tile[j][k], of the transpose tile[k][j]
-  const float* from = &tile[0][0];
-  const int sr = sh.tall ? 1 : 33, sc = sh.tall ? 33 : 1;
+  // element (row0 + j, col0 + k) is at (j, k) of the tile, of the transpose at (k, j)
+  const uint32_t sr = sh.tall ? 4 : 132, sc = sh.tall ? 132 : 4;
   if (p.vec) {
     const int k = 4 * (lane & 7), col = col0 + k;
     if (col < sh.n) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const int j = 4 * i + (lane >> 3), row = row0 + j;
-        const float* x = from + j * sr + k * sc;
-        const float4 o = make_float4(x[0], x[sc], x[2 * sc], x[3 * sc]);
+        const uint32_t x = tile + j * sr + k * sc;
+        const float4 o = make_float4(lds_f32(x), lds_f32(x + sc), lds_f32(x + 2 * sc), lds_f32(x + 3 * sc));
         if (row < sh.m) {
           if (p.update)
             *reinterpret_cast<uint2*>(p.update + (static_cast<int64_t>(b) * sh.m + row) * sh.n + col) =
@@ -505,12 +521,12 @@ __device__ __forceinline__ void final_out(const MmArgs& p, int b, int r0, int c0
   const int col = col0 + lane, rows = col < sh.n ? sh.m - row0 : 0;
   uint16_t* up = p.update ? p.update + (static_cast<int64_t>(b) * sh.m + row0) * sh.n + col : nullptr;
   const int64_t w0 = b * p.stride_w + row0 * p.ld_w + col;
-  from += lane * sc;
+  const uint32_t from = tile + lane * sc;
 #pragma unroll 1
   for (int j0 = 0; j0 < 32; j0 += 8) {
     float x[8], y[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = from[(j0 + j) * sr];
+    for (int j = 0; j < 8; ++j) x[j] = lds_f32(from + (j0 + j) * sr);
     if (p.weights) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) y[j] = j0 + j < rows ? p.weights[w0 + (j0 + j) * p.ld_w] : 0.f;
@@ -715,7 +731,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
     constexpr int NBLK = TILE / 64;
     const int q = warp & 3, first = ((warp - 2) >> 2) * NBLK;
     uint8_t* slabs = sm + NS * STAGE_BYTES + (warp - 2) * EPI_BYTES;
-    float(*tile)[33] = reinterpret_cast<float(*)[33]>(slabs);
+    const uint32_t tile = smem_addr(slabs);
     uint32_t slab = 0;
     uint32_t t = 0;
     for (int item = unit; item < n_items; item += units) {
@@ -797,7 +813,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
           if (lane == 0) tc::bulk_wait_read_1();  // the slab's previous store has read it
           __syncwarp();
         }
-        fill_slab(sb, i & 1, lane, w);
+        fill_slab(smem_addr(sb), i & 1, lane, w);
         if (i & 1) {
           fence_proxy_async_smem();
           __syncwarp();
@@ -902,13 +918,16 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(const __grid_co
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) uint64_t loaded, accf;
   __shared__ uint32_t tbase;
-  __shared__ float d[kSmallSide], e[128];
+  __shared__ __align__(16) float d[kSmallSide];
+  __shared__ float e[128];
   uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_ctarank();
   const int b = blockIdx.x / 2, lp = p.sh.lp, q = warp & 3, half = warp >> 2;
   const SmallSmem at = small_smem(lp);
   const int row = 32 * q + lane, grow = static_cast<int>(rank) * 128 + row;  // this lane's row: here, of the matrix
+  d[threadIdx.x] = 0.f;  // rows and columns past the matrix's last block of 64 stay so
+  if (threadIdx.x < 128) e[threadIdx.x] = 0.f;
   if (threadIdx.x == 0) {
     mbar_init(&loaded, 1);
     mbar_init(&accf, 1);
@@ -941,19 +960,20 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(const __grid_co
   };
   // X, normalised and scaled, into TMEM
   const float inv = p.inv[b];
-  const int nblk = lp / 64, first = half * nblk;  // this warp's 32-column blocks of X
-  for (int i = 0; i < nblk; ++i) {
+  // 64-column blocks of Ao and Bo, and of X, that hold anything; a warp's 32-column blocks are every other one
+  const int ks = (p.sh.s + 63) / 64, kx = (p.sh.l + 63) / 64;
+  for (int cb = half; cb < 2 * kx; cb += 2) {
     float v[32];
-    load_block_row(x_block(p.x, p.sh, b, grow >> 5, first + i), lane, v);
+    load_block_row(x_block(p.x, p.sh, b, grow >> 5, cb), lane, v);
 #pragma unroll
     for (int j = 0; j < 32; ++j) v[j] = v[j] * inv * kXScale;
-    tmem_st32(xt + (first + i) * 32, v);
+    tmem_st32(xt + cb * 32, v);
   }
   wait(&loaded, 0);
   __syncthreads();
 
   const uint64_t k_major = tc::desc_kmajor_sw128(0), mn_major = tc::desc_mnmajor_sw128(0, 2 * kBlk, 1024);
-  const uint32_t base = smem_addr(sm) >> 4;
+  const uint32_t own = smem_addr(sm), base = own >> 4;
   // The products whose operands both CTAs have written by now; everyone returns when they are done.
   uint32_t rounds = 0;
   auto multiply = [&](uint32_t left, uint32_t right, int n, int k_blocks, bool right_mn) {
@@ -984,73 +1004,65 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(const __grid_co
 #pragma unroll 1
   for (int step = 0; step < steps; ++step) {
     // ---- A = X X^T: its diagonal to both CTAs' d, the rest to sy
-    multiply(at.xk, at.xk, kSmallSide, lp / 64, false);
+    multiply(at.xk, at.xk, kSmallSide, kx, false);
 #pragma unroll 1
-    for (int i = 0; i < 4; ++i) {
-      const int cb = 4 * half + i, c0 = 32 * cb;  // the block and its first column
+    for (int cb = half; cb < 2 * ks; cb += 2) {
+      const int c0 = 32 * cb;
       float v[32];
       tc::tmem_ld32(acc + c0, v);
 #pragma unroll
       for (int j = 0; j < 32; ++j) v[j] *= kAScale / (kXScale * kXScale);
       if (c0 == (grow & ~31)) {
-        float own = 0.f;
-#pragma unroll
-        for (int j = 0; j < 32; ++j)
-          if (j == lane) {
-            own = v[j] * (1.f / kAScale);
-            v[j] = 0.f;
-          }
-        d[grow] = own;
-        asm volatile("st.shared::cluster.f32 [%0], %1;" :: "r"(map_to_rank(smem_addr(&d[grow]), rank ^ 1)), "f"(own) : "memory");
+        const float di = take_diagonal(v, lane, 0.f) * (1.f / kAScale);
+        d[grow] = di;
+        asm volatile("st.shared::cluster.f32 [%0], %1;" :: "r"(map_to_rank(smem_addr(&d[grow]), rank ^ 1)), "f"(di) : "memory");
       }
       uint4 w[4];
       pack_row(v, w);
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        *reinterpret_cast<uint4*>(sm + chunk(at.sy + (cb >> 1) * kBlk, 4 * (cb & 1) + k)) = w[k];
+      for (int k = 0; k < 4; ++k) sts_u4(chunk(own + at.sy + (cb >> 1) * kBlk, 4 * (cb & 1) + k), w[k]);
     }
     // ---- B = b A + c A^2: a + its diagonal to e, the rest in Ao's place
-    multiply(at.sy, at.sy, kSmallSide, kSmallSide / 64, false);
+    multiply(at.sy, at.sy, kSmallSide, ks, false);
     const float di = d[grow];
     const float k2 = p.cc * (kBScale / kAScale), k3 = p.cc * (kBScale / (kAScale * kAScale));
     const float k1 = fmaf(k2, di, p.cb * (kBScale / kAScale));
 #pragma unroll 1
-    for (int i = 0; i < 4; ++i) {
-      const int cb = 4 * half + i, c0 = 32 * cb;
+    for (int cb = half; cb < 2 * ks; cb += 2) {
+      const int c0 = 32 * cb;
       float v[32];
       tc::tmem_ld32(acc + c0, v);
-      const bool on_diagonal = c0 == (grow & ~31);
-      if (on_diagonal) {
-#pragma unroll
-        for (int j = 0; j < 32; ++j)
-          if (j == lane) e[row] = p.ca + fmaf(p.cb, di, p.cc * fmaf(di, di, v[j] * (1.f / (kAScale * kAScale))));
-      }
+      if (c0 == (grow & ~31))
+        e[row] = p.ca + fmaf(p.cb, di, p.cc * fmaf(di, di, take_diagonal(v, lane, 0.f) * (1.f / (kAScale * kAScale))));
+      uint32_t blk[4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        uint4* w = reinterpret_cast<uint4*>(sm + chunk(at.sy + (cb >> 1) * kBlk, 4 * (cb & 1) + k));
-        const uint4 h = *w;
+        blk[k] = chunk(own + at.sy + (cb >> 1) * kBlk, 4 * (cb & 1) + k);
+        const uint4 h = lds_u4(blk[k]);
         const uint32_t hh[4] = {h.x, h.y, h.z, h.w};
-        uint32_t o[4];
 #pragma unroll
-        for (int m = 0; m < 4; ++m) {
-          const int j = 8 * k + 2 * m;
-          const float2 a = unpack_half2(hh[m]);
-          float x = fmaf(a.x, fmaf(k2, d[c0 + j], k1), k3 * v[j]);
-          float y = fmaf(a.y, fmaf(k2, d[c0 + j + 1], k1), k3 * v[j + 1]);
-          if (on_diagonal && j == lane) x = 0.f;
-          if (on_diagonal && j + 1 == lane) y = 0.f;
-          o[m] = pack_half2(x, y);
+        for (int m = 0; m < 2; ++m) {
+          const float4 dj = *reinterpret_cast<const float4*>(d + c0 + 8 * k + 4 * m);
+          const float2 a0 = unpack_half2(hh[2 * m]), a1 = unpack_half2(hh[2 * m + 1]);
+          float* o = v + 8 * k + 4 * m;
+          o[0] = fmaf(a0.x, fmaf(k2, dj.x, k1), k3 * o[0]);
+          o[1] = fmaf(a0.y, fmaf(k2, dj.y, k1), k3 * o[1]);
+          o[2] = fmaf(a1.x, fmaf(k2, dj.z, k1), k3 * o[2]);
+          o[3] = fmaf(a1.y, fmaf(k2, dj.w, k1), k3 * o[3]);
         }
-        *w = make_uint4(o[0], o[1], o[2], o[3]);
       }
+      uint4 w[4];
+      pack_row(v, w);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) sts_u4(blk[k], w[k]);
     }
     // ---- X <- e X + Bo X, kept in TMEM and as operands of the next step
-    multiply(at.sy, at.xn, lp, kSmallSide / 64, true);
+    multiply(at.sy, at.xn, lp, ks, true);
     const float f = e[row];
     const bool last = step == steps - 1;
 #pragma unroll 1
-    for (int i = 0; i < nblk; ++i) {
-      const int cb = first + i, c0 = 32 * cb;
+    for (int cb = half; cb < 2 * kx; cb += 2) {
+      const int c0 = 32 * cb;
       float v[32], x[32];
       tc::tmem_ld32(acc + c0, v);
       tc::tmem_ld32(xt + c0, x);
@@ -1060,7 +1072,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(const __grid_co
         float4 wts[8];
         const int r0 = grow & ~31;
         if (p.vec && p.weights) load_weights(p, b, r0, c0, lane, wts);
-        final_out(p, b, r0, c0, lane, v, reinterpret_cast<float(*)[33]>(sm + at.sy + warp * 4352), wts);
+        final_out(p, b, r0, c0, lane, v, own + at.sy + warp * 4352, wts);
         continue;
       }
       tmem_st32(xt + c0, v);
@@ -1068,10 +1080,10 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(const __grid_co
       pack_row(v, w);
       // columns [c0, c0 + 32) in xk, and in xn of the CTA that has them
       const int owner = c0 / (lp / 2), cn = c0 - owner * (lp / 2);
-      const uint32_t to = map_to_rank(smem_addr(sm), owner) + at.xn + (cn / 64) * 2 * kBlk + rank * kBlk;
+      const uint32_t to = map_to_rank(own, owner) + at.xn + (cn / 64) * 2 * kBlk + rank * kBlk;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        *reinterpret_cast<uint4*>(sm + chunk(at.xk + (cb >> 1) * kBlk, 4 * (cb & 1) + k)) = w[k];
+        sts_u4(chunk(own + at.xk + (cb >> 1) * kBlk, 4 * (cb & 1) + k), w[k]);
         st_cluster_u4(chunk(to, 4 * (cb & 1) + k), w[k]);
       }
     }
