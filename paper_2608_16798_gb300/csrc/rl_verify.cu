@@ -189,41 +189,97 @@ __device__ __forceinline__ void exps(float (&z)[N], float ref, float c) {
   }
 }
 
-template <typename T, bool GREEDY>
-__device__ __forceinline__ Fold fold(const Segment<T>& seg, float c, int lane, int& arg) {
-  constexpr int N = Elem<T>::N;
-  float m = minus_inf();
-  float2 s = make_float2(0.f, 0.f);
-  const int nb = seg.blocks();
-#pragma unroll 2
-  for (int k = lane; k < nb; k += 32) {
-    float z[N];
-    seg.load(k, z);
-    float top = z[0];
+constexpr int kTileBlocks = 4;  // 16-byte blocks per lane and tile
+
+__device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+
+// The largest entry of a lane's blocks (NaNs do not count unless there is nothing else).
+template <typename T>
+__device__ __forceinline__ float largest(const uint4 (&w)[kTileBlocks]) {
+  if (sizeof(T) == 2) {
+    uint32_t t = w[0].x;
 #pragma unroll
-    for (int e = 1; e < N; ++e) top = fmaxf(top, z[e]);
-    if (top > m) {
-      const float f = power(m, top, c);
-      s.x *= f;
-      s.y *= f;
-      m = top;
-      if (GREEDY) {
+    for (int i = 0; i < kTileBlocks; ++i)
+      t = max_bf16x2(t, max_bf16x2(max_bf16x2(w[i].x, w[i].y), max_bf16x2(w[i].z, w[i].w)));
+    return fmaxf(bf16_lo(t), bf16_hi(t));
+  }
+  float m = __uint_as_float(w[0].x);
+#pragma unroll
+  for (int i = 0; i < kTileBlocks; ++i)
+    m = fmaxf(m, fmaxf(fmaxf(__uint_as_float(w[i].x), __uint_as_float(w[i].y)),
+                       fmaxf(__uint_as_float(w[i].z), __uint_as_float(w[i].w))));
+  return m;
+}
+
+// A lane's sums over what it has seen.
+struct Running {
+  float m;
+  float2 s;
+  int32_t arg;  // greedy: first largest entry
+};
+
+template <typename T, bool GREEDY>
+__device__ __forceinline__ void add_tile(Running& r, const uint4 (&w)[kTileBlocks], int k0, float c) {
+  constexpr int N = Elem<T>::N;
+  const float top = largest<T>(w);
+  if (top > r.m) {
+    const float f = power(r.m, top, c);
+    r.s.x *= f;
+    r.s.y *= f;
+    r.m = top;
+    if (GREEDY) {
+#pragma unroll
+      for (int i = kTileBlocks - 1; i >= 0; --i) {
+        float z[N];
+        Elem<T>::unpack(w[i], z);
 #pragma unroll
         for (int e = N - 1; e >= 0; --e)
-          if (z[e] == top) arg = k * N + e - seg.lo;
+          if (z[e] == top) r.arg = (k0 + 32 * i) * N + e;
       }
     }
-    exps(z, m == minus_inf() ? 0.f : m, c);
+  }
+  const float ref = r.m == minus_inf() ? 0.f : r.m;
 #pragma unroll
-    for (int e = 0; e < N; e += 2) s = add2(s, make_float2(z[e], z[e + 1]));
+  for (int i = 0; i < kTileBlocks; ++i) {
+    float z[N];
+    Elem<T>::unpack(w[i], z);
+    exps(z, ref, c);
+#pragma unroll
+    for (int e = 0; e < N; e += 2) r.s = add2(r.s, make_float2(z[e], z[e + 1]));
   }
-  const float mine = s.x + s.y, M = redux_max(m);
-  const float sum = warp_sum(mine == 0.f ? 0.f : mine * power(m, M, c));
+}
+
+// The warp's sums of all its lanes.
+__device__ __forceinline__ Fold of_warp(const Running& r, float c) {
+  const float mine = r.s.x + r.s.y, M = redux_max(r.m);
+  return Fold{M, warp_sum(mine == 0.f ? 0.f : mine * power(r.m, M, c))};
+}
+
+// A segment of a row: a tile of blocks at a time, one reference each.
+template <typename T, bool GREEDY>
+__device__ __forceinline__ Fold fold(const Segment<T>& seg, float c, int lane, int& arg) {
+  constexpr uint32_t none = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;
+  const int nb = seg.blocks();
+  Running r{minus_inf(), {0.f, 0.f}, 0};
+  for (int k0 = lane; k0 - lane < nb; k0 += 32 * kTileBlocks) {
+    uint4 w[kTileBlocks];
+#pragma unroll
+    for (int i = 0; i < kTileBlocks; ++i) {
+      const int k = k0 + 32 * i;
+      w[i] = k < nb ? *reinterpret_cast<const uint4*>(seg.at + k * Elem<T>::N) : make_uint4(none, none, none, none);
+    }
+    add_tile<T, GREEDY>(r, w, k0, c);
+  }
+  const Fold f = of_warp(r, c);
   if (GREEDY) {
-    const uint32_t best = __reduce_min_sync(0xffffffffu, m == M ? static_cast<uint32_t>(arg) : 0xffffffffu);
-    arg = static_cast<int>(best);
+    const uint32_t best = __reduce_min_sync(0xffffffffu, r.m == f.m ? static_cast<uint32_t>(r.arg) : 0xffffffffu);
+    arg = static_cast<int>(best) - seg.lo;
   }
-  return Fold{M, sum};
+  return f;
 }
 
 // One entry per segment, the same table in every CTA of the cluster.
@@ -257,6 +313,28 @@ __device__ __forceinline__ Fold merged(const Fold* f, int n, float c, int lane) 
   float s = 0.f;
   for (int k = lane; k < n; k += 32) s += f[k].s == 0.f ? 0.f : f[k].s * power(f[k].m, M, c);
   return Fold{M, warp_sum(s)};
+}
+
+// Two rows' at once: their chains of reductions overlap.
+__device__ __forceinline__ void merged2(const Fold* f, const Fold* g, int n, float c, int lane, Fold& rf, Fold& rg) {
+  float mf = minus_inf(), mg = mf;
+  for (int k = lane; k < n; k += 32) {
+    mf = fmaxf(mf, f[k].m);
+    mg = fmaxf(mg, g[k].m);
+  }
+  const float M = redux_max(mf), G = redux_max(mg);
+  float sf = 0.f, sg = 0.f;
+  for (int k = lane; k < n; k += 32) {
+    sf += f[k].s == 0.f ? 0.f : f[k].s * power(f[k].m, M, c);
+    sg += g[k].s == 0.f ? 0.f : g[k].s * power(g[k].m, G, c);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    sf += __shfl_xor_sync(0xffffffffu, sf, o);
+    sg += __shfl_xor_sync(0xffffffffu, sg, o);
+  }
+  rf = Fold{M, sf};
+  rg = Fold{G, sg};
 }
 
 // No numbers: a row without a finite largest entry, or with a NaN.
@@ -471,9 +549,9 @@ __global__ void __launch_bounds__(kWarps * 32) verify_kernel(const Args p) {
     return [seg_t, ht, c](int k) { return seg_t[k].s == 0.f ? 0.f : seg_t[k].s * power(seg_t[k].m, ht.m, c); };
   };
   if (warp == 0) {
-    const Fold ht = merged(tab.t, n_seg, c, lane);
-    Fold hd{0.f, 1.f};
-    if (two) hd = merged(tab.d, n_seg, c, lane);
+    Fold ht, hd{0.f, 1.f};
+    if (two) merged2(tab.t, tab.d, n_seg, c, lane, ht, hd);
+    else ht = merged(tab.t, n_seg, c, lane);
     const bool bad = is_bad(ht) || is_bad(hd);
     int token = -1;  // greedy
     if (GREEDY && !bad) {
@@ -549,6 +627,7 @@ __global__ void __launch_bounds__(kWarps * 32) verify_kernel(const Args p) {
   if (!plain) {
     float2 r = make_float2(0.f, 0.f);
     const int nb = st.blocks();
+#pragma unroll 2
     for (int k = lane; k < nb; k += 32) {
       float w[Elem<T>::N];
       weights_r(k, w);
@@ -585,7 +664,6 @@ __global__ void __launch_bounds__(kWarps * 32) verify_kernel(const Args p) {
 // cluster per row with both rows in shared memory, whose exchanges leave the copies idle half of the time.
 
 constexpr int kRowWarps = 16;      // of a CTA
-constexpr int kTileBlocks = 4;      // 16-byte blocks per lane and tile
 constexpr int kMaxTiles = 1024;     // of a row
 
 // A row in 16-byte blocks of memory, the first at the block that holds its first element.
@@ -614,74 +692,6 @@ struct Blocks {
     return make_uint4(w[0], w[1], w[2], w[3]);
   }
 };
-
-__device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {
-  uint32_t r;
-  asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  return r;
-}
-
-// The largest entry of a lane's blocks (NaNs do not count unless there is nothing else).
-template <typename T>
-__device__ __forceinline__ float largest(const uint4 (&w)[kTileBlocks]) {
-  if (sizeof(T) == 2) {
-    uint32_t t = w[0].x;
-#pragma unroll
-    for (int i = 0; i < kTileBlocks; ++i)
-      t = max_bf16x2(t, max_bf16x2(max_bf16x2(w[i].x, w[i].y), max_bf16x2(w[i].z, w[i].w)));
-    return fmaxf(bf16_lo(t), bf16_hi(t));
-  }
-  float m = __uint_as_float(w[0].x);
-#pragma unroll
-  for (int i = 0; i < kTileBlocks; ++i)
-    m = fmaxf(m, fmaxf(fmaxf(__uint_as_float(w[i].x), __uint_as_float(w[i].y)),
-                       fmaxf(__uint_as_float(w[i].z), __uint_as_float(w[i].w))));
-  return m;
-}
-
-// A lane's sums over what it has seen.
-struct Running {
-  float m;
-  float2 s;
-  int32_t arg;  // greedy: first largest entry
-};
-
-template <typename T, bool GREEDY>
-__device__ __forceinline__ void add_tile(Running& r, const uint4 (&w)[kTileBlocks], int k0, float c) {
-  constexpr int N = Elem<T>::N;
-  const float top = largest<T>(w);
-  if (top > r.m) {
-    const float f = power(r.m, top, c);
-    r.s.x *= f;
-    r.s.y *= f;
-    r.m = top;
-    if (GREEDY) {
-#pragma unroll
-      for (int i = kTileBlocks - 1; i >= 0; --i) {
-        float z[N];
-        Elem<T>::unpack(w[i], z);
-#pragma unroll
-        for (int e = N - 1; e >= 0; --e)
-          if (z[e] == top) r.arg = (k0 + 32 * i) * N + e;
-      }
-    }
-  }
-  const float ref = r.m == minus_inf() ? 0.f : r.m;
-#pragma unroll
-  for (int i = 0; i < kTileBlocks; ++i) {
-    float z[N];
-    Elem<T>::unpack(w[i], z);
-    exps(z, ref, c);
-#pragma unroll
-    for (int e = 0; e < N; e += 2) r.s = add2(r.s, make_float2(z[e], z[e + 1]));
-  }
-}
-
-// The warp's sums of all its lanes.
-__device__ __forceinline__ Fold of_warp(const Running& r, float c) {
-  const float mine = r.s.x + r.s.y, M = redux_max(r.m);
-  return Fold{M, warp_sum(mine == 0.f ? 0.f : mine * power(r.m, M, c))};
-}
 
 template <typename T, bool GREEDY>
 __global__ void __launch_bounds__(kRowWarps * 32, 32 / kRowWarps) row_kernel(const Args p) {
