@@ -289,3 +289,17 @@ def test_many_long_rows_without_numbers(R):
     R.rl_workspace_init(ws)
     good = VC.make([1] * n, 33000, "bf16", True, seed=24)
     check(R, good, call(R, good, ws=ws)[0], ws)
+
+
+@pytest.mark.parametrize("V,dtype", [(900, "f32"), (30000, "bf16")])
+@pytest.mark.parametrize("longest", [31, 32, 70])
+def test_long_drafts(R, V, dtype, longest):
+    """Rows behind a refusal finish before and after it is known."""
+    rng = np.random.default_rng(25)
+    counts = list(rng.integers(0, longest, 6)) + [longest, 0, longest]
+    c = VC.make(counts, V, dtype, True, noise=0.05, likely=0.9, seed=longest)
+    assert c["max_draft"] == longest
+    for _ in range(2):
+        check(R, c, *call(R, c))
+    c = VC.make(counts, V, dtype, False, T=0.0, seed=longest)
+    check(R, c, *call(R, c))
