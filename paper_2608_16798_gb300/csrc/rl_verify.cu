@@ -392,6 +392,7 @@ __device__ __forceinline__ int locate(int lo, int nb, float left, int lane, W w)
   constexpr int N = Elem<T>::N;
   int last = -1;
   float before = 0.f;
+#pragma unroll 1
   for (int k0 = 0; k0 < nb; k0 += 32) {
     const int k = k0 + lane;
     float x[N], sum = 0.f;
@@ -663,7 +664,6 @@ __global__ void __launch_bounds__(kWarps * 32) verify_kernel(const Args p) {
 // close behind (16 per clock and SM; at 6.8 TB/s 11.8 bf16 entries arrive in that time). Measured against a
 // cluster per row with both rows in shared memory, whose exchanges leave the copies idle half of the time.
 
-constexpr int kRowWarps = 16;      // of a CTA
 constexpr int kMaxTiles = 1024;     // of a row
 
 // A row in 16-byte blocks of memory, the first at the block that holds its first element.
@@ -693,13 +693,13 @@ struct Blocks {
   }
 };
 
-template <typename T, bool GREEDY>
-__global__ void __launch_bounds__(kRowWarps * 32, 32 / kRowWarps) row_kernel(const Args p) {
+template <typename T, bool GREEDY, int WARPS>
+__global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) row_kernel(const Args p) {
   constexpr int N = Elem<T>::N;
   constexpr int kTile = kTileBlocks * 32 * N;  // elements of a tile
   __shared__ Fold tiles[kMaxTiles];            // a draw's weights by tile: sums, or (in s) max(p - q, 0)
-  __shared__ Fold rows[2][kRowWarps];
-  __shared__ int32_t args[kRowWarps];
+  __shared__ Fold rows[2][WARPS];
+  __shared__ int32_t args[WARPS];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int j = blockIdx.x / p.n_seq, b = blockIdx.x % p.n_seq;
   const float c = p.c;
@@ -729,6 +729,7 @@ __global__ void __launch_bounds__(kRowWarps * 32, 32 / kRowWarps) row_kernel(con
   const Blocks<T> bt(zt, p.V), bd(zd, p.V);
   int x = -1;
   float zx = 0.f, zdx = 0.f, ua = 0.f;
+  const float us = p.sample_u[b];
   if (tested) {
     x = p.draft_ids[drow];
     ua = p.accept_u[drow];
@@ -764,13 +765,13 @@ __global__ void __launch_bounds__(kRowWarps * 32, 32 / kRowWarps) row_kernel(con
     int t = warp;
     if (t < n) load(w[0], t);
     while (t < n) {
-      load(w[1], t + kRowWarps);
+      load(w[1], t + WARPS);
       take(w[0], t);
-      t += kRowWarps;
+      t += WARPS;
       if (t >= n) break;
-      load(w[0], t + kRowWarps);
+      load(w[0], t + WARPS);
       take(w[1], t);
-      t += kRowWarps;
+      t += WARPS;
     }
     if (draws) return;
     const Fold f = of_warp(run, c);
@@ -784,15 +785,31 @@ __global__ void __launch_bounds__(kRowWarps * 32, 32 / kRowWarps) row_kernel(con
   if (two) pass(bd, 1);
   __syncthreads();
 
-  // ---- the decision, by every warp alike
-  const Fold ht = draws ? merged(tiles, nt, c, lane) : merged(rows[0], kRowWarps, c, lane);
-  Fold hd{0.f, 1.f};
-  if (two) hd = merged(rows[1], kRowWarps, c, lane);
+  // ---- the decision, by every warp that has work after it
+  if (!two && warp != 0) return;
+  Fold ht, hd{0.f, 1.f};
+  if (two) {
+    merged2(rows[0], rows[1], WARPS, c, lane, ht, hd);
+  } else if (GREEDY) {
+    ht = merged(rows[0], WARPS, c, lane);
+  } else {
+    // the tiles' weights become relative to the row's largest entry
+    float m = minus_inf(), s = 0.f;
+    for (int k = lane; k < nt; k += 32) m = fmaxf(m, tiles[k].m);
+    const float M = redux_max(m);
+    for (int k = lane; k < nt; k += 32) {
+      const Fold f = tiles[k];
+      const float mine = f.s == 0.f ? 0.f : f.s * power(f.m, M, c);
+      tiles[k].s = mine;
+      s += mine;
+    }
+    ht = Fold{M, warp_sum(s)};
+  }
   const bool bad = is_bad(ht) || is_bad(hd);
   int token = -1;
   bool accept = false;
   if (GREEDY && !bad) {
-    const uint32_t best = lane < kRowWarps && rows[0][lane].m == ht.m ? static_cast<uint32_t>(args[lane]) : 0xffffffffu;
+    const uint32_t best = lane < WARPS && rows[0][lane].m == ht.m ? static_cast<uint32_t>(args[lane]) : 0xffffffffu;
     token = static_cast<int>(__reduce_min_sync(0xffffffffu, best)) - bt.lo;
   }
   if (tested && !bad && x >= 0) {
@@ -820,7 +837,7 @@ __global__ void __launch_bounds__(kRowWarps * 32, 32 / kRowWarps) row_kernel(con
   }
 
   // ---- the draw: from max(p - q, 0) after a refusal, else from p
-  const float it = 1.f / ht.s, id_ = 1.f / hd.s, us = p.sample_u[b];
+  const float it = 1.f / ht.s, id_ = 1.f / hd.s;
   const int shift = bd.lo - bt.lo;
   auto weights_p = [&](int k, float (&w)[N]) {
     Elem<T>::unpack(bt.load(k), w);
@@ -832,8 +849,8 @@ __global__ void __launch_bounds__(kRowWarps * 32, 32 / kRowWarps) row_kernel(con
 #pragma unroll
     for (int e = 0; e < N; ++e) w[e] = fmaxf(fmaf(-y[e], id_, w[e] * it), 0.f);
   };
-  auto weights_r = [&](int k, float (&w)[N]) {
-    weights_p(k, w);
+  // from the exponentials of p, of what a refusal draws from
+  auto rest_of = [&](int k, float (&w)[N]) {
     if (two) {
       float y[N];
       if (shift == 0) {
@@ -853,6 +870,10 @@ __global__ void __launch_bounds__(kRowWarps * 32, 32 / kRowWarps) row_kernel(con
         if (e == i) w[e] = 0.f;
     }
   };
+  auto weights_r = [&](int k, float (&w)[N]) {
+    weights_p(k, w);
+    rest_of(k, w);
+  };
   // the weight of tile t, by a warp
   auto weigh = [&](int t, auto weights) {
     float2 r = make_float2(0.f, 0.f);
@@ -864,12 +885,12 @@ __global__ void __launch_bounds__(kRowWarps * 32, 32 / kRowWarps) row_kernel(con
       for (int e = 0; e < N; e += 2) r = add2(r, make_float2(w[e], w[e + 1]));
     }
     const float sum = warp_sum(r.x + r.y);
-    if (lane == 0) tiles[t] = Fold{ht.m, sum};
+    if (lane == 0) tiles[t].s = sum;
     __syncwarp();
   };
   if (two && shift == 0) {
     // as weigh, with a tile of both rows in flight
-    for (int t = warp; t < nt; t += kRowWarps) {
+    for (int t = warp; t < nt; t += WARPS) {
       const int k0 = t * kTileBlocks * 32 + lane;
       uint4 w4[kTileBlocks], y4[kTileBlocks];
 #pragma unroll
@@ -888,17 +909,17 @@ __global__ void __launch_bounds__(kRowWarps * 32, 32 / kRowWarps) row_kernel(con
         for (int e = 0; e < N; e += 2) r = add2(r, make_float2(w[e], w[e + 1]));
       }
       const float sum = warp_sum(r.x + r.y);
-      if (lane == 0) tiles[t] = Fold{ht.m, sum};
+      if (lane == 0) tiles[t].s = sum;
     }
   } else if (two) {
-    for (int t = warp; t < nt; t += kRowWarps) weigh(t, weights_r);
+    for (int t = warp; t < nt; t += WARPS) weigh(t, weights_r);
   }
   if (two) __syncthreads();
   if (warp != 0) return;
   if (tested && !two && x >= 0) weigh((x + bt.lo) / kTile, weights_r);  // p without the token
   bool plain = !tested;
   float left;
-  auto weight = [&](int k) { return tiles[k].s == 0.f ? 0.f : tiles[k].s * power(tiles[k].m, ht.m, c); };
+  auto weight = [&](int k) { return tiles[k].s; };
   int at = pick(nt, us, lane, weight, left);
   if (at < 0) {
     // p and q are equal up to rounding: a draw from p, whose tiles are weighed by this warp alone
@@ -908,8 +929,19 @@ __global__ void __launch_bounds__(kRowWarps * 32, 32 / kRowWarps) row_kernel(con
   }
   const int first = at * kTileBlocks * 32;  // the tile's first block
   const int nb = min(kTileBlocks * 32, (bt.hi + N - 1) / N - first);
-  const int i = plain ? locate<T>(0, nb, left, lane, [&](int k, float (&w)[N]) { weights_p(first + k, w); })
-                      : locate<T>(0, nb, left, lane, [&](int k, float (&w)[N]) { weights_r(first + k, w); });
+  // the tile's loads at once
+  uint4 w4[kTileBlocks];
+#pragma unroll
+  for (int i = 0; i < kTileBlocks; ++i) w4[i] = bt.load(first + 32 * i + lane);
+  const int i = locate<T>(0, nb, left, lane, [&](int k, float (&w)[N]) {
+    uint4 mine = w4[0];
+#pragma unroll
+    for (int i = 1; i < kTileBlocks; ++i)
+      if (k >= 32 * i) mine = w4[i];
+    Elem<T>::unpack(mine, w);
+    exps(w, ht.m, c);
+    if (!plain) rest_of(first + k, w);
+  });
   if (lane == 0) {
     const int drawn = min(max(first * N + i - bt.lo, 0), p.V - 1);
     result(drawn, logp_of(Elem<T>::one(zt[drawn]), ht, c), tested);
@@ -945,10 +977,18 @@ inline bool by_rows(int64_t V, int es, int64_t rows) {
   return rows >= kSMs && V * es >= 48 * 1024 && V * es <= int64_t(kMaxTiles - 2) * kTileBlocks * 32 * 16;
 }
 
+// Half the warps in a CTA (twice the CTAs) where nothing is drafted and CTAs of 16 warps, two per SM, would take
+// more than one turn. Measured, us with 8 / 16 warps: 305 rows of 304 KB 33.5 / 41.6, 509 43.7 / 49.8, 2,000
+// 131.7 / 137.9, but 160 29.3 / 25.2; 509 rows of 80 KB 19.2 / 25.2. With drafted tokens more rows begin before
+// their sequence's refusal is known: 256 sequences of up to 8 looked-up tokens 75.6 / 65.3.
+inline bool small_ctas(const Args& a) { return a.max_draft == 0 && a.n_seq > 2 * kSMs; }
+
 template <typename T, bool GREEDY>
 rl_status run(Args& a, cudaStream_t s) {
   if (by_rows(a.V, sizeof(T), a.n_draft + a.n_seq)) {
-    row_kernel<T, GREEDY><<<static_cast<unsigned>(a.n_seq) * (a.max_draft + 1), kRowWarps * 32, 0, s>>>(a);
+    const unsigned grid = static_cast<unsigned>(a.n_seq) * (a.max_draft + 1);
+    if (small_ctas(a)) row_kernel<T, GREEDY, 8><<<grid, 8 * 32, 0, s>>>(a);
+    else row_kernel<T, GREEDY, 16><<<grid, 16 * 32, 0, s>>>(a);
     const cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? RL_OK : cuda_error(e, "row_kernel launch");
   }

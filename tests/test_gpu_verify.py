@@ -303,3 +303,22 @@ def test_long_drafts(R, V, dtype, longest):
         check(R, c, *call(R, c))
     c = VC.make(counts, V, dtype, False, T=0.0, seed=longest)
     check(R, c, *call(R, c))
+
+
+@pytest.mark.parametrize("V,dtype,pad", [(12289, "f32", 0), (20000, "f32", 3), (33003, "bf16", 5), (25000, "bf16", 0)])
+@pytest.mark.parametrize("T", [1.0, 0.0])
+def test_more_draws_than_run_at_once(R, V, dtype, pad, T):
+    n = 330
+    c = VC.make([0] * n, V, dtype, False, T=T, masked=0.3, seed=V)
+    out, ws = call(R, c, pad=pad)
+    check(R, c, out, ws)
+    again, _ = call(R, c, ws=ws, pad=pad)
+    assert all(torch.equal(a, b) for a, b in zip(out, again))
+    c["target"][7] = -np.inf
+    c["target"][311, V - 1] = np.nan
+    (ids, acc, lp), ws = call(R, c, pad=pad)
+    assert R.rl_query_status(ws)[1] == R.RL_DEV_BAD_VALUE
+    lp, bad = lp.cpu().numpy(), np.isin(np.arange(n), [7, 311])
+    assert (acc == 0).all() and np.array_equal(np.isnan(lp), bad)
+    assert np.array_equal(ids.cpu().numpy()[~bad], out[0].cpu().numpy()[~bad])
+    assert (ids.cpu().numpy()[bad] == -1).all()
