@@ -23,6 +23,8 @@
  *     (Sec. 3.2.1-3.2.3);
  *   - sequence-level importance weights (Sec. 3.2.4) and batch summaries of the
  *     per-token statistics (entropy, clip fraction; Sec. 4);
+ *   - on either side of the loss, without a counterpart in the paper: the verification
+ *     of drafted tokens (the rollout) and the orthogonalised weight update;
  *   - a self-test of the failure path that every bounded device wait shares
  *     (rl_selftest_bounded_wait).
  *
@@ -659,7 +661,8 @@ typedef struct rl_muon_params {
 } rl_muon_params;
 
 /* Workspace bytes of rl_muon_update on `batch` matrices [m x n] (0 for sizes that it refuses). With s
- * the shorter and l the longer side, about 8 s l + 6 s^2 bytes per matrix. */
+ * the shorter and l the longer side, about 8 s l + 6 s^2 bytes per matrix (sides rounded up to 128 and 64,
+ * of matrices of at most 256 x 256 to 256 and 128), and fp32 parts of A where few matrices have a long side. */
 size_t rl_muon_workspace_size(int32_t batch, int64_t m, int64_t n);
 
 /*

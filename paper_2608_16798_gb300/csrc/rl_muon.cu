@@ -186,8 +186,9 @@ constexpr int kPrepWarps = 8;
 
 // u and its sum of squares. A warp forms one 32 x 32 block of X; a CTA's warps take eight blocks that
 // lie side by side in the caller's rows, and such groups in turn, so that the CTAs' last steps (a fence and
-// an atomic) are few. VEC: rows begin at multiples of four elements, and a lane takes 4 x 4 elements
-// twice, as vectors of the caller's rows and, transposed in registers if the matrix is tall, of X.
+// an atomic) are few. Bound by HBM: 6 or 8 bytes read and 8 written per element with a momentum. VEC: rows begin
+// at multiples of four elements, and a lane takes 4 x 4 elements twice, as vectors of the caller's rows and,
+// transposed in registers if the matrix is tall, of X.
 template <bool BF16, bool VEC>
 __global__ void __launch_bounds__(kPrepWarps * 32, VEC ? 3 : 2) momentum_kernel(const PrepArgs p) {
   __shared__ float tile[VEC ? 1 : kPrepWarps][32][33];
@@ -564,6 +565,13 @@ __device__ __forceinline__ void load_weights(const MmArgs& p, int b, int r0, int
 // Per stage of 64 along the contraction a CTA holds 128 rows of the left operand and 128 of the right
 // one's (of a pair's 256). Two accumulators in TMEM, so that the epilogue of one tile runs under the
 // products of the next.
+//
+// Measured on 4,096 x 4,096 (pairs), us: A 52 (one triangle of tiles, 73 GFLOP: 1.4 PFLOP/s), B 57, the
+// new X 111 (1.24 PFLOP/s). The products issue at 150-157 cycles per 256 x 256 x 16, the rate of a library product
+// of this size; the tensor pipe is active 66-71% of the active cycles. The rest is the last turn of tiles (136
+// symmetric or 256 tiles on 76 pairs) and, for X, the epilogue's 128 MB of fp32 state (11K cycles a tile; twice the
+// epilogue warps gave 1,203 us against 1,185 for the whole update). Smaller matrices take 3 to 5 us more than their
+// products per launch: prologue, first loads, epilogue.
 template <int MODE, int CG>
 __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_constant__ CUtensorMap tmA,
                                                               const __grid_constant__ CUtensorMap tmAt,
@@ -878,6 +886,9 @@ __global__ void __launch_bounds__(256) gram_sum_kernel(const MmArgs p) {
 //   xn  all rows of X, its half of the columns: right operand of Bo X (MN-major)
 //   sy  its rows of Ao, then, in their place, of Bo: operands of Ao Ao (K-major) and Bo X
 // so that the pair's MMAs find their halves without an exchange; only the new X goes to both CTAs' xn.
+//
+// 256 x 256, five steps: 61 us a call (104 by launches), nearly all of it this kernel; the tensor pipe is active 29%
+// of the time. What bounds it is the chain: three products and three epilogues a step, a cluster barrier after each.
 
 constexpr int kSmallSide = 256;
 constexpr int kSmallThreads = 256;
