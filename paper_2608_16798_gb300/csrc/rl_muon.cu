@@ -885,13 +885,18 @@ __global__ void __launch_bounds__(256) gram_sum_kernel(const MmArgs p) {
 //   xk  its rows of X: left and right operand of X X^T (K-major), half of the right one's rows each
 //   xn  all rows of X, its half of the columns: right operand of Bo X (MN-major)
 //   sy  its rows of Ao, then, in their place, of Bo: operands of Ao Ao (K-major) and Bo X
-// so that the pair's MMAs find their halves without an exchange; only the new X goes to both CTAs' xn.
+// so that the pair's MMAs find their halves; of the new X the 64-column blocks in xk are, as they lie, halves of blocks
+// of xn, and go there by bulk copies to both CTAs under the next step's first product.
 //
-// 256 x 256, five steps: 61 us a call (104 by launches), nearly all of it this kernel; the tensor pipe is active 29%
-// of the time. What bounds it is the chain: three products and three epilogues a step, a cluster barrier after each.
+// 256 x 256, five steps: 54 us a call (104 by launches), nearly all of it this kernel. What bounds it is the chain of
+// a step, in cycles: three products of 2,500 each, their epilogues 1,250 (A), 2,280 (B) and about 2,500 (X), and 800
+// for the fence and the cluster barrier before each product. Stores of the new X straight to the other CTA made the
+// last epilogue 4,000 and its fence 1,200 (59 us); 16 warps gave 60.
 
 constexpr int kSmallSide = 256;
-constexpr int kSmallThreads = 256;
+constexpr int kSmallWarps = 8;
+constexpr int kSmallThreads = 32 * kSmallWarps;
+constexpr int kSmallParts = kSmallWarps / 4;  // warps that share the rows of a TMEM lane quarter
 constexpr uint32_t kBlk = 128 * 128;  // bytes of 128 rows of a 64-column block
 
 struct SmallSmem {
@@ -899,7 +904,8 @@ struct SmallSmem {
 };
 __host__ __device__ constexpr SmallSmem small_smem(int lp) {
   return SmallSmem{0, static_cast<uint32_t>(lp) / 64 * kBlk, static_cast<uint32_t>(lp) / 64 * kBlk * 2,
-                   static_cast<uint32_t>(lp) / 64 * kBlk * 2 + 4 * kBlk};
+                   static_cast<uint32_t>(lp) / 64 * kBlk * 2 +
+                       (4 * kBlk > kSmallWarps * 4352 ? 4 * kBlk : kSmallWarps * 4352)};
 }
 
 // 32 fp32 columns of this warp's 32 TMEM lanes.
@@ -918,30 +924,29 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const float (&v)[32]) 
   asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
 }
 
-__device__ __forceinline__ void st_cluster_u4(uint32_t addr, uint4 v) {
-  asm volatile("st.shared::cluster.v4.u32 [%0], {%1, %2, %3, %4};"
-               :: "r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+// Bulk copy of shared memory to a CTA of the cluster (addresses and barrier from map_to_rank).
+__device__ __forceinline__ void bulk_s2s(uint32_t to, uint32_t from, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               :: "r"(to), "r"(from), "r"(bytes), "r"(bar) : "memory");
 }
 
-__global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(const __grid_constant__ CUtensorMap tmK,
-                                                                 const __grid_constant__ CUtensorMap tmN, const MmArgs p,
-                                                                 int steps) {
+__global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(const MmArgs p, int steps) {
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t loaded, accf;
+  __shared__ __align__(8) uint64_t accf, spread;
   __shared__ uint32_t tbase;
   __shared__ __align__(16) float d[kSmallSide];
   __shared__ float e[128];
   uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_ctarank();
-  const int b = blockIdx.x / 2, lp = p.sh.lp, q = warp & 3, half = warp >> 2;
+  const int b = blockIdx.x / 2, lp = p.sh.lp, q = warp & 3, part = warp >> 2;
   const SmallSmem at = small_smem(lp);
   const int row = 32 * q + lane, grow = static_cast<int>(rank) * 128 + row;  // this lane's row: here, of the matrix
-  d[threadIdx.x] = 0.f;  // rows and columns past the matrix's last block of 64 stay so
+  if (threadIdx.x < kSmallSide) d[threadIdx.x] = 0.f;  // rows and columns past the matrix's last block of 64 stay so
   if (threadIdx.x < 128) e[threadIdx.x] = 0.f;
   if (threadIdx.x == 0) {
-    mbar_init(&loaded, 1);
     mbar_init(&accf, 1);
+    mbar_init(&spread, 1);
     fence_mbar_init();
   }
   if (warp == 0) tc::tmem_alloc_pair(&tbase, 512);
@@ -951,17 +956,6 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(const __grid_co
   const uint32_t acc = tbase + (static_cast<uint32_t>(32 * q) << 16), xt = acc + 256;
   pdl_launch();
   pdl_wait();
-  if (threadIdx.x == 0) {
-    asm volatile("fence.proxy.async.global;" ::: "memory");
-    mbar_arrive_expect_tx(&loaded, at.sy);  // xk and xn
-    const int y0 = b * kSmallSide;
-    for (int c = 0; c < lp / 64; ++c)
-      tc::tma_load_2d(sm + at.xk + c * kBlk, &tmK, c * 64, y0 + static_cast<int>(rank) * 128, &loaded);
-    for (int c = 0; c < lp / 128; ++c)
-      for (int r = 0; r < 4; ++r)
-        tc::tma_load_2d(sm + at.xn + c * 2 * kBlk + r * (kBlk / 2), &tmN, static_cast<int>(rank) * (lp / 2) + c * 64,
-                        y0 + r * 64, &loaded);
-  }
   bool dead = false;  // a wait ran out: the rest runs through without waiting
   auto wait = [&](uint64_t* bar, uint32_t parity) {
     if (!mbar_wait_bounded(bar, parity, dead ? 1000 : kWaitLimitNs)) {
@@ -969,25 +963,43 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(const __grid_co
       dead = true;
     }
   };
-  // X, normalised and scaled, into TMEM
+  // this lane's row of the 64-column block of 128 rows at `blk`, 16-byte chunk k
+  auto chunk = [&](uint32_t blk, int k) -> uint32_t { return blk + row * 128 + ((k ^ (row & 7)) << 4); };
+  const uint32_t own = smem_addr(sm), base = own >> 4;
+  // columns [32 cb, 32 cb + 32) of this lane's row, as fp16 into a CTA's 128 rows of X, Ao or Bo
+  auto put = [&](uint32_t region, int cb, const float (&v)[32]) {
+    uint4 w[4];
+    pack_row(v, w);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) sts_u4(chunk(own + region + (cb >> 1) * kBlk, 4 * (cb & 1) + k), w[k]);
+  };
+  // this CTA's rows of X, blocks of 64 columns, to xn of the CTA that has the columns
+  auto spread_x = [&] {
+    mbar_arrive_expect_tx(&spread, at.sy - at.xn);
+    for (int c = 0; c < lp / 64; ++c) {
+      const int owner = c / (lp / 128), cn = c % (lp / 128);
+      bulk_s2s(map_to_rank(own + at.xn + cn * 2 * kBlk + rank * kBlk, owner), own + at.xk + c * kBlk, kBlk,
+               map_to_rank(smem_addr(&spread), owner));
+    }
+  };
+  // X, normalised and scaled, into TMEM and the operands
   const float inv = p.inv[b];
   // 64-column blocks of Ao and Bo, and of X, that hold anything; a warp's 32-column blocks are every other one
   const int ks = (p.sh.s + 63) / 64, kx = (p.sh.l + 63) / 64;
-  for (int cb = half; cb < 2 * kx; cb += 2) {
+#pragma unroll 1
+  for (int cb = part; cb < lp / 32; cb += kSmallParts) {
     float v[32];
     load_block_row(x_block(p.x, p.sh, b, grow >> 5, cb), lane, v);
 #pragma unroll
     for (int j = 0; j < 32; ++j) v[j] = v[j] * inv * kXScale;
     tmem_st32(xt + cb * 32, v);
+    put(at.xk, cb, v);
   }
-  wait(&loaded, 0);
-  __syncthreads();
 
   const uint64_t k_major = tc::desc_kmajor_sw128(0), mn_major = tc::desc_mnmajor_sw128(0, 2 * kBlk, 1024);
-  const uint32_t own = smem_addr(sm), base = own >> 4;
   // The products whose operands both CTAs have written by now; everyone returns when they are done.
   uint32_t rounds = 0;
-  auto multiply = [&](uint32_t left, uint32_t right, int n, int k_blocks, bool right_mn) {
+  auto multiply = [&](uint32_t left, uint32_t right, int n, int k_blocks, bool right_mn, auto then) {
     asm volatile("fence.proxy.async;" ::: "memory");  // what was written for the MMAs, here and in the peer
     __syncwarp();
     tc::fence_before_sync();
@@ -1006,18 +1018,18 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(const __grid_co
       }
       tc::mma_commit_pair(&accf, 0x3);
     }
+    then();
     wait(&accf, rounds++ & 1);
     tc::fence_after_sync();
   };
-  // this lane's row of the 64-column block of 128 rows at `blk`, 16-byte chunk k
-  auto chunk = [&](uint32_t blk, int k) -> uint32_t { return blk + row * 128 + ((k ^ (row & 7)) << 4); };
-
 #pragma unroll 1
   for (int step = 0; step < steps; ++step) {
     // ---- A = X X^T: its diagonal to both CTAs' d, the rest to sy
-    multiply(at.xk, at.xk, kSmallSide, kx, false);
+    multiply(at.xk, at.xk, kSmallSide, kx, false, [&] {
+      if (threadIdx.x == 0) spread_x();
+    });
 #pragma unroll 1
-    for (int cb = half; cb < 2 * ks; cb += 2) {
+    for (int cb = part; cb < 2 * ks; cb += kSmallParts) {
       const int c0 = 32 * cb;
       float v[32];
       tc::tmem_ld32(acc + c0, v);
@@ -1028,18 +1040,15 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(const __grid_co
         d[grow] = di;
         asm volatile("st.shared::cluster.f32 [%0], %1;" :: "r"(map_to_rank(smem_addr(&d[grow]), rank ^ 1)), "f"(di) : "memory");
       }
-      uint4 w[4];
-      pack_row(v, w);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) sts_u4(chunk(own + at.sy + (cb >> 1) * kBlk, 4 * (cb & 1) + k), w[k]);
+      put(at.sy, cb, v);
     }
     // ---- B = b A + c A^2: a + its diagonal to e, the rest in Ao's place
-    multiply(at.sy, at.sy, kSmallSide, ks, false);
+    multiply(at.sy, at.sy, kSmallSide, ks, false, [] {});
     const float di = d[grow];
     const float k2 = p.cc * (kBScale / kAScale), k3 = p.cc * (kBScale / (kAScale * kAScale));
     const float k1 = fmaf(k2, di, p.cb * (kBScale / kAScale));
 #pragma unroll 1
-    for (int cb = half; cb < 2 * ks; cb += 2) {
+    for (int cb = part; cb < 2 * ks; cb += kSmallParts) {
       const int c0 = 32 * cb;
       float v[32];
       tc::tmem_ld32(acc + c0, v);
@@ -1068,11 +1077,12 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(const __grid_co
       for (int k = 0; k < 4; ++k) sts_u4(blk[k], w[k]);
     }
     // ---- X <- e X + Bo X, kept in TMEM and as operands of the next step
-    multiply(at.sy, at.xn, lp, ks, true);
+    wait(&spread, step & 1);  // and the peer's, behind the barrier
+    multiply(at.sy, at.xn, lp, ks, true, [] {});
     const float f = e[row];
     const bool last = step == steps - 1;
 #pragma unroll 1
-    for (int cb = half; cb < 2 * kx; cb += 2) {
+    for (int cb = part; cb < 2 * kx; cb += kSmallParts) {
       const int c0 = 32 * cb;
       float v[32], x[32];
       tc::tmem_ld32(acc + c0, v);
@@ -1087,16 +1097,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(const __grid_co
         continue;
       }
       tmem_st32(xt + c0, v);
-      uint4 w[4];
-      pack_row(v, w);
-      // columns [c0, c0 + 32) in xk, and in xn of the CTA that has them
-      const int owner = c0 / (lp / 2), cn = c0 - owner * (lp / 2);
-      const uint32_t to = map_to_rank(own, owner) + at.xn + (cn / 64) * 2 * kBlk + rank * kBlk;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        sts_u4(chunk(own + at.xk + (cb >> 1) * kBlk, 4 * (cb & 1) + k), w[k]);
-        st_cluster_u4(chunk(to, 4 * (cb & 1) + k), w[k]);
-      }
+      put(at.xk, cb, v);
     }
   }
   tc::fence_before_sync();
@@ -1172,7 +1173,7 @@ Shape shape_of(int32_t batch, int64_t m, int64_t n) {
 }
 
 Layout layout_of(const Shape& s) {
-  Layout w;
+  Layout w = {};
   size_t at = kWsHeader;
   auto take = [&](size_t bytes) {
     const size_t here = at;
@@ -1184,6 +1185,12 @@ Layout layout_of(const Shape& s) {
   w.n_parts = static_cast<int32_t>(std::min<int64_t>((along + kPrepWarps - 1) / kPrepWarps * across,
                                                      std::max<int64_t>(1, 6 * kSMs / s.batch)));
   w.x = take(B * sp * lp * 4);
+  w.inv = take(B * 4);
+  w.partial = take(B * w.n_parts * 8);
+  if (is_small(s)) {
+    w.bytes = at;
+    return w;
+  }
   w.x16a = take(B * sp * lp * 2);
   w.x16b = take(B * sp * lp * 2);
   w.a16 = take(B * sp * sp * 2);
@@ -1191,8 +1198,6 @@ Layout layout_of(const Shape& s) {
   w.b16 = take(B * sp * sp * 2);
   w.d = take(B * sp * 4);
   w.e = take(B * sp * 4);
-  w.inv = take(B * 4);
-  w.partial = take(B * w.n_parts * 8);
   const Plan p = plan_of(s.batch, s.sp, s.lp);
   const size_t T = 128 * p.cg_gram;
   w.parts = take(p.splits > 1 ? p.splits * B * symmetric_items(s.sp, p.cg_gram) * T * T * 4 : 0);
@@ -1255,7 +1260,7 @@ rl_status product(const CUtensorMap& a, const CUtensorMap& at, const CUtensorMap
                 out, p);
 }
 
-rl_status small(const CUtensorMap& k, const CUtensorMap& n, const MmArgs& p, int steps, cudaStream_t s) {
+rl_status small(const MmArgs& p, int steps, cudaStream_t s) {
   const size_t smem = small_smem(p.sh.lp).bytes + 1024;
   static std::mutex mu;
   static std::map<int, bool> done;
@@ -1271,8 +1276,7 @@ rl_status small(const CUtensorMap& k, const CUtensorMap& n, const MmArgs& p, int
       done[dev] = true;
     }
   }
-  return launch("small_kernel launch", small_kernel, 2 * static_cast<int64_t>(p.sh.batch), kSmallThreads, smem, 2, s, k, n,
-                p, steps);
+  return launch("small_kernel launch", small_kernel, 2 * static_cast<int64_t>(p.sh.batch), kSmallThreads, smem, 2, s, p, steps);
 }
 
 }  // namespace muon
@@ -1369,10 +1373,12 @@ rl_status rl_muon_update(int32_t batch, int64_t m, int64_t n, const void* grad, 
   st = launch("momentum_kernel launch", momentum_pass, static_cast<int64_t>(batch) * w.n_parts, kPrepWarps * 32, 0, 1, s,
               pa);
   if (st != RL_OK) return st;
-  const int64_t blocks = static_cast<int64_t>(batch) * (sh.sp / 32) * (sh.lp / 32);
-  st = launch("normalise_kernel launch", normalise_kernel, (blocks + kPrepWarps - 1) / kPrepWarps, kPrepWarps * 32, 0, 1,
-              s, pa);
-  if (st != RL_OK) return st;
+  if (!is_small(sh)) {
+    const int64_t blocks = static_cast<int64_t>(batch) * (sh.sp / 32) * (sh.lp / 32);
+    st = launch("normalise_kernel launch", normalise_kernel, (blocks + kPrepWarps - 1) / kPrepWarps, kPrepWarps * 32, 0,
+                1, s, pa);
+    if (st != RL_OK) return st;
+  }
 
   MmArgs a = {};
   a.sh = sh;
@@ -1398,14 +1404,7 @@ rl_status rl_muon_update(int32_t batch, int64_t m, int64_t n, const void* grad, 
   a.step = static_cast<float>(static_cast<double>(P.lr) * P.update_scale / kXScale);
   a.status = status;
   a.inv = pa.inv;
-  if (is_small(sh)) {
-    CUtensorMap k, nmap;
-    const int64_t rows = static_cast<int64_t>(batch) * sh.sp, stride = static_cast<int64_t>(sh.lp) * 2;
-    const auto F16 = CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
-    st = tmap_2d(&k, F16, pa.x16, sh.lp, rows, stride, 64, 128, CU_TENSOR_MAP_SWIZZLE_128B);
-    if (st == RL_OK) st = tmap_2d(&nmap, F16, pa.x16, sh.lp, rows, stride, 64, 64, CU_TENSOR_MAP_SWIZZLE_128B);
-    return st == RL_OK ? small(k, nmap, a, P.ns_steps, s) : st;
-  }
+  if (is_small(sh)) return small(a, P.ns_steps, s);
 
   // boxes of 64 columns: 128 rows of a K-major operand, 64 of an MN-major one, 32 of an output
   uint16_t* x16[2] = {reinterpret_cast<uint16_t*>(base + w.x16a), reinterpret_cast<uint16_t*>(base + w.x16b)};
