@@ -861,13 +861,22 @@ __global__ void __launch_bounds__(256) gram_sum_kernel(const MmArgs p) {
   if (!symmetric_tile<CG>(tile - b * p.per, p.nt_m, ti, tj)) return;
   const int r0 = ti * TILE + in / NB * 32, c0 = tj * TILE + in % NB * 32;
   if (r0 >= p.sh.sp || c0 >= p.sh.sp) return;
-  float v[32], t[32];
+  // two parts' loads in flight
+  float v[32], t[2][32];
   const float* src = p.parts + static_cast<int64_t>(tile) * TILE * TILE + static_cast<int64_t>(in) * 1024;
-  load_block_row(src, lane, v);
-  for (int k = 1; k < p.splits; ++k) {
-    load_block_row(src + static_cast<int64_t>(k) * n_tiles * TILE * TILE, lane, t);
+  auto load = [&](int k, float (&to)[32]) {
+    if (k < p.splits) load_block_row(src + static_cast<int64_t>(k) * n_tiles * TILE * TILE, lane, to);
+  };
+  load(0, v);
+  load(1, t[0]);
+  for (int k = 1; k < p.splits; k += 2) {
+    load(k + 1, t[1]);
 #pragma unroll
-    for (int j = 0; j < 32; ++j) v[j] += t[j];
+    for (int j = 0; j < 32; ++j) v[j] += t[0][j];
+    if (k + 1 == p.splits) break;
+    load(k + 2, t[0]);
+#pragma unroll
+    for (int j = 0; j < 32; ++j) v[j] += t[1][j];
   }
   uint4 w[4];
   gram_of(p, b, r0, c0, lane, v, w);
@@ -1127,7 +1136,7 @@ inline int64_t symmetric_items(int64_t sp, int cg) {
 
 // The cheapest by what the kernels take, measured from 256 x 256 to 4,096 x 4,096, us: per wave of tiles
 // 3 + 0.3 per K block with single CTAs and 4.6 + 0.45 with pairs (both are bound by what L2 delivers, a
-// pair's block does four times the work), and 5.5 for a sum of parts. E.g. X X^T of 2,048 x 2,048: singles
+// pair's block does four times the work), and 5.5 for a sum of parts (about 4 with two parts' loads in flight). E.g. X X^T of 2,048 x 2,048: singles
 // 16.5, pairs in two parts 13.7 + 5.8; B X of 1,000 x 2,777: singles 18.6 (176 tiles, two waves), pairs 16.0.
 Plan plan_of(int64_t batch, int64_t sp, int64_t lp) {
   Plan p = {};
