@@ -1136,8 +1136,9 @@ inline int64_t symmetric_items(int64_t sp, int cg) {
 
 // The cheapest by what the kernels take, measured from 256 x 256 to 4,096 x 4,096, us: per wave of tiles
 // 3 + 0.3 per K block with single CTAs and 4.6 + 0.45 with pairs (both are bound by what L2 delivers, a
-// pair's block does four times the work), and 5.5 for a sum of parts (about 4 with two parts' loads in flight). E.g. X X^T of 2,048 x 2,048: singles
-// 16.5, pairs in two parts 13.7 + 5.8; B X of 1,000 x 2,777: singles 18.6 (176 tiles, two waves), pairs 16.0.
+// pair's block does four times the work), and 5.5 for a sum of parts (about 4 with two parts' loads in flight). E.g.
+// X X^T of 2,048 x 2,048: singles 16.5, pairs in two parts 13.7 + 5.8; B X of 1,000 x 2,777: singles 18.6 (176 tiles,
+// two waves), pairs 16.0.
 Plan plan_of(int64_t batch, int64_t sp, int64_t lp) {
   Plan p = {};
   auto cost = [](int cg, int64_t items, double nkb) {
@@ -1285,7 +1286,8 @@ rl_status small(const MmArgs& p, int steps, cudaStream_t s) {
       done[dev] = true;
     }
   }
-  return launch("small_kernel launch", small_kernel, 2 * static_cast<int64_t>(p.sh.batch), kSmallThreads, smem, 2, s, p, steps);
+  return launch("small_kernel launch", small_kernel, 2 * static_cast<int64_t>(p.sh.batch), kSmallThreads, smem, 2, s, p,
+                steps);
 }
 
 }  // namespace muon
