@@ -20,8 +20,8 @@
 // max(p - q, 0) takes a second pass over the segments, still in shared memory, and a second exchange.
 // The warp whose segment holds the token finds it by a scan. HBM is read once.
 //
-// Measured on bf16 rows of 304 KB: one sequence of 4 drafts (9 rows, 80 CTAs) 10.5-12 us a call with host and
-// launch, 61 sequences of 1 to 7 drafts on fp32 rows of 128 KB 30 us. What bounds it is the chain of a row (offsets,
+// Measured: one sequence of 4 drafts on bf16 rows of 304 KB (5 target and 4 draft rows, 80 CTAs) 11-12.7 us a call with
+// host and launch, 8 sequences of 1 to 5 drafts on rows of 8 KB 12.4-15.5. What bounds it is the chain of a row (offsets,
 // copy, folds, exchange, draw, result), each step a trip to L2 or to the other CTAs, and the fetch of its code from a
 // cold L2; with 80 CTAs 7 of the 16.6 us that the profiler gives are the SMs' own.
 #include <algorithm>
