@@ -477,12 +477,16 @@ __global__ void __launch_bounds__(kWarps * 32) verify_kernel(const Args p) {
   // another CTA's shared memory may be written once that CTA has started
   asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
   if (id >= p.check_from) {
-    // one CTA asks, so that the cluster decides as one
+    // one lane of one CTA asks and all are told what it saw, so that the cluster decides as one (loads of the
+    // same word by several lanes could differ, and a CTA that stays would write to one that has left)
     asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
-    if (rank == 0 && threadIdx.x < C) {
-      const int f = *reinterpret_cast<volatile int32_t*>(p.refused + b);
-      asm volatile("st.shared::cluster.u32 [%0], %1;"
-                   :: "r"(map_to_rank(smem_addr(&skip), threadIdx.x)), "r"(f && kFirst - f < j ? 1 : 0) : "memory");
+    if (rank == 0 && warp == 0) {
+      int f = 0;
+      if (lane == 0) f = *reinterpret_cast<volatile int32_t*>(p.refused + b);
+      f = __shfl_sync(0xffffffffu, f, 0);
+      if (lane < C)
+        asm volatile("st.shared::cluster.u32 [%0], %1;"
+                     :: "r"(map_to_rank(smem_addr(&skip), lane)), "r"(f && kFirst - f < j ? 1 : 0) : "memory");
     }
     __syncwarp();
     cluster_sync_all();

@@ -322,3 +322,19 @@ def test_more_draws_than_run_at_once(R, V, dtype, pad, T):
     assert (acc == 0).all() and np.array_equal(np.isnan(lp), bad)
     assert np.array_equal(ids.cpu().numpy()[~bad], out[0].cpu().numpy()[~bad])
     assert (ids.cpu().numpy()[bad] == -1).all()
+
+
+@pytest.mark.parametrize("V,dtype,n", [(20000, "bf16", 400), (11000, "f32", 400), (150000, "f32", 40)])
+def test_clusters_of_several_ctas_that_skip(R, V, dtype, n):
+    """Clusters of two CTAs and of more, in more turns than one: all CTAs of a row behind a refusal leave, or
+    none does. Most sequences are refused early, and the same call repeats bit for bit."""
+    rng = np.random.default_rng(26)
+    counts = rng.integers(1, 4 if n == 40 else 6, n)
+    assert n != 40 or counts.sum() + n < 152  # not a CTA per row
+    c = VC.make(counts, V, dtype, True, noise=3.0, likely=0.0, seed=V)
+    out, ws = call(R, c)
+    check(R, c, out, ws)
+    for max_draft in (None, 9):
+        again, _ = call(R, c, ws=ws, max_draft=max_draft)
+        assert R.rl_query_status(ws)[1] == 0
+        assert all(torch.equal(a, b) for a, b in zip(out, again))
