@@ -815,6 +815,7 @@ __global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) row_kernel(const Args 
       tiles[k].s = mine;
       s += mine;
     }
+    __syncwarp();  // other lanes read the table in pick, and write to it in weigh
     ht = Fold{M, warp_sum(s)};
   }
   const bool bad = is_bad(ht) || is_bad(hd);
@@ -936,6 +937,7 @@ __global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) row_kernel(const Args 
   if (at < 0) {
     // p and q are equal up to rounding: a draw from p, whose tiles are weighed by this warp alone
     plain = true;
+    __syncwarp();  // pick has read the table
     for (int t = 0; t < nt; ++t) weigh(t, weights_p);
     at = pick(nt, us, lane, weight, left);
   }

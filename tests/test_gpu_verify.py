@@ -338,3 +338,30 @@ def test_clusters_of_several_ctas_that_skip(R, V, dtype, n):
         again, _ = call(R, c, ws=ws, max_draft=max_draft)
         assert R.rl_query_status(ws)[1] == 0
         assert all(torch.equal(a, b) for a, b in zip(out, again))
+
+
+@pytest.mark.parametrize("V,dtype", [(33003, "bf16"), (151936, "bf16"), (33003, "f32")])
+def test_tables_of_tile_weights(R, V, dtype):
+    """A CTA per row, all three readers of its table: draws, draws without the looked-up token, and draws from p
+    where nothing is left without it. The tokens are those of the sums in 64 bits, each time."""
+    n = 170
+    for counts, draft in (([0] * n, False), ([1] * n, False)):
+        c = VC.make(counts, V, dtype, draft, noise=0.0, likely=0.0, seed=V)
+        if counts[0]:
+            c["u"][:] = np.float32(1 - 2.0 ** -24)  # every looked-up token is refused
+            for b in range(n):
+                p = VC.O.softmax(c["target"][2 * b], 1.0)
+                q = np.zeros(V)
+                q[c["ids"][b]] = 1.0
+                c["s"][b] = VC.inside(VC.O.residual(p, q), float(c["s"][b]))
+        ws = R.new_workspace(2 * n, V)
+        for _ in range(4):
+            check(R, c, call(R, c, ws=ws)[0], ws)
+    # one token, drafted and refused by its number: nothing is left of p without it, so the draw is from p
+    c["target"][0::2] = -np.inf
+    c["target"][np.arange(0, 2 * n, 2), c["ids"]] = 1.0
+    c["u"][:] = 1.0
+    for _ in range(4):
+        out, ws = call(R, c)
+        check(R, c, out, ws)
+        assert torch.equal(out[0][0::2].cpu(), torch.from_numpy(c["ids"])) and not out[1].any()
