@@ -166,21 +166,29 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
 }
 
 // Exponents are taken relative to the rounded product ref c, in one fused operation with z c, and every
-// change of reference uses the same rounded products, so that it adds no error of its own. Where ref c
-// could overflow (rows of the type's lowest value) the difference comes first.
-__device__ __forceinline__ bool large(float ref) { return !(fabsf(ref) < 1e30f); }
+// change of reference uses the same rounded products, so that it adds no error of its own. The product's rounding
+// error, at most half a unit below 2^24, would leave fp32's range as an exponent beyond about 2^31 (rows, or a lane's
+// part of one, at finite masks of -1e10), so from 2^24 on they are relative to ref itself: the difference comes first,
+// exact where it matters.
+constexpr float kFused = 16777216.f;
+__device__ __forceinline__ bool large(float ref_c) { return !(fabsf(ref_c) < kFused); }
 __device__ __forceinline__ float exponent(float z, float ref, float c) {
-  return large(ref) ? (z - ref) * c : fmaf(z, c, -__fmul_rn(ref, c));
+  const float rc = __fmul_rn(ref, c);
+  return large(rc) ? (z - ref) * c : fmaf(z, c, -rc);
 }
-// The factor from sums relative to m to sums relative to M >= m.
+// The factor from sums relative to m to sums relative to M >= m, whichever each of them is taken relative to.
 __device__ __forceinline__ float power(float m, float M, float c) {
-  return ex2(large(M) ? (m - M) * c : __fsub_rn(__fmul_rn(m, c), __fmul_rn(M, c)));
+  const float mc = __fmul_rn(m, c), Mc = __fmul_rn(M, c);
+  float x = __fsub_rn(mc, Mc);
+  if (large(mc)) x = fmaf(m, c, -Mc);
+  if (large(Mc)) x = large(mc) ? (m - M) * c : -fmaf(M, c, -mc);
+  return ex2(x);
 }
 // 2^exponent of a block.
 template <int N>
 __device__ __forceinline__ void exps(float (&z)[N], float ref, float c) {
-  if (!large(ref)) {
-    const float rc = -__fmul_rn(ref, c);
+  const float rc = -__fmul_rn(ref, c);
+  if (!large(rc)) {
     const float2 cc = make_float2(c, c), r = make_float2(rc, rc);
 #pragma unroll
     for (int e = 0; e < N; e += 2) {

@@ -365,3 +365,45 @@ def test_tables_of_tile_weights(R, V, dtype):
         out, ws = call(R, c)
         check(R, c, out, ws)
         assert torch.equal(out[0][0::2].cpu(), torch.from_numpy(c["ids"])) and not out[1].any()
+
+
+# few rows: clusters; many long ones: a CTA per row
+FEW, MANY = ([3, 2, 0, 5], 3000), ([2] * 54, 33003)
+
+
+@pytest.mark.parametrize("value", [-1e9, -1e10, -1e15, -1e20])
+@pytest.mark.parametrize("T", [1.0, 0.3, 0.1, 0.0])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("counts,V", [FEW, MANY])
+def test_finite_masks(R, value, T, dtype, counts, V):
+    """Masks whose exponent has a rounding error of more than fp32's range: single entries, and whole stretches, so
+    that some threads see nothing else."""
+    for draft in (True, False):
+        c = VC.make(counts, V, dtype, draft, masked=0.3, mask_value=value, mask_from=V // 3, T=T, seed=27)
+        check(R, c, *call(R, c))
+        c = VC.make(counts, V, dtype, draft, masked=0.95, mask_value=value, T=T, seed=28)
+        check(R, c, *call(R, c))
+
+
+@pytest.mark.parametrize("T", [1.0, 0.3])
+@pytest.mark.parametrize("V", [151936])
+def test_padded_vocabulary(R, T, V):
+    """Draws from rows whose last 293 entries are padding at -1e10."""
+    for n in (3, 160):
+        c = VC.make([0] * n, V, "bf16", False, masked=1e-9, mask_value=-1e10, mask_from=V - 293, T=T, seed=29)
+        check(R, c, *call(R, c))
+
+
+# log2(e) 11629080 is 2^24
+@pytest.mark.parametrize("shift", [11629080, -11629080, 1e10, -1e10, 1e20, -1e20, 3e38, -3e38])
+@pytest.mark.parametrize("T", [1.0, 0.3, 0.0])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("counts,V", [FEW, MANY])
+def test_rows_of_large_entries(R, shift, T, dtype, counts, V):
+    """Rows whose entries, the largest among them, all have a large exponent. In fp32 the first two shifts leave whole
+    numbers next to each other, on both sides of 2^24 as exponents; beyond them the rows are uniform."""
+    for draft in (True, False):
+        c = VC.make(counts, V, dtype, draft, shift=shift, T=T, seed=30)
+        if V == 33003 and dtype == "f32" and abs(shift) < 1e9:
+            assert (np.abs(c["target"]) < 2.0 ** 24 / np.log2(np.e)).any() and (np.abs(c["target"]) > 2.0 ** 24 / np.log2(np.e)).any()
+        check(R, c, *call(R, c))

@@ -31,8 +31,9 @@ def inside(weights, s):
 
 
 def make(counts, V, dtype="f32", draft=True, T=1.0, std=2.0, noise=0.7, masked=0.0, mask_value=-np.inf, seed=0,
-         likely=0.5):
-    """dict(target, draft, ids, offsets, u, s, T): float64 rows with exactly representable entries."""
+         likely=0.5, mask_from=None, shift=None):
+    """dict(target, draft, ids, offsets, u, s, T): float64 rows with exactly representable entries. Entries are masked at
+    random and, with mask_from, from there on; with shift they are whole numbers around it."""
     rng = np.random.default_rng(seed)
     K = np.asarray(counts, np.int64)
     offsets = np.concatenate([[0], np.cumsum(K)]).astype(np.int32)
@@ -41,8 +42,12 @@ def make(counts, V, dtype="f32", draft=True, T=1.0, std=2.0, noise=0.7, masked=0
     zd = z[[r for b in range(n) for r in range(offsets[b] + b, offsets[b + 1] + b)]] + rng.normal(0, noise, (nd, V))
     hot = rng.integers(0, V, nd + n)
     z[np.arange(nd + n), hot] += np.where(rng.random(nd + n) < likely, np.log(V) + std * std / 2, 0)
+    if shift is not None:
+        z, zd = np.rint(z) + shift, np.rint(zd) + shift
     if masked:
         off = rng.random(z.shape) < masked
+        if mask_from is not None:
+            off[:, mask_from:] = True
         off[np.arange(nd + n), hot] = False
         z = np.where(off, mask_value, z)
         if nd:
