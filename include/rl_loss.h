@@ -629,7 +629,8 @@ typedef struct rl_verify_params {
  *
  * A row without a finite largest entry, or with a NaN (of the target's or of the draft's), ends its
  * sequence with token -1 and a NaN log-probability, and sets RL_DEV_BAD_VALUE. Rows behind a sequence's
- * first refusal are read only if they are looked at before the refusal is known.
+ * first refusal are read only if they are looked at before the refusal is known; neither they nor their tokens set
+ * a status bit.
  */
 rl_status rl_verify_drafts(const void* target_logits, const void* draft_logits, rl_dtype dtype, int32_t n_seq,
                            int64_t n_draft, int32_t max_draft, int64_t V, int64_t ld_target, int64_t ld_draft,

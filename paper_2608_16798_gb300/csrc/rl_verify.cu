@@ -39,7 +39,13 @@ namespace verify {
 constexpr int kWarps = 8;
 constexpr int kMaxCluster = 16;
 constexpr int kMaxSeg = kWarps * kMaxCluster;
-constexpr int kFirst = 1 << 30;  // a refusal at place j is kept as kFirst - j: the earliest is the largest
+// A refusal at place j is kept as kFirst - j, the earliest is the largest, with two bits below it: what was wrong
+// with the row. They are reported with the sequence's result, and so not for rows behind its end, which may or may
+// not have been looked at.
+constexpr int kFirst = 1 << 28;
+constexpr int kNoToken = 1, kNoNumbers = 2;
+__device__ __forceinline__ int refusal(int j, int wrong) { return ((kFirst - j) << 2) | wrong; }
+__device__ __forceinline__ int place_of(int f) { return kFirst - (f >> 2); }
 
 struct Args {
   const void* target;
@@ -60,7 +66,7 @@ struct Args {
   float* out_logp;
   int32_t* n_accepted;
   uint32_t* finished;      // [n_seq] rows that have finished
-  int32_t* refused;        // [n_seq] kFirst - (place of the earliest refusal so far), 0: none
+  int32_t* refused;        // [n_seq] the earliest refusal so far, 0: none
   int32_t* status;
 };
 
@@ -440,6 +446,10 @@ __device__ __forceinline__ int locate(int lo, int nb, float left, int lane, W w)
   return static_cast<int>(__reduce_max_sync(0xffffffffu, last));
 }
 
+__device__ __forceinline__ void report(const Args& p, int wrong) {
+  if (wrong) flag_status(p.status, (wrong & kNoToken ? RL_DEV_BAD_TOKEN : 0) | (wrong & kNoNumbers ? RL_DEV_BAD_VALUE : 0));
+}
+
 // A row is finished (its result written, if it has one): the last of its sequence writes what the
 // sequence comes to and leaves the sequence's words at zero. By one thread.
 __device__ __forceinline__ void finish(const Args& p, int b, int o, int K) {
@@ -452,7 +462,8 @@ __device__ __forceinline__ void finish(const Args& p, int b, int o, int K) {
   __threadfence();
   const int f = atomicExch(p.refused + b, 0);
   p.finished[b] = 0;
-  const int n = f ? kFirst - f : K;
+  const int n = f ? place_of(f) : K;
+  report(p, f & 3);
   p.n_accepted[b] = n;
   for (int j = n + 1; j <= K; ++j) {
     p.out_ids[o + b + j] = -1;
@@ -494,7 +505,7 @@ __global__ void __launch_bounds__(kWarps * 32) verify_kernel(const Args p) {
       f = __shfl_sync(0xffffffffu, f, 0);
       if (lane < C)
         asm volatile("st.shared::cluster.u32 [%0], %1;"
-                     :: "r"(map_to_rank(smem_addr(&skip), lane)), "r"(f && kFirst - f < j ? 1 : 0) : "memory");
+                     :: "r"(map_to_rank(smem_addr(&skip), lane)), "r"(f && place_of(f) < j ? 1 : 0) : "memory");
     }
     __syncwarp();
     cluster_sync_all();
@@ -528,7 +539,6 @@ __global__ void __launch_bounds__(kWarps * 32) verify_kernel(const Args p) {
     x = p.draft_ids[drow];
     ua = p.accept_u[drow];
     if (x < 0 || x >= p.V) {
-      if (rank == 0 && threadIdx.x == 0) flag_status(p.status, RL_DEV_BAD_TOKEN);
       x = -1;
     } else {
       zx = Elem<T>::one(zt[x]);
@@ -594,16 +604,17 @@ __global__ void __launch_bounds__(kWarps * 32) verify_kernel(const Args p) {
     if (!over && !tested) at = pick(n_seg, us, lane, weight_p(ht), left);
     if (lane == 0) {
       dec = Decision{ht, hd, left, at, over};
+      const int wrong = (tested && x < 0 ? kNoToken : 0) | (bad ? kNoNumbers : 0);
       if (rank == 0 && over) {
-        if (bad) flag_status(p.status, RL_DEV_BAD_VALUE);
-        if (!accept && p.max_draft > 0) atomicMax(p.refused + b, kFirst - j);
+        if (p.max_draft == 0) report(p, wrong);
+        else if (!accept) atomicMax(p.refused + b, refusal(j, wrong));
         p.out_ids[row] = accept ? x : token;
         p.out_logp[row] = bad ? __int_as_float(0x7fffffff)
                               : logp_of(accept ? zx : Elem<T>::one(zt[token]), ht, c);
         finish(p, b, o, K);
       }
       // ordered before the sequence's result by the cluster barrier that follows a refusal
-      if (rank == 0 && !over && tested) atomicMax(p.refused + b, kFirst - j);
+      if (rank == 0 && !over && tested) atomicMax(p.refused + b, refusal(j, wrong));
     }
   }
   __syncthreads();
@@ -737,7 +748,7 @@ __global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) row_kernel(const Args 
     // one thread asks, so that the CTA decides as one
     int f = 0;
     if (threadIdx.x == 0) f = *reinterpret_cast<volatile int32_t*>(p.refused + b);
-    if (__syncthreads_or(f && kFirst - f < j)) {
+    if (__syncthreads_or(f && place_of(f) < j)) {
       if (threadIdx.x == 0) finish(p, b, o, K);
       return;
     }
@@ -754,7 +765,6 @@ __global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) row_kernel(const Args 
     x = p.draft_ids[drow];
     ua = p.accept_u[drow];
     if (x < 0 || x >= p.V) {
-      if (threadIdx.x == 0) flag_status(p.status, RL_DEV_BAD_TOKEN);
       x = -1;
     } else {
       zx = Elem<T>::one(zt[x]);
@@ -842,15 +852,16 @@ __global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) row_kernel(const Args 
       accept = ua * qx < px;
     }
   }
-  auto result = [&](int id, float lp, bool refusal) {
-    if (refusal && p.max_draft > 0) atomicMax(p.refused + b, kFirst - j);
+  auto result = [&](int id, float lp, bool refused) {
+    const int wrong = (tested && x < 0 ? kNoToken : 0) | (bad ? kNoNumbers : 0);
+    if (p.max_draft == 0) report(p, wrong);
+    else if (refused) atomicMax(p.refused + b, refusal(j, wrong));
     p.out_ids[row] = id;
     p.out_logp[row] = lp;
     finish(p, b, o, K);
   };
   if (accept || bad || GREEDY) {
     if (threadIdx.x == 0) {
-      if (bad) flag_status(p.status, RL_DEV_BAD_VALUE);
       result(accept ? x : token, bad ? __int_as_float(0x7fffffff) : logp_of(accept ? zx : Elem<T>::one(zt[token]), ht, c),
              !accept);
     }

@@ -407,3 +407,40 @@ def test_rows_of_large_entries(R, shift, T, dtype, counts, V):
         if V == 33003 and dtype == "f32" and abs(shift) < 1e9:
             assert (np.abs(c["target"]) < 2.0 ** 24 / np.log2(np.e)).any() and (np.abs(c["target"]) > 2.0 ** 24 / np.log2(np.e)).any()
         check(R, c, *call(R, c))
+
+
+@pytest.mark.parametrize("n,V,dtype", [(4, 500, "f32"), (4, 3000, "bf16"), (400, 1500, "bf16"), (60, 33003, "bf16"), (60, 20000, "f32")])
+@pytest.mark.parametrize("T", [1.0, 0.0])
+def test_status_of_rows_behind_a_refusal(R, n, V, dtype, T):
+    """What is wrong with rows and tokens behind a sequence's end is not reported, whether or not they were looked
+    at; what is wrong with the row that ends it is, by itself."""
+    c = VC.make([3] * n, V, dtype, True, T=T, noise=0.0, likely=0.0, seed=31)
+    row, drow = 4 * np.arange(n), 3 * np.arange(n)
+    c["target"][row, 5] = 30.0  # the first token, another one, is refused
+    c["ids"][drow] = 7
+    c["u"][drow] = 0.5
+    c["s"][:] = 0.5
+    ref = VC.expected(c)
+    assert (ref[1] == 0).all()
+    hurt = dict(c, target=c["target"].copy(), draft=c["draft"].copy(), ids=c["ids"].copy())
+    hurt["target"][row + 1, 11] = np.nan
+    hurt["target"][row + 2] = -np.inf
+    hurt["target"][row + 3, V - 1] = np.inf
+    hurt["draft"][drow + 1, 3] = np.nan
+    hurt["ids"][drow + 1], hurt["ids"][drow + 2] = -5, V
+    for max_draft in (3, 5):
+        out, ws = call(R, hurt, max_draft=max_draft)
+        ids, acc, lp = (x.cpu().numpy() for x in out)
+        assert R.rl_query_status(ws)[1] == 0
+        assert np.array_equal(ids, ref[0]) and np.array_equal(acc, ref[1])
+        assert (np.abs(lp - ref[2]) <= 2e-5 * (1 + np.abs(ref[2]))).all()
+    hurt["ids"][drow[-1]] = V + 3
+    out, ws = call(R, hurt)
+    assert R.rl_query_status(ws)[1] == R.RL_DEV_BAD_TOKEN and not out[1].any()
+    hurt["ids"][drow[-1]] = 7
+    hurt["target"][row[1], 9] = np.nan
+    out, ws = call(R, hurt, ws=ws)
+    assert R.rl_query_status(ws)[1] == R.RL_DEV_BAD_TOKEN | R.RL_DEV_BAD_VALUE and not out[1].any()
+    R.rl_workspace_init(ws)
+    out, ws = call(R, hurt, ws=ws)
+    assert R.rl_query_status(ws)[1] == R.RL_DEV_BAD_VALUE and out[0][4].item() == -1
