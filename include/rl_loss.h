@@ -90,7 +90,8 @@ enum {
   RL_DEV_BAD_TRAJ = 2,    /* token_traj outside [0, n_traj); same treatment */
   RL_DEV_BAD_OFFSETS = 4, /* group / trajectory offsets not non-decreasing within range */
   RL_DEV_TIMEOUT = 8,     /* a bounded wait for an asynchronous copy ran out */
-  RL_DEV_BAD_VALUE = 16   /* a non-finite or out-of-range input value (rl_sequence_is_weights) */
+  RL_DEV_BAD_VALUE = 16   /* a non-finite or out-of-range input value (rl_sequence_is_weights, rl_verify_drafts,
+                             rl_muon_update) */
 };
 
 typedef struct rl_loss_params {

@@ -90,10 +90,11 @@ rl_status rl_query_status(const void* ws, rl_stream_t stream, int32_t* device_st
     return RL_ERR_TIMEOUT;
   }
   char buf[160];
-  std::snprintf(buf, sizeof(buf), "device status 0x%x:%s%s%s", word,
+  std::snprintf(buf, sizeof(buf), "device status 0x%x:%s%s%s%s", word,
                 (word & RL_DEV_BAD_TOKEN) ? " token id out of range;" : "",
                 (word & RL_DEV_BAD_TRAJ) ? " trajectory index out of range;" : "",
-                (word & RL_DEV_BAD_OFFSETS) ? " inconsistent offsets;" : "");
+                (word & RL_DEV_BAD_OFFSETS) ? " inconsistent offsets;" : "",
+                (word & RL_DEV_BAD_VALUE) ? " non-finite or out-of-range value;" : "");
   return rl::set_error(RL_ERR_DEVICE_CHECK, buf);
 }
 

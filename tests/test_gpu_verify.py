@@ -444,3 +444,17 @@ def test_status_of_rows_behind_a_refusal(R, n, V, dtype, T):
     R.rl_workspace_init(ws)
     out, ws = call(R, hurt, ws=ws)
     assert R.rl_query_status(ws)[1] == R.RL_DEV_BAD_VALUE and out[0][4].item() == -1
+
+
+def test_status_texts(R):
+    """Each bit of the status word that the call can set has its words in the error's text."""
+    c = VC.make([1, 1, 1], 500, "f32", True, noise=0.0, likely=0.0, seed=32)
+    c["target"][0, 3], c["ids"][1], c["offsets"][3] = np.nan, -1, 9
+    _, ws = call(R, c)
+    assert R.rl_query_status(ws) == (6, R.RL_DEV_BAD_VALUE | R.RL_DEV_BAD_TOKEN | R.RL_DEV_BAD_OFFSETS)
+    text = R.rl_last_error_message()
+    assert "token id out of range" in text and "inconsistent offsets" in text and "non-finite" in text
+    R.rl_workspace_init(ws)
+    c["ids"][1], c["offsets"][3] = 0, 3
+    call(R, c, ws=ws)
+    assert R.rl_query_status(ws)[1] == R.RL_DEV_BAD_VALUE and "non-finite" in R.rl_last_error_message()
