@@ -984,8 +984,11 @@ __global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) row_kernel(const Args 
 // ---------------------------------------------------------------- host
 
 constexpr int kSMs = 152;
-// Shared memory per CTA beyond the tables (7 KB, static).
+// Shared memory per CTA for segments, beyond the table, barriers and decision (3.2 KB, static), and the block that may
+// be read past the last segment.
 constexpr int64_t kMostBytes = 220 * 1024;
+constexpr int64_t kPastBytes = 16;
+static_assert(sizeof(Table) == 3072 && kMostBytes + kPastBytes + sizeof(Table) + 512 <= 227 * 1024, "a CTA's shared memory");
 constexpr int64_t kGoodBytes = 72 * 1024;  // three CTAs per SM: one's copies run under the others' arithmetic
 
 inline int64_t segment(int64_t V, int64_t C) { return ((V + C * kWarps - 1) / (C * kWarps) + 7) / 8 * 8; }
@@ -1032,7 +1035,7 @@ rl_status run(Args& a, cudaStream_t s) {
   a.seg = static_cast<int32_t>(segment(a.V, C));
   a.seg_bytes = static_cast<int32_t>(segment_bytes(a.V, C, es));
   a.held = held;
-  const size_t smem = static_cast<size_t>(kWarps) * held * a.seg_bytes + 16;  // a block read past the last segment
+  const size_t smem = static_cast<size_t>(kWarps) * held * a.seg_bytes + kPastBytes;
   auto kern = verify_kernel<T, GREEDY>;
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute attr[1];
@@ -1056,7 +1059,8 @@ rl_status run(Args& a, cudaStream_t s) {
     const auto key = std::make_pair(dev, std::make_pair(C, smem));
     auto it = resident.find(key);
     if (it == resident.end()) {
-      e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kMostBytes));
+      e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                               static_cast<int>(kMostBytes + kPastBytes));
       if (e == cudaSuccess) e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
       if (e != cudaSuccess) return cuda_error(e, "cudaFuncSetAttribute(verify_kernel)");
       int n = 0;

@@ -458,3 +458,10 @@ def test_status_texts(R):
     c["ids"][1], c["offsets"][3] = 0, 3
     call(R, c, ws=ws)
     assert R.rl_query_status(ws)[1] == R.RL_DEV_BAD_VALUE and "non-finite" in R.rl_last_error_message()
+
+
+# the most entries of which 16 CTAs hold a row, or a row and its draft row, and the first of that segment size
+@pytest.mark.parametrize("draft,V", [(True, 899073), (True, 900096), (False, 1800193), (False, 1801216)])
+def test_rows_that_fill_the_shared_memory(R, draft, V):
+    c = VC.make([1, 0] if draft else [0, 0], V, "bf16", draft, seed=33)
+    check(R, c, *call(R, c))
