@@ -614,8 +614,9 @@ typedef struct rl_verify_params {
  *   draft_logits   [n_draft rows x ld_draft] of `dtype`, base 16-byte aligned, or NULL
  *   n_seq, n_draft sequences and drafted tokens (0: nothing, and only draws)
  *   max_draft      an upper bound of K_b (rows are laid out for it: a tight one is faster)
- *   V              entries of a row, at most 2^24; a row and its draft row have to fit in the shared
- *                  memory of 16 CTAs (3.5 MB), else RL_ERR_UNSUPPORTED
+ *   V              entries of a row, at most 2^24; a row of more than 2,093,056 bytes has to fit, with its
+ *                  draft row (if there are draft rows and T > 0), in the shared memory of 16 CTAs (3.6 MB),
+ *                  else RL_ERR_UNSUPPORTED
  *   draft_ids      int32 [n_draft] (out of range -> refused, RL_DEV_BAD_TOKEN)
  *   draft_offsets  int32 [n_seq + 1], from 0 to n_draft (a sequence whose offsets are not in order, in range
  *                  and at most max_draft apart: n_accepted = -1, nothing else written, RL_DEV_BAD_OFFSETS)

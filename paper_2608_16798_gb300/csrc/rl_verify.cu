@@ -1005,12 +1005,15 @@ int cluster_of(int64_t V, int es, int rows_held, int64_t clusters) {
   return C;
 }
 
+// A row's tiles fit in the table.
+inline bool fits_table(int64_t V, int es) { return V * es <= int64_t(kMaxTiles - 2) * kTileBlocks * 32 * 16; }
+
 // Whether a CTA takes a row: where every SM has a row, rows are long, and a row's tiles fit in the table.
 // Measured, a CTA per row against a cluster per row, us: 160 rows of 304 KB with drafts' rows 36.5 / 43.7,
 // 152 without 15.4 / 22.0, 305 of 128 KB 23.0 / 27.2, 512 of 64 KB 24.0 / 27.9; 1,280 of 16 KB 30.1 / 22.0,
 // 1,500 of 8 KB 30.4 / 20.7 (the ends of short rows are most of them).
 inline bool by_rows(int64_t V, int es, int64_t rows) {
-  return rows >= kSMs && V * es >= 48 * 1024 && V * es <= int64_t(kMaxTiles - 2) * kTileBlocks * 32 * 16;
+  return rows >= kSMs && V * es >= 48 * 1024 && fits_table(V, es);
 }
 
 // Half the warps in a CTA (twice the CTAs) where nothing is drafted and CTAs of 16 warps, two per SM, would take
@@ -1021,17 +1024,18 @@ inline bool small_ctas(const Args& a) { return a.max_draft == 0 && a.n_seq > 2 *
 
 template <typename T, bool GREEDY>
 rl_status run(Args& a, cudaStream_t s) {
-  if (by_rows(a.V, sizeof(T), a.n_draft + a.n_seq)) {
-    const unsigned grid = static_cast<unsigned>(a.n_seq) * (a.max_draft + 1);
-    if (small_ctas(a)) row_kernel<T, GREEDY, 8><<<grid, 8 * 32, 0, s>>>(a);
-    else row_kernel<T, GREEDY, 16><<<grid, 16 * 32, 0, s>>>(a);
-    const cudaError_t e = cudaGetLastError();
-    return e == cudaSuccess ? RL_OK : cuda_error(e, "row_kernel launch");
-  }
   const int held = a.draft && !GREEDY ? 2 : 1, es = sizeof(T);
   const int64_t clusters = static_cast<int64_t>(a.n_seq) * (a.max_draft + 1);
   const int C = cluster_of(a.V, es, held, clusters);
-  if (C == 0) return set_error(RL_ERR_UNSUPPORTED, "rl_verify_drafts: V is too large for 16 CTAs of 220 KB per row");
+  if (C == 0 && !fits_table(a.V, es))
+    return set_error(RL_ERR_UNSUPPORTED, "rl_verify_drafts: V is too large (above 2.09 MB, and for 16 CTAs of 220 KB)");
+  // a CTA per row also where 16 CTAs do not hold a row and its draft row, whatever the number of rows
+  if (C == 0 || by_rows(a.V, es, a.n_draft + a.n_seq)) {
+    if (small_ctas(a)) row_kernel<T, GREEDY, 8><<<static_cast<unsigned>(clusters), 8 * 32, 0, s>>>(a);
+    else row_kernel<T, GREEDY, 16><<<static_cast<unsigned>(clusters), 16 * 32, 0, s>>>(a);
+    const cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? RL_OK : cuda_error(e, "row_kernel launch");
+  }
   a.seg = static_cast<int32_t>(segment(a.V, C));
   a.seg_bytes = static_cast<int32_t>(segment_bytes(a.V, C, es));
   a.held = held;

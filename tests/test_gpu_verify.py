@@ -465,3 +465,15 @@ def test_status_texts(R):
 def test_rows_that_fill_the_shared_memory(R, draft, V):
     c = VC.make([1, 0] if draft else [0, 0], V, "bf16", draft, seed=33)
     check(R, c, *call(R, c))
+
+
+@pytest.mark.parametrize("V,dtype", [(500000, "f32"), (523264, "f32"), (900097, "bf16"), (1046528, "bf16")])
+def test_rows_beyond_the_shared_memory(R, V, dtype):
+    """A row and its draft row that 16 CTAs do not hold: whether they are taken depends on V alone, not on the rows."""
+    c = VC.make([1, 0], V, dtype, True, noise=1.0, seed=34)
+    check(R, c, *call(R, c))
+    c = VC.make([1, 2], V, dtype, True, T=0.0, seed=35)
+    check(R, c, *call(R, c))
+    c = VC.make([3], 523265 if dtype == "f32" else 1046529, dtype, True, seed=36)
+    with pytest.raises(R.RLError):
+        call(R, c)
