@@ -27,7 +27,7 @@ constexpr size_t kWsValueDoneOffset = 20;
 // Work-item counter of the fused head's backward products (set back by the rescale before it).
 constexpr size_t kWsHeadCounterOffset = 24;
 // The statistics summary's finished clusters, and its clusters' totals (5 doubles each, to the
-// header's end).
+// verification's words).
 constexpr size_t kWsSummaryDoneOffset = 28;
 constexpr size_t kWsSummaryOffset = 32;
 // The orthogonalised update's finished CTAs of its norm pass.
@@ -35,6 +35,9 @@ constexpr size_t kWsMuonDoneOffset = 8;
 // Words of the verification of up to kWsVerifySeqs sequences, two each (zero before and after a call).
 constexpr size_t kWsVerifyOffset = 232;
 constexpr int kWsVerifySeqs = 3;
+static_assert(kWsVerifyOffset + kWsVerifySeqs * 2 * sizeof(uint32_t) <= kWsHeader, "the verification's words fit the header");
+static_assert(kWsMuonDoneOffset >= sizeof(int32_t) && kWsMuonDoneOffset + sizeof(uint32_t) <= kWsDoneOffset,
+              "the norm pass's counter lies between the status word and the loss kernel's");
 
 rl_status set_error(rl_status st, const std::string& msg);
 rl_status cuda_error(cudaError_t e, const char* what);

@@ -33,7 +33,8 @@ constexpr int kSumThreads = 1024;
 constexpr int kSumCluster = 16;  // 8 where the device has no room for one of 16
 constexpr int kSumUnroll = 4;
 constexpr int kSumSlots = 5;
-static_assert(kWsSummaryOffset + kSumSlots * 5 * sizeof(double) <= kWsHeader, "summary slots fit the header");
+static_assert(kWsSummaryOffset + kSumSlots * 5 * sizeof(double) <= kWsVerifyOffset,
+              "summary slots end before the verification's words");
 
 __device__ __forceinline__ void st_cluster_f64(uint32_t addr, double v) {
   asm volatile("st.shared::cluster.f64 [%0], %1;" :: "r"(addr), "d"(v) : "memory");
