@@ -708,7 +708,7 @@ def _matrices(t, name, dtype, shape, ix):
         raise ValueError(f"{name} must have the shape of grad, got {tuple(t.shape)}")
     if t.shape[-1] > 1 and t.stride(-1) != 1:
         raise ValueError(f"{name} must have unit stride along its rows")
-    ld = t.stride(-2) if t.shape[-2] > 1 else max(t.stride(-2), t.shape[-1])
+    ld = t.stride(-2) if t.shape[-2] > 1 else t.shape[-1]  # the stride of a single row says nothing
     return t.data_ptr(), ld, t.stride(0) if t.dim() == 3 and shape[0] > 1 else 0
 
 

@@ -236,3 +236,19 @@ def test_rows_at_and_off_multiples_of_four(R, batch, m, n, pad, dtype):
     # both ways round alike, but for the order in which the norm's squares are added
     for a, b in zip(*results):
         assert (a.float() - b.float()).norm() <= 1e-3 * a.float().norm()
+
+
+def test_strides_of_a_single_row(R):
+    """A weight of one row cut out of a wider buffer, its copy contiguous: the row's own stride says nothing."""
+    for batch in (1, 3):
+        g, w = matrices("normal", batch, 1, 40, 15).cuda(), matrices("normal", batch, 1, 40, 16).cuda()
+        P = R.make_muon_params(lr=0.1, momentum=0.0)
+        ws = R.new_muon_workspace(batch, 1, 40)
+        plain = w.clone()
+        R.rl_muon_update(g, P, ws, weights=plain)
+        wide = torch.full((batch, 5, 8), 7.0, device="cuda")
+        cut = wide.as_strided((batch, 1, 40), (40, 64, 1))
+        cut.copy_(w)
+        copy = torch.empty(batch, 1, 40, dtype=torch.bfloat16, device="cuda")
+        R.rl_muon_update(g, P, ws, weights=cut, weights_bf16=copy)
+        assert torch.equal(cut, plain) and torch.equal(copy, plain.bfloat16())
