@@ -680,8 +680,10 @@ size_t rl_muon_workspace_size(int32_t batch, int64_t m, int64_t n);
  *   ws, ws_bytes   rl_muon_workspace_size(...) bytes, initialised by rl_workspace_init
  *
  * The products run on the tensor cores with fp16 operands and fp32 accumulation; X and the diagonals of
- * A and b A + c A A are held in fp32. The result is within about 1e-3 of the exact X in 2-norm, less
- * than its rounding to bf16 costs (1.7e-3). A zero matrix gives X = 0. A gradient or buffer with a NaN
+ * A and b A + c A A are held in fp32. After up to eight steps the result is within 4e-3 of the exact X
+ * in 2-norm over random, decaying, low-rank and rank-one matrices, mostly within 1.5e-3 (matrices of fewer
+ * than eight rows or columns: 7e-3); its rounding to bf16 costs 1.7e-3. Directions that the matrix lacks grow
+ * by a factor a per step, and beyond eight steps the roundings of the operands with them. A zero matrix gives X = 0. A gradient or buffer with a NaN
  * or an infinity makes its whole matrix's results NaN and sets RL_DEV_BAD_VALUE. Results do not depend
  * on the schedule: repeated calls give the same bits.
  */

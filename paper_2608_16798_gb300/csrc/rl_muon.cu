@@ -16,9 +16,16 @@
 // of A and B, an order larger than the rest once the singular values are near 1, are held in fp32
 // and taken out of the products:
 //   A = D + Ao:  (A^2)_ij = (Ao Ao)_ij + (d_i + d_j) Ao_ij, i != j;  (A^2)_ii = d_i^2 + (Ao Ao)_ii
-//   B = E + Bo:  X <- (a + e_i) X_i + Bo X
-// which halves what is left: 2e-4 to 1e-3 of the result in 2-norm, below the 1.7e-3 of its rounding
-// to bf16.
+//   B = E + Bo:  X <- (a + e_i) X_i + Bo X   in the last two steps
+//                X <- a X_i + (e_i X'_i + Bo X')  before them, X' the operand's fp16 copy of X
+// In the second form B as a whole multiplies one and the same X'. With X' = X + r it adds B r, which lies where B,
+// and so the singular values that are already large, lie. The first form adds Bo r = B r - E r, half of it or less
+// once the values are near 1, but E r lies in all directions, and what lies where X is small every further step
+// multiplies by a: on a single direction 2e-2 of the result at 16 rows, 5e-1 after eight steps. Emulated over random,
+// decaying, low-rank and rank-one matrices: at most 4e-3 of the result in 2-norm after up to eight steps (fewer
+// than eight rows: 7e-3), 5e-5 to 1.5e-3 mostly; the result's rounding to bf16 costs 1.7e-3. Beyond eight steps the
+// operands' other roundings show: directions that the matrix lacks grow by a per step from 1e-5. What the rounding of
+// the old X costs: 0 to 0.4% of a call, 3% of small_kernel's.
 #include <cuda.h>
 #include <cuda_fp16.h>
 
@@ -355,6 +362,7 @@ struct MmArgs {
   float* e;              // [batch x sp] a + the diagonal of B
   float* x;
   const float* inv;      // first step: X is still u, to be multiplied by this
+  int32_t early;         // not one of the last two steps
   float* parts;          // GRAM with splits > 1: [split][tile][TILE x TILE] sums
   // the last step's outputs
   float scale;           // of the update, 2^-12 taken in
@@ -434,6 +442,23 @@ __device__ __forceinline__ float take_diagonal(float (&v)[32], int lane, float t
     v[j] = j == lane ? to : v[j];
   }
   return own;
+}
+
+// The new X (scaled) of 32 elements of a row from the old x and v = 2^10 Bo X', with e = a + the diagonal of B: see
+// the precision of the early steps above.
+__device__ __forceinline__ void new_x(float (&v)[32], const float (&x)[32], float e, float a, bool early) {
+  if (early) {
+    const float eb = e - a;
+#pragma unroll
+    for (int j = 0; j < 32; j += 2) {
+      const float2 r = unpack_half2(pack_half2(x[j], x[j + 1]));
+      v[j] = fmaf(a, x[j], fmaf(eb, r.x, v[j] * (1.f / kBScale)));
+      v[j + 1] = fmaf(a, x[j + 1], fmaf(eb, r.y, v[j + 1] * (1.f / kBScale)));
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 32; ++j) v[j] = fmaf(e, x[j], v[j] * (1.f / kBScale));
+  }
 }
 
 // What becomes of a 32 x 32 block (lane: row) of X X^T, scaled by 2^24: A off its diagonal, scaled, in w
@@ -806,8 +831,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
 #pragma unroll
             for (int j = 0; j < 32; ++j) x[j] = x[j] * inv * kXScale;
           }
-#pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] = fmaf(f, x[j], v[j] * (1.f / kBScale));
+          new_x(v, x, f, p.ca, MODE == APPLY && p.early);
         }
         prefetch(i + 1);
         if (MODE == FINAL) {
@@ -1096,8 +1120,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(const MmArgs p,
       float v[32], x[32];
       tc::tmem_ld32(acc + c0, v);
       tc::tmem_ld32(xt + c0, x);
-#pragma unroll
-      for (int j = 0; j < 32; ++j) v[j] = fmaf(f, x[j], v[j] * (1.f / kBScale));
+      new_x(v, x, f, p.ca, step < steps - 2);
       if (last) {
         float4 wts[8];
         const int r0 = grow & ~31;
@@ -1467,6 +1490,7 @@ rl_status rl_muon_update(int32_t batch, int64_t m, int64_t n, const void* grad, 
     a.nt_n = static_cast<int32_t>(round_up(sh.lp, TA) / TA);
     a.per = a.nt_m * a.nt_n;
     a.inv = k == 0 ? pa.inv : nullptr;
+    a.early = k < P.ns_steps - 2;
     const CUtensorMap &xr = xn[k & 1], &xo = xout[(k + 1) & 1];
     if (k == P.ns_steps - 1)
       st = plan.cg_apply == 2 ? product<FINAL, 2>(bk, bt, xr, xo, a, s) : product<FINAL, 1>(bk, bt, xr, xo, a, s);

@@ -252,3 +252,31 @@ def test_strides_of_a_single_row(R):
         copy = torch.empty(batch, 1, 40, dtype=torch.bfloat16, device="cuda")
         R.rl_muon_update(g, P, ws, weights=cut, weights_bf16=copy)
         assert torch.equal(cut, plain) and torch.equal(copy, plain.bfloat16())
+
+
+# One or two directions and noise: directions in which the matrix is small, or 0, grow by a per step, and whatever the
+# operands' roundings put there with them. Emulated as the file's bounds (these shapes, noises, three seeds): at most
+# 2.0e-3 in 2-norm after 3 and 5 steps, 3.8e-3 after 8, and 3.1e-2 of the root mean square in an element; twice that is
+# allowed.
+FEW_DIRECTIONS = {3: 4e-3, 5: 4e-3, 8: 7.6e-3}
+
+
+@pytest.mark.parametrize("m,n", [(8, 64), (16, 16), (16, 8000), (8000, 16), (64, 8000), (192, 3000), (256, 256), (300, 700)])
+@pytest.mark.parametrize("directions", [1, 2])
+@pytest.mark.parametrize("steps", [3, 5, 8])
+def test_few_directions(R, m, n, directions, steps):
+    ws = R.new_muon_workspace(1, m, n)
+    for noise in (1e-1, 1e-3, 1e-5, 0.0):
+        g = torch.Generator().manual_seed(17)
+        x = torch.randn(m, directions, generator=g) @ torch.randn(directions, n, generator=g)
+        x = x + noise * torch.randn(m, n, generator=g)
+        ref = O.newton_schulz(x.numpy(), steps)
+        norm = np.linalg.norm(ref)
+        w = torch.zeros(m, n, device="cuda")
+        update = torch.empty(m, n, dtype=torch.bfloat16, device="cuda")
+        R.rl_muon_update(x.cuda(), R.make_muon_params(lr=-1.0, momentum=0.0, ns_steps=steps), ws, weights=w, update=update)
+        assert R.rl_query_status(ws)[1] == 0
+        for got, bf16 in ((w, 0.0), (update, 1.0)):
+            d = got.double().cpu().numpy() - ref
+            assert np.linalg.norm(d) <= (FEW_DIRECTIONS[steps] + bf16 * 2.0 ** -9) * norm, (noise, np.linalg.norm(d) / norm)
+            assert (np.abs(d) <= 6.2e-2 * norm / np.sqrt(m * n) + bf16 * 2.0 ** -8 * np.abs(ref)).all(), noise
