@@ -280,3 +280,101 @@ def test_few_directions(R, m, n, directions, steps):
             d = got.double().cpu().numpy() - ref
             assert np.linalg.norm(d) <= (FEW_DIRECTIONS[steps] + bf16 * 2.0 ** -9) * norm, (noise, np.linalg.norm(d) / norm)
             assert (np.abs(d) <= 6.2e-2 * norm / np.sqrt(m * n) + bf16 * 2.0 ** -8 * np.abs(ref)).all(), noise
+
+
+# Sides above 256: not the kernel that takes a whole matrix. Singles and pairs of CTAs, a padded short side that is an odd
+# multiple of 128 (a pair's tile then holds rows of the next matrix), a contraction in parts.
+TILED = [(4, 300, 700), (3, 700, 300), (20, 640, 900), (5, 1400, 1150), (3, 640, 6000), (4, 128, 9000)]
+
+
+@pytest.mark.parametrize("batch,m,n", TILED)
+def test_zero_and_non_finite_in_tiles(R, batch, m, n):
+    """A NaN or an infinity fills its own matrix and no other; a zero matrix stays zero, also without eps."""
+    g = matrices("normal", batch, m, n, 18)
+    P, ws = R.make_muon_params(momentum=0.0, eps=0.0), R.new_muon_workspace(batch, m, n)
+    clean = R.rl_muon_update(g.cuda(), P, ws)
+    assert R.rl_query_status(ws)[1] == 0
+    check_x(clean[:1], O.newton_schulz(g[0].numpy(), eps=0.0)[None], "update", True)
+    for value in (float("nan"), float("inf"), -float("inf")):
+        hurt = g.clone()
+        hurt[1, m - 1, 3] = value
+        hurt[2] = 0
+        got = R.rl_muon_update(hurt.cuda(), P, ws)
+        assert R.rl_query_status(ws)[1] == R.RL_DEV_BAD_VALUE
+        assert got[1].isnan().all() and not got[2].any()
+        for b in range(batch):
+            assert b in (1, 2) or torch.equal(got[b], clean[b]), b
+        R.rl_workspace_init(ws)
+    again = R.rl_muon_update(g.cuda(), P, ws)
+    assert R.rl_query_status(ws)[1] == 0 and torch.equal(again, clean)
+
+
+@pytest.mark.parametrize("scale", [1e-38, 1e-30, 1e-20, 1e20, 1e30, 1e37])
+@pytest.mark.parametrize("m,n", [(300, 520), (520, 300), (100, 5000)])
+def test_scale_of_the_gradient_in_tiles(R, scale, m, n):
+    """As test_scale_of_the_gradient, with sides above 256."""
+    g = (matrices("normal", 1, m, n, 19).double() * scale).float()
+    ws = R.new_muon_workspace(1, m, n)
+    got = R.rl_muon_update(g.cuda(), R.make_muon_params(momentum=0.0, eps=0.0), ws)
+    assert R.rl_query_status(ws)[1] == 0
+    check_x(got, O.newton_schulz(g[0].double().numpy(), eps=0.0)[None], "update", True)
+
+
+@pytest.mark.parametrize("batch,m,n", [(3, 300, 520), (2, 520, 300), (4, 128, 900)])
+def test_interleaved_batch_in_tiles(R, batch, m, n):
+    """As test_interleaved_batch, with sides above 256, a momentum and a bf16 copy."""
+    grad, w, mom = (matrices("normal", batch, m, n, k).cuda() for k in (20, 21, 22))
+    P = R.make_muon_params(lr=0.1, weight_decay=0.1)
+    ws = R.new_muon_workspace(batch, m, n)
+    plain, copy, plain_mom = w.clone(), torch.zeros_like(w, dtype=torch.bfloat16), mom.clone()
+    R.rl_muon_update(grad, P, ws, momentum=plain_mom, weights=plain, weights_bf16=copy)
+    g2, w2 = grad.transpose(0, 1).contiguous(), w.transpose(0, 1).contiguous()
+    copy2, mom2 = torch.zeros_like(w2, dtype=torch.bfloat16), mom.clone()
+    R.rl_muon_update(g2.transpose(0, 1), P, ws, momentum=mom2, weights=w2.transpose(0, 1), weights_bf16=copy2.transpose(0, 1))
+    assert torch.equal(w2.transpose(0, 1), plain) and torch.equal(copy2.transpose(0, 1), copy)
+    assert torch.equal(mom2, plain_mom) and torch.equal(copy, plain.bfloat16())
+
+
+def known(m, n, seed):
+    """(G, X) in float64 on the GPU: G = U S R with U of orthonormal columns (cosines, rows with random signs), R of three
+    reflections and decaying singular values, and X after five steps, from those alone."""
+    l, s = max(m, n), min(m, n)
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    f64 = dict(dtype=torch.float64, device="cuda")
+    k = torch.arange(s, **f64)
+    u = torch.cos((torch.arange(l, **f64) + 0.5)[:, None] * (k * (np.pi / l)))
+    u.mul_(torch.where(k == 0, 1.0, 2.0 ** 0.5) / l ** 0.5)
+    u.mul_(torch.randint(0, 2, (l, 1), generator=g, device="cuda").double() * 2 - 1)
+    sigma = 1 / (1 + k / 8)
+    x = sigma / (sigma.norm() + float(np.float32(1e-7)))
+    a, b, c = (float(np.float32(t)) for t in O.NS_COEF)
+    for _ in range(5):
+        x = a * x + b * x ** 3 + c * x ** 5
+    grad, ref = u * sigma, u.mul_(x)
+    for _ in range(3):
+        v = torch.randn(s, generator=g, **f64)
+        v /= v.norm()
+        for t in (grad, ref):
+            t.addr_(t @ v, v, alpha=-2.0)
+    return (grad, ref) if m > n else (grad.T.contiguous(), ref.T.contiguous())
+
+
+@pytest.mark.parametrize("m,n", [(300, 520), (4500, 4600), (151936, 4096), (4096, 20000)])
+def test_large_matrices(R, m, n):
+    """Sides above 4,096, more tiles per CTA pair than accumulators, and the fused head's d_weight at V = 151,936, D = 4,096.
+    To the bound of the roundings comes one unit of fp32 per 16 elements of the longest contraction."""
+    grad, ref = known(m, n, 23)
+    grad = grad.float()
+    ws = R.new_muon_workspace(1, m, n)
+    w = torch.zeros(m, n, device="cuda")
+    copy = torch.empty(m, n, dtype=torch.bfloat16, device="cuda")
+    update = torch.empty(m, n, dtype=torch.bfloat16, device="cuda")
+    R.rl_muon_update(grad, R.make_muon_params(lr=-1.0, momentum=0.0), ws, weights=w, weights_bf16=copy, update=update)
+    assert R.rl_query_status(ws)[1] == 0
+    assert torch.equal(copy, w.bfloat16()) and torch.equal(update, copy)
+    norm, tol = ref.norm(), NS_REL + max(m, n) / 16 * 2.0 ** -23
+    d = ref.sub_(w)
+    assert d.norm() <= tol * norm, (d.norm() / norm).item()
+    assert d.abs_().max() <= (NS_MAX + tol) * norm / (m * n) ** 0.5
+    del grad, ref, d, w, copy, update, ws
+    torch.cuda.empty_cache()
