@@ -1159,9 +1159,11 @@ inline int64_t symmetric_items(int64_t sp, int cg) {
 
 // The cheapest by what the kernels take, measured from 256 x 256 to 4,096 x 4,096, us: per wave of tiles
 // 3 + 0.3 per K block with single CTAs and 4.6 + 0.45 with pairs (both are bound by what L2 delivers, a
-// pair's block does four times the work), and 5.5 for a sum of parts (about 4 with two parts' loads in flight). E.g.
-// X X^T of 2,048 x 2,048: singles 16.5, pairs in two parts 13.7 + 5.8; B X of 1,000 x 2,777: singles 18.6 (176 tiles,
-// two waves), pairs 16.0.
+// pair's block does four times the work), and 4 for a sum of parts. E.g. X X^T of 2,048 x 2,048: singles 16.5, pairs in
+// two parts 13.7 and their sum; B X of 1,000 x 2,777: singles 18.6 (176 tiles, two waves), pairs 16.0. A charge of 5.5
+// for the sum, as it was with one part's loads in flight, cuts A differently for one shape in 15; of 18 such ones 17 take
+// less with 4 (whole updates: 2 x 467 x 1,217 136 for 146, 1,969 x 5,674 499 for 527, 12 x 363 x 5,303 522 for 542), one
+// more (4 x 723 x 2,793 292 for 284).
 Plan plan_of(int64_t batch, int64_t sp, int64_t lp) {
   Plan p = {};
   auto cost = [](int cg, int64_t items, double nkb) {
@@ -1176,7 +1178,7 @@ Plan plan_of(int64_t batch, int64_t sp, int64_t lp) {
     if (cost(cg, all, sp / BK) < apply) apply = cost(cg, all, sp / BK), p.cg_apply = cg;
     // parts of at least four K blocks that all run at once
     for (int64_t k = 1; k == 1 || (k * sym <= kSMs / cg && lp / BK >= 4 * k); ++k) {
-      const double t = cost(cg, k * sym, static_cast<double>(lp / BK) / k) + (k > 1 ? 5.5 : 0.0);
+      const double t = cost(cg, k * sym, static_cast<double>(lp / BK) / k) + (k > 1 ? 4.0 : 0.0);
       if (t < gram) gram = t, p.cg_gram = cg, p.splits = static_cast<int>(k);
     }
   }
