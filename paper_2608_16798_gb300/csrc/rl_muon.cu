@@ -102,13 +102,12 @@ __device__ __forceinline__ float2 unpack_half2(uint32_t w) {
   return __half22float2(h);
 }
 
-// 32 values of one row as fp16 (64 contiguous, 16-byte aligned bytes).
-__device__ __forceinline__ void store_half_row(uint16_t* to, const float (&v)[32]) {
+// 32 values of one row as fp16.
+__device__ __forceinline__ void pack_row(const float (&v)[32], uint4 (&w)[4]) {
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
-    *reinterpret_cast<uint4*>(to + 8 * j) =
-        make_uint4(pack_half2(v[8 * j], v[8 * j + 1]), pack_half2(v[8 * j + 2], v[8 * j + 3]),
-                   pack_half2(v[8 * j + 4], v[8 * j + 5]), pack_half2(v[8 * j + 6], v[8 * j + 7]));
+  for (int k = 0; k < 4; ++k)
+    w[k] = make_uint4(pack_half2(v[8 * k], v[8 * k + 1]), pack_half2(v[8 * k + 2], v[8 * k + 3]),
+                      pack_half2(v[8 * k + 4], v[8 * k + 5]), pack_half2(v[8 * k + 6], v[8 * k + 7]));
 }
 
 // Shared memory by its 32-bit address (a pointer made of an aligned integer is a generic one to the compiler,
@@ -342,7 +341,11 @@ __global__ void __launch_bounds__(kPrepWarps * 32) normalise_kernel(const PrepAr
   const float f = p.inv[b];
 #pragma unroll
   for (int j = 0; j < 32; ++j) v[j] = v[j] * f * kXScale;
-  store_half_row(p.x16 + (static_cast<int64_t>(b) * sh.sp + R * 32 + lane) * sh.lp + C * 32, v);
+  uint4 w[4];
+  pack_row(v, w);
+  uint16_t* to = p.x16 + (static_cast<int64_t>(b) * sh.sp + R * 32 + lane) * sh.lp + C * 32;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) *reinterpret_cast<uint4*>(to + 8 * k) = w[k];
 }
 
 // ---------------------------------------------------------------- the products
@@ -351,7 +354,7 @@ enum Mode { GRAM = 0, POLY = 1, APPLY = 2, FINAL = 3 };  // FINAL: the last step
 
 struct MmArgs {
   Shape sh;
-  int32_t nt_m, nt_n;    // tiles of the product's rows and columns
+  int32_t nt_m;          // tiles of the product's rows
   int32_t per;           // items of one matrix (GRAM, POLY: see symmetric_tile)
   int32_t nkb;           // 64-element blocks of the contraction
   int32_t splits;        // GRAM: parts of the contraction, each an item
@@ -420,12 +423,6 @@ __device__ __forceinline__ void fill_slab(uint32_t slab, int h, int lane, const 
 #pragma unroll
   for (int k = 0; k < 4; ++k) sts_u4(slab + lane * 128 + (((4 * h + k) ^ (lane & 7)) << 4), w[k]);
 }
-__device__ __forceinline__ void pack_row(const float (&v)[32], uint4 (&w)[4]) {
-#pragma unroll
-  for (int k = 0; k < 4; ++k)
-    w[k] = make_uint4(pack_half2(v[8 * k], v[8 * k + 1]), pack_half2(v[8 * k + 2], v[8 * k + 3]),
-                      pack_half2(v[8 * k + 4], v[8 * k + 5]), pack_half2(v[8 * k + 6], v[8 * k + 7]));
-}
 
 __device__ __forceinline__ uint16_t* a_block(const MmArgs& p, int b, int r0, int c0) {
   const int nb = p.sh.sp >> 5;
@@ -475,33 +472,43 @@ __device__ __forceinline__ void gram_of(const MmArgs& p, int b, int r0, int c0, 
   for (int k = 0; k < 4; ++k) *reinterpret_cast<uint4*>(blk + k * 256) = w[k];
 }
 
+// B = b A + c A^2 from Ao Ao, scaled by 2^24, and the diagonal of A, di at this lane's row.
+struct Poly {
+  float ca, cb, cc, di, k1, k2, k3;
+  __device__ __forceinline__ Poly(const MmArgs& p, float di)
+      : ca(p.ca), cb(p.cb), cc(p.cc), di(di), k2(p.cc * (kBScale / kAScale)), k3(p.cc * (kBScale / (kAScale * kAScale))) {
+    k1 = fmaf(k2, di, p.cb * (kBScale / kAScale));
+  }
+  // a + the element on the diagonal, from that of Ao Ao
+  __device__ __forceinline__ float diagonal(float v) const {
+    return ca + fmaf(cb, di, cc * fmaf(di, di, v * (1.f / (kAScale * kAScale))));
+  }
+  // Eight elements off it, scaled: B_ij = h_ij (k1 + k2 d_j) + k3 v_ij with h the fp16 values of A_ij
+  __device__ __forceinline__ void off_diagonal(float* o, uint4 h, const float4* d) const {
+    const uint32_t w[4] = {h.x, h.y, h.z, h.w};
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      const float4 dj = d[m];
+      const float2 a0 = unpack_half2(w[2 * m]), a1 = unpack_half2(w[2 * m + 1]);
+      o[4 * m] = fmaf(a0.x, fmaf(k2, dj.x, k1), k3 * o[4 * m]);
+      o[4 * m + 1] = fmaf(a0.y, fmaf(k2, dj.y, k1), k3 * o[4 * m + 1]);
+      o[4 * m + 2] = fmaf(a1.x, fmaf(k2, dj.z, k1), k3 * o[4 * m + 2]);
+      o[4 * m + 3] = fmaf(a1.y, fmaf(k2, dj.w, k1), k3 * o[4 * m + 3]);
+    }
+  }
+};
+
 // The same of Ao Ao, scaled by 2^24: B off its diagonal, scaled. a: this lane's row of the block of A;
 // di: the diagonal of A at its row.
 __device__ __forceinline__ void poly_of(const MmArgs& p, int b, int r0, int c0, int lane, float (&v)[32],
                                         const uint4 (&a)[4], float di) {
   const int64_t row = static_cast<int64_t>(b) * p.sh.sp;
+  const Poly poly(p, di);
   // (Ao Ao)_ii goes into e; what it leaves in its place comes to k3 0 + 0 (..) = 0, as Ao_ii is 0
-  if (r0 == c0)
-    p.e[row + r0 + lane] =
-        p.ca + fmaf(p.cb, di, p.cc * fmaf(di, di, take_diagonal(v, lane, 0.f) * (1.f / (kAScale * kAScale))));
-  // B_ij = h_ij (k1 + k2 d_j) + k3 v_ij with h the fp16 value of A_ij and k1 for this row
-  const float k2 = p.cc * (kBScale / kAScale), k3 = p.cc * (kBScale / (kAScale * kAScale));
-  const float k1 = fmaf(k2, di, p.cb * (kBScale / kAScale));
+  if (r0 == c0) p.e[row + r0 + lane] = poly.diagonal(take_diagonal(v, lane, 0.f));
   const float4* d = reinterpret_cast<const float4*>(p.d + row + c0);
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const uint32_t w[4] = {a[k].x, a[k].y, a[k].z, a[k].w};
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const float4 dj = d[2 * k + h];
-      const float2 a0 = unpack_half2(w[2 * h]), a1 = unpack_half2(w[2 * h + 1]);
-      float* o = v + 8 * k + 4 * h;
-      o[0] = fmaf(a0.x, fmaf(k2, dj.x, k1), k3 * o[0]);
-      o[1] = fmaf(a0.y, fmaf(k2, dj.y, k1), k3 * o[1]);
-      o[2] = fmaf(a1.x, fmaf(k2, dj.z, k1), k3 * o[2]);
-      o[3] = fmaf(a1.y, fmaf(k2, dj.w, k1), k3 * o[3]);
-    }
-  }
+  for (int k = 0; k < 4; ++k) poly.off_diagonal(v + 8 * k, a[k], d + 2 * k);
 }
 
 // The last step's X (lane: row) to the caller's outputs, through 32 x 33 floats of shared memory so that
@@ -1077,32 +1084,18 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(const MmArgs p,
     }
     // ---- B = b A + c A^2: a + its diagonal to e, the rest in Ao's place
     multiply(at.sy, at.sy, kSmallSide, ks, false, [] {});
-    const float di = d[grow];
-    const float k2 = p.cc * (kBScale / kAScale), k3 = p.cc * (kBScale / (kAScale * kAScale));
-    const float k1 = fmaf(k2, di, p.cb * (kBScale / kAScale));
+    const Poly poly(p, d[grow]);
 #pragma unroll 1
     for (int cb = part; cb < 2 * ks; cb += kSmallParts) {
       const int c0 = 32 * cb;
       float v[32];
       tc::tmem_ld32(acc + c0, v);
-      if (c0 == (grow & ~31))
-        e[row] = p.ca + fmaf(p.cb, di, p.cc * fmaf(di, di, take_diagonal(v, lane, 0.f) * (1.f / (kAScale * kAScale))));
+      if (c0 == (grow & ~31)) e[row] = poly.diagonal(take_diagonal(v, lane, 0.f));
       uint32_t blk[4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         blk[k] = chunk(own + at.sy + (cb >> 1) * kBlk, 4 * (cb & 1) + k);
-        const uint4 h = lds_u4(blk[k]);
-        const uint32_t hh[4] = {h.x, h.y, h.z, h.w};
-#pragma unroll
-        for (int m = 0; m < 2; ++m) {
-          const float4 dj = *reinterpret_cast<const float4*>(d + c0 + 8 * k + 4 * m);
-          const float2 a0 = unpack_half2(hh[2 * m]), a1 = unpack_half2(hh[2 * m + 1]);
-          float* o = v + 8 * k + 4 * m;
-          o[0] = fmaf(a0.x, fmaf(k2, dj.x, k1), k3 * o[0]);
-          o[1] = fmaf(a0.y, fmaf(k2, dj.y, k1), k3 * o[1]);
-          o[2] = fmaf(a1.x, fmaf(k2, dj.z, k1), k3 * o[2]);
-          o[3] = fmaf(a1.y, fmaf(k2, dj.w, k1), k3 * o[3]);
-        }
+        poly.off_diagonal(v + 8 * k, lds_u4(blk[k]), reinterpret_cast<const float4*>(d + c0 + 8 * k));
       }
       uint4 w[4];
       pack_row(v, w);
@@ -1467,7 +1460,7 @@ rl_status rl_muon_update(int32_t batch, int64_t m, int64_t n, const void* grad, 
   const Plan plan = plan_of(batch, sh.sp, sh.lp);
   for (int k = 0; k < P.ns_steps; ++k) {
     const int T = 128 * plan.cg_gram;
-    a.nt_m = a.nt_n = static_cast<int32_t>(round_up(sh.sp, T) / T);
+    a.nt_m = static_cast<int32_t>(round_up(sh.sp, T) / T);
     a.per = static_cast<int32_t>(symmetric_items(sh.sp, plan.cg_gram));
     a.splits = plan.splits;
     a.nkb = sh.lp / BK;
@@ -1481,7 +1474,7 @@ rl_status rl_muon_update(int32_t batch, int64_t m, int64_t n, const void* grad, 
       if (st != RL_OK) return st;
     }
     const int TP = 128 * plan.cg_poly;
-    a.nt_m = a.nt_n = static_cast<int32_t>(round_up(sh.sp, TP) / TP);
+    a.nt_m = static_cast<int32_t>(round_up(sh.sp, TP) / TP);
     a.per = static_cast<int32_t>(symmetric_items(sh.sp, plan.cg_poly));
     a.splits = 1;
     a.nkb = sh.sp / BK;
@@ -1489,8 +1482,7 @@ rl_status rl_muon_update(int32_t batch, int64_t m, int64_t n, const void* grad, 
     if (st != RL_OK) return st;
     const int TA = 128 * plan.cg_apply;
     a.nt_m = static_cast<int32_t>(round_up(sh.sp, TA) / TA);
-    a.nt_n = static_cast<int32_t>(round_up(sh.lp, TA) / TA);
-    a.per = a.nt_m * a.nt_n;
+    a.per = a.nt_m * static_cast<int32_t>(round_up(sh.lp, TA) / TA);
     a.inv = k == 0 ? pa.inv : nullptr;
     a.early = k < P.ns_steps - 2;
     const CUtensorMap &xr = xn[k & 1], &xo = xout[(k + 1) & 1];

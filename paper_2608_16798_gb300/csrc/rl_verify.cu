@@ -363,6 +363,13 @@ __device__ __forceinline__ float logp_of(float z, const Fold& row, float c) {
   return (exponent(z, row.m, c) - log2f(row.s)) * kLn2;
 }
 
+// Whether the drafted token is accepted: u q < p with p and q from its entries in both rows (q = 1 without one).
+__device__ __forceinline__ bool accepts(float u, float zt, const Fold& t, float zd, const Fold& d, bool two, float c) {
+  const float px = ex2(exponent(zt, t.m, c)) / t.s;
+  const float qx = two ? ex2(exponent(zd, d.m, c)) / d.s : 1.f;
+  return u * qx < px;
+}
+
 // The segment in which the running sum of the weights w(k) passes u times their total, and what is left
 // to pass within it. The last segment with any weight where rounding leaves none; -1: no weight at all.
 // In fp32: the running sum of some hundred weights (the FP64 form took half of the kernel's time).
@@ -589,15 +596,7 @@ __global__ void __launch_bounds__(kWarps * 32) verify_kernel(const Args p) {
       token = static_cast<int>(__reduce_min_sync(0xffffffffu, best));
     }
     bool accept = false;
-    if (tested && !bad && x >= 0) {
-      if (GREEDY) {
-        accept = x == token;
-      } else {
-        const float px = ex2(exponent(zx, ht.m, c)) / ht.s;
-        const float qx = two ? ex2(exponent(zdx, hd.m, c)) / hd.s : 1.f;
-        accept = ua * qx < px;
-      }
-    }
+    if (tested && !bad && x >= 0) accept = GREEDY ? x == token : accepts(ua, zx, ht, zdx, hd, two, c);
     const bool over = accept || bad || GREEDY;
     float left = 0.f;
     int at = -1;
@@ -843,15 +842,7 @@ __global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) row_kernel(const Args 
     const uint32_t best = lane < WARPS && rows[0][lane].m == ht.m ? static_cast<uint32_t>(args[lane]) : 0xffffffffu;
     token = static_cast<int>(__reduce_min_sync(0xffffffffu, best)) - bt.lo;
   }
-  if (tested && !bad && x >= 0) {
-    if (GREEDY) {
-      accept = x == token;
-    } else {
-      const float px = ex2(exponent(zx, ht.m, c)) / ht.s;
-      const float qx = two ? ex2(exponent(zdx, hd.m, c)) / hd.s : 1.f;
-      accept = ua * qx < px;
-    }
-  }
+  if (tested && !bad && x >= 0) accept = GREEDY ? x == token : accepts(ua, zx, ht, zdx, hd, two, c);
   auto result = [&](int id, float lp, bool refused) {
     const int wrong = (tested && x < 0 ? kNoToken : 0) | (bad ? kNoNumbers : 0);
     if (p.max_draft == 0) report(p, wrong);
