@@ -598,9 +598,9 @@ __device__ __forceinline__ void load_weights(const MmArgs& p, int b, int r0, int
 // one's (of a pair's 256). Two accumulators in TMEM, so that the epilogue of one tile runs under the
 // products of the next.
 //
-// Measured on 4,096 x 4,096 (pairs), us: A 52 (one triangle of tiles, 73 GFLOP: 1.4 PFLOP/s), B 57, the
-// new X 111 (1.24 PFLOP/s). The products issue at 150-157 cycles per 256 x 256 x 16, the rate of a library product
-// of this size; the tensor pipe is active 66-71% of the active cycles. The rest is the last turn of tiles (136
+// Measured on 4,096 x 4,096 (pairs), us: A 51 (one triangle of tiles, 73 GFLOP: 1.4 PFLOP/s), B 57, the
+// new X 107 (1.28 PFLOP/s; a library's fp16 product of this size, which writes fp16 and nothing else, 81: 1.70). The
+// products issue at 150-157 cycles per 256 x 256 x 16; the tensor pipe is active 66-71% of the active cycles. The rest is the last turn of tiles (136
 // symmetric or 256 tiles on 76 pairs) and, for X, the epilogue's 128 MB of fp32 state (11K cycles a tile; twice the
 // epilogue warps gave 1,203 us against 1,185 for the whole update). Smaller matrices take 3 to 5 us more than their
 // products per launch: prologue, first loads, epilogue.
@@ -928,9 +928,9 @@ __global__ void __launch_bounds__(256) gram_sum_kernel(const MmArgs p) {
 // so that the pair's MMAs find their halves; of the new X the 64-column blocks in xk are, as they lie, halves of blocks
 // of xn, and go there by bulk copies to both CTAs under the next step's first product.
 //
-// 256 x 256, five steps: 54 us a call (104 by launches), nearly all of it this kernel. What bounds it is the chain of
-// a step, in cycles: three products of 2,500 each, their epilogues 1,250 (A), 2,280 (B) and about 2,500 (X), and 800
-// for the fence and the cluster barrier before each product. Stores of the new X straight to the other CTA made the
+// 256 x 256, five steps: 55.6 us a call (104 by launches), nearly all of it this kernel. What bounds it is the chain of
+// a step, in cycles: three products of 2,500 each, their epilogues 1,250 (A), 2,280 (B) and about 2,500 (X; before the
+// last two steps about 1,000 more for the rounding of the old X, by the call's time with and without it), and 800 for the fence and the cluster barrier before each product. Stores of the new X straight to the other CTA made the
 // last epilogue 4,000 and its fence 1,200 (59 us); 16 warps gave 60.
 
 constexpr int kSmallSide = 256;

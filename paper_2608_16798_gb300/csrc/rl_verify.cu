@@ -20,10 +20,10 @@
 // max(p - q, 0) takes a second pass over the segments, still in shared memory, and a second exchange.
 // The warp whose segment holds the token finds it by a scan. HBM is read once.
 //
-// Measured: one sequence of 4 drafts on bf16 rows of 304 KB (5 target and 4 draft rows, 80 CTAs) 11-12.7 us a call with
-// host and launch, 8 sequences of 1 to 5 drafts on rows of 8 KB 12.4-15.5. What bounds it is the chain of a row (offsets,
+// Measured: one sequence of 4 drafts on bf16 rows of 304 KB (5 target and 4 draft rows, 80 CTAs) 11-13.4 us a call with
+// host and launch, 8 sequences of 1 to 5 drafts on rows of 8 KB 12.7-16.8. What bounds it is the chain of a row (offsets,
 // copy, folds, exchange, draw, result), each step a trip to L2 or to the other CTAs, and the fetch of its code from a
-// cold L2; with 80 CTAs 7 of the 16.6 us that the profiler gives are the SMs' own.
+// cold L2; with 80 CTAs 7 of the 16.7 us that the profiler gives are the SMs' own.
 #include <algorithm>
 #include <cmath>
 #include <map>
@@ -690,7 +690,7 @@ __global__ void __launch_bounds__(kWarps * 32) verify_kernel(const Args p) {
 // twice. What bounds it is HBM with the exponentials
 // close behind (16 per clock and SM; at 6.8 TB/s 11.8 bf16 entries arrive in that time). Measured against a
 // cluster per row with both rows in shared memory, whose exchanges leave the copies idle half of the time.
-// 128 sequences of 4 drafts at V = 151,936 (bf16): 85 us, 369 MB read at 4.4 TB/s; 509 draws 36.6 us, 155 MB at
+// 128 sequences of 4 drafts at V = 151,936 (bf16): 87.5 us, 369 MB read at 4.2 TB/s; 509 draws 36.9 us, 155 MB at
 // 4.2 TB/s. The passes run at 5.8-6 TB/s; what is lost is the rows' ends, 7-10K cycles of the 43K of a draw
 // (the sums' merge 2.5K, the tile 3.5K, the place in it 3.5K), and the second turn of CTAs.
 
