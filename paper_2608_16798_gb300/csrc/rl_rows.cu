@@ -165,7 +165,14 @@ __device__ __forceinline__ bool block_inside(const T* src, const T* end) {
   return src - block_offset(src) + 16 / sizeof(T) <= end;
 }
 
-// fold one value into a per-thread online-softmax partial whose max is already >= z
+// The reference for a largest value: not below -1e9. The rounding error of a reference's product with log2(e) is an
+// exponent of up to 512 at -1e10, and a thread that has seen nothing but finite masks there would make its row's sum
+// infinite; relative to -1e9 they weigh 0, as they do beside any other value, and the next value raises the reference.
+// (A NaN stays NaN.) Without the entropy a block takes its first reference as it is and comes here only if its sum is
+// too large: what a smaller error leaves weighs 0 beside the row's other values.
+__device__ __forceinline__ float reference(float m) { return m < -1e9f ? -1e9f : m; }
+
+// fold one value into a per-thread online-softmax partial whose reference is already >= reference(z)
 template <bool ENT>
 __device__ __forceinline__ void accumulate(SoftmaxPartial& ps, float z, float neg_m_l2e) {
   if (ENT) {
@@ -262,7 +269,7 @@ __device__ __forceinline__ void fold_block(SoftmaxPartial& ps, const uint4 (&x)[
     float m0 = vmax(x[0]);
     if (!(m0 > -1e38f)) m0 = all_max();
     if (NAN_REF ? m0 <= -1e38f : !(m0 > -1e38f)) return;
-    ps.m = m0;
+    ps.m = ENT ? reference(m0) : m0;
   }
   // x = (z - m) log2(e) by one fused multiply-add against nm = fl(-m log2(e)); with the
   // entropy, u accumulates e x (log2 units, scaled by ln 2 at the end). A logit at -inf gives
@@ -297,7 +304,7 @@ __device__ __forceinline__ void fold_block(SoftmaxPartial& ps, const uint4 (&x)[
   if (!(se <= 1e30f) || (ENT && ue != ue)) {
     // rare: a value far above the reference (move it up to the exact maximum) or a logit at
     // -inf with the entropy on; redo from shared memory on the clamped path
-    if (!(se <= 1e30f)) raise_max<ENT>(ps, all_max());
+    if (!(se <= 1e30f)) raise_max<ENT>(ps, reference(all_max()));
     s0 = z2; s1 = z2; u0 = z2;
     for (int k = 0; k < NV; ++k) exps(Clamped{}, reload(k), s0, s1, u0);
     sacc = __fadd2_rn(s0, s1);
@@ -685,7 +692,7 @@ __global__ void __launch_bounds__((NW + 1) * 32, MINB) rows_kernel(const RowArgs
           const float z = Vec<T>::to_f(buf[(warp == 0 ? m.e_at : edge0 + EPV) + lane]);
           tail_z = z;
           if (z != RL_NEG_INF) {
-            raise_max<ENT>(ps, z);
+            raise_max<ENT>(ps, reference(z));
             accumulate<ENT>(ps, z, -ps.m * kLog2e);
           }
         }
@@ -1085,7 +1092,7 @@ __global__ void __launch_bounds__((kF32Warps + 1) * 32, 3) rows_f32_kernel(const
         const float z = Vec<T>::to_f(buf[nv * EPV + tid]);
         tail_z = z;
         if (z != RL_NEG_INF) {
-          raise_max<ENT>(ps, z);
+          raise_max<ENT>(ps, reference(z));
           accumulate<ENT>(ps, z, -ps.m * kLog2e);
         }
       }
@@ -1316,7 +1323,7 @@ struct SmallRow {
       }
     }
     if (edge >= 0 && ez != RL_NEG_INF) {
-      raise_max<ENT>(ps, ez);
+      raise_max<ENT>(ps, reference(ez));
       accumulate<ENT>(ps, ez, -ps.m * kLog2e);
     }
     return merge_lanes<T, ENT>(ps);
@@ -1713,7 +1720,7 @@ __global__ void __launch_bounds__((NW + 1) * 32, MINB) stream_logprobs_kernel(co
         if (lane < (warp == 0 ? ci.edges & 15 : (ci.edges >> 4) & 15)) {
           const float z = Vec<T>::to_f(buf[at]);
           if (z != RL_NEG_INF) {
-            raise_max<ENT>(ps, z);
+            raise_max<ENT>(ps, reference(z));
             accumulate<ENT>(ps, z, -ps.m * kLog2e);
           }
         }
