@@ -24,7 +24,9 @@
  *   - sequence-level importance weights (Sec. 3.2.4) and batch summaries of the
  *     per-token statistics (entropy, clip fraction; Sec. 4);
  *   - on either side of the loss, without a counterpart in the paper: the verification
- *     of drafted tokens (the rollout) and the orthogonalised weight update;
+ *     of drafted tokens (the rollout) and the orthogonalised weight update; the policy model's
+ *     ends: the embedding of the tokens and the layer norm before the LM head, forward and
+ *     backward;
  *   - a self-test of the failure path that every bounded device wait shares
  *     (rl_selftest_bounded_wait).
  *
@@ -691,6 +693,89 @@ rl_status rl_muon_update(int32_t batch, int64_t m, int64_t n, const void* grad, 
                          int64_t ld_grad, int64_t stride_grad, float* momentum, float* weights,
                          uint16_t* weights_bf16, int64_t ld_w, int64_t stride_w, uint16_t* update,
                          const rl_muon_params* params, void* ws, size_t ws_bytes, rl_stream_t stream);
+
+/*
+ * Layer norm of the rows of a matrix (no counterpart in the paper: the norm before the LM head, whose output
+ * is the `hidden` of the fused head and whose backward pass takes its d_hidden). Per row x [D]:
+ *
+ *   mean = sum x / D;   rstd = 1 / sqrt(sum (x - mean)^2 / D + eps);   y = (x - mean) rstd w + b
+ *
+ *   x              [rows x ld_x] of x_dtype, aligned to its elements
+ *   rows, D        rows >= 0, 1 <= D <= 2^20, at most 2^40 elements; ld_x, ld_y >= D
+ *   weight, bias   [D] of w_dtype, or NULL (1 and 0)
+ *   eps            >= 0; with eps = 0 a row of equal entries gives NaNs
+ *   y              [rows x ld_y] of y_dtype; may be x (same type and leading dimension)
+ *   mean, rstd     float [rows], written: what the backward pass reads
+ *
+ * The row is summed twice, the squares of x - mean after its mean is known; sums, mean and rstd are fp32.
+ * Elements behind D of a row are neither read into the result nor written. A NaN or an infinity in a row makes
+ * that row NaN; rows whose squares leave fp32's range (entries of about 1e19) come out as zeros times w plus b.
+ * A row's results do not depend on the other rows.
+ */
+rl_status rl_layer_norm_fwd(const void* x, rl_dtype x_dtype, int64_t rows, int64_t D, int64_t ld_x, const void* weight,
+                            const void* bias, rl_dtype w_dtype, float eps, void* y, rl_dtype y_dtype, int64_t ld_y,
+                            float* mean, float* rstd, rl_stream_t stream);
+
+/* Workspace bytes of rl_layer_norm_bwd (0 for sizes that it refuses): the parts of the columns' sums. */
+size_t rl_layer_norm_workspace_size(int64_t rows, int64_t D);
+
+/*
+ * The gradients of rl_layer_norm_fwd. With h = (x - mean) rstd and g = dy w, per row
+ *
+ *   dx = rstd (g - sum g / D - h (sum g h) / D),   and over the rows   dw += sum dy h,   db += sum dy.
+ *
+ *   d_y            [rows x ld_dy] of dy_dtype
+ *   x, mean, rstd  as given to and written by rl_layer_norm_fwd
+ *   weight         as for rl_layer_norm_fwd
+ *   mask           uint8 [rows] or NULL (all): rows with 0 have no gradient; d_y and x of such a row are not read
+ *                  and its d_x is zero (the loss mask: the fused head's d_hidden is zero there)
+ *   d_x            [rows x ld_dx] of x_dtype, written; may be d_y or x (same type and leading dimension)
+ *   d_weight, d_bias  float [D] or NULL; the sums are ADDED to them
+ *   ws, ws_bytes   rl_layer_norm_workspace_size(rows, D) bytes, initialised by rl_workspace_init
+ *
+ * Sums are fp32; the columns' are added up in parts of the rows in a fixed order that depends on rows, D, the types
+ * and the alignment alone: repeated calls give the same bits.
+ */
+rl_status rl_layer_norm_bwd(const void* d_y, rl_dtype dy_dtype, int64_t ld_dy, const void* x, rl_dtype x_dtype, int64_t ld_x,
+                            int64_t rows, int64_t D, const void* weight, rl_dtype w_dtype, const float* mean,
+                            const float* rstd, const uint8_t* mask, void* d_x, int64_t ld_dx, float* d_weight,
+                            float* d_bias, void* ws, size_t ws_bytes, rl_stream_t stream);
+
+/*
+ * The embedding of tokens (no counterpart in the paper: the other end of the policy model, whose matrix is often
+ * that of the LM head): out_t = scale W[id_t].
+ *
+ *   token_ids      int32 [T]: an id outside [0, V) gives a row of zeros and sets RL_DEV_BAD_TOKEN
+ *   weight         [V x ld_w] of w_dtype, aligned to its elements
+ *   T, V, D        T >= 0 up to 2^30, V up to 2^31 - 2, D up to 2^20, at most 2^40 elements each; ld_w, ld_out >= D
+ *   scale          finite; the product is rounded once, to out_dtype
+ *   out            [T x ld_out] of out_dtype; elements behind D of a row are not written
+ *   ws, ws_bytes   any initialised workspace: its status word is used (256 bytes suffice)
+ */
+rl_status rl_embedding_fwd(const int32_t* token_ids, int64_t T, const void* weight, rl_dtype w_dtype, int64_t V, int64_t D,
+                           int64_t ld_w, float scale, void* out, rl_dtype out_dtype, int64_t ld_out, void* ws,
+                           size_t ws_bytes, rl_stream_t stream);
+
+/* Workspace bytes of rl_embedding_bwd (0 for sizes that it refuses): the tokens sorted by id (16 bytes each), and
+ * the parts of the sums of ids that come often (D / 8 to D / 2 bytes per token). */
+size_t rl_embedding_workspace_size(int64_t T, int64_t V, int64_t D);
+
+/*
+ * The gradient of rl_embedding_fwd, added to d_weight: d_weight[v] += scale sum over the tokens t with id_t = v of d_t.
+ * d_weight may be the one that rl_fused_head_loss_fwd_bwd adds to (a tied head).
+ *
+ *   token_ids      int32 [T]: tokens with an id outside [0, V) are left out (their d_out is not read) and set
+ *                  RL_DEV_BAD_TOKEN
+ *   d_out          [T x ld_d] of d_dtype, aligned to its elements
+ *   T, V, D        as for rl_embedding_fwd
+ *   d_weight       float [V x D]; rows that no token names are not touched
+ *   ws, ws_bytes   rl_embedding_workspace_size(T, V, D) bytes, initialised by rl_workspace_init
+ *
+ * The tokens are sorted by id; each sum is fp32, of the tokens of an id in their order, in parts that depend on the
+ * ids and T alone, and is added to d_weight once: repeated calls give the same bits.
+ */
+rl_status rl_embedding_bwd(const int32_t* token_ids, int64_t T, const void* d_out, rl_dtype d_dtype, int64_t ld_d, int64_t V,
+                           int64_t D, float scale, float* d_weight, void* ws, size_t ws_bytes, rl_stream_t stream);
 
 #ifdef __cplusplus
 }

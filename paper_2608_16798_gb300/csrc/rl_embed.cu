@@ -1,0 +1,641 @@
+// The embedding of tokens, scaled, and its gradient.
+//
+//   out_t = scale W[id_t];      dW[v] += scale sum over the tokens t with id_t = v, in token order, of d_t
+//
+// The gradient's sums want the tokens of a row of W side by side: the tokens are sorted by id, stably (a radix sort in
+// digits of up to 9 bits), the sorted list is cut into chunks of equal length whatever the ids, and a chunk's threads,
+// a few columns each, go down its tokens. A run of equal ids that lies in one chunk is added to dW there; the parts of
+// one that crosses a border go to the workspace and are added up in order afterwards, so that a token that comes very
+// often is shared by as many CTAs as it has chunks. Every element of dW gets one addition per call, and the order of all
+// sums depends on the ids alone: repeated calls give the same bits.
+#include <algorithm>
+#include <cmath>
+#include <string>
+
+#include "rl_device.cuh"
+#include "rl_host.h"
+
+namespace rl {
+namespace embed {
+
+// N elements as floats, from memory aligned for them.
+template <typename T, int N>
+struct Block;
+template <>
+struct Block<uint16_t, 8> {
+  uint4 w;
+  __device__ __forceinline__ void load(const uint16_t* p) { w = __ldcs(reinterpret_cast<const uint4*>(p)); }
+  __device__ __forceinline__ void clear() { w = make_uint4(0, 0, 0, 0); }
+  __device__ __forceinline__ void get(float (&v)[8]) const {
+    v[0] = bf16_lo(w.x), v[1] = bf16_hi(w.x), v[2] = bf16_lo(w.y), v[3] = bf16_hi(w.y);
+    v[4] = bf16_lo(w.z), v[5] = bf16_hi(w.z), v[6] = bf16_lo(w.w), v[7] = bf16_hi(w.w);
+  }
+};
+template <>
+struct Block<float, 4> {
+  float4 w;
+  __device__ __forceinline__ void load(const float* p) { w = __ldcs(reinterpret_cast<const float4*>(p)); }
+  __device__ __forceinline__ void clear() { w = make_float4(0.f, 0.f, 0.f, 0.f); }
+  __device__ __forceinline__ void get(float (&v)[4]) const { v[0] = w.x, v[1] = w.y, v[2] = w.z, v[3] = w.w; }
+};
+template <>
+struct Block<uint16_t, 1> {
+  uint16_t w;
+  __device__ __forceinline__ void load(const uint16_t* p) { w = __ldcs(p); }
+  __device__ __forceinline__ void clear() { w = 0; }
+  __device__ __forceinline__ void get(float (&v)[1]) const { v[0] = bf16_to_f32(w); }
+};
+template <>
+struct Block<float, 1> {
+  float w;
+  __device__ __forceinline__ void load(const float* p) { w = __ldcs(p); }
+  __device__ __forceinline__ void clear() { w = 0.f; }
+  __device__ __forceinline__ void get(float (&v)[1]) const { v[0] = w; }
+};
+
+// ---------------------------------------------------------------- forward
+
+struct FwdArgs {
+  const int32_t* ids;
+  const void* w;
+  void* out;
+  int64_t T, D, ld_w, ld_out;
+  int32_t V;
+  float scale;
+  int32_t* status;
+};
+
+constexpr int kFwdWarps = 8;
+constexpr int kFwdElems = 32;  // elements per lane: a warp takes 1,024 columns of a token
+
+__device__ __forceinline__ uint32_t pack(float a, float b) { return pack_bf16x2(a, b); }
+
+// V8: rows of both matrices begin on 16-byte boundaries and D is a multiple of 8.
+template <typename TW, typename TO, bool V8>
+__global__ void __launch_bounds__(kFwdWarps * 32) lookup_kernel(const FwdArgs p) {
+  const int lane = threadIdx.x & 31;
+  const int64_t t = static_cast<int64_t>(blockIdx.x) * kFwdWarps + threadIdx.x / 32;
+  if (t >= p.T) return;
+  const int32_t id = p.ids[t];
+  const bool ok = id >= 0 && id < p.V;
+  if (!ok && lane == 0 && blockIdx.y == 0) flag_status(p.status, RL_DEV_BAD_TOKEN);
+  const TW* w = static_cast<const TW*>(p.w) + (ok ? id : 0) * p.ld_w;
+  TO* out = static_cast<TO*>(p.out) + t * p.ld_out;
+  const int64_t c0 = static_cast<int64_t>(blockIdx.y) * (32 * kFwdElems);
+  if (V8) {
+    constexpr int N = kFwdElems / 8;
+    float v[N][8];
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const int64_t c = c0 + (j * 32 + lane) * 8;
+      if (c < p.D && ok) {
+        if (sizeof(TW) == 2) {
+          const uint4 q = *reinterpret_cast<const uint4*>(w + c);
+          v[j][0] = bf16_lo(q.x), v[j][1] = bf16_hi(q.x), v[j][2] = bf16_lo(q.y), v[j][3] = bf16_hi(q.y);
+          v[j][4] = bf16_lo(q.z), v[j][5] = bf16_hi(q.z), v[j][6] = bf16_lo(q.w), v[j][7] = bf16_hi(q.w);
+        } else {
+          const float4 a = *reinterpret_cast<const float4*>(w + c), b = *reinterpret_cast<const float4*>(w + c + 4);
+          v[j][0] = a.x, v[j][1] = a.y, v[j][2] = a.z, v[j][3] = a.w;
+          v[j][4] = b.x, v[j][5] = b.y, v[j][6] = b.z, v[j][7] = b.w;
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[j][e] = 0.f;
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const int64_t c = c0 + (j * 32 + lane) * 8;
+      if (c >= p.D) continue;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[j][e] *= p.scale;
+      if (sizeof(TO) == 2) {
+        __stcs(reinterpret_cast<uint4*>(out + c), make_uint4(pack(v[j][0], v[j][1]), pack(v[j][2], v[j][3]),
+                                                             pack(v[j][4], v[j][5]), pack(v[j][6], v[j][7])));
+      } else {
+        __stcs(reinterpret_cast<float4*>(out + c), make_float4(v[j][0], v[j][1], v[j][2], v[j][3]));
+        __stcs(reinterpret_cast<float4*>(out + c + 4), make_float4(v[j][4], v[j][5], v[j][6], v[j][7]));
+      }
+    }
+  } else {
+#pragma unroll 8
+    for (int j = 0; j < kFwdElems; ++j) {
+      const int64_t c = c0 + j * 32 + lane;
+      if (c >= p.D) break;
+      float v = 0.f;
+      if (ok) v = sizeof(TW) == 2 ? bf16_to_f32(reinterpret_cast<const uint16_t*>(w)[c]) : reinterpret_cast<const float*>(w)[c];
+      v *= p.scale;
+      if (sizeof(TO) == 2) reinterpret_cast<uint16_t*>(out)[c] = f32_to_bf16(v);
+      else reinterpret_cast<float*>(out)[c] = v;
+    }
+  }
+}
+
+// ---------------------------------------------------------------- sorting the tokens by id
+
+constexpr int kSortThreads = 256, kSortWarps = kSortThreads / 32;
+constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits;
+constexpr int64_t kMostTiles = 4096;
+
+// What a sort is laid out for, from T and V alone.
+struct Plan {
+  int passes, bits;  // digits of `bits` bits
+  int64_t rounds;    // a tile is kSortThreads * rounds tokens
+  int64_t tiles;
+  int64_t chunk, chunks;
+  int64_t most_tiles, most_chunks;  // of any sort of up to T tokens: what the workspace has room for
+};
+
+struct SortArgs {
+  const int32_t* keys;  // nullptr: the ids of the first pass
+  const int32_t* ids;
+  const int32_t* toks;  // nullptr in the first pass: the token's own index
+  int32_t* keys_out;
+  int32_t* toks_out;
+  int64_t T, rounds, tiles;
+  int32_t V, shift, mask;
+  uint32_t* counts;  // [digits x tiles]
+  uint32_t* totals;  // [digits]
+  uint32_t* crossing;  // set to zero for the sums
+  int32_t* status;
+};
+
+// The key of position i: ids outside [0, V) become V and sort behind all others.
+__device__ __forceinline__ uint32_t key_at(const SortArgs& p, int64_t i) {
+  if (p.keys) return static_cast<uint32_t>(p.keys[i]);
+  const int32_t id = p.ids[i];
+  return static_cast<uint32_t>(id >= 0 && id < p.V ? id : p.V);
+}
+
+// How often each warp's part of the tile has each digit, in the order of the positions.
+__device__ __forceinline__ void count_tile(const SortArgs& p, uint32_t (&n)[kSortWarps][kDigits]) {
+  const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+  for (int i = threadIdx.x; i < kSortWarps * kDigits; i += kSortThreads) (&n[0][0])[i] = 0;
+  __syncthreads();
+  const int64_t first = (static_cast<int64_t>(blockIdx.x) * kSortWarps + warp) * p.rounds * 32;
+  for (int64_t k = 0; k < p.rounds; ++k) {
+    const int64_t i = first + k * 32 + lane;
+    const bool in = i < p.T;
+    const uint32_t live = __ballot_sync(0xffffffffu, in);
+    if (in) {
+      const uint32_t d = (key_at(p, i) >> p.shift) & p.mask;
+      const uint32_t peers = __match_any_sync(live, d);
+      if (lane == __ffs(peers) - 1) n[warp][d] += __popc(peers);
+    }
+    __syncwarp();
+  }
+  __syncthreads();
+}
+
+__global__ void __launch_bounds__(kSortThreads) count_kernel(const SortArgs p) {
+  __shared__ uint32_t n[kSortWarps][kDigits];
+  count_tile(p, n);
+  for (int d = threadIdx.x; d <= p.mask; d += kSortThreads) {
+    uint32_t s = 0;
+#pragma unroll
+    for (int w = 0; w < kSortWarps; ++w) s += n[w][d];
+    p.counts[d * p.tiles + blockIdx.x] = s;
+  }
+  if (p.keys) return;
+  bool bad = false;
+  const int64_t first = static_cast<int64_t>(blockIdx.x) * kSortThreads * p.rounds;
+  for (int64_t i = first + threadIdx.x; i < min(p.T, first + kSortThreads * p.rounds); i += kSortThreads)
+    bad |= p.ids[i] < 0 || p.ids[i] >= p.V;
+  if (bad) flag_status(p.status, RL_DEV_BAD_TOKEN);
+}
+
+// Per digit (a warp each) the tiles' counts become the sums of the tiles before, and the total.
+__global__ void __launch_bounds__(kSortThreads) prefix_kernel(const SortArgs p) {
+  const int d = blockIdx.x * kSortWarps + threadIdx.x / 32, lane = threadIdx.x & 31;
+  if (d > p.mask) return;
+  uint32_t* c = p.counts + d * p.tiles;
+  uint32_t run = 0;
+  for (int64_t k = 0; k < p.tiles; k += 32) {
+    const uint32_t mine = k + lane < p.tiles ? c[k + lane] : 0;
+    uint32_t s = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t v = __shfl_up_sync(0xffffffffu, s, o);
+      if (lane >= o) s += v;
+    }
+    if (k + lane < p.tiles) c[k + lane] = run + s - mine;
+    run += __shfl_sync(0xffffffffu, s, 31);
+  }
+  if (lane == 0) p.totals[d] = run;
+  if (d == 0 && lane == 0) *p.crossing = 0;
+}
+
+__global__ void __launch_bounds__(kSortThreads) scatter_kernel(const SortArgs p) {
+  __shared__ uint32_t n[kSortWarps][kDigits];
+  __shared__ uint32_t sums[kSortWarps];
+  count_tile(p, n);
+  const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+  // where each digit begins: the totals of the lower ones, two digits a thread
+  const int d0 = 2 * threadIdx.x;
+  const uint32_t a = d0 <= p.mask ? p.totals[d0] : 0, b = d0 + 1 <= p.mask ? p.totals[d0 + 1] : 0;
+  uint32_t s = a + b;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint32_t v = __shfl_up_sync(0xffffffffu, s, o);
+    if (lane >= o) s += v;
+  }
+  if (lane == 31) sums[warp] = s;
+  __syncthreads();
+  uint32_t before = s - a - b;
+  for (int w = 0; w < warp; ++w) before += sums[w];
+  // and within it this tile's, and within that each warp's
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const int d = d0 + e;
+    if (d > p.mask) break;
+    uint32_t at = before + (e ? a : 0) + p.counts[d * p.tiles + blockIdx.x];
+#pragma unroll
+    for (int w = 0; w < kSortWarps; ++w) {
+      const uint32_t c = n[w][d];
+      n[w][d] = at;
+      at += c;
+    }
+  }
+  __syncthreads();
+  const int64_t first = (static_cast<int64_t>(blockIdx.x) * kSortWarps + warp) * p.rounds * 32;
+  for (int64_t k = 0; k < p.rounds; ++k) {
+    const int64_t i = first + k * 32 + lane;
+    const bool in = i < p.T;
+    const uint32_t live = __ballot_sync(0xffffffffu, in);
+    if (in) {
+      const uint32_t key = key_at(p, i), d = (key >> p.shift) & p.mask;
+      const uint32_t peers = __match_any_sync(live, d);
+      const uint32_t at = n[warp][d] + __popc(peers & ((1u << lane) - 1));
+      __syncwarp(live);
+      if (lane == __ffs(peers) - 1) n[warp][d] += __popc(peers);
+      p.keys_out[at] = static_cast<int32_t>(key);
+      p.toks_out[at] = p.toks ? p.toks[i] : static_cast<int32_t>(i);
+    }
+    __syncwarp();
+  }
+}
+
+// ---------------------------------------------------------------- the sums
+
+struct SumArgs {
+  const int32_t* keys;  // sorted
+  const int32_t* toks;
+  const void* d;
+  float* dw;
+  float* head;  // [chunks x D]: the part of a run that came in from the chunk before
+  float* tail;  // [chunks x D]: the part of a run that goes on into the next chunk
+  int32_t* list;       // the chunks in which a run begins that goes on into the next one, in any order
+  uint32_t* crossing;  // how many there are
+  int64_t T, D, ld, chunk, chunks;
+  int32_t V;
+  float scale;
+};
+
+constexpr int kSumThreads = 128;
+constexpr int kMostChunk = 64;
+constexpr int kAhead = 4;  // rows in flight
+
+// N columns a thread, CX threads along a row, kSumThreads / CX chunks a CTA.
+template <typename T, int N, int CX>
+__global__ void __launch_bounds__(kSumThreads) sum_kernel(const SumArgs p) {
+  constexpr int kChunks = kSumThreads / CX;
+  __shared__ int32_t key[kChunks][kMostChunk + 2];  // with one neighbour on either side (-1: none)
+  __shared__ int32_t tok[kChunks][kMostChunk];
+  const int y = threadIdx.x / CX, x = threadIdx.x % CX;
+  const int64_t ch = static_cast<int64_t>(blockIdx.x) * kChunks + y;
+  const int64_t a = ch * p.chunk;
+  const int n = static_cast<int>(max(int64_t(0), min(p.chunk, p.T - a)));
+  for (int i = x; i < n + 2; i += CX) {
+    const int64_t at = a + i - 1;
+    key[y][i] = n > 0 && at >= 0 && at < p.T ? p.keys[at] : -1;
+  }
+  for (int i = x; i < n; i += CX) tok[y][i] = p.toks[a + i];
+  __syncthreads();
+  const int64_t c = (static_cast<int64_t>(blockIdx.y) * CX + x) * N;
+  if (c >= p.D || n <= 0) return;
+  const T* d = static_cast<const T*>(p.d) + c;
+  float acc[N];
+#pragma unroll
+  for (int e = 0; e < N; ++e) acc[e] = 0.f;
+  bool came_in = key[y][0] == key[y][1];  // the run began in the chunk before
+  for (int i = 0; i < n; i += kAhead) {
+    Block<T, N> rows[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      rows[k].clear();
+      if (i + k < n && key[y][i + k + 1] < p.V) rows[k].load(d + tok[y][i + k] * p.ld);
+    }
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      if (i + k >= n) break;
+      const int32_t v = key[y][i + k + 1];
+      if (v >= p.V) return;  // ids out of range: the last of the list
+      float f[N];
+      rows[k].get(f);
+#pragma unroll
+      for (int e = 0; e < N; ++e) acc[e] += f[e];
+      if (key[y][i + k + 2] == v && i + k + 1 < n) continue;
+      const bool goes_on = key[y][i + k + 2] == v;
+      if (goes_on && !came_in && c == 0) p.list[atomicAdd(p.crossing, 1u)] = static_cast<int32_t>(ch);
+      if (came_in || goes_on) {
+        float* to = (came_in ? p.head : p.tail) + ch * p.D + c;
+#pragma unroll
+        for (int e = 0; e < N; ++e) to[e] = acc[e];
+      } else {
+        float* to = p.dw + v * p.D + c;
+#pragma unroll
+        for (int e = 0; e < N; ++e) to[e] = fmaf(p.scale, acc[e], to[e]);
+      }
+#pragma unroll
+      for (int e = 0; e < N; ++e) acc[e] = 0.f;
+      came_in = false;
+    }
+  }
+}
+
+constexpr int kJoinWarps = 8;
+constexpr int kJoinCtas = 4 * 152;
+
+// The chunk after `ch` in which the run of v that goes on into chunk ch + 1 ends, by a whole warp.
+__device__ __forceinline__ int64_t last_chunk(const SumArgs& p, int64_t ch, int32_t v, int lane) {
+  for (int64_t k = ch + 1;; k += 32) {
+    const int64_t next = (k + lane + 1) * p.chunk;
+    const uint32_t ends = __ballot_sync(0xffffffffu, next >= p.T || p.keys[next] != v);
+    if (ends) return k + __ffs(ends) - 1;
+  }
+}
+
+// The runs that cross chunks. An item is one of them and kJoinWarps * 32 * N columns: a warp each takes 32 * N of them, or
+// where the run is long all warps take a part of its chunks, slice after slice, and the parts are added up in order.
+template <int N>
+__global__ void __launch_bounds__(kJoinWarps * 32) join_kernel(const SumArgs p) {
+  __shared__ float sum[kJoinWarps][32 * N];
+  const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+  constexpr int kSlice = 32 * N;
+  const int64_t groups = (p.D + kJoinWarps * kSlice - 1) / (kJoinWarps * kSlice);
+  const int64_t items = *p.crossing * groups;
+  for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
+    const int64_t ch = p.list[it / groups], first = it % groups * kJoinWarps;
+    const int32_t v = p.keys[(ch + 1) * p.chunk];
+    const int64_t last = last_chunk(p, ch, v, lane);
+    auto add = [&](float (&s)[N], const float* from) {
+      float f[N];
+      Block<float, N> b;
+      b.load(from);
+      b.get(f);
+#pragma unroll
+      for (int e = 0; e < N; ++e) s[e] += f[e];
+    };
+    auto finish = [&](const float (&s)[N], int64_t c) {
+      float* out = p.dw + v * p.D + c;
+#pragma unroll
+      for (int e = 0; e < N; ++e) out[e] = fmaf(p.scale, s[e], out[e]);
+    };
+    if (last - ch <= kJoinWarps) {
+      const int64_t c = (first + warp) * kSlice + lane * N;
+      if (c >= p.D) continue;
+      float s[N] = {};
+      add(s, p.tail + ch * p.D + c);
+#pragma unroll 4
+      for (int64_t k = ch + 1; k <= last; ++k) add(s, p.head + k * p.D + c);
+      finish(s, c);
+      continue;
+    }
+    const int64_t per = (last - ch + kJoinWarps - 1) / kJoinWarps;
+    const int64_t from = ch + 1 + warp * per, to = min(from + per, last + 1);
+    for (int64_t slice = first; slice < first + kJoinWarps && slice * kSlice < p.D; ++slice) {
+      const int64_t c = slice * kSlice + lane * N;
+      float s[N] = {};
+      if (c < p.D) {
+        if (warp == 0) add(s, p.tail + ch * p.D + c);
+#pragma unroll 8
+        for (int64_t k = from; k < to; ++k) add(s, p.head + k * p.D + c);
+      }
+#pragma unroll
+      for (int e = 0; e < N; ++e) sum[warp][lane * N + e] = s[e];
+      __syncthreads();
+      if (warp == 0 && c < p.D) {
+#pragma unroll
+        for (int w = 1; w < kJoinWarps; ++w)
+#pragma unroll
+          for (int e = 0; e < N; ++e) s[e] += sum[w][lane * N + e];
+        finish(s, c);
+      }
+      __syncthreads();
+    }
+  }
+}
+
+// ---------------------------------------------------------------- host
+
+constexpr int64_t kMostT = int64_t(1) << 30, kMostV = (int64_t(1) << 31) - 2, kMostD = 1 << 20;
+
+Plan plan(int64_t T, int64_t V) {
+  Plan q;
+  int bits = 1;
+  while ((V >> bits) != 0) ++bits;  // keys up to V itself
+  q.passes = (bits + kDigitBits - 1) / kDigitBits;
+  q.bits = (bits + q.passes - 1) / q.passes;
+  q.rounds = std::max<int64_t>(4, (T + kSortThreads * kMostTiles - 1) / (kSortThreads * kMostTiles));
+  const int64_t tile = kSortThreads * q.rounds;
+  q.tiles = std::max<int64_t>(1, (T + tile - 1) / tile);
+  q.chunk = T <= 4096 ? 16 : T <= 65536 ? 32 : 64;
+  q.chunks = (T + q.chunk - 1) / q.chunk;
+  q.most_tiles = std::min<int64_t>(kMostTiles, (T + kSortThreads * 4 - 1) / (kSortThreads * 4));
+  q.most_chunks = std::max<int64_t>(
+      {(std::min<int64_t>(T, 4096) + 15) / 16, (std::min<int64_t>(T, 65536) + 31) / 32, (T + 63) / 64});
+  return q;
+}
+
+inline size_t up(size_t n) { return (n + 255) / 256 * 256; }
+
+struct Layout {
+  size_t keys[2], toks[2], counts, totals, list, crossing, head, tail, bytes;
+};
+Layout layout(const Plan& q, int64_t T, int64_t D) {
+  Layout l;
+  size_t at = kWsHeader;
+  auto take = [&](size_t n) {
+    const size_t o = at;
+    at += up(n);
+    return o;
+  };
+  for (int i = 0; i < 2; ++i) {
+    l.keys[i] = take(size_t(T) * 4);
+    l.toks[i] = take(size_t(T) * 4);
+  }
+  l.counts = take(size_t(q.most_tiles) * kDigits * 4);
+  l.totals = take(kDigits * 4);
+  l.crossing = take(4);
+  l.list = take(size_t(q.most_chunks) * 4);
+  l.head = take(size_t(q.most_chunks) * D * 4);
+  l.tail = take(size_t(q.most_chunks) * D * 4);
+  l.bytes = at;
+  return l;
+}
+
+rl_status check_sizes(const std::string& f, int64_t T, int64_t V, int64_t D) {
+  if (T < 0 || V < 1 || D < 1) return set_error(RL_ERR_INVALID_ARG, f + "bad size");
+  if (T > kMostT || V > kMostV || D > kMostD || V > (int64_t(1) << 40) / D || T > (int64_t(1) << 40) / D)
+    return set_error(RL_ERR_UNSUPPORTED, f + "at most 2^30 tokens, 2^31 - 2 rows, 2^20 columns and 2^40 elements");
+  return RL_OK;
+}
+inline bool element_aligned(const void* p, rl_dtype t) {
+  return reinterpret_cast<uintptr_t>(p) % (t == RL_BF16 ? 2 : 4) == 0;
+}
+inline bool whole_blocks(const void* p, int64_t ld, size_t es) { return aligned16(p) && ld * es % 16 == 0; }
+
+template <typename TW, typename TO>
+rl_status forward(const FwdArgs& a, cudaStream_t s) {
+  const dim3 grid(static_cast<unsigned>((a.T + kFwdWarps - 1) / kFwdWarps),
+                  static_cast<unsigned>((a.D + 32 * kFwdElems - 1) / (32 * kFwdElems)));
+  if (a.D % 8 == 0 && whole_blocks(a.w, a.ld_w, sizeof(TW)) && whole_blocks(a.out, a.ld_out, sizeof(TO)))
+    lookup_kernel<TW, TO, true><<<grid, kFwdWarps * 32, 0, s>>>(a);
+  else
+    lookup_kernel<TW, TO, false><<<grid, kFwdWarps * 32, 0, s>>>(a);
+  const cudaError_t e = cudaGetLastError();
+  return e == cudaSuccess ? RL_OK : cuda_error(e, "lookup_kernel launch");
+}
+
+template <typename T, int N>
+void launch_sums(const SumArgs& a, cudaStream_t s) {
+  const int64_t threads = (a.D + N - 1) / N;
+  auto go = [&](auto kern, int cx) {
+    const int64_t per = kSumThreads / cx;
+    kern<<<dim3(static_cast<unsigned>((a.chunks + per - 1) / per), static_cast<unsigned>((threads + cx - 1) / cx)),
+           kSumThreads, 0, s>>>(a);
+  };
+  if (threads > 64) go(sum_kernel<T, N, 128>, 128);
+  else if (threads > 32) go(sum_kernel<T, N, 64>, 64);
+  else if (threads > 16) go(sum_kernel<T, N, 32>, 32);
+  else go(sum_kernel<T, N, 16>, 16);
+}
+
+template <typename T>
+rl_status backward(SumArgs& a, cudaStream_t s) {
+  constexpr int N = 16 / sizeof(T);
+  const bool blocks = a.D % N == 0 && whole_blocks(a.d, a.ld, sizeof(T)) && aligned16(a.dw);
+  if (blocks) launch_sums<T, N>(a, s);
+  else launch_sums<T, 1>(a, s);
+  cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) return cuda_error(e, "sum_kernel launch");
+  if (a.chunks > 1) {
+    if (blocks) join_kernel<4><<<kJoinCtas, kJoinWarps * 32, 0, s>>>(a);
+    else join_kernel<1><<<kJoinCtas, kJoinWarps * 32, 0, s>>>(a);
+    e = cudaGetLastError();
+    if (e != cudaSuccess) return cuda_error(e, "join_kernel launch");
+  }
+  return RL_OK;
+}
+
+}  // namespace embed
+}  // namespace rl
+
+extern "C" {
+
+rl_status rl_embedding_fwd(const int32_t* token_ids, int64_t T, const void* weight, rl_dtype w_dtype, int64_t V, int64_t D,
+                           int64_t ld_w, float scale, void* out, rl_dtype out_dtype, int64_t ld_out, void* ws,
+                           size_t ws_bytes, rl_stream_t stream) {
+  using namespace rl;
+  clear_error();
+  const std::string f = "rl_embedding_fwd: ";
+  const rl_status st = embed::check_sizes(f, T, V, D);
+  if (st != RL_OK) return st;
+  if ((w_dtype != RL_BF16 && w_dtype != RL_F32) || (out_dtype != RL_BF16 && out_dtype != RL_F32))
+    return set_error(RL_ERR_INVALID_ARG, f + "bad dtype");
+  if (ld_w < D || ld_out < D) return set_error(RL_ERR_INVALID_ARG, f + "a leading dimension is below D");
+  if (!std::isfinite(scale)) return set_error(RL_ERR_INVALID_ARG, f + "scale is not finite");
+  if (T == 0) return RL_OK;
+  if (!token_ids || !weight || !out || !ws) return set_error(RL_ERR_INVALID_ARG, f + "a required pointer is NULL");
+  if (!embed::element_aligned(weight, w_dtype) || !embed::element_aligned(out, out_dtype) || !aligned16(ws))
+    return set_error(RL_ERR_ALIGNMENT, f + "matrices must be aligned to their elements and ws to 16 bytes");
+  if (ws_bytes < kWsHeader) return set_error(RL_ERR_WORKSPACE_TOO_SMALL, f + "workspace smaller than its header");
+  embed::FwdArgs a = {};
+  a.ids = token_ids;
+  a.w = weight;
+  a.out = out;
+  a.T = T;
+  a.D = D;
+  a.ld_w = ld_w;
+  a.ld_out = ld_out;
+  a.V = static_cast<int32_t>(V);
+  a.scale = scale;
+  a.status = static_cast<int32_t*>(ws);
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  if (w_dtype == RL_BF16)
+    return out_dtype == RL_BF16 ? embed::forward<uint16_t, uint16_t>(a, s) : embed::forward<uint16_t, float>(a, s);
+  return out_dtype == RL_BF16 ? embed::forward<float, uint16_t>(a, s) : embed::forward<float, float>(a, s);
+}
+
+size_t rl_embedding_workspace_size(int64_t T, int64_t V, int64_t D) {
+  using namespace rl;
+  clear_error();
+  if (embed::check_sizes("rl_embedding_workspace_size: ", T, V, D) != RL_OK) return 0;
+  return embed::layout(embed::plan(T, V), T, D).bytes;
+}
+
+rl_status rl_embedding_bwd(const int32_t* token_ids, int64_t T, const void* d_out, rl_dtype d_dtype, int64_t ld_d, int64_t V,
+                           int64_t D, float scale, float* d_weight, void* ws, size_t ws_bytes, rl_stream_t stream) {
+  using namespace rl;
+  clear_error();
+  const std::string f = "rl_embedding_bwd: ";
+  const rl_status st = embed::check_sizes(f, T, V, D);
+  if (st != RL_OK) return st;
+  if (d_dtype != RL_BF16 && d_dtype != RL_F32) return set_error(RL_ERR_INVALID_ARG, f + "bad dtype");
+  if (ld_d < D) return set_error(RL_ERR_INVALID_ARG, f + "the leading dimension is below D");
+  if (!std::isfinite(scale)) return set_error(RL_ERR_INVALID_ARG, f + "scale is not finite");
+  if (T == 0) return RL_OK;
+  if (!token_ids || !d_out || !d_weight || !ws) return set_error(RL_ERR_INVALID_ARG, f + "a required pointer is NULL");
+  if (!embed::element_aligned(d_out, d_dtype) || !embed::element_aligned(d_weight, RL_F32) || !aligned16(ws))
+    return set_error(RL_ERR_ALIGNMENT, f + "matrices must be aligned to their elements and ws to 16 bytes");
+  const embed::Plan q = embed::plan(T, V);
+  const embed::Layout l = embed::layout(q, T, D);
+  if (ws_bytes < l.bytes)
+    return set_error(RL_ERR_WORKSPACE_TOO_SMALL, f + "ws_bytes below rl_embedding_workspace_size(T, V, D)");
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  uint8_t* base = static_cast<uint8_t*>(ws);
+  auto ints = [&](size_t o) { return reinterpret_cast<int32_t*>(base + o); };
+  embed::SortArgs o = {};
+  o.ids = token_ids;
+  o.T = T;
+  o.rounds = q.rounds;
+  o.tiles = q.tiles;
+  o.V = static_cast<int32_t>(V);
+  o.mask = (1 << q.bits) - 1;
+  o.counts = reinterpret_cast<uint32_t*>(base + l.counts);
+  o.totals = reinterpret_cast<uint32_t*>(base + l.totals);
+  o.crossing = reinterpret_cast<uint32_t*>(base + l.crossing);
+  o.status = reinterpret_cast<int32_t*>(base);
+  const unsigned tiles = static_cast<unsigned>(q.tiles);
+  for (int i = 0; i < q.passes; ++i) {
+    o.shift = i * q.bits;
+    o.keys_out = ints(l.keys[i & 1]);
+    o.toks_out = ints(l.toks[i & 1]);
+    embed::count_kernel<<<tiles, embed::kSortThreads, 0, s>>>(o);
+    embed::prefix_kernel<<<(o.mask + embed::kSortWarps) / embed::kSortWarps, embed::kSortThreads, 0, s>>>(o);
+    embed::scatter_kernel<<<tiles, embed::kSortThreads, 0, s>>>(o);
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return cuda_error(e, "rl_embedding_bwd: sort launch");
+    o.keys = o.keys_out;
+    o.toks = o.toks_out;
+  }
+  embed::SumArgs a = {};
+  a.keys = o.keys;
+  a.toks = o.toks;
+  a.d = d_out;
+  a.dw = d_weight;
+  a.head = reinterpret_cast<float*>(base + l.head);
+  a.tail = reinterpret_cast<float*>(base + l.tail);
+  a.list = ints(l.list);
+  a.crossing = reinterpret_cast<uint32_t*>(base + l.crossing);
+  a.T = T;
+  a.D = D;
+  a.ld = ld_d;
+  a.chunk = q.chunk;
+  a.chunks = q.chunks;
+  a.V = static_cast<int32_t>(V);
+  a.scale = scale;
+  return d_dtype == RL_BF16 ? embed::backward<uint16_t>(a, s) : embed::backward<float>(a, s);
+}
+
+}  // extern "C"

@@ -58,6 +58,13 @@ EXPORTS = {
                                 _SZ, _P]),
     "rl_muon_workspace_size": (_SZ, [_I32, _I64, _I64]),
     "rl_muon_update": (_I32, [_I32, _I64, _I64, _P, _I32, _I64, _I64, _P, _P, _P, _I64, _I64, _P, _P, _P, _SZ, _P]),
+    "rl_layer_norm_fwd": (_I32, [_P, _I32, _I64, _I64, _I64, _P, _P, _I32, _F, _P, _I32, _I64, _P, _P, _P]),
+    "rl_layer_norm_workspace_size": (_SZ, [_I64, _I64]),
+    "rl_layer_norm_bwd": (_I32, [_P, _I32, _I64, _P, _I32, _I64, _I64, _I64, _P, _I32, _P, _P, _P, _P, _I64, _P, _P, _P,
+                                 _SZ, _P]),
+    "rl_embedding_fwd": (_I32, [_P, _I64, _P, _I32, _I64, _I64, _I64, _F, _P, _I32, _I64, _P, _SZ, _P]),
+    "rl_embedding_workspace_size": (_SZ, [_I64, _I64, _I64]),
+    "rl_embedding_bwd": (_I32, [_P, _I64, _P, _I32, _I64, _I64, _I64, _F, _P, _P, _SZ, _P]),
 }
 
 
@@ -747,3 +754,140 @@ def rl_muon_update(grad, params: rl_muon_params, ws, momentum=None, weights=None
 
 def _refuse_dtype(name, t):
     raise ValueError(f"{name} must be bfloat16 or float32, got {t.dtype}")
+
+
+def _rows(t, name, shape, ix):
+    """(pointer, dtype code, leading dimension) of a matrix with unit stride along its rows (of `shape`, if given)."""
+    if t.dtype not in (torch.bfloat16, torch.float32):
+        _refuse_dtype(name, t)
+    if t.dim() != 2 or (shape is not None and tuple(t.shape) != shape):
+        raise ValueError(f"{name} must be a matrix{'' if shape is None else f' [{shape[0]}, {shape[1]}]'}, got {tuple(t.shape)}")
+    if not t.is_cuda or (ix is not None and t.get_device() != ix):
+        raise ValueError(f"{name} must be a CUDA tensor on the other arguments' device, got {t.device}")
+    rows, n = t.shape
+    if n > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name} must have unit stride along its rows")
+    ld = t.stride(0) if rows > 1 else n  # the stride of a single row says nothing
+    return t.data_ptr(), RL_BF16 if t.dtype == torch.bfloat16 else RL_F32, ld
+
+
+def _vector_pair(weight, bias, D, ix):
+    """(weight's pointer, bias' pointer, their dtype code) of a norm's parameters [D]."""
+    dt = None
+    for t, name in ((weight, "weight"), (bias, "bias")):
+        if t is None:
+            continue
+        if t.dtype not in (torch.bfloat16, torch.float32):
+            _refuse_dtype(name, t)
+        if t.numel() != D:
+            raise ValueError(f"{name} has {t.numel()} elements, needs {D}")
+        if dt is not None and t.dtype != dt:
+            raise ValueError("weight and bias must have the same dtype")
+        dt = t.dtype
+        _need(t, name, dt, D, index=ix)
+    return _ptr(weight), _ptr(bias), RL_BF16 if dt == torch.bfloat16 else RL_F32
+
+
+def rl_layer_norm_fwd(x, weight=None, bias=None, eps=1e-5, y=None, y_dtype=None, mean=None, rstd=None, stream=None):
+    """Layer norm of the rows of ``x`` ([rows, D], bf16 or float32, any row stride). ``weight`` and ``bias`` ([D],
+    both bf16 or both float32) may be None. ``y`` is created in ``y_dtype`` (default: that of ``x``) if not given; it
+    may be ``x``. Returns (y, mean, rstd), the last two float32 [rows]."""
+    p_x, dt_x, ld_x = _rows(x, "x", None, None)
+    rows, D = x.shape
+    ix = x.get_device()
+    y = torch.empty(rows, D, dtype=y_dtype or x.dtype, device=x.device) if y is None else y
+    p_y, dt_y, ld_y = _rows(y, "y", (rows, D), ix)
+    p_w, p_b, dt_w = _vector_pair(weight, bias, D, ix)
+    mean = torch.empty(rows, dtype=torch.float32, device=x.device) if mean is None else mean
+    rstd = torch.empty(rows, dtype=torch.float32, device=x.device) if rstd is None else rstd
+    p_mean = _need(mean, "mean", torch.float32, rows, index=ix)
+    p_rstd = _need(rstd, "rstd", torch.float32, rows, index=ix)
+    st = lib().rl_layer_norm_fwd(p_x, dt_x, rows, D, ld_x, p_w, p_b, dt_w, float(eps), p_y, dt_y, ld_y, p_mean, p_rstd,
+                                 _stream(stream))
+    _check("rl_layer_norm_fwd", st)
+    return y, mean, rstd
+
+
+def rl_layer_norm_workspace_size(rows: int, D: int) -> int:
+    return int(lib().rl_layer_norm_workspace_size(rows, D))
+
+
+def new_layer_norm_workspace(rows: int, D: int, device=None, stream=None) -> torch.Tensor:
+    """Allocate (with torch) and initialise a workspace of rl_layer_norm_bwd for matrices of this shape."""
+    return _new_sized_workspace("rl_layer_norm_workspace_size", rl_layer_norm_workspace_size(rows, D), device, stream)
+
+
+def _new_sized_workspace(fn, nbytes, device, stream):
+    if nbytes == 0:
+        raise RLError(fn, 2, rl_last_error_message())
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=device or "cuda")
+    rl_workspace_init(ws, stream)
+    return ws
+
+
+def rl_layer_norm_bwd(d_y, x, mean, rstd, ws, weight=None, mask=None, d_x=None, d_weight=None, d_bias=None, stream=None):
+    """Gradients of rl_layer_norm_fwd: writes ``d_x`` (created if not given; of ``x``'s dtype; may be ``d_y`` or ``x``)
+    and ADDS the sums over the rows to ``d_weight`` and ``d_bias`` (float32 [D], either may be None). Rows with
+    ``mask`` (uint8 [rows]) 0 are not read and get a zero gradient. Returns d_x."""
+    p_x, dt_x, ld_x = _rows(x, "x", None, None)
+    rows, D = x.shape
+    ix = x.get_device()
+    p_dy, dt_dy, ld_dy = _rows(d_y, "d_y", (rows, D), ix)
+    d_x = torch.empty(rows, D, dtype=x.dtype, device=x.device) if d_x is None else d_x
+    p_dx, dt_dx, ld_dx = _rows(d_x, "d_x", (rows, D), ix)
+    if dt_dx != dt_x:
+        raise ValueError(f"d_x must have the dtype of x ({x.dtype}), got {d_x.dtype}")
+    p_w, _, dt_w = _vector_pair(weight, None, D, ix)
+    p_mean = _need(mean, "mean", torch.float32, rows, index=ix)
+    p_rstd = _need(rstd, "rstd", torch.float32, rows, index=ix)
+    p_mask = _opt(mask, "mask", torch.uint8, rows, index=ix)
+    p_dw = _opt(d_weight, "d_weight", torch.float32, D, index=ix)
+    p_db = _opt(d_bias, "d_bias", torch.float32, D, index=ix)
+    p_ws = _need(ws, "ws", torch.uint8, index=ix)
+    st = lib().rl_layer_norm_bwd(p_dy, dt_dy, ld_dy, p_x, dt_x, ld_x, rows, D, p_w, dt_w, p_mean, p_rstd, p_mask, p_dx,
+                                 ld_dx, p_dw, p_db, p_ws, ws.numel(), _stream(stream))
+    _check("rl_layer_norm_bwd", st)
+    return d_x
+
+
+def rl_embedding_fwd(token_ids, weight, ws, scale=1.0, out=None, out_dtype=None, stream=None):
+    """``scale`` times the rows of ``weight`` ([V, D], bf16 or float32, any row stride) that ``token_ids`` (int32 [T])
+    name. ``out`` ([T, D]) is created in ``out_dtype`` (default: that of ``weight``) if not given. Returns out."""
+    p_w, dt_w, ld_w = _rows(weight, "weight", None, None)
+    V, D = weight.shape
+    ix = weight.get_device()
+    T = token_ids.numel()
+    p_ids = _need(token_ids, "token_ids", torch.int32, index=ix)
+    out = torch.empty(T, D, dtype=out_dtype or weight.dtype, device=weight.device) if out is None else out
+    p_out, dt_out, ld_out = _rows(out, "out", (T, D), ix)
+    p_ws = _need(ws, "ws", torch.uint8, index=ix)
+    st = lib().rl_embedding_fwd(p_ids, T, p_w, dt_w, V, D, ld_w, float(scale), p_out, dt_out, ld_out, p_ws, ws.numel(),
+                                _stream(stream))
+    _check("rl_embedding_fwd", st)
+    return out
+
+
+def rl_embedding_workspace_size(T: int, V: int, D: int) -> int:
+    return int(lib().rl_embedding_workspace_size(T, V, D))
+
+
+def new_embedding_workspace(T: int, V: int, D: int, device=None, stream=None) -> torch.Tensor:
+    """Allocate (with torch) and initialise a workspace of rl_embedding_bwd for up to T tokens."""
+    return _new_sized_workspace("rl_embedding_workspace_size", rl_embedding_workspace_size(T, V, D), device, stream)
+
+
+def rl_embedding_bwd(token_ids, d_out, d_weight, ws, scale=1.0, stream=None):
+    """ADDS the gradient of rl_embedding_fwd to ``d_weight`` (float32 [V, D], contiguous): per row of it ``scale`` times
+    the sum of the rows of ``d_out`` ([T, D], bf16 or float32, any row stride) whose token names it. Returns d_weight."""
+    if d_weight.dim() != 2:
+        raise ValueError("d_weight must be a matrix [V, D]")
+    V, D = d_weight.shape
+    ix = d_weight.get_device()
+    T = token_ids.numel()
+    p_dw = _need(d_weight, "d_weight", torch.float32, V * D, index=ix)
+    p_d, dt_d, ld_d = _rows(d_out, "d_out", (T, D), ix)
+    p_ids = _need(token_ids, "token_ids", torch.int32, T, index=ix)
+    p_ws = _need(ws, "ws", torch.uint8, index=ix)
+    st = lib().rl_embedding_bwd(p_ids, T, p_d, dt_d, ld_d, V, D, float(scale), p_dw, p_ws, ws.numel(), _stream(stream))
+    _check("rl_embedding_bwd", st)
+    return d_weight
