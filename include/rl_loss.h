@@ -24,7 +24,7 @@
  *   - sequence-level importance weights (Sec. 3.2.4) and batch summaries of the
  *     per-token statistics (entropy, clip fraction; Sec. 4);
  *   - on either side of the loss, without a counterpart in the paper: the verification
- *     of drafted tokens (the rollout) and the orthogonalised weight update; the policy model's
+ *     of drafted tokens and the sampling of tokens (the rollout) and the orthogonalised weight update; the policy model's
  *     ends: the embedding of the tokens and the layer norm before the LM head, forward and
  *     backward;
  *   - a self-test of the failure path that every bounded device wait shares
@@ -93,7 +93,7 @@ enum {
   RL_DEV_BAD_OFFSETS = 4, /* group / trajectory offsets not non-decreasing within range */
   RL_DEV_TIMEOUT = 8,     /* a bounded wait for an asynchronous copy ran out */
   RL_DEV_BAD_VALUE = 16   /* a non-finite or out-of-range input value (rl_sequence_is_weights, rl_verify_drafts,
-                             rl_muon_update) */
+                             rl_muon_update, rl_sample_tokens) */
 };
 
 typedef struct rl_loss_params {
@@ -693,6 +693,51 @@ rl_status rl_muon_update(int32_t batch, int64_t m, int64_t n, const void* grad, 
                          int64_t ld_grad, int64_t stride_grad, float* momentum, float* weights,
                          uint16_t* weights_bf16, int64_t ld_w, int64_t stride_w, uint16_t* update,
                          const rl_muon_params* params, void* ws, size_t ws_bytes, rl_stream_t stream);
+
+/*
+ * The next token of every request from its logits row, by temperature, top-k, top-p and min-p, from given random
+ * numbers (the rollout engine's draw; the paper does not describe its sampling). With p = softmax(z / T) and the
+ * entries in the order of their size, the lower index first among equals:
+ *
+ *   top_k  (0: off)  keeps the first top_k;
+ *   top_p  (1: off)  keeps those before which less than top_p of the mass of what top_k keeps lies;
+ *   min_p  (0: off)  keeps those with p >= min_p max p;
+ *
+ * what all of them keep is kept, and always the first. The token is the lowest kept v at which the running sum of the
+ * kept p, in vocabulary order, passes sample_u times their total. T = 0 is greedy: the lowest index of the largest
+ * entry. Entries of -infinity are never kept.
+ */
+typedef struct rl_sample_params {
+  float temperature; /* T: 0 (greedy) or at least 1e-4 */
+  int32_t top_k;     /* >= 0 */
+  float top_p;       /* in (0, 1] */
+  float min_p;       /* in [0, 1] */
+} rl_sample_params;
+
+/*
+ *   logits         [rows x ld] of `dtype`, base 16-byte aligned
+ *   rows, V, ld    rows up to 2^26, 1 <= V <= ld; a row has to fit in the shared memory of 16 CTAs (1,638,000 bf16 or
+ *                  819,000 fp32 entries), else RL_ERR_UNSUPPORTED
+ *   sample_u       float [rows] in [0, 1)
+ *   params         host pointer: the settings of every row but for those given per row:
+ *   row_temperature, row_top_k, row_top_p, row_min_p   float / int32 / float / float [rows], each may be NULL
+ *   out_ids        int32 [rows]
+ *   out_logp       float [rows]: log p of the token (T = 0: of softmax(z)): with T = 1 the rollout_logp of
+ *                  rl_policy_loss_fwd_bwd
+ *   out_filtered_logp  float [rows] or NULL: log of its share of the kept tokens' mass (T = 0: 0)
+ *   n_kept         int32 [rows] or NULL: how many tokens are kept
+ *   ws, ws_bytes   any initialised workspace: its status word is used (256 bytes suffice)
+ *
+ * A row without a finite largest entry, or with a NaN, and one whose settings or number are outside the ranges above,
+ * gets token -1, NaN log-probabilities and n_kept 0 and sets RL_DEV_BAD_VALUE. Masses are sums of fp32 exponentials:
+ * where top_p ends, and which token u selects, is that of exact sums but for borders within 1e-6 of the mass; an entry's
+ * own exponential is relative 2^-22 and what the rounding of z / T makes of it. A row's results do not depend on the
+ * other rows.
+ */
+rl_status rl_sample_tokens(const void* logits, rl_dtype dtype, int64_t rows, int64_t V, int64_t ld, const float* sample_u,
+                           const rl_sample_params* params, const float* row_temperature, const int32_t* row_top_k,
+                           const float* row_top_p, const float* row_min_p, int32_t* out_ids, float* out_logp,
+                           float* out_filtered_logp, int32_t* n_kept, void* ws, size_t ws_bytes, rl_stream_t stream);
 
 /*
  * Layer norm of the rows of a matrix (no counterpart in the paper: the norm before the LM head, whose output

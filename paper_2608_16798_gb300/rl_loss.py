@@ -58,6 +58,7 @@ EXPORTS = {
                                 _SZ, _P]),
     "rl_muon_workspace_size": (_SZ, [_I32, _I64, _I64]),
     "rl_muon_update": (_I32, [_I32, _I64, _I64, _P, _I32, _I64, _I64, _P, _P, _P, _I64, _I64, _P, _P, _P, _SZ, _P]),
+    "rl_sample_tokens": (_I32, [_P, _I32, _I64, _I64, _I64, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _SZ, _P]),
     "rl_layer_norm_fwd": (_I32, [_P, _I32, _I64, _I64, _I64, _P, _P, _I32, _F, _P, _I32, _I64, _P, _P, _P]),
     "rl_layer_norm_workspace_size": (_SZ, [_I64, _I64]),
     "rl_layer_norm_bwd": (_I32, [_P, _I32, _I64, _P, _I32, _I64, _I64, _I64, _P, _I32, _P, _P, _P, _P, _I64, _P, _P, _P,
@@ -86,6 +87,14 @@ class rl_verify_params(ctypes.Structure):
 
 def make_verify_params(temperature=1.0) -> rl_verify_params:
     return rl_verify_params(temperature)
+
+
+class rl_sample_params(ctypes.Structure):
+    _fields_ = [("temperature", _F), ("top_k", _I32), ("top_p", _F), ("min_p", _F)]
+
+
+def make_sample_params(temperature=1.0, top_k=0, top_p=1.0, min_p=0.0) -> rl_sample_params:
+    return rl_sample_params(temperature, top_k, top_p, min_p)
 
 
 class rl_muon_params(ctypes.Structure):
@@ -690,6 +699,37 @@ def rl_verify_drafts(target_logits, draft_ids, draft_offsets, accept_u, sample_u
                                 p_out_logp, p_ws, ws.numel(), _stream(stream))
     _check("rl_verify_drafts", st)
     return out_ids, n_accepted, out_logp
+
+
+def rl_sample_tokens(logits, sample_u, params: rl_sample_params, ws, row_temperature=None, row_top_k=None, row_top_p=None,
+                     row_min_p=None, out_ids=None, out_logp=None, out_filtered_logp=None, n_kept=None, stream=None):
+    """The next token of every row of ``logits`` ([rows, V]) from the numbers ``sample_u`` (float32 [rows], in [0, 1)):
+    temperature, top-k, top-p and min-p of ``params``, or per row (float32, int32, float32, float32 [rows]). Returns
+    (out_ids, out_logp): the tokens (int32) and their log-probabilities under softmax(z / T). ``out_filtered_logp``
+    (float32 [rows]) and ``n_kept`` (int32 [rows]), if given, receive the log-probabilities among the kept tokens and
+    their number."""
+    rows, V, ld = _rows_view(logits)
+    dt = _logits_dtype(logits)
+    dev = logits.device
+    ix = logits.get_device()
+    if not logits.is_cuda:
+        raise ValueError("logits must be a CUDA tensor")
+    p_u = _need(sample_u, "sample_u", torch.float32, rows, index=ix)
+    p_t = _opt(row_temperature, "row_temperature", torch.float32, rows, index=ix)
+    p_k = _opt(row_top_k, "row_top_k", torch.int32, rows, index=ix)
+    p_p = _opt(row_top_p, "row_top_p", torch.float32, rows, index=ix)
+    p_m = _opt(row_min_p, "row_min_p", torch.float32, rows, index=ix)
+    out_ids = torch.empty(rows, dtype=torch.int32, device=dev) if out_ids is None else out_ids
+    out_logp = torch.empty(rows, dtype=torch.float32, device=dev) if out_logp is None else out_logp
+    p_ids = _need(out_ids, "out_ids", torch.int32, rows, index=ix)
+    p_logp = _need(out_logp, "out_logp", torch.float32, rows, index=ix)
+    p_f = _opt(out_filtered_logp, "out_filtered_logp", torch.float32, rows, index=ix)
+    p_n = _opt(n_kept, "n_kept", torch.int32, rows, index=ix)
+    p_ws = _need(ws, "ws", torch.uint8, index=ix)
+    st = lib().rl_sample_tokens(logits.data_ptr(), dt, rows, V, ld if rows > 1 else max(ld, V), p_u, ctypes.byref(params), p_t,
+                                p_k, p_p, p_m, p_ids, p_logp, p_f, p_n, p_ws, ws.numel(), _stream(stream))
+    _check("rl_sample_tokens", st)
+    return out_ids, out_logp
 
 
 def rl_muon_workspace_size(batch: int, m: int, n: int) -> int:
