@@ -6,6 +6,7 @@
 // The simple form: a CTA per row that reads it once for each of the sums, and for the columns' sums threads that go
 // down a part of the rows.
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <string>
 
@@ -130,131 +131,181 @@ __global__ void __launch_bounds__(kLoopThreads) loop_bwd_kernel(const BwdArgs p)
 
 // ---------------------------------------------------------------- forward, the row in registers
 
-// Eight elements from or to memory aligned for them (two blocks of four floats).
-__device__ __forceinline__ void load8(const uint16_t* p, float (&v)[8]) {
-  uint4 q;
-  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w) : "l"(p));
-  v[0] = bf16_lo(q.x), v[1] = bf16_hi(q.x), v[2] = bf16_lo(q.y), v[3] = bf16_hi(q.y);
-  v[4] = bf16_lo(q.z), v[5] = bf16_hi(q.z), v[6] = bf16_lo(q.w), v[7] = bf16_hi(q.w);
-}
-__device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
-  asm volatile("ld.global.L1::no_allocate.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "l"(p));
-  asm volatile("ld.global.L1::no_allocate.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]) : "l"(p + 4));
-}
-__device__ __forceinline__ void store8(uint16_t* p, const float (&v)[8]) {
-  __stcs(reinterpret_cast<uint4*>(p),
-         make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])));
-}
-__device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
-  __stcs(reinterpret_cast<float4*>(p), make_float4(v[0], v[1], v[2], v[3]));
-  __stcs(reinterpret_cast<float4*>(p + 4), make_float4(v[4], v[5], v[6], v[7]));
-}
-// Eight parameters (L1 keeps them for the next rows).
-__device__ __forceinline__ void load8(const Vec& w, int64_t c, float (&v)[8]) {
-  if (!w.at) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = w.none;
-  } else if (w.bf16) {
-    const uint4 q = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(w.at) + c));
-    v[0] = bf16_lo(q.x), v[1] = bf16_hi(q.x), v[2] = bf16_lo(q.y), v[3] = bf16_hi(q.y);
-    v[4] = bf16_lo(q.z), v[5] = bf16_hi(q.z), v[6] = bf16_lo(q.w), v[7] = bf16_hi(q.w);
-  } else {
-    const float4 a = __ldg(reinterpret_cast<const float4*>(static_cast<const float*>(w.at) + c));
-    const float4 b = __ldg(reinterpret_cast<const float4*>(static_cast<const float*>(w.at) + c + 4));
-    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+// Four elements as they lie in memory aligned for them: a warp's lanes side by side in either type, so that its requests
+// are whole lines. Loads come before the first use of any of them and are not under a condition: behind one each, or with
+// the conversion between them, they waited for one another (32,768 rows of 4,096: 185 us).
+template <typename T>
+struct Raw;
+template <>
+struct Raw<uint16_t> {
+  uint2 q;
+  __device__ __forceinline__ void get(float2 (&v)[2]) const {
+    v[0] = make_float2(bf16_lo(q.x), bf16_hi(q.x)), v[1] = make_float2(bf16_lo(q.y), bf16_hi(q.y));
   }
-}
+  __device__ __forceinline__ void stream(const uint16_t* p) { q = __ldcs(reinterpret_cast<const uint2*>(p)); }
+  __device__ __forceinline__ void shared(const uint16_t* p) { q = *reinterpret_cast<const uint2*>(p); }
+};
+template <>
+struct Raw<float> {
+  float4 q;
+  __device__ __forceinline__ void get(float2 (&v)[2]) const { v[0] = make_float2(q.x, q.y), v[1] = make_float2(q.z, q.w); }
+  __device__ __forceinline__ void stream(const float* p) { q = __ldcs(reinterpret_cast<const float4*>(p)); }
+  __device__ __forceinline__ void shared(const float* p) { q = *reinterpret_cast<const float4*>(p); }
+};
 
 constexpr int kMostWarps = 16;
 
-// The sum over a row's W warps, in every thread of them; `red` has a word per warp and is free again after the next sum.
+// The sum over a row's W warps, in every thread of them; `red` has kMostWarps words, zero behind the W-th, and is free again
+// after the next barrier.
 __device__ __forceinline__ float row_sum(float v, int W, int w, float* red) {
   v = warp_sum(v);
   if (W == 1) return v;
   if ((threadIdx.x & 31) == 0) red[w] = v;
   __syncthreads();
   float s = 0.f;
-  for (int i = 0; i < W; ++i) s += red[i];
+#pragma unroll
+  for (int i = 0; i < kMostWarps; i += 4) {
+    if (i >= W) break;
+    const float4 q = *reinterpret_cast<const float4*>(red + i);
+    s += (q.x + q.y) + (q.z + q.w);
+  }
   return s;
 }
 
-// A row on W warps (blockDim = 32 W, rows per CTA), NV * 8 elements a thread, held in registers between the two sums and
-// the result: x is read once. WHOLE: rows in 16-byte blocks, D a multiple of 8; else an element at a time.
-template <typename TX, typename TY, int NV, bool WHOLE>
+// 1 / sqrt(x), the fast one and a step of Newton's.
+__device__ __forceinline__ float inverse_root(float x) {
+  const float r = rsqrtf(x);
+  return x > 0.f && x < 3e38f ? r * fmaf(-0.5f * x * r, r, 1.5f) : r;
+}
+
+// The columns of thread t of n: blocks of four (WHOLE), or one apart.
+template <bool WHOLE>
+__device__ __forceinline__ int column_of(int j, int e, int n, int t) {
+  return WHOLE ? (j * n + t) * 4 + e : (j * 4 + e) * n + t;
+}
+
+// The statistics of a row whose elements v the threads hold, two columns a word; leaves x - mean in v, and 0 behind D.
+// Two passes over the registers: the squares are of x - mean.
+template <int NG, bool WHOLE>
+__device__ __forceinline__ void statistics(float2 (&v)[NG][2], int D, float inv, float eps, int W, int w, int n, int t, float* red0,
+                                           float* red1, float& mean, float& rstd) {
+  const bool full = D == 4 * NG * n;
+  auto clear = [&]() {
+    if (full) return;
+#pragma unroll
+    for (int j = 0; j < NG; ++j)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        if (column_of<WHOLE>(j, 2 * e, n, t) >= D) v[j][e].x = 0.f;
+        if (column_of<WHOLE>(j, 2 * e + 1, n, t) >= D) v[j][e].y = 0.f;
+      }
+  };
+  clear();
+  float2 s = make_float2(0.f, 0.f), q = s;
+#pragma unroll
+  for (int j = 0; j < NG; ++j)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) s = __fadd2_rn(s, v[j][e]);
+  const float sum = row_sum(s.x + s.y, W, w, red0), m0 = sum * inv;
+  mean = fmaf(fmaf(-m0, static_cast<float>(D), sum), inv, m0);  // the quotient, rounded once
+  const float2 off = make_float2(-mean, -mean);
+#pragma unroll
+  for (int j = 0; j < NG; ++j)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) v[j][e] = __fadd2_rn(v[j][e], off);
+  clear();
+#pragma unroll
+  for (int j = 0; j < NG; ++j)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) q = __ffma2_rn(v[j][e], v[j][e], q);
+  rstd = inverse_root(fmaf(row_sum(q.x + q.y, W, w, red1), inv, eps));
+}
+
+__device__ __forceinline__ void put4(uint16_t* p, float2 a, float2 b) {
+  __stcs(reinterpret_cast<uint2*>(p), make_uint2(pack_bf16x2(a.x, a.y), pack_bf16x2(b.x, b.y)));
+}
+__device__ __forceinline__ void put4(float* p, float2 a, float2 b) {
+  __stcs(reinterpret_cast<float4*>(p), make_float4(a.x, a.y, b.x, b.y));
+}
+// Writes a thread's elements of a row.
+template <int NG, bool WHOLE, typename T>
+__device__ __forceinline__ void put_row(T* row, const float2 (&v)[NG][2], int D, int n, int t) {
+#pragma unroll
+  for (int j = 0; j < NG; ++j) {
+    if (WHOLE) {
+      if (column_of<true>(j, 0, n, t) < D) put4(row + column_of<true>(j, 0, n, t), v[j][0], v[j][1]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int c0 = column_of<false>(j, 2 * e, n, t), c1 = column_of<false>(j, 2 * e + 1, n, t);
+        if (c0 < D) row[c0] = Io<T>::put(v[j][e].x);
+        if (c1 < D) row[c1] = Io<T>::put(v[j][e].y);
+      }
+    }
+  }
+}
+// A thread's parameters (`behind` behind D).
+template <int NG, bool WHOLE>
+__device__ __forceinline__ void get_parameters(float2 (&v)[NG][2], const Vec& w, float behind, int D, int n, int t) {
+#pragma unroll
+  for (int j = 0; j < NG; ++j)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int c0 = column_of<WHOLE>(j, 2 * e, n, t), c1 = column_of<WHOLE>(j, 2 * e + 1, n, t);
+      v[j][e] = make_float2(c0 < D ? w[c0] : behind, c1 < D ? w[c1] : behind);
+    }
+}
+
+// A row on W warps (blockDim = 32 W, rows per CTA), 4 NG elements a thread, held in registers between the two sums and
+// the result. For few rows: nothing is fetched ahead, and every thread has little to do.
+template <typename TX, typename TY, int NG, bool WHOLE>
 __global__ void __launch_bounds__(kMostWarps * 32) fwd_kernel(const FwdArgs p) {
-  __shared__ float red[2][kMostWarps];
+  __shared__ __align__(16) float red[2][kMostWarps];
   const int W = blockDim.x / 32, n = blockDim.x, t = threadIdx.x, w = t / 32;
   const int64_t r = static_cast<int64_t>(blockIdx.x) * blockDim.y + threadIdx.y;
   if (W == 1 && r >= p.rows) return;  // several rows a CTA: no barriers
+  if (W > 1 && t < 2 * kMostWarps && t % kMostWarps >= W) red[t / kMostWarps][t % kMostWarps] = 0.f;
   const TX* x = static_cast<const TX*>(p.x) + r * p.ld_x;
   TY* y = static_cast<TY*>(p.y) + r * p.ld_y;
   const int D = static_cast<int>(p.D);
-  float v[NV][8];
+  float2 v[NG][2];
+  if (WHOLE) {
+    Raw<TX> raw[NG];
 #pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    if (WHOLE) {
-      const int c = (j * n + t) * 8;
-      if (c < D) load8(x + c, v[j]);
-    } else {
+    for (int j = 0; j < NG; ++j) raw[j].stream(x + (column_of<true>(j, 0, n, t) < D ? column_of<true>(j, 0, n, t) : 0));
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int c = (j * 8 + e) * n + t;
-        if (c < D) v[j][e] = Io<TX>::get(__ldcs(x + c));
-      }
-    }
+    for (int j = 0; j < NG; ++j) raw[j].get(v[j]);
+  } else {
+    TX raw[NG][4];
+#pragma unroll
+    for (int j = 0; j < NG; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) raw[j][e] = __ldcs(x + (column_of<false>(j, e, n, t) < D ? column_of<false>(j, e, n, t) : 0));
+#pragma unroll
+    for (int j = 0; j < NG; ++j)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) v[j][e] = make_float2(Io<TX>::get(raw[j][2 * e]), Io<TX>::get(raw[j][2 * e + 1]));
   }
-  auto each = [&](auto f) {
+  float2 g[NG][2], b[NG][2];
+  get_parameters<NG, WHOLE>(g, p.w, 0.f, D, n, t);
+  get_parameters<NG, WHOLE>(b, p.b, 0.f, D, n, t);
+  if (W > 1) __syncthreads();  // red's zeros
+  float mean, rstd;
+  statistics<NG, WHOLE>(v, D, 1.f / static_cast<float>(D), p.eps, W, w, n, t, red[0], red[1], mean, rstd);
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      if (WHOLE) {
-        if ((j * n + t) * 8 < D) {
+  for (int j = 0; j < NG; ++j)
 #pragma unroll
-          for (int e = 0; e < 8; ++e) f(v[j][e]);
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if ((j * 8 + e) * n + t < D) f(v[j][e]);
-      }
-    }
-  };
-  float s = 0.f;
-  each([&](float a) { s += a; });
-  const float mean = row_sum(s, W, w, red[0]) / static_cast<float>(D);
-  float q = 0.f;
-  each([&](float& a) {
-    a -= mean;
-    q = fmaf(a, a, q);
-  });
-  const float rstd = 1.f / sqrtf(row_sum(q, W, w, red[1]) / static_cast<float>(D) + p.eps);
-#pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    if (WHOLE) {
-      const int c = (j * n + t) * 8;
-      if (c >= D) continue;
-      float g[8], b[8];
-      load8(p.w, c, g);
-      load8(p.b, c, b);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) g[e] = fmaf(v[j][e] * rstd, g[e], b[e]);
-      store8(y + c, g);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int c = (j * 8 + e) * n + t;
-        if (c < D) y[c] = Io<TY>::put(fmaf(v[j][e] * rstd, p.w[c], p.b[c]));
-      }
-    }
-  }
+    for (int e = 0; e < 2; ++e) v[j][e] = __ffma2_rn(__fmul2_rn(v[j][e], make_float2(rstd, rstd)), g[j][e], b[j][e]);
+  put_row<NG, WHOLE>(y, v, D, n, t);
   if (t == 0) {
     p.mean[r] = mean;
     p.rstd[r] = rstd;
   }
 }
 
-// ---------------------------------------------------------------- backward, rows through shared memory
+// ---------------------------------------------------------------- rows through shared memory
 
-constexpr int kBwdStages = 8;
+constexpr int kStages = 8;
 constexpr int kRowInfo = 32;  // rows whose mask, mean and rstd are fetched at once
 
 struct Stages {
@@ -275,15 +326,113 @@ __device__ __forceinline__ Span span(const void* row, int64_t bytes, bool first,
   if (s.to < s.from) s.to = s.from;
   return s;
 }
+// Starts the copy of a span to a stage.
+__device__ __forceinline__ void copy(const Span& s, uint8_t* to, uint64_t* bar) {
+  if (s.to > s.from)
+    bulk_g2s(to + (s.from - s.at), reinterpret_cast<const void*>(s.from), static_cast<uint32_t>(s.to - s.from), bar);
+}
 
-// Persistent CTAs of W warps that share a row, 4 NG columns a thread; the rows' x and dy come by bulk copies into a ring
-// of stages. A thread keeps the same columns for all rows and with them the columns' sums in registers: both matrices are
-// read once. WHOLE: rows in 16-byte blocks, D a multiple of 4, a thread's columns in groups of four; else one apart.
+// A thread's elements of a row in its stage; those behind D are not the row's. `edge`: the matrix' first or last row, whose
+// outermost elements may not have been copied.
+template <int NG, bool WHOLE, typename T>
+__device__ __forceinline__ void get_row(float2 (&v)[NG][2], const uint8_t* stage, const T* row, bool first, bool last, int D, int n,
+                                        int t) {
+  if (WHOLE) {
+    const T* at = reinterpret_cast<const T*>(stage);
+    Raw<T> raw[NG];
+#pragma unroll
+    for (int j = 0; j < NG; ++j) raw[j].shared(at + (column_of<true>(j, 0, n, t) < D ? column_of<true>(j, 0, n, t) : 0));
+#pragma unroll
+    for (int j = 0; j < NG; ++j) raw[j].get(v[j]);
+  } else {
+    const T* at = reinterpret_cast<const T*>(stage + (reinterpret_cast<uintptr_t>(row) & 15));
+    T raw[NG][4];
+    if (!first && !last) {
+#pragma unroll
+      for (int j = 0; j < NG; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) raw[j][e] = at[column_of<false>(j, e, n, t) < D ? column_of<false>(j, e, n, t) : 0];
+    } else {
+      const Span s = span(row, D * sizeof(T), first, last);
+#pragma unroll
+      for (int j = 0; j < NG; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int c = column_of<false>(j, e, n, t) < D ? column_of<false>(j, e, n, t) : 0;
+          const uintptr_t a = reinterpret_cast<uintptr_t>(row + c);
+          raw[j][e] = a >= s.from && a < s.to ? at[c] : row[c];
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < NG; ++j)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) v[j][e] = make_float2(Io<T>::get(raw[j][2 * e]), Io<T>::get(raw[j][2 * e + 1]));
+  }
+}
+
+// Persistent CTAs of W warps that share a row, 4 NG columns a thread, whose parameters stay in registers; the rows come by
+// bulk copies into a ring of stages, as many bytes ahead as an SM has shared memory for: what one row per CTA has in
+// flight, in registers, kept the memory at half its rate (32,768 rows of 4,096 bf16: 155 us).
+template <typename TX, typename TY, int NG, bool WHOLE>
+__global__ void __launch_bounds__(kMostWarps * 32) fwd_ring_kernel(const FwdArgs p, const Stages st) {
+  extern __shared__ __align__(16) uint8_t smem[];
+  __shared__ __align__(8) uint64_t full[kStages];
+  __shared__ __align__(16) float red[2][kMostWarps];
+  const int W = blockDim.x / 32, n = blockDim.x, t = threadIdx.x, warp = t / 32;
+  const int D = static_cast<int>(p.D);
+  const float inv = 1.f / static_cast<float>(D);
+  const int64_t G = gridDim.x;
+  if (t < st.n) mbar_init(&full[t], 1);
+  if (t == 0) fence_mbar_init();
+  if (t < st.n) fence_proxy_async_smem();
+  for (int i = t; i < 2 * kMostWarps; i += n) (&red[0][0])[i] = 0.f;
+  __syncthreads();
+  const TX* x = static_cast<const TX*>(p.x);
+  auto fetch = [&](int64_t r, int stage) {
+    const Span s = span(x + r * p.ld_x, D * sizeof(TX), r == 0, r == p.rows - 1);
+    mbar_arrive_expect_tx(&full[stage], static_cast<uint32_t>(s.to - s.from));
+    copy(s, smem + static_cast<size_t>(stage) * st.bytes, &full[stage]);
+  };
+  if (t == 0)
+    for (int i = 0; i < st.n && blockIdx.x + i * G < p.rows; ++i) fetch(blockIdx.x + i * G, i);
+  float2 g[NG][2], b[NG][2];
+  get_parameters<NG, WHOLE>(g, p.w, 0.f, D, n, t);
+  get_parameters<NG, WHOLE>(b, p.b, 0.f, D, n, t);
+  int stage = 0;
+  uint32_t parity = 0;
+  bool in_time = true;
+  for (int64_t r = blockIdx.x; r < p.rows; r += G) {
+    in_time = in_time && mbar_wait_bounded(&full[stage], parity);
+    float2 v[NG][2];
+    get_row<NG, WHOLE>(v, smem + static_cast<size_t>(stage) * st.bytes, x + r * p.ld_x, r == 0, r == p.rows - 1, D, n, t);
+    float mean, rstd;
+    statistics<NG, WHOLE>(v, D, inv, p.eps, W, warp, n, t, red[0], red[1], mean, rstd);
+    if (!in_time) mean = rstd = __int_as_float(0x7fc00000);  // there is no status word: NaNs say that a wait ran out
+    if (W == 1) __syncwarp();
+    if (t == 0 && r + st.n * G < p.rows) fetch(r + st.n * G, stage);  // the sums' barriers: everyone has read the stage
+    if (++stage == st.n) {
+      stage = 0;
+      parity ^= 1;
+    }
+#pragma unroll
+    for (int j = 0; j < NG; ++j)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) v[j][e] = __ffma2_rn(__fmul2_rn(v[j][e], make_float2(rstd, rstd)), g[j][e], b[j][e]);
+    put_row<NG, WHOLE>(static_cast<TY*>(p.y) + r * p.ld_y, v, D, n, t);
+    if (t == 0) {
+      p.mean[r] = mean;
+      p.rstd[r] = rstd;
+    }
+  }
+}
+
+// The same for the gradient: x and dy of the rows that have one come through the ring. A thread keeps the same columns for
+// all rows and with them the columns' sums in registers: both matrices are read once.
 template <typename TX, typename TD, int NG, bool WHOLE>
 __global__ void __launch_bounds__(kMostWarps * 32) bwd_kernel(const BwdArgs p, const Stages st, int32_t* status) {
   extern __shared__ __align__(16) uint8_t smem[];
-  __shared__ __align__(8) uint64_t full[kBwdStages];
-  __shared__ float2 red[2][kMostWarps];
+  __shared__ __align__(8) uint64_t full[kStages];
+  __shared__ __align__(16) float2 red[2][kMostWarps];
   const int W = blockDim.x / 32, n = blockDim.x, t = threadIdx.x, warp = t / 32, lane = t & 31;
   const int D = static_cast<int>(p.D);
   const float inv = 1.f / static_cast<float>(D);
@@ -291,9 +440,9 @@ __global__ void __launch_bounds__(kMostWarps * 32) bwd_kernel(const BwdArgs p, c
   if (t < st.n) mbar_init(&full[t], 1);
   if (t == 0) fence_mbar_init();
   if (t < st.n) fence_proxy_async_smem();
+  for (int i = t; i < 2 * kMostWarps; i += n) (&red[0][0])[i] = make_float2(0.f, 0.f);
   __syncthreads();
-  auto column = [&](int j, int e) { return WHOLE ? (j * n + t) * 4 + e : (j * 4 + e) * n + t; };
-  auto live_rows = [&](int64_t base) {  // the batch of rows base .. base + 31 of the CTA's that have a gradient
+  auto live_rows = [&](int64_t base) {  // which of the CTA's rows base .. base + 31 have a gradient
     const int64_t i = base + lane;
     return __ballot_sync(0xffffffffu, i < mine && (!p.mask || p.mask[b0 + i * G] != 0));
   };
@@ -313,11 +462,10 @@ __global__ void __launch_bounds__(kMostWarps * 32) bwd_kernel(const BwdArgs p, c
       const bool first = r == 0, last = r == p.rows - 1;
       const Span sx = span(static_cast<const TX*>(p.x) + r * p.ld_x, D * sizeof(TX), first, last);
       const Span sd = span(static_cast<const TD*>(p.dy) + r * p.ld_dy, D * sizeof(TD), first, last);
-      const uint32_t nx = static_cast<uint32_t>(sx.to - sx.from), nd = static_cast<uint32_t>(sd.to - sd.from);
       uint8_t* to = smem + static_cast<size_t>(stage) * st.bytes;
-      mbar_arrive_expect_tx(&full[stage], nx + nd);
-      if (nx) bulk_g2s(to + (sx.from - sx.at), reinterpret_cast<const void*>(sx.from), nx, &full[stage]);
-      if (nd) bulk_g2s(to + st.x_bytes + (sd.from - sd.at), reinterpret_cast<const void*>(sd.from), nd, &full[stage]);
+      mbar_arrive_expect_tx(&full[stage], static_cast<uint32_t>((sx.to - sx.from) + (sd.to - sd.from)));
+      copy(sx, to, &full[stage]);
+      copy(sd, to + st.x_bytes, &full[stage]);
     }
     __syncwarp();
     return true;
@@ -325,19 +473,18 @@ __global__ void __launch_bounds__(kMostWarps * 32) bwd_kernel(const BwdArgs p, c
   if (warp == 0)
     for (int i = 0; i < st.n && fetch_next(i); ++i) {}
 
-  float wt[NG][4], dw[NG][4], db[NG][4];
+  float2 wt[NG][2], dw[NG][2], db[NG][2];
+  get_parameters<NG, WHOLE>(wt, p.w, 0.f, D, n, t);
 #pragma unroll
   for (int j = 0; j < NG; ++j)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int c = column(j, e);
-      wt[j][e] = c < D ? p.w[c] : 0.f;
-      dw[j][e] = db[j][e] = 0.f;
-    }
+    for (int e = 0; e < 2; ++e) dw[j][e] = db[j][e] = make_float2(0.f, 0.f);
+  const bool full_width = D == 4 * NG * n;
 
   int stage = 0;
   uint32_t parity = 0, odd = 0;
   bool in_time = true;
+  int64_t r = b0;
   for (int64_t base = 0; base < mine; base += kRowInfo) {
     const uint32_t live = live_rows(base);
     float mean_l = 0.f, rstd_l = 0.f;
@@ -346,133 +493,77 @@ __global__ void __launch_bounds__(kMostWarps * 32) bwd_kernel(const BwdArgs p, c
       rstd_l = p.rstd[b0 + (base + lane) * G];
     }
     const int here = static_cast<int>(min(static_cast<int64_t>(kRowInfo), mine - base));
-    for (int i = 0; i < here; ++i) {
-      const int64_t r = b0 + (base + i) * G;
+    for (int i = 0; i < here; ++i, r += G) {
       TX* dx = static_cast<TX*>(p.dx) + r * p.ld_dx;
-      float out[NG][4];
-      if (live >> i & 1) {
-        const float mean = __shfl_sync(0xffffffffu, mean_l, i), rstd = __shfl_sync(0xffffffffu, rstd_l, i);
-        // a wait that ran out is reported and not tried again
-        in_time = in_time && mbar_wait_bounded(&full[stage], parity);
-        const uint8_t* at = smem + static_cast<size_t>(stage) * st.bytes;
-        const TX* x = static_cast<const TX*>(p.x) + r * p.ld_x;
-        const TD* dy = static_cast<const TD*>(p.dy) + r * p.ld_dy;
-        float h[NG][4], g[NG][4], s = 0.f, q = 0.f;
-        const bool edge = r == 0 || r == p.rows - 1;
-        const Span sx = span(x, D * sizeof(TX), r == 0, r == p.rows - 1), sd = span(dy, D * sizeof(TD), r == 0, r == p.rows - 1);
-        const TX* xs = reinterpret_cast<const TX*>(at + (reinterpret_cast<uintptr_t>(x) - sx.at));
-        const TD* ds = reinterpret_cast<const TD*>(at + st.x_bytes + (reinterpret_cast<uintptr_t>(dy) - sd.at));
-        auto in = [](const void* a, const Span& v) {
-          return reinterpret_cast<uintptr_t>(a) >= v.from && reinterpret_cast<uintptr_t>(a) < v.to;
-        };
+      if (!(live >> i & 1)) {
+        float2 zero[NG][2];
 #pragma unroll
-        for (int j = 0; j < NG; ++j) {
-          float xv[4], dv[4];
-          if (WHOLE) {
-            const int c = (j * n + t) * 4;
-            if (c >= D) {
+        for (int j = 0; j < NG; ++j) zero[j][0] = zero[j][1] = make_float2(0.f, 0.f);
+        put_row<NG, WHOLE>(dx, zero, D, n, t);
+        continue;
+      }
+      const float mean = __shfl_sync(0xffffffffu, mean_l, i), rstd = __shfl_sync(0xffffffffu, rstd_l, i);
+      // a wait that ran out is reported and not tried again
+      in_time = in_time && mbar_wait_bounded(&full[stage], parity);
+      const uint8_t* at = smem + static_cast<size_t>(stage) * st.bytes;
+      float2 h[NG][2], g[NG][2], s = make_float2(0.f, 0.f), q = s;
+      get_row<NG, WHOLE>(h, at, static_cast<const TX*>(p.x) + r * p.ld_x, r == 0, r == p.rows - 1, D, n, t);
+      get_row<NG, WHOLE>(g, at + st.x_bytes, static_cast<const TD*>(p.dy) + r * p.ld_dy, r == 0, r == p.rows - 1, D, n, t);
+      const float2 off = make_float2(-mean, -mean), scale = make_float2(rstd, rstd);
 #pragma unroll
-              for (int e = 0; e < 4; ++e) h[j][e] = g[j][e] = 0.f;
-              continue;
-            }
-            if (sizeof(TX) == 2) {
-              const uint2 v = *reinterpret_cast<const uint2*>(xs + c);
-              xv[0] = bf16_lo(v.x), xv[1] = bf16_hi(v.x), xv[2] = bf16_lo(v.y), xv[3] = bf16_hi(v.y);
-            } else {
-              const float4 v = *reinterpret_cast<const float4*>(xs + c);
-              xv[0] = v.x, xv[1] = v.y, xv[2] = v.z, xv[3] = v.w;
-            }
-            if (sizeof(TD) == 2) {
-              const uint2 v = *reinterpret_cast<const uint2*>(ds + c);
-              dv[0] = bf16_lo(v.x), dv[1] = bf16_hi(v.x), dv[2] = bf16_lo(v.y), dv[3] = bf16_hi(v.y);
-            } else {
-              const float4 v = *reinterpret_cast<const float4*>(ds + c);
-              dv[0] = v.x, dv[1] = v.y, dv[2] = v.z, dv[3] = v.w;
-            }
-          } else {
+      for (int j = 0; j < NG; ++j)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int c = column(j, e);
-              xv[e] = mean;
-              dv[e] = 0.f;
-              if (c >= D) continue;
-              xv[e] = Io<TX>::get(!edge || in(x + c, sx) ? xs[c] : x[c]);
-              dv[e] = Io<TD>::get(!edge || in(dy + c, sd) ? ds[c] : dy[c]);
-            }
+        for (int e = 0; e < 2; ++e) {
+          float2 d = g[j][e];
+          if (!full_width) {
+            if (column_of<WHOLE>(j, 2 * e, n, t) >= D) d.x = 0.f;
+            if (column_of<WHOLE>(j, 2 * e + 1, n, t) >= D) d.y = 0.f;
           }
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            h[j][e] = (xv[e] - mean) * rstd;
-            g[j][e] = dv[e] * wt[j][e];
-            s += g[j][e];
-            q = fmaf(g[j][e], h[j][e], q);
-            dw[j][e] = fmaf(dv[e], h[j][e], dw[j][e]);
-            db[j][e] += dv[e];
-          }
+          h[j][e] = __fmul2_rn(__fadd2_rn(h[j][e], off), scale);
+          g[j][e] = __fmul2_rn(d, wt[j][e]);
+          s = __fadd2_rn(s, g[j][e]);
+          q = __ffma2_rn(g[j][e], h[j][e], q);
+          dw[j][e] = __ffma2_rn(d, h[j][e], dw[j][e]);
+          db[j][e] = __fadd2_rn(db[j][e], d);
         }
+      float2 sq = make_float2(s.x + s.y, q.x + q.y);
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-          s += __shfl_xor_sync(0xffffffffu, s, o);
-          q += __shfl_xor_sync(0xffffffffu, q, o);
-        }
-        if (W > 1 && lane == 0) red[odd][warp] = make_float2(s, q);
-        // everyone has read the stage, and the sums are there
-        if (W > 1) __syncthreads();
-        else __syncwarp();
-        if (warp == 0) fetch_next(stage);
-        if (W > 1) {
-          s = q = 0.f;
-          for (int w = 0; w < W; ++w) {
-            const float2 v = red[odd][w];
-            s += v.x;
-            q += v.y;
-          }
-          odd ^= 1;
-        }
-        s *= inv;
-        q *= inv;
-        if (++stage == st.n) {
-          stage = 0;
-          parity ^= 1;
-        }
+      for (int o = 16; o > 0; o >>= 1)
+        sq = __fadd2_rn(sq, make_float2(__shfl_xor_sync(0xffffffffu, sq.x, o), __shfl_xor_sync(0xffffffffu, sq.y, o)));
+      // everyone has read the stage, and the sums are there
+      if (W > 1) {
+        if (lane == 0) red[odd][warp] = sq;
+        __syncthreads();
+        sq = make_float2(0.f, 0.f);
 #pragma unroll
-        for (int j = 0; j < NG; ++j)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) out[j][e] = rstd * (g[j][e] - s - h[j][e] * q);
+        for (int w = 0; w < kMostWarps; w += 4) {
+          if (w >= W) break;
+          const float4 a = *reinterpret_cast<const float4*>(&red[odd][w]), b = *reinterpret_cast<const float4*>(&red[odd][w + 2]);
+          sq = __fadd2_rn(sq, __fadd2_rn(__fadd2_rn(make_float2(a.x, a.y), make_float2(a.z, a.w)),
+                                         __fadd2_rn(make_float2(b.x, b.y), make_float2(b.z, b.w))));
+        }
+        odd ^= 1;
       } else {
-#pragma unroll
-        for (int j = 0; j < NG; ++j)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) out[j][e] = 0.f;
+        __syncwarp();
       }
-#pragma unroll
-      for (int j = 0; j < NG; ++j) {
-        if (WHOLE) {
-          const int c = (j * n + t) * 4;
-          if (c >= D) continue;
-          if (sizeof(TX) == 2)
-            __stcs(reinterpret_cast<uint2*>(dx + c), make_uint2(pack_bf16x2(out[j][0], out[j][1]), pack_bf16x2(out[j][2], out[j][3])));
-          else
-            __stcs(reinterpret_cast<float4*>(dx + c), make_float4(out[j][0], out[j][1], out[j][2], out[j][3]));
-        } else {
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (column(j, e) < D) dx[column(j, e)] = Io<TX>::put(out[j][e]);
-        }
+      if (warp == 0) fetch_next(stage);
+      if (++stage == st.n) {
+        stage = 0;
+        parity ^= 1;
       }
+      // rstd g - rstd (mean of g) - h rstd (mean of g h)
+      const float m = -sq.x * inv * rstd, k = -sq.y * inv * rstd;
+#pragma unroll
+      for (int j = 0; j < NG; ++j)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          g[j][e] = __ffma2_rn(h[j][e], make_float2(k, k), __ffma2_rn(g[j][e], scale, make_float2(m, m)));
+      put_row<NG, WHOLE>(dx, g, D, n, t);
     }
   }
   if (!in_time && lane == 0) flag_status(status, RL_DEV_TIMEOUT);
-  const int64_t part = b0 * p.D;
-#pragma unroll
-  for (int j = 0; j < NG; ++j)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int c = column(j, e);
-      if (c >= D) continue;
-      if (p.part_w) p.part_w[part + c] = dw[j][e];
-      if (p.part_b) p.part_b[part + c] = db[j][e];
-    }
+  if (p.part_w) put_row<NG, WHOLE>(p.part_w + b0 * p.D, dw, D, n, t);
+  if (p.part_b) put_row<NG, WHOLE>(p.part_b + b0 * p.D, db, D, n, t);
 }
 
 // The columns' sums over part blockIdx.y of the rows, a thread per column.
@@ -522,10 +613,11 @@ __global__ void __launch_bounds__(32 * kPartLanes) add_parts_kernel(const float*
 constexpr int kSMs = 152;
 constexpr int64_t kMaxD = 1 << 20;
 
-// Columns of a warp, and warps of a row, in the backward kernel; 0: a row has too many columns for it.
-inline int bwd_groups(int64_t D) { return D <= 256 ? 2 : 4; }
-inline int bwd_warps(int64_t D) {
-  const int64_t per = 128 * bwd_groups(D), W = (D + per - 1) / per;
+// Blocks of four columns a thread holds in the backward kernel, and the warps of a row; 0: a row has too many columns for
+// it. An element at a time two blocks: four spill (128 registers), and with the stages in the way of L1 that cost 3 times the time.
+inline int bwd_groups(int64_t D, bool whole) { return D <= 256 || (!whole && D <= 256 * kMostWarps) ? 2 : 4; }
+inline int bwd_warps(int64_t D, bool whole) {
+  const int64_t per = 128 * bwd_groups(D, whole), W = (D + per - 1) / per;
   return W <= kMostWarps ? static_cast<int>(W) : 0;
 }
 // CTAs of it on an SM: 16 warps at up to 128 registers a thread.
@@ -533,7 +625,7 @@ inline int bwd_ctas(int W) { return 16 / W; }
 
 // Parts of the columns' sums.
 inline int parts_of(int64_t rows, int64_t D) {
-  const int W = bwd_warps(D);
+  const int W = bwd_warps(D, true);  // the fewest of a row
   return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(rows, W ? bwd_ctas(W) * kSMs : 2 * kSMs)));
 }
 
@@ -543,45 +635,81 @@ inline bool element_aligned(const void* p, rl_dtype t) {
 
 inline bool whole_blocks(const void* p, int64_t ld, size_t es) { return aligned16(p) && ld * es % 16 == 0; }
 
-template <typename TX, typename TY, int NV>
-void launch_fwd(const FwdArgs& a, int W, bool whole, cudaStream_t s) {
+constexpr int64_t kStageRoom = 216 * 1024;  // of an SM's shared memory
+
+// The kernel may take kStageRoom, once per device.
+template <typename K>
+rl_status allow_room(K kern, std::atomic<uint64_t>& ready, const char* what) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return cuda_error(e, "cudaGetDevice");
+  const uint64_t bit = dev < 64 ? uint64_t(1) << dev : 0;
+  if (ready.load() & bit) return RL_OK;
+  e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kStageRoom));
+  if (e != cudaSuccess) return cuda_error(e, what);
+  ready |= bit;
+  return RL_OK;
+}
+
+inline Stages stages(int64_t x_bytes, int64_t d_bytes, bool whole, int ctas) {
+  auto room = [&](int64_t n) { return static_cast<int32_t>(n ? (n + 15) / 16 * 16 + (whole ? 0 : 16) : 0); };
+  Stages st;
+  st.x_bytes = room(x_bytes);
+  st.bytes = st.x_bytes + room(d_bytes);
+  st.n = static_cast<int32_t>(std::min<int64_t>(kStages, (kStageRoom / ctas - 2048) / st.bytes));
+  return st;
+}
+
+template <typename TX, typename TY, int NG, bool WHOLE>
+void launch_fwd(const FwdArgs& a, int W, cudaStream_t s) {
   const int per = W == 1 ? 4 : 1;  // rows a CTA
-  const dim3 grid(static_cast<unsigned>((a.rows + per - 1) / per)), block(32 * W, per);
-  if (whole) fwd_kernel<TX, TY, NV, true><<<grid, block, 0, s>>>(a);
-  else fwd_kernel<TX, TY, NV < 4 ? NV : 2, false><<<grid, block, 0, s>>>(a);
+  fwd_kernel<TX, TY, NG, WHOLE><<<static_cast<unsigned>((a.rows + per - 1) / per), dim3(32 * W, per), 0, s>>>(a);
+}
+
+template <typename TX, typename TY, int NG, bool WHOLE>
+rl_status launch_ring(const FwdArgs& a, int W, int ctas, cudaStream_t s) {
+  static std::atomic<uint64_t> ready{0};
+  auto kern = fwd_ring_kernel<TX, TY, NG, WHOLE>;
+  const rl_status r = allow_room(kern, ready, "cudaFuncSetAttribute(fwd_ring_kernel)");
+  if (r != RL_OK) return r;
+  const Stages st = stages(a.D * sizeof(TX), 0, WHOLE, ctas);
+  kern<<<static_cast<unsigned>(std::min<int64_t>(a.rows, ctas * kSMs)), 32 * W, static_cast<size_t>(st.n) * st.bytes, s>>>(a, st);
+  return RL_OK;
 }
 
 template <typename TX, typename TY>
 rl_status fwd(const FwdArgs& a, cudaStream_t s) {
-  const bool whole = a.D % 8 == 0 && whole_blocks(a.x, a.ld_x, sizeof(TX)) && whole_blocks(a.y, a.ld_y, sizeof(TY)) &&
-                     aligned16(a.w.at) && aligned16(a.b.at);
-  auto warps = [&](int nv) { return static_cast<int>((a.D + 256 * nv - 1) / (256 * nv)); };
-  const int most = whole ? 4 : 2;
-  if (a.rows < (int64_t(1) << 31) && warps(most) <= kMostWarps) {
-    // few rows: as many threads on each as have a block of it; else up to four blocks a thread
-    if (warps(1) == 1 || (a.rows * warps(1) <= 16 * kSMs && warps(1) <= kMostWarps)) launch_fwd<TX, TY, 1>(a, warps(1), whole, s);
-    else if (most == 2 || warps(2) == 1) launch_fwd<TX, TY, 2>(a, warps(2), whole, s);
-    else launch_fwd<TX, TY, 4>(a, warps(4), whole, s);
-    const cudaError_t e = cudaGetLastError();
-    return e == cudaSuccess ? RL_OK : cuda_error(e, "fwd_kernel launch");
+  const bool whole = a.D % 4 == 0 && a.D * sizeof(TX) % 16 == 0 && whole_blocks(a.x, a.ld_x, sizeof(TX)) &&
+                     reinterpret_cast<uintptr_t>(a.y) % (4 * sizeof(TY)) == 0 && a.ld_y % 4 == 0;
+  auto warps = [&](int ng) { return static_cast<int>((a.D + 128 * ng - 1) / (128 * ng)); };
+  cudaError_t e;
+  if (warps(4) > kMostWarps || a.rows >= (int64_t(1) << 31)) {
+    loop_fwd_kernel<TX, TY><<<static_cast<unsigned>(std::min<int64_t>(a.rows, 4 * kSMs)), kLoopThreads, 0, s>>>(a);
+    e = cudaGetLastError();
+    return e == cudaSuccess ? RL_OK : cuda_error(e, "loop_fwd_kernel launch");
   }
-  loop_fwd_kernel<TX, TY><<<static_cast<unsigned>(std::min<int64_t>(a.rows, 4 * kSMs)), kLoopThreads, 0, s>>>(a);
-  const cudaError_t e = cudaGetLastError();
-  return e == cudaSuccess ? RL_OK : cuda_error(e, "loop_fwd_kernel launch");
+  const int W = warps(4), ctas = std::max(1, (whole ? 32 : 16) / W);
+  rl_status r = RL_OK;
+  if (warps(2) <= kMostWarps && a.rows * warps(2) <= 24 * kSMs) {
+    if (whole) launch_fwd<TX, TY, 2, true>(a, warps(2), s);
+    else launch_fwd<TX, TY, 2, false>(a, warps(2), s);
+  } else if (warps(2) == 1) {
+    r = whole ? launch_ring<TX, TY, 2, true>(a, 1, 24, s) : launch_ring<TX, TY, 2, false>(a, 1, 24, s);
+  } else {
+    r = whole ? launch_ring<TX, TY, 4, true>(a, W, ctas, s) : launch_ring<TX, TY, 4, false>(a, W, ctas, s);
+  }
+  if (r != RL_OK) return r;
+  e = cudaGetLastError();
+  return e == cudaSuccess ? RL_OK : cuda_error(e, "fwd_kernel launch");
 }
-
-constexpr int64_t kStageRoom = 216 * 1024;  // of an SM's shared memory
 
 template <typename TX, typename TD, int NG, bool WHOLE>
 rl_status launch_bwd(const BwdArgs& a, int W, int32_t* status, cudaStream_t s) {
-  Stages st;
-  st.x_bytes = static_cast<int32_t>((a.D * sizeof(TX) + 15) / 16 * 16 + (WHOLE ? 0 : 16));
-  st.bytes = st.x_bytes + static_cast<int32_t>((a.D * sizeof(TD) + 15) / 16 * 16 + (WHOLE ? 0 : 16));
-  st.n = static_cast<int32_t>(std::min<int64_t>(kBwdStages, (kStageRoom / bwd_ctas(W) - 2048) / st.bytes));
+  static std::atomic<uint64_t> ready{0};
   auto kern = bwd_kernel<TX, TD, NG, WHOLE>;
-  // set on every call: the attribute is a device's, and cheap
-  const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kStageRoom));
-  if (e != cudaSuccess) return cuda_error(e, "cudaFuncSetAttribute(bwd_kernel)");
+  const rl_status r = allow_room(kern, ready, "cudaFuncSetAttribute(bwd_kernel)");
+  if (r != RL_OK) return r;
+  const Stages st = stages(a.D * sizeof(TX), a.D * sizeof(TD), WHOLE, bwd_ctas(W));
   kern<<<a.parts, 32 * W, static_cast<size_t>(st.n) * st.bytes, s>>>(a, st, status);
   return RL_OK;
 }
@@ -590,11 +718,12 @@ template <typename TX, typename TD>
 rl_status bwd(BwdArgs& a, float* d_weight, float* d_bias, int32_t* status, cudaStream_t s) {
   a.parts = parts_of(a.rows, a.D);
   cudaError_t e = cudaSuccess;
-  if (const int W = bwd_warps(a.D)) {
-    const bool whole = a.D * sizeof(TX) % 16 == 0 && a.D * sizeof(TD) % 16 == 0 && whole_blocks(a.x, a.ld_x, sizeof(TX)) &&
-                       whole_blocks(a.dy, a.ld_dy, sizeof(TD)) && whole_blocks(a.dx, a.ld_dx, sizeof(TX));
+  const bool whole = a.D * sizeof(TX) % 16 == 0 && a.D * sizeof(TD) % 16 == 0 && whole_blocks(a.x, a.ld_x, sizeof(TX)) &&
+                     whole_blocks(a.dy, a.ld_dy, sizeof(TD)) && whole_blocks(a.dx, a.ld_dx, sizeof(TX));
+  if (const int W = bwd_warps(a.D, whole)) {
+    a.parts = static_cast<int32_t>(std::min<int64_t>(a.parts, bwd_ctas(W) * kSMs));
     rl_status r;
-    if (bwd_groups(a.D) == 2) r = whole ? launch_bwd<TX, TD, 2, true>(a, W, status, s) : launch_bwd<TX, TD, 2, false>(a, W, status, s);
+    if (bwd_groups(a.D, whole) == 2) r = whole ? launch_bwd<TX, TD, 2, true>(a, W, status, s) : launch_bwd<TX, TD, 2, false>(a, W, status, s);
     else r = whole ? launch_bwd<TX, TD, 4, true>(a, W, status, s) : launch_bwd<TX, TD, 4, false>(a, W, status, s);
     if (r != RL_OK) return r;
     e = cudaGetLastError();

@@ -16,11 +16,9 @@
 //   3. every warp sums the kept weights of its segment and counts the entries equal to the threshold; a second exchange;
 //      the warp whose segment holds the token finds it by a scan.
 #include <algorithm>
+#include <atomic>
 #include <cmath>
-#include <map>
-#include <mutex>
 #include <string>
-#include <utility>
 
 #include "rl_device.cuh"
 #include "rl_host.h"
@@ -514,16 +512,14 @@ rl_status launch(Args& a, int C, cudaStream_t s) {
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return cuda_error(e, "cudaGetDevice");
-  static std::mutex mu;
-  static std::map<int, bool> ready;  // by device
-  {
-    std::lock_guard<std::mutex> lock(mu);
-    if (!ready[dev]) {
-      e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kMostBytes + kPastBytes));
-      if (e == cudaSuccess) e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-      if (e != cudaSuccess) return cuda_error(e, "cudaFuncSetAttribute(sample_kernel)");
-      ready[dev] = true;
-    }
+  // once per device
+  static std::atomic<uint64_t> ready{0};
+  const uint64_t bit = dev < 64 ? uint64_t(1) << dev : 0;
+  if (!(ready.load() & bit)) {
+    e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kMostBytes + kPastBytes));
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e != cudaSuccess) return cuda_error(e, "cudaFuncSetAttribute(sample_kernel)");
+    ready |= bit;
   }
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute attr[1];

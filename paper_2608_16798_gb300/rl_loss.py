@@ -796,43 +796,44 @@ def _refuse_dtype(name, t):
     raise ValueError(f"{name} must be bfloat16 or float32, got {t.dtype}")
 
 
-def _rows(t, name, shape, ix):
-    """(pointer, dtype code, leading dimension) of a matrix with unit stride along its rows (of `shape`, if given)."""
-    if t.dtype not in (torch.bfloat16, torch.float32):
+_FLOATS = {torch.bfloat16: RL_BF16, torch.float32: RL_F32}
+
+
+def _rows(t, name, shape=None, ix=None):
+    """(pointer, dtype code, leading dimension) of a matrix with unit stride along its rows (of `shape` and on device
+    `ix`, if given). As in _need the checks are a few cheap queries; the reason for a refusal is worked out afterwards."""
+    dt, s = _FLOATS.get(t.dtype), t.shape
+    if dt is not None and len(s) == 2 and (shape is None or s == shape) and t.is_cuda and (ix is None or t.get_device() == ix):
+        ld, unit = t.stride()
+        if unit == 1 or s[1] <= 1:
+            return t.data_ptr(), dt, ld if s[0] > 1 else s[1]  # the stride of a single row says nothing
+        raise ValueError(f"{name} must have unit stride along its rows")
+    if dt is None:
         _refuse_dtype(name, t)
-    if t.dim() != 2 or (shape is not None and tuple(t.shape) != shape):
-        raise ValueError(f"{name} must be a matrix{'' if shape is None else f' [{shape[0]}, {shape[1]}]'}, got {tuple(t.shape)}")
     if not t.is_cuda or (ix is not None and t.get_device() != ix):
         raise ValueError(f"{name} must be a CUDA tensor on the other arguments' device, got {t.device}")
-    rows, n = t.shape
-    if n > 1 and t.stride(1) != 1:
-        raise ValueError(f"{name} must have unit stride along its rows")
-    ld = t.stride(0) if rows > 1 else n  # the stride of a single row says nothing
-    return t.data_ptr(), RL_BF16 if t.dtype == torch.bfloat16 else RL_F32, ld
+    raise ValueError(f"{name} must be a matrix{'' if shape is None else f' [{shape[0]}, {shape[1]}]'}, got {tuple(t.shape)}")
 
 
 def _vector_pair(weight, bias, D, ix):
     """(weight's pointer, bias' pointer, their dtype code) of a norm's parameters [D]."""
-    dt = None
-    for t, name in ((weight, "weight"), (bias, "bias")):
-        if t is None:
-            continue
-        if t.dtype not in (torch.bfloat16, torch.float32):
-            _refuse_dtype(name, t)
-        if t.numel() != D:
-            raise ValueError(f"{name} has {t.numel()} elements, needs {D}")
-        if dt is not None and t.dtype != dt:
-            raise ValueError("weight and bias must have the same dtype")
-        dt = t.dtype
-        _need(t, name, dt, D, index=ix)
-    return _ptr(weight), _ptr(bias), RL_BF16 if dt == torch.bfloat16 else RL_F32
+    given = weight if weight is not None else bias
+    if given is None:
+        return None, None, RL_F32
+    dt = _FLOATS.get(given.dtype)
+    if dt is None:
+        _refuse_dtype("weight" if weight is not None else "bias", given)
+    p_w, p_b = _opt(weight, "weight", given.dtype, D, index=ix), _opt(bias, "bias", given.dtype, D, index=ix)
+    if given.numel() != D or (bias is not None and bias.numel() != D):
+        raise ValueError(f"weight and bias must have {D} elements")
+    return p_w, p_b, dt
 
 
 def rl_layer_norm_fwd(x, weight=None, bias=None, eps=1e-5, y=None, y_dtype=None, mean=None, rstd=None, stream=None):
     """Layer norm of the rows of ``x`` ([rows, D], bf16 or float32, any row stride). ``weight`` and ``bias`` ([D],
     both bf16 or both float32) may be None. ``y`` is created in ``y_dtype`` (default: that of ``x``) if not given; it
     may be ``x``. Returns (y, mean, rstd), the last two float32 [rows]."""
-    p_x, dt_x, ld_x = _rows(x, "x", None, None)
+    p_x, dt_x, ld_x = _rows(x, "x")
     rows, D = x.shape
     ix = x.get_device()
     y = torch.empty(rows, D, dtype=y_dtype or x.dtype, device=x.device) if y is None else y
@@ -869,7 +870,7 @@ def rl_layer_norm_bwd(d_y, x, mean, rstd, ws, weight=None, mask=None, d_x=None, 
     """Gradients of rl_layer_norm_fwd: writes ``d_x`` (created if not given; of ``x``'s dtype; may be ``d_y`` or ``x``)
     and ADDS the sums over the rows to ``d_weight`` and ``d_bias`` (float32 [D], either may be None). Rows with
     ``mask`` (uint8 [rows]) 0 are not read and get a zero gradient. Returns d_x."""
-    p_x, dt_x, ld_x = _rows(x, "x", None, None)
+    p_x, dt_x, ld_x = _rows(x, "x")
     rows, D = x.shape
     ix = x.get_device()
     p_dy, dt_dy, ld_dy = _rows(d_y, "d_y", (rows, D), ix)
@@ -893,7 +894,7 @@ def rl_layer_norm_bwd(d_y, x, mean, rstd, ws, weight=None, mask=None, d_x=None, 
 def rl_embedding_fwd(token_ids, weight, ws, scale=1.0, out=None, out_dtype=None, stream=None):
     """``scale`` times the rows of ``weight`` ([V, D], bf16 or float32, any row stride) that ``token_ids`` (int32 [T])
     name. ``out`` ([T, D]) is created in ``out_dtype`` (default: that of ``weight``) if not given. Returns out."""
-    p_w, dt_w, ld_w = _rows(weight, "weight", None, None)
+    p_w, dt_w, ld_w = _rows(weight, "weight")
     V, D = weight.shape
     ix = weight.get_device()
     T = token_ids.numel()
