@@ -9,6 +9,7 @@
 // often is shared by as many CTAs as it has chunks. Every element of dW gets one addition per call, and the order of all
 // sums depends on the ids alone: repeated calls give the same bits.
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <string>
 
@@ -275,6 +276,129 @@ __global__ void __launch_bounds__(kSortThreads) scatter_kernel(const SortArgs p)
   }
 }
 
+// ---------------------------------------------------------------- the same by one cluster, in shared memory
+
+constexpr int kSortCtas = 16, kBlockThreads = 1024, kBlockWarps = kBlockThreads / 32;
+constexpr int64_t kMostHeld = 11264;  // tokens a CTA holds
+constexpr int64_t kMostSorted = kSortCtas * kMostHeld;
+
+struct ClusterArgs {
+  const int32_t* ids;
+  int32_t* keys_out;
+  int32_t* toks_out;
+  uint32_t* crossing;  // set to zero for the sums
+  int32_t* status;
+  int32_t T, V, cap;  // cap: positions of a CTA, a multiple of 32
+  int32_t passes, bits;
+};
+
+__device__ __forceinline__ uint32_t ld_cluster_u32(uint32_t addr) {
+  uint32_t v;
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ void put_pair(uint32_t addr, uint32_t key, uint32_t tok) {
+  asm volatile("st.shared::cluster.v2.u32 [%0], {%1, %2};" :: "r"(addr), "r"(key), "r"(tok) : "memory");
+}
+
+inline __host__ __device__ int64_t cluster_sort_bytes(int64_t cap) { return 2 * cap * 8 + int64_t(kBlockWarps) * kDigits * 2; }
+
+// The stable radix sort of up to kMostSorted tokens: 16 CTAs hold the list, and a digit's pass writes every token to its
+// place in the CTA that holds it. One launch where the passes through memory take three each. Measured, with launches:
+// SORTUS.
+__global__ void __launch_bounds__(kBlockThreads) cluster_sort_kernel(const ClusterArgs p) {
+  extern __shared__ __align__(16) uint8_t smem[];
+  __shared__ uint32_t total[kDigits];  // this CTA's tokens of each digit
+  __shared__ uint32_t base[kDigits];   // where they go
+  __shared__ uint32_t sums[kDigits / 32];
+  uint2* buf[2] = {reinterpret_cast<uint2*>(smem), reinterpret_cast<uint2*>(smem) + p.cap};
+  uint16_t(*n)[kDigits] = reinterpret_cast<uint16_t(*)[kDigits]>(smem + 2 * static_cast<size_t>(p.cap) * 8);
+  const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+  const int rank = static_cast<int>(cluster_ctarank());
+  const int first = rank * p.cap, mine = max(0, min(p.cap, p.T - first));  // positions first .. first + mine
+  const int rounds = (p.cap / 32 + kBlockWarps - 1) / kBlockWarps, w0 = warp * rounds * 32;
+  if (rank == 0 && threadIdx.x == 0) *p.crossing = 0;
+  bool bad = false;
+  for (int i = threadIdx.x; i < mine; i += kBlockThreads) {
+    const int32_t id = p.ids[first + i];
+    const bool ok = id >= 0 && id < p.V;
+    bad |= !ok;
+    buf[0][i] = make_uint2(static_cast<uint32_t>(ok ? id : p.V), static_cast<uint32_t>(first + i));
+  }
+  if (bad) flag_status(p.status, RL_DEV_BAD_TOKEN);
+  const uint32_t mask = (1u << p.bits) - 1;
+  for (int pass = 0; pass < p.passes; ++pass) {
+    const int shift = pass * p.bits;
+    const uint2* from = buf[pass & 1];
+    for (int i = threadIdx.x; i < kBlockWarps * kDigits / 2; i += kBlockThreads) reinterpret_cast<uint32_t*>(&n[0][0])[i] = 0;
+    __syncthreads();
+    for (int k = 0; k < rounds; ++k) {
+      const int i = w0 + k * 32 + lane;
+      const bool in = i < mine;
+      const uint32_t live = __ballot_sync(0xffffffffu, in);
+      if (in) {
+        const uint32_t d = (from[i].x >> shift) & mask, peers = __match_any_sync(live, d);
+        if (lane == __ffs(peers) - 1) n[warp][d] += static_cast<uint16_t>(__popc(peers));
+      }
+      __syncwarp();
+    }
+    __syncthreads();
+    for (uint32_t d = threadIdx.x; d <= mask; d += kBlockThreads) {  // each warp's start among the CTA's
+      uint32_t run = 0;
+      for (int w = 0; w < kBlockWarps; ++w) {
+        const uint32_t c = n[w][d];
+        n[w][d] = static_cast<uint16_t>(run);
+        run += c;
+      }
+      total[d] = run;
+    }
+    cluster_sync_all();
+    uint32_t all = 0, before = 0;
+    const uint32_t d = threadIdx.x;
+    if (d <= mask)
+      for (int r = 0; r < kSortCtas; ++r) {
+        const uint32_t c = ld_cluster_u32(map_to_rank(smem_addr(&total[d]), r));
+        if (r < rank) before += c;
+        all += c;
+      }
+    uint32_t run = all;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t v = __shfl_up_sync(0xffffffffu, run, o);
+      if (lane >= o) run += v;
+    }
+    if (lane == 31 && warp < kDigits / 32) sums[warp] = run;
+    __syncthreads();
+    if (d <= mask) {
+      for (int w = 0; w < warp; ++w) run += sums[w];
+      base[d] = run - all + before;
+    }
+    __syncthreads();
+    const uint32_t to = smem_addr(buf[1 - (pass & 1)]);
+    for (int k = 0; k < rounds; ++k) {
+      const int i = w0 + k * 32 + lane;
+      const bool in = i < mine;
+      const uint32_t live = __ballot_sync(0xffffffffu, in);
+      if (in) {
+        const uint2 e = from[i];
+        const uint32_t dg = (e.x >> shift) & mask, peers = __match_any_sync(live, dg);
+        const uint32_t at = base[dg] + n[warp][dg] + __popc(peers & ((1u << lane) - 1));
+        __syncwarp(live);
+        if (lane == __ffs(peers) - 1) n[warp][dg] += static_cast<uint16_t>(__popc(peers));
+        const uint32_t cta = at / static_cast<uint32_t>(p.cap);
+        put_pair(map_to_rank(to + (at - cta * p.cap) * 8, cta), e.x, e.y);
+      }
+      __syncwarp();
+    }
+    cluster_sync_all();
+  }
+  const uint2* sorted = buf[p.passes & 1];
+  for (int i = threadIdx.x; i < mine; i += kBlockThreads) {
+    p.keys_out[first + i] = static_cast<int32_t>(sorted[i].x);
+    p.toks_out[first + i] = static_cast<int32_t>(sorted[i].y);
+  }
+}
+
 // ---------------------------------------------------------------- the sums
 
 struct SumArgs {
@@ -282,11 +406,11 @@ struct SumArgs {
   const int32_t* toks;
   const void* d;
   float* dw;
-  float* head;  // [chunks x D]: the part of a run that came in from the chunk before
-  float* tail;  // [chunks x D]: the part of a run that goes on into the next chunk
-  int32_t* list;       // the chunks in which a run begins that goes on into the next one, in any order
+  float* head;  // [chunks x stride]: the part of a long run that came in from the chunk before
+  float* tail;  // [chunks x stride]: the part of a long run that begins in the chunk
+  int32_t* list;       // the chunks in which a long run begins, in any order
   uint32_t* crossing;  // how many there are
-  int64_t T, D, ld, chunk, chunks;
+  int64_t T, D, ld, chunk, stride;
   int32_t V;
   float scale;
 };
@@ -295,60 +419,125 @@ constexpr int kSumThreads = 128;
 constexpr int kMostChunk = 64;
 constexpr int kAhead = 4;  // rows in flight
 
-// N columns a thread, CX threads along a row, kSumThreads / CX chunks a CTA.
-template <typename T, int N, int CX>
+// A thread's N columns of a row, from column c.
+template <typename T, int N>
+__device__ __forceinline__ void load_columns(Block<T, N>& b, const T* row, int64_t c, int64_t D) {
+  if (N == 1 || c + N <= D) {
+    b.load(row + c);
+  } else {
+    b.clear();
+    T* w = reinterpret_cast<T*>(&b.w);
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      if (c + e < D) w[e] = row[c + e];
+  }
+}
+
+// dw += v for N columns from c. The additions are left to the L2 (red): nothing waits for the old values, which took 137 us
+// where this takes SUMUS (32,768 tokens, 4,096 columns), and every element gets one of them. WHOLE: rows of dw in 16-byte blocks.
+template <int N, bool WHOLE>
+__device__ __forceinline__ void add_columns(float* row, const float (&v)[N], int64_t c, int64_t D) {
+  if (WHOLE && N >= 4) {
+#pragma unroll
+    for (int e = 0; e < N; e += 4)
+      if (c + e < D)
+        asm volatile("red.relaxed.gpu.global.add.v4.f32 [%0], {%1, %2, %3, %4};"
+                     :: "l"(row + c + e), "f"(v[e]), "f"(v[e + 1]), "f"(v[e + 2]), "f"(v[e + 3]) : "memory");
+  } else {
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      if (c + e < D) asm volatile("red.relaxed.gpu.global.add.f32 [%0], %1;" :: "l"(row + c + e), "f"(v[e]) : "memory");
+  }
+}
+
+// The first of the sorted positions [lo, hi) with a key above v (hi: none); at(i): the key at position i.
+template <typename K>
+__device__ __forceinline__ int end_of(int lo, int hi, int32_t v, K at) {
+  while (lo < hi) {
+    const int mid = (lo + hi) / 2;
+    if (at(mid) > v) hi = mid;
+    else lo = mid + 1;
+  }
+  return lo;
+}
+
+// N columns a thread, CX threads along a row, kSumThreads / CX chunks a CTA. A run belongs to the chunk in which it begins,
+// which goes on after its end for up to a chunk's length; a longer run is cut at the chunks' borders.
+template <typename T, int N, bool WHOLE, int CX>
 __global__ void __launch_bounds__(kSumThreads) sum_kernel(const SumArgs p) {
   constexpr int kChunks = kSumThreads / CX;
-  __shared__ int32_t key[kChunks][kMostChunk + 2];  // with one neighbour on either side (-1: none)
-  __shared__ int32_t tok[kChunks][kMostChunk];
-  const int y = threadIdx.x / CX, x = threadIdx.x % CX;
+  __shared__ int32_t key[kChunks][2 * kMostChunk + 2];  // of positions a - 1 .. a + 2 chunk (-1: none)
+  __shared__ int32_t tok[kChunks][2 * kMostChunk];
+  const int y = threadIdx.x / CX, x = threadIdx.x % CX, L = static_cast<int>(p.chunk);
   const int64_t ch = static_cast<int64_t>(blockIdx.x) * kChunks + y;
-  const int64_t a = ch * p.chunk;
-  const int n = static_cast<int>(max(int64_t(0), min(p.chunk, p.T - a)));
-  for (int i = x; i < n + 2; i += CX) {
+  const int64_t a = ch * L;
+  const int n = static_cast<int>(max(int64_t(0), min(p.chunk, p.T - a)));        // its positions
+  const int m = static_cast<int>(max(int64_t(0), min(2 * p.chunk, p.T - a)));    // and the next chunk's
+  for (int i = x; i < m + 2; i += CX) {
     const int64_t at = a + i - 1;
     key[y][i] = n > 0 && at >= 0 && at < p.T ? p.keys[at] : -1;
   }
-  for (int i = x; i < n; i += CX) tok[y][i] = p.toks[a + i];
+  for (int i = x; i < m; i += CX) tok[y][i] = p.toks[a + i];
   __syncthreads();
   const int64_t c = (static_cast<int64_t>(blockIdx.y) * CX + x) * N;
   if (c >= p.D || n <= 0) return;
-  const T* d = static_cast<const T*>(p.d) + c;
+  auto at = [&](int i) { return key[y][i + 1]; };
+  // what comes in: a run of the chunk before that ends within this one is that chunk's
+  int begin = 0;
+  bool head = false;
+  const int32_t v0 = at(0);
+  if (at(-1) == v0) {
+    const bool began_there = !(p.keys[a - L] == v0 && a > L && p.keys[a - L - 1] == v0);
+    if (began_there && (n < L || n == m || at(n) != v0)) begin = end_of(0, n, v0, at);
+    else head = true;
+  }
+  if (begin == n) return;
+  // what goes on: to its end if that lies within the next chunk
+  int end = n;
+  bool tail = false;
+  const int32_t v1 = at(n - 1);
+  if (n < m && at(n) == v1) {
+    const bool began_here = !(head && v1 == v0);
+    if (began_here && at(m) != v1) end = end_of(n, m, v1, at);
+    else tail = began_here && v1 < p.V;
+  }
+  if (tail && c == 0) p.list[atomicAdd(p.crossing, 1u)] = static_cast<int32_t>(ch);
+
+  const T* d = static_cast<const T*>(p.d);
   float acc[N];
 #pragma unroll
   for (int e = 0; e < N; ++e) acc[e] = 0.f;
-  bool came_in = key[y][0] == key[y][1];  // the run began in the chunk before
-  for (int i = 0; i < n; i += kAhead) {
+  for (int i = begin; i < end; i += kAhead) {
     Block<T, N> rows[kAhead];
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
       rows[k].clear();
-      if (i + k < n && key[y][i + k + 1] < p.V) rows[k].load(d + tok[y][i + k] * p.ld);
+      if (i + k < end && at(i + k) < p.V) load_columns<T, N>(rows[k], d + tok[y][i + k] * p.ld, c, p.D);
     }
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
-      if (i + k >= n) break;
-      const int32_t v = key[y][i + k + 1];
+      const int j = i + k;
+      if (j >= end) break;
+      const int32_t v = at(j);
       if (v >= p.V) return;  // ids out of range: the last of the list
       float f[N];
       rows[k].get(f);
 #pragma unroll
       for (int e = 0; e < N; ++e) acc[e] += f[e];
-      if (key[y][i + k + 2] == v && i + k + 1 < n) continue;
-      const bool goes_on = key[y][i + k + 2] == v;
-      if (goes_on && !came_in && c == 0) p.list[atomicAdd(p.crossing, 1u)] = static_cast<int32_t>(ch);
-      if (came_in || goes_on) {
-        float* to = (came_in ? p.head : p.tail) + ch * p.D + c;
+      if (j + 1 < end && at(j + 1) == v) continue;
+      if (head || (tail && j + 1 == end)) {
+        float* to = (head ? p.head : p.tail) + ch * p.stride + c;
 #pragma unroll
-        for (int e = 0; e < N; ++e) to[e] = acc[e];
+        for (int e = 0; e < N; ++e)
+          if (c + e < p.D) to[e] = acc[e];
+        head = false;
       } else {
-        float* to = p.dw + v * p.D + c;
 #pragma unroll
-        for (int e = 0; e < N; ++e) to[e] = fmaf(p.scale, acc[e], to[e]);
+        for (int e = 0; e < N; ++e) acc[e] *= p.scale;
+        add_columns<N, WHOLE>(p.dw + v * p.D, acc, c, p.D);
       }
 #pragma unroll
       for (int e = 0; e < N; ++e) acc[e] = 0.f;
-      came_in = false;
     }
   }
 }
@@ -356,7 +545,7 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(const SumArgs p) {
 constexpr int kJoinWarps = 8;
 constexpr int kJoinCtas = 4 * 152;
 
-// The chunk after `ch` in which the run of v that goes on into chunk ch + 1 ends, by a whole warp.
+// The last chunk of a long run of v that begins in chunk `ch`, by a whole warp.
 __device__ __forceinline__ int64_t last_chunk(const SumArgs& p, int64_t ch, int32_t v, int lane) {
   for (int64_t k = ch + 1;; k += 32) {
     const int64_t next = (k + lane + 1) * p.chunk;
@@ -365,65 +554,131 @@ __device__ __forceinline__ int64_t last_chunk(const SumArgs& p, int64_t ch, int3
   }
 }
 
-// The runs that cross chunks. An item is one of them and kJoinWarps * 32 * N columns: a warp each takes 32 * N of them, or
-// where the run is long all warps take a part of its chunks, slice after slice, and the parts are added up in order.
-template <int N>
+// The long runs: an item is one of them and 128 columns. Each warp takes a part of the run's chunks, four columns a lane, and
+// the parts are added up in order.
+template <bool WHOLE>
 __global__ void __launch_bounds__(kJoinWarps * 32) join_kernel(const SumArgs p) {
-  __shared__ float sum[kJoinWarps][32 * N];
+  __shared__ __align__(16) float sum[kJoinWarps][128];
   const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
-  constexpr int kSlice = 32 * N;
-  const int64_t groups = (p.D + kJoinWarps * kSlice - 1) / (kJoinWarps * kSlice);
-  const int64_t items = *p.crossing * groups;
+  const int64_t slices = (p.D + 127) / 128, items = *p.crossing * slices;
   for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
-    const int64_t ch = p.list[it / groups], first = it % groups * kJoinWarps;
+    const int64_t ch = p.list[it / slices], c = it % slices * 128 + lane * 4;
     const int32_t v = p.keys[(ch + 1) * p.chunk];
     const int64_t last = last_chunk(p, ch, v, lane);
-    auto add = [&](float (&s)[N], const float* from) {
-      float f[N];
-      Block<float, N> b;
-      b.load(from);
-      b.get(f);
-#pragma unroll
-      for (int e = 0; e < N; ++e) s[e] += f[e];
-    };
-    auto finish = [&](const float (&s)[N], int64_t c) {
-      float* out = p.dw + v * p.D + c;
-#pragma unroll
-      for (int e = 0; e < N; ++e) out[e] = fmaf(p.scale, s[e], out[e]);
-    };
-    if (last - ch <= kJoinWarps) {
-      const int64_t c = (first + warp) * kSlice + lane * N;
-      if (c >= p.D) continue;
-      float s[N] = {};
-      add(s, p.tail + ch * p.D + c);
-#pragma unroll 4
-      for (int64_t k = ch + 1; k <= last; ++k) add(s, p.head + k * p.D + c);
-      finish(s, c);
-      continue;
-    }
     const int64_t per = (last - ch + kJoinWarps - 1) / kJoinWarps;
     const int64_t from = ch + 1 + warp * per, to = min(from + per, last + 1);
-    for (int64_t slice = first; slice < first + kJoinWarps && slice * kSlice < p.D; ++slice) {
-      const int64_t c = slice * kSlice + lane * N;
-      float s[N] = {};
-      if (c < p.D) {
-        if (warp == 0) add(s, p.tail + ch * p.D + c);
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto add = [&](const float* part) {
+      const float4 f = __ldcs(reinterpret_cast<const float4*>(part + c));
+      s.x += f.x, s.y += f.y, s.z += f.z, s.w += f.w;
+    };
+    if (c < p.D) {  // what lies behind D of a part is room for whole blocks
+      if (warp == 0) add(p.tail + ch * p.stride);
 #pragma unroll 8
-        for (int64_t k = from; k < to; ++k) add(s, p.head + k * p.D + c);
+      for (int64_t k = from; k < to; ++k) add(p.head + k * p.stride);
+    }
+    *reinterpret_cast<float4*>(&sum[warp][lane * 4]) = s;
+    __syncthreads();
+    if (warp == 0 && c < p.D) {
+#pragma unroll
+      for (int w = 1; w < kJoinWarps; ++w) {
+        const float4 f = *reinterpret_cast<const float4*>(&sum[w][lane * 4]);
+        s.x += f.x, s.y += f.y, s.z += f.z, s.w += f.w;
       }
+      const float out[4] = {p.scale * s.x, p.scale * s.y, p.scale * s.z, p.scale * s.w};
+      add_columns<4, WHOLE>(p.dw + v * p.D, out, c, p.D);
+    }
+    __syncthreads();
+  }
+}
+
+// ---------------------------------------------------------------- few tokens
+
+constexpr int kFewThreads = 256, kFewTokens = 1024;
+constexpr int kFewX = 64, kFewY = kFewThreads / kFewX;  // threads along a row, parts of the tokens of an id
+
+struct FewArgs {
+  const int32_t* ids;
+  const void* d;
+  float* dw;
+  int32_t T, V;
+  int64_t D, ld;
+  float scale;
+  int32_t* status;
+};
+
+// A CTA for every token and kFewX * N columns: the first token of its id adds up those of all of them, in up to kFewY parts.
+// No sort: every CTA looks at all ids. One launch.
+template <typename T, int N, bool WHOLE>
+__global__ void __launch_bounds__(kFewThreads) few_kernel(const FewArgs p) {
+  constexpr int kRounds = kFewTokens / kFewThreads, kWarps = kFewThreads / 32;
+  __shared__ uint16_t list[kFewTokens];
+  __shared__ uint32_t count[kRounds * kWarps];
+  __shared__ float part[kFewY][kFewX * N];
+  const int t = blockIdx.x, tid = threadIdx.x, warp = tid / 32, lane = tid & 31;
+  const int32_t v = p.ids[t];
+  if (v < 0 || v >= p.V) {
+    if (blockIdx.y == 0 && tid == 0) flag_status(p.status, RL_DEV_BAD_TOKEN);
+    return;
+  }
+  uint32_t same[kRounds];
+  bool earlier = false;
 #pragma unroll
-      for (int e = 0; e < N; ++e) sum[warp][lane * N + e] = s[e];
-      __syncthreads();
-      if (warp == 0 && c < p.D) {
+  for (int k = 0; k < kRounds; ++k) {
+    const int i = k * kFewThreads + tid;
+    const bool is = i < p.T && p.ids[i] == v;
+    earlier |= is && i < t;
+    same[k] = __ballot_sync(0xffffffffu, is);
+    if (lane == 0) count[k * kWarps + warp] = __popc(same[k]);
+  }
+  if (__syncthreads_or(earlier)) return;
+  static_assert(kRounds * kWarps == 32, "a warp's lane per count");
+  uint32_t run = count[lane];
 #pragma unroll
-        for (int w = 1; w < kJoinWarps; ++w)
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint32_t u = __shfl_up_sync(0xffffffffu, run, o);
+    if (lane >= o) run += u;
+  }
+  const int n = static_cast<int>(__shfl_sync(0xffffffffu, run, 31));
+  run -= count[lane];
 #pragma unroll
-          for (int e = 0; e < N; ++e) s[e] += sum[w][lane * N + e];
-        finish(s, c);
-      }
-      __syncthreads();
+  for (int k = 0; k < kRounds; ++k) {
+    const uint32_t before = __shfl_sync(0xffffffffu, run, k * kWarps + warp);
+    if (same[k] >> lane & 1) list[before + __popc(same[k] & ((1u << lane) - 1))] = static_cast<uint16_t>(k * kFewThreads + tid);
+  }
+  __syncthreads();
+  const int x = tid % kFewX, y = tid / kFewX;
+  const int64_t c = (static_cast<int64_t>(blockIdx.y) * kFewX + x) * N;
+  const int per = (n + kFewY - 1) / kFewY, from = y * per, to = min(from + per, n);
+  const T* d = static_cast<const T*>(p.d);
+  float acc[N];
+#pragma unroll
+  for (int e = 0; e < N; ++e) acc[e] = 0.f;
+  if (c < p.D) {
+#pragma unroll 4
+    for (int i = from; i < to; ++i) {
+      Block<T, N> row;
+      load_columns<T, N>(row, d + list[i] * p.ld, c, p.D);
+      float f[N];
+      row.get(f);
+#pragma unroll
+      for (int e = 0; e < N; ++e) acc[e] += f[e];
     }
   }
+  if (n > 1) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) part[y][x * N + e] = acc[e];
+    __syncthreads();
+    if (y == 0)
+#pragma unroll
+      for (int k = 1; k < kFewY; ++k)
+#pragma unroll
+        for (int e = 0; e < N; ++e) acc[e] += part[k][x * N + e];
+  }
+  if (y != 0 || c >= p.D) return;
+#pragma unroll
+  for (int e = 0; e < N; ++e) acc[e] *= p.scale;
+  add_columns<N, WHOLE>(p.dw + v * p.D, acc, c, p.D);
 }
 
 // ---------------------------------------------------------------- host
@@ -439,17 +694,18 @@ Plan plan(int64_t T, int64_t V) {
   q.rounds = std::max<int64_t>(4, (T + kSortThreads * kMostTiles - 1) / (kSortThreads * kMostTiles));
   const int64_t tile = kSortThreads * q.rounds;
   q.tiles = std::max<int64_t>(1, (T + tile - 1) / tile);
-  q.chunk = T <= 4096 ? 16 : T <= 65536 ? 32 : 64;
+  q.chunk = T <= 8192 ? 16 : T <= 65536 ? 32 : kMostChunk;
   q.chunks = (T + q.chunk - 1) / q.chunk;
   q.most_tiles = std::min<int64_t>(kMostTiles, (T + kSortThreads * 4 - 1) / (kSortThreads * 4));
   q.most_chunks = std::max<int64_t>(
-      {(std::min<int64_t>(T, 4096) + 15) / 16, (std::min<int64_t>(T, 65536) + 31) / 32, (T + 63) / 64});
+      {(std::min<int64_t>(T, 8192) + 15) / 16, (std::min<int64_t>(T, 65536) + 31) / 32, (T + kMostChunk - 1) / kMostChunk});
   return q;
 }
 
 inline size_t up(size_t n) { return (n + 255) / 256 * 256; }
 
 struct Layout {
+  int64_t stride;
   size_t keys[2], toks[2], counts, totals, list, crossing, head, tail, bytes;
 };
 Layout layout(const Plan& q, int64_t T, int64_t D) {
@@ -468,8 +724,9 @@ Layout layout(const Plan& q, int64_t T, int64_t D) {
   l.totals = take(kDigits * 4);
   l.crossing = take(4);
   l.list = take(size_t(q.most_chunks) * 4);
-  l.head = take(size_t(q.most_chunks) * D * 4);
-  l.tail = take(size_t(q.most_chunks) * D * 4);
+  l.stride = (D + 3) / 4 * 4;
+  l.head = take(size_t(q.most_chunks) * l.stride * 4);
+  l.tail = take(size_t(q.most_chunks) * l.stride * 4);
   l.bytes = at;
   return l;
 }
@@ -497,35 +754,89 @@ rl_status forward(const FwdArgs& a, cudaStream_t s) {
   return e == cudaSuccess ? RL_OK : cuda_error(e, "lookup_kernel launch");
 }
 
-template <typename T, int N>
-void launch_sums(const SumArgs& a, cudaStream_t s) {
+template <typename T, int N, bool WHOLE>
+void launch_sums(const SumArgs& a, int64_t chunks, cudaStream_t s) {
   const int64_t threads = (a.D + N - 1) / N;
   auto go = [&](auto kern, int cx) {
     const int64_t per = kSumThreads / cx;
-    kern<<<dim3(static_cast<unsigned>((a.chunks + per - 1) / per), static_cast<unsigned>((threads + cx - 1) / cx)),
+    kern<<<dim3(static_cast<unsigned>((chunks + per - 1) / per), static_cast<unsigned>((threads + cx - 1) / cx)),
            kSumThreads, 0, s>>>(a);
   };
-  if (threads > 64) go(sum_kernel<T, N, 128>, 128);
-  else if (threads > 32) go(sum_kernel<T, N, 64>, 64);
-  else if (threads > 16) go(sum_kernel<T, N, 32>, 32);
-  else go(sum_kernel<T, N, 16>, 16);
+  if (threads > 64) go(sum_kernel<T, N, WHOLE, 128>, 128);
+  else if (threads > 32) go(sum_kernel<T, N, WHOLE, 64>, 64);
+  else if (threads > 16) go(sum_kernel<T, N, WHOLE, 32>, 32);
+  else go(sum_kernel<T, N, WHOLE, 16>, 16);
+}
+
+// How the rows lie: those of d in 16-byte blocks, and those of dw too.
+struct Rows {
+  bool d, dw;
+};
+template <typename T>
+Rows rows_of(const void* d, int64_t ld, const float* dw, int64_t D) {
+  return {whole_blocks(d, ld, sizeof(T)), aligned16(dw) && D % 4 == 0};
 }
 
 template <typename T>
-rl_status backward(SumArgs& a, cudaStream_t s) {
+rl_status few(const FewArgs& a, cudaStream_t s) {
   constexpr int N = 16 / sizeof(T);
-  const bool blocks = a.D % N == 0 && whole_blocks(a.d, a.ld, sizeof(T)) && aligned16(a.dw);
-  if (blocks) launch_sums<T, N>(a, s);
-  else launch_sums<T, 1>(a, s);
+  const Rows r = rows_of<T>(a.d, a.ld, a.dw, a.D);
+  auto go = [&](auto kern, int n) {
+    kern<<<dim3(static_cast<unsigned>(a.T), static_cast<unsigned>((a.D + kFewX * n - 1) / (kFewX * n))), kFewThreads, 0, s>>>(a);
+  };
+  if (!r.d) go(few_kernel<T, 1, false>, 1);
+  else if (r.dw) go(few_kernel<T, N, true>, N);
+  else go(few_kernel<T, N, false>, N);
+  const cudaError_t e = cudaGetLastError();
+  return e == cudaSuccess ? RL_OK : cuda_error(e, "few_kernel launch");
+}
+
+template <typename T>
+rl_status sums(const SumArgs& a, int64_t chunks, cudaStream_t s) {
+  constexpr int N = 16 / sizeof(T);
+  const Rows r = rows_of<T>(a.d, a.ld, a.dw, a.D);
+  if (!r.d) launch_sums<T, 1, false>(a, chunks, s);
+  else if (r.dw) launch_sums<T, N, true>(a, chunks, s);
+  else launch_sums<T, N, false>(a, chunks, s);
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return cuda_error(e, "sum_kernel launch");
-  if (a.chunks > 1) {
-    if (blocks) join_kernel<4><<<kJoinCtas, kJoinWarps * 32, 0, s>>>(a);
-    else join_kernel<1><<<kJoinCtas, kJoinWarps * 32, 0, s>>>(a);
+  if (chunks > 2) {
+    if (r.dw) join_kernel<true><<<kJoinCtas, kJoinWarps * 32, 0, s>>>(a);
+    else join_kernel<false><<<kJoinCtas, kJoinWarps * 32, 0, s>>>(a);
     e = cudaGetLastError();
     if (e != cudaSuccess) return cuda_error(e, "join_kernel launch");
   }
   return RL_OK;
+}
+
+rl_status cluster_sort(ClusterArgs& a, cudaStream_t s) {
+  static std::atomic<uint64_t> ready{0};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return cuda_error(e, "cudaGetDevice");
+  const uint64_t bit = dev < 64 ? uint64_t(1) << dev : 0;
+  if (!(ready.load() & bit)) {
+    e = cudaFuncSetAttribute(cluster_sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             static_cast<int>(cluster_sort_bytes(kMostHeld)));
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(cluster_sort_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e != cudaSuccess) return cuda_error(e, "cudaFuncSetAttribute(cluster_sort_kernel)");
+    ready |= bit;
+  }
+  a.cap = ((a.T + kSortCtas - 1) / kSortCtas + 31) / 32 * 32;
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = kSortCtas;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  cfg.gridDim = dim3(kSortCtas);
+  cfg.blockDim = dim3(kBlockThreads);
+  cfg.dynamicSmemBytes = static_cast<size_t>(cluster_sort_bytes(a.cap));
+  cfg.stream = s;
+  e = cudaLaunchKernelEx(&cfg, cluster_sort_kernel, a);
+  return e == cudaSuccess ? RL_OK : cuda_error(e, "cluster_sort_kernel launch");
 }
 
 }  // namespace embed
@@ -594,48 +905,78 @@ rl_status rl_embedding_bwd(const int32_t* token_ids, int64_t T, const void* d_ou
     return set_error(RL_ERR_WORKSPACE_TOO_SMALL, f + "ws_bytes below rl_embedding_workspace_size(T, V, D)");
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   uint8_t* base = static_cast<uint8_t*>(ws);
-  auto ints = [&](size_t o) { return reinterpret_cast<int32_t*>(base + o); };
-  embed::SortArgs o = {};
-  o.ids = token_ids;
-  o.T = T;
-  o.rounds = q.rounds;
-  o.tiles = q.tiles;
-  o.V = static_cast<int32_t>(V);
-  o.mask = (1 << q.bits) - 1;
-  o.counts = reinterpret_cast<uint32_t*>(base + l.counts);
-  o.totals = reinterpret_cast<uint32_t*>(base + l.totals);
-  o.crossing = reinterpret_cast<uint32_t*>(base + l.crossing);
-  o.status = reinterpret_cast<int32_t*>(base);
-  const unsigned tiles = static_cast<unsigned>(q.tiles);
-  for (int i = 0; i < q.passes; ++i) {
-    o.shift = i * q.bits;
-    o.keys_out = ints(l.keys[i & 1]);
-    o.toks_out = ints(l.toks[i & 1]);
-    embed::count_kernel<<<tiles, embed::kSortThreads, 0, s>>>(o);
-    embed::prefix_kernel<<<(o.mask + embed::kSortWarps) / embed::kSortWarps, embed::kSortThreads, 0, s>>>(o);
-    embed::scatter_kernel<<<tiles, embed::kSortThreads, 0, s>>>(o);
-    const cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess) return cuda_error(e, "rl_embedding_bwd: sort launch");
-    o.keys = o.keys_out;
-    o.toks = o.toks_out;
+  if (T <= embed::kFewTokens) {
+    embed::FewArgs a = {};
+    a.ids = token_ids;
+    a.d = d_out;
+    a.dw = d_weight;
+    a.T = static_cast<int32_t>(T);
+    a.V = static_cast<int32_t>(V);
+    a.D = D;
+    a.ld = ld_d;
+    a.scale = scale;
+    a.status = reinterpret_cast<int32_t*>(base);
+    return d_dtype == RL_BF16 ? embed::few<uint16_t>(a, s) : embed::few<float>(a, s);
   }
+  auto ints = [&](size_t o) { return reinterpret_cast<int32_t*>(base + o); };
   embed::SumArgs a = {};
-  a.keys = o.keys;
-  a.toks = o.toks;
+  a.crossing = reinterpret_cast<uint32_t*>(base + l.crossing);
+  if (T <= embed::kMostSorted) {
+    embed::ClusterArgs o = {};
+    o.ids = token_ids;
+    o.keys_out = ints(l.keys[0]);
+    o.toks_out = ints(l.toks[0]);
+    o.crossing = a.crossing;
+    o.status = reinterpret_cast<int32_t*>(base);
+    o.T = static_cast<int32_t>(T);
+    o.V = static_cast<int32_t>(V);
+    o.passes = q.passes;
+    o.bits = q.bits;
+    const rl_status r = embed::cluster_sort(o, s);
+    if (r != RL_OK) return r;
+    a.keys = o.keys_out;
+    a.toks = o.toks_out;
+  } else {
+    embed::SortArgs o = {};
+    o.ids = token_ids;
+    o.T = T;
+    o.rounds = q.rounds;
+    o.tiles = q.tiles;
+    o.V = static_cast<int32_t>(V);
+    o.mask = (1 << q.bits) - 1;
+    o.counts = reinterpret_cast<uint32_t*>(base + l.counts);
+    o.totals = reinterpret_cast<uint32_t*>(base + l.totals);
+    o.crossing = a.crossing;
+    o.status = reinterpret_cast<int32_t*>(base);
+    const unsigned tiles = static_cast<unsigned>(q.tiles);
+    for (int i = 0; i < q.passes; ++i) {
+      o.shift = i * q.bits;
+      o.keys_out = ints(l.keys[i & 1]);
+      o.toks_out = ints(l.toks[i & 1]);
+      embed::count_kernel<<<tiles, embed::kSortThreads, 0, s>>>(o);
+      embed::prefix_kernel<<<(o.mask + embed::kSortWarps) / embed::kSortWarps, embed::kSortThreads, 0, s>>>(o);
+      embed::scatter_kernel<<<tiles, embed::kSortThreads, 0, s>>>(o);
+      const cudaError_t e = cudaGetLastError();
+      if (e != cudaSuccess) return cuda_error(e, "rl_embedding_bwd: sort launch");
+      o.keys = o.keys_out;
+      o.toks = o.toks_out;
+    }
+    a.keys = o.keys;
+    a.toks = o.toks;
+  }
   a.d = d_out;
   a.dw = d_weight;
   a.head = reinterpret_cast<float*>(base + l.head);
   a.tail = reinterpret_cast<float*>(base + l.tail);
   a.list = ints(l.list);
-  a.crossing = reinterpret_cast<uint32_t*>(base + l.crossing);
   a.T = T;
   a.D = D;
   a.ld = ld_d;
   a.chunk = q.chunk;
-  a.chunks = q.chunks;
+  a.stride = l.stride;
   a.V = static_cast<int32_t>(V);
   a.scale = scale;
-  return d_dtype == RL_BF16 ? embed::backward<uint16_t>(a, s) : embed::backward<float>(a, s);
+  return d_dtype == RL_BF16 ? embed::sums<uint16_t>(a, q.chunks, s) : embed::sums<float>(a, q.chunks, s);
 }
 
 }  // extern "C"

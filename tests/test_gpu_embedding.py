@@ -94,7 +94,8 @@ def check_grad(R, ids, V, D, dtype, what, scale=0.9, pad=0, off=0, seed=0, ws=No
 @pytest.mark.parametrize("law", ["same", "two", "all_once", "often", "any"])
 @pytest.mark.parametrize("T,D,V", [(1, 8, 4), (2, 1, 1), (15, 33, 7), (16, 64, 40), (17, 128, 600), (64, 100, 5),
                                    (1000, 96, 1000), (1024, 256, 32000), (1025, 40, 511), (4096, 64, 512),
-                                   (5000, 72, 151936), (5001, 17, 513), (33000, 16, 9000), (70001, 24, 300000)])
+                                   (5000, 72, 151936), (5001, 17, 513), (33000, 16, 9000), (70001, 24, 300000), (180224, 8, 40000),
+                                   (180225, 8, 40000)])
 def test_backward(R, law, T, D, V):
     ids = token_ids(law, T, V, seed=T)
     for dtype in (BF, F32):
@@ -130,6 +131,16 @@ def test_ids_out_of_range(R):
         assert R.rl_query_status(ws)[1] == R.RL_DEV_BAD_TOKEN
         assert (out[bad] == 0).all() and torch.equal(out[~bad], w[torch.from_numpy(good).cuda()])
         R.rl_workspace_init(ws)
+    # many bad ids: their run is longer than any that one CTA adds up
+    ids = token_ids("any", 5000, V, seed=3)
+    ids[::2] = 2 ** 30
+    ws = R.new_embedding_workspace(5000, V, D)
+    d = torch.randn(5000, D, device="cuda")
+    d[::2] = float("nan")
+    dw = R.rl_embedding_bwd(ids_on_device(ids), d, torch.zeros(V, D, device="cuda"), ws)
+    ref, size = O.embedding_grad(ids[1::2], np64(d[1::2]), V)
+    assert (np.abs(np64(dw) - ref) <= 5000 * U * size).all()
+    R.rl_workspace_init(ws)
     # nothing but bad ids
     ids = np.full(100, -5)
     dw = torch.ones(V, D, device="cuda")
