@@ -281,6 +281,8 @@ __global__ void __launch_bounds__(kSortThreads) scatter_kernel(const SortArgs p)
 constexpr int kSortCtas = 16, kBlockThreads = 1024, kBlockWarps = kBlockThreads / 32;
 constexpr int64_t kMostHeld = 11264;  // tokens a CTA holds
 constexpr int64_t kMostSorted = kSortCtas * kMostHeld;
+constexpr int kMostRounds = static_cast<int>(kMostHeld / kBlockThreads);
+static_assert(kMostHeld % kBlockThreads == 0 && kMostHeld < 65536, "rounds of a warp, and its counters of 16 bits");
 
 struct ClusterArgs {
   const int32_t* ids;
@@ -332,35 +334,50 @@ __global__ void __launch_bounds__(kBlockThreads) cluster_sort_kernel(const Clust
     const uint2* from = buf[pass & 1];
     for (int i = threadIdx.x; i < kBlockWarps * kDigits / 2; i += kBlockThreads) reinterpret_cast<uint32_t*>(&n[0][0])[i] = 0;
     __syncthreads();
-    for (int k = 0; k < rounds; ++k) {
+    uint32_t peers[kMostRounds];  // the lanes with the same digit, round by round
+#pragma unroll
+    for (int k = 0; k < kMostRounds; ++k) {
+      if (k >= rounds) break;
       const int i = w0 + k * 32 + lane;
       const bool in = i < mine;
       const uint32_t live = __ballot_sync(0xffffffffu, in);
+      peers[k] = 0;
       if (in) {
-        const uint32_t d = (from[i].x >> shift) & mask, peers = __match_any_sync(live, d);
-        if (lane == __ffs(peers) - 1) n[warp][d] += static_cast<uint16_t>(__popc(peers));
+        const uint32_t d = (from[i].x >> shift) & mask;
+        peers[k] = __match_any_sync(live, d);
+        if (lane == __ffs(peers[k]) - 1) n[warp][d] += static_cast<uint16_t>(__popc(peers[k]));
       }
       __syncwarp();
     }
     __syncthreads();
     for (uint32_t d = threadIdx.x; d <= mask; d += kBlockThreads) {  // each warp's start among the CTA's
       uint32_t run = 0;
-      for (int w = 0; w < kBlockWarps; ++w) {
-        const uint32_t c = n[w][d];
-        n[w][d] = static_cast<uint16_t>(run);
-        run += c;
+#pragma unroll
+      for (int w0 = 0; w0 < kBlockWarps; w0 += 16) {
+        uint32_t c[16];
+#pragma unroll
+        for (int w = 0; w < 16; ++w) c[w] = n[w0 + w][d];
+#pragma unroll
+        for (int w = 0; w < 16; ++w) {
+          n[w0 + w][d] = static_cast<uint16_t>(run);
+          run += c[w];
+        }
       }
       total[d] = run;
     }
     cluster_sync_all();
     uint32_t all = 0, before = 0;
     const uint32_t d = threadIdx.x;
-    if (d <= mask)
+    if (d <= mask) {
+      uint32_t c[kSortCtas];
+#pragma unroll
+      for (int r = 0; r < kSortCtas; ++r) c[r] = ld_cluster_u32(map_to_rank(smem_addr(&total[d]), r));
+#pragma unroll
       for (int r = 0; r < kSortCtas; ++r) {
-        const uint32_t c = ld_cluster_u32(map_to_rank(smem_addr(&total[d]), r));
-        if (r < rank) before += c;
-        all += c;
+        before += r < rank ? c[r] : 0;
+        all += c[r];
       }
+    }
     uint32_t run = all;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -370,21 +387,21 @@ __global__ void __launch_bounds__(kBlockThreads) cluster_sort_kernel(const Clust
     if (lane == 31 && warp < kDigits / 32) sums[warp] = run;
     __syncthreads();
     if (d <= mask) {
-      for (int w = 0; w < warp; ++w) run += sums[w];
+#pragma unroll
+      for (int w = 0; w < kDigits / 32; ++w) run += w < warp ? sums[w] : 0;
       base[d] = run - all + before;
     }
     __syncthreads();
     const uint32_t to = smem_addr(buf[1 - (pass & 1)]);
-    for (int k = 0; k < rounds; ++k) {
-      const int i = w0 + k * 32 + lane;
-      const bool in = i < mine;
-      const uint32_t live = __ballot_sync(0xffffffffu, in);
-      if (in) {
-        const uint2 e = from[i];
-        const uint32_t dg = (e.x >> shift) & mask, peers = __match_any_sync(live, dg);
-        const uint32_t at = base[dg] + n[warp][dg] + __popc(peers & ((1u << lane) - 1));
-        __syncwarp(live);
-        if (lane == __ffs(peers) - 1) n[warp][dg] += static_cast<uint16_t>(__popc(peers));
+#pragma unroll
+    for (int k = 0; k < kMostRounds; ++k) {
+      if (k >= rounds) break;
+      const uint2 e = peers[k] != 0 ? from[w0 + k * 32 + lane] : make_uint2(0u, 0u);
+      const uint32_t dg = (e.x >> shift) & mask;
+      const uint32_t at = base[dg] + n[warp][dg] + __popc(peers[k] & ((1u << lane) - 1));
+      __syncwarp();
+      if (peers[k] != 0) {
+        if (lane == __ffs(peers[k]) - 1) n[warp][dg] += static_cast<uint16_t>(__popc(peers[k]));
         const uint32_t cta = at / static_cast<uint32_t>(p.cap);
         put_pair(map_to_rank(to + (at - cta * p.cap) * 8, cta), e.x, e.y);
       }
@@ -417,7 +434,7 @@ struct SumArgs {
 
 constexpr int kSumThreads = 128;
 constexpr int kMostChunk = 64;
-constexpr int kAhead = 4;  // rows in flight
+constexpr int kAhead = 8;  // rows in flight
 
 // A thread's N columns of a row, from column c.
 template <typename T, int N>
