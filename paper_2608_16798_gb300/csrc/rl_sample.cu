@@ -100,7 +100,6 @@ __device__ __forceinline__ void put_u1(uint32_t addr, uint32_t a) {
 struct Border {
   uint32_t key, m, above;
   unsigned long long mass, unit;  // of the entries above; of one entry equal to it
-  int32_t hit;
 };
 
 template <int WARPS>
@@ -110,11 +109,12 @@ struct Shared {
   float sum[kSegs];      // of the kept weights above the threshold
   uint32_t above[kSegs]; // kept entries above it
   uint32_t equal[kSegs]; // entries equal to it
-  uint32_t count[kBins]; // this CTA's
-  unsigned long long mass[kBins];
+  alignas(16) uint32_t count[kBins];  // this CTA's
+  alignas(16) unsigned long long mass[kBins];
   uint32_t warp_count[WARPS];
   unsigned long long warp_mass[WARPS];
   Border found;
+  int32_t bin;  // that found is of (-1: none)
   uint64_t bar[WARPS];
 };
 
@@ -122,7 +122,6 @@ struct Shared {
 struct Level {
   uint32_t d0;
   int shift;
-  __device__ __forceinline__ bool operator==(const Level& o) const { return d0 == o.d0 && shift == o.shift; }
 };
 
 template <typename T, int WARPS>
@@ -134,125 +133,197 @@ struct Row {
   uint32_t top;  // the largest entry's key
   int C;
   bool masses;   // weights are wanted
-  Level level{0xffffffffu, 0};  // what the bins hold
   static constexpr int N = Elem<T>::N, kThreads = WARPS * 32, kOwn = kBins / kThreads;
   static constexpr int kSingle = sizeof(T) == 2 ? kBf16Shift : 0;  // bins of at most these patterns hold one value
+  Level level{0u, -1};  // what the bins hold
+  uint32_t above = 0;   // entries before the level's first bin
+  unsigned long long mass = 0;
+  uint32_t n[kOwn], run_n, all_n;            // this thread's bins over the cluster; entries before them; all bins'
+  unsigned long long w[kOwn], run_w, all_w;  // the same for masses
 
   __device__ __forceinline__ float weight(float z) const { return ex2(exponent(z, all.m, c)); }
 
-  // Counts the cluster's entries by the bins of `to`.
-  __device__ void count(const Level& to) {
-    const int lane = threadIdx.x & 31;
-    const bool weigh = masses && to.shift > kSingle;
-    if (level.d0 != 0xffffffffu) cluster_sync_all();  // the other CTAs have read the last level's
-    for (int i = threadIdx.x; i < kBins; i += kThreads) {
-      sh.count[i] = 0;
-      sh.mass[i] = 0;
-    }
-    __syncthreads();
-    const int nb = mine.blocks();
+  // bf16 entries by their patterns, to bins of one step each below the largest entry's. The patterns of entries of its sign
+  // fall (or, below zero, rise) by one a step; those of the other sign are out of range either way.
+  __device__ __forceinline__ void count_near() {
+    const int lane = threadIdx.x & 31, nb = mine.blocks();
+    const uint32_t m = __float_as_uint(all.m) >> 16;
+    const bool down = m < 0x8000u;
     for (int k = lane; k < nb; k += 32) {
-      float z[N];
-      mine.load(k, z);
+      const uint4 q = *reinterpret_cast<const uint4*>(mine.at + k * N);
+      const uint32_t v[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-      for (int e = 0; e < N; ++e) {
-        const uint32_t d = top - key_of(z[e]), bin = (d - to.d0) >> to.shift;
-        if (z[e] > minus_inf() && d >= to.d0 && bin < kBins) {
-          atomicAdd(&sh.count[bin], 1u);
-          if (weigh) atomicAdd(&sh.mass[bin], mass_of(weight(z[e])));
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t lo = v[i] & 0xffffu, hi = v[i] >> 16;
+        const uint32_t a = down ? m - lo : lo - m, b = down ? m - hi : hi - m;
+        if (a < kBins) atomicAdd(&sh.count[a], 1u);
+        if (b < kBins) atomicAdd(&sh.count[b], 1u);
+      }
+    }
+  }
+
+  // Counts the cluster's entries by the bins of `to`, and this thread's bins over the cluster with what lies before them.
+  __device__ __forceinline__ void count(const Level& to) {
+    const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+    const bool single = to.shift <= kSingle, weigh = masses && !single;
+    if (level.shift >= 0) {
+      cluster_sync_all();  // the other CTAs have read the last level's
+      for (int i = threadIdx.x; i < kBins; i += kThreads) {
+        sh.count[i] = 0;
+        if (weigh) sh.mass[i] = 0;
+      }
+      __syncthreads();
+    }
+    const uint32_t m = __float_as_uint(all.m) >> 16;
+    // (negative infinity is 0xff80: out of reach of a largest entry below zero only from steps that its bins do not have)
+    if (sizeof(T) == 2 && to.d0 == 0 && to.shift == kBf16Shift && ((m >= kBins && m < 0x8000u) || (m > 0x8000u && m + kBins <= 0xff80u))) {
+      count_near();
+    } else {
+      const int nb = mine.blocks();
+      for (int k = lane; k < nb; k += 32) {
+        float z[N];
+        mine.load(k, z);
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+          const uint32_t d = top - key_of(z[e]), bin = (d - to.d0) >> to.shift;
+          if (z[e] > minus_inf() && d >= to.d0 && bin < kBins) {
+            atomicAdd(&sh.count[bin], 1u);
+            if (weigh) atomicAdd(&sh.mass[bin], mass_of(weight(z[e])));
+          }
         }
       }
     }
     level = to;
     cluster_sync_all();
-  }
-
-  // The border at which the number of entries (BY_MASS: their mass) reaches `goal`; false: it never does.
-  template <bool BY_MASS>
-  __device__ bool search(unsigned long long goal, Border& b) {
-    const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
-    Level at{0u, kBf16Shift};
-    uint32_t above = 0;
-    unsigned long long mass = 0;
-    while (true) {
-      if (!(level == at)) count(at);
-      const bool single = at.shift <= kSingle;
-      uint32_t n[kOwn], mine_n = 0;
-      unsigned long long w[kOwn], mine_w = 0;
+    // the cluster's sums: this thread's bins of every CTA
 #pragma unroll
-      for (int i = 0; i < kOwn; ++i) {
-        const int bin = threadIdx.x * kOwn + i;
-        n[i] = 0;
-        w[i] = 0;
-        for (int r = 0; r < C; ++r) n[i] += ld_cluster_u32(map_to_rank(smem_addr(&sh.count[bin]), r));
-        if (masses && !single)
-          for (int r = 0; r < C; ++r) w[i] += ld_cluster_u64(map_to_rank(smem_addr(&sh.mass[bin]), r));
-        if (masses && single && n[i] != 0)
-          w[i] = n[i] * mass_of(weight(value_of(entry_key<T>(top - (at.d0 + (static_cast<uint32_t>(bin) << at.shift))))));
-        mine_n += n[i];
-        mine_w += w[i];
+    for (int i = 0; i < kOwn; ++i) {
+      n[i] = 0;
+      w[i] = 0;
+    }
+    const uint32_t at_n = smem_addr(&sh.count[threadIdx.x * kOwn]), at_w = smem_addr(&sh.mass[threadIdx.x * kOwn]);
+#pragma unroll 4
+    for (int r = 0; r < C; ++r) {
+      const uint32_t from = map_to_rank(at_n, r);
+#pragma unroll
+      for (int i = 0; i < kOwn; i += 2) {
+        const unsigned long long two = ld_cluster_u64(from + 4 * i);
+        n[i] += static_cast<uint32_t>(two);
+        n[i + 1] += static_cast<uint32_t>(two >> 32);
       }
-      uint32_t run_n = mine_n;
-      unsigned long long run_w = mine_w;
+    }
+    if (weigh)
+      for (int r = 0; r < C; ++r) {
+        const uint32_t from = map_to_rank(at_w, r);
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) w[i] += ld_cluster_u64(from + 8 * i);
+      }
+    uint32_t mine_n = 0;
+    unsigned long long mine_w = 0;
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i) {
+      if (masses && single && n[i] != 0)
+        w[i] = n[i] * mass_of(weight(value_of(entry_key<T>(top - (to.d0 + (static_cast<uint32_t>(threadIdx.x * kOwn + i) << to.shift))))));
+      mine_n += n[i];
+      mine_w += w[i];
+    }
+    // what lies before them
+    run_n = mine_n;
+    run_w = mine_w;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t a = __shfl_up_sync(0xffffffffu, run_n, o);
+      if (lane >= o) run_n += a;
+    }
+    if (masses)
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
-        const uint32_t a = __shfl_up_sync(0xffffffffu, run_n, o);
-        const unsigned long long m = __shfl_up_sync(0xffffffffu, run_w, o);
-        if (lane >= o) run_n += a, run_w += m;
+        const unsigned long long a = __shfl_up_sync(0xffffffffu, run_w, o);
+        if (lane >= o) run_w += a;
       }
-      __syncthreads();  // the last level's border has been read
-      if (lane == 31) {
-        sh.warp_count[warp] = run_n;
-        sh.warp_mass[warp] = run_w;
-      }
-      if (threadIdx.x == 0) sh.found.hit = 0;
-      __syncthreads();
-      uint32_t all_n = 0;
-      unsigned long long all_w = 0;
-      run_n += above - mine_n;
-      run_w += mass - mine_w;
+    if (lane == 31) {
+      sh.warp_count[warp] = run_n;
+      sh.warp_mass[warp] = run_w;
+    }
+    __syncthreads();
+    run_n += above - mine_n;
+    run_w += mass - mine_w;
+    all_n = 0;
+    all_w = 0;
 #pragma unroll
-      for (int v = 0; v < WARPS; ++v) {
-        if (v < warp) run_n += sh.warp_count[v], run_w += sh.warp_mass[v];
-        all_n += sh.warp_count[v];
-        all_w += sh.warp_mass[v];
+    for (int v = 0; v < WARPS; ++v) {
+      const uint32_t a = sh.warp_count[v];
+      run_n += v < warp ? a : 0;
+      all_n += a;
+      if (masses) {
+        const unsigned long long b = sh.warp_mass[v];
+        run_w += v < warp ? b : 0;
+        all_w += b;
       }
+    }
+  }
+
+  // The border of what top_k (0: off) and top_p (1: off) keep of the row; false: they keep everything.
+  __device__ __forceinline__ bool search(int32_t top_k, float top_p, Border& found) {
+    bool any = false, by_mass = top_k == 0;
+    auto mass_goal = [&](double total) { return max(1ull, static_cast<unsigned long long>(ceil(static_cast<double>(top_p) * total))); };
+    unsigned long long goal = by_mass ? mass_goal(static_cast<double>(all.s) * kMassUnit) : static_cast<unsigned long long>(top_k);
+    Level to{0u, kBf16Shift};
+    while (true) {
+      if (to.d0 != level.d0 || to.shift != level.shift) count(to);
+      if (threadIdx.x == 0) sh.bin = -1;
+      __syncthreads();
+      uint32_t a = run_n;
+      unsigned long long m = run_w;
 #pragma unroll
       for (int i = 0; i < kOwn; ++i) {
-        if (BY_MASS ? run_w < goal && run_w + w[i] >= goal : run_n < goal && run_n + n[i] >= goal) {
-          const uint32_t bin = threadIdx.x * kOwn + i;
-          sh.found.hit = 1;
-          sh.found.key = bin;
-          sh.found.above = run_n;
-          sh.found.mass = run_w;
+        if (by_mass ? m < goal && m + w[i] >= goal : a < goal && a + n[i] >= goal) {
+          sh.bin = threadIdx.x * kOwn + i;
+          sh.found.above = a;
+          sh.found.mass = m;
           sh.found.m = n[i];
         }
-        run_n += n[i];
-        run_w += w[i];
+        a += n[i];
+        m += w[i];
       }
       __syncthreads();
-      if (!sh.found.hit) {
-        if (at.d0 != 0 || at.shift != kBf16Shift) return false;
-        // not among the nearest: all that is farther away
-        above += all_n;
-        mass += all_w;
-        at = Level{static_cast<uint32_t>(kBins) << kBf16Shift, kRestShift};
-        continue;
+      const int bin = sh.bin;
+      Border b = sh.found;
+      __syncthreads();  // and may be written again
+      bool none = false;
+      if (bin < 0) {
+        none = to.d0 != 0 || to.shift != kBf16Shift;
+        if (!none) {
+          // not among the nearest: all that is farther away
+          above += all_n;
+          mass += all_w;
+          to = Level{static_cast<uint32_t>(kBins) << kBf16Shift, kRestShift};
+          continue;
+        }
+      } else {
+        const uint32_t d0 = to.d0 + (static_cast<uint32_t>(bin) << to.shift);
+        if (to.shift > kSingle) {
+          above = b.above;
+          mass = b.mass;
+          to = Level{d0, max(0, to.shift - kBinBits)};
+          continue;
+        }
+        b.key = entry_key<T>(top - d0);
+        b.unit = masses ? mass_of(weight(value_of(b.key))) : 0;
+        if (!by_mass) b.m = static_cast<uint32_t>(goal) - b.above;
+        else if (b.unit) b.m = static_cast<uint32_t>(min(static_cast<unsigned long long>(b.m), (goal - b.mass + b.unit - 1) / b.unit));
+        found = b;
+        any = true;
       }
-      b = sh.found;
-      at.d0 += b.key << at.shift;
-      above = b.above;
-      mass = b.mass;
-      if (!single) {
-        at.shift = max(0, at.shift - kBinBits);
-        continue;
+      if (by_mass || top_p >= 1.f) return any;
+      // then top_p, of the mass of what top_k keeps
+      by_mass = true;
+      goal = mass_goal(none ? static_cast<double>(all.s) * kMassUnit : static_cast<double>(b.mass + b.m * b.unit));
+      if (level.d0 != 0 || level.shift != kBf16Shift) {
+        above = 0;
+        mass = 0;
       }
-      b.key = entry_key<T>(top - at.d0);
-      b.unit = masses ? mass_of(weight(value_of(b.key))) : 0;
-      const uint32_t there = b.m;
-      if (BY_MASS) b.m = b.unit ? static_cast<uint32_t>(min(static_cast<unsigned long long>(there), (goal - b.mass + b.unit - 1) / b.unit)) : there;
-      else b.m = static_cast<uint32_t>(goal) - b.above;
-      return true;
+      to = Level{0u, kBf16Shift};
     }
   }
 };
@@ -277,6 +348,10 @@ __global__ void __launch_bounds__(WARPS * 32, 1024 / (WARPS * 32)) sample_kernel
   __syncwarp();
   const T* end = static_cast<const T*>(p.logits) + (p.rows - 1) * p.ld + p.V;
   const Segment<T> mine = fetch(z, e0, n, end, smem + static_cast<size_t>(warp) * p.seg_bytes, &sh.bar[warp], lane);
+  for (int i = threadIdx.x; i < kBins; i += WARPS * 32) {  // while the row is on its way
+    sh.count[i] = 0;
+    sh.mass[i] = 0;
+  }
   Settings set{p.temperature, p.top_p, p.min_p, p.u[row], p.top_k};
   if (p.row_temperature) set.T = p.row_temperature[row];
   if (p.row_top_k) set.top_k = p.row_top_k[row];
@@ -317,19 +392,9 @@ __global__ void __launch_bounds__(WARPS * 32, 1024 / (WARPS * 32)) sample_kernel
     zt = all.m;
     ties = 1;
   }
-  double total = static_cast<double>(all.s) * kMassUnit;
-  if (by_k) {
+  if (by_k || by_p) {
     Border b;
-    if (r.template search<false>(set.top_k, b)) {
-      zt = value_of(b.key);
-      ties = b.m;
-      total = static_cast<double>(b.mass + b.m * b.unit);
-    }
-  }
-  if (by_p) {
-    Border b;
-    const double goal = ceil(static_cast<double>(set.top_p) * total);
-    if (r.template search<true>(max(1ull, static_cast<unsigned long long>(goal)), b)) {
+    if (r.search(by_k ? set.top_k : 0, set.top_p, b)) {
       zt = value_of(b.key);
       ties = b.m;
     }
@@ -347,20 +412,25 @@ __global__ void __launch_bounds__(WARPS * 32, 1024 / (WARPS * 32)) sample_kernel
   if (pass) {
     float sum = 0.f;
     uint32_t above = 0, equal = 0;
-    for (int k = lane; k < nb; k += 32) {
+    for (int k = lane; k - lane < nb; k += 32) {
       float v[N];
-      mine.load(k, v);
+      bool any = false;
+      if (k < nb) {
+        mine.load(k, v);
+        float most = v[0];
+#pragma unroll
+        for (int e = 1; e < N; ++e) most = fmaxf(most, v[e]);
+        any = most >= zt;
+      }
+      if (!__ballot_sync(0xffffffffu, any)) continue;  // most blocks hold nothing that is kept
+      if (!any) continue;
 #pragma unroll
       for (int e = 0; e < N; ++e) {
-        if (!(v[e] >= zt) || v[e] == minus_inf()) continue;
         const float x = exponent_of(v[e]);
-        if (!(x >= least)) continue;
-        if (v[e] > zt) {
-          sum += ex2(x);
-          ++above;
-        } else {
-          ++equal;
-        }
+        const bool in = x >= least, over = v[e] > zt && in;
+        sum += over ? ex2(x) : 0.f;
+        above += over;
+        equal += v[e] == zt && in;
       }
     }
     sum = warp_sum(sum);
