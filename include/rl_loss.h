@@ -716,8 +716,7 @@ typedef struct rl_sample_params {
 
 /*
  *   logits         [rows x ld] of `dtype`, base 16-byte aligned
- *   rows, V, ld    rows up to 2^26, 1 <= V <= ld; a row has to fit in the shared memory of 16 CTAs (1,638,000 bf16 or
- *                  819,000 fp32 entries), else RL_ERR_UNSUPPORTED
+ *   rows, V, ld    rows up to 2^26, 1 <= V <= ld, V up to 2^24 (bf16) or 2^23 (fp32)
  *   sample_u       float [rows] in [0, 1)
  *   params         host pointer: the settings of every row but for those given per row:
  *   row_temperature, row_top_k, row_top_p, row_min_p   float / int32 / float / float [rows], each may be NULL

@@ -6,17 +6,18 @@
 // of those equal to it the first few by index. The token is the lowest kept one, in vocabulary order, at which the
 // running sum of the kept ones' weights passes u times their total.
 //
-// A thread-block cluster takes a row and holds it in shared memory, a segment per warp, so that HBM is read once:
-//   1. every warp folds its segment into (max, sum of exponentials); one exchange gives every CTA the row's.
-//   2. the threshold, only where a filter asks for one: counts of the entries by their distance from the largest in
-//      steps of bf16 (the upper half of the ordered bit pattern), 1,024 bins, added up over the cluster. A bin of a bf16
-//      row is one value, whose mass is its count times its weight; fp32 rows add up the weights too, as integers of 2^-40,
-//      and go on into the bin that holds the border, 64 patterns a bin and then one. Borders farther below the largest
-//      entry (8 powers of two) take coarser bins first. Integer sums: any order gives the same bits.
-//   3. every warp sums the kept weights of its segment and counts the entries equal to the threshold; a second exchange;
-//      the warp whose segment holds the token finds it by a scan.
+// A CTA takes a row, or with few rows a cluster of them; the row is cut into tiles of 2 KB, a warp each in turn.
+//   1. every warp folds its tiles into (max, sum of exponentials); one exchange gives the row's.
+//   2. the threshold, only where top-k or top-p ask for one: counts of the entries in 1,024 bins, added up over the cluster,
+//      and a scan. A bf16 row's bins are single values, whose mass is their count times their weight; entries of 0.5 to 128
+//      are counted in the first pass already, on the guess that the largest entry and the border are among them. Where
+//      they are not, and for fp32 rows, more passes count by the distance of the ordered bit patterns from the largest
+//      entry's, in steps of 2^16 patterns, then down to single ones within the bin that holds the border; masses are then
+//      added up as integers of 2^-36. Integer sums: any order gives the same bits. min-p is a value, found by bisection.
+//   3. a pass sums the kept weights of every tile and counts the entries equal to the threshold; a second exchange; the tile
+//      that holds the token is found by a scan, and the token in it by another.
+// HBM is read once: the rows at work at a time fit in L2, where the later passes find them.
 #include <algorithm>
-#include <atomic>
 #include <cmath>
 #include <string>
 
@@ -29,10 +30,13 @@ namespace sample {
 
 using namespace seg;
 
-constexpr int kMaxCluster = 16;
+constexpr int kMostCluster = 16;
 constexpr int kBinBits = 10, kBins = 1 << kBinBits;
 constexpr int kBf16Shift = 16;  // patterns of a bf16 step
 constexpr int kRestShift = 22;  // the bins cover all patterns
+constexpr int kTileBlocks32 = kTileBlocks * 32;  // 16-byte blocks of a tile
+// The window of the first pass: bf16 patterns of 0.5 up to 128, the largest first.
+constexpr uint32_t kWindowLow = 0x3f00u, kWindowTop = kWindowLow + kBins - 1;
 
 struct Args {
   const void* logits;
@@ -45,7 +49,7 @@ struct Args {
   const int32_t* row_top_k;
   const float* row_top_p;
   const float* row_min_p;
-  int32_t seg, seg_bytes;
+  int32_t tiles;  // of a CTA
   int32_t* ids;
   float* logp;
   float* among;     // or NULL
@@ -79,22 +83,75 @@ __device__ __forceinline__ uint32_t entry_key(uint32_t key) {
   return (key & 0xffffu) == 0xffffu ? key : (key & 0xffff0000u) - 1u;
 }
 
-constexpr float kMassUnit = 1099511627776.f;  // 2^40
+constexpr float kMassUnit = 68719476736.f;  // 2^36
 __device__ __forceinline__ unsigned long long mass_of(float w) { return __float2ull_rn(w * kMassUnit); }
 
-__device__ __forceinline__ uint32_t ld_cluster_u32(uint32_t addr) {
-  uint32_t v;
-  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
-  return v;
-}
 __device__ __forceinline__ unsigned long long ld_cluster_u64(uint32_t addr) {
   unsigned long long v;
   asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(addr) : "memory");
   return v;
 }
-__device__ __forceinline__ void put_u1(uint32_t addr, uint32_t a) {
-  asm volatile("st.shared::cluster.u32 [%0], %1;" :: "r"(addr), "r"(a) : "memory");
+__device__ __forceinline__ void put_u2(uint32_t addr, uint32_t a, uint32_t b) {
+  asm volatile("st.shared::cluster.v2.u32 [%0], {%1, %2};" :: "r"(addr), "r"(a), "r"(b) : "memory");
 }
+
+// Both halves of a pair of bf16 against a value: all ones where it holds.
+__device__ __forceinline__ uint32_t above2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("set.gt.u32.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ uint32_t least2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("set.ge.u32.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ uint32_t equal2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("set.eq.u32.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+
+// A row as the 16-byte blocks of memory that it covers.
+template <typename T>
+struct RowBlocks {
+  static constexpr int N = Elem<T>::N;
+  static constexpr uint32_t kNone = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;
+  const T* at;   // the first block
+  const T* end;  // of the whole array
+  int lo, hi;    // the row's elements are [lo, hi) from `at`
+  int nb;        // blocks
+  __device__ __forceinline__ RowBlocks(const T* row, int V, const T* array_end) : end(array_end) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(row), a0 = a & ~uintptr_t(15);
+    at = reinterpret_cast<const T*>(a0);
+    lo = static_cast<int>(a - a0) / static_cast<int>(sizeof(T));
+    hi = lo + V;
+    nb = (hi + N - 1) / N;
+  }
+  // Block k; elements of other rows, and blocks behind the last, are minus infinity.
+  __device__ __forceinline__ uint4 block(int k) const {
+    if (k > 0 && k < nb - 1) return __ldcg(reinterpret_cast<const uint4*>(at + static_cast<int64_t>(k) * N));
+    uint4 q = make_uint4(kNone, kNone, kNone, kNone);
+    if (k < 0 || k >= nb) return q;
+    T* e = reinterpret_cast<T*>(&q);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (k * N + i >= lo && k * N + i < hi) e[i] = at[k * N + i];
+    return q;
+  }
+  // A lane's blocks of tile t.
+  __device__ __forceinline__ void tile(int t, int lane, uint4 (&w)[kTileBlocks]) const {
+    const int k = t * kTileBlocks32 + lane;
+    if (t > 0 && (t + 1) * kTileBlocks32 < nb) {
+      const uint4* p = reinterpret_cast<const uint4*>(at) + k;
+#pragma unroll
+      for (int i = 0; i < kTileBlocks; ++i) w[i] = __ldcg(p + 32 * i);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kTileBlocks; ++i) w[i] = block(k + 32 * i);
+    }
+  }
+};
 
 // A border: entries above `key` and the first m of those equal to it; their number above it and their mass.
 struct Border {
@@ -102,23 +159,40 @@ struct Border {
   unsigned long long mass, unit;  // of the entries above; of one entry equal to it
 };
 
+// A CTA's kept entries.
+struct Part {
+  float sum;  // weights of those above the threshold
+  uint32_t equal, above;
+};
+
 template <int WARPS>
 struct Shared {
-  static constexpr int kSegs = WARPS * kMaxCluster;
-  Fold fold[kSegs];      // every segment's, the same in every CTA of the cluster
-  float sum[kSegs];      // of the kept weights above the threshold
-  uint32_t above[kSegs]; // kept entries above it
-  uint32_t equal[kSegs]; // entries equal to it
-  alignas(16) uint32_t count[kBins];  // this CTA's
-  alignas(16) unsigned long long mass[kBins];
+  Fold fold[WARPS * kMostCluster];    // every warp's, the same in every CTA of the cluster
+  alignas(16) uint32_t count[kBins];  // this CTA's entries
+  alignas(16) uint32_t low[kBins];    // and their mass
+  alignas(16) uint32_t high[kBins];
   uint32_t warp_count[WARPS];
   unsigned long long warp_mass[WARPS];
   Border found;
   int32_t bin;  // that found is of (-1: none)
-  uint64_t bar[WARPS];
+  Fold all;     // the row's
+  uint32_t least_key;  // min_p's value
+  alignas(8) uint2 part_a[kMostCluster];  // every CTA's (sum, equal)
+  uint32_t part_b[kMostCluster];          // above
+  float warp_sum[WARPS];
+  uint32_t warp_equal[WARPS], warp_above[WARPS];
 };
 
-// The bins of distances d0 .. d0 + (kBins << shift) from the largest entry's key.
+// A tile's (max, sum) where nothing is filtered, else the kept weights above the threshold and the entries equal to it.
+union Tile {
+  Fold fold;
+  struct {
+    float sum;
+    uint32_t equal;
+  } kept;
+};
+
+// The bins of distances d0 .. d0 + (kBins << shift) from the largest entry's key; shift < 0: the window.
 struct Level {
   uint32_t d0;
   int shift;
@@ -127,81 +201,76 @@ struct Level {
 template <typename T, int WARPS>
 struct Row {
   Shared<WARPS>& sh;
-  Segment<T> mine;
-  Fold all;  // the row's
+  const RowBlocks<T>& row;
+  int t0, t1;  // this CTA's tiles
+  Fold all;    // the row's
   float c;
   uint32_t top;  // the largest entry's key
   int C;
   bool masses;   // weights are wanted
   static constexpr int N = Elem<T>::N, kThreads = WARPS * 32, kOwn = kBins / kThreads;
   static constexpr int kSingle = sizeof(T) == 2 ? kBf16Shift : 0;  // bins of at most these patterns hold one value
-  Level level{0u, -1};  // what the bins hold
-  uint32_t above = 0;   // entries before the level's first bin
+  uint32_t above = 0;  // entries before the level's first bin
   unsigned long long mass = 0;
   uint32_t n[kOwn], run_n, all_n;            // this thread's bins over the cluster; entries before them; all bins'
   unsigned long long w[kOwn], run_w, all_w;  // the same for masses
 
   __device__ __forceinline__ float weight(float z) const { return ex2(exponent(z, all.m, c)); }
 
-  // bf16 entries by their patterns, to bins of one step each below the largest entry's. The patterns of entries of its sign
-  // fall (or, below zero, rise) by one a step; those of the other sign are out of range either way.
-  __device__ __forceinline__ void count_near() {
-    const int lane = threadIdx.x & 31, nb = mine.blocks();
-    const uint32_t m = __float_as_uint(all.m) >> 16;
-    const bool down = m < 0x8000u;
-    for (int k = lane; k < nb; k += 32) {
-      const uint4 q = *reinterpret_cast<const uint4*>(mine.at + k * N);
-      const uint32_t v[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t lo = v[i] & 0xffffu, hi = v[i] >> 16;
-        const uint32_t a = down ? m - lo : lo - m, b = down ? m - hi : hi - m;
-        if (a < kBins) atomicAdd(&sh.count[a], 1u);
-        if (b < kBins) atomicAdd(&sh.count[b], 1u);
-      }
-    }
-  }
-
-  // Counts the cluster's entries by the bins of `to`, and this thread's bins over the cluster with what lies before them.
+  // Counts this CTA's entries by the bins of `to`.
   __device__ __forceinline__ void count(const Level& to) {
     const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
-    const bool single = to.shift <= kSingle, weigh = masses && !single;
-    if (level.shift >= 0) {
-      cluster_sync_all();  // the other CTAs have read the last level's
-      for (int i = threadIdx.x; i < kBins; i += kThreads) {
-        sh.count[i] = 0;
-        if (weigh) sh.mass[i] = 0;
-      }
-      __syncthreads();
+    const bool weigh = masses && to.shift > kSingle;
+    cluster_sync_all();  // the other CTAs have read the last level's
+    for (int i = threadIdx.x; i < kBins; i += kThreads) {
+      sh.count[i] = 0;
+      sh.low[i] = 0;
+      sh.high[i] = 0;
     }
-    const uint32_t m = __float_as_uint(all.m) >> 16;
-    // (negative infinity is 0xff80: out of reach of a largest entry below zero only from steps that its bins do not have)
-    if (sizeof(T) == 2 && to.d0 == 0 && to.shift == kBf16Shift && ((m >= kBins && m < 0x8000u) || (m > 0x8000u && m + kBins <= 0xff80u))) {
-      count_near();
-    } else {
-      const int nb = mine.blocks();
-      for (int k = lane; k < nb; k += 32) {
+    __syncthreads();
+    for (int t = t0 + warp; t < t1; t += WARPS) {
+      uint4 q[kTileBlocks];
+      row.tile(t, lane, q);
+#pragma unroll 1
+      for (int i = 0; i < kTileBlocks; ++i) {
         float z[N];
-        mine.load(k, z);
+        Elem<T>::unpack(q[0], z);
+        q[0] = q[1], q[1] = q[2], q[2] = q[3];
 #pragma unroll
         for (int e = 0; e < N; ++e) {
           const uint32_t d = top - key_of(z[e]), bin = (d - to.d0) >> to.shift;
           if (z[e] > minus_inf() && d >= to.d0 && bin < kBins) {
             atomicAdd(&sh.count[bin], 1u);
-            if (weigh) atomicAdd(&sh.mass[bin], mass_of(weight(z[e])));
+            if (weigh) {
+              const unsigned long long m = mass_of(weight(z[e]));
+              const uint32_t lo = static_cast<uint32_t>(m), old = atomicAdd(&sh.low[bin], lo);
+              const uint32_t hi = static_cast<uint32_t>(m >> 32) + (old + lo < old ? 1u : 0u);
+              if (hi) atomicAdd(&sh.high[bin], hi);
+            }
           }
         }
       }
     }
-    level = to;
     cluster_sync_all();
-    // the cluster's sums: this thread's bins of every CTA
+  }
+
+  // The key of the first entry of a bin.
+  __device__ __forceinline__ uint32_t key_at(const Level& l, int bin) const {
+    if (l.shift < 0) return 0x8000ffffu | (kWindowTop - bin) << 16;
+    return top - (l.d0 + (static_cast<uint32_t>(bin) << l.shift));
+  }
+
+  // The cluster's sums of the bins that the CTAs have counted: this thread's, and what lies before them.
+  __device__ __forceinline__ void add_up(const Level& l) {
+    const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+    const bool single = l.shift < 0 ? sizeof(T) == 2 : l.shift <= kSingle;
 #pragma unroll
     for (int i = 0; i < kOwn; ++i) {
       n[i] = 0;
       w[i] = 0;
     }
-    const uint32_t at_n = smem_addr(&sh.count[threadIdx.x * kOwn]), at_w = smem_addr(&sh.mass[threadIdx.x * kOwn]);
+    const int own = threadIdx.x * kOwn;
+    const uint32_t at_n = smem_addr(&sh.count[own]), at_l = smem_addr(&sh.low[own]), at_h = smem_addr(&sh.high[own]);
 #pragma unroll 4
     for (int r = 0; r < C; ++r) {
       const uint32_t from = map_to_rank(at_n, r);
@@ -212,22 +281,24 @@ struct Row {
         n[i + 1] += static_cast<uint32_t>(two >> 32);
       }
     }
-    if (weigh)
+    if (masses && !single)
       for (int r = 0; r < C; ++r) {
-        const uint32_t from = map_to_rank(at_w, r);
+        const uint32_t from_l = map_to_rank(at_l, r), from_h = map_to_rank(at_h, r);
 #pragma unroll
-        for (int i = 0; i < kOwn; ++i) w[i] += ld_cluster_u64(from + 8 * i);
+        for (int i = 0; i < kOwn; i += 2) {
+          const unsigned long long lo = ld_cluster_u64(from_l + 4 * i), hi = ld_cluster_u64(from_h + 4 * i);
+          w[i] += (hi << 32) + (lo & 0xffffffffu);
+          w[i + 1] += (hi & 0xffffffff00000000ull) + (lo >> 32);
+        }
       }
     uint32_t mine_n = 0;
     unsigned long long mine_w = 0;
 #pragma unroll
     for (int i = 0; i < kOwn; ++i) {
-      if (masses && single && n[i] != 0)
-        w[i] = n[i] * mass_of(weight(value_of(entry_key<T>(top - (to.d0 + (static_cast<uint32_t>(threadIdx.x * kOwn + i) << to.shift))))));
+      if (masses && single && n[i] != 0) w[i] = n[i] * mass_of(weight(value_of(entry_key<T>(key_at(l, own + i)))));
       mine_n += n[i];
       mine_w += w[i];
     }
-    // what lies before them
     run_n = mine_n;
     run_w = mine_w;
 #pragma unroll
@@ -263,14 +334,19 @@ struct Row {
     }
   }
 
-  // The border of what top_k (0: off) and top_p (1: off) keep of the row; false: they keep everything.
-  __device__ __forceinline__ bool search(int32_t top_k, float top_p, Border& found) {
-    bool any = false, by_mass = top_k == 0;
+  // The border of what top_k (0: off) and top_p (1: off) keep of the row; false: they keep everything. `first`: the level
+  // to begin with, counted already if it is the window.
+  __device__ __forceinline__ bool search(int32_t top_k, float top_p, const Level& first, Border& found) {
+    bool any = false, by_mass = top_k == 0, fresh = true;
     auto mass_goal = [&](double total) { return max(1ull, static_cast<unsigned long long>(ceil(static_cast<double>(top_p) * total))); };
     unsigned long long goal = by_mass ? mass_goal(static_cast<double>(all.s) * kMassUnit) : static_cast<unsigned long long>(top_k);
-    Level to{0u, kBf16Shift};
+    Level outer = first, to = first;
     while (true) {
-      if (to.d0 != level.d0 || to.shift != level.shift) count(to);
+      if (fresh) {
+        if (to.shift >= 0) count(to);
+        add_up(to);
+      }
+      fresh = true;
       if (threadIdx.x == 0) sh.bin = -1;
       __syncthreads();
       uint32_t a = run_n;
@@ -291,21 +367,23 @@ struct Row {
       Border b = sh.found;
       __syncthreads();  // and may be written again
       bool none = false;
+      const bool outermost = to.d0 == outer.d0 && to.shift == outer.shift;
       if (bin < 0) {
-        none = to.d0 != 0 || to.shift != kBf16Shift;
+        none = !outermost;
         if (!none) {
           // not among the nearest: all that is farther away
           above += all_n;
           mass += all_w;
-          to = Level{static_cast<uint32_t>(kBins) << kBf16Shift, kRestShift};
+          to = Level{to.shift < 0 ? top - (0x8000ffffu | (kWindowLow - 1) << 16) : static_cast<uint32_t>(kBins) << kBf16Shift, kRestShift};
           continue;
         }
       } else {
-        const uint32_t d0 = to.d0 + (static_cast<uint32_t>(bin) << to.shift);
-        if (to.shift > kSingle) {
+        const uint32_t k = key_at(to, bin), d0 = k > top ? 0u : top - k;  // the window's first bin may reach above the largest
+        const int shift = to.shift < 0 ? kBf16Shift : to.shift;
+        if (shift > kSingle) {
           above = b.above;
           mass = b.mass;
-          to = Level{d0, max(0, to.shift - kBinBits)};
+          to = Level{d0, max(0, shift - kBinBits)};
           continue;
         }
         b.key = entry_key<T>(top - d0);
@@ -319,12 +397,109 @@ struct Row {
       // then top_p, of the mass of what top_k keeps
       by_mass = true;
       goal = mass_goal(none ? static_cast<double>(all.s) * kMassUnit : static_cast<double>(b.mass + b.m * b.unit));
-      if (level.d0 != 0 || level.shift != kBf16Shift) {
+      fresh = !outermost;
+      if (fresh) {
         above = 0;
         mass = 0;
+        to = outer = Level{0u, kBf16Shift};  // the window's bins, if it had any, are gone
       }
-      to = Level{0u, kBf16Shift};
     }
+  }
+};
+
+// The smallest key of an entry of this type whose exponent is at least `least`.
+template <typename T, typename X>
+__device__ __forceinline__ uint32_t least_key(uint32_t top, float least, X exponent_of) {
+  auto widen = [](uint32_t i) { return sizeof(T) == 4 ? i : i << 16 | (i & 0x8000u ? 0u : 0xffffu); };
+  uint32_t lo = sizeof(T) == 4 ? 0x00800000u : 0x80u, hi = sizeof(T) == 4 ? top : top >> 16;  // the lowest finite; one that is
+  while (lo < hi) {
+    const uint32_t mid = lo + (hi - lo) / 2;
+    if (exponent_of(value_of(widen(mid))) >= least) hi = mid;
+    else lo = mid + 1;
+  }
+  return widen(hi);
+}
+
+// As pick, but with the goal itself: the place among n weights w(k) at which their running sum passes `goal`.
+template <typename W>
+__device__ __forceinline__ int pick_at(int n, float goal, int lane, W w, float& left) {
+  const int M = (n + 31) / 32, k0 = min(lane * M, n), k1 = min(k0 + M, n);
+  float sum = 0.f;
+  for (int k = k0; k < k1; ++k) sum += w(k);
+  float run = sum;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const float up = __shfl_up_sync(0xffffffffu, run, o);
+    if (lane >= o) run += up;
+  }
+  float before = run - sum, rest = 0.f, last_rest = 0.f;
+  int at = -1, last = -1;
+  for (int k = k0; k < k1; ++k) {
+    const float mine = w(k);
+    if (mine > 0.f) {
+      last = k;
+      last_rest = goal - before;
+      if (at < 0 && before + mine > goal) {
+        at = k;
+        rest = last_rest;
+      }
+    }
+    before += mine;
+  }
+  const uint32_t found = __ballot_sync(0xffffffffu, at >= 0), any = __ballot_sync(0xffffffffu, last >= 0);
+  const int from = found ? __ffs(found) - 1 : any ? 31 - __clz(any) : 0;
+  left = __shfl_sync(0xffffffffu, found ? rest : last_rest, from);
+  return max(0, __shfl_sync(0xffffffffu, found ? at : last, from));
+}
+
+// What a pass over the row keeps: entries above (GE: and at) zt.
+template <typename T, bool GE>
+struct Keep {
+  static constexpr int N = Elem<T>::N;
+  float zt, ref, c;
+  // A block's kept entries, the others minus infinity; false: it has none. Adds those equal to zt (not GE) to `equal`, and
+  // with `count` the kept ones to `kept`.
+  __device__ __forceinline__ bool block(const uint4& q, float (&z)[N], uint32_t& equal, uint32_t& kept, bool count) const {
+    if constexpr (sizeof(T) == 2) {
+      const uint32_t t = __float_as_uint(zt) >> 16, t2 = t | t << 16;
+      const uint32_t v[4] = {q.x, q.y, q.z, q.w};
+      uint32_t m[4], r[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        m[i] = GE ? least2(v[i], t2) : above2(v[i], t2);
+        r[i] = (v[i] & m[i]) | (0xff80ff80u & ~m[i]);
+        if (!GE) equal += __popc(equal2(v[i], t2));
+        if (count) kept += __popc(m[i]);
+      }
+      Elem<T>::unpack(make_uint4(r[0], r[1], r[2], r[3]), z);
+      return (m[0] | m[1] | m[2] | m[3]) != 0;
+    } else {
+      Elem<T>::unpack(q, z);
+      bool any = false;
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const bool in = GE ? z[e] >= zt : z[e] > zt;
+        if (!GE) equal += z[e] == zt ? 16 : 0;
+        if (count) kept += in ? 16 : 0;
+        any |= in;
+        z[e] = in ? z[e] : minus_inf();
+      }
+      return any;
+    }
+  }
+  // The kept weights of a lane's blocks of a tile. (equal and kept count 16 an entry.)
+  __device__ __forceinline__ float tile(const uint4 (&q)[kTileBlocks], uint32_t& equal, uint32_t& kept, bool count) const {
+    float2 s = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < kTileBlocks; ++i) {
+      float z[N];
+      const bool any = block(q[i], z, equal, kept, count);
+      if (!__any_sync(0xffffffffu, any)) continue;
+      exps(z, ref, c);
+#pragma unroll
+      for (int e = 0; e < N; e += 2) s = add2(s, make_float2(z[e], z[e + 1]));
+    }
+    return s.x + s.y;
   }
 };
 
@@ -332,265 +507,283 @@ template <typename T, int WARPS>
 __global__ void __launch_bounds__(WARPS * 32, 1024 / (WARPS * 32)) sample_kernel(const Args p) {
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ __align__(16) Shared<WARPS> sh;
+  Tile* tiles = reinterpret_cast<Tile*>(smem);
   constexpr int N = Elem<T>::N;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const uint32_t rank = cluster_ctarank(), C = cluster_nctarank();
-  const int64_t row = blockIdx.x / C;
-  const int n_seg = static_cast<int>(C) * WARPS, g = static_cast<int>(rank) * WARPS + warp;
+  const int rank = static_cast<int>(cluster_ctarank()), C = static_cast<int>(cluster_nctarank());
+  const int64_t r = blockIdx.x / C;
+  const T* z = static_cast<const T*>(p.logits) + r * p.ld;
+  const RowBlocks<T> row(z, p.V, static_cast<const T*>(p.logits) + (p.rows - 1) * p.ld + p.V);
+  const int all_tiles = (row.nb + kTileBlocks32 - 1) / kTileBlocks32;
+  const int t0 = min(rank * p.tiles, all_tiles), t1 = min(t0 + p.tiles, all_tiles);
   asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");  // the other CTAs have started
-  const T* z = static_cast<const T*>(p.logits) + row * p.ld;
-  const int e0 = min(g * p.seg, p.V), n = min(p.seg, p.V - e0);
-  if (lane == 0) {
-    mbar_init(&sh.bar[warp], 1);
-    fence_mbar_init();
-    fence_proxy_async_smem();
-  }
-  __syncwarp();
-  const T* end = static_cast<const T*>(p.logits) + (p.rows - 1) * p.ld + p.V;
-  const Segment<T> mine = fetch(z, e0, n, end, smem + static_cast<size_t>(warp) * p.seg_bytes, &sh.bar[warp], lane);
-  for (int i = threadIdx.x; i < kBins; i += WARPS * 32) {  // while the row is on its way
-    sh.count[i] = 0;
-    sh.mass[i] = 0;
-  }
-  Settings set{p.temperature, p.top_p, p.min_p, p.u[row], p.top_k};
-  if (p.row_temperature) set.T = p.row_temperature[row];
-  if (p.row_top_k) set.top_k = p.row_top_k[row];
-  if (p.row_top_p) set.top_p = p.row_top_p[row];
-  if (p.row_min_p) set.min_p = p.row_min_p[row];
+  uint4 q[kTileBlocks];
+  if (t0 + warp < t1) row.tile(t0 + warp, lane, q);
+  Settings set{p.temperature, p.top_p, p.min_p, p.u[r], p.top_k};
+  if (p.row_temperature) set.T = p.row_temperature[r];
+  if (p.row_top_k) set.top_k = p.row_top_k[r];
+  if (p.row_top_p) set.top_p = p.row_top_p[r];
+  if (p.row_min_p) set.min_p = p.row_min_p[r];
+  for (int i = threadIdx.x; i < kBins; i += WARPS * 32) sh.count[i] = 0;
+  __syncthreads();
   const bool greedy = set.T == 0.f, known = set.ok();
   const float c = greedy || !known ? kLog2e : kLog2e / set.T;
+  const bool by_k = !greedy && set.top_k > 0 && set.top_k < p.V, by_p = !greedy && set.top_p < 1.f;
+  const bool by_m = !greedy && set.min_p > 0.f, filtered = greedy || by_k || by_p || by_m;
+  const bool window = (by_k || by_p) && (sizeof(T) == 2 || !by_p);
 
   // ---- the row's largest entry and its normaliser
-  const bool in_time = mbar_wait_bounded(&sh.bar[warp], 0);
-  if (!in_time && lane == 0) flag_status(p.status, RL_DEV_TIMEOUT);
-  mine.blank_edges(lane);
-  int unused = 0;
-  const Fold f = fold<T, false>(mine, c, lane, unused);
+  Running run{minus_inf(), {0.f, 0.f}, 0};
+  Fold f{minus_inf(), 0.f};
+  for (int t = t0 + warp; t < t1; t += WARPS) {
+    uint4 now[kTileBlocks];
+#pragma unroll
+    for (int i = 0; i < kTileBlocks; ++i) now[i] = q[i];
+    if (t + WARPS < t1) row.tile(t + WARPS, lane, q);
+    add_tile<T, false>(run, now, 0, c);
+    if (window) {
+#pragma unroll
+      for (int i = 0; i < kTileBlocks; ++i) {
+        const uint32_t v[4] = {now[i].x, now[i].y, now[i].z, now[i].w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t hi = kWindowTop - (v[e] >> 16);
+          if (hi < kBins) atomicAdd(&sh.count[hi], 1u);
+          if (sizeof(T) == 2) {
+            const uint32_t lo = kWindowTop - (v[e] & 0xffffu);
+            if (lo < kBins) atomicAdd(&sh.count[lo], 1u);
+          }
+        }
+      }
+    } else if (!filtered) {
+      const Fold of = of_warp(run, c);
+      if (lane == 0) tiles[t - t0].fold = of;
+      const float m = fmaxf(f.m, of.m);
+      f.s = (f.s == 0.f ? 0.f : f.s * power(f.m, m, c)) + (of.s == 0.f ? 0.f : of.s * power(of.m, m, c));
+      f.m = m;
+      run = Running{minus_inf(), {0.f, 0.f}, 0};
+    }
+  }
+  if (filtered) f = of_warp(run, c);
   asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
-  if (lane < C) put_f2(map_to_rank(smem_addr(&sh.fold[g]), lane), f.m, f.s);
+  if (lane < C) put_f2(map_to_rank(smem_addr(&sh.fold[rank * WARPS + warp]), lane), f.m, f.s);
   __syncwarp();
   cluster_sync_all();
-  const Fold all = merged(sh.fold, n_seg, c, lane);
+  if (warp == 0) {
+    const Fold all = merged(sh.fold, C * WARPS, c, lane);
+    if (lane == 0) {
+      sh.all = all;
+      if (by_m && !is_bad(all) && known) {
+        // min_p, as an exponent from that of the largest entry, which the rounding of its product moves as all others
+        auto x = [&](float v) { return exponent(v, all.m, c); };
+        sh.least_key = least_key<T>(key_of(all.m), x(all.m) + log2f(set.min_p), x);
+      }
+    }
+  }
+  __syncthreads();
+  const Fold all = sh.all;
   if (is_bad(all) || !known) {  // the whole cluster
     if (rank == 0 && threadIdx.x == 0) {
       flag_status(p.status, RL_DEV_BAD_VALUE);
-      p.ids[row] = -1;
-      p.logp[row] = __int_as_float(0x7fc00000);
-      if (p.among) p.among[row] = __int_as_float(0x7fc00000);
-      if (p.n_kept) p.n_kept[row] = 0;
+      p.ids[r] = -1;
+      p.logp[r] = __int_as_float(0x7fc00000);
+      if (p.among) p.among[r] = __int_as_float(0x7fc00000);
+      if (p.n_kept) p.n_kept[r] = 0;
     }
     return;
   }
 
-  // ---- the threshold: entries above zt are kept, and the first ties of those equal to it
-  Row<T, WARPS> r{sh, mine, all, c, key_of(all.m), static_cast<int>(C), set.top_p < 1.f};
+  // ---- the threshold: entries above zt are kept, and the first ties of those equal to it (GE: all of them)
   float zt = minus_inf();
   uint32_t ties = 0;
-  const bool by_k = !greedy && set.top_k > 0 && set.top_k < p.V, by_p = !greedy && set.top_p < 1.f;
-  const bool by_m = !greedy && set.min_p > 0.f;
+  int64_t kept = -1;  // not known yet
+  bool ge = false;
   if (greedy) {
     zt = all.m;
     ties = 1;
-  }
-  if (by_k || by_p) {
+    kept = 1;
+  } else if (by_k || by_p) {
+    const uint32_t top = key_of(all.m);
+    Row<T, WARPS> s{sh, row, t0, t1, all, c, top, C, by_p};
     Border b;
-    if (r.search(by_k ? set.top_k : 0, set.top_p, b)) {
+    const bool in_window = window && top >= (0x80000000u | kWindowLow << 16) && top <= (0x8000ffffu | kWindowTop << 16);
+    if (s.search(by_k ? set.top_k : 0, set.top_p, in_window ? Level{0u, -1} : Level{0u, kBf16Shift}, b)) {
       zt = value_of(b.key);
       ties = b.m;
+      kept = static_cast<int64_t>(b.above) + b.m;
     }
   }
-  const float rc = __fmul_rn(all.m, c);
-  const bool apart = large(rc);
-  auto exponent_of = [&](float v) { return apart ? (v - all.m) * c : fmaf(v, c, -rc); };
-  // min_p, as an exponent from that of the largest entry, which the rounding of its product moves as all others
-  const float least = by_m ? exponent_of(all.m) + log2f(set.min_p) : minus_inf();
+  if (by_m && value_of(sh.least_key) > zt) {
+    zt = value_of(sh.least_key);
+    ge = true;
+    ties = 0;
+    kept = -1;
+  }
 
-  // ---- the kept weights of every segment
-  const bool filtered = greedy || by_k || by_p || by_m;
-  const bool pass = filtered || p.n_kept;
-  const int nb = mine.blocks();
+  // ---- the kept weights of every tile
+  const bool count = p.n_kept && kept < 0, pass = filtered || count;
   if (pass) {
     float sum = 0.f;
-    uint32_t above = 0, equal = 0;
-    for (int k = lane; k - lane < nb; k += 32) {
-      float v[N];
-      bool any = false;
-      if (k < nb) {
-        mine.load(k, v);
-        float most = v[0];
-#pragma unroll
-        for (int e = 1; e < N; ++e) most = fmaxf(most, v[e]);
-        any = most >= zt;
+    uint32_t equal = 0, above = 0;
+    auto over = [&](const auto& keep) {
+      for (int t = t0 + warp; t < t1; t += WARPS) {
+        row.tile(t, lane, q);
+        uint32_t eq = 0;
+        const float s = warp_sum(keep.tile(q, eq, above, count));
+        eq = __reduce_add_sync(0xffffffffu, eq) / 16;
+        if (lane == 0 && filtered) {
+          tiles[t - t0].kept.sum = s;
+          tiles[t - t0].kept.equal = eq;
+        }
+        sum += s;
+        equal += eq;
       }
-      if (!__ballot_sync(0xffffffffu, any)) continue;  // most blocks hold nothing that is kept
-      if (!any) continue;
-#pragma unroll
-      for (int e = 0; e < N; ++e) {
-        const float x = exponent_of(v[e]);
-        const bool in = x >= least, over = v[e] > zt && in;
-        sum += over ? ex2(x) : 0.f;
-        above += over;
-        equal += v[e] == zt && in;
-      }
+    };
+    if (ge) over(Keep<T, true>{zt, all.m, c});
+    else over(Keep<T, false>{zt, all.m, c});
+    above = __reduce_add_sync(0xffffffffu, above) / 16;
+    if (lane == 0) {
+      sh.warp_sum[warp] = sum;
+      sh.warp_equal[warp] = equal;
+      sh.warp_above[warp] = above;
+    }
+  } else if (lane == 0) {
+    sh.warp_sum[warp] = f.s == 0.f ? 0.f : f.s * power(f.m, all.m, c);
+    sh.warp_equal[warp] = sh.warp_above[warp] = 0;
+  }
+  __syncthreads();
+  if (warp == 0) {
+    float sum = lane < WARPS ? sh.warp_sum[lane] : 0.f;
+    if (pass && !filtered) {  // the entries were counted only
+      const Fold mine = lane < WARPS ? sh.fold[rank * WARPS + lane] : Fold{minus_inf(), 0.f};
+      sum = mine.s == 0.f ? 0.f : mine.s * power(mine.m, all.m, c);
     }
     sum = warp_sum(sum);
-    above = __reduce_add_sync(0xffffffffu, above);
-    equal = __reduce_add_sync(0xffffffffu, equal);
+    const uint32_t equal = __reduce_add_sync(0xffffffffu, lane < WARPS ? sh.warp_equal[lane] : 0u);
+    const uint32_t above = __reduce_add_sync(0xffffffffu, lane < WARPS ? sh.warp_above[lane] : 0u);
     if (lane < C) {
-      put_f1(map_to_rank(smem_addr(&sh.sum[g]), lane), sum);
-      put_u1(map_to_rank(smem_addr(&sh.above[g]), lane), above);
-      put_u1(map_to_rank(smem_addr(&sh.equal[g]), lane), equal);
+      put_u2(map_to_rank(smem_addr(&sh.part_a[rank]), lane), __float_as_uint(sum), equal);
+      asm volatile("st.shared::cluster.u32 [%0], %1;" :: "r"(map_to_rank(smem_addr(&sh.part_b[rank]), lane)), "r"(above) : "memory");
     }
     __syncwarp();
-    cluster_sync_all();
-  } else {
-    __syncthreads();
   }
+  cluster_sync_all();
+  if (warp != 0) return;
 
-  // ---- the segment that holds the token, by every warp alike
-  const float wt = ties ? ex2(exponent_of(zt)) : 0.f;
-  const int M = (n_seg + 31) / 32, k0 = min(lane * M, n_seg), k1 = min(k0 + M, n_seg);
-  uint32_t before = 0, kept = 0;  // entries equal to the threshold in the segments before; all kept
-  if (pass) {
-    uint32_t here = 0;
-    for (int k = k0; k < k1; ++k) {
-      here += sh.equal[k];
-      kept += sh.above[k];
+  // ---- the CTA that holds the token, by the first warp of each alike
+  const float wt = ties ? ex2(exponent(zt, all.m, c)) : 0.f;
+  const Part part = lane < C ? Part{__uint_as_float(sh.part_a[lane].x), sh.part_a[lane].y, sh.part_b[lane]} : Part{0.f, 0u, 0u};
+  uint32_t upto = part.equal;
+#pragma unroll
+  for (int o = 1; o < kMostCluster; o <<= 1) {
+    const uint32_t a = __shfl_up_sync(0xffffffffu, upto, o);
+    if (lane >= o) upto += a;
+  }
+  const uint32_t before = upto - part.equal, mine_ties = before >= ties ? 0u : min(ties - before, part.equal);
+  const float mine = fmaf(static_cast<float>(mine_ties), wt, part.sum);
+  const float total = warp_sum(mine);
+  float left;
+  const int at_cta = pick_at(C, set.u * total, lane, [&](int) { return mine; }, left);  // a lane has one
+  if (at_cta != rank) return;
+  if (kept < 0) kept = __reduce_add_sync(0xffffffffu, part.above);
+  const uint32_t ties_before = __shfl_sync(0xffffffffu, before, rank);
+
+  // ---- its tile
+  const int nt = t1 - t0, M = (nt + 31) / 32, k0 = min(lane * M, nt), k1 = min(k0 + M, nt);
+  uint32_t rank_eq = 0;
+  if (ties)
+    for (int k = k0; k < k1; ++k) rank_eq += tiles[k].kept.equal;
+  uint32_t eq_run = rank_eq;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint32_t a = __shfl_up_sync(0xffffffffu, eq_run, o);
+    if (lane >= o) eq_run += a;
+  }
+  const uint32_t lane_before = ties_before + eq_run - rank_eq;
+  auto ties_until = [&](int k) {  // entries equal to the threshold before tile k of this lane's
+    uint32_t b = lane_before;
+    for (int i = k0; i < k; ++i) b += tiles[i].kept.equal;
+    return b;
+  };
+  const int at = pick_at(nt, left, lane, [&](int k) {
+    if (!filtered) return tiles[k].fold.s == 0.f ? 0.f : tiles[k].fold.s * power(tiles[k].fold.m, all.m, c);
+    if (!ties) return tiles[k].kept.sum;
+    const uint32_t b = ties_until(k);
+    return fmaf(b >= ties ? 0.f : static_cast<float>(min(ties - b, tiles[k].kept.equal)), wt, tiles[k].kept.sum);
+  }, left);
+  uint32_t used = ties ? __shfl_sync(0xffffffffu, at >= k0 && at < k1 ? ties_until(at) : 0u, at / M) : 0u;
+
+  // ---- and the token in it: the weights in order, ties by their rank
+  row.tile(t0 + at, lane, q);
+  int token = -1, last = -1;
+  float acc0 = 0.f;
+#pragma unroll
+  for (int i = 0; i < kTileBlocks; ++i) {
+    float v[N], w[N], s = 0.f;
+    uint32_t eq = 0;
+    Elem<T>::unpack(q[i], v);
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      w[e] = (ge ? v[e] >= zt : v[e] > zt) ? v[e] : minus_inf();
+      eq += ties && v[e] == zt;
     }
-    uint32_t run = here;
+    exps(w, all.m, c);
+    uint32_t eq_here = eq;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const uint32_t a = __shfl_up_sync(0xffffffffu, run, o);
-      if (lane >= o) run += a;
+      const uint32_t a = __shfl_up_sync(0xffffffffu, eq_here, o);
+      if (lane >= o) eq_here += a;
     }
-    before = run - here;
-    kept = __reduce_add_sync(0xffffffffu, kept) + min(ties, __shfl_sync(0xffffffffu, run, 31));
-  }
-  // a lane's segments are asked for in order: the ties of segment k come after those of the lane's segments before it
-  auto ties_of = [&](int k) -> uint32_t {
-    uint32_t b = before;
-    for (int i = k0; i < k; ++i) b += sh.equal[i];
-    return b >= ties ? 0u : min(ties - b, sh.equal[k]);
-  };
-  float total_kept = 0.f;
-  auto weight = [&](int k) {
-    if (!filtered) return sh.fold[k].s == 0.f ? 0.f : sh.fold[k].s * power(sh.fold[k].m, all.m, c);
-    return fmaf(static_cast<float>(ties_of(k)), wt, sh.sum[k]);
-  };
-  for (int k = k0; k < k1; ++k) total_kept += weight(k);
-  total_kept = warp_sum(total_kept);
-  float left;
-  const int at = pick(n_seg, set.u, lane, weight, left);
-  // how many of the threshold's entries that segment keeps
-  const uint32_t ties_there = filtered ? __shfl_sync(0xffffffffu, at >= k0 && at < k1 ? ties_of(at) : 0u, max(at, 0) / M) : 0u;
-  if (at != g) return;
-  uint32_t rest = ties_there;
-  // the entries' weights in order, ties by their rank
-  int token = -1;
-  {
-    int last = -1;
-    float acc0 = 0.f;
-    for (int b0 = 0; b0 < nb && token < 0; b0 += 32) {
-      const int k = b0 + lane;
-      float v[N], w[N], s = 0.f;
-      uint32_t eq = 0, bits = 0;
+    uint32_t nth = used + eq_here - eq;
+    used += __shfl_sync(0xffffffffu, eq_here, 31);
 #pragma unroll
-      for (int e = 0; e < N; ++e) w[e] = 0.f;
-      if (k < nb) {
-        mine.load(k, v);
-#pragma unroll
-        for (int e = 0; e < N; ++e) {
-          if (!(v[e] >= zt) || v[e] == minus_inf()) continue;
-          const float x = exponent_of(v[e]);
-          if (!(x >= least)) continue;
-          if (v[e] > zt || !filtered) {
-            w[e] = ex2(x);
-          } else {
-            ++eq;
-            bits |= 1u << e;
-          }
-        }
+    for (int e = 0; e < N; ++e) {
+      if (ties && v[e] == zt) {
+        if (nth < ties) w[e] = wt;
+        ++nth;
       }
-      uint32_t rank_eq = eq;
+      s += w[e];
+      if (w[e] > 0.f) last = ((t0 + at) * kTileBlocks32 + 32 * i + lane) * N + e;
+    }
+    float run_s = s;
 #pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const uint32_t a = __shfl_up_sync(0xffffffffu, rank_eq, o);
-        if (lane >= o) rank_eq += a;
-      }
-      const uint32_t eq_all = __shfl_sync(0xffffffffu, rank_eq, 31);
-      uint32_t used = rank_eq - eq;
-#pragma unroll
-      for (int e = 0; e < N; ++e)
-        if (bits >> e & 1) {
-          if (used < rest) w[e] = wt;
-          ++used;
-        }
-      rest -= min(rest, eq_all);
+    for (int o = 1; o < 32; o <<= 1) {
+      const float a = __shfl_up_sync(0xffffffffu, run_s, o);
+      if (lane >= o) run_s += a;
+    }
+    const uint32_t hit = __ballot_sync(0xffffffffu, token < 0 && s > 0.f && acc0 + run_s > left);
+    if (hit) {
+      const int from = __ffs(hit) - 1;
+      float acc = acc0 + (run_s - s);
+      int here = -1;
 #pragma unroll
       for (int e = 0; e < N; ++e) {
-        s += w[e];
-        if (w[e] > 0.f) last = k * N + e;
+        acc += w[e];
+        if (here < 0 && w[e] > 0.f && acc > left) here = ((t0 + at) * kTileBlocks32 + 32 * i + lane) * N + e;
       }
-      float run = s;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const float a = __shfl_up_sync(0xffffffffu, run, o);
-        if (lane >= o) run += a;
-      }
-      const uint32_t over = __ballot_sync(0xffffffffu, s > 0.f && acc0 + run > left);
-      if (over) {
-        const int from = __ffs(over) - 1;
-        float acc = acc0 + (run - s);
-        int here = -1;
-#pragma unroll
-        for (int e = 0; e < N; ++e) {
-          acc += w[e];
-          if (here < 0 && w[e] > 0.f && acc > left) here = k * N + e;
-        }
-        token = __shfl_sync(0xffffffffu, here >= 0 ? here : last, from);
-      }
-      acc0 += __shfl_sync(0xffffffffu, run, 31);
+      token = __shfl_sync(0xffffffffu, here >= 0 ? here : last, from);
     }
-    // where rounding leaves the sum short of its goal: the last that has any weight
-    if (token < 0) token = static_cast<int>(__reduce_max_sync(0xffffffffu, last));
+    acc0 += __shfl_sync(0xffffffffu, run_s, 31);
   }
+  // where rounding leaves the sum short of its goal: the last that has any weight
+  if (token < 0) token = static_cast<int>(__reduce_max_sync(0xffffffffu, last));
   if (lane != 0) return;
-  token = min(max(e0 + token - mine.lo, 0), p.V - 1);
+  token = min(max(token - row.lo, 0), p.V - 1);
   const float zx = Elem<T>::one(z[token]);
-  p.ids[row] = token;
-  p.logp[row] = logp_of(zx, all, c);
-  if (p.among) p.among[row] = (exponent_of(zx) - log2f(total_kept)) * kLn2;
-  if (p.n_kept) p.n_kept[row] = static_cast<int32_t>(kept);
+  p.ids[r] = token;
+  p.logp[r] = logp_of(zx, all, c);
+  if (p.among) p.among[r] = (exponent(zx, all.m, c) - log2f(total)) * kLn2;
+  if (p.n_kept) p.n_kept[r] = static_cast<int32_t>(kept);
 }
 
 // ---------------------------------------------------------------- host
 
 constexpr int kSMs = 152;
-constexpr int64_t kPastBytes = 16;
-constexpr int64_t kGoodBytes = 84 * 1024;   // two CTAs per SM: one's copies run under the other's arithmetic
-constexpr int64_t kMostBytes = 200 * 1024;  // beside the tables
-static_assert(sizeof(Shared<16>) <= 24 * 1024 && kMostBytes + kPastBytes + sizeof(Shared<16>) <= 227 * 1024, "a CTA's shared memory");
-
-inline int64_t segment(int64_t V, int64_t parts) { return ((V + parts - 1) / parts + 7) / 8 * 8; }
-inline int64_t segment_bytes(int64_t V, int64_t parts, int es) { return segment(V, parts) * es + 16; }
 
 template <typename T, int WARPS>
-rl_status launch(Args& a, int C, cudaStream_t s) {
-  a.seg = static_cast<int32_t>(segment(a.V, C * WARPS));
-  a.seg_bytes = static_cast<int32_t>(segment_bytes(a.V, C * WARPS, sizeof(T)));
+rl_status launch(Args& a, int C, int64_t all_tiles, cudaStream_t s) {
+  a.tiles = static_cast<int32_t>((all_tiles + C - 1) / C);
   auto kern = sample_kernel<T, WARPS>;
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess) return cuda_error(e, "cudaGetDevice");
-  // once per device
-  static std::atomic<uint64_t> ready{0};
-  const uint64_t bit = dev < 64 ? uint64_t(1) << dev : 0;
-  if (!(ready.load() & bit)) {
-    e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kMostBytes + kPastBytes));
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-    if (e != cudaSuccess) return cuda_error(e, "cudaFuncSetAttribute(sample_kernel)");
-    ready |= bit;
-  }
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -598,26 +791,27 @@ rl_status launch(Args& a, int C, cudaStream_t s) {
   attr[0].val.clusterDim.y = 1;
   attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = C > 1 ? 1 : 0;
   cfg.blockDim = dim3(WARPS * 32);
   cfg.gridDim = dim3(static_cast<unsigned>(a.rows * C));
-  cfg.dynamicSmemBytes = static_cast<size_t>(WARPS) * a.seg_bytes + kPastBytes;
+  cfg.dynamicSmemBytes = static_cast<size_t>(a.tiles) * sizeof(Tile);
   cfg.stream = s;
-  e = cudaLaunchKernelEx(&cfg, kern, a);
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, a);
   return e == cudaSuccess ? RL_OK : cuda_error(e, "sample_kernel launch");
 }
 
+constexpr int64_t kMostTiles = 2064;  // of a CTA: their table, 16 KB, and the others fit in what any kernel may take
+
 template <typename T>
 rl_status run(Args& a, cudaStream_t s) {
-  const int es = sizeof(T);
-  auto bytes = [&](int C) { return segment_bytes(a.V, C * 16, es) * 16; };
+  const int64_t nb = (a.V + 7) * sizeof(T) / 16 + 1, tiles = (nb + kTileBlocks32 - 1) / kTileBlocks32;
+  // short rows: a tile for each of four warps
+  if (tiles <= 8 && a.rows > kSMs) return launch<T, 4>(a, 1, tiles, s);
+  // as many CTAs a row as fill the SMs twice over while each of their warps has a tile
   int C = 1;
-  while (C < kMaxCluster && bytes(C) > kGoodBytes) C *= 2;
-  if (bytes(C) > kMostBytes)
-    return set_error(RL_ERR_UNSUPPORTED, "rl_sample_tokens: V is too large (a row has to fit in 16 CTAs of 200 KB)");
-  if (C == 1 && a.V * es <= 16 * 1024) return launch<T, 4>(a, 1, s);
-  while (C < kMaxCluster && a.rows * C < kSMs && segment_bytes(a.V, 2 * C * 16, es) >= 1024) C *= 2;
-  return launch<T, 16>(a, C, s);
+  while (C < 8 && ((a.rows * C * 2 <= 2 * kSMs && tiles >= 2 * C * 16) || tiles > kMostTiles * C)) C *= 2;
+  if (tiles > kMostTiles * C) return set_error(RL_ERR_UNSUPPORTED, "rl_sample_tokens: V is too large");
+  return launch<T, 16>(a, C, tiles, s);
 }
 
 }  // namespace sample
@@ -646,7 +840,7 @@ extern "C" rl_status rl_sample_tokens(const void* logits, rl_dtype dtype, int64_
   if (!logits || !sample_u || !out_ids || !out_logp || !ws)
     return set_error(RL_ERR_INVALID_ARG, f + "a required pointer is NULL");
   if (!aligned16(logits) || !aligned16(ws)) return set_error(RL_ERR_ALIGNMENT, f + "logits and ws must be 16-byte aligned");
-  if (V > (1 << 24) || rows > (1 << 26)) return set_error(RL_ERR_UNSUPPORTED, f + "at most 2^24 entries and 2^26 rows");
+  if (V > (dtype == RL_BF16 ? 1 << 24 : 1 << 23) || rows > (1 << 26)) return set_error(RL_ERR_UNSUPPORTED, f + "at most 2^24 entries (fp32: 2^23) and 2^26 rows");
   if (ws_bytes < kWsHeader) return set_error(RL_ERR_WORKSPACE_TOO_SMALL, f + "workspace smaller than its header");
   sample::Args a = {};
   a.logits = logits;
