@@ -153,6 +153,18 @@ struct RowBlocks {
   }
 };
 
+// A barrier of all CTAs of a row, and a word of shared memory of one of them.
+template <bool CLUSTER>
+__device__ __forceinline__ void sync_all() {
+  if (CLUSTER) cluster_sync_all();
+  else __syncthreads();
+}
+template <bool CLUSTER>
+__device__ __forceinline__ unsigned long long of_cta(const uint32_t* two, int r) {
+  if (CLUSTER) return ld_cluster_u64(map_to_rank(smem_addr(two), r));
+  return *reinterpret_cast<const unsigned long long*>(two);
+}
+
 // A border: entries above `key` and the first m of those equal to it; their number above it and their mass.
 struct Border {
   uint32_t key, m, above;
@@ -198,7 +210,7 @@ struct Level {
   int shift;
 };
 
-template <typename T, int WARPS>
+template <typename T, int WARPS, bool CLUSTER>
 struct Row {
   Shared<WARPS>& sh;
   const RowBlocks<T>& row;
@@ -221,7 +233,7 @@ struct Row {
   __device__ __forceinline__ void count(const Level& to) {
     const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
     const bool weigh = masses && to.shift > kSingle;
-    cluster_sync_all();  // the other CTAs have read the last level's
+    sync_all<CLUSTER>();  // the other CTAs have read the last level's
     for (int i = threadIdx.x; i < kBins; i += kThreads) {
       sh.count[i] = 0;
       sh.low[i] = 0;
@@ -251,7 +263,7 @@ struct Row {
         }
       }
     }
-    cluster_sync_all();
+    sync_all<CLUSTER>();
   }
 
   // The key of the first entry of a bin.
@@ -270,23 +282,22 @@ struct Row {
       w[i] = 0;
     }
     const int own = threadIdx.x * kOwn;
-    const uint32_t at_n = smem_addr(&sh.count[own]), at_l = smem_addr(&sh.low[own]), at_h = smem_addr(&sh.high[own]);
 #pragma unroll 4
     for (int r = 0; r < C; ++r) {
-      const uint32_t from = map_to_rank(at_n, r);
 #pragma unroll
       for (int i = 0; i < kOwn; i += 2) {
-        const unsigned long long two = ld_cluster_u64(from + 4 * i);
-        n[i] += static_cast<uint32_t>(two);
-        n[i + 1] += static_cast<uint32_t>(two >> 32);
+        // the window's patterns rise where its bins fall
+        const unsigned long long two = of_cta<CLUSTER>(&sh.count[l.shift < 0 ? kBins - 2 - own - i : own + i], r);
+        const uint32_t a = static_cast<uint32_t>(two), b = static_cast<uint32_t>(two >> 32);
+        n[i] += l.shift < 0 ? b : a;
+        n[i + 1] += l.shift < 0 ? a : b;
       }
     }
     if (masses && !single)
       for (int r = 0; r < C; ++r) {
-        const uint32_t from_l = map_to_rank(at_l, r), from_h = map_to_rank(at_h, r);
 #pragma unroll
         for (int i = 0; i < kOwn; i += 2) {
-          const unsigned long long lo = ld_cluster_u64(from_l + 4 * i), hi = ld_cluster_u64(from_h + 4 * i);
+          const unsigned long long lo = of_cta<CLUSTER>(&sh.low[own + i], r), hi = of_cta<CLUSTER>(&sh.high[own + i], r);
           w[i] += (hi << 32) + (lo & 0xffffffffu);
           w[i + 1] += (hi & 0xffffffff00000000ull) + (lo >> 32);
         }
@@ -457,9 +468,18 @@ template <typename T, bool GE>
 struct Keep {
   static constexpr int N = Elem<T>::N;
   float zt, ref, c;
-  // A block's kept entries, the others minus infinity; false: it has none. Adds those equal to zt (not GE) to `equal`, and
+  // Whether a block has an entry of at least zt.
+  __device__ __forceinline__ bool reaches(const uint4& q) const {
+    if constexpr (sizeof(T) == 2) {
+      const uint32_t t = __float_as_uint(zt) >> 16, t2 = t | t << 16;
+      return (least2(q.x, t2) | least2(q.y, t2) | least2(q.z, t2) | least2(q.w, t2)) != 0;
+    } else {
+      return fmaxf(fmaxf(__uint_as_float(q.x), __uint_as_float(q.y)), fmaxf(__uint_as_float(q.z), __uint_as_float(q.w))) >= zt;
+    }
+  }
+  // A block's kept entries, the others minus infinity. Adds those equal to zt (not GE) to `equal`, and
   // with `count` the kept ones to `kept`.
-  __device__ __forceinline__ bool block(const uint4& q, float (&z)[N], uint32_t& equal, uint32_t& kept, bool count) const {
+  __device__ __forceinline__ void block(const uint4& q, float (&z)[N], uint32_t& equal, uint32_t& kept, bool count) const {
     if constexpr (sizeof(T) == 2) {
       const uint32_t t = __float_as_uint(zt) >> 16, t2 = t | t << 16;
       const uint32_t v[4] = {q.x, q.y, q.z, q.w};
@@ -472,19 +492,15 @@ struct Keep {
         if (count) kept += __popc(m[i]);
       }
       Elem<T>::unpack(make_uint4(r[0], r[1], r[2], r[3]), z);
-      return (m[0] | m[1] | m[2] | m[3]) != 0;
     } else {
       Elem<T>::unpack(q, z);
-      bool any = false;
 #pragma unroll
       for (int e = 0; e < N; ++e) {
         const bool in = GE ? z[e] >= zt : z[e] > zt;
         if (!GE) equal += z[e] == zt ? 16 : 0;
         if (count) kept += in ? 16 : 0;
-        any |= in;
         z[e] = in ? z[e] : minus_inf();
       }
-      return any;
     }
   }
   // The kept weights of a lane's blocks of a tile. (equal and kept count 16 an entry.)
@@ -492,9 +508,9 @@ struct Keep {
     float2 s = make_float2(0.f, 0.f);
 #pragma unroll
     for (int i = 0; i < kTileBlocks; ++i) {
+      if (!__any_sync(0xffffffffu, reaches(q[i]))) continue;  // most blocks of most rows
       float z[N];
-      const bool any = block(q[i], z, equal, kept, count);
-      if (!__any_sync(0xffffffffu, any)) continue;
+      block(q[i], z, equal, kept, count);
       exps(z, ref, c);
 #pragma unroll
       for (int e = 0; e < N; e += 2) s = add2(s, make_float2(z[e], z[e + 1]));
@@ -503,20 +519,27 @@ struct Keep {
   }
 };
 
-template <typename T, int WARPS>
+// One more of the pattern's bin of the window, if it has one.
+__device__ __forceinline__ void count_pattern(uint32_t bins, uint32_t pattern) {
+  const uint32_t off = pattern * 4u - kWindowLow * 4u;
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.lt.u32 p, %0, %2;\n\t@p red.shared.add.u32 [%1], 1;\n\t}"
+               :: "r"(off), "r"(bins + off), "n"(kBins * 4) : "memory");
+}
+
+template <typename T, int WARPS, bool CLUSTER>
 __global__ void __launch_bounds__(WARPS * 32, 1024 / (WARPS * 32)) sample_kernel(const Args p) {
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ __align__(16) Shared<WARPS> sh;
   Tile* tiles = reinterpret_cast<Tile*>(smem);
   constexpr int N = Elem<T>::N;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int rank = static_cast<int>(cluster_ctarank()), C = static_cast<int>(cluster_nctarank());
+  const int rank = CLUSTER ? static_cast<int>(cluster_ctarank()) : 0, C = CLUSTER ? static_cast<int>(cluster_nctarank()) : 1;
   const int64_t r = blockIdx.x / C;
   const T* z = static_cast<const T*>(p.logits) + r * p.ld;
   const RowBlocks<T> row(z, p.V, static_cast<const T*>(p.logits) + (p.rows - 1) * p.ld + p.V);
   const int all_tiles = (row.nb + kTileBlocks32 - 1) / kTileBlocks32;
   const int t0 = min(rank * p.tiles, all_tiles), t1 = min(t0 + p.tiles, all_tiles);
-  asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");  // the other CTAs have started
+  if (CLUSTER) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");  // the other CTAs have started
   uint4 q[kTileBlocks];
   if (t0 + warp < t1) row.tile(t0 + warp, lane, q);
   Settings set{p.temperature, p.top_p, p.min_p, p.u[r], p.top_k};
@@ -533,6 +556,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1024 / (WARPS * 32)) sample_kernel
   const bool window = (by_k || by_p) && (sizeof(T) == 2 || !by_p);
 
   // ---- the row's largest entry and its normaliser
+  const uint32_t bins = smem_addr(sh.count);
   Running run{minus_inf(), {0.f, 0.f}, 0};
   Fold f{minus_inf(), 0.f};
   for (int t = t0 + warp; t < t1; t += WARPS) {
@@ -547,12 +571,8 @@ __global__ void __launch_bounds__(WARPS * 32, 1024 / (WARPS * 32)) sample_kernel
         const uint32_t v[4] = {now[i].x, now[i].y, now[i].z, now[i].w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const uint32_t hi = kWindowTop - (v[e] >> 16);
-          if (hi < kBins) atomicAdd(&sh.count[hi], 1u);
-          if (sizeof(T) == 2) {
-            const uint32_t lo = kWindowTop - (v[e] & 0xffffu);
-            if (lo < kBins) atomicAdd(&sh.count[lo], 1u);
-          }
+          count_pattern(bins, v[e] >> 16);
+          if (sizeof(T) == 2) count_pattern(bins, v[e] & 0xffffu);
         }
       }
     } else if (!filtered) {
@@ -565,10 +585,14 @@ __global__ void __launch_bounds__(WARPS * 32, 1024 / (WARPS * 32)) sample_kernel
     }
   }
   if (filtered) f = of_warp(run, c);
-  asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
-  if (lane < C) put_f2(map_to_rank(smem_addr(&sh.fold[rank * WARPS + warp]), lane), f.m, f.s);
-  __syncwarp();
-  cluster_sync_all();
+  if (CLUSTER) {
+    asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+    if (lane < C) put_f2(map_to_rank(smem_addr(&sh.fold[rank * WARPS + warp]), lane), f.m, f.s);
+    __syncwarp();
+  } else if (lane == 0) {
+    sh.fold[warp] = f;
+  }
+  sync_all<CLUSTER>();
   if (warp == 0) {
     const Fold all = merged(sh.fold, C * WARPS, c, lane);
     if (lane == 0) {
@@ -604,7 +628,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1024 / (WARPS * 32)) sample_kernel
     kept = 1;
   } else if (by_k || by_p) {
     const uint32_t top = key_of(all.m);
-    Row<T, WARPS> s{sh, row, t0, t1, all, c, top, C, by_p};
+    Row<T, WARPS, CLUSTER> s{sh, row, t0, t1, all, c, top, C, by_p};
     Border b;
     const bool in_window = window && top >= (0x80000000u | kWindowLow << 16) && top <= (0x8000ffffu | kWindowTop << 16);
     if (s.search(by_k ? set.top_k : 0, set.top_p, in_window ? Level{0u, -1} : Level{0u, kBf16Shift}, b)) {
@@ -661,13 +685,18 @@ __global__ void __launch_bounds__(WARPS * 32, 1024 / (WARPS * 32)) sample_kernel
     sum = warp_sum(sum);
     const uint32_t equal = __reduce_add_sync(0xffffffffu, lane < WARPS ? sh.warp_equal[lane] : 0u);
     const uint32_t above = __reduce_add_sync(0xffffffffu, lane < WARPS ? sh.warp_above[lane] : 0u);
-    if (lane < C) {
+    if (!CLUSTER) {
+      if (lane == 0) {
+        sh.part_a[0] = make_uint2(__float_as_uint(sum), equal);
+        sh.part_b[0] = above;
+      }
+    } else if (lane < C) {
       put_u2(map_to_rank(smem_addr(&sh.part_a[rank]), lane), __float_as_uint(sum), equal);
       asm volatile("st.shared::cluster.u32 [%0], %1;" :: "r"(map_to_rank(smem_addr(&sh.part_b[rank]), lane)), "r"(above) : "memory");
     }
     __syncwarp();
   }
-  cluster_sync_all();
+  if (CLUSTER) cluster_sync_all();
   if (warp != 0) return;
 
   // ---- the CTA that holds the token, by the first warp of each alike
@@ -780,10 +809,10 @@ __global__ void __launch_bounds__(WARPS * 32, 1024 / (WARPS * 32)) sample_kernel
 
 constexpr int kSMs = 152;
 
-template <typename T, int WARPS>
+template <typename T, int WARPS, bool CLUSTER>
 rl_status launch(Args& a, int C, int64_t all_tiles, cudaStream_t s) {
   a.tiles = static_cast<int32_t>((all_tiles + C - 1) / C);
-  auto kern = sample_kernel<T, WARPS>;
+  auto kern = sample_kernel<T, WARPS, CLUSTER>;
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -805,13 +834,14 @@ constexpr int64_t kMostTiles = 2064;  // of a CTA: their table, 16 KB, and the o
 template <typename T>
 rl_status run(Args& a, cudaStream_t s) {
   const int64_t nb = (a.V + 7) * sizeof(T) / 16 + 1, tiles = (nb + kTileBlocks32 - 1) / kTileBlocks32;
-  // short rows: a tile for each of four warps
-  if (tiles <= 8 && a.rows > kSMs) return launch<T, 4>(a, 1, tiles, s);
+  // many rows: small CTAs, which wait less for one another, and do what a row takes beside its entries with fewer warps
+  if (tiles <= 8 && a.rows > kSMs) return launch<T, 4, false>(a, 1, tiles, s);
+  if (a.rows > 2 * kSMs && tiles <= kMostTiles) return launch<T, 8, false>(a, 1, tiles, s);
   // as many CTAs a row as fill the SMs twice over while each of their warps has a tile
   int C = 1;
   while (C < 8 && ((a.rows * C * 2 <= 2 * kSMs && tiles >= 2 * C * 16) || tiles > kMostTiles * C)) C *= 2;
   if (tiles > kMostTiles * C) return set_error(RL_ERR_UNSUPPORTED, "rl_sample_tokens: V is too large");
-  return launch<T, 16>(a, C, tiles, s);
+  return C > 1 ? launch<T, 16, true>(a, C, tiles, s) : launch<T, 16, false>(a, 1, tiles, s);
 }
 
 }  // namespace sample
