@@ -167,7 +167,9 @@ __device__ __forceinline__ unsigned long long of_cta(const uint32_t* two, int r)
 
 // A border: entries above `key` and the first m of those equal to it; their number above it and their mass.
 struct Border {
-  uint32_t key, m, above;
+  alignas(8) uint32_t key;
+  uint32_t m;
+  alignas(8) uint32_t above;
   unsigned long long mass, unit;  // of the entries above; of one entry equal to it
 };
 
@@ -181,8 +183,17 @@ template <int WARPS>
 struct Shared {
   Fold fold[WARPS * kMostCluster];    // every warp's, the same in every CTA of the cluster
   alignas(16) uint32_t count[kBins];  // this CTA's entries
-  alignas(16) uint32_t low[kBins];    // and their mass
-  alignas(16) uint32_t high[kBins];
+  union {
+    struct {
+      alignas(16) uint32_t low[kBins];  // and their mass
+      alignas(16) uint32_t high[kBins];
+    };
+    unsigned long long list[kBins];  // the entries that may be kept, where they are few: by size, then by index
+  };
+  alignas(8) uint32_t n_list;
+  uint32_t n_equal;
+  unsigned long long total;
+  uint32_t others[32];
   uint32_t warp_count[WARPS];
   unsigned long long warp_mass[WARPS];
   Border found;
@@ -196,12 +207,13 @@ struct Shared {
 };
 
 // A tile's (max, sum) where nothing is filtered, else the kept weights above the threshold and the entries equal to it.
+struct KeptOfTile {
+  float sum;
+  uint32_t equal;
+};
 union Tile {
   Fold fold;
-  struct {
-    float sum;
-    uint32_t equal;
-  } kept;
+  KeptOfTile kept;
 };
 
 // The bins of distances d0 .. d0 + (kBins << shift) from the largest entry's key; shift < 0: the window.
@@ -293,7 +305,7 @@ struct Row {
         n[i + 1] += l.shift < 0 ? a : b;
       }
     }
-    if (masses && !single)
+    if (masses && !single && l.shift >= 0)
       for (int r = 0; r < C; ++r) {
 #pragma unroll
         for (int i = 0; i < kOwn; i += 2) {
@@ -306,7 +318,9 @@ struct Row {
     unsigned long long mine_w = 0;
 #pragma unroll
     for (int i = 0; i < kOwn; ++i) {
-      if (masses && single && n[i] != 0) w[i] = n[i] * mass_of(weight(value_of(entry_key<T>(key_at(l, own + i)))));
+      // (of an fp32 row's window at least that: a bin's smallest value)
+      if (masses && (single || l.shift < 0) && n[i] != 0)
+        w[i] = n[i] * mass_of(weight(value_of(l.shift < 0 ? key_at(l, own + i) & 0xffff0000u : entry_key<T>(key_at(l, own + i)))));
       mine_n += n[i];
       mine_w += w[i];
     }
@@ -343,6 +357,138 @@ struct Row {
         all_w += b;
       }
     }
+  }
+
+  // The same for an fp32 row whose window says that few entries can be kept: they are gathered in the first CTA and sorted,
+  // and the border is read off the running sum. false: they are not few, or the border is not in the window.
+  __device__ __forceinline__ bool search_list(int32_t top_k, float top_p, const float* tile_max, Border& found) {
+    const int warp = threadIdx.x / 32, lane = threadIdx.x & 31, rank = CLUSTER ? static_cast<int>(cluster_ctarank()) : 0;
+    const Level level{0u, -1};
+    add_up(level);
+    if (threadIdx.x == 0) {
+      sh.bin = -1;
+      sh.n_list = 0;
+      sh.n_equal = 0;
+    }
+    __syncthreads();
+    {
+      // the bin by whose end top_k entries, or certainly top_p of the mass, have come
+      const unsigned long long goal = static_cast<unsigned long long>(static_cast<double>(top_p) * static_cast<double>(all.s) * kMassUnit * (1.0 + 4e-6));
+      uint32_t a = run_n;
+      unsigned long long m = run_w;
+#pragma unroll
+      for (int i = 0; i < kOwn; ++i) {
+        if (top_k ? a < top_k && a + n[i] >= top_k : m < goal && m + w[i] >= goal) {
+          sh.bin = threadIdx.x * kOwn + i;
+          sh.found.above = a + n[i];
+        }
+        a += n[i];
+        m += w[i];
+      }
+    }
+    __syncthreads();
+    const int bin = sh.bin;
+    const uint32_t most = sh.found.above;
+    if (bin < 0 || most > kBins) return false;  // the same in every CTA
+    const float edge = value_of(key_at(level, bin) & 0xffff0000u);
+    for (int t = t0 + warp; t < t1; t += WARPS) {
+      if (!(tile_max[t - t0] >= edge)) continue;
+      uint4 q[kTileBlocks];
+      row.tile(t, lane, q);
+#pragma unroll
+      for (int i = 0; i < kTileBlocks; ++i) {
+        float z[N];
+        Elem<T>::unpack(q[i], z);
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+          if (z[e] >= edge)
+            sh.list[atomicAdd(&sh.n_list, 1u)] =
+                static_cast<unsigned long long>(~key_of(z[e])) << 32 | static_cast<uint32_t>((t * kTileBlocks32 + 32 * i + lane) * N + e);
+      }
+    }
+    sync_all<CLUSTER>();
+    if (rank == 0) {
+      int have = static_cast<int>(sh.n_list);
+      for (int r = 1; r < C; ++r) {  // (C == 1 without a cluster)
+        const int more = static_cast<int>(static_cast<uint32_t>(ld_cluster_u64(map_to_rank(smem_addr(&sh.n_list), r))));
+        for (int i = threadIdx.x; i < more; i += kThreads) sh.list[have + i] = ld_cluster_u64(map_to_rank(smem_addr(&sh.list[i]), r));
+        have += more;
+      }
+      int size = 32;
+      while (size < have) size *= 2;
+      for (int i = have + threadIdx.x; i < size; i += kThreads) sh.list[i] = ~0ull;
+      __syncthreads();
+      for (int k = 2; k <= size; k *= 2)
+        for (int j = k / 2; j > 0; j /= 2) {
+          for (int i = threadIdx.x; i < size / 2; i += kThreads) {
+            const int x = 2 * i - (i & (j - 1)), y = x + j;  // the i-th pair at distance j
+            const unsigned long long a = sh.list[x], b = sh.list[y];
+            if ((a > b) == ((x & k) == 0)) {
+              sh.list[x] = b;
+              sh.list[y] = a;
+            }
+          }
+          __syncthreads();
+        }
+      // the running mass
+      unsigned long long v[kOwn], mine = 0;
+#pragma unroll
+      for (int i = 0; i < kOwn; ++i) {
+        const int at = threadIdx.x * kOwn + i;
+        v[i] = masses && at < have ? mass_of(weight(value_of(~static_cast<uint32_t>(sh.list[at] >> 32)))) : 0;
+        mine += v[i];
+      }
+      unsigned long long run = mine;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const unsigned long long a = __shfl_up_sync(0xffffffffu, run, o);
+        if (lane >= o) run += a;
+      }
+      if (lane == 31) sh.warp_mass[warp] = run;
+      if (threadIdx.x == 0) sh.bin = top_k ? top_k - 1 : have - 1;  // the last kept
+      __syncthreads();
+      run -= mine;
+      for (int u = 0; u < warp; ++u) run += sh.warp_mass[u];
+      if (masses) {
+        unsigned long long r = run;
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) {
+          r += v[i];
+          if (top_k && static_cast<int>(threadIdx.x) * kOwn + i == top_k - 1) sh.total = r;
+        }
+        __syncthreads();
+        const double total = top_k ? static_cast<double>(sh.total) : static_cast<double>(all.s) * kMassUnit;
+        const unsigned long long goal = max(1ull, static_cast<unsigned long long>(ceil(static_cast<double>(top_p) * total)));
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) {
+          if (run < goal && run + v[i] >= goal && static_cast<int>(threadIdx.x) * kOwn + i < have)
+            atomicMin(&sh.bin, static_cast<int>(threadIdx.x) * kOwn + i);
+          run += v[i];
+        }
+        __syncthreads();
+      }
+      const int last = sh.bin;
+      const uint32_t key = ~static_cast<uint32_t>(sh.list[last] >> 32);
+      uint32_t same = 0;
+      for (int i = threadIdx.x; i <= last; i += kThreads) same += ~static_cast<uint32_t>(sh.list[i] >> 32) == key;
+      if (same) atomicAdd(&sh.n_equal, same);
+      __syncthreads();
+      if (threadIdx.x == 0) {
+        sh.found.key = key;
+        sh.found.m = sh.n_equal;
+        sh.found.above = last + 1 - sh.n_equal;
+      }
+    }
+    sync_all<CLUSTER>();
+    if (CLUSTER) {
+      const unsigned long long two = ld_cluster_u64(map_to_rank(smem_addr(&sh.found.key), 0));
+      found.key = static_cast<uint32_t>(two);
+      found.m = static_cast<uint32_t>(two >> 32);
+      found.above = static_cast<uint32_t>(ld_cluster_u64(map_to_rank(smem_addr(&sh.found.above), 0)));
+    } else {
+      found = sh.found;
+    }
+    return true;
   }
 
   // The border of what top_k (0: off) and top_p (1: off) keep of the row; false: they keep everything. `first`: the level
@@ -477,6 +623,15 @@ struct Keep {
       return fmaxf(fmaxf(__uint_as_float(q.x), __uint_as_float(q.y)), fmaxf(__uint_as_float(q.z), __uint_as_float(q.w))) >= zt;
     }
   }
+  // 16 for each of a block's kept entries.
+  __device__ __forceinline__ uint32_t number(const uint4& q) const {
+    if constexpr (sizeof(T) == 2) {
+      const uint32_t t = __float_as_uint(zt) >> 16, t2 = t | t << 16;
+      return __popc(above2(q.x, t2)) + __popc(above2(q.y, t2)) + __popc(above2(q.z, t2)) + __popc(above2(q.w, t2));
+    } else {
+      return ((__uint_as_float(q.x) > zt) + (__uint_as_float(q.y) > zt) + (__uint_as_float(q.z) > zt) + (__uint_as_float(q.w) > zt)) * 16;
+    }
+  }
   // A block's kept entries, the others minus infinity. Adds those equal to zt (not GE) to `equal`, and
   // with `count` the kept ones to `kept`.
   __device__ __forceinline__ void block(const uint4& q, float (&z)[N], uint32_t& equal, uint32_t& kept, bool count) const {
@@ -505,25 +660,71 @@ struct Keep {
   }
   // The kept weights of a lane's blocks of a tile. (equal and kept count 16 an entry.)
   __device__ __forceinline__ float tile(const uint4 (&q)[kTileBlocks], uint32_t& equal, uint32_t& kept, bool count) const {
+    const float rc = -__fmul_rn(ref, c);
+    const bool apart = large(rc);  // of the row
+    const float2 cc = make_float2(c, c), off = make_float2(rc, rc);
     float2 s = make_float2(0.f, 0.f);
 #pragma unroll
     for (int i = 0; i < kTileBlocks; ++i) {
       if (!__any_sync(0xffffffffu, reaches(q[i]))) continue;  // most blocks of most rows
       float z[N];
       block(q[i], z, equal, kept, count);
-      exps(z, ref, c);
 #pragma unroll
-      for (int e = 0; e < N; e += 2) s = add2(s, make_float2(z[e], z[e + 1]));
+      for (int e = 0; e < N; e += 2) {
+        float2 x = fma2(make_float2(z[e], z[e + 1]), cc, off);
+        if (apart) x = make_float2((z[e] - ref) * c, (z[e + 1] - ref) * c);
+        s = add2(s, make_float2(ex2(x.x), ex2(x.y)));
+      }
     }
     return s.x + s.y;
   }
 };
 
-// One more of the pattern's bin of the window, if it has one.
-__device__ __forceinline__ void count_pattern(uint32_t bins, uint32_t pattern) {
+// One more of the pattern's bin of the window; a lane's others are counted in a word of its own, since a condition on the
+// addition costs more than the addition. (`one` is 1, where the compiler does not see it: it adds a known 1 by a longer sequence.)
+__device__ __forceinline__ void count_pattern(uint32_t bins, uint32_t other, uint32_t pattern, uint32_t one) {
   const uint32_t off = pattern * 4u - kWindowLow * 4u;
-  asm volatile("{\n\t.reg .pred p;\n\tsetp.lt.u32 p, %0, %2;\n\t@p red.shared.add.u32 [%1], 1;\n\t}"
-               :: "r"(off), "r"(bins + off), "n"(kBins * 4) : "memory");
+  const uint32_t at = off < kBins * 4u ? bins + off : other;
+  asm volatile("red.shared.add.u32 [%0], %1;" :: "r"(at), "r"(one) : "memory");
+}
+
+// As add_tile, with the exponents' form decided once for the tile; the largest of the lane's entries.
+template <typename T>
+__device__ __forceinline__ float fold_tile(Running& r, const uint4 (&w)[kTileBlocks], float c) {
+  constexpr int N = Elem<T>::N;
+  const float top = largest<T>(w);
+  if (top > r.m) {
+    const float f = power(r.m, top, c);
+    r.s.x *= f;
+    r.s.y *= f;
+    r.m = top;
+  }
+  const float ref = r.m == minus_inf() ? 0.f : r.m, rc = -__fmul_rn(ref, c);
+  if (large(rc)) {
+#pragma unroll 1
+    for (int i = 0; i < kTileBlocks; ++i) {
+      float z[N];
+      Elem<T>::unpack(i < 2 ? (i == 0 ? w[0] : w[1]) : (i == 2 ? w[2] : w[3]), z);
+#pragma unroll
+      for (int e = 0; e < N; ++e) r.s.x += ex2((z[e] - ref) * c);
+    }
+    return top;
+  }
+  const float2 cc = make_float2(c, c), off = make_float2(rc, rc);
+  float2 s0 = make_float2(0.f, 0.f), s1 = s0;  // two chains
+#pragma unroll
+  for (int i = 0; i < kTileBlocks; ++i) {
+    float z[N];
+    Elem<T>::unpack(w[i], z);
+#pragma unroll
+    for (int e = 0; e < N; e += 4) {
+      const float2 a = fma2(make_float2(z[e], z[e + 1]), cc, off), b = fma2(make_float2(z[e + 2], z[e + 3]), cc, off);
+      s0 = add2(s0, make_float2(ex2(a.x), ex2(a.y)));
+      s1 = add2(s1, make_float2(ex2(b.x), ex2(b.y)));
+    }
+  }
+  r.s = add2(r.s, add2(s0, s1));
+  return top;
 }
 
 template <typename T, int WARPS, bool CLUSTER>
@@ -531,6 +732,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1024 / (WARPS * 32)) sample_kernel
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ __align__(16) Shared<WARPS> sh;
   Tile* tiles = reinterpret_cast<Tile*>(smem);
+  float* tile_max = reinterpret_cast<float*>(tiles + p.tiles);
   constexpr int N = Elem<T>::N;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = CLUSTER ? static_cast<int>(cluster_ctarank()) : 0, C = CLUSTER ? static_cast<int>(cluster_nctarank()) : 1;
@@ -553,29 +755,38 @@ __global__ void __launch_bounds__(WARPS * 32, 1024 / (WARPS * 32)) sample_kernel
   const float c = greedy || !known ? kLog2e : kLog2e / set.T;
   const bool by_k = !greedy && set.top_k > 0 && set.top_k < p.V, by_p = !greedy && set.top_p < 1.f;
   const bool by_m = !greedy && set.min_p > 0.f, filtered = greedy || by_k || by_p || by_m;
-  const bool window = (by_k || by_p) && (sizeof(T) == 2 || !by_p);
+  const bool window = by_k || by_p;
 
   // ---- the row's largest entry and its normaliser
-  const uint32_t bins = smem_addr(sh.count);
+  const uint32_t bins = smem_addr(sh.count), other = smem_addr(&sh.others[lane]);
+  uint32_t one;
+  asm volatile("mov.u32 %0, 1;" : "=r"(one));
   Running run{minus_inf(), {0.f, 0.f}, 0};
   Fold f{minus_inf(), 0.f};
+  const bool count_all = !filtered && p.n_kept;
+  uint32_t live = 0;  // entries above minus infinity, 16 each
   for (int t = t0 + warp; t < t1; t += WARPS) {
     uint4 now[kTileBlocks];
 #pragma unroll
     for (int i = 0; i < kTileBlocks; ++i) now[i] = q[i];
     if (t + WARPS < t1) row.tile(t + WARPS, lane, q);
-    add_tile<T, false>(run, now, 0, c);
+    const float most = redux_max(fold_tile<T>(run, now, c));
+    if (filtered && lane == 0) tile_max[t - t0] = most;
     if (window) {
 #pragma unroll
       for (int i = 0; i < kTileBlocks; ++i) {
         const uint32_t v[4] = {now[i].x, now[i].y, now[i].z, now[i].w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          count_pattern(bins, v[e] >> 16);
-          if (sizeof(T) == 2) count_pattern(bins, v[e] & 0xffffu);
+          count_pattern(bins, other, v[e] >> 16, one);
+          if (sizeof(T) == 2) count_pattern(bins, other, v[e] & 0xffffu, one);
         }
       }
     } else if (!filtered) {
+      if (count_all) {
+#pragma unroll
+        for (int i = 0; i < kTileBlocks; ++i) live += Keep<T, false>{minus_inf(), 0.f, 1.f}.number(now[i]);
+      }
       const Fold of = of_warp(run, c);
       if (lane == 0) tiles[t - t0].fold = of;
       const float m = fmaxf(f.m, of.m);
@@ -630,8 +841,10 @@ __global__ void __launch_bounds__(WARPS * 32, 1024 / (WARPS * 32)) sample_kernel
     const uint32_t top = key_of(all.m);
     Row<T, WARPS, CLUSTER> s{sh, row, t0, t1, all, c, top, C, by_p};
     Border b;
-    const bool in_window = window && top >= (0x80000000u | kWindowLow << 16) && top <= (0x8000ffffu | kWindowTop << 16);
-    if (s.search(by_k ? set.top_k : 0, set.top_p, in_window ? Level{0u, -1} : Level{0u, kBf16Shift}, b)) {
+    const bool in_window = top >= (0x80000000u | kWindowLow << 16) && top <= (0x8000ffffu | kWindowTop << 16);
+    bool is = sizeof(T) == 4 && in_window && s.search_list(by_k ? set.top_k : 0, set.top_p, tile_max, b);
+    if (!is) is = s.search(by_k ? set.top_k : 0, set.top_p, in_window && (sizeof(T) == 2 || !by_p) ? Level{0u, -1} : Level{0u, kBf16Shift}, b);
+    if (is) {
       zt = value_of(b.key);
       ties = b.m;
       kept = static_cast<int64_t>(b.above) + b.m;
@@ -645,20 +858,33 @@ __global__ void __launch_bounds__(WARPS * 32, 1024 / (WARPS * 32)) sample_kernel
   }
 
   // ---- the kept weights of every tile
-  const bool count = p.n_kept && kept < 0, pass = filtered || count;
-  if (pass) {
+  const bool count = p.n_kept && kept < 0;
+  if (filtered) {
     float sum = 0.f;
     uint32_t equal = 0, above = 0;
     auto over = [&](const auto& keep) {
-      for (int t = t0 + warp; t < t1; t += WARPS) {
-        row.tile(t, lane, q);
-        uint32_t eq = 0;
-        const float s = warp_sum(keep.tile(q, eq, above, count));
-        eq = __reduce_add_sync(0xffffffffu, eq) / 16;
-        if (lane == 0 && filtered) {
-          tiles[t - t0].kept.sum = s;
-          tiles[t - t0].kept.equal = eq;
+      // this warp's tiles that have an entry to keep; the ones read last first: they are the likeliest to be in L2 still
+      const int first = t0 + warp;
+      auto before = [&](int t) {
+        for (; t >= first; t -= WARPS) {
+          if (tile_max[t - t0] >= zt) break;
+          if (lane == 0) tiles[t - t0].kept = {0.f, 0u};
         }
+        return t;
+      };
+      int t = first < t1 ? before(first + (t1 - 1 - first) / WARPS * WARPS) : first - WARPS;
+      if (t >= first) row.tile(t, lane, q);
+      while (t >= first) {
+        uint4 now[kTileBlocks];
+#pragma unroll
+        for (int i = 0; i < kTileBlocks; ++i) now[i] = q[i];
+        const int here = t;
+        t = before(t - WARPS);
+        if (t >= first) row.tile(t, lane, q);
+        uint32_t eq = 0;
+        const float s = warp_sum(keep.tile(now, eq, above, count));
+        eq = __reduce_add_sync(0xffffffffu, eq) / 16;
+        if (lane == 0) tiles[here - t0].kept = {s, eq};
         sum += s;
         equal += eq;
       }
@@ -671,17 +897,17 @@ __global__ void __launch_bounds__(WARPS * 32, 1024 / (WARPS * 32)) sample_kernel
       sh.warp_equal[warp] = equal;
       sh.warp_above[warp] = above;
     }
-  } else if (lane == 0) {
-    sh.warp_sum[warp] = f.s == 0.f ? 0.f : f.s * power(f.m, all.m, c);
-    sh.warp_equal[warp] = sh.warp_above[warp] = 0;
+  } else {
+    live = __reduce_add_sync(0xffffffffu, live) / 16;
+    if (lane == 0) {
+      sh.warp_sum[warp] = f.s == 0.f ? 0.f : f.s * power(f.m, all.m, c);
+      sh.warp_equal[warp] = 0;
+      sh.warp_above[warp] = live;
+    }
   }
   __syncthreads();
   if (warp == 0) {
     float sum = lane < WARPS ? sh.warp_sum[lane] : 0.f;
-    if (pass && !filtered) {  // the entries were counted only
-      const Fold mine = lane < WARPS ? sh.fold[rank * WARPS + lane] : Fold{minus_inf(), 0.f};
-      sum = mine.s == 0.f ? 0.f : mine.s * power(mine.m, all.m, c);
-    }
     sum = warp_sum(sum);
     const uint32_t equal = __reduce_add_sync(0xffffffffu, lane < WARPS ? sh.warp_equal[lane] : 0u);
     const uint32_t above = __reduce_add_sync(0xffffffffu, lane < WARPS ? sh.warp_above[lane] : 0u);
@@ -823,25 +1049,25 @@ rl_status launch(Args& a, int C, int64_t all_tiles, cudaStream_t s) {
   cfg.numAttrs = C > 1 ? 1 : 0;
   cfg.blockDim = dim3(WARPS * 32);
   cfg.gridDim = dim3(static_cast<unsigned>(a.rows * C));
-  cfg.dynamicSmemBytes = static_cast<size_t>(a.tiles) * sizeof(Tile);
+  cfg.dynamicSmemBytes = static_cast<size_t>(a.tiles) * (sizeof(Tile) + sizeof(float));
   cfg.stream = s;
   const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, a);
   return e == cudaSuccess ? RL_OK : cuda_error(e, "sample_kernel launch");
 }
 
-constexpr int64_t kMostTiles = 2064;  // of a CTA: their table, 16 KB, and the others fit in what any kernel may take
+constexpr int64_t kMostTiles = 2064;  // of a CTA: their tables, 24 KB, and the others fit in what any kernel may take
 
 template <typename T>
 rl_status run(Args& a, cudaStream_t s) {
   const int64_t nb = (a.V + 7) * sizeof(T) / 16 + 1, tiles = (nb + kTileBlocks32 - 1) / kTileBlocks32;
   // many rows: small CTAs, which wait less for one another, and do what a row takes beside its entries with fewer warps
   if (tiles <= 8 && a.rows > kSMs) return launch<T, 4, false>(a, 1, tiles, s);
-  if (a.rows > 2 * kSMs && tiles <= kMostTiles) return launch<T, 8, false>(a, 1, tiles, s);
-  // as many CTAs a row as fill the SMs twice over while each of their warps has a tile
+  // else as many CTAs a row as fill the SMs twice over while each of their warps has a tile
   int C = 1;
-  while (C < 8 && ((a.rows * C * 2 <= 2 * kSMs && tiles >= 2 * C * 16) || tiles > kMostTiles * C)) C *= 2;
+  while (C < 8 && ((a.rows * C * 2 <= 2 * kSMs && tiles >= 2 * C * 8) || tiles > kMostTiles * C)) C *= 2;
   if (tiles > kMostTiles * C) return set_error(RL_ERR_UNSUPPORTED, "rl_sample_tokens: V is too large");
-  return C > 1 ? launch<T, 16, true>(a, C, tiles, s) : launch<T, 16, false>(a, 1, tiles, s);
+  if (C > 1) return launch<T, 16, true>(a, C, tiles, s);
+  return a.rows <= 2 * kSMs ? launch<T, 16, false>(a, 1, tiles, s) : launch<T, 8, false>(a, 1, tiles, s);
 }
 
 }  // namespace sample

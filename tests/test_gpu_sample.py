@@ -68,12 +68,12 @@ def logp_tolerance(z, T, V):
     return (x + (4 + V / 2048 + 64) * U) * 0.7 + 4 * U
 
 
-def check(R, law, n, V, dtype, seed, pad=0):
+def check(R, law, n, V, dtype, seed, pad=0, choices=SETTINGS):
     rng = np.random.default_rng(seed)
     z = SC.rows(law, n, V, dtype, rng)
     settings, us = [], []
     for r in range(n):
-        T, k, p, m = SETTINGS[(r + seed) % len(SETTINGS)]
+        T, k, p, m = choices[(r + seed) % len(choices)]
         T = float(np.float32(T))
         p, m, u = SC.away_from_edges(z[r], T, k, p, m, rng.random())
         settings.append((T, k, p, m))
@@ -115,6 +115,14 @@ def test_lengths_and_strides(R, V, dtype):
     for pad in (0, 5, 64):
         for law in ("likely", "normal"):
             assert check(R, law, 13, V, dtype, seed=pad + 1, pad=pad) >= 6
+
+
+@pytest.mark.parametrize("law", ["likely", "normal", "ties", "close", "far", "negative"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_numbers_kept_around_what_a_list_holds(R, law, dtype):
+    choices = [(1.0, k, p, m) for k in (1, 2, 33, 1000, 1023, 1024, 1025, 3000) for p, m in ((1.0, 0.0), (0.9, 0.0), (0.97, 0.01))]
+    seen = sum(check(R, law, len(choices), V, dtype, seed=0, choices=choices) for V in (1500, 30000))
+    assert seen >= 20
 
 
 @pytest.mark.parametrize("V,dtype", [(800000, "f32"), (1600001, "bf16")])
