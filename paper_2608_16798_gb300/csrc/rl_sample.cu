@@ -18,6 +18,7 @@
 //      that holds the token is found by a scan, and the token in it by another.
 // HBM is read once: the rows at work at a time fit in L2, where the later passes find them.
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <string>
 
@@ -183,16 +184,18 @@ template <int WARPS>
 struct Shared {
   Fold fold[WARPS * kMostCluster];    // every warp's, the same in every CTA of the cluster
   alignas(16) uint32_t count[kBins];  // this CTA's entries
+  static constexpr int kList = WARPS == 4 ? 1024 : 4096;
   union {
     struct {
       alignas(16) uint32_t low[kBins];  // and their mass
       alignas(16) uint32_t high[kBins];
     };
-    unsigned long long list[kBins];  // the entries that may be kept, where they are few: by size, then by index
+    unsigned long long list[kList];  // the entries that may be kept, where they are few: by size, then by index
   };
   alignas(8) uint32_t n_list;
   uint32_t n_equal;
   unsigned long long total;
+  int32_t first, last;  // of the list's entries by index: the one at which the sum passes its goal, and the last of any weight
   uint32_t others[32];
   uint32_t warp_count[WARPS];
   unsigned long long warp_mass[WARPS];
@@ -359,9 +362,35 @@ struct Row {
     }
   }
 
-  // The same for an fp32 row whose window says that few entries can be kept: they are gathered in the first CTA and sorted,
-  // and the border is read off the running sum. false: they are not few, or the border is not in the window.
-  __device__ __forceinline__ bool search_list(int32_t top_k, float top_p, const float* tile_max, Border& found) {
+  // Sorts the first `size` (a power of two) of the list, by all threads.
+  __device__ __forceinline__ void sort_list(int size) {
+    for (int k = 2; k <= size; k *= 2)
+      for (int j = k / 2; j > 0; j /= 2) {
+        for (int i = threadIdx.x; i < size / 2; i += kThreads) {
+          const int x = 2 * i - (i & (j - 1)), y = x + j;  // the i-th pair at distance j
+          const unsigned long long a = sh.list[x], b = sh.list[y];
+          if ((a > b) == ((x & k) == 0)) {
+            sh.list[x] = b;
+            sh.list[y] = a;
+          }
+        }
+        __syncthreads();
+      }
+  }
+  // Fills the list up to a power of two behind its first `have`.
+  __device__ __forceinline__ int fill_list(int have) {
+    int size = 32;
+    while (size < have) size *= 2;
+    for (int i = have + threadIdx.x; i < size; i += kThreads) sh.list[i] = ~0ull;
+    __syncthreads();
+    return size;
+  }
+
+  // For an fp32 row whose window says that few entries can be kept: they are gathered in the first CTA and sorted by size,
+  // the border is read off the running mass, what is kept is sorted by index, and the token is found by a scan. false: they are
+  // not few, or the border is not in the window. True: the row is done. `least`: min_p, as an exponent.
+  __device__ __forceinline__ bool finish_by_list(int32_t top_k, float top_p, float least, const Args& p, int64_t out, float u,
+                                                 const T* z_row, const float* tile_max) {
     const int warp = threadIdx.x / 32, lane = threadIdx.x & 31, rank = CLUSTER ? static_cast<int>(cluster_ctarank()) : 0;
     const Level level{0u, -1};
     add_up(level);
@@ -369,6 +398,8 @@ struct Row {
       sh.bin = -1;
       sh.n_list = 0;
       sh.n_equal = 0;
+      sh.first = Shared<WARPS>::kList;
+      sh.last = 0;
     }
     __syncthreads();
     {
@@ -389,7 +420,8 @@ struct Row {
     __syncthreads();
     const int bin = sh.bin;
     const uint32_t most = sh.found.above;
-    if (bin < 0 || most > kBins) return false;  // the same in every CTA
+    constexpr int kList = Shared<WARPS>::kList, kEach = kList / kThreads;
+    if (bin < 0 || most > kList) return false;  // the same in every CTA
     const float edge = value_of(key_at(level, bin) & 0xffff0000u);
     for (int t = t0 + warp; t < t1; t += WARPS) {
       if (!(tile_max[t - t0] >= edge)) continue;
@@ -407,35 +439,24 @@ struct Row {
       }
     }
     sync_all<CLUSTER>();
-    if (rank == 0) {
-      int have = static_cast<int>(sh.n_list);
-      for (int r = 1; r < C; ++r) {  // (C == 1 without a cluster)
+    int have = static_cast<int>(sh.n_list);
+    if (rank == 0)
+      for (int r = 1; r < C; ++r) {
         const int more = static_cast<int>(static_cast<uint32_t>(ld_cluster_u64(map_to_rank(smem_addr(&sh.n_list), r))));
         for (int i = threadIdx.x; i < more; i += kThreads) sh.list[have + i] = ld_cluster_u64(map_to_rank(smem_addr(&sh.list[i]), r));
         have += more;
       }
-      int size = 32;
-      while (size < have) size *= 2;
-      for (int i = have + threadIdx.x; i < size; i += kThreads) sh.list[i] = ~0ull;
-      __syncthreads();
-      for (int k = 2; k <= size; k *= 2)
-        for (int j = k / 2; j > 0; j /= 2) {
-          for (int i = threadIdx.x; i < size / 2; i += kThreads) {
-            const int x = 2 * i - (i & (j - 1)), y = x + j;  // the i-th pair at distance j
-            const unsigned long long a = sh.list[x], b = sh.list[y];
-            if ((a > b) == ((x & k) == 0)) {
-              sh.list[x] = b;
-              sh.list[y] = a;
-            }
-          }
-          __syncthreads();
-        }
-      // the running mass
-      unsigned long long v[kOwn], mine = 0;
+    if (CLUSTER) cluster_sync_all();
+    if (rank != 0) return true;
+    sort_list(fill_list(have));
+    const int own = threadIdx.x * kEach;
+    // the number kept: top_k's, then top_p's of the running mass, then min_p's
+    if (threadIdx.x == 0) sh.bin = top_k ? top_k - 1 : have - 1;  // the last one
+    if (masses) {
+      unsigned long long v[kEach], mine = 0;
 #pragma unroll
-      for (int i = 0; i < kOwn; ++i) {
-        const int at = threadIdx.x * kOwn + i;
-        v[i] = masses && at < have ? mass_of(weight(value_of(~static_cast<uint32_t>(sh.list[at] >> 32)))) : 0;
+      for (int i = 0; i < kEach; ++i) {
+        v[i] = own + i < have ? mass_of(weight(value_of(~static_cast<uint32_t>(sh.list[own + i] >> 32)))) : 0;
         mine += v[i];
       }
       unsigned long long run = mine;
@@ -445,48 +466,80 @@ struct Row {
         if (lane >= o) run += a;
       }
       if (lane == 31) sh.warp_mass[warp] = run;
-      if (threadIdx.x == 0) sh.bin = top_k ? top_k - 1 : have - 1;  // the last kept
       __syncthreads();
       run -= mine;
-      for (int u = 0; u < warp; ++u) run += sh.warp_mass[u];
-      if (masses) {
-        unsigned long long r = run;
+      for (int w = 0; w < warp; ++w) run += sh.warp_mass[w];
+      unsigned long long upto = run;
 #pragma unroll
-        for (int i = 0; i < kOwn; ++i) {
-          r += v[i];
-          if (top_k && static_cast<int>(threadIdx.x) * kOwn + i == top_k - 1) sh.total = r;
-        }
-        __syncthreads();
-        const double total = top_k ? static_cast<double>(sh.total) : static_cast<double>(all.s) * kMassUnit;
-        const unsigned long long goal = max(1ull, static_cast<unsigned long long>(ceil(static_cast<double>(top_p) * total)));
-#pragma unroll
-        for (int i = 0; i < kOwn; ++i) {
-          if (run < goal && run + v[i] >= goal && static_cast<int>(threadIdx.x) * kOwn + i < have)
-            atomicMin(&sh.bin, static_cast<int>(threadIdx.x) * kOwn + i);
-          run += v[i];
-        }
-        __syncthreads();
+      for (int i = 0; i < kEach; ++i) {
+        upto += v[i];
+        if (top_k && own + i == top_k - 1) sh.total = upto;
       }
-      const int last = sh.bin;
-      const uint32_t key = ~static_cast<uint32_t>(sh.list[last] >> 32);
-      uint32_t same = 0;
-      for (int i = threadIdx.x; i <= last; i += kThreads) same += ~static_cast<uint32_t>(sh.list[i] >> 32) == key;
-      if (same) atomicAdd(&sh.n_equal, same);
       __syncthreads();
-      if (threadIdx.x == 0) {
-        sh.found.key = key;
-        sh.found.m = sh.n_equal;
-        sh.found.above = last + 1 - sh.n_equal;
+      const double total = top_k ? static_cast<double>(sh.total) : static_cast<double>(all.s) * kMassUnit;
+      const unsigned long long goal = max(1ull, static_cast<unsigned long long>(ceil(static_cast<double>(top_p) * total)));
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        if (run < goal && run + v[i] >= goal && own + i < have) atomicMin(&sh.bin, own + i);
+        run += v[i];
       }
     }
-    sync_all<CLUSTER>();
-    if (CLUSTER) {
-      const unsigned long long two = ld_cluster_u64(map_to_rank(smem_addr(&sh.found.key), 0));
-      found.key = static_cast<uint32_t>(two);
-      found.m = static_cast<uint32_t>(two >> 32);
-      found.above = static_cast<uint32_t>(ld_cluster_u64(map_to_rank(smem_addr(&sh.found.above), 0)));
-    } else {
-      found = sh.found;
+    __syncthreads();
+    int kept = sh.bin + 1;
+    if (least > minus_inf()) {
+      uint32_t over = 0;
+      for (int i = threadIdx.x; i < kept; i += kThreads)
+        over += exponent(value_of(~static_cast<uint32_t>(sh.list[i] >> 32)), all.m, c) >= least;
+      if (over) atomicAdd(&sh.n_equal, over);
+      __syncthreads();
+      kept = max(1, static_cast<int>(sh.n_equal));
+    }
+    // the kept ones by index, with their weights
+    for (int i = threadIdx.x; i < kept; i += kThreads) {
+      const unsigned long long e = sh.list[i];
+      sh.list[i] = e << 32 | __float_as_uint(weight(value_of(~static_cast<uint32_t>(e >> 32))));
+    }
+    sort_list(fill_list(kept));
+    float v[kEach], mine = 0.f;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      v[i] = own + i < kept ? __uint_as_float(static_cast<uint32_t>(sh.list[own + i])) : 0.f;
+      mine += v[i];
+    }
+    float run = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const float a = __shfl_up_sync(0xffffffffu, run, o);
+      if (lane >= o) run += a;
+    }
+    if (lane == 31) sh.warp_sum[warp] = run;
+    __syncthreads();
+    float before = 0.f, total = 0.f;
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) {
+      const float a = sh.warp_sum[w];
+      before += w < warp ? a : 0.f;
+      total += a;
+    }
+    run += before - mine;
+    const float goal = u * total;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      run += v[i];
+      if (v[i] > 0.f) {
+        atomicMax(&sh.last, own + i);  // where rounding leaves the sum short of its goal
+        if (run > goal) atomicMin(&sh.first, own + i);
+      }
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      const int at = sh.first < kList ? sh.first : sh.last;
+      const int token = min(max(static_cast<int>(sh.list[at] >> 32) - row.lo, 0), p.V - 1);
+      const float zx = Elem<T>::one(z_row[token]);
+      p.ids[out] = token;
+      p.logp[out] = logp_of(zx, all, c);
+      if (p.among) p.among[out] = (exponent(zx, all.m, c) - log2f(total)) * kLn2;
+      if (p.n_kept) p.n_kept[out] = kept;
     }
     return true;
   }
@@ -842,8 +895,11 @@ __global__ void __launch_bounds__(WARPS * 32, 1024 / (WARPS * 32)) sample_kernel
     Row<T, WARPS, CLUSTER> s{sh, row, t0, t1, all, c, top, C, by_p};
     Border b;
     const bool in_window = top >= (0x80000000u | kWindowLow << 16) && top <= (0x8000ffffu | kWindowTop << 16);
-    bool is = sizeof(T) == 4 && in_window && s.search_list(by_k ? set.top_k : 0, set.top_p, tile_max, b);
-    if (!is) is = s.search(by_k ? set.top_k : 0, set.top_p, in_window && (sizeof(T) == 2 || !by_p) ? Level{0u, -1} : Level{0u, kBf16Shift}, b);
+    if (sizeof(T) == 4 && in_window) {
+      const float least = by_m ? exponent(all.m, all.m, c) + log2f(set.min_p) : minus_inf();
+      if (s.finish_by_list(by_k ? set.top_k : 0, set.top_p, least, p, r, set.u, z, tile_max)) return;
+    }
+    const bool is = s.search(by_k ? set.top_k : 0, set.top_p, in_window && (sizeof(T) == 2 || !by_p) ? Level{0u, -1} : Level{0u, kBf16Shift}, b);
     if (is) {
       zt = value_of(b.key);
       ties = b.m;
@@ -1034,11 +1090,26 @@ __global__ void __launch_bounds__(WARPS * 32, 1024 / (WARPS * 32)) sample_kernel
 // ---------------------------------------------------------------- host
 
 constexpr int kSMs = 152;
+constexpr int64_t kMostTiles = 2064;  // of a CTA: their tables take 24 KB beside the others
+static_assert(sizeof(Shared<16>) + kMostTiles * 12 <= 100 * 1024 && sizeof(Shared<8>) <= 48 * 1024 && sizeof(Shared<16>) <= 48 * 1024,
+              "two CTAs on an SM");
 
 template <typename T, int WARPS, bool CLUSTER>
 rl_status launch(Args& a, int C, int64_t all_tiles, cudaStream_t s) {
   a.tiles = static_cast<int32_t>((all_tiles + C - 1) / C);
   auto kern = sample_kernel<T, WARPS, CLUSTER>;
+  // once per device
+  static std::atomic<uint64_t> ready{0};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return cuda_error(e, "cudaGetDevice");
+  const uint64_t bit = dev < 64 ? uint64_t(1) << dev : 0;
+  if (!(ready.load() & bit)) {
+    e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             static_cast<int>(kMostTiles * (sizeof(Tile) + sizeof(float))));
+    if (e != cudaSuccess) return cuda_error(e, "cudaFuncSetAttribute(sample_kernel)");
+    ready |= bit;
+  }
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -1051,11 +1122,10 @@ rl_status launch(Args& a, int C, int64_t all_tiles, cudaStream_t s) {
   cfg.gridDim = dim3(static_cast<unsigned>(a.rows * C));
   cfg.dynamicSmemBytes = static_cast<size_t>(a.tiles) * (sizeof(Tile) + sizeof(float));
   cfg.stream = s;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, a);
+  e = cudaLaunchKernelEx(&cfg, kern, a);
   return e == cudaSuccess ? RL_OK : cuda_error(e, "sample_kernel launch");
 }
 
-constexpr int64_t kMostTiles = 2064;  // of a CTA: their tables, 24 KB, and the others fit in what any kernel may take
 
 template <typename T>
 rl_status run(Args& a, cudaStream_t s) {
