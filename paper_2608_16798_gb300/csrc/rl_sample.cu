@@ -184,7 +184,7 @@ template <int WARPS>
 struct Shared {
   Fold fold[WARPS * kMostCluster];    // every warp's, the same in every CTA of the cluster
   alignas(16) uint32_t count[kBins];  // this CTA's entries
-  static constexpr int kList = WARPS == 4 ? 1024 : 4096;
+  static constexpr int kList = WARPS == 4 ? 256 : 4096;  // (of short rows, whose passes are short, what is sorted soon)
   union {
     struct {
       alignas(16) uint32_t low[kBins];  // and their mass
@@ -676,17 +676,17 @@ struct Keep {
       return fmaxf(fmaxf(__uint_as_float(q.x), __uint_as_float(q.y)), fmaxf(__uint_as_float(q.z), __uint_as_float(q.w))) >= zt;
     }
   }
-  // 16 for each of a block's kept entries.
-  __device__ __forceinline__ uint32_t number(const uint4& q) const {
+  // Adds the number of a block's kept entries: pairs of counts of 16 bits.
+  __device__ __forceinline__ void number(const uint4& q, uint32_t& n) const {
     if constexpr (sizeof(T) == 2) {
       const uint32_t t = __float_as_uint(zt) >> 16, t2 = t | t << 16;
-      return __popc(above2(q.x, t2)) + __popc(above2(q.y, t2)) + __popc(above2(q.z, t2)) + __popc(above2(q.w, t2));
+      n += (above2(q.x, t2) & 0x00010001u) + (above2(q.y, t2) & 0x00010001u) + (above2(q.z, t2) & 0x00010001u) + (above2(q.w, t2) & 0x00010001u);
     } else {
-      return ((__uint_as_float(q.x) > zt) + (__uint_as_float(q.y) > zt) + (__uint_as_float(q.z) > zt) + (__uint_as_float(q.w) > zt)) * 16;
+      n += (__uint_as_float(q.x) > zt) + (__uint_as_float(q.y) > zt) + (__uint_as_float(q.z) > zt) + (__uint_as_float(q.w) > zt);
     }
   }
-  // A block's kept entries, the others minus infinity. Adds those equal to zt (not GE) to `equal`, and
-  // with `count` the kept ones to `kept`.
+  // A block's kept entries, the others minus infinity. Adds the number of those equal to zt (not GE) to `equal`, and
+  // with `count` that of the kept ones to `kept`, both pairs of counts of 16 bits.
   __device__ __forceinline__ void block(const uint4& q, float (&z)[N], uint32_t& equal, uint32_t& kept, bool count) const {
     if constexpr (sizeof(T) == 2) {
       const uint32_t t = __float_as_uint(zt) >> 16, t2 = t | t << 16;
@@ -694,10 +694,11 @@ struct Keep {
       uint32_t m[4], r[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        m[i] = GE ? least2(v[i], t2) : above2(v[i], t2);
+        const uint32_t ge = least2(v[i], t2);
+        m[i] = GE ? ge : above2(v[i], t2);
         r[i] = (v[i] & m[i]) | (0xff80ff80u & ~m[i]);
-        if (!GE) equal += __popc(equal2(v[i], t2));
-        if (count) kept += __popc(m[i]);
+        if (!GE) equal += (ge ^ m[i]) & 0x00010001u;
+        if (count) kept += m[i] & 0x00010001u;
       }
       Elem<T>::unpack(make_uint4(r[0], r[1], r[2], r[3]), z);
     } else {
@@ -705,18 +706,27 @@ struct Keep {
 #pragma unroll
       for (int e = 0; e < N; ++e) {
         const bool in = GE ? z[e] >= zt : z[e] > zt;
-        if (!GE) equal += z[e] == zt ? 16 : 0;
-        if (count) kept += in ? 16 : 0;
+        if (!GE) equal += z[e] == zt;
+        if (count) kept += in;
         z[e] = in ? z[e] : minus_inf();
       }
     }
   }
-  // The kept weights of a lane's blocks of a tile. (equal and kept count 16 an entry.)
+  // The kept weights of a lane's blocks of a tile.
   __device__ __forceinline__ float tile(const uint4 (&q)[kTileBlocks], uint32_t& equal, uint32_t& kept, bool count) const {
     const float rc = -__fmul_rn(ref, c);
-    const bool apart = large(rc);  // of the row
     const float2 cc = make_float2(c, c), off = make_float2(rc, rc);
     float2 s = make_float2(0.f, 0.f);
+    if (large(rc)) {  // of the row
+#pragma unroll 1
+      for (int i = 0; i < kTileBlocks; ++i) {
+        float z[N];
+        block(i < 2 ? (i == 0 ? q[0] : q[1]) : (i == 2 ? q[2] : q[3]), z, equal, kept, count);
+#pragma unroll
+        for (int e = 0; e < N; ++e) s.x += ex2((z[e] - ref) * c);
+      }
+      return s.x;
+    }
 #pragma unroll
     for (int i = 0; i < kTileBlocks; ++i) {
       if (!__any_sync(0xffffffffu, reaches(q[i]))) continue;  // most blocks of most rows
@@ -724,14 +734,15 @@ struct Keep {
       block(q[i], z, equal, kept, count);
 #pragma unroll
       for (int e = 0; e < N; e += 2) {
-        float2 x = fma2(make_float2(z[e], z[e + 1]), cc, off);
-        if (apart) x = make_float2((z[e] - ref) * c, (z[e + 1] - ref) * c);
-        s = add2(s, make_float2(ex2(x.x), ex2(x.y)));
+        const float2 x = __ffma2_rn(make_float2(z[e], z[e + 1]), cc, off);
+        s = __fadd2_rn(s, make_float2(ex2(x.x), ex2(x.y)));
       }
     }
     return s.x + s.y;
   }
 };
+// The sum of a warp's pairs of counts of 16 bits.
+__device__ __forceinline__ uint32_t of_pairs(uint32_t n) { return __reduce_add_sync(0xffffffffu, (n & 0xffffu) + (n >> 16)); }
 
 // One more of the pattern's bin of the window; a lane's others are counted in a word of its own, since a condition on the
 // addition costs more than the addition. (`one` is 1, where the compiler does not see it: it adds a known 1 by a longer sequence.)
@@ -771,9 +782,9 @@ __device__ __forceinline__ float fold_tile(Running& r, const uint4 (&w)[kTileBlo
     Elem<T>::unpack(w[i], z);
 #pragma unroll
     for (int e = 0; e < N; e += 4) {
-      const float2 a = fma2(make_float2(z[e], z[e + 1]), cc, off), b = fma2(make_float2(z[e + 2], z[e + 3]), cc, off);
-      s0 = add2(s0, make_float2(ex2(a.x), ex2(a.y)));
-      s1 = add2(s1, make_float2(ex2(b.x), ex2(b.y)));
+      const float2 a = __ffma2_rn(make_float2(z[e], z[e + 1]), cc, off), b = __ffma2_rn(make_float2(z[e + 2], z[e + 3]), cc, off);
+      s0 = __fadd2_rn(s0, make_float2(ex2(a.x), ex2(a.y)));
+      s1 = __fadd2_rn(s1, make_float2(ex2(b.x), ex2(b.y)));
     }
   }
   r.s = add2(r.s, add2(s0, s1));
@@ -817,7 +828,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1024 / (WARPS * 32)) sample_kernel
   Running run{minus_inf(), {0.f, 0.f}, 0};
   Fold f{minus_inf(), 0.f};
   const bool count_all = !filtered && p.n_kept;
-  uint32_t live = 0;  // entries above minus infinity, 16 each
+  uint32_t live = 0;  // entries above minus infinity
   for (int t = t0 + warp; t < t1; t += WARPS) {
     uint4 now[kTileBlocks];
 #pragma unroll
@@ -838,7 +849,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1024 / (WARPS * 32)) sample_kernel
     } else if (!filtered) {
       if (count_all) {
 #pragma unroll
-        for (int i = 0; i < kTileBlocks; ++i) live += Keep<T, false>{minus_inf(), 0.f, 1.f}.number(now[i]);
+        for (int i = 0; i < kTileBlocks; ++i) Keep<T, false>{minus_inf(), 0.f, 1.f}.number(now[i], live);
       }
       const Fold of = of_warp(run, c);
       if (lane == 0) tiles[t - t0].fold = of;
@@ -939,7 +950,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1024 / (WARPS * 32)) sample_kernel
         if (t >= first) row.tile(t, lane, q);
         uint32_t eq = 0;
         const float s = warp_sum(keep.tile(now, eq, above, count));
-        eq = __reduce_add_sync(0xffffffffu, eq) / 16;
+        eq = of_pairs(eq);
         if (lane == 0) tiles[here - t0].kept = {s, eq};
         sum += s;
         equal += eq;
@@ -947,14 +958,14 @@ __global__ void __launch_bounds__(WARPS * 32, 1024 / (WARPS * 32)) sample_kernel
     };
     if (ge) over(Keep<T, true>{zt, all.m, c});
     else over(Keep<T, false>{zt, all.m, c});
-    above = __reduce_add_sync(0xffffffffu, above) / 16;
+    above = of_pairs(above);
     if (lane == 0) {
       sh.warp_sum[warp] = sum;
       sh.warp_equal[warp] = equal;
       sh.warp_above[warp] = above;
     }
   } else {
-    live = __reduce_add_sync(0xffffffffu, live) / 16;
+    live = of_pairs(live);
     if (lane == 0) {
       sh.warp_sum[warp] = f.s == 0.f ? 0.f : f.s * power(f.m, all.m, c);
       sh.warp_equal[warp] = 0;
