@@ -183,7 +183,7 @@ struct Part {
 template <int WARPS>
 struct Shared {
   Fold fold[WARPS * kMostCluster];    // every warp's, the same in every CTA of the cluster
-  alignas(16) uint32_t count[kBins];  // this CTA's entries
+  alignas(16) uint32_t count[kBins + 32];  // this CTA's entries (and behind the bins those outside the window)
   static constexpr int kList = WARPS == 4 ? 256 : 4096;  // (of short rows, whose passes are short, what is sorted soon)
   union {
     struct {
@@ -196,7 +196,6 @@ struct Shared {
   uint32_t n_equal;
   unsigned long long total;
   int32_t first, last;  // of the list's entries by index: the one at which the sum passes its goal, and the last of any weight
-  uint32_t others[32];
   uint32_t warp_count[WARPS];
   unsigned long long warp_mass[WARPS];
   Border found;
@@ -744,12 +743,17 @@ struct Keep {
 // The sum of a warp's pairs of counts of 16 bits.
 __device__ __forceinline__ uint32_t of_pairs(uint32_t n) { return __reduce_add_sync(0xffffffffu, (n & 0xffffu) + (n >> 16)); }
 
-// One more of the pattern's bin of the window; a lane's others are counted in a word of its own, since a condition on the
-// addition costs more than the addition. (`one` is 1, where the compiler does not see it: it adds a known 1 by a longer sequence.)
-__device__ __forceinline__ void count_pattern(uint32_t bins, uint32_t other, uint32_t pattern, uint32_t one) {
-  const uint32_t off = pattern * 4u - kWindowLow * 4u;
-  const uint32_t at = off < kBins * 4u ? bins + off : other;
-  asm volatile("red.shared.add.u32 [%0], %1;" :: "r"(at), "r"(one) : "memory");
+// One more of the bins of the window of a pair of patterns, both halves at a time: the smaller of a pattern's distance from
+// the window's lowest, which wraps for lower ones, and of a word behind the bins, a lane's own (a condition on the
+// addition costs more than the addition).
+__device__ __forceinline__ void count_patterns(uint32_t bins, uint32_t pair, uint32_t behind, uint32_t one) {
+  const uint32_t i = __viaddmin_u16x2(pair, ((0x10000u - kWindowLow) << 16) | (0x10000u - kWindowLow), behind);
+  asm volatile("red.shared.add.u32 [%0], %1;" :: "r"(bins + (i & 0xffffu) * 4u), "r"(one) : "memory");
+  asm volatile("red.shared.add.u32 [%0], %1;" :: "r"(bins + (i >> 16) * 4u), "r"(one) : "memory");
+}
+__device__ __forceinline__ void count_pattern(uint32_t bins, uint32_t pattern, uint32_t behind, uint32_t one) {
+  const uint32_t i = min(pattern - kWindowLow, behind & 0xffffu);
+  asm volatile("red.shared.add.u32 [%0], %1;" :: "r"(bins + i * 4u), "r"(one) : "memory");
 }
 
 // As add_tile, with the exponents' form decided once for the tile; the largest of the lane's entries.
@@ -822,7 +826,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1024 / (WARPS * 32)) sample_kernel
   const bool window = by_k || by_p;
 
   // ---- the row's largest entry and its normaliser
-  const uint32_t bins = smem_addr(sh.count), other = smem_addr(&sh.others[lane]);
+  const uint32_t bins = smem_addr(sh.count), behind = (kBins + lane) * 0x10001u;
   uint32_t one;
   asm volatile("mov.u32 %0, 1;" : "=r"(one));
   Running run{minus_inf(), {0.f, 0.f}, 0};
@@ -842,8 +846,8 @@ __global__ void __launch_bounds__(WARPS * 32, 1024 / (WARPS * 32)) sample_kernel
         const uint32_t v[4] = {now[i].x, now[i].y, now[i].z, now[i].w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          count_pattern(bins, other, v[e] >> 16, one);
-          if (sizeof(T) == 2) count_pattern(bins, other, v[e] & 0xffffu, one);
+          if (sizeof(T) == 2) count_patterns(bins, v[e], behind, one);
+          else count_pattern(bins, v[e] >> 16, behind, one);
         }
       }
     } else if (!filtered) {
