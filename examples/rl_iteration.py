@@ -1,7 +1,7 @@
 """Iterations of RL on a toy policy, with the library on both sides of the loss.
 
 The policy sees the last token only: hidden = tanh(embedding[token] W1^T), logits = hidden W^T. A smaller
-model (the policy's own matrices as they were at the start) drafts ``DRAFTED`` tokens at a time,
+model (the policy's own matrices as they were at the start) drafts ``DRAFTED`` tokens at a time (``rl_sample_tokens``),
 ``rl_verify_drafts`` accepts or replaces them by the policy's probabilities, and the log-probabilities it
 emits are the rollout's. The reward is the share of tokens from the lower half of the vocabulary. Then
 group advantages, the loss through the fused head with the truncated importance weight against the rollout's
@@ -24,8 +24,12 @@ import paper_2608_16798_gb300.rl_loss as R  # noqa: E402
 VOCAB, HIDDEN, PROMPTS, GROUP, TOKENS, DRAFTED = 1000, 128, 4, 16, 24, 3
 
 
-def hidden_of(tokens, embedding, w1):
-    return torch.tanh(embedding[tokens.long()].float() @ w1.float().T).bfloat16()
+def embedded(tokens, embedding, ws):
+    return R.rl_embedding_fwd(tokens, embedding, ws, out_dtype=torch.float32)
+
+
+def hidden_of(tokens, embedding, w1, ws):
+    return torch.tanh(embedded(tokens, embedding, ws) @ w1.float().T).bfloat16()
 
 
 def rollout(policy, drafter, embedding, start, g):
@@ -35,10 +39,8 @@ def rollout(policy, drafter, embedding, start, g):
     tokens = torch.full((n, TOKENS + DRAFTED + 1), -1, dtype=torch.int32, device=dev)
     logp = torch.zeros(n, TOKENS + DRAFTED + 1, device=dev)
     at, last, accepted, drafted = torch.zeros(n, dtype=torch.int64, device=dev), start.clone(), 0, 0
-    one, params = R.make_verify_params(1.0), R.make_verify_params(1.0)
-    no_offsets = torch.zeros(n + 1, dtype=torch.int32, device=dev)
+    draw, params = R.make_sample_params(1.0), R.make_verify_params(1.0)
     offsets = torch.arange(0, n * DRAFTED + 1, DRAFTED, dtype=torch.int32, device=dev)
-    none_i, none_f = torch.empty(0, dtype=torch.int32, device=dev), torch.empty(0, device=dev)
     ws = R.new_workspace(n * (DRAFTED + 1), VOCAB, device=dev)
     while int(at.min()) < TOKENS:
         # the drafter's tokens, one draw after the other
@@ -46,13 +48,12 @@ def rollout(policy, drafter, embedding, start, g):
         draft = torch.empty(n, DRAFTED, VOCAB, dtype=torch.bfloat16, device=dev)
         prev = last
         for j in range(DRAFTED):
-            draft[:, j] = hidden_of(prev, embedding, drafter[0]) @ drafter[1].T
-            z = draft[:, j].contiguous()
-            prev, _, _ = R.rl_verify_drafts(z, none_i, no_offsets, none_f, torch.rand(n, generator=g, device=dev), 0, one, ws)
-            ids[:, j] = prev
+            z = hidden_of(prev, embedding, drafter[0], ws) @ drafter[1].T
+            prev, _ = R.rl_sample_tokens(z, torch.rand(n, generator=g, device=dev), draw, ws)
+            draft[:, j], ids[:, j] = z, prev
         # the policy's rows at all places at once
         before = torch.cat([last[:, None], ids], 1).reshape(-1)
-        target = hidden_of(before, embedding, policy[0]) @ policy[1].T
+        target = hidden_of(before, embedding, policy[0], ws) @ policy[1].T
         out, acc, lp = R.rl_verify_drafts(target, ids.reshape(-1), offsets,
                                           torch.rand(n * DRAFTED, generator=g, device=dev),
                                           torch.rand(n, generator=g, device=dev), DRAFTED, params, ws,
@@ -99,14 +100,14 @@ def train(iterations=12, seed=0, device="cuda"):
         accepted_seen.append(accepted)
         # the policy gradient through the head
         adv, coef, _, owner = R.rl_group_advantages(group_offsets, rewards, traj_offsets, mask, params, ws)
-        ids, h = tokens.reshape(-1), hidden_of(before.reshape(-1), embedding, copies[0])
+        ids, h = tokens.reshape(-1), hidden_of(before.reshape(-1), embedding, copies[0], ws)
         old_logp, _, _ = R.rl_fused_head_token_logprobs(h, copies[1], ids, ws)
         loss = torch.zeros(1, dtype=torch.float64, device=device)
         d_head = torch.zeros(VOCAB, HIDDEN, device=device)
         d_h = R.rl_fused_head_loss_fwd_bwd(h, copies[1], ids, mask, owner, adv, coef, old_logp, params, ws, loss, d_head,
                                            d_hidden_dtype=torch.float32, rollout_logp=rollout_logp.reshape(-1))
         d_pre = d_h * (1.0 - h.float() ** 2)
-        d_w1 = d_pre.T @ embedding[before.reshape(-1).long()].float()
+        d_w1 = d_pre.T @ embedded(before.reshape(-1), embedding, ws)
         # the updates
         for k, (w, grad) in enumerate(((w1, d_w1), (head, d_head))):
             R.rl_muon_update(grad.contiguous(), steps[k], spaces[k], momentum=momenta[k], weights=w, weights_bf16=copies[k])

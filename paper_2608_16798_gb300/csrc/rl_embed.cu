@@ -875,8 +875,9 @@ rl_status rl_embedding_fwd(const int32_t* token_ids, int64_t T, const void* weig
   if (!std::isfinite(scale)) return set_error(RL_ERR_INVALID_ARG, f + "scale is not finite");
   if (T == 0) return RL_OK;
   if (!token_ids || !weight || !out || !ws) return set_error(RL_ERR_INVALID_ARG, f + "a required pointer is NULL");
-  if (!embed::element_aligned(weight, w_dtype) || !embed::element_aligned(out, out_dtype) || !aligned16(ws))
-    return set_error(RL_ERR_ALIGNMENT, f + "matrices must be aligned to their elements and ws to 16 bytes");
+  if (!embed::element_aligned(token_ids, RL_F32) || !embed::element_aligned(weight, w_dtype) ||
+      !embed::element_aligned(out, out_dtype) || !aligned16(ws))
+    return set_error(RL_ERR_ALIGNMENT, f + "ids and matrices must be aligned to their elements and ws to 16 bytes");
   if (ws_bytes < kWsHeader) return set_error(RL_ERR_WORKSPACE_TOO_SMALL, f + "workspace smaller than its header");
   embed::FwdArgs a = {};
   a.ids = token_ids;
@@ -914,8 +915,9 @@ rl_status rl_embedding_bwd(const int32_t* token_ids, int64_t T, const void* d_ou
   if (!std::isfinite(scale)) return set_error(RL_ERR_INVALID_ARG, f + "scale is not finite");
   if (T == 0) return RL_OK;
   if (!token_ids || !d_out || !d_weight || !ws) return set_error(RL_ERR_INVALID_ARG, f + "a required pointer is NULL");
-  if (!embed::element_aligned(d_out, d_dtype) || !embed::element_aligned(d_weight, RL_F32) || !aligned16(ws))
-    return set_error(RL_ERR_ALIGNMENT, f + "matrices must be aligned to their elements and ws to 16 bytes");
+  if (!embed::element_aligned(token_ids, RL_F32) || !embed::element_aligned(d_out, d_dtype) ||
+      !embed::element_aligned(d_weight, RL_F32) || !aligned16(ws))
+    return set_error(RL_ERR_ALIGNMENT, f + "ids and matrices must be aligned to their elements and ws to 16 bytes");
   const embed::Plan q = embed::plan(T, V);
   const embed::Layout l = embed::layout(q, T, D);
   if (ws_bytes < l.bytes)

@@ -781,6 +781,8 @@ rl_status rl_layer_norm_fwd(const void* x, rl_dtype x_dtype, int64_t rows, int64
   if (!(eps >= 0.f) || !std::isfinite(eps)) return set_error(RL_ERR_INVALID_ARG, f + "eps must be finite and not negative");
   if (rows == 0) return RL_OK;
   if (!mean || !rstd) return set_error(RL_ERR_INVALID_ARG, f + "mean or rstd is NULL");
+  if (!norm::element_aligned(mean, RL_F32) || !norm::element_aligned(rstd, RL_F32))
+    return set_error(RL_ERR_ALIGNMENT, f + "mean or rstd is not aligned to its elements");
   if (x == y && (x_dtype != y_dtype || ld_x != ld_y))
     return set_error(RL_ERR_INVALID_ARG, f + "y may be x only with its type and leading dimension");
   norm::FwdArgs a = {};
@@ -824,6 +826,8 @@ rl_status rl_layer_norm_bwd(const void* d_y, rl_dtype dy_dtype, int64_t ld_dy, c
   if ((d_x == d_y && (x_dtype != dy_dtype || ld_dx != ld_dy)) || (d_x == x && ld_dx != ld_x))
     return set_error(RL_ERR_INVALID_ARG, f + "d_x may be d_y or x only with its type and leading dimension");
   if (!aligned16(ws)) return set_error(RL_ERR_ALIGNMENT, f + "ws must be 16-byte aligned");
+  for (const float* v : {mean, rstd, static_cast<const float*>(d_weight), static_cast<const float*>(d_bias)})
+    if (!norm::element_aligned(v, RL_F32)) return set_error(RL_ERR_ALIGNMENT, f + "a vector is not aligned to its elements");
   if (ws_bytes < rl_layer_norm_workspace_size(rows, D))
     return set_error(RL_ERR_WORKSPACE_TOO_SMALL, f + "ws_bytes below rl_layer_norm_workspace_size(rows, D)");
   norm::BwdArgs a = {};
