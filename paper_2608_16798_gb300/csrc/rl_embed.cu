@@ -319,6 +319,7 @@ __global__ void __launch_bounds__(kBlockThreads) cluster_sort_kernel(const Clust
   const int rank = static_cast<int>(cluster_ctarank());
   const int first = rank * p.cap, mine = max(0, min(p.cap, p.T - first));  // positions first .. first + mine
   const int rounds = (p.cap / 32 + kBlockWarps - 1) / kBlockWarps, w0 = warp * rounds * 32;
+  next_may_start();  // the sums' CTAs, on the SMs that this kernel leaves free
   if (rank == 0 && threadIdx.x == 0) *p.crossing = 0;
   bool bad = false;
   for (int i = threadIdx.x; i < mine; i += kBlockThreads) {
@@ -490,6 +491,7 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(const SumArgs p) {
   const int64_t a = ch * L;
   const int n = static_cast<int>(max(int64_t(0), min(p.chunk, p.T - a)));        // its positions
   const int m = static_cast<int>(max(int64_t(0), min(2 * p.chunk, p.T - a)));    // and the next chunk's
+  after_previous();
   for (int i = x; i < m + 2; i += CX) {
     const int64_t at = a + i - 1;
     key[y][i] = n > 0 && at >= 0 && at < p.T ? p.keys[at] : -1;
@@ -577,6 +579,7 @@ template <bool WHOLE>
 __global__ void __launch_bounds__(kJoinWarps * 32) join_kernel(const SumArgs p) {
   __shared__ __align__(16) float sum[kJoinWarps][128];
   const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+  after_previous();
   const int64_t slices = (p.D + 127) / 128, items = *p.crossing * slices;
   for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
     const int64_t ch = p.list[it / slices], c = it % slices * 128 + lane * 4;
@@ -772,17 +775,19 @@ rl_status forward(const FwdArgs& a, cudaStream_t s) {
 }
 
 template <typename T, int N, bool WHOLE>
-void launch_sums(const SumArgs& a, int64_t chunks, cudaStream_t s) {
+cudaError_t launch_sums(const SumArgs& a, int64_t chunks, cudaStream_t s) {
   const int64_t threads = (a.D + N - 1) / N;
+  cudaError_t e = cudaSuccess;
   auto go = [&](auto kern, int cx) {
     const int64_t per = kSumThreads / cx;
-    kern<<<dim3(static_cast<unsigned>((chunks + per - 1) / per), static_cast<unsigned>((threads + cx - 1) / cx)),
-           kSumThreads, 0, s>>>(a);
+    e = launch_after(kern, dim3(static_cast<unsigned>((chunks + per - 1) / per), static_cast<unsigned>((threads + cx - 1) / cx)),
+                     dim3(kSumThreads), 0, s, a);
   };
   if (threads > 64) go(sum_kernel<T, N, WHOLE, 128>, 128);
   else if (threads > 32) go(sum_kernel<T, N, WHOLE, 64>, 64);
   else if (threads > 16) go(sum_kernel<T, N, WHOLE, 32>, 32);
   else go(sum_kernel<T, N, WHOLE, 16>, 16);
+  return e;
 }
 
 // How the rows lie: those of d in 16-byte blocks, and those of dw too.
@@ -812,15 +817,11 @@ template <typename T>
 rl_status sums(const SumArgs& a, int64_t chunks, cudaStream_t s) {
   constexpr int N = 16 / sizeof(T);
   const Rows r = rows_of<T>(a.d, a.ld, a.dw, a.D);
-  if (!r.d) launch_sums<T, 1, false>(a, chunks, s);
-  else if (r.dw) launch_sums<T, N, true>(a, chunks, s);
-  else launch_sums<T, N, false>(a, chunks, s);
-  cudaError_t e = cudaGetLastError();
+  cudaError_t e = !r.d ? launch_sums<T, 1, false>(a, chunks, s)
+                       : r.dw ? launch_sums<T, N, true>(a, chunks, s) : launch_sums<T, N, false>(a, chunks, s);
   if (e != cudaSuccess) return cuda_error(e, "sum_kernel launch");
   if (chunks > 2) {
-    if (r.dw) join_kernel<true><<<kJoinCtas, kJoinWarps * 32, 0, s>>>(a);
-    else join_kernel<false><<<kJoinCtas, kJoinWarps * 32, 0, s>>>(a);
-    e = cudaGetLastError();
+    e = launch_after(r.dw ? join_kernel<true> : join_kernel<false>, dim3(kJoinCtas), dim3(kJoinWarps * 32), 0, s, a);
     if (e != cudaSuccess) return cuda_error(e, "join_kernel launch");
   }
   return RL_OK;

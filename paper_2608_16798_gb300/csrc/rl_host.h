@@ -63,6 +63,23 @@ rl_status head_grad(const Tokens& tok, int group, int64_t rows, const uint16_t* 
                     float* d_weight, float* part_sums, int parts, const double* row_loss, double* loss_accum,
                     uint32_t* counter, int32_t* status, cudaStream_t s);
 
+// Launches `kern` so that it may start while the kernel before it in the stream still runs (it waits with after_previous() before
+// it touches what that one writes). kern's arguments have to have its parameters' types.
+template <typename... P, typename... A>
+cudaError_t launch_after(void (*kern)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t s, A... args) {
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  return cudaLaunchKernelEx(&cfg, kern, P(args)...);
+}
+
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 }  // namespace rl

@@ -595,6 +595,7 @@ __global__ void __launch_bounds__(32 * kPartLanes) add_parts_kernel(const float*
   const int lane = threadIdx.x & 31, row = threadIdx.x / 32;
   const int64_t c = static_cast<int64_t>(blockIdx.x) * 32 + lane;
   float s = 0.f;
+  after_previous();
   if (c < D) {
 #pragma unroll 8
     for (int i = row; i < parts; i += kPartLanes) s += part[i * D + c];
@@ -740,9 +741,8 @@ rl_status bwd(BwdArgs& a, float* d_weight, float* d_bias, int32_t* status, cudaS
     if (e != cudaSuccess) return cuda_error(e, "loop_bwd_kernel launch");
   }
   if (!d_weight && !d_bias) return RL_OK;
-  add_parts_kernel<<<dim3(static_cast<unsigned>((a.D + 31) / 32), 2), 32 * kPartLanes, 0, s>>>(a.part_w, a.part_b, a.parts, a.D,
-                                                                                              d_weight, d_bias);
-  e = cudaGetLastError();
+  e = launch_after(add_parts_kernel, dim3(static_cast<unsigned>((a.D + 31) / 32), 2), dim3(32 * kPartLanes), 0, s, a.part_w,
+                   a.part_b, a.parts, a.D, d_weight, d_bias);
   return e == cudaSuccess ? RL_OK : cuda_error(e, "add_parts_kernel launch");
 }
 
