@@ -291,6 +291,7 @@ struct ClusterArgs {
   uint32_t* crossing;  // set to zero for the sums
   int32_t* status;
   int32_t T, V, cap;  // cap: positions of a CTA, a multiple of 32
+  uint32_t inverse;   // 2^32 / cap, rounded up
   int32_t passes, bits;
 };
 
@@ -403,7 +404,7 @@ __global__ void __launch_bounds__(kBlockThreads) cluster_sort_kernel(const Clust
       __syncwarp();
       if (peers[k] != 0) {
         if (lane == __ffs(peers[k]) - 1) n[warp][dg] += static_cast<uint16_t>(__popc(peers[k]));
-        const uint32_t cta = at / static_cast<uint32_t>(p.cap);
+        const uint32_t cta = __umulhi(at, p.inverse);  // at / cap: exact, at is below 2^18 and cap below 2^14
         put_pair(map_to_rank(to + (at - cta * p.cap) * 8, cta), e.x, e.y);
       }
       __syncwarp();
@@ -562,7 +563,7 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(const SumArgs p) {
 }
 
 constexpr int kJoinWarps = 8;
-constexpr int kJoinCtas = 4 * 152;
+constexpr int kJoinCtas = 8 * 152;
 
 // The last chunk of a long run of v that begins in chunk `ch`, by a whole warp.
 __device__ __forceinline__ int64_t last_chunk(const SumArgs& p, int64_t ch, int32_t v, int lane) {
@@ -841,6 +842,7 @@ rl_status cluster_sort(ClusterArgs& a, cudaStream_t s) {
     ready |= bit;
   }
   a.cap = ((a.T + kSortCtas - 1) / kSortCtas + 31) / 32 * 32;
+  a.inverse = static_cast<uint32_t>(((uint64_t(1) << 32) + a.cap - 1) / a.cap);
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
