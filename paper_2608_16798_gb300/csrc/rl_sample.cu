@@ -344,21 +344,26 @@ struct Row {
       sh.warp_mass[warp] = run_w;
     }
     __syncthreads();
-    run_n += above - mine_n;
-    run_w += mass - mine_w;
-    all_n = 0;
-    all_w = 0;
+    // the warps' sums, by every warp: a lane each
+    uint32_t of_n = lane < WARPS ? sh.warp_count[lane] : 0u;
+    unsigned long long of_w = masses && lane < WARPS ? sh.warp_mass[lane] : 0ull;
 #pragma unroll
-    for (int v = 0; v < WARPS; ++v) {
-      const uint32_t a = sh.warp_count[v];
-      run_n += v < warp ? a : 0;
-      all_n += a;
-      if (masses) {
-        const unsigned long long b = sh.warp_mass[v];
-        run_w += v < warp ? b : 0;
-        all_w += b;
-      }
+    for (int o = 1; o < WARPS; o <<= 1) {
+      const uint32_t x = __shfl_up_sync(0xffffffffu, of_n, o);
+      if (lane >= o) of_n += x;
     }
+    if (masses)
+#pragma unroll
+      for (int o = 1; o < WARPS; o <<= 1) {
+        const unsigned long long x = __shfl_up_sync(0xffffffffu, of_w, o);
+        if (lane >= o) of_w += x;
+      }
+    all_n = __shfl_sync(0xffffffffu, of_n, WARPS - 1);
+    all_w = __shfl_sync(0xffffffffu, of_w, WARPS - 1);
+    const uint32_t prev_n = __shfl_sync(0xffffffffu, of_n, max(warp - 1, 0));
+    const unsigned long long prev_w = __shfl_sync(0xffffffffu, of_w, max(warp - 1, 0));
+    run_n += above - mine_n + (warp ? prev_n : 0u);
+    run_w += mass - mine_w + (warp ? prev_w : 0ull);
   }
 
   // Sorts the first `size` (a power of two) of the list, by all threads.
@@ -558,18 +563,28 @@ struct Row {
       fresh = true;
       if (threadIdx.x == 0) sh.bin = -1;
       __syncthreads();
-      uint32_t a = run_n;
-      unsigned long long m = run_w;
+      const int shift = to.shift < 0 ? kBf16Shift : to.shift;
+      uint32_t a = run_n, a_hit = 0, n_hit = 0;
+      unsigned long long m = run_w, m_hit = 0, w_hit = 0;
+      int hit = -1;
 #pragma unroll
       for (int i = 0; i < kOwn; ++i) {
         if (by_mass ? m < goal && m + w[i] >= goal : a < goal && a + n[i] >= goal) {
-          sh.bin = threadIdx.x * kOwn + i;
-          sh.found.above = a;
-          sh.found.mass = m;
-          sh.found.m = n[i];
+          hit = threadIdx.x * kOwn + i;
+          a_hit = a, m_hit = m, n_hit = n[i], w_hit = w[i];
         }
         a += n[i];
         m += w[i];
+      }
+      if (hit >= 0) {  // one thread of all: the bin's border, if it is of one value
+        Border f{entry_key<T>(key_at(to, hit)), n_hit, a_hit, m_hit, 0};
+        if (shift <= kSingle) {
+          f.unit = w_hit / n_hit;  // w is n times the value's mass
+          if (!by_mass) f.m = static_cast<uint32_t>(goal) - a_hit;
+          else f.m = static_cast<uint32_t>(min(static_cast<unsigned long long>(n_hit), (goal - m_hit + f.unit - 1) / f.unit));
+        }
+        sh.found = f;
+        sh.bin = hit;
       }
       __syncthreads();
       const int bin = sh.bin;
@@ -587,18 +602,13 @@ struct Row {
           continue;
         }
       } else {
-        const uint32_t k = key_at(to, bin), d0 = k > top ? 0u : top - k;  // the window's first bin may reach above the largest
-        const int shift = to.shift < 0 ? kBf16Shift : to.shift;
         if (shift > kSingle) {
+          const uint32_t k = key_at(to, bin);  // the window's first bin may reach above the largest
           above = b.above;
           mass = b.mass;
-          to = Level{d0, max(0, shift - kBinBits)};
+          to = Level{k > top ? 0u : top - k, max(0, shift - kBinBits)};
           continue;
         }
-        b.key = entry_key<T>(top - d0);
-        b.unit = masses ? mass_of(weight(value_of(b.key))) : 0;
-        if (!by_mass) b.m = static_cast<uint32_t>(goal) - b.above;
-        else if (b.unit) b.m = static_cast<uint32_t>(min(static_cast<unsigned long long>(b.m), (goal - b.mass + b.unit - 1) / b.unit));
         found = b;
         any = true;
       }
@@ -899,12 +909,13 @@ __global__ void __launch_bounds__(WARPS * 32, 1024 / (WARPS * 32)) sample_kernel
   // ---- the threshold: entries above zt are kept, and the first ties of those equal to it (GE: all of them)
   float zt = minus_inf();
   uint32_t ties = 0;
-  int64_t kept = -1;  // not known yet
-  bool ge = false;
+  uint32_t kept = 0;
+  bool known_kept = false, ge = false;
   if (greedy) {
     zt = all.m;
     ties = 1;
     kept = 1;
+    known_kept = true;
   } else if (by_k || by_p) {
     const uint32_t top = key_of(all.m);
     Row<T, WARPS, CLUSTER> s{sh, row, t0, t1, all, c, top, C, by_p};
@@ -918,18 +929,19 @@ __global__ void __launch_bounds__(WARPS * 32, 1024 / (WARPS * 32)) sample_kernel
     if (is) {
       zt = value_of(b.key);
       ties = b.m;
-      kept = static_cast<int64_t>(b.above) + b.m;
+      kept = b.above + b.m;
+      known_kept = true;
     }
   }
   if (by_m && value_of(sh.least_key) > zt) {
     zt = value_of(sh.least_key);
     ge = true;
     ties = 0;
-    kept = -1;
+    known_kept = false;
   }
 
   // ---- the kept weights of every tile
-  const bool count = p.n_kept && kept < 0;
+  const bool count = p.n_kept && !known_kept;
   if (filtered) {
     float sum = 0.f;
     uint32_t equal = 0, above = 0;
@@ -1011,7 +1023,8 @@ __global__ void __launch_bounds__(WARPS * 32, 1024 / (WARPS * 32)) sample_kernel
   float left;
   const int at_cta = pick_at(C, set.u * total, lane, [&](int) { return mine; }, left);  // a lane has one
   if (at_cta != rank) return;
-  if (kept < 0) kept = __reduce_add_sync(0xffffffffu, part.above);
+  // (not under the condition that its result is wanted: built so, a number that was known came out as this one)
+  const uint32_t counted = __reduce_add_sync(0xffffffffu, part.above);
   const uint32_t ties_before = __shfl_sync(0xffffffffu, before, rank);
 
   // ---- its tile
@@ -1099,7 +1112,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1024 / (WARPS * 32)) sample_kernel
   p.ids[r] = token;
   p.logp[r] = logp_of(zx, all, c);
   if (p.among) p.among[r] = (exponent(zx, all.m, c) - log2f(total)) * kLn2;
-  if (p.n_kept) p.n_kept[r] = static_cast<int32_t>(kept);
+  if (p.n_kept) p.n_kept[r] = static_cast<int32_t>(known_kept ? kept : counted);
 }
 
 // ---------------------------------------------------------------- host
