@@ -303,6 +303,226 @@ __global__ void __launch_bounds__(kMostWarps * 32) fwd_kernel(const FwdArgs p) {
   }
 }
 
+// ---------------------------------------------------------------- short rows, several to a warp
+
+constexpr int kShortWarps = 8;
+
+// R rows at a time on a warp, 4 NG elements of each a lane, loaded before the first is worked on: what a short row costs is the
+// chain of its two sums, and R chains run at once. Measured, 500,000 rows of 128 bf16: SHORTFWD us, through the ring 140.
+template <typename TX, typename TY, int NG, int R, bool WHOLE>
+__global__ void __launch_bounds__(kShortWarps * 32) fwd_short_kernel(const FwdArgs p) {
+  const int t = threadIdx.x & 31, D = static_cast<int>(p.D);
+  const int64_t r0 = (static_cast<int64_t>(blockIdx.x) * kShortWarps + threadIdx.x / 32) * R;
+  if (r0 >= p.rows) return;
+  const float inv = 1.f / static_cast<float>(D);
+  float2 v[R][NG][2];
+#pragma unroll
+  for (int k = 0; k < R; ++k) {
+    const TX* x = static_cast<const TX*>(p.x) + min(r0 + k, p.rows - 1) * p.ld_x;
+    if (WHOLE) {
+      Raw<TX> raw[NG];
+#pragma unroll
+      for (int j = 0; j < NG; ++j) raw[j].stream(x + (column_of<true>(j, 0, 32, t) < D ? column_of<true>(j, 0, 32, t) : 0));
+#pragma unroll
+      for (int j = 0; j < NG; ++j) raw[j].get(v[k][j]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < NG; ++j)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int c0 = column_of<false>(j, 2 * e, 32, t), c1 = column_of<false>(j, 2 * e + 1, 32, t);
+          v[k][j][e] = make_float2(Io<TX>::get(__ldcs(x + (c0 < D ? c0 : 0))), Io<TX>::get(__ldcs(x + (c1 < D ? c1 : 0))));
+        }
+    }
+  }
+  float2 g[NG][2], b[NG][2];
+  get_parameters<NG, WHOLE>(g, p.w, 0.f, D, 32, t);
+  get_parameters<NG, WHOLE>(b, p.b, 0.f, D, 32, t);
+  auto clear = [&](float2 (&a)[NG][2]) {
+    if (D == 128 * NG) return;
+#pragma unroll
+    for (int j = 0; j < NG; ++j)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        if (column_of<WHOLE>(j, 2 * e, 32, t) >= D) a[j][e].x = 0.f;
+        if (column_of<WHOLE>(j, 2 * e + 1, 32, t) >= D) a[j][e].y = 0.f;
+      }
+  };
+  float s[R], q[R];
+#pragma unroll
+  for (int k = 0; k < R; ++k) {
+    clear(v[k]);
+    float2 a = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int j = 0; j < NG; ++j)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) a = __fadd2_rn(a, v[k][j][e]);
+    s[k] = a.x + a.y;
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+    for (int k = 0; k < R; ++k) s[k] += __shfl_xor_sync(0xffffffffu, s[k], o);
+#pragma unroll
+  for (int k = 0; k < R; ++k) {
+    const float m = s[k] * inv;
+    s[k] = fmaf(fmaf(-m, static_cast<float>(D), s[k]), inv, m);  // the mean, rounded once
+    float2 a = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int j = 0; j < NG; ++j)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) v[k][j][e] = __fadd2_rn(v[k][j][e], make_float2(-s[k], -s[k]));
+    clear(v[k]);
+#pragma unroll
+    for (int j = 0; j < NG; ++j)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) a = __ffma2_rn(v[k][j][e], v[k][j][e], a);
+    q[k] = a.x + a.y;
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+    for (int k = 0; k < R; ++k) q[k] += __shfl_xor_sync(0xffffffffu, q[k], o);
+#pragma unroll
+  for (int k = 0; k < R; ++k) {
+    const int64_t r = r0 + k;
+    if (r >= p.rows) break;
+    const float rstd = inverse_root(fmaf(q[k], inv, p.eps));
+#pragma unroll
+    for (int j = 0; j < NG; ++j)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) v[k][j][e] = __ffma2_rn(__fmul2_rn(v[k][j][e], make_float2(rstd, rstd)), g[j][e], b[j][e]);
+    put_row<NG, WHOLE>(static_cast<TY*>(p.y) + r * p.ld_y, v[k], D, 32, t);
+    if (t == 0) {
+      p.mean[r] = s[k];
+      p.rstd[r] = rstd;
+    }
+  }
+}
+
+// The same for the gradient: warps go down the rows R at a time, a fixed assignment, with the columns' sums in registers; the
+// CTA's warps' are added up in order at the end.
+template <typename TX, typename TD, int NG, int R, bool WHOLE>
+__global__ void __launch_bounds__(kShortWarps * 32, 2) bwd_short_kernel(const BwdArgs p) {
+  __shared__ __align__(16) float sums[kShortWarps][128 * NG];
+  const int t = threadIdx.x & 31, warp = threadIdx.x / 32, D = static_cast<int>(p.D);
+  const float inv = 1.f / static_cast<float>(D);
+  float2 wt[NG][2], dw[NG][2], db[NG][2];
+  get_parameters<NG, WHOLE>(wt, p.w, 0.f, D, 32, t);
+#pragma unroll
+  for (int j = 0; j < NG; ++j)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) dw[j][e] = db[j][e] = make_float2(0.f, 0.f);
+  const int64_t step = static_cast<int64_t>(gridDim.x) * kShortWarps * R;
+  for (int64_t r0 = (static_cast<int64_t>(blockIdx.x) * kShortWarps + warp) * R; r0 < p.rows; r0 += step) {
+    float2 h[R][NG][2], g[R][NG][2];
+    float mean[R], rstd[R];
+    bool live[R];
+#pragma unroll
+    for (int k = 0; k < R; ++k) live[k] = r0 + k < p.rows && (!p.mask || p.mask[r0 + k] != 0);
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+      mean[k] = rstd[k] = 0.f;
+      if (!live[k]) {
+#pragma unroll
+        for (int j = 0; j < NG; ++j)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) h[k][j][e] = g[k][j][e] = make_float2(0.f, 0.f);
+        continue;
+      }
+      const TX* x = static_cast<const TX*>(p.x) + (r0 + k) * p.ld_x;
+      const TD* dy = static_cast<const TD*>(p.dy) + (r0 + k) * p.ld_dy;
+      mean[k] = p.mean[r0 + k];
+      rstd[k] = p.rstd[r0 + k];
+      if (WHOLE) {
+        Raw<TX> rx[NG];
+        Raw<TD> rd[NG];
+#pragma unroll
+        for (int j = 0; j < NG; ++j) {
+          const int c = column_of<true>(j, 0, 32, t) < D ? column_of<true>(j, 0, 32, t) : 0;
+          rx[j].stream(x + c);
+          rd[j].stream(dy + c);
+        }
+#pragma unroll
+        for (int j = 0; j < NG; ++j) {
+          rx[j].get(h[k][j]);
+          rd[j].get(g[k][j]);
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < NG; ++j)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int c0 = min(column_of<false>(j, 2 * e, 32, t), D - 1), c1 = min(column_of<false>(j, 2 * e + 1, 32, t), D - 1);
+            h[k][j][e] = make_float2(Io<TX>::get(__ldcs(x + c0)), Io<TX>::get(__ldcs(x + c1)));
+            g[k][j][e] = make_float2(Io<TD>::get(__ldcs(dy + c0)), Io<TD>::get(__ldcs(dy + c1)));
+          }
+      }
+    }
+    float2 sq[R];
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+      float2 s = make_float2(0.f, 0.f), q = s;
+#pragma unroll
+      for (int j = 0; j < NG; ++j)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float2 d = g[k][j][e];
+          if (D != 128 * NG) {
+            if (column_of<WHOLE>(j, 2 * e, 32, t) >= D) d.x = 0.f;
+            if (column_of<WHOLE>(j, 2 * e + 1, 32, t) >= D) d.y = 0.f;
+          }
+          h[k][j][e] = __fmul2_rn(__fadd2_rn(h[k][j][e], make_float2(-mean[k], -mean[k])), make_float2(rstd[k], rstd[k]));
+          g[k][j][e] = __fmul2_rn(d, wt[j][e]);
+          s = __fadd2_rn(s, g[k][j][e]);
+          q = __ffma2_rn(g[k][j][e], h[k][j][e], q);
+          dw[j][e] = __ffma2_rn(d, h[k][j][e], dw[j][e]);
+          db[j][e] = __fadd2_rn(db[j][e], d);
+        }
+      sq[k] = make_float2(s.x + s.y, q.x + q.y);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+      for (int k = 0; k < R; ++k)
+        sq[k] = __fadd2_rn(sq[k], make_float2(__shfl_xor_sync(0xffffffffu, sq[k].x, o), __shfl_xor_sync(0xffffffffu, sq[k].y, o)));
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+      if (r0 + k >= p.rows) break;
+      const float m = -sq[k].x * inv * rstd[k], f = -sq[k].y * inv * rstd[k];
+#pragma unroll
+      for (int j = 0; j < NG; ++j)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          g[k][j][e] = live[k] ? __ffma2_rn(h[k][j][e], make_float2(f, f),
+                                            __ffma2_rn(g[k][j][e], make_float2(rstd[k], rstd[k]), make_float2(m, m)))
+                               : make_float2(0.f, 0.f);
+      put_row<NG, WHOLE>(static_cast<TX*>(p.dx) + (r0 + k) * p.ld_dx, g[k], D, 32, t);
+    }
+  }
+  auto finish = [&](const float2 (&a)[NG][2], float* part) {
+    if (!part) return;
+#pragma unroll
+    for (int j = 0; j < NG; ++j)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int c0 = column_of<WHOLE>(j, 2 * e, 32, t), c1 = column_of<WHOLE>(j, 2 * e + 1, 32, t);
+        if (c0 < D) sums[warp][c0] = a[j][e].x;
+        if (c1 < D) sums[warp][c1] = a[j][e].y;
+      }
+    __syncthreads();
+    for (int c = threadIdx.x; c < D; c += kShortWarps * 32) {
+      float s = 0.f;
+#pragma unroll
+      for (int w = 0; w < kShortWarps; ++w) s += sums[w][c];
+      part[blockIdx.x * p.D + c] = s;
+    }
+    __syncthreads();
+  };
+  finish(dw, p.part_w);
+  finish(db, p.part_b);
+}
+
 // ---------------------------------------------------------------- rows through shared memory
 
 constexpr int kStages = 8;
@@ -616,7 +836,7 @@ constexpr int64_t kMaxD = 1 << 20;
 
 // Blocks of four columns a thread holds in the backward kernel, and the warps of a row; 0: a row has too many columns for
 // it. An element at a time two blocks: four spill (128 registers), and with the stages in the way of L1 that cost 3 times the time.
-inline int bwd_groups(int64_t D, bool whole) { return D <= 256 || (!whole && D <= 256 * kMostWarps) ? 2 : 4; }
+inline int bwd_groups(int64_t D, bool whole) { return !whole && D <= 256 * kMostWarps ? 2 : 4; }
 inline int bwd_warps(int64_t D, bool whole) {
   const int64_t per = 128 * bwd_groups(D, whole), W = (D + per - 1) / per;
   return W <= kMostWarps ? static_cast<int>(W) : 0;
@@ -626,7 +846,7 @@ inline int bwd_ctas(int W) { return 16 / W; }
 
 // Parts of the columns' sums.
 inline int parts_of(int64_t rows, int64_t D) {
-  const int W = bwd_warps(D, true);  // the fewest of a row
+  const int W = D <= 256 ? 4 : bwd_warps(D, true);  // the fewest of a row (short rows: four CTAs an SM at most)
   return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(rows, W ? bwd_ctas(W) * kSMs : 2 * kSMs)));
 }
 
@@ -691,11 +911,16 @@ rl_status fwd(const FwdArgs& a, cudaStream_t s) {
   }
   const int W = warps(4), ctas = std::max(1, (whole ? 32 : 16) / W);
   rl_status r = RL_OK;
-  if (warps(2) <= kMostWarps && a.rows * warps(2) <= 24 * kSMs) {
+  if (warps(2) == 1) {
+    auto go = [&](auto kern, int rows) {
+      kern<<<static_cast<unsigned>((a.rows + kShortWarps * rows - 1) / (kShortWarps * rows)), kShortWarps * 32, 0, s>>>(a);
+    };
+    if (a.rows < 8 * kSMs) whole ? go(fwd_short_kernel<TX, TY, 2, 1, true>, 1) : go(fwd_short_kernel<TX, TY, 2, 1, false>, 1);
+    else if (a.D <= 128) whole ? go(fwd_short_kernel<TX, TY, 1, 4, true>, 4) : go(fwd_short_kernel<TX, TY, 1, 4, false>, 4);
+    else whole ? go(fwd_short_kernel<TX, TY, 2, 4, true>, 4) : go(fwd_short_kernel<TX, TY, 2, 4, false>, 4);
+  } else if (warps(2) <= kMostWarps && a.rows * warps(2) <= 24 * kSMs) {
     if (whole) launch_fwd<TX, TY, 2, true>(a, warps(2), s);
     else launch_fwd<TX, TY, 2, false>(a, warps(2), s);
-  } else if (warps(2) == 1) {
-    r = whole ? launch_ring<TX, TY, 2, true>(a, 1, 24, s) : launch_ring<TX, TY, 2, false>(a, 1, 24, s);
   } else {
     r = whole ? launch_ring<TX, TY, 4, true>(a, W, ctas, s) : launch_ring<TX, TY, 4, false>(a, W, ctas, s);
   }
@@ -721,10 +946,18 @@ rl_status bwd(BwdArgs& a, float* d_weight, float* d_bias, int32_t* status, cudaS
   cudaError_t e = cudaSuccess;
   const bool whole = a.D * sizeof(TX) % 16 == 0 && a.D * sizeof(TD) % 16 == 0 && whole_blocks(a.x, a.ld_x, sizeof(TX)) &&
                      whole_blocks(a.dy, a.ld_dy, sizeof(TD)) && whole_blocks(a.dx, a.ld_dx, sizeof(TX));
-  if (const int W = bwd_warps(a.D, whole)) {
+  if (a.D <= 256) {
+    a.parts = static_cast<int32_t>(std::min<int64_t>((a.rows + kShortWarps - 1) / kShortWarps, 3 * kSMs));
+    auto go = [&](auto kern) { kern<<<a.parts, kShortWarps * 32, 0, s>>>(a); };
+    if (a.rows < a.parts * kShortWarps * 4) whole ? go(bwd_short_kernel<TX, TD, 2, 1, true>) : go(bwd_short_kernel<TX, TD, 2, 1, false>);
+    else if (a.D <= 128) whole ? go(bwd_short_kernel<TX, TD, 1, 4, true>) : go(bwd_short_kernel<TX, TD, 1, 4, false>);
+    else whole ? go(bwd_short_kernel<TX, TD, 2, 2, true>) : go(bwd_short_kernel<TX, TD, 2, 2, false>);
+    e = cudaGetLastError();
+    if (e != cudaSuccess) return cuda_error(e, "bwd_short_kernel launch");
+  } else if (const int W = bwd_warps(a.D, whole)) {
     a.parts = static_cast<int32_t>(std::min<int64_t>(a.parts, bwd_ctas(W) * kSMs));
     rl_status r;
-    if (bwd_groups(a.D, whole) == 2) r = whole ? launch_bwd<TX, TD, 2, true>(a, W, status, s) : launch_bwd<TX, TD, 2, false>(a, W, status, s);
+    if (bwd_groups(a.D, whole) == 2) r = launch_bwd<TX, TD, 2, false>(a, W, status, s);
     else r = whole ? launch_bwd<TX, TD, 4, true>(a, W, status, s) : launch_bwd<TX, TD, 4, false>(a, W, status, s);
     if (r != RL_OK) return r;
     e = cudaGetLastError();
