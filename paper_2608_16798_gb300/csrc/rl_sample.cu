@@ -184,14 +184,11 @@ template <int WARPS>
 struct Shared {
   Fold fold[WARPS * kMostCluster];    // every warp's, the same in every CTA of the cluster
   alignas(16) uint32_t count[kBins + 32];  // this CTA's entries (and behind the bins those outside the window)
-  static constexpr int kList = WARPS == 4 ? 256 : 4096;  // (of short rows, whose passes are short, what is sorted soon)
-  union {
-    struct {
-      alignas(16) uint32_t low[kBins];  // and their mass
-      alignas(16) uint32_t high[kBins];
-    };
-    unsigned long long list[kList];  // the entries that may be kept, where they are few: by size, then by index
-  };
+  static constexpr int kSort = WARPS == 4 ? 256 : 512;  // as many are sorted sooner than counted
+  static constexpr int kList = WARPS == 4 ? 256 : 4096;
+  alignas(16) uint32_t low[kBins];  // and their mass
+  alignas(16) uint32_t high[kBins];
+  unsigned long long list[kList];  // the entries that may be kept, where they are few: by size, then by index
   alignas(8) uint32_t n_list;
   uint32_t n_equal;
   unsigned long long total;
@@ -236,6 +233,7 @@ struct Row {
   bool masses;   // weights are wanted
   static constexpr int N = Elem<T>::N, kThreads = WARPS * 32, kOwn = kBins / kThreads;
   static constexpr int kSingle = sizeof(T) == 2 ? kBf16Shift : 0;  // bins of at most these patterns hold one value
+  bool listed = false;  // the CTA's entries that count are in its list
   uint32_t above = 0;  // entries before the level's first bin
   unsigned long long mass = 0;
   uint32_t n[kOwn], run_n, all_n;            // this thread's bins over the cluster; entries before them; all bins'
@@ -254,26 +252,29 @@ struct Row {
       sh.high[i] = 0;
     }
     __syncthreads();
-    for (int t = t0 + warp; t < t1; t += WARPS) {
-      uint4 q[kTileBlocks];
-      row.tile(t, lane, q);
+    auto add = [&](float z) {
+      const uint32_t d = top - key_of(z), bin = (d - to.d0) >> to.shift;
+      if (!(z > minus_inf()) || d < to.d0 || bin >= kBins) return;
+      atomicAdd(&sh.count[bin], 1u);
+      if (!weigh) return;
+      const unsigned long long m = mass_of(weight(z));
+      const uint32_t lo = static_cast<uint32_t>(m), old = atomicAdd(&sh.low[bin], lo);
+      const uint32_t hi = static_cast<uint32_t>(m >> 32) + (old + lo < old ? 1u : 0u);
+      if (hi) atomicAdd(&sh.high[bin], hi);
+    };
+    if (sizeof(T) == 4 && listed) {
+      for (int i = threadIdx.x; i < static_cast<int>(sh.n_list); i += kThreads) add(value_of(~static_cast<uint32_t>(sh.list[i] >> 32)));
+    } else {
+      for (int t = t0 + warp; t < t1; t += WARPS) {
+        uint4 q[kTileBlocks];
+        row.tile(t, lane, q);
 #pragma unroll 1
-      for (int i = 0; i < kTileBlocks; ++i) {
-        float z[N];
-        Elem<T>::unpack(q[0], z);
-        q[0] = q[1], q[1] = q[2], q[2] = q[3];
+        for (int i = 0; i < kTileBlocks; ++i) {
+          float z[N];
+          Elem<T>::unpack(q[0], z);
+          q[0] = q[1], q[1] = q[2], q[2] = q[3];
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-          const uint32_t d = top - key_of(z[e]), bin = (d - to.d0) >> to.shift;
-          if (z[e] > minus_inf() && d >= to.d0 && bin < kBins) {
-            atomicAdd(&sh.count[bin], 1u);
-            if (weigh) {
-              const unsigned long long m = mass_of(weight(z[e]));
-              const uint32_t lo = static_cast<uint32_t>(m), old = atomicAdd(&sh.low[bin], lo);
-              const uint32_t hi = static_cast<uint32_t>(m >> 32) + (old + lo < old ? 1u : 0u);
-              if (hi) atomicAdd(&sh.high[bin], hi);
-            }
-          }
+          for (int e = 0; e < N; ++e) add(z[e]);
         }
       }
     }
@@ -390,9 +391,10 @@ struct Row {
     return size;
   }
 
-  // For an fp32 row whose window says that few entries can be kept: they are gathered in the first CTA and sorted by size,
-  // the border is read off the running mass, what is kept is sorted by index, and the token is found by a scan. false: they are
-  // not few, or the border is not in the window. True: the row is done. `least`: min_p, as an exponent.
+  // For an fp32 row whose window says that few entries can be kept: they are listed, so that the levels of a search count them
+  // and not the row's; and the fewest are gathered in the first CTA and sorted by size, the border is read off the running
+  // mass, what is kept is sorted by index, and the token is found by a scan: the row is done (true). `least`: min_p, as an
+  // exponent. Measured, 254 rows of 151,936: LISTUS.
   __device__ __forceinline__ bool finish_by_list(int32_t top_k, float top_p, float least, const Args& p, int64_t out, float u,
                                                  const T* z_row, const float* tile_max) {
     const int warp = threadIdx.x / 32, lane = threadIdx.x & 31, rank = CLUSTER ? static_cast<int>(cluster_ctarank()) : 0;
@@ -402,7 +404,7 @@ struct Row {
       sh.bin = -1;
       sh.n_list = 0;
       sh.n_equal = 0;
-      sh.first = Shared<WARPS>::kList;
+      sh.first = Shared<WARPS>::kSort;
       sh.last = 0;
     }
     __syncthreads();
@@ -424,8 +426,8 @@ struct Row {
     __syncthreads();
     const int bin = sh.bin;
     const uint32_t most = sh.found.above;
-    constexpr int kList = Shared<WARPS>::kList, kEach = kList / kThreads;
-    if (bin < 0 || most > kList) return false;  // the same in every CTA
+    constexpr int kSort = Shared<WARPS>::kSort, kEach = kSort > kThreads ? kSort / kThreads : 1;
+    if (bin < 0 || most > Shared<WARPS>::kList) return false;  // the same in every CTA
     const float edge = value_of(key_at(level, bin) & 0xffff0000u);
     for (int t = t0 + warp; t < t1; t += WARPS) {
       if (!(tile_max[t - t0] >= edge)) continue;
@@ -443,6 +445,10 @@ struct Row {
       }
     }
     sync_all<CLUSTER>();
+    if (most > kSort) {
+      listed = true;
+      return false;
+    }
     int have = static_cast<int>(sh.n_list);
     if (rank == 0)
       for (int r = 1; r < C; ++r) {
@@ -537,7 +543,7 @@ struct Row {
     }
     __syncthreads();
     if (threadIdx.x == 0) {
-      const int at = sh.first < kList ? sh.first : sh.last;
+      const int at = sh.first < kSort ? sh.first : sh.last;
       const int token = min(max(static_cast<int>(sh.list[at] >> 32) - row.lo, 0), p.V - 1);
       const float zx = Elem<T>::one(z_row[token]);
       p.ids[out] = token;
@@ -925,7 +931,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1024 / (WARPS * 32)) sample_kernel
       const float least = by_m ? exponent(all.m, all.m, c) + log2f(set.min_p) : minus_inf();
       if (s.finish_by_list(by_k ? set.top_k : 0, set.top_p, least, p, r, set.u, z, tile_max)) return;
     }
-    const bool is = s.search(by_k ? set.top_k : 0, set.top_p, in_window && (sizeof(T) == 2 || !by_p) ? Level{0u, -1} : Level{0u, kBf16Shift}, b);
+    const bool is = s.search(by_k ? set.top_k : 0, set.top_p, in_window && (sizeof(T) == 2 || (!by_p && !s.listed)) ? Level{0u, -1} : Level{0u, kBf16Shift}, b);
     if (is) {
       zt = value_of(b.key);
       ties = b.m;
