@@ -185,7 +185,7 @@ struct Shared {
   Fold fold[WARPS * kMostCluster];    // every warp's, the same in every CTA of the cluster
   alignas(16) uint32_t count[kBins + 32];  // this CTA's entries (and behind the bins those outside the window)
   static constexpr int kSort = WARPS == 4 ? 256 : 512;  // as many are sorted sooner than counted
-  static constexpr int kList = WARPS == 4 ? 256 : 4096;
+  static constexpr int kList = WARPS == 4 ? 1024 : 4096;
   alignas(16) uint32_t low[kBins];  // and their mass
   alignas(16) uint32_t high[kBins];
   unsigned long long list[kList];  // the entries that may be kept, where they are few: by size, then by index
@@ -1164,8 +1164,11 @@ rl_status launch(Args& a, int C, int64_t all_tiles, cudaStream_t s) {
 template <typename T>
 rl_status run(Args& a, cudaStream_t s) {
   const int64_t nb = (a.V + 7) * sizeof(T) / 16 + 1, tiles = (nb + kTileBlocks32 - 1) / kTileBlocks32;
-  // many rows: small CTAs, which wait less for one another, and do what a row takes beside its entries with fewer warps
-  if (tiles <= 8 && a.rows > kSMs) return launch<T, 4, false>(a, 1, tiles, s);
+  // many rows: small CTAs, which wait less for one another, and do what a row takes beside its entries with fewer warps.
+  // Measured, us by 8 / 4 warps, top-k 50: 2,000 rows of 32,000 bf16 80.5 / 70.2, 1,200 of 60,000 69.2 / 64.3, 1,000 of 32,000
+  // fp32 50.9 / 41.8, but 600 of 32,000 bf16 25.4 / 27.0 and 509 of 151,936 62.0 / 64.4; by 16 / 8 warps 300 of 151,936 37.8 /
+  // 41.7, 509 104 / 82
+  if ((tiles <= 8 && a.rows > kSMs) || (tiles <= 64 && a.rows > 6 * kSMs)) return launch<T, 4, false>(a, 1, tiles, s);
   // else as many CTAs a row as fill the SMs twice over while each of their warps has a tile
   int C = 1;
   while (C < 8 && ((a.rows * C * 2 <= 2 * kSMs && tiles >= 2 * C * 8) || tiles > kMostTiles * C)) C *= 2;
