@@ -730,8 +730,8 @@ typedef struct rl_sample_params {
  * A row without a finite largest entry, or with a NaN, and one whose settings or number are outside the ranges above,
  * gets token -1, NaN log-probabilities and n_kept 0 and sets RL_DEV_BAD_VALUE. Masses are sums of fp32 exponentials:
  * where top_p ends, and which token u selects, is that of exact sums but for borders within 1e-6 of the mass; an entry's
- * own exponential is relative 2^-22 and what the rounding of z / T makes of it. A row's results do not depend on the
- * other rows.
+ * own exponential is relative 2^-22 and what the rounding of z / T makes of it. A row's results do not depend on what
+ * the other rows hold; the number of rows decides how many CTAs share one, and with it the last bits of its sums.
  */
 rl_status rl_sample_tokens(const void* logits, rl_dtype dtype, int64_t rows, int64_t V, int64_t ld, const float* sample_u,
                            const rl_sample_params* params, const float* row_temperature, const int32_t* row_top_k,
@@ -754,7 +754,9 @@ rl_status rl_sample_tokens(const void* logits, rl_dtype dtype, int64_t rows, int
  * The row is summed twice, the squares of x - mean after its mean is known; sums, mean and rstd are fp32.
  * Elements behind D of a row are neither read into the result nor written. A NaN or an infinity in a row makes
  * that row NaN; rows whose squares leave fp32's range (entries of about 1e19) come out as zeros times w plus b.
- * A row's results do not depend on the other rows.
+ * A row's results do not depend on what the other rows hold; the number of rows, D and the alignment decide the order
+ * of its sums. (A bounded wait that ran out, which nothing but a fault of the device can cause, makes rows NaN here:
+ * there is no status word.)
  */
 rl_status rl_layer_norm_fwd(const void* x, rl_dtype x_dtype, int64_t rows, int64_t D, int64_t ld_x, const void* weight,
                             const void* bias, rl_dtype w_dtype, float eps, void* y, rl_dtype y_dtype, int64_t ld_y,
@@ -816,7 +818,8 @@ size_t rl_embedding_workspace_size(int64_t T, int64_t V, int64_t D);
  *   ws, ws_bytes   rl_embedding_workspace_size(T, V, D) bytes, initialised by rl_workspace_init
  *
  * The tokens are sorted by id; each sum is fp32, of the tokens of an id in their order, in parts that depend on the
- * ids and T alone, and is added to d_weight once: repeated calls give the same bits.
+ * ids, T, D, the type and the alignment alone, and is added to d_weight once (by the L2, which takes subnormal numbers
+ * for zeros): repeated calls give the same bits.
  */
 rl_status rl_embedding_bwd(const int32_t* token_ids, int64_t T, const void* d_out, rl_dtype d_dtype, int64_t ld_d, int64_t V,
                            int64_t D, float scale, float* d_weight, void* ws, size_t ws_bytes, rl_stream_t stream);

@@ -4,10 +4,15 @@
 //
 // The gradient's sums want the tokens of a row of W side by side: the tokens are sorted by id, stably (a radix sort in
 // digits of up to 9 bits), the sorted list is cut into chunks of equal length whatever the ids, and a chunk's threads,
-// a few columns each, go down its tokens. A run of equal ids that lies in one chunk is added to dW there; the parts of
-// one that crosses a border go to the workspace and are added up in order afterwards, so that a token that comes very
-// often is shared by as many CTAs as it has chunks. Every element of dW gets one addition per call, and the order of all
-// sums depends on the ids alone: repeated calls give the same bits.
+// a few columns each, go down its tokens. A run of equal ids is added up by the chunk in which it begins, up to a chunk's
+// length into the next one; the parts of a longer run go to the workspace and are added up in order afterwards, so that a
+// token that comes very often is shared by as many CTAs as it has chunks. Every element of dW gets one addition per call,
+// and the order of all sums depends on the ids alone: repeated calls give the same bits. Up to 1,024 tokens are not sorted:
+// every token's CTA looks for its like among all ids.
+//
+// Memory bounds both. Measured: 32,768 tokens of 4,096 columns, ids with frequencies that fall as 1 / rank over 151,936:
+// forward 60 us (91% of the copy's rate over the rows that are named and written), backward 150 (the sort 17, the sums 118 at 80%
+// of the copy's rate, the long runs 10). The digits' passes, chains of a few microseconds each, are what the sort costs.
 #include <algorithm>
 #include <atomic>
 #include <cmath>
@@ -307,8 +312,8 @@ __device__ __forceinline__ void put_pair(uint32_t addr, uint32_t key, uint32_t t
 inline __host__ __device__ int64_t cluster_sort_bytes(int64_t cap) { return 2 * cap * 8 + int64_t(kBlockWarps) * kDigits * 2; }
 
 // The stable radix sort of up to kMostSorted tokens: 16 CTAs hold the list, and a digit's pass writes every token to its
-// place in the CTA that holds it. One launch where the passes through memory take three each. Measured, with launches:
-// SORTUS.
+// place in the CTA that holds it. One launch where the passes through memory take three each. Measured (the kernel alone
+// against the six): 32,768 tokens 17 / 39 us, 155,959 34 / 40.
 __global__ void __launch_bounds__(kBlockThreads) cluster_sort_kernel(const ClusterArgs p) {
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ uint32_t total[kDigits];  // this CTA's tokens of each digit
@@ -453,7 +458,7 @@ __device__ __forceinline__ void load_columns(Block<T, N>& b, const T* row, int64
 }
 
 // dw += v for N columns from c. The additions are left to the L2 (red): nothing waits for the old values, which took 137 us
-// where this takes SUMUS (32,768 tokens, 4,096 columns), and every element gets one of them. WHOLE: rows of dw in 16-byte blocks.
+// where this takes 118 (32,768 tokens, 4,096 columns), and every element gets one of them. WHOLE: rows of dw in 16-byte blocks.
 template <int N, bool WHOLE>
 __device__ __forceinline__ void add_columns(float* row, const float (&v)[N], int64_t c, int64_t D) {
   if (WHOLE && N >= 4) {

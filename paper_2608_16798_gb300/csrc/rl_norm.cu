@@ -3,8 +3,16 @@
 //   h = (x - mean) rstd,   y = h w + b,   rstd = 1 / sqrt(mean of (x - mean)^2 + eps)
 //   g = dy w,   dx = rstd (g - mean of g - h (mean of g h)),   dw += sum over rows dy h,   db += sum over rows dy
 //
-// The simple form: a CTA per row that reads it once for each of the sums, and for the columns' sums threads that go
-// down a part of the rows.
+// Memory bounds all of it: 16 bytes of operations a byte at most. Rows of up to 8,192 columns (forward 8,192, or 8,192 bf16
+// elements of any alignment) are read once, into registers:
+//   - up to 256 columns: several rows to a warp, whose sums' chains run side by side (fwd_short_kernel, bwd_short_kernel);
+//   - few rows forward: as many threads on a row as have two blocks of four of it (fwd_kernel);
+//   - else persistent CTAs that share a row at a time, whose rows bulk copies bring ahead (fwd_ring_kernel, bwd_kernel).
+// Backward a thread has the same columns of all its rows, and the weight's and bias' sums of them stay in its registers; a second
+// launch adds up the CTAs' parts. Wider rows: a CTA per row that reads it once for each sum, and threads that go down the columns.
+// Measured, of the copy's 6.78 TB/s: 32,768 rows of 4,096 forward 77% (bf16) and 84% (fp32 to bf16), backward 84% (bf16), 85%
+// (fp32, bf16 gradient), 81% with 60% of the rows trained on; 131,072 of 512 70% and 71%; odd widths at 130,000 x 1,001 bf16
+// 46% and 42% (an element a load and a store), fp32 83% and 88%.
 #include <algorithm>
 #include <atomic>
 #include <cmath>
@@ -308,7 +316,7 @@ __global__ void __launch_bounds__(kMostWarps * 32) fwd_kernel(const FwdArgs p) {
 constexpr int kShortWarps = 8;
 
 // R rows at a time on a warp, 4 NG elements of each a lane, loaded before the first is worked on: what a short row costs is the
-// chain of its two sums, and R chains run at once. Measured, 500,000 rows of 128 bf16: SHORTFWD us, through the ring 140.
+// chain of its two sums, and R chains run at once. Measured, 500,000 rows of 128 bf16: 66 us, through the ring 140.
 template <typename TX, typename TY, int NG, int R, bool WHOLE>
 __global__ void __launch_bounds__(kShortWarps * 32) fwd_short_kernel(const FwdArgs p) {
   const int t = threadIdx.x & 31, D = static_cast<int>(p.D);
