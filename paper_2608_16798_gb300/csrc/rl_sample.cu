@@ -762,6 +762,29 @@ struct Keep {
     return s.x + s.y;
   }
 };
+// The same for a bf16 row that keeps few entries: a lane takes the ones of at least zt of a block one after the other.
+__device__ __forceinline__ float few_of_tile(const uint4 (&q)[kTileBlocks], float zt, float ref, float c, uint32_t& equal) {
+  const uint32_t t = __float_as_uint(zt) >> 16, t2 = t | t << 16;
+  const float rc = -__fmul_rn(ref, c);
+  const bool apart = large(rc);  // of the row
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < kTileBlocks; ++i) {
+    // bit w: the low half of word w, bit 16 + w: the high one
+    uint32_t b = (least2(q[i].x, t2) & 0x00010001u) | (least2(q[i].y, t2) & 0x00020002u) | (least2(q[i].z, t2) & 0x00040004u) |
+                 (least2(q[i].w, t2) & 0x00080008u);
+    while (b) {
+      const int k = __ffs(b) - 1;
+      b &= b - 1;
+      const uint32_t w = k & 2 ? (k & 1 ? q[i].w : q[i].z) : (k & 1 ? q[i].y : q[i].x);
+      const float z = k & 16 ? bf16_hi(w) : bf16_lo(w);
+      if (z > zt) s += ex2(apart ? (z - ref) * c : fmaf(z, c, rc));
+      else ++equal;
+    }
+  }
+  return s;
+}
+
 // The sum of a warp's pairs of counts of 16 bits.
 __device__ __forceinline__ uint32_t of_pairs(uint32_t n) { return __reduce_add_sync(0xffffffffu, (n & 0xffffu) + (n >> 16)); }
 
@@ -957,6 +980,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1024 / (WARPS * 32)) sample_kernel
   if (filtered) {
     float sum = 0.f;
     uint32_t equal = 0, above = 0;
+    const bool sparse = sizeof(T) == 2 && known_kept && kept <= static_cast<uint32_t>(p.V) / 16;
     auto over = [&](const auto& keep) {
       // this warp's tiles that have an entry to keep; the ones read last first: they are the likeliest to be in L2 still
       const int first = t0 + warp;
@@ -977,7 +1001,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1024 / (WARPS * 32)) sample_kernel
         t = before(t - WARPS);
         if (t >= first) row.tile(t, lane, q);
         uint32_t eq = 0;
-        const float s = warp_sum(keep.tile(now, eq, above, count));
+        const float s = warp_sum(sparse ? few_of_tile(now, zt, all.m, c, eq) : keep.tile(now, eq, above, count));
         eq = of_pairs(eq);
         if (lane == 0) tiles[here - t0].kept = {s, eq};
         sum += s;
