@@ -21,8 +21,8 @@
 //
 // What bounds it is the arithmetic beside the one exponential an entry (unpacking, the bins, the comparisons: 8 instructions
 // an entry for the first pass, 6 for the bins, up to 8 for the pass over what is kept) and the chain of a row's steps. Measured:
-// one row of 151,936 bf16 11 us without filters, 17 with top-k 50 or top-p; 509 rows 38 without (61% of the copy's rate), 62 with
-// top-k 50, 84 with top-p 0.4, 58 with 0.7 / 20 / 0.8. The first form held a row in the shared memory of a cluster (155 with
+// one row of 151,936 bf16 11 us without filters, 15 with top-k 50, 19 with top-p 0.4; 509 rows 40 without (57% of the copy's
+// rate), 62 with top-k 50, 81 with top-p 0.4 (85 before a tile's few kept entries were taken one by one), 58 with 0.7 / 20 / 0.8. The first form held a row in the shared memory of a cluster (155 with
 // top-k 50, 207 with top-p 0.95): 76 rows at work at a time instead of 304, each through four exchanges.
 #include <algorithm>
 #include <atomic>
@@ -400,7 +400,7 @@ struct Row {
   // For an fp32 row whose window says that few entries can be kept: they are listed, so that the levels of a search count them
   // and not the row's; and the fewest are gathered in the first CTA and sorted by size, the border is read off the running
   // mass, what is kept is sorted by index, and the token is found by a scan: the row is done (true). `least`: min_p, as an
-  // exponent. Measured, 254 rows of 151,936, listed / by levels over the row: the 50 largest 44 / 115 us, 0.4 of the mass 101 / 218.
+  // exponent. Measured, 254 rows of 151,936, listed / by levels over the row: the 50 largest 45 / 115 us, 0.4 of the mass 101 / 218.
   __device__ __forceinline__ bool finish_by_list(int32_t top_k, float top_p, float least, const Args& p, int64_t out, float u,
                                                  const T* z_row, const float* tile_max) {
     const int warp = threadIdx.x / 32, lane = threadIdx.x & 31, rank = CLUSTER ? static_cast<int>(cluster_ctarank()) : 0;
