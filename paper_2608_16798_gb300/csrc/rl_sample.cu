@@ -22,8 +22,9 @@
 // What bounds it is the arithmetic beside the one exponential an entry (unpacking, the bins, the comparisons: 8 instructions
 // an entry for the first pass, 6 for the bins, up to 8 for the pass over what is kept) and the chain of a row's steps. Measured:
 // one row of 151,936 bf16 11 us without filters, 15 with top-k 50, 19 with top-p 0.4; 509 rows 40 without (57% of the copy's
-// rate), 62 with top-k 50, 81 with top-p 0.4 (85 before a tile's few kept entries were taken one by one), 58 with 0.7 / 20 / 0.8. The first form held a row in the shared memory of a cluster (155 with
-// top-k 50, 207 with top-p 0.95): 76 rows at work at a time instead of 304, each through four exchanges.
+// rate), 62 with top-k 50, 81 with top-p 0.4 (85 before a tile's few kept entries were taken one by one), 58 with 0.7 / 20 /
+// 0.8. The first form held a row in the shared memory of a cluster (155 with top-k 50, 207 with top-p 0.95): 76 rows at work
+// at a time instead of 304, each through four exchanges.
 #include <algorithm>
 #include <atomic>
 #include <cmath>
