@@ -723,7 +723,7 @@ typedef struct rl_sample_params {
  *   out_ids        int32 [rows]
  *   out_logp       float [rows]: log p of the token (T = 0: of softmax(z)): with T = 1 the rollout_logp of
  *                  rl_policy_loss_fwd_bwd
- *   out_filtered_logp  float [rows] or NULL: log of its share of the kept tokens' mass (T = 0: 0)
+ *   out_filtered_logp  float [rows] or NULL: log of its share of the kept tokens' mass, at most 0 (kept alone, and T = 0: 0)
  *   n_kept         int32 [rows] or NULL: how many tokens are kept
  *   ws, ws_bytes   any initialised workspace: its status word is used (256 bytes suffice)
  *

@@ -93,6 +93,13 @@ __device__ __forceinline__ uint32_t entry_key(uint32_t key) {
 }
 
 constexpr float kMassUnit = 68719476736.f;  // 2^36
+// The logarithm of a token's share of the kept mass, x being its exponent. A token that has all of it, or all but what rounding
+// takes, has a share of 1: x is not 0 for the largest entry (a fused operation's remainder), and log2 of a rounded 2^x is not x.
+// (By the others' mass, log1p, it is no more exact: half a step of the sum, 2^-24 of it, is what is left; 128 rows 34.4 us
+// against 32.8.)
+__device__ __forceinline__ float log_share(float x, float total) {
+  return ex2(x) >= total ? 0.f : fminf((x - log2f(total)) * kLn2, 0.f);
+}
 __device__ __forceinline__ unsigned long long mass_of(float w) { return __float2ull_rn(w * kMassUnit); }
 
 __device__ __forceinline__ unsigned long long ld_cluster_u64(uint32_t addr) {
@@ -555,7 +562,7 @@ struct Row {
       const float zx = Elem<T>::one(z_row[token]);
       p.ids[out] = token;
       p.logp[out] = logp_of(zx, all, c);
-      if (p.among) p.among[out] = (exponent(zx, all.m, c) - log2f(total)) * kLn2;
+      if (p.among) p.among[out] = log_share(exponent(zx, all.m, c), total);
       if (p.n_kept) p.n_kept[out] = kept;
     }
     return true;
@@ -1148,7 +1155,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1024 / (WARPS * 32)) sample_kernel
   const float zx = Elem<T>::one(z[token]);
   p.ids[r] = token;
   p.logp[r] = logp_of(zx, all, c);
-  if (p.among) p.among[r] = (exponent(zx, all.m, c) - log2f(total)) * kLn2;
+  if (p.among) p.among[r] = log_share(exponent(zx, all.m, c), total);
   if (p.n_kept) p.n_kept[r] = static_cast<int32_t>(known_kept ? kept : counted);
 }
 

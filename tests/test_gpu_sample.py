@@ -250,3 +250,36 @@ def test_repeats_streams_and_graphs(R):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(first, out))
+
+
+ALONE = [("greedy", (0.0, 0, 1.0, 0.0)), ("top_k", (1.0, 1, 1.0, 0.0)), ("top_k, cold", (0.7, 1, 0.9, 0.1)),
+         ("top_p", (0.7, 0, 1e-6, 0.0)), ("min_p", (0.6, 0, 1.0, 1.0))]
+
+
+@pytest.mark.parametrize("rows,V", [(1, 5), (3, 151936), (61, 32003), (300, 4001), (1833, 1472)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("name,settings", ALONE, ids=[n for n, _ in ALONE])
+def test_a_token_kept_alone_has_the_whole_mass(R, name, settings, dtype, rows, V):
+    """Its share is 1, whatever its value: the logarithm is 0, not the rounding of the weight's own exponential."""
+    rng = np.random.default_rng(rows + V)
+    z = rng.normal(0, 2.0, (rows, V))
+    z[np.arange(rows), rng.integers(0, V, rows)] = rng.uniform(14.0, 25.0, rows)  # the only largest one, in bf16 too
+    z = SC.values(z, dtype)
+    (ids, _, among, kept), status = run(R, z, dtype, [settings] * rows, rng.random(rows))
+    assert status == 0
+    assert (kept == 1).all() and (ids == z.argmax(1)).all()
+    assert (among == 0.0).all(), among[among != 0.0][:8]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_no_share_is_above_the_whole(R, dtype):
+    """Two tokens, the smaller down to a 2^-30 of the larger: the logarithm of the larger one's share is never positive."""
+    rows = 512
+    rng = np.random.default_rng(5)
+    z = np.full((rows, 700), -40.0)
+    z[:, 3] = rng.uniform(1.0, 20.0, rows)
+    z = SC.values(z, dtype)
+    z[:, 600] = SC.values(z[:, 3] - rng.uniform(5.0, 21.0, rows), dtype)
+    (ids, _, among, kept), status = run(R, z, dtype, [(1.0, 2, 1.0, 0.0)] * rows, np.zeros(rows))
+    assert status == 0 and (kept == 2).all() and (ids == 3).all()
+    assert (among <= 0.0).all(), among[among > 0.0][:8]
