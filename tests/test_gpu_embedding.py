@@ -110,6 +110,42 @@ def test_backward_widths_and_strides(R, D):
             check_grad(R, ids, 60, D, dtype, (D, dtype, pad, off), pad=pad, off=off)
 
 
+@pytest.mark.parametrize("T,D", [(1025, 1024), (3000, 129), (3000, 513), (3000, 1024), (3000, 4096), (3000, 5000), (9001, 1001),
+                                 (9001, 2048), (70001, 129), (70001, 520), (180300, 136)])
+@pytest.mark.parametrize("law", ["same", "two", "often", "any"])
+def test_backward_of_sorted_tokens_over_many_columns(R, law, T, D):
+    """Rows that several CTAs share, whose runs of equal ids are cut at the chunks' borders: the parts and the list of the long
+    runs are of all columns. The reference is summed in float64 on the GPU; every tenth id is out of range."""
+    V = 60
+    ids = ids_on_device(token_ids(law, T, V, seed=T + D))
+    ids[5::10] = torch.where(torch.arange(len(ids[5::10]), device="cuda") % 2 == 0, -1, V).int()
+    ok = (ids >= 0) & (ids < V)
+    g = torch.Generator(device="cuda").manual_seed(D)
+    ws = R.new_embedding_workspace(T, V, D)
+    for dtype in (BF, F32):
+        values = (torch.randn(T, D, generator=g, device="cuda") * 1e-2).to(dtype)
+        before = torch.randn(V, D, generator=g, device="cuda")
+        # the formula, and the sum of the terms' sizes
+        ref, size = torch.zeros(2, V, D, dtype=torch.float64, device="cuda")
+        terms = values[ok].double() * float(np.float32(0.9))
+        ref.index_add_(0, ids[ok].long(), terms)
+        size.index_add_(0, ids[ok].long(), terms.abs())
+        del terms
+        n = torch.bincount(ids[ok].long(), minlength=V)[:, None]
+        tol = (n + 2) * U * size + U * (before.double().abs() + ref.abs())
+        for pad, off in ((0, 0), (8, 0), (3, 0), (5, 1)):
+            buf = torch.full((T * (D + pad) + off,), float("nan"), dtype=dtype, device="cuda")
+            d = buf[off:].view(T, D + pad)[:, :D]
+            d.copy_(values)
+            d[~ok] = float("nan")  # not read
+            dw = before.clone()
+            R.rl_embedding_bwd(ids, d, dw, ws, scale=0.9)
+            err = (dw.double() - before.double() - ref).abs()
+            assert bool((err <= tol * (1 + 1e-3)).all()), (law, T, D, dtype, pad, off, float((err / tol.clamp(min=1e-300)).max()))
+            assert torch.equal(dw[n[:, 0] == 0], before[n[:, 0] == 0])
+    assert R.rl_query_status(ws)[1] == R.RL_DEV_BAD_TOKEN
+
+
 def test_ids_out_of_range(R):
     V, D = 50, 64
     for T in (20, 3000):
