@@ -729,9 +729,10 @@ typedef struct rl_sample_params {
  *
  * A row without a finite largest entry, or with a NaN, and one whose settings or number are outside the ranges above,
  * gets token -1, NaN log-probabilities and n_kept 0 and sets RL_DEV_BAD_VALUE. Masses are sums of fp32 exponentials:
- * where top_p ends, and which token u selects, is that of exact sums but for borders within 1e-6 of the mass; an entry's
- * own exponential is relative 2^-22 and what the rounding of z / T makes of it. A row's results do not depend on what
- * the other rows hold; the number of rows decides how many CTAs share one, and with it the last bits of its sums.
+ * where top_p ends, and which token u selects, is that of exact sums but for borders within (48 + min(V / 4096, 256)) 2^-24
+ * + V 2^-39 of the mass (5.4e-6 at 151,936 entries, 4.9e-5 at 2^24); an entry's own exponential is relative 2^-22 and
+ * what the rounding of z / T makes of it. A row's results do not depend on what the other rows hold; the number of rows
+ * decides how many CTAs share one, and with it the last bits of its sums.
  */
 rl_status rl_sample_tokens(const void* logits, rl_dtype dtype, int64_t rows, int64_t V, int64_t ld, const float* sample_u,
                            const rl_sample_params* params, const float* row_temperature, const int32_t* row_top_k,

@@ -13,7 +13,7 @@
 //      are counted in the first pass already, on the guess that the largest entry and the border are among them. Where
 //      they are not, and for fp32 rows, more passes count by the distance of the ordered bit patterns from the largest
 //      entry's, in steps of 2^16 patterns, then down to single ones within the bin that holds the border; masses are then
-//      added up as integers of 2^-36. Integer sums: any order gives the same bits. min-p is a value, found by bisection.
+//      added up as integers of 2^-38. Integer sums: any order gives the same bits. min-p is a value, found by bisection.
 //   3. a pass sums the kept weights of every tile and counts the entries equal to the threshold; a second exchange; the tile
 //      that holds the token is found by a scan, and the token in it by another.
 // HBM is read once: the rows at work at a time fit in L2, where the later passes find them, and tiles whose largest entry is
@@ -92,7 +92,9 @@ __device__ __forceinline__ uint32_t entry_key(uint32_t key) {
   return (key & 0xffffu) == 0xffffu ? key : (key & 0xffff0000u) - 1u;
 }
 
-constexpr float kMassUnit = 68719476736.f;  // 2^36
+// Masses are integers of 2^-38 of the largest entry's weight: the sum of 2^24 of them stays below 2^63, and the roundings of V
+// entries come to V 2^-39 of it at most, whichever way they go (2^-36 put the border of long flat tails elsewhere: 1.2e-4 at 2^24).
+constexpr float kMassUnit = 274877906944.f;
 // The logarithm of a token's share of the kept mass, x being its exponent. A token that has all of it, or all but what rounding
 // takes, has a share of 1: x is not 0 for the largest entry (a fused operation's remainder), and log2 of a rounded 2^x is not x.
 // (By the others' mass, log1p, it is no more exact: half a step of the sum, 2^-24 of it, is what is left; 128 rows 34.4 us

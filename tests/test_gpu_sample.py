@@ -283,3 +283,33 @@ def test_no_share_is_above_the_whole(R, dtype):
     (ids, _, among, kept), status = run(R, z, dtype, [(1.0, 2, 1.0, 0.0)] * rows, np.zeros(rows))
     assert status == 0 and (kept == 2).all() and (ids == 3).all()
     assert (among <= 0.0).all(), among[among > 0.0][:8]
+
+
+def where_top_p_may_end(V):
+    """How far from top_p, as a share of the mass, the border may come out: a thread adds up at most min(V / 4096, 256) tiles of
+    a row, 8 entries on a way within one, and 20 sums of others, each of them rounded; an exponential is relative 2^-22 here and in
+    the row's normaliser, and its mass is rounded to 2^-38."""
+    return (48 + min(V / 4096, 256)) * U + V * 2.0 ** -39
+
+
+@pytest.mark.parametrize("V,dtype,low,top_k", [
+    (1 << 24, "bf16", -9.6875, 0), (1 << 24, "bf16", -9.0, 0), (1 << 24, "bf16", -9.6875, 1 << 23), (1 << 24, "bf16", 16.0, 0),
+    (1 << 23, "f32", -9.7, 0), (1 << 23, "f32", -9.7, 6000000), (1 << 23, "f32", 16.0, 0), (1 << 20, "f32", -2.0, 0)])
+@pytest.mark.parametrize("rows", [1, 3])
+def test_where_top_p_ends_in_a_long_flat_tail(R, V, dtype, low, top_k, rows):
+    """One entry and millions of equal ones, each of them down to 2^-37 of its mass: half of what they have together is kept
+    (and not all of it, as where their masses come out as nothing)."""
+    z = torch.full((rows, V), low, dtype=DT[dtype], device="cuda")
+    z[:, V // 3] = 16.0
+    w = float(np.exp(low - 16.0))
+    of_k = top_k - 1 if top_k else V - 1
+    total = 1.0 + of_k * w
+    top_p = float(np.float32((1.0 + 0.5 * of_k * w) / total))
+    kept = torch.empty(rows, dtype=torch.int32, device="cuda")
+    ws = R.new_workspace(0, 0)
+    R.rl_sample_tokens(z, column(np.full(rows, 0.5), torch.float32), R.make_sample_params(1.0, top_k, top_p, 0.0), ws, n_kept=kept)
+    assert R.rl_query_status(ws)[1] == 0
+    for n in kept.cpu().numpy().astype(np.float64):
+        before, upto = (1.0 + (n - 2) * w) / total, (1.0 + (n - 1) * w) / total
+        tol = where_top_p_may_end(V)
+        assert before < top_p + tol and upto >= top_p - tol, (n, (upto - top_p) / U)
