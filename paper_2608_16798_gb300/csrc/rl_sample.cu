@@ -95,12 +95,17 @@ __device__ __forceinline__ uint32_t entry_key(uint32_t key) {
 // Masses are integers of 2^-38 of the largest entry's weight: the sum of 2^24 of them stays below 2^63, and the roundings of V
 // entries come to V 2^-39 of it at most, whichever way they go (2^-36 put the border of long flat tails elsewhere: 1.2e-4 at 2^24).
 constexpr float kMassUnit = 274877906944.f;
-// The logarithm of a token's share of the kept mass, x being its exponent. A token that has all of it, or all but what rounding
-// takes, has a share of 1: x is not 0 for the largest entry (a fused operation's remainder), and log2 of a rounded 2^x is not x.
-// (By the others' mass, log1p, it is no more exact: half a step of the sum, 2^-24 of it, is what is left; 128 rows 34.4 us
-// against 32.8.)
-__device__ __forceinline__ float log_share(float x, float total) {
-  return ex2(x) >= total ? 0.f : fminf((x - log2f(total)) * kLn2, 0.f);
+// The logarithm of a token's share of the kept mass, x being its exponent and `others` the sum of the other kept weights, which has
+// never been added to its own: a share close to 1 is then as exact as the small weights are. (From the total, whose half step is
+// 2^-24 of it, the logarithm of a share of 1 - 2^-10 was relative 6e-5.) log(1 + r) = 2 artanh(r / (2 + r)), by its power series.
+__device__ __forceinline__ float log_share(float x, float others, float total) {
+  const float w = ex2(x);
+  if (!(others < w)) return (x - log2f(total)) * kLn2;
+  const float t = __fdividef(others, others + 2.f * w), y = t * t;  // up to 1/3: the first term left out is 2^-26 of the sum
+  float s = 1.f / 13.f;
+#pragma unroll
+  for (int k = 11; k > 0; k -= 2) s = fmaf(s, y, 1.f / k);
+  return 0.f - 2.f * t * s;
 }
 __device__ __forceinline__ unsigned long long mass_of(float w) { return __float2ull_rn(w * kMassUnit); }
 
@@ -558,13 +563,18 @@ struct Row {
       }
     }
     __syncthreads();
-    if (threadIdx.x == 0) {
+    if (warp == 0) {
       const int at = sh.first < kSort ? sh.first : sh.last;
       const int token = min(max(static_cast<int>(sh.list[at] >> 32) - row.lo, 0), p.V - 1);
       const float zx = Elem<T>::one(z_row[token]);
+      float others = 0.f;  // while the token's entry is on its way
+      if (p.among)
+        for (int i = lane; i < kept; i += 32) others += i != at ? __uint_as_float(static_cast<uint32_t>(sh.list[i])) : 0.f;
+      others = warp_sum(others);
+      if (lane != 0) return true;
       p.ids[out] = token;
       p.logp[out] = logp_of(zx, all, c);
-      if (p.among) p.among[out] = log_share(exponent(zx, all.m, c), total);
+      if (p.among) p.among[out] = log_share(exponent(zx, all.m, c), others, total);
       if (p.n_kept) p.n_kept[out] = kept;
     }
     return true;
@@ -661,9 +671,15 @@ __device__ __forceinline__ uint32_t least_key(uint32_t top, float least, X expon
   return widen(hi);
 }
 
-// As pick, but with the goal itself: the place among n weights w(k) at which their running sum passes `goal`.
+// As pick, but with the goal itself: the place among n weights w(k) at which their running sum passes `goal`; whether it does
+// (rounding may leave it short); and the sum of the lane's other weights.
+struct Picked {
+  int at;
+  float left, others;
+  bool passed;
+};
 template <typename W>
-__device__ __forceinline__ int pick_at(int n, float goal, int lane, W w, float& left) {
+__device__ __forceinline__ Picked pick_at(int n, float goal, int lane, W w) {
   const int M = (n + 31) / 32, k0 = min(lane * M, n), k1 = min(k0 + M, n);
   float sum = 0.f;
   for (int k = k0; k < k1; ++k) sum += w(k);
@@ -673,24 +689,27 @@ __device__ __forceinline__ int pick_at(int n, float goal, int lane, W w, float& 
     const float up = __shfl_up_sync(0xffffffffu, run, o);
     if (lane >= o) run += up;
   }
-  float before = run - sum, rest = 0.f, last_rest = 0.f;
+  float before = run - sum, rest = 0.f, last_rest = 0.f, others = 0.f;
   int at = -1, last = -1;
   for (int k = k0; k < k1; ++k) {
     const float mine = w(k);
+    bool here = false;
     if (mine > 0.f) {
       last = k;
       last_rest = goal - before;
-      if (at < 0 && before + mine > goal) {
+      here = at < 0 && before + mine > goal;
+      if (here) {
         at = k;
         rest = last_rest;
       }
     }
+    others += here ? 0.f : mine;
     before += mine;
   }
   const uint32_t found = __ballot_sync(0xffffffffu, at >= 0), any = __ballot_sync(0xffffffffu, last >= 0);
   const int from = found ? __ffs(found) - 1 : any ? 31 - __clz(any) : 0;
-  left = __shfl_sync(0xffffffffu, found ? rest : last_rest, from);
-  return max(0, __shfl_sync(0xffffffffu, found ? at : last, from));
+  return {max(0, __shfl_sync(0xffffffffu, found ? at : last, from)), __shfl_sync(0xffffffffu, found ? rest : last_rest, from),
+          lane == from ? others : sum, found != 0};
 }
 
 // What a pass over the row keeps: entries above (GE: and at) zt.
@@ -1066,9 +1085,8 @@ __global__ void __launch_bounds__(WARPS * 32, 1024 / (WARPS * 32)) sample_kernel
   const uint32_t before = upto - part.equal, mine_ties = before >= ties ? 0u : min(ties - before, part.equal);
   const float mine = fmaf(static_cast<float>(mine_ties), wt, part.sum);
   const float total = warp_sum(mine);
-  float left;
-  const int at_cta = pick_at(C, set.u * total, lane, [&](int) { return mine; }, left);  // a lane has one
-  if (at_cta != rank) return;
+  const Picked cta = pick_at(C, set.u * total, lane, [&](int) { return mine; });  // a lane has one
+  if (cta.at != rank) return;
   // (not under the condition that its result is wanted: built so, a number that was known came out as this one)
   const uint32_t counted = __reduce_add_sync(0xffffffffu, part.above);
   const uint32_t ties_before = __shfl_sync(0xffffffffu, before, rank);
@@ -1090,18 +1108,20 @@ __global__ void __launch_bounds__(WARPS * 32, 1024 / (WARPS * 32)) sample_kernel
     for (int i = k0; i < k; ++i) b += tiles[i].kept.equal;
     return b;
   };
-  const int at = pick_at(nt, left, lane, [&](int k) {
+  const Picked tile = pick_at(nt, cta.left, lane, [&](int k) {
     if (!filtered) return tiles[k].fold.s == 0.f ? 0.f : tiles[k].fold.s * power(tiles[k].fold.m, all.m, c);
     if (!ties) return tiles[k].kept.sum;
     const uint32_t b = ties_until(k);
     return fmaf(b >= ties ? 0.f : static_cast<float>(min(ties - b, tiles[k].kept.equal)), wt, tiles[k].kept.sum);
-  }, left);
+  });
+  const int at = tile.at;
+  const float left = tile.left;
   uint32_t used = ties ? __shfl_sync(0xffffffffu, at >= k0 && at < k1 ? ties_until(at) : 0u, at / M) : 0u;
 
   // ---- and the token in it: the weights in order, ties by their rank
   row.tile(t0 + at, lane, q);
   int token = -1, last = -1;
-  float acc0 = 0.f;
+  float acc0 = 0.f, others = cta.others + tile.others;  // the lane's part of what is kept beside the token
 #pragma unroll
   for (int i = 0; i < kTileBlocks; ++i) {
     float v[N], w[N], s = 0.f;
@@ -1139,25 +1159,35 @@ __global__ void __launch_bounds__(WARPS * 32, 1024 / (WARPS * 32)) sample_kernel
     const uint32_t hit = __ballot_sync(0xffffffffu, token < 0 && s > 0.f && acc0 + run_s > left);
     if (hit) {
       const int from = __ffs(hit) - 1;
-      float acc = acc0 + (run_s - s);
+      float acc = acc0 + (run_s - s), beside = 0.f;
       int here = -1;
 #pragma unroll
       for (int e = 0; e < N; ++e) {
         acc += w[e];
         if (here < 0 && w[e] > 0.f && acc > left) here = ((t0 + at) * kTileBlocks32 + 32 * i + lane) * N + e;
       }
-      token = __shfl_sync(0xffffffffu, here >= 0 ? here : last, from);
+      if (here < 0) here = last;
+#pragma unroll
+      for (int e = 0; e < N; ++e) beside += here == ((t0 + at) * kTileBlocks32 + 32 * i + lane) * N + e ? 0.f : w[e];
+      token = __shfl_sync(0xffffffffu, here, from);
+      s = lane == from ? beside : s;
     }
+    others += s;
     acc0 += __shfl_sync(0xffffffffu, run_s, 31);
   }
   // where rounding leaves the sum short of its goal: the last that has any weight
+  const bool passed = cta.passed && tile.passed && token >= 0;
   if (token < 0) token = static_cast<int>(__reduce_max_sync(0xffffffffu, last));
-  if (lane != 0) return;
   token = min(max(token - row.lo, 0), p.V - 1);
   const float zx = Elem<T>::one(z[token]);
+  others = warp_sum(others);
+  if (lane != 0) return;
   p.ids[r] = token;
   p.logp[r] = logp_of(zx, all, c);
-  if (p.among) p.among[r] = log_share(exponent(zx, all.m, c), total);
+  if (p.among) {
+    const float x = exponent(zx, all.m, c);
+    p.among[r] = log_share(x, passed ? others : fmaxf(total - ex2(x), 0.f), total);
+  }
   if (p.n_kept) p.n_kept[r] = static_cast<int32_t>(known_kept ? kept : counted);
 }
 

@@ -313,3 +313,32 @@ def test_where_top_p_ends_in_a_long_flat_tail(R, V, dtype, low, top_k, rows):
         before, upto = (1.0 + (n - 2) * w) / total, (1.0 + (n - 1) * w) / total
         tol = where_top_p_may_end(V)
         assert before < top_p + tol and upto >= top_p - tol, (n, (upto - top_p) / U)
+
+@pytest.mark.parametrize("rows,V", [(1, 700), (1, 151936), (61, 32003), (300, 4001), (600, 20000), (1833, 1472)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("settings", [(1.0, 6, 1.0, 0.0), (0.7, 6, 0.9999999, 0.0), (1.0, 0, 1.0, 1e-16), (1.0, 0, 1.0, 0.0)])
+def test_a_share_close_to_the_whole(R, settings, dtype, rows, V):
+    """The largest entry and five others 4 to 30 below it: the logarithm of its share is as exact, relative, as the others'
+    weights. An exponent (z - max) c has c's two roundings and its own, 2.5 2^-24 of its size in all; the two exponentials are
+    relative 2^-22, five weights are added up, and the quotient (two units, and its divisor's rounding), the series and the
+    result are 10 roundings."""
+    rng = np.random.default_rng(rows + V)
+    z = np.full((rows, V), -np.inf)
+    at = np.argsort(rng.random((rows, V)), axis=1)[:, :6] if V < 2000 else rng.integers(0, V // 6, (rows, 6)) + np.arange(6) * (V // 6)
+    r = np.arange(rows)
+    z[r, at[:, 0]] = rng.uniform(14.0, 25.0, rows)
+    for i in range(1, 6):
+        z[r, at[:, i]] = z[r, at[:, 0]] - rng.uniform(4.0, 30.0, rows) * settings[0]
+    z = SC.values(z, dtype)
+    (ids, _, among, kept), status = run(R, z, dtype, [settings] * rows, np.full(rows, 0.5))
+    assert status == 0 and (ids == at[:, 0]).all()
+    T = float(np.float32(settings[0]))
+    for k in range(rows):
+        p, left = O.kept_tokens(z[k], T, 6)
+        if settings[2] == 1.0 and settings[3] == 0.0:
+            assert kept[k] == 6
+        order = left[np.argsort(-z[k][left], kind="stable")][: kept[k]]
+        x = (z[k][order[1:]] - z[k][order[0]]) / T
+        ref = -np.log1p(np.exp(x).sum())
+        tol = (2.5 * np.abs(x).max(initial=0.0) + 8 + 5 + 10) * U
+        assert abs(among[k] - ref) <= tol * abs(ref), (k, among[k], ref, (among[k] / ref - 1) / U)
