@@ -71,7 +71,7 @@ struct Settings {
   float T, top_p, min_p, u;
   int32_t top_k;
   __device__ __forceinline__ bool ok() const {
-    return (T == 0.f || (T >= 1e-4f && T < 3e38f)) && top_k >= 0 && top_p > 0.f && top_p <= 1.f && min_p >= 0.f &&
+    return (T == 0.f || (T >= 1e-4f && T < __int_as_float(0x7f800000))) && top_k >= 0 && top_p > 0.f && top_p <= 1.f && min_p >= 0.f &&
            min_p <= 1.f && u >= 0.f && u < 1.f;
   }
 };

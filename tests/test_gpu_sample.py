@@ -342,3 +342,19 @@ def test_a_share_close_to_the_whole(R, settings, dtype, rows, V):
         ref = -np.log1p(np.exp(x).sum())
         tol = (2.5 * np.abs(x).max(initial=0.0) + 8 + 5 + 10) * U
         assert abs(among[k] - ref) <= tol * abs(ref), (k, among[k], ref, (among[k] / ref - 1) / U)
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_the_largest_temperatures(R, dtype):
+    """Every finite temperature is one that the header allows; these make all entries equally likely."""
+    V = 1000
+    rng = np.random.default_rng(1)
+    u = (np.arange(V) + 0.5) / V
+    z = np.tile(SC.rows("normal", 1, V, dtype, rng), (V, 1))
+    largest = float(np.finfo(np.float32).max)
+    for T in (2.9e38, 3e38, 3.3e38, largest):
+        (ids, logp, among, kept), status = run(R, z, dtype, [(T, 0, 1.0, 0.0)] * V, u)
+        assert status == 0 and (ids == np.arange(V)).all() and (kept == V).all()
+        assert (np.abs(logp + np.log(V)) <= 100 * U).all() and (np.abs(among + np.log(V)) <= 100 * U).all()
+        ws = R.new_workspace(0, 0)
+        once, _ = R.rl_sample_tokens(on_device(z, dtype), column(u, torch.float32), R.make_sample_params(T), ws)
+        assert (once.cpu().numpy() == np.arange(V)).all() and R.rl_query_status(ws)[1] == 0
