@@ -1087,7 +1087,9 @@ __global__ void __launch_bounds__(WARPS * 32, 1024 / (WARPS * 32)) sample_kernel
   const float total = warp_sum(mine);
   const Picked cta = pick_at(C, set.u * total, lane, [&](int) { return mine; });  // a lane has one
   if (cta.at != rank) return;
-  // (not under the condition that its result is wanted: built so, a number that was known came out as this one)
+  // Not under the condition that the number is wanted. Built so (nvcc 13.0.88), every number came out as 0, known ones too,
+  // though the condition is the same in all lanes: with a ballot of it in the code, or with the sum taken by shuffles,
+  // the results are right. No kernel smaller than this one shows it. (Intrinsic and redux.sync alike, so what follows the PTX.)
   const uint32_t counted = __reduce_add_sync(0xffffffffu, part.above);
   const uint32_t ties_before = __shfl_sync(0xffffffffu, before, rank);
 
@@ -1177,7 +1179,11 @@ __global__ void __launch_bounds__(WARPS * 32, 1024 / (WARPS * 32)) sample_kernel
   }
   // where rounding leaves the sum short of its goal: the last that has any weight
   const bool passed = cta.passed && tile.passed && token >= 0;
-  if (token < 0) token = static_cast<int>(__reduce_max_sync(0xffffffffu, last));
+  if (token < 0) {  // (by shuffles: as above)
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) last = max(last, __shfl_xor_sync(0xffffffffu, last, o));
+    token = last;
+  }
   token = min(max(token - row.lo, 0), p.V - 1);
   const float zx = Elem<T>::one(z[token]);
   others = warp_sum(others);

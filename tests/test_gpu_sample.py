@@ -358,3 +358,33 @@ def test_the_largest_temperatures(R, dtype):
         ws = R.new_workspace(0, 0)
         once, _ = R.rl_sample_tokens(on_device(z, dtype), column(u, torch.float32), R.make_sample_params(T), ws)
         assert (once.cpu().numpy() == np.arange(V)).all() and R.rl_query_status(ws)[1] == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_the_largest_number_takes_the_last_of_the_mass(R, dtype):
+    """sample_u = 1 - 2^-24: where the rounded goal is not passed, the last kept token of any weight is taken; the mass behind
+    it stays within the bound of the header (the sums' error)."""
+    last = 1 - 2.0 ** -24
+    for V, n in ((100, 300), (5000, 300), (40000, 60)):
+        rng = np.random.default_rng(V)
+        z = rng.normal(0, 2.0, (n, V))
+        z[:, V // 2:] -= 3.0
+        z = SC.values(z, dtype)
+        order = np.argsort(-z, axis=1, kind="stable")
+        for T, k, p, m in SETTINGS:
+            T = float(np.float32(T))
+            (ids, _, among, kept), status = run(R, z, dtype, [(T, k, p, m)] * n, np.full(n, last))
+            assert status == 0
+            for r in range(n):
+                if T == 0:
+                    assert ids[r] == z[r].argmax() and among[r] == 0
+                    continue
+                left = np.sort(order[r][: kept[r]])
+                w = np.exp((z[r][left] - z[r].max()) / T)
+                at = np.nonzero(left == ids[r])[0]
+                assert len(at) == 1, (V, T, k, p, m, r)
+                share = w / w.sum()
+                behind = share[at[0] + 1:].sum()
+                assert behind <= (48 + V / 4096) * U + 2.0 ** -24, (V, T, k, p, m, r, behind)
+                tol = logp_tolerance(z[r], T, V)
+                assert abs(among[r] - np.log(share[at[0]])) <= tol + 2 * U * abs(among[r]), (V, T, k, p, m, r)
