@@ -36,6 +36,10 @@ struct Block<uint16_t, 8> {
     v[0] = bf16_lo(w.x), v[1] = bf16_hi(w.x), v[2] = bf16_lo(w.y), v[3] = bf16_hi(w.y);
     v[4] = bf16_lo(w.z), v[5] = bf16_hi(w.z), v[6] = bf16_lo(w.w), v[7] = bf16_hi(w.w);
   }
+  __device__ __forceinline__ void put(int e, uint16_t x) {  // into a cleared block
+    uint32_t& word = e < 4 ? (e < 2 ? w.x : w.y) : (e < 6 ? w.z : w.w);
+    word |= static_cast<uint32_t>(x) << (e & 1) * 16;
+  }
 };
 template <>
 struct Block<float, 4> {
@@ -43,12 +47,14 @@ struct Block<float, 4> {
   __device__ __forceinline__ void load(const float* p) { w = __ldcs(reinterpret_cast<const float4*>(p)); }
   __device__ __forceinline__ void clear() { w = make_float4(0.f, 0.f, 0.f, 0.f); }
   __device__ __forceinline__ void get(float (&v)[4]) const { v[0] = w.x, v[1] = w.y, v[2] = w.z, v[3] = w.w; }
+  __device__ __forceinline__ void put(int e, float x) { (e < 2 ? (e == 0 ? w.x : w.y) : (e == 2 ? w.z : w.w)) = x; }
 };
 template <>
 struct Block<uint16_t, 1> {
   uint16_t w;
   __device__ __forceinline__ void load(const uint16_t* p) { w = __ldcs(p); }
   __device__ __forceinline__ void clear() { w = 0; }
+  __device__ __forceinline__ void put(int, uint16_t x) { w = x; }
   __device__ __forceinline__ void get(float (&v)[1]) const { v[0] = bf16_to_f32(w); }
 };
 template <>
@@ -56,6 +62,7 @@ struct Block<float, 1> {
   float w;
   __device__ __forceinline__ void load(const float* p) { w = __ldcs(p); }
   __device__ __forceinline__ void clear() { w = 0.f; }
+  __device__ __forceinline__ void put(int, float x) { w = x; }
   __device__ __forceinline__ void get(float (&v)[1]) const { v[0] = w; }
 };
 
@@ -450,10 +457,9 @@ __device__ __forceinline__ void load_columns(Block<T, N>& b, const T* row, int64
     b.load(row + c);
   } else {
     b.clear();
-    T* w = reinterpret_cast<T*>(&b.w);
 #pragma unroll
     for (int e = 0; e < N; ++e)
-      if (c + e < D) w[e] = row[c + e];
+      if (c + e < D) b.put(e, row[c + e]);
   }
 }
 

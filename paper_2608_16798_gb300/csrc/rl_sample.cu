@@ -135,6 +135,13 @@ __device__ __forceinline__ uint32_t equal2(uint32_t a, uint32_t b) {
   return r;
 }
 
+// Element i of a block's words.
+template <typename T>
+__device__ __forceinline__ void put_element(uint32_t (&w)[4], int i, T x) {
+  if (sizeof(T) == 4) w[i] = Elem<T>::bits(x);
+  else w[i / 2] = i & 1 ? (w[i / 2] & 0xffffu) | Elem<T>::bits(x) << 16 : (w[i / 2] & 0xffff0000u) | Elem<T>::bits(x);
+}
+
 // A row as the 16-byte blocks of memory that it covers.
 template <typename T>
 struct RowBlocks {
@@ -153,13 +160,13 @@ struct RowBlocks {
   // Block k; elements of other rows, and blocks behind the last, are minus infinity.
   __device__ __forceinline__ uint4 block(int k) const {
     if (k > 0 && k < nb - 1) return __ldcg(reinterpret_cast<const uint4*>(at + static_cast<int64_t>(k) * N));
-    uint4 q = make_uint4(kNone, kNone, kNone, kNone);
-    if (k < 0 || k >= nb) return q;
-    T* e = reinterpret_cast<T*>(&q);
+    uint32_t w[4] = {kNone, kNone, kNone, kNone};
+    if (k >= 0 && k < nb) {
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (k * N + i >= lo && k * N + i < hi) e[i] = at[k * N + i];
-    return q;
+      for (int i = 0; i < N; ++i)
+        if (k * N + i >= lo && k * N + i < hi) put_element<T>(w, i, at[k * N + i]);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
   }
   // A lane's blocks of tile t.
   __device__ __forceinline__ void tile(int t, int lane, uint4 (&w)[kTileBlocks]) const {
@@ -175,7 +182,7 @@ struct RowBlocks {
   }
 };
 
-// A barrier of all CTAs of a row, and a word of shared memory of one of them.
+// A barrier of all CTAs of a row, and two words of shared memory of one of them.
 template <bool CLUSTER>
 __device__ __forceinline__ void sync_all() {
   if (CLUSTER) cluster_sync_all();
@@ -184,7 +191,9 @@ __device__ __forceinline__ void sync_all() {
 template <bool CLUSTER>
 __device__ __forceinline__ unsigned long long of_cta(const uint32_t* two, int r) {
   if (CLUSTER) return ld_cluster_u64(map_to_rank(smem_addr(two), r));
-  return *reinterpret_cast<const unsigned long long*>(two);
+  unsigned long long v;
+  asm volatile("ld.shared.u64 %0, [%1];" : "=l"(v) : "r"(smem_addr(two)) : "memory");
+  return v;
 }
 
 // A border: entries above `key` and the first m of those equal to it; their number above it and their mass.
