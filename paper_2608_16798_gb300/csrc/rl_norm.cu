@@ -560,7 +560,19 @@ __device__ __forceinline__ void copy(const Span& s, uint8_t* to, uint64_t* bar) 
     bulk_g2s(to + (s.from - s.at), reinterpret_cast<const void*>(s.from), static_cast<uint32_t>(s.to - s.from), bar);
 }
 
-// A thread's elements of a row in its stage; those behind D are not the row's. `edge`: the matrix' first or last row, whose
+// After a wait at `stage` in phase `parity` that ran out: waits, a little each, for the copies that may be on their way still, so that
+// none of them arrives in the shared memory of the CTA's successor. By the thread that started them, which has started none since.
+__device__ __noinline__ void await_copies(uint64_t* full, int n, int stage, uint32_t parity) {
+  for (int i = 0; i < n; ++i) {
+    mbar_wait_bounded(&full[stage], parity, 10000000ull);
+    if (++stage == n) {
+      stage = 0;
+      parity ^= 1;
+    }
+  }
+}
+
+// A thread's elements of a row in its stage; those behind D are not the row's. `first`, `last`: of the matrix' rows, whose
 // outermost elements may not have been copied.
 template <int NG, bool WHOLE, typename T>
 __device__ __forceinline__ void get_row(float2 (&v)[NG][2], const uint8_t* stage, const T* row, bool first, bool last, int D, int n,
@@ -626,18 +638,17 @@ __global__ void __launch_bounds__(kMostWarps * 32) fwd_ring_kernel(const FwdArgs
   float2 g[NG][2], b[NG][2];
   get_parameters<NG, WHOLE>(g, p.w, 0.f, D, n, t);
   get_parameters<NG, WHOLE>(b, p.b, 0.f, D, n, t);
-  int stage = 0;
+  int stage = 0, late = -1;  // late: 2 stage + parity of the wait that ran out
   uint32_t parity = 0;
-  bool in_time = true;
   for (int64_t r = blockIdx.x; r < p.rows; r += G) {
-    in_time = in_time && mbar_wait_bounded(&full[stage], parity);
+    if (late < 0 && !mbar_wait_bounded(&full[stage], parity)) late = 2 * stage + parity;  // reported, and not tried again
     float2 v[NG][2];
     get_row<NG, WHOLE>(v, smem + static_cast<size_t>(stage) * st.bytes, x + r * p.ld_x, r == 0, r == p.rows - 1, D, n, t);
+    if (late >= 0) v[0][0].x = __int_as_float(0x7fc00000);  // there is no status word: a row of NaNs says that a wait ran out
     float mean, rstd;
     statistics<NG, WHOLE>(v, D, inv, p.eps, W, warp, n, t, red[0], red[1], mean, rstd);
-    if (!in_time) mean = rstd = __int_as_float(0x7fc00000);  // there is no status word: NaNs say that a wait ran out
     if (W == 1) __syncwarp();
-    if (t == 0 && r + st.n * G < p.rows) fetch(r + st.n * G, stage);  // the sums' barriers: everyone has read the stage
+    if (t == 0 && late < 0 && r + st.n * G < p.rows) fetch(r + st.n * G, stage);  // the sums' barriers: everyone has read the stage
     if (++stage == st.n) {
       stage = 0;
       parity ^= 1;
@@ -652,6 +663,7 @@ __global__ void __launch_bounds__(kMostWarps * 32) fwd_ring_kernel(const FwdArgs
       p.rstd[r] = rstd;
     }
   }
+  if (t == 0 && late >= 0) await_copies(full, st.n, late / 2, late & 1);
 }
 
 // The same for the gradient: x and dy of the rows that have one come through the ring. A thread keeps the same columns for
@@ -678,7 +690,7 @@ __global__ void __launch_bounds__(kMostWarps * 32) bwd_kernel(const BwdArgs p, c
   // the first warp fetches ahead: the rows that have a gradient, in order
   int64_t ahead_base = 0;
   uint32_t ahead = warp == 0 ? live_rows(0) : 0u;
-  auto fetch_next = [&](int stage) {
+  auto fetch_next = [&](int stage, bool in_time) {
     while (ahead == 0) {
       if (ahead_base + kRowInfo >= mine) return false;
       ahead_base += kRowInfo;
@@ -686,7 +698,7 @@ __global__ void __launch_bounds__(kMostWarps * 32) bwd_kernel(const BwdArgs p, c
     }
     const int64_t r = b0 + (ahead_base + __ffs(ahead) - 1) * G;
     ahead &= ahead - 1;
-    if (lane == 0) {
+    if (lane == 0 && in_time) {
       const bool first = r == 0, last = r == p.rows - 1;
       const Span sx = span(static_cast<const TX*>(p.x) + r * p.ld_x, D * sizeof(TX), first, last);
       const Span sd = span(static_cast<const TD*>(p.dy) + r * p.ld_dy, D * sizeof(TD), first, last);
@@ -699,7 +711,7 @@ __global__ void __launch_bounds__(kMostWarps * 32) bwd_kernel(const BwdArgs p, c
     return true;
   };
   if (warp == 0)
-    for (int i = 0; i < st.n && fetch_next(i); ++i) {}
+    for (int i = 0; i < st.n && fetch_next(i, true); ++i) {}
 
   float2 wt[NG][2], dw[NG][2], db[NG][2];
   get_parameters<NG, WHOLE>(wt, p.w, 0.f, D, n, t);
@@ -709,9 +721,8 @@ __global__ void __launch_bounds__(kMostWarps * 32) bwd_kernel(const BwdArgs p, c
     for (int e = 0; e < 2; ++e) dw[j][e] = db[j][e] = make_float2(0.f, 0.f);
   const bool full_width = D == 4 * NG * n;
 
-  int stage = 0;
+  int stage = 0, late = -1;  // late: 2 stage + parity of the wait that ran out
   uint32_t parity = 0, odd = 0;
-  bool in_time = true;
   int64_t r = b0;
   for (int64_t base = 0; base < mine; base += kRowInfo) {
     const uint32_t live = live_rows(base);
@@ -731,8 +742,7 @@ __global__ void __launch_bounds__(kMostWarps * 32) bwd_kernel(const BwdArgs p, c
         continue;
       }
       const float mean = __shfl_sync(0xffffffffu, mean_l, i), rstd = __shfl_sync(0xffffffffu, rstd_l, i);
-      // a wait that ran out is reported and not tried again
-      in_time = in_time && mbar_wait_bounded(&full[stage], parity);
+      if (late < 0 && !mbar_wait_bounded(&full[stage], parity)) late = 2 * stage + parity;  // reported, and not tried again
       const uint8_t* at = smem + static_cast<size_t>(stage) * st.bytes;
       float2 h[NG][2], g[NG][2], s = make_float2(0.f, 0.f), q = s;
       get_row<NG, WHOLE>(h, at, static_cast<const TX*>(p.x) + r * p.ld_x, r == 0, r == p.rows - 1, D, n, t);
@@ -774,7 +784,7 @@ __global__ void __launch_bounds__(kMostWarps * 32) bwd_kernel(const BwdArgs p, c
       } else {
         __syncwarp();
       }
-      if (warp == 0) fetch_next(stage);
+      if (warp == 0) fetch_next(stage, late < 0);
       if (++stage == st.n) {
         stage = 0;
         parity ^= 1;
@@ -789,7 +799,10 @@ __global__ void __launch_bounds__(kMostWarps * 32) bwd_kernel(const BwdArgs p, c
       put_row<NG, WHOLE>(dx, g, D, n, t);
     }
   }
-  if (!in_time && lane == 0) flag_status(status, RL_DEV_TIMEOUT);
+  if (late >= 0) {
+    flag_status(status, RL_DEV_TIMEOUT);
+    if (t == 0) await_copies(full, st.n, late / 2, late & 1);
+  }
   if (p.part_w) put_row<NG, WHOLE>(p.part_w + b0 * p.D, dw, D, n, t);
   if (p.part_b) put_row<NG, WHOLE>(p.part_b + b0 * p.D, db, D, n, t);
 }
