@@ -332,7 +332,6 @@ __global__ void __launch_bounds__(kBlockThreads) cluster_sort_kernel(const Clust
   const int rank = static_cast<int>(cluster_ctarank());
   const int first = rank * p.cap, mine = max(0, min(p.cap, p.T - first));  // positions first .. first + mine
   const int rounds = (p.cap / 32 + kBlockWarps - 1) / kBlockWarps, w0 = warp * rounds * 32;
-  next_may_start();  // the sums' CTAs, on the SMs that this kernel leaves free
   if (rank == 0 && threadIdx.x == 0) *p.crossing = 0;
   bool bad = false;
   for (int i = threadIdx.x; i < mine; i += kBlockThreads) {
@@ -423,6 +422,7 @@ __global__ void __launch_bounds__(kBlockThreads) cluster_sort_kernel(const Clust
     }
     cluster_sync_all();
   }
+  next_may_start();  // not before: until here the SMs that this kernel leaves free are other streams'
   const uint2* sorted = buf[p.passes & 1];
   for (int i = threadIdx.x; i < mine; i += kBlockThreads) {
     p.keys_out[first + i] = static_cast<int32_t>(sorted[i].x);
