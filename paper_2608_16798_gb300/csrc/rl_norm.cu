@@ -264,15 +264,14 @@ __device__ __forceinline__ void get_parameters(float2 (&v)[NG][2], const Vec& w,
     }
 }
 
-// A row on W warps (blockDim = 32 W, rows per CTA), 4 NG elements a thread, held in registers between the two sums and
-// the result. For few rows: nothing is fetched ahead, and every thread has little to do.
+// A row on the W >= 2 warps of a CTA, 4 NG elements a thread, held in registers between the two sums and the result. For few
+// rows: nothing is fetched ahead, and every thread has little to do.
 template <typename TX, typename TY, int NG, bool WHOLE>
 __global__ void __launch_bounds__(kMostWarps * 32) fwd_kernel(const FwdArgs p) {
   __shared__ __align__(16) float red[2][kMostWarps];
   const int W = blockDim.x / 32, n = blockDim.x, t = threadIdx.x, w = t / 32;
-  const int64_t r = static_cast<int64_t>(blockIdx.x) * blockDim.y + threadIdx.y;
-  if (W == 1 && r >= p.rows) return;  // several rows a CTA: no barriers
-  if (W > 1 && t < 2 * kMostWarps && t % kMostWarps >= W) red[t / kMostWarps][t % kMostWarps] = 0.f;
+  const int64_t r = blockIdx.x;
+  if (t < 2 * kMostWarps && t % kMostWarps >= W) red[t / kMostWarps][t % kMostWarps] = 0.f;
   const TX* x = static_cast<const TX*>(p.x) + r * p.ld_x;
   TY* y = static_cast<TY*>(p.y) + r * p.ld_y;
   const int D = static_cast<int>(p.D);
@@ -297,7 +296,7 @@ __global__ void __launch_bounds__(kMostWarps * 32) fwd_kernel(const FwdArgs p) {
   float2 g[NG][2], b[NG][2];
   get_parameters<NG, WHOLE>(g, p.w, 0.f, D, n, t);
   get_parameters<NG, WHOLE>(b, p.b, 0.f, D, n, t);
-  if (W > 1) __syncthreads();  // red's zeros
+  __syncthreads();  // red's zeros
   float mean, rstd;
   statistics<NG, WHOLE>(v, D, 1.f / static_cast<float>(D), p.eps, W, w, n, t, red[0], red[1], mean, rstd);
 #pragma unroll
@@ -904,8 +903,7 @@ inline Stages stages(int64_t x_bytes, int64_t d_bytes, bool whole, int ctas) {
 
 template <typename TX, typename TY, int NG, bool WHOLE>
 void launch_fwd(const FwdArgs& a, int W, cudaStream_t s) {
-  const int per = W == 1 ? 4 : 1;  // rows a CTA
-  fwd_kernel<TX, TY, NG, WHOLE><<<static_cast<unsigned>((a.rows + per - 1) / per), dim3(32 * W, per), 0, s>>>(a);
+  fwd_kernel<TX, TY, NG, WHOLE><<<static_cast<unsigned>(a.rows), 32 * W, 0, s>>>(a);
 }
 
 template <typename TX, typename TY, int NG, bool WHOLE>

@@ -39,7 +39,7 @@ namespace sample {
 
 using namespace seg;
 
-constexpr int kMostCluster = 16;
+constexpr int kMostCluster = 8;
 constexpr int kBinBits = 10, kBins = 1 << kBinBits;
 constexpr int kBf16Shift = 16;  // patterns of a bf16 step
 constexpr int kRestShift = 22;  // the bins cover all patterns
@@ -1256,7 +1256,7 @@ rl_status run(Args& a, cudaStream_t s) {
   if ((tiles <= 8 && a.rows > kSMs) || (tiles <= 64 && a.rows > 6 * kSMs)) return launch<T, 4, false>(a, 1, tiles, s);
   // else as many CTAs a row as fill the SMs twice over while each of their warps has a tile
   int C = 1;
-  while (C < 8 && ((a.rows * C * 2 <= 2 * kSMs && tiles >= 2 * C * 8) || tiles > kMostTiles * C)) C *= 2;
+  while (C < kMostCluster && ((a.rows * C * 2 <= 2 * kSMs && tiles >= 2 * C * 8) || tiles > kMostTiles * C)) C *= 2;
   if (tiles > kMostTiles * C) return set_error(RL_ERR_UNSUPPORTED, "rl_sample_tokens: V is too large");
   if (C > 1) return launch<T, 16, true>(a, C, tiles, s);
   return a.rows <= 2 * kSMs ? launch<T, 16, false>(a, 1, tiles, s) : launch<T, 8, false>(a, 1, tiles, s);
