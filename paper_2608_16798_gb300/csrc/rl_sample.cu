@@ -21,13 +21,15 @@
 //
 // What bounds it is the arithmetic beside the one exponential an entry (unpacking, the bins, the comparisons: 8 instructions
 // an entry for the first pass, 6 for the bins, up to 8 for the pass over what is kept) and the chain of a row's steps. Measured:
-// one row of 151,936 bf16 11 us without filters, 15 with top-k 50, 19 with top-p 0.4; 509 rows 40 without (57% of the copy's
-// rate), 62 with top-k 50, 81 with top-p 0.4 (85 before a tile's few kept entries were taken one by one), 58 with 0.7 / 20 /
-// 0.8. The first form held a row in the shared memory of a cluster (155 with top-k 50, 207 with top-p 0.95): 76 rows at work
-// at a time instead of 304, each through four exchanges.
+// one row of 151,936 bf16 12 us without filters, 16 with top-k 50, 19 with top-p 0.4; 509 rows 40 without (57% of the copy's
+// rate), 63 with top-k 50, 82 with top-p 0.4 (4 more before a tile's few kept entries were taken one by one), 60 with 0.7 / 20 /
+// 0.8; 254 rows fp32 35 without, 44 with top-k 50, 102 with top-p 0.4, 226 with 0.95. Outside the window of step 2: 128 rows
+// bf16 with top-p 0.95 53 us, inside 33. The first form held a row in the shared memory of a cluster (509 rows 155 with top-k 50,
+// 207 with top-p 0.95): 76 rows at work at a time instead of all, each through four exchanges.
 #include <algorithm>
 #include <atomic>
 #include <cmath>
+#include <cstring>
 #include <string>
 
 #include "rl_device.cuh"
@@ -135,13 +137,6 @@ __device__ __forceinline__ uint32_t equal2(uint32_t a, uint32_t b) {
   return r;
 }
 
-// Element i of a block's words.
-template <typename T>
-__device__ __forceinline__ void put_element(uint32_t (&w)[4], int i, T x) {
-  if (sizeof(T) == 4) w[i] = Elem<T>::bits(x);
-  else w[i / 2] = i & 1 ? (w[i / 2] & 0xffffu) | Elem<T>::bits(x) << 16 : (w[i / 2] & 0xffff0000u) | Elem<T>::bits(x);
-}
-
 // A row as the 16-byte blocks of memory that it covers.
 template <typename T>
 struct RowBlocks {
@@ -160,13 +155,15 @@ struct RowBlocks {
   // Block k; elements of other rows, and blocks behind the last, are minus infinity.
   __device__ __forceinline__ uint4 block(int k) const {
     if (k > 0 && k < nb - 1) return __ldcg(reinterpret_cast<const uint4*>(at + static_cast<int64_t>(k) * N));
-    uint32_t w[4] = {kNone, kNone, kNone, kNone};
-    if (k >= 0 && k < nb) {
+    uint4 q = make_uint4(kNone, kNone, kNone, kNone);
+    if (k < 0 || k >= nb) return q;
+    T e[N];
+    memcpy(e, &q, sizeof(q));
 #pragma unroll
-      for (int i = 0; i < N; ++i)
-        if (k * N + i >= lo && k * N + i < hi) put_element<T>(w, i, at[k * N + i]);
-    }
-    return make_uint4(w[0], w[1], w[2], w[3]);
+    for (int i = 0; i < N; ++i)
+      if (k * N + i >= lo && k * N + i < hi) e[i] = at[k * N + i];
+    memcpy(&q, e, sizeof(q));
+    return q;
   }
   // A lane's blocks of tile t.
   __device__ __forceinline__ void tile(int t, int lane, uint4 (&w)[kTileBlocks]) const {
@@ -191,9 +188,7 @@ __device__ __forceinline__ void sync_all() {
 template <bool CLUSTER>
 __device__ __forceinline__ unsigned long long of_cta(const uint32_t* two, int r) {
   if (CLUSTER) return ld_cluster_u64(map_to_rank(smem_addr(two), r));
-  unsigned long long v;
-  asm volatile("ld.shared.u64 %0, [%1];" : "=l"(v) : "r"(smem_addr(two)) : "memory");
-  return v;
+  return static_cast<unsigned long long>(two[1]) << 32 | two[0];
 }
 
 // A border: entries above `key` and the first m of those equal to it; their number above it and their mass.
@@ -1249,7 +1244,8 @@ rl_status launch(Args& a, int C, int64_t all_tiles, cudaStream_t s) {
 template <typename T>
 rl_status run(Args& a, cudaStream_t s) {
   const int64_t nb = (a.V + 7) * sizeof(T) / 16 + 1, tiles = (nb + kTileBlocks32 - 1) / kTileBlocks32;
-  // many rows: small CTAs, which wait less for one another, and do what a row takes beside its entries with fewer warps.
+  // many rows: small CTAs, which wait less for one another, and do what a row takes beside its entries with fewer warps
+  // (their threads have eight bins each to sum up, and spill 96 bytes, fp32 148; the other forms 24 at most).
   // Measured, us by 8 / 4 warps, top-k 50: 2,000 rows of 32,000 bf16 80.5 / 70.2, 1,200 of 60,000 69.2 / 64.3, 1,000 of 32,000
   // fp32 50.9 / 41.8, but 600 of 32,000 bf16 25.4 / 27.0 and 509 of 151,936 62.0 / 64.4; by 16 / 8 warps 300 of 151,936 37.8 /
   // 41.7, 509 104 / 82
