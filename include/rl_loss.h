@@ -731,8 +731,10 @@ typedef struct rl_sample_params {
  * gets token -1, NaN log-probabilities and n_kept 0 and sets RL_DEV_BAD_VALUE. Masses are sums of fp32 exponentials:
  * where top_p ends, and which token u selects, is that of exact sums but for borders within (48 + min(V / 4096, 256)) 2^-24
  * + V 2^-39 of the mass (5.4e-6 at 151,936 entries, 4.9e-5 at 2^24); an entry's own exponential is relative 2^-22 and
- * what the rounding of z / T makes of it. A row's results do not depend on what the other rows hold; the number of rows
- * decides how many CTAs share one, and with it the last bits of its sums.
+ * what the rounding of z / T makes of it. out_logp is off by what the normaliser's sum is rounded, 2^-22 where the token
+ * has nearly all of the mass; out_filtered_logp, from the sum of the other kept tokens, is relative there. A row's results
+ * do not depend on what the other rows hold; the number of rows decides how many CTAs share one, and with it the last bits
+ * of its sums.
  */
 rl_status rl_sample_tokens(const void* logits, rl_dtype dtype, int64_t rows, int64_t V, int64_t ld, const float* sample_u,
                            const rl_sample_params* params, const float* row_temperature, const int32_t* row_top_k,
@@ -754,7 +756,8 @@ rl_status rl_sample_tokens(const void* logits, rl_dtype dtype, int64_t rows, int
  *
  * The row is summed twice, the squares of x - mean after its mean is known; sums, mean and rstd are fp32.
  * Elements behind D of a row are neither read into the result nor written. A NaN or an infinity in a row makes
- * that row NaN; rows whose squares leave fp32's range (entries of about 1e19) come out as zeros times w plus b.
+ * that row NaN, and so does a sum that leaves fp32's range; rows whose squares alone leave it (entries of about 1e19)
+ * come out as zeros times w plus b.
  * A row's results do not depend on what the other rows hold; the number of rows, D and the alignment decide the order
  * of its sums. (A bounded wait that ran out, which nothing but a fault of the device can cause, makes rows NaN here:
  * there is no status word.)

@@ -292,3 +292,18 @@ def test_repeats_streams_and_graphs(R):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, c) for a, c in zip(first, (y, dx, dw)))
+
+
+@pytest.mark.parametrize("rows,D", [(6, 100), (6, 1000), (900, 4096), (2000, 4097), (5, 9001)])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_rows_beyond_the_range(R, rows, D, dtype):
+    """Squares beyond fp32's range: rstd is 0 and the row comes out as the bias; a sum beyond it: NaN. The rows beside stay."""
+    x, _, w, b = make(rows, D, dtype, F32, seed=31)
+    clean = [t.clone() for t in R.rl_layer_norm_fwd(x, weight=w, bias=b, y_dtype=F32)]
+    x[1] = torch.where(torch.arange(D, device="cuda") % 2 == 0, 1e25, -2e25).to(dtype)
+    x[3] = 3e38
+    y, mean, rstd = R.rl_layer_norm_fwd(x, weight=w, bias=b, y_dtype=F32)
+    assert torch.equal(y[1], b) and float(rstd[1]) == 0.0 and torch.isfinite(mean[1])
+    assert torch.isnan(y[3]).all()
+    keep = [i for i in range(rows) if i not in (1, 3)]
+    assert all(torch.equal(a[keep], c[keep]) for a, c in zip((y, mean, rstd), clean))
