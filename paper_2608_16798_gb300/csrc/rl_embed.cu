@@ -13,6 +13,7 @@
 // Memory bounds both. Measured: 32,768 tokens of 4,096 columns, ids with frequencies that fall as 1 / rank over 151,936:
 // forward 60 us (91% of the copy's rate over the rows that are named and written), backward 150 (the sort 17, the sums 118 at 80%
 // of the copy's rate, the long runs 10). The digits' passes, chains of a few microseconds each, are what the sort costs.
+// Rows that do not lie in 16-byte blocks, an element at a time: forward 72,544 x 1,792 bf16 in rows of 1,795 180 us.
 #include <algorithm>
 #include <atomic>
 #include <cmath>
@@ -640,7 +641,7 @@ struct FewArgs {
 };
 
 // A CTA for every token and kFewX * N columns: the first token of its id adds up those of all of them, in up to kFewY parts.
-// No sort: every CTA looks at all ids. One launch.
+// No sort: every CTA looks at all ids. One launch. Measured, bf16: 512 x 1,024 of 32,000 7 us; 1,024 tokens of one id x 1,024 78.
 template <typename T, int N, bool WHOLE>
 __global__ void __launch_bounds__(kFewThreads) few_kernel(const FewArgs p) {
   constexpr int kRounds = kFewTokens / kFewThreads, kWarps = kFewThreads / 32;

@@ -10,9 +10,10 @@
 //   - else persistent CTAs that share a row at a time, whose rows bulk copies bring ahead (fwd_ring_kernel, bwd_kernel).
 // Backward a thread has the same columns of all its rows, and the weight's and bias' sums of them stay in its registers; a second
 // launch adds up the CTAs' parts. Wider rows: a CTA per row that reads it once for each sum, and threads that go down the columns.
-// Measured, of the copy's 6.78 TB/s: 32,768 rows of 4,096 forward 77% (bf16) and 84% (fp32 to bf16), backward 84% (bf16), 85%
-// (fp32, bf16 gradient), 81% with 60% of the rows trained on; 131,072 of 512 70% and 71%; odd widths at 130,000 x 1,001 bf16
-// 46% and 42% (an element a load and a store), fp32 83% and 88%.
+// Measured, of the copy's 6.78 TB/s: 32,768 rows of 4,096 forward 77% (bf16) and 84% (fp32 to bf16), backward 83% (bf16), 85%
+// (fp32, bf16 gradient), 79% with 60% of the rows trained on; 131,072 of 512 71% and 70%; odd widths at 130,000 x 1,001 bf16
+// 46% and 42% (an element a load and a store), fp32 83% and 88%, 17,950 x 6,626 bf16 35% and 20% (spills: bwd_groups); more
+// than 8,192 columns, 10,000 x 12,288 bf16, 30% and 17%.
 #include <algorithm>
 #include <atomic>
 #include <cmath>
@@ -215,7 +216,7 @@ __device__ __forceinline__ void statistics(float2 (&v)[NG][2], int D, float inv,
 #pragma unroll
     for (int e = 0; e < 2; ++e) s = __fadd2_rn(s, v[j][e]);
   const float sum = row_sum(s.x + s.y, W, w, red0), m0 = sum * inv;
-  mean = fmaf(fmaf(-m0, static_cast<float>(D), sum), inv, m0);  // the quotient, rounded once
+  mean = fmaf(fmaf(-m0, static_cast<float>(D), sum), inv, m0);  // sum / D, by one correction from the product's residual
   const float2 off = make_float2(-mean, -mean);
 #pragma unroll
   for (int j = 0; j < NG; ++j)
@@ -373,7 +374,7 @@ __global__ void __launch_bounds__(kShortWarps * 32) fwd_short_kernel(const FwdAr
 #pragma unroll
   for (int k = 0; k < R; ++k) {
     const float m = s[k] * inv;
-    s[k] = fmaf(fmaf(-m, static_cast<float>(D), s[k]), inv, m);  // the mean, rounded once
+    s[k] = fmaf(fmaf(-m, static_cast<float>(D), s[k]), inv, m);  // the mean, corrected likewise
     float2 a = make_float2(0.f, 0.f);
 #pragma unroll
     for (int j = 0; j < NG; ++j)
@@ -408,7 +409,8 @@ __global__ void __launch_bounds__(kShortWarps * 32) fwd_short_kernel(const FwdAr
 }
 
 // The same for the gradient: warps go down the rows R at a time, a fixed assignment, with the columns' sums in registers; the
-// CTA's warps' are added up in order at the end.
+// CTA's warps' are added up in order at the end. Measured, 500,000 rows of 128 bf16: 100 us. (bf16 x an element at a time, four
+// rows: 28 bytes spilled.)
 template <typename TX, typename TD, int NG, int R, bool WHOLE>
 __global__ void __launch_bounds__(kShortWarps * 32, 2) bwd_short_kernel(const BwdArgs p) {
   __shared__ __align__(16) float sums[kShortWarps][128 * NG];
@@ -855,7 +857,9 @@ constexpr int kSMs = 152;
 constexpr int64_t kMaxD = 1 << 20;
 
 // Blocks of four columns a thread holds in the backward kernel, and the warps of a row; 0: a row has too many columns for
-// it. An element at a time two blocks: four spill (128 registers), and with the stages in the way of L1 that cost 3 times the time.
+// it. An element at a time two blocks: four spill (164 bytes at 128 registers), and with the stages in the way of L1 that cost 3 times
+// the time. Rows of 4,097 to 8,192 columns would want 32 warps then, so they have four blocks all the same: 17,950 x 6,626 bf16
+// 536 us (its bytes: 105), and 200 forward, where nothing spills.
 inline int bwd_groups(int64_t D, bool whole) { return !whole && D <= 256 * kMostWarps ? 2 : 4; }
 inline int bwd_warps(int64_t D, bool whole) {
   const int64_t per = 128 * bwd_groups(D, whole), W = (D + per - 1) / per;
