@@ -1091,9 +1091,10 @@ __global__ void __launch_bounds__(WARPS * 32, 1024 / (WARPS * 32)) sample_kernel
   const float total = warp_sum(mine);
   const Picked cta = pick_at(C, set.u * total, lane, [&](int) { return mine; });  // a lane has one
   if (cta.at != rank) return;
-  // Not under the condition that the number is wanted. Built so (nvcc 13.0.88), every number came out as 0, known ones too,
-  // though the condition is the same in all lanes: with a ballot of it in the code, or with the sum taken by shuffles,
-  // the results are right. No kernel smaller than this one shows it. (Intrinsic and redux.sync alike, so what follows the PTX.)
+  // Not under the condition that the number is wanted. Built so (nvcc 13.0.88), a known number came out as the sum, 0, and under
+  // a vote on the condition an unknown one as 0 too, though the condition is the same in all lanes: with a ballot of it
+  // in the code, or with the sum taken by shuffles, the results are right. No kernel smaller than this one shows it.
+  // (Intrinsic and redux.sync alike, so what follows the PTX.)
   const uint32_t counted = __reduce_add_sync(0xffffffffu, part.above);
   const uint32_t ties_before = __shfl_sync(0xffffffffu, before, rank);
 
